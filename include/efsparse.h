@@ -305,6 +305,76 @@ efs_status sparse_apply(const int32_t *const *idx, const float *const *val,
                         int64_t d, int mode, float *x, float *m, float beta, float gamma,
                         void *workspace, size_t workspace_bytes, void *stream);
 
+/* Element types of the operators that take more than one. */
+enum { EFS_FP32 = 0, EFS_BF16 = 1 };
+
+/* Newton-Schulz orthogonalisation of a batch of matrices: with the singular
+ * value decomposition G = U S V^T of one matrix, the result approximates
+ * U V^T (the direction that the orthogonalised model update takes,
+ * muon_apply).  With X = G / (||G||_F + eps), transposed where it has more
+ * rows than columns, `steps` times
+ *     A = X X^T ;  B = b A + c A A ;  X = a X + B X
+ * and the last X, transposed back.  Everything between reading g and writing
+ * out is held to binary32's precision or better, whatever the type.
+ *
+ *   g          batch matrices of rows x cols; element (i, r, c) is
+ *              g[i * stride_g + r * ld_g + c] (in elements; ld_g >= cols).  Read
+ *              only; matrices may overlap (stride_g = 0 repeats one).
+ *   out        the same with ld_out, stride_out; matrices must not overlap
+ *              each other.  May be g itself: g is not read any more when out is
+ *              written.
+ *   dtype      EFS_FP32 or EFS_BF16, of g and out.
+ *   batch, rows, cols   >= 0; rows * cols <= INT32_MAX, batch <=
+ *              EFS_MUON_MAX_MATRICES.  0 of any: a call that does nothing.
+ *   steps      1..EFS_MUON_MAX_STEPS (5 is usual).
+ *   coeffs     HOST float[3] a, b, c (finite), or NULL for 3.4445, -4.7750,
+ *              2.0315.  Iterates are held in a form that reaches to singular
+ *              values s of 1.99, with |b s^2 + c s^4| below 15, which
+ *              coefficients that keep the singular values near 1 stay below;
+ *              beyond it they become infinite.
+ *   eps        added to the norm (finite, >= 0): a matrix of zeros gives zeros
+ *              (with eps = 0 NaN, as 0 / 0).
+ *   workspace  >= muon_workspace_bytes for these matrices, 16-byte aligned;
+ *              contents need no initialisation and are not kept.  Not
+ *              shareable between concurrent calls.
+ * A matrix that holds NaN or infinities gives NaN; the others of the batch
+ * are not affected. */
+#define EFS_MUON_MAX_MATRICES 65536
+#define EFS_MUON_MAX_STEPS 64
+/* Bytes for nmat matrices of rows[i] x cols[i] (HOST arrays); 0 if the
+ * arguments are out of range. */
+size_t muon_workspace_bytes(int32_t nmat, const int32_t *rows, const int32_t *cols);
+efs_status muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, void *out,
+                              int64_t ld_out, int64_t stride_out, int dtype, int32_t batch,
+                              int32_t rows, int32_t cols, int32_t steps, const float *coeffs,
+                              float eps, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Model update of a flat vector's weight matrices from the averaged update,
+ * orthogonalised matrix by matrix (the update of Algorithm 2, App. C.6.2, with
+ * the direction orthogonalised; it takes what sparse_accumulate writes):
+ *     m = beta * m + avg ;  u = avg + beta * m (nesterov) or m ;
+ *     O = muon_orthogonalize(u) with the default coefficients ;
+ *     x = (1 - gamma * decay) * x - gamma * sqrt(max(1, rows / cols)) * O
+ * each a separately rounded fp32 operation in the order written.
+ *
+ *   avg        fp32 vector of d elements, read only.
+ *   x, m       fp32 vectors of d elements, in place.  avg, x and m must not
+ *              overlap.  Any 4-byte alignment.
+ *   d          0..INT32_MAX.
+ *   nmat, offsets, rows, cols
+ *              HOST arrays: matrix i is the row-major rows[i] x cols[i] at
+ *              offsets[i] of each vector.  In ascending order and not
+ *              overlapping; nmat <= EFS_MUON_MAX_MATRICES; empty matrices are
+ *              skipped.  Elements outside every matrix keep x and m.
+ *   beta, gamma, decay   finite.
+ *   nesterov   0 or 1.
+ *   steps, eps, workspace   as for muon_orthogonalize (a matrix whose u is zero
+ *              only decays). */
+efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t nmat,
+                      const int64_t *offsets, const int32_t *rows, const int32_t *cols, float beta,
+                      float gamma, float decay, int nesterov, int32_t steps, float eps,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
 /* Streaming copy dst[0..n) = src[0..n) with the same 16-byte access pattern
  * and grid as the hard-threshold kernel: the reference transfer for
  * measurements, not part of the method.  src and dst 16-byte aligned,

@@ -90,6 +90,15 @@ def declare(lib):
                                  ctypes.POINTER(i64), i32, i64, ctypes.c_int, vp, vp, f32, f32, vp,
                                  ctypes.c_size_t, vp]
     lib.sparse_apply.restype = ctypes.c_int
+    lib.muon_workspace_bytes.argtypes = [i32, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+    lib.muon_workspace_bytes.restype = ctypes.c_size_t
+    lib.muon_orthogonalize.argtypes = [vp, i64, i64, vp, i64, i64, ctypes.c_int, i32, i32, i32, i32,
+                                       ctypes.POINTER(f32), f32, vp, ctypes.c_size_t, vp]
+    lib.muon_orthogonalize.restype = ctypes.c_int
+    lib.muon_apply.argtypes = [vp, vp, vp, i64, i32, ctypes.POINTER(i64), ctypes.POINTER(i32),
+                               ctypes.POINTER(i32), f32, f32, f32, ctypes.c_int, i32, f32, vp,
+                               ctypes.c_size_t, vp]
+    lib.muon_apply.restype = ctypes.c_int
     lib.efs_copy_probe.argtypes = [vp, vp, i64, vp]
     lib.efs_copy_probe.restype = ctypes.c_int
     lib.efs_stream_probe.argtypes = [vp, vp, i64, ctypes.c_int, vp]
@@ -437,6 +446,111 @@ def sparse_accumulate_static(payloads: Sequence[Tuple], d: int, out, stream=None
     idx_arr, val_arr, cnt_arr, caps = _payload_arrays(payloads)
     _check(lib, lib.sparse_accumulate_static(idx_arr, val_arr, cnt_arr, caps, len(payloads), int(d),
                                              _ptr(out), _stream_handle(stream)))
+
+
+FP32, BF16 = 0, 1
+
+
+def _dtype_code(t, name) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return FP32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+
+
+def _require_rows(t, name):
+    """A device tensor whose rows are contiguous (they may lie further apart)."""
+    if t.device.type != "cuda":
+        raise TypeError("%s must be a device tensor" % name)
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise TypeError("%s must have contiguous rows" % name)
+
+
+def _row_stride(t) -> int:
+    """Elements between the rows of a matrix (a single row has none)."""
+    return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
+
+
+def _shape_arrays(shapes: Sequence[Tuple[int, int]]):
+    n = max(len(shapes), 1)
+    rows, cols = (ctypes.c_int32 * n)(), (ctypes.c_int32 * n)()
+    for i, (r, c) in enumerate(shapes):
+        rows[i], cols[i] = int(r), int(c)
+    return rows, cols
+
+
+def muon_workspace_bytes(shapes: Sequence[Tuple[int, int]]) -> int:
+    rows, cols = _shape_arrays(shapes)
+    return int(load_library().muon_workspace_bytes(len(shapes), rows, cols))
+
+
+def new_muon_workspace(shapes: Sequence[Tuple[int, int]], device="cuda"):
+    """A workspace for muon_orthogonalize or muon_apply over matrices of these
+    (rows, cols)."""
+    import torch
+    return torch.empty(max(muon_workspace_bytes(shapes), 16), dtype=torch.uint8, device=device)
+
+
+def muon_orthogonalize(g, out, workspace, steps: int = 5, coeffs=None, eps: float = 1e-7,
+                       stream=None) -> None:
+    """Newton-Schulz orthogonalisation of a matrix [rows, cols] or a batch of
+    them [batch, rows, cols], fp32 or bf16; see muon_orthogonalize in
+    include/efsparse.h.  Rows may lie further apart than they are long."""
+    import torch
+    lib = load_library()
+    if g.shape != out.shape or g.dim() not in (2, 3):
+        raise ValueError("g and out must be [rows, cols] or [batch, rows, cols], the same for both")
+    if g.dtype != out.dtype:
+        raise TypeError("g and out must have one dtype")
+    dtype = _dtype_code(g, "g")
+    _require_rows(g, "g")
+    _require_rows(out, "out")
+    _require(workspace, torch.uint8, "workspace")
+    batch = g.shape[0] if g.dim() == 3 else 1
+    rows, cols = g.shape[-2:]
+    co = None if coeffs is None else (ctypes.c_float * 3)(*(float(v) for v in coeffs))
+    rc = lib.muon_orthogonalize(_ptr(g), _row_stride(g), g.stride(0) if batch > 1 else 0, _ptr(out),
+                                _row_stride(out), out.stride(0) if batch > 1 else 0, dtype, batch, rows, cols,
+                                int(steps), co, float(eps), _ptr(workspace), workspace.numel(),
+                                _stream_handle(stream))
+    _check(lib, rc)
+
+
+def prepare_muon_apply(avg, x, m, layers: Sequence[Tuple[int, int, int]], workspace, beta: float,
+                       gamma: float, weight_decay: float = 0.0, nesterov: bool = True, steps: int = 5,
+                       eps: float = 1e-7, stream=None):
+    """muon_apply with its arguments marshalled once (see prepare_sparse_apply)."""
+    import torch
+    lib = load_library()
+    _require(avg, torch.float32, "avg")
+    _require(x, torch.float32, "x")
+    _require(m, torch.float32, "m")
+    _require(workspace, torch.uint8, "workspace")
+    if not avg.numel() == x.numel() == m.numel():
+        raise ValueError("avg, x and m must have one length")
+    offsets = (ctypes.c_int64 * max(len(layers), 1))(*(int(v[0]) for v in layers))
+    rows, cols = _shape_arrays([v[1:] for v in layers])
+    args = (_ptr(avg), _ptr(x), _ptr(m), x.numel(), len(layers), offsets, rows, cols, float(beta),
+            float(gamma), float(weight_decay), int(bool(nesterov)), int(steps), float(eps),
+            _ptr(workspace), workspace.numel(), _stream_handle(stream))
+    fn = lib.muon_apply
+
+    def call():
+        _check(lib, fn(*args))
+    call.tensors = (avg, x, m, workspace)   # alive as long as the pointers in args
+    return call
+
+
+def muon_apply(avg, x, m, layers: Sequence[Tuple[int, int, int]], workspace, beta: float, gamma: float,
+               weight_decay: float = 0.0, nesterov: bool = True, steps: int = 5, eps: float = 1e-7,
+               stream=None) -> None:
+    """Orthogonalised update of a flat vector's matrices from the averaged
+    update; see muon_apply in include/efsparse.h.  layers: (offset, rows, cols)
+    of each matrix, ascending; workspace from new_muon_workspace."""
+    prepare_muon_apply(avg, x, m, layers, workspace, beta, gamma, weight_decay, nesterov, steps, eps,
+                       stream)()
 
 
 def copy_probe(src, dst, stream=None) -> None:

@@ -17,6 +17,8 @@ static_assert(efs::kSparseTruncated == EFS_SPARSE_TRUNCATED, "status bit differs
 static_assert(efs::kSparseBadIndex == EFS_SPARSE_BAD_INDEX, "status bit differs from the header");
 static_assert(efs::kMaxSegments == EFS_SEG_MAX, "segment limit differs from the header");
 static_assert(efs::kStaticScratchBytes == EFS_STATIC_SCRATCH_BYTES, "scratch size differs from the header");
+static_assert(efs::kMuonMaxMatrices == EFS_MUON_MAX_MATRICES, "matrix limit differs from the header");
+static_assert(efs::kMuonMaxSteps == EFS_MUON_MAX_STEPS, "step limit differs from the header");
 static_assert(sizeof(efs::Telemetry) == EFS_TELEMETRY_BYTES, "telemetry layout differs from the header");
 
 namespace {
@@ -42,6 +44,12 @@ efs_status check_launch(hipError_t err, const char *what) {
 bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 constexpr int64_t kMaxLen = INT32_MAX;
+
+// Whether two vectors of d floats share any byte.
+bool overlap(const float *a, const float *b, int64_t d) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + uintptr_t(d) * 4 && y < x + uintptr_t(d) * 4;
+}
 
 int g_cu_count[64];  // per device; 0 = not queried yet
 
@@ -323,6 +331,106 @@ efs_status sparse_apply(const int32_t *const *idx, const float *const *val,
                                           gamma, workspace, workspace_bytes,
                                           static_cast<hipStream_t>(stream)),
                         "sparse_apply");
+}
+
+// What the two orthogonalising calls check alike.  next: from one matrix's
+// entry of rows and cols to the next's (0: all alike).
+static efs_status check_muon(const char *name, int32_t nmat, const int32_t *rows, const int32_t *cols,
+                             int32_t next, int32_t steps, float eps, const void *workspace, size_t workspace_bytes) {
+    if (steps < 1 || steps > efs::kMuonMaxSteps)
+        return fail(EFS_EINVAL, "%s: steps=%d outside [1, %d]", name, steps, efs::kMuonMaxSteps);
+    if (!std::isfinite(eps) || eps < 0.0f) return fail(EFS_EINVAL, "%s: eps must be finite and >= 0", name);
+    size_t need = 0;
+    if (!efs::muon_workspace_size(nmat, rows, cols, next, &need))
+        return fail(EFS_EINVAL, "%s: the matrices are too many for one call", name);
+    if (workspace == nullptr || !aligned(workspace, 16))
+        return fail(EFS_EINVAL, "%s: workspace must be non-NULL and 16-byte aligned", name);
+    if (workspace_bytes < need)
+        return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    return EFS_OK;
+}
+
+size_t muon_workspace_bytes(int32_t nmat, const int32_t *rows, const int32_t *cols) {
+    if (nmat < 0 || nmat > efs::kMuonMaxMatrices || (nmat > 0 && (rows == nullptr || cols == nullptr))) return 0;
+    for (int32_t i = 0; i < nmat; ++i)
+        if (rows[i] < 0 || cols[i] < 0 || int64_t(rows[i]) * cols[i] > kMaxLen) return 0;
+    size_t bytes = 0;
+    return efs::muon_workspace_size(nmat, rows, cols, 1, &bytes) ? bytes : 0;
+}
+
+efs_status muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, void *out, int64_t ld_out,
+                              int64_t stride_out, int dtype, int32_t batch, int32_t rows, int32_t cols,
+                              int32_t steps, const float *coeffs, float eps, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    const char *name = "muon_orthogonalize";
+    static const float kCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+    if (dtype != EFS_FP32 && dtype != EFS_BF16)
+        return fail(EFS_EINVAL, "%s: dtype %d is neither EFS_FP32 nor EFS_BF16", name, dtype);
+    if (batch < 0 || batch > efs::kMuonMaxMatrices)
+        return fail(EFS_EINVAL, "%s: batch=%d outside [0, %d]", name, batch, efs::kMuonMaxMatrices);
+    if (rows < 0 || cols < 0 || int64_t(rows) * cols > kMaxLen)
+        return fail(EFS_EINVAL, "%s: %d x %d is negative or has more than 2^31-1 elements", name, rows, cols);
+    if (coeffs == nullptr) coeffs = kCoeffs;
+    for (int k = 0; k < 3; ++k)
+        if (!std::isfinite(coeffs[k])) return fail(EFS_EINVAL, "%s: coeffs must be finite", name);
+    if (batch == 0 || rows == 0 || cols == 0) return EFS_OK;
+    const uintptr_t size = dtype == EFS_BF16 ? 2 : 4;
+    if (g == nullptr || out == nullptr || !aligned(g, size) || !aligned(out, size))
+        return fail(EFS_EINVAL, "%s: g and out must be non-NULL and aligned to their type", name);
+    if (ld_g < cols || ld_out < cols || ld_g > kMaxLen || ld_out > kMaxLen)
+        return fail(EFS_EINVAL, "%s: ld_g and ld_out must be in [cols, 2^31-1]", name);
+    if (stride_g < 0 || stride_out < 0 || stride_g > INT64_MAX / 4 / (int64_t(batch) + 1) ||
+        stride_out > INT64_MAX / 4 / (int64_t(batch) + 1))
+        return fail(EFS_EINVAL, "%s: stride_g or stride_out is negative or too large", name);
+    // one matrix after the other, or their rows in turn
+    if (batch > 1 && stride_out < (int64_t(rows) - 1) * ld_out + cols &&
+        (stride_out < cols || ld_out < (int64_t(batch) - 1) * stride_out + cols))
+        return fail(EFS_EINVAL, "%s: the matrices of out overlap", name);
+    const efs_status s = check_muon(name, batch, &rows, &cols, 0, steps, eps, workspace, workspace_bytes);
+    if (s != EFS_OK) return s;
+    return check_launch(efs::launch_muon_orthogonalize(g, ld_g, stride_g, out, ld_out, stride_out,
+                                                       dtype == EFS_BF16, batch, rows, cols, steps, coeffs,
+                                                       eps, workspace, static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t nmat, const int64_t *offsets,
+                      const int32_t *rows, const int32_t *cols, float beta, float gamma, float decay,
+                      int nesterov, int32_t steps, float eps, void *workspace, size_t workspace_bytes,
+                      void *stream) {
+    const char *name = "muon_apply";
+    static const float kCoeffs[3] = {3.4445f, -4.7750f, 2.0315f};
+    if (d < 0 || d > kMaxLen) return fail(EFS_EINVAL, "%s: d=%lld outside [0, 2^31-1]", name, (long long)d);
+    if (nmat < 0 || nmat > efs::kMuonMaxMatrices)
+        return fail(EFS_EINVAL, "%s: nmat=%d outside [0, %d]", name, nmat, efs::kMuonMaxMatrices);
+    if (nmat > 0 && (offsets == nullptr || rows == nullptr || cols == nullptr))
+        return fail(EFS_EINVAL, "%s: offsets, rows and cols must be host arrays", name);
+    if (!std::isfinite(beta) || !std::isfinite(gamma) || !std::isfinite(decay))
+        return fail(EFS_EINVAL, "%s: beta, gamma and decay must be finite", name);
+    if (nesterov != 0 && nesterov != 1) return fail(EFS_EINVAL, "%s: nesterov must be 0 or 1", name);
+    int64_t end = 0;
+    bool any = false;
+    for (int32_t i = 0; i < nmat; ++i) {
+        if (rows[i] < 0 || cols[i] < 0 || int64_t(rows[i]) * cols[i] > kMaxLen)
+            return fail(EFS_EINVAL, "%s: matrix %d of %d x %d is negative or has more than 2^31-1 elements", name,
+                        i, rows[i], cols[i]);
+        const int64_t size = int64_t(rows[i]) * cols[i];
+        if (offsets[i] < end || offsets[i] > d - size)
+            return fail(EFS_EINVAL, "%s: matrix %d starts before the one before it ends, or ends past d", name, i);
+        end = offsets[i] + size;
+        any = any || size > 0;
+    }
+    if (!any) return EFS_OK;
+    if (avg == nullptr || x == nullptr || m == nullptr || !aligned(avg, 4) || !aligned(x, 4) || !aligned(m, 4))
+        return fail(EFS_EINVAL, "%s: avg, x and m must be non-NULL and 4-byte aligned", name);
+    if (overlap(avg, x, d) || overlap(avg, m, d) || overlap(x, m, d))
+        return fail(EFS_EINVAL, "%s: avg, x and m must not overlap", name);
+    const efs_status s = check_muon(name, nmat, rows, cols, 1, steps, eps, workspace, workspace_bytes);
+    if (s != EFS_OK) return s;
+    return check_launch(efs::launch_muon_apply(avg, nmat, offsets, rows, cols, x, m, beta, gamma, decay,
+                                               nesterov != 0, steps, kCoeffs, eps, workspace,
+                                               static_cast<hipStream_t>(stream)),
+                        name);
 }
 
 // The probes address at most INT32_MAX tiles (one workgroup each in the

@@ -47,6 +47,21 @@ hipError_t launch_apply(const int32_t *const *idx, const float *const *val,
 constexpr size_t kStaticScratchBytes = size_t(64) << 20;
 hipError_t static_scratch(void **ptr);
 
+// Orthogonalised update of weight matrices (muon.hip).  muon_workspace_size
+// returns false where the matrices together need more workgroups than a grid
+// has; `next` steps through rows and cols (0: all matrices alike).
+constexpr int32_t kMuonMaxMatrices = 1 << 16;
+constexpr int32_t kMuonMaxSteps = 64;
+bool muon_workspace_size(int32_t nmat, const int32_t *rows, const int32_t *cols, int32_t next, size_t *bytes);
+hipError_t launch_muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, void *o, int64_t ld_o,
+                                     int64_t stride_o, bool bf16, int32_t batch, int32_t rows, int32_t cols,
+                                     int steps, const float *coeffs, float eps, void *workspace,
+                                     hipStream_t stream);
+hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offsets, const int32_t *rows,
+                             const int32_t *cols, float *x, float *m, float beta, float gamma, float decay,
+                             bool nesterov, int steps, const float *coeffs, float eps, void *workspace,
+                             hipStream_t stream);
+
 hipError_t launch_copy(const float *src, float *dst, int64_t n, bool per_tile, hipStream_t stream);
 hipError_t launch_stream_probe(const float *x, float *y, int64_t n, int mode, bool per_tile,
                                hipStream_t stream);

@@ -1,0 +1,244 @@
+// A tile of C = A B^T on the matrix cores (gfx950): the product that the
+// orthogonalised update (muon.hip) and the cross entropy (xent.hip) share.
+//
+// Both operands are stored along the summed axis: row r of A holds A[r, 0..K).
+// A row is read in steps of 128 bytes, which hold
+//   kBf16   64 bf16 values;
+//   kSplit  32 fp32 values as 32 fp16 high parts and then their 32 low parts:
+//           v s = hi + lo with s a power of two, hi = fp16(v s),
+//           lo = fp16(v s - hi).  The product is hi hi + hi lo + lo hi, three
+//           fp16 products in fp32 accumulators: what is left out, lo lo and
+//           the rounding of lo, is 2^-22 of a product at most, as much as an
+//           fp32 product's own sums lose.  It runs at a third of the 16-bit
+//           rate (2500 TFLOP/s), five times that of the fp32 matrix
+//           instructions (157).
+// A workgroup of WM x WN waves computes WM TM 32 rows by WN TN 32 columns, a
+// wave TM x TN accumulators of the 32 x 32 x 16 instruction.  Steps go from
+// memory straight to LDS (16 bytes a lane, no registers), into one of two
+// buffers while the other one is multiplied.  In LDS a row's eight 16-byte
+// units are permuted by the row's low bits, so that the eight rows that a
+// quarter wave reads at once lie in different banks.  A step's reads from LDS
+// are spread between the products by scheduling groups.  Measured, 8192 x 8192
+// x 4096, 256 x 256 tile: kSplit 441 TFLOP/s (1322 of fp16 products), kBf16
+// 1124; without the groups 396 and 1056.  With 128 x 128 tiles 380 and 948,
+// but 1024 x 4096 x 1024 runs at 286 and 532 against 131 and 288, since it has
+// only 64 tiles of the larger kind for 256 compute units.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "device_common.hpp"
+
+namespace efs {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+enum class Prec { kBf16, kSplit };
+
+constexpr int kStepBytes = 128;   // of one row, a step of the summed axis
+// values of a row in one step
+template <Prec P>
+constexpr int kStepValues = P == Prec::kSplit ? 32 : 64;
+
+// Bytes of a row of `len` values, padded with zeros to whole steps.
+template <Prec P>
+__host__ __device__ constexpr int64_t row_bytes(int64_t len) {
+    return (len + kStepValues<P> - 1) / kStepValues<P> * kStepBytes;
+}
+
+// `rows` >= 1 rows of `stride` bytes (a multiple of 16, as `base` is).  Rows
+// past the last are read as the last: what they give is not used.
+struct Operand {
+    const char *base;
+    int64_t stride;
+    int32_t rows;
+};
+
+// The scaled value as its two halves.  An infinite or NaN value has no low
+// part, so that it stays what it is.
+__device__ __forceinline__ void split_value(float y, _Float16 &hi, _Float16 &lo) {
+    hi = _Float16(y);
+    const float h = float(hi);
+    lo = fabsf(h) < INFINITY ? _Float16(__fsub_rn(y, h)) : _Float16(0.0f);
+}
+
+// Bytes from a split row's start to the high part of value c; its low part
+// is 64 bytes further.
+__device__ __forceinline__ int64_t split_offset(int32_t c) {
+    return int64_t(c >> 5) * kStepBytes + (c & 31) * 2;
+}
+
+__device__ __forceinline__ void store_split(char *row, int32_t c, float y) {
+    _Float16 hi, lo;
+    split_value(y, hi, lo);
+    char *p = row + split_offset(c);
+    *reinterpret_cast<_Float16 *>(p) = hi;
+    *reinterpret_cast<_Float16 *>(p + 64) = lo;
+}
+
+__device__ __forceinline__ float load_split(const char *row, int32_t c) {
+    const char *p = row + split_offset(c);
+    return __fadd_rn(float(*reinterpret_cast<const _Float16 *>(p)),
+                     float(*reinterpret_cast<const _Float16 *>(p + 64)));
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+template <Prec P, int WM, int WN, int TM, int TN>
+struct MfmaTile {
+    static constexpr int kRows = WM * TM * 32;
+    static constexpr int kCols = WN * TN * 32;
+    static constexpr int kThreads = WM * WN * kWave;
+    static constexpr int kBufferBytes = (kRows + kCols) * kStepBytes;
+    static constexpr int kLdsBytes = 2 * kBufferBytes;
+    static constexpr int kLoadsA = kRows / 8 / (WM * WN);   // a wave's, 8 rows each
+    static constexpr int kLoadsB = kCols / 8 / (WM * WN);
+    static constexpr int kTilesM = TM, kTilesN = TN;
+
+    f32x16 acc[TM][TN];
+
+    // Row and column, within the workgroup's tile, of element e of acc[i][j]:
+    // a lane holds one column and four consecutive rows in each eight.
+    static __device__ __forceinline__ int row_of(int i, int e) {
+        const int wave = threadIdx.x / kWave, half = (threadIdx.x & (kWave - 1)) >> 5;
+        return (wave / WN * TM + i) * 32 + (e >> 2) * 8 + half * 4 + (e & 3);
+    }
+    static __device__ __forceinline__ int col_of(int j) {
+        const int wave = threadIdx.x / kWave;
+        return (wave % WN * TN + j) * 32 + (threadIdx.x & 31);
+    }
+
+    static __device__ __forceinline__ f32x16 mfma(f16x8 a, f16x8 b, f32x16 c) {
+        if constexpr (P == Prec::kBf16)
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                           __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+        else
+            return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+
+    // acc = A[row0.., step0..step0+steps) B[col0.., ...)^T, in the operands'
+    // scaled units.  `lds` has kLdsBytes, 16-byte aligned; it is free again
+    // after a barrier.  Called by every thread of the workgroup.
+    __device__ __forceinline__ void run(const Operand &a, const Operand &b, int32_t row0, int32_t col0,
+                                        int32_t step0, int32_t steps, char *lds) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const int wave = threadIdx.x / kWave;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+        // a load covers 8 rows of 128 bytes; lane l fills unit l % 8 of row
+        // l / 8 in LDS, which holds unit (l % 8) ^ (row % 8) of memory
+        const char *pa[kLoadsA], *pb[kLoadsB];
+        const int unit = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+        for (int i = 0; i < kLoadsA; ++i) {
+            const int r = (wave * kLoadsA + i) * 8 + (lane >> 3);
+            pa[i] = a.base + int64_t(min(row0 + r, a.rows - 1)) * a.stride + unit * 16;
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsB; ++i) {
+            const int r = (wave * kLoadsB + i) * 8 + (lane >> 3);
+            pb[i] = b.base + int64_t(min(col0 + r, b.rows - 1)) * b.stride + unit * 16;
+        }
+        auto load = [&](int buffer, int32_t step) {
+            char *to = lds + buffer * kBufferBytes;
+            const int64_t at = int64_t(step) * kStepBytes;
+#pragma unroll
+            for (int i = 0; i < kLoadsA; ++i)
+                __builtin_amdgcn_global_load_lds((global_void *)(pa[i] + at),
+                                                 (lds_void *)(to + (wave * kLoadsA + i) * 1024), 16, 0, 0);
+#pragma unroll
+            for (int i = 0; i < kLoadsB; ++i)
+                __builtin_amdgcn_global_load_lds(
+                    (global_void *)(pb[i] + at),
+                    (lds_void *)(to + kRows * kStepBytes + (wave * kLoadsB + i) * 1024), 16, 0, 0);
+        };
+
+        const int ra = wave / WN * TM * 32, rb = wave % WN * TN * 32;
+        if (steps > 0) load(0, step0);
+        for (int32_t s = 0; s < steps; ++s) {
+            // this step is in LDS once every wave's loads have come back, and
+            // every wave has left the other buffer
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (s + 1 < steps) load((s + 1) & 1, step0 + s + 1);
+
+            const char *la = lds + (s & 1) * kBufferBytes + ra * kStepBytes;
+            const char *lb = lds + (s & 1) * kBufferBytes + (kRows + rb) * kStepBytes;
+            auto read = [&](const char *from, int tile, int q) {
+                const int r = tile * 32 + (lane & 31);
+                return *reinterpret_cast<const f16x8 *>(from + r * kStepBytes +
+                                                        (((q * 2 + (lane >> 5)) ^ (r & 7)) * 16));
+            };
+            // the four quarters of a step, 16 values each; for kSplit the high
+            // and low parts of the first 16 values, then of the second
+            f16x8 fa[4][TM], fb[4][TN];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = P == Prec::kSplit ? (q >> 1) | ((q & 1) << 1) : q;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[q][j] = read(lb, j, at);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[q][i] = read(la, i, at);
+            }
+            constexpr int kProducts = P == Prec::kSplit ? 6 : 4;
+#pragma unroll
+            for (int p = 0; p < kProducts; ++p) {
+                const int qa = P == Prec::kSplit ? p / 3 * 2 + (p % 3 == 2) : p;
+                const int qb = P == Prec::kSplit ? p / 3 * 2 + (p % 3 == 1) : p;
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fa[qa][i], fb[qb][j], acc[i][j]);
+            }
+            // the first quarter's reads, then one read for every few products
+            constexpr int kReads = 4 * (TM + TN), kFirst = TM + TN + 1;
+            constexpr int kAll = kProducts * TM * TN;
+            constexpr int kEach = kAll * 3 / 4 / (kReads - kFirst);
+            __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
+#pragma unroll
+            for (int x = 0; x < kReads - kFirst; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x8, kEach > 0 ? kEach : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, kAll, 0);
+        }
+    }
+};
+
+// The two shapes in use: 256 x 256 by eight waves, one workgroup a compute
+// unit, and 128 x 128 by four, two a compute unit.
+template <Prec P>
+using LargeTile = MfmaTile<P, 2, 4, 4, 2>;
+template <Prec P>
+using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
+
+// The workgroup's place in a grid whose consecutive places should share an
+// XCD's cache: workgroups are dispatched to the eight XCDs in turn.
+__device__ __forceinline__ uint32_t xcd_place(uint32_t id, uint32_t n) {
+    const uint32_t x = id % kXcds, q = n / kXcds, r = n % kXcds;
+    return x * q + min(x, r) + id / kXcds;
+}
+
+// Place t of a grid of rows x cols tiles, walked in bands of eight rows so
+// that neighbours share the operands of eight tiles each way.
+__device__ __forceinline__ void banded(uint32_t t, uint32_t rows, uint32_t cols, uint32_t &r, uint32_t &c) {
+    constexpr uint32_t kBand = 8;
+    const uint32_t band = t / (kBand * cols), in = t - band * kBand * cols;
+    const uint32_t high = min(kBand, rows - band * kBand);
+    r = band * kBand + in % high;
+    c = in / high;
+}
+
+}  // namespace efs

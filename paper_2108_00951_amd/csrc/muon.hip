@@ -1,0 +1,745 @@
+// Orthogonalised update of weight matrices (the Muon form of the model update).
+//
+//   m <- beta m + avg ;  u = avg + beta m (Nesterov) or m        element by element
+//   X0 = u / (||u||_F + eps), as an m x n matrix with m <= n (u^T where it is taller)
+//   five times:  A = X X^T ;  B = b A + c A A ;  X <- a X + B X
+//   x <- (1 - gamma decay) x - gamma sqrt(max(1, rows / cols)) X
+//
+// Every singular value of X0 goes through the odd polynomial
+// a s + b s^3 + c s^5 of the step and tends to 1; the singular vectors stay.
+//
+// X and A are kept as split values (mfma_tile.hpp) scaled by 2^14, B by 2^12.
+// No entry of a matrix is larger than its largest singular value, and with
+// ||X0||_F <= 1 those of the iterates stay below 1.3, A's below 1.5 and B's
+// (b s^2 + c s^4) below 3, so that the fp16 parts (65504 at most) do not
+// overflow, and hold 22 bits of every entry above 2^-17 of that.  (At 2^10 the
+// entries of a matrix whose norm eps outweighs lost some.)  Three fp16 products give the error of fp32 products
+// (1.0-1.1 times at 256 x 256 to 256 x 1024, low-rank and ill-conditioned
+// inputs among them); one product gives 1e-3, and iterating on the small Gram
+// matrix alone, cheaper for wide matrices, 1e-4 to 1e-1.  a X is added in fp32
+// to the product B X and not folded into B: twice the error otherwise where
+// the singular values differ much.
+//
+// A call is a setup launch (the table of matrices), two passes over the
+// elements (momentum and sums of squares; the split operands) and three
+// products a step over all matrices together.  X X^T and A A are symmetric:
+// tiles on and below the diagonal are computed and written to both places, so
+// that a step is 3 m^2 n + m^3 operations instead of 4 m^2 n + 2 m^3.  X is
+// kept along both axes, since X X^T sums over one and B X over the other.
+#include "mfma_tile.hpp"
+#include "launch.hpp"
+
+#include <math.h>
+
+namespace efs {
+
+namespace {
+
+constexpr float kScale = 0x1p14f;          // of X and A in their split form
+constexpr float kUnscale = 0x1p-14f;
+constexpr float kScaleB = 0x1p12f;         // of B
+constexpr float kUnscaleB = 0x1p-12f;
+constexpr int kSumBlock = 256;
+constexpr int kMaxChunks = 1024;           // partial sums of one matrix
+constexpr int64_t kChunkMin = 4096;        // elements
+constexpr int kPackTile = 64;
+constexpr int kSetupBlock = 256;
+
+using Small = SmallTile<Prec::kSplit>;
+using Large = LargeTile<Prec::kSplit>;
+
+enum Product { kGram, kPolynomial, kApply, kLast };
+
+// Running counts over the matrices before one: where its tiles, sums and
+// operands start.
+struct Place {
+    int64_t bytes;      // operands
+    int32_t sym[2];     // tiles on and below the diagonal of m x m; [small, large]
+    int32_t full[2];    // tiles of m x n
+    int32_t chunks;     // partial sums
+    int32_t packs;      // 64 x 64 tiles of the caller's matrix
+};
+
+struct Mat {
+    int64_t src, dst;           // first element in the caller's arrays
+    int32_t rows, cols;         // the caller's
+    Place at;
+};
+
+struct Given {   // what the host passes of a matrix
+    int64_t offset;
+    int32_t rows, cols;
+};
+constexpr int kGivenPerLaunch = 192;
+struct GivenArray {
+    Given mat[kGivenPerLaunch];
+};
+
+__host__ __device__ inline int64_t low(const int32_t r, const int32_t c) { return r < c ? r : c; }
+__host__ __device__ inline int64_t high(const int32_t r, const int32_t c) { return r < c ? c : r; }
+
+__host__ __device__ inline int32_t chunks_of(int64_t size) {
+    const int64_t c = (size + kChunkMin - 1) / kChunkMin;
+    return int32_t(c < kMaxChunks ? c : kMaxChunks);
+}
+
+// Elements of one partial sum: whole 16-byte vectors.
+__host__ __device__ inline int64_t chunk_of(int64_t size) {
+    const int64_t c = chunks_of(size);
+    return ((size + c - 1) / c + 3) / 4 * 4;
+}
+
+// Bytes of one X and of one X^T, A and B.
+__host__ __device__ inline int64_t x_bytes(int64_t m, int64_t n) { return m * row_bytes<Prec::kSplit>(n); }
+
+__host__ __device__ inline int64_t operand_bytes(int32_t rows, int32_t cols) {
+    const int64_t m = low(rows, cols), n = high(rows, cols);
+    return 2 * x_bytes(m, n) + 2 * x_bytes(n, m) + 2 * x_bytes(m, m);
+}
+
+__host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols) {
+    const int32_t m = int32_t(low(rows, cols)), n = int32_t(high(rows, cols));
+    p.bytes += operand_bytes(rows, cols);
+    for (int k = 0; k < 2; ++k) {
+        const int32_t t = k == 0 ? Small::kRows : Large::kRows;
+        const int32_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
+        p.sym[k] += tm * (tm + 1) / 2;
+        p.full[k] += tm * tn;
+    }
+    p.chunks += chunks_of(int64_t(rows) * cols);
+    p.packs += ((rows + kPackTile - 1) / kPackTile) * ((cols + kPackTile - 1) / kPackTile);
+}
+
+__device__ inline void add(Place &p, const Place &q) {
+    p.bytes += q.bytes;
+    for (int k = 0; k < 2; ++k) {
+        p.sym[k] += q.sym[k];
+        p.full[k] += q.full[k];
+    }
+    p.chunks += q.chunks;
+    p.packs += q.packs;
+}
+
+// Workspace: the table, the partial sums, the operands.
+struct Layout {
+    int64_t table, sums, operands, total;
+};
+
+inline int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+
+inline Layout layout_of(int64_t nmat, const Place &end) {
+    Layout l;
+    l.table = 0;
+    l.sums = round256((nmat + 1) * int64_t(sizeof(Mat)));
+    l.operands = l.sums + round256(int64_t(end.chunks) * 8);
+    l.total = l.operands + end.bytes;
+    return l;
+}
+
+// The caller's arrays, as both passes and the last product see them.
+struct Io {
+    const void *in;        // avg, or the matrices to orthogonalise
+    float *m;              // momentum; null without
+    void *out;             // x, or the orthogonalised matrices
+    int64_t ld_in, ld_out; // elements between rows; 0: the matrix's own columns
+    float beta, gamma, keep;   // keep = 1 - gamma decay
+    float eps;
+    int nesterov, bf16;
+};
+
+// A matrix's operands in the workspace: X twice, X^T twice, A, B.
+struct Operands {
+    char *base;
+    int64_t m, n;
+    int64_t x_row, t_row;   // bytes of a row of X (n values) and of X^T, A, B (m values)
+    __device__ Operands(char *operands, const Mat &mat)
+        : base(operands + mat.at.bytes), m(low(mat.rows, mat.cols)), n(high(mat.rows, mat.cols)),
+          x_row(row_bytes<Prec::kSplit>(n)), t_row(row_bytes<Prec::kSplit>(m)) {}
+    __device__ char *x(int k) const { return base + k * m * x_row; }
+    __device__ char *xt(int k) const { return base + 2 * m * x_row + k * n * t_row; }
+    __device__ char *a() const { return xt(2); }
+    __device__ char *b() const { return a() + m * t_row; }
+};
+
+// The table.  Entry nmat holds the totals.  `first`: the matrices before
+// `given`, already in the table.  With `given.mat` unused (batch), the matrices
+// are alike and `stride` elements apart.
+__global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, GivenArray given, int32_t first,
+                                                                 int32_t count, int32_t batch,
+                                                                 int64_t stride_in, int64_t stride_out) {
+    if (batch) {   // alike: each place is a multiple
+        for (int32_t i = blockIdx.x * kSetupBlock + threadIdx.x; i <= count; i += gridDim.x * kSetupBlock) {
+            Place one = {};
+            advance(one, given.mat[0].rows, given.mat[0].cols);
+            Mat &t = table[i];
+            t.src = i * stride_in;
+            t.dst = i * stride_out;
+            t.rows = given.mat[0].rows;
+            t.cols = given.mat[0].cols;
+            t.at.bytes = one.bytes * i;
+            for (int k = 0; k < 2; ++k) {
+                t.at.sym[k] = one.sym[k] * i;
+                t.at.full[k] = one.full[k] * i;
+            }
+            t.at.chunks = one.chunks * i;
+            t.at.packs = one.packs * i;
+        }
+        return;
+    }
+    // at most kGivenPerLaunch: running sums by doubling distances
+    __shared__ Place s_sum[kSetupBlock];
+    const int32_t i = threadIdx.x;
+    Place p = {};
+    if (i == 0 && first > 0) p = table[first].at;
+    if (i > 0 && i <= count) advance(p, given.mat[i - 1].rows, given.mat[i - 1].cols);
+    for (int32_t d = 1; d <= count; d *= 2) {
+        s_sum[i] = p;
+        __syncthreads();
+        if (i >= d) add(p, s_sum[i - d]);
+        __syncthreads();
+    }
+    if (i > count) return;
+    // entry first + count is the next launch's first, or the totals
+    Mat &t = table[first + i];
+    if (i < count) {
+        t.src = given.mat[i].offset;
+        t.dst = given.mat[i].offset;
+        t.rows = given.mat[i].rows;
+        t.cols = given.mat[i].cols;
+    }
+    if (i > 0 || first == 0) t.at = p;
+}
+
+// The last matrix whose count starts at or before `at`: none of them is
+// empty, so the starts differ.
+template <class F>
+__device__ __forceinline__ int32_t matrix_of(const Mat *table, int32_t nmat, int32_t at, F start) {
+    int32_t lo = 0, hi = nmat;
+    while (hi - lo > 1) {
+        const int32_t mid = (lo + hi) / 2;
+        if (start(table[mid].at) <= at) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ float direction(const Io &io, float avg, float m) {
+    return io.nesterov ? __fadd_rn(avg, __fmul_rn(io.beta, m)) : m;
+}
+
+__device__ __forceinline__ float read_in(const Io &io, int64_t i) {
+    return io.bf16 ? float(static_cast<const __bf16 *>(io.in)[i]) : static_cast<const float *>(io.in)[i];
+}
+
+// gamma sqrt(max(1, rows / cols))
+__device__ __forceinline__ float step_scale(const Io &io, int32_t rows, int32_t cols) {
+    return __fmul_rn(io.gamma, sqrtf(fmaxf(1.0f, __fdiv_rn(float(rows), float(cols)))));
+}
+
+// The orthogonalised value o of element `at`: into x, or out.
+__device__ __forceinline__ void write_out(const Io &io, int64_t at, float o, float scale) {
+    if (io.m != nullptr) {
+        float *x = static_cast<float *>(io.out) + at;
+        *x = __fsub_rn(__fmul_rn(io.keep, *x), __fmul_rn(scale, o));
+    } else if (io.bf16) {
+        static_cast<__bf16 *>(io.out)[at] = __bf16(o);   // the one rounding to 8 bits
+    } else {
+        static_cast<float *>(io.out)[at] = o;
+    }
+}
+
+// First pass: the momentum in place, and each chunk's sum of u^2 in binary64
+// (a fixed order: the same sum every time).
+__global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *table, int32_t nmat, Io io,
+                                                                  double *sums) {
+    __shared__ double s_f64[kWaves];
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.chunks; });
+    const Mat &mat = table[mi];
+    const int64_t size = int64_t(mat.rows) * mat.cols;
+    const int64_t chunk = chunk_of(size);
+    const int64_t lo = chunk * (int64_t(blockIdx.x) - mat.at.chunks);
+    const int64_t hi = min(size, lo + chunk);
+    double sum = 0.0;
+    if (io.m != nullptr) {
+        const float *avg = static_cast<const float *>(io.in) + mat.src;
+        float *m = io.m + mat.src;
+        int64_t i = lo + int64_t(threadIdx.x) * 4;
+        for (; i + 4 <= hi; i += kSumBlock * 4) {
+            const f32x4u g = *reinterpret_cast<const f32x4u *>(avg + i);
+            f32x4u v = *reinterpret_cast<const f32x4u *>(m + i);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                v[c] = __fadd_rn(__fmul_rn(io.beta, v[c]), g[c]);
+                const double u = direction(io, g[c], v[c]);
+                sum += u * u;
+            }
+            *reinterpret_cast<f32x4u *>(m + i) = v;
+        }
+        for (; i < hi; ++i) {   // the last matrix elements, fewer than four, of one thread
+            const float g = avg[i];
+            const float v = __fadd_rn(__fmul_rn(io.beta, m[i]), g);
+            m[i] = v;
+            const double u = direction(io, g, v);
+            sum += u * u;
+        }
+    } else {
+        const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
+        for (int64_t i = lo + threadIdx.x; i < hi; i += kSumBlock) {
+            const uint32_t r = uint32_t(i) / uint32_t(mat.cols), c = uint32_t(i) - r * uint32_t(mat.cols);
+            const double u = read_in(io, mat.src + r * ld + c);
+            sum += u * u;
+        }
+    }
+    sum = block_sum_f64(sum, s_f64);
+    if (threadIdx.x == 0) sums[blockIdx.x] = sum;
+}
+
+// Second pass: u / (||u|| + eps) as X and X^T, a 64 x 64 tile of the caller's
+// matrix at a time (turned in LDS).
+__global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, int32_t nmat, Io io,
+                                                              const double *sums, char *operands) {
+    __shared__ double s_f64[kWaves];
+    __shared__ float s_norm;
+    __shared__ float tile[kPackTile][kPackTile + 1];
+    const int tid = threadIdx.x;
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.packs; });
+    const Mat &mat = table[mi];
+    const int32_t nsums = chunks_of(int64_t(mat.rows) * mat.cols);
+    double sum = 0.0;
+    for (int32_t i = tid; i < nsums; i += kSumBlock) sum += sums[mat.at.chunks + i];
+    sum = block_sum_f64(sum, s_f64);
+    if (tid == 0) s_norm = __fadd_rn(float(sqrt(sum)), io.eps);
+    __syncthreads();
+    const float norm = s_norm;
+
+    const int32_t across = (mat.cols + kPackTile - 1) / kPackTile;
+    const int32_t t = int32_t(blockIdx.x) - mat.at.packs;
+    const int32_t r0 = t / across * kPackTile, c0 = t % across * kPackTile;
+    const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
+    for (int i = tid; i < kPackTile * kPackTile; i += kSumBlock) {
+        const int32_t r = r0 + i / kPackTile, c = c0 + i % kPackTile;
+        float v = 0.0f;
+        if (r < mat.rows && c < mat.cols) {
+            const int64_t at = mat.src + r * ld + c;
+            const float in = read_in(io, at);
+            v = io.m != nullptr ? direction(io, in, io.m[at]) : in;
+            v = __fmul_rn(__fdiv_rn(v, norm), kScale);
+        }
+        tile[i / kPackTile][i % kPackTile] = v;
+    }
+    __syncthreads();
+
+    const Operands op(operands, mat);
+    const bool wide = mat.rows <= mat.cols;
+    // along the caller's rows, then along its columns; a thread writes eight
+    // values of a row, both halves
+    char *along = wide ? op.x(0) : op.xt(0);
+    char *other = wide ? op.xt(0) : op.x(0);
+    const int64_t along_row = wide ? op.x_row : op.t_row, other_row = wide ? op.t_row : op.x_row;
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+        char *base = turn ? other : along;
+        const int64_t stride = turn ? other_row : along_row;
+        const int32_t row_first = turn ? c0 : r0, col_first = turn ? r0 : c0;
+        const int32_t row_end = turn ? mat.cols : mat.rows;
+        const int32_t col_end = (turn ? mat.rows : mat.cols) + 31 & ~31;
+        for (int i = tid; i < kPackTile * 8; i += kSumBlock) {
+            const int r = turn ? i % kPackTile : i / 8, c = (turn ? i / kPackTile : i % 8) * 8;
+            if (row_first + r >= row_end || col_first + c >= col_end) continue;
+            f16x8 hi, lo;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                _Float16 h, l;
+                split_value(turn ? tile[c + k][r] : tile[r][c + k], h, l);
+                hi[k] = h;
+                lo[k] = l;
+            }
+            char *p = base + (row_first + r) * stride + split_offset(col_first + c);
+            *reinterpret_cast<f16x8 *>(p) = hi;
+            *reinterpret_cast<f16x8 *>(p + 64) = lo;
+        }
+    }
+}
+
+// Four consecutive values of a split row, the first a multiple of four.
+__device__ __forceinline__ void store_split4(char *row, int32_t c, const float (&y)[4]) {
+    f16x4 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        _Float16 h, l;
+        split_value(y[k], h, l);
+        hi[k] = h;
+        lo[k] = l;
+    }
+    char *p = row + split_offset(c);
+    *reinterpret_cast<f16x4 *>(p) = hi;
+    *reinterpret_cast<f16x4 *>(p + 64) = lo;
+}
+
+// One product of a step over all matrices, a tile a workgroup.
+//   kGram        A = X X^T             tiles on and below the diagonal
+//   kPolynomial  B = b A + c A A       the same
+//   kApply       X' = a X + B X        into the other pair of buffers
+//   kLast        the same, into the caller's x or out
+// `cur`: which pair of buffers holds X.
+template <int kProduct, class Tile>
+__global__ __launch_bounds__(Tile::kThreads, 2) void muon_product_kernel(const Mat *table, int32_t nmat,
+                                                                         char *operands, int cur, float a,
+                                                                         float b, float c, Io io) {
+    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    constexpr int kSize = Tile::kRows == Small::kRows ? 0 : 1;
+    constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
+    static_assert(Tile::kRows == Tile::kCols, "tiles of the diagonal are square");
+    const int32_t place = int32_t(xcd_place(blockIdx.x, gridDim.x));
+    const int32_t mi = matrix_of(table, nmat, place, [](const Place &p) { return kSym ? p.sym[kSize] : p.full[kSize]; });
+    const Mat &mat = table[mi];
+    const Operands op(operands, mat);
+    const int32_t m = int32_t(op.m), n = int32_t(op.n);
+    // the caller's orientation in the last product: its rows are X's columns
+    // where the matrix is tall
+    const bool turned = kProduct == kLast && mat.rows > mat.cols;
+    uint32_t tr, tc;
+    const uint32_t t = uint32_t(place - (kSym ? mat.at.sym[kSize] : mat.at.full[kSize]));
+    if (kSym) {
+        tr = uint32_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
+        while (tr * (tr + 1) / 2 > t) --tr;
+        while ((tr + 1) * (tr + 2) / 2 <= t) ++tr;
+        tc = t - tr * (tr + 1) / 2;
+    } else {
+        const uint32_t tm = (m + Tile::kRows - 1) / Tile::kRows, tn = (n + Tile::kCols - 1) / Tile::kCols;
+        if (turned) banded(t, tn, tm, tr, tc);
+        else banded(t, tm, tn, tr, tc);
+    }
+    const int32_t row0 = int32_t(tr) * Tile::kRows, col0 = int32_t(tc) * Tile::kCols;
+
+    const Operand x{op.x(cur), op.x_row, m}, xt{op.xt(cur), op.t_row, n};
+    const Operand oa{op.a(), op.t_row, m}, ob{op.b(), op.t_row, m};
+    Operand left, right;
+    int32_t steps = int32_t(op.t_row / kStepBytes);
+    if (kProduct == kGram) {
+        left = right = x;
+        steps = int32_t(op.x_row / kStepBytes);
+    } else if (kProduct == kPolynomial) {
+        left = right = oa;
+    } else {
+        left = turned ? xt : ob;
+        right = turned ? ob : xt;
+    }
+    Tile tile;
+    tile.run(left, right, row0, col0, 0, steps, lds);
+
+    const int32_t rows = turned ? n : m, cols = kSym ? m : turned ? m : n;
+    const int32_t padded_cols = (cols + 31) & ~31, padded_rows = (rows + 31) & ~31;
+    // what is added to the product: A, or X (turned: X^T)
+    const char *add = kProduct == kPolynomial ? op.a() : turned ? op.xt(cur) : op.x(cur);
+    const int64_t add_row = kProduct == kPolynomial || turned ? op.t_row : op.x_row;
+    const float f_add = kProduct == kPolynomial ? b * (kScaleB * kUnscale) : a;
+    const float f_acc = kProduct == kGram ? kUnscale : kProduct == kPolynomial ? c * (kScaleB * kUnscale * kUnscale) : kUnscaleB;
+    // results: along the rows, and turned
+    char *to = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.x(cur ^ 1);
+    char *to_t = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.xt(cur ^ 1);
+    const int64_t to_row = kSym ? op.t_row : op.x_row;
+    const bool mirror = !kSym || tr != tc;
+    const float scale = step_scale(io, mat.rows, mat.cols);
+    const int64_t ld_out = io.ld_out ? io.ld_out : mat.cols;
+#pragma unroll
+    for (int i = 0; i < Tile::kTilesM; ++i)
+#pragma unroll
+        for (int j = 0; j < Tile::kTilesN; ++j) {
+            const int32_t col = col0 + Tile::col_of(j);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t row4 = row0 + Tile::row_of(i, 4 * q);
+                float y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int32_t row = row4 + k;
+                    const bool in = row < rows && col < cols;
+                    float v = __fmul_rn(tile.acc[i][j][4 * q + k], f_acc);
+                    if (kProduct != kGram && in)
+                        v = __fadd_rn(__fmul_rn(f_add, load_split(add + row * add_row, col)), v);
+                    y[k] = in ? v : 0.0f;
+                    if (kProduct == kLast) {
+                        if (in) write_out(io, mat.dst + row * ld_out + col, __fmul_rn(v, kUnscale), scale);
+                    } else if (row < rows && col < padded_cols) {
+                        store_split(to + row * to_row, col, y[k]);
+                    }
+                }
+                if (kProduct != kLast && mirror && col < cols && row4 < padded_rows)
+                    store_split4(to_t + col * op.t_row, row4, y);
+            }
+        }
+}
+
+// ---- small matrices -------------------------------------------------------
+// A matrix whose X fits in LDS as fp32 is one workgroup's from its gradient to
+// its update: one launch, nothing in the workspace, the fp32 matrix
+// instructions (16 x 16 x 4).  Rows are padded with zeros to 16 values and lie
+// 4 values further apart, so that the 16 rows x 4 values that an instruction
+// takes are in 64 different banks.
+constexpr int kLdsBlock = 512;
+constexpr int kLdsWaves = kLdsBlock / kWave;
+constexpr int kLdsMaxM = 64;
+constexpr int kLdsFloats[2] = {8 << 10, 39 << 10};   // 32 KB: four a compute unit; 156 KB
+
+__host__ __device__ inline int32_t round16(int64_t v) { return int32_t((v + 15) / 16 * 16); }
+
+// LDS of a matrix: X, A, B.
+__host__ __device__ inline int64_t lds_floats(int32_t rows, int32_t cols) {
+    const int64_t m = round16(low(rows, cols)), n = round16(high(rows, cols));
+    return m * (n + 4) + 2 * m * (m + 4);
+}
+
+// 0, 1: the size of the workgroup that takes the matrix; -1: none does.
+__host__ inline int lds_class(int32_t rows, int32_t cols) {
+    if (low(rows, cols) > kLdsMaxM) return -1;
+    const int64_t f = lds_floats(rows, cols);
+    return f <= kLdsFloats[0] ? 0 : f <= kLdsFloats[1] ? 1 : -1;
+}
+
+// One 16 x 16 tile: sum over k < len of left(row, k) right(k, col).  Lane l
+// holds row l % 16 of the left, column l % 16 of the right, k = l / 16; of the
+// result column l % 16, rows l / 16 * 4 + e.
+template <class L, class R>
+__device__ __forceinline__ f32x4 mfma_f32(int32_t len, L left, R right) {
+    const int lane = threadIdx.x & (kWave - 1);
+    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t k = lane >> 4; k < len; k += 4)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(left(lane & 15, k), right(k, lane & 15), acc, 0, 0, 0);
+    return acc;
+}
+
+template <int kClass>
+__global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, bool batch, int64_t stride_in,
+                                                             int64_t stride_out, Io io, int steps, float a, float b,
+                                                             float c) {
+    __shared__ float lds[kLdsFloats[kClass]];
+    __shared__ double s_sum[kLdsWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const Given mat = given.mat[batch ? 0 : blockIdx.x];
+    const int64_t src = batch ? blockIdx.x * stride_in : mat.offset;
+    const int64_t dst = batch ? blockIdx.x * stride_out : mat.offset;
+    const int64_t ld_in = io.ld_in ? io.ld_in : mat.cols, ld_out = io.ld_out ? io.ld_out : mat.cols;
+    const bool tall = mat.rows > mat.cols;
+    const int32_t m = round16(low(mat.rows, mat.cols)), n = round16(high(mat.rows, mat.cols));
+    const int32_t lx = n + 4, la = m + 4;
+    float *X = lds, *A = X + m * lx, *B = A + m * la;
+
+    for (int32_t i = tid; i < m * lx; i += kLdsBlock) X[i] = 0.0f;
+    __syncthreads();
+    const int32_t size = mat.rows * mat.cols;
+    double sum = 0.0;
+    for (int32_t i = tid; i < size; i += kLdsBlock) {
+        const int32_t r = i / mat.cols, col = i - r * mat.cols;
+        const int64_t at = src + r * ld_in + col;
+        float u = read_in(io, at);
+        if (io.m != nullptr) {
+            const float v = __fadd_rn(__fmul_rn(io.beta, io.m[at]), u);
+            io.m[at] = v;
+            u = direction(io, u, v);
+        }
+        X[tall ? col * lx + r : r * lx + col] = u;
+        sum += double(u) * double(u);
+    }
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < kLdsWaves; ++w) sum += s_sum[w];
+    const float norm = __fadd_rn(float(sqrt(sum)), io.eps);
+    // the padding stays zero, also where the norm is zero, infinite or NaN
+    for (int32_t i = tid; i < size; i += kLdsBlock) {
+        const int32_t r = i / mat.cols, col = i - r * mat.cols;
+        float *p = X + (tall ? col * lx + r : r * lx + col);
+        *p = __fdiv_rn(*p, norm);
+    }
+    __syncthreads();
+
+    const int32_t tm = m / 16, tn = n / 16;
+    const int32_t row4 = (lane >> 4) * 4, col = lane & 15;
+    for (int s = 0; s < steps; ++s) {
+        for (int32_t t = wave; t < tm * tm; t += kLdsWaves) {
+            const int32_t r0 = t / tm * 16, c0 = t % tm * 16;
+            const f32x4 g = mfma_f32(n, [&](int r, int k) { return X[(r0 + r) * lx + k]; },
+                                     [&](int k, int q) { return X[(c0 + q) * lx + k]; });
+#pragma unroll
+            for (int e = 0; e < 4; ++e) A[(r0 + row4 + e) * la + c0 + col] = g[e];
+        }
+        __syncthreads();
+        for (int32_t t = wave; t < tm * tm; t += kLdsWaves) {
+            const int32_t r0 = t / tm * 16, c0 = t % tm * 16;
+            const f32x4 g = mfma_f32(m, [&](int r, int k) { return A[(r0 + r) * la + k]; },
+                                     [&](int k, int q) { return A[k * la + c0 + q]; });
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t at = (r0 + row4 + e) * la + c0 + col;
+                B[at] = __fadd_rn(__fmul_rn(b, A[at]), __fmul_rn(c, g[e]));
+            }
+        }
+        __syncthreads();
+        // sixteen columns of X are one wave's, all rows, and replaced in place
+        for (int32_t t = wave; t < tn; t += kLdsWaves) {
+            f32x4 g[kLdsMaxM / 16];
+#pragma unroll
+            for (int i = 0; i < kLdsMaxM / 16; ++i)
+                if (i < tm)
+                    g[i] = mfma_f32(m, [&](int r, int k) { return B[(i * 16 + r) * la + k]; },
+                                    [&](int k, int q) { return X[k * lx + t * 16 + q]; });
+#pragma unroll
+            for (int i = 0; i < kLdsMaxM / 16; ++i)
+                if (i < tm) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float *p = X + (i * 16 + row4 + e) * lx + t * 16 + col;
+                        *p = __fadd_rn(__fmul_rn(a, *p), g[i][e]);
+                    }
+                }
+        }
+        __syncthreads();
+    }
+    const float scale = step_scale(io, mat.rows, mat.cols);
+    for (int32_t i = tid; i < size; i += kLdsBlock) {
+        const int32_t r = i / mat.cols, q = i - r * mat.cols;
+        write_out(io, dst + r * ld_out + q, X[tall ? q * lx + r : r * lx + q], scale);
+    }
+}
+
+// Tiles of the larger kind pay once they fill the compute units; until then
+// four times as many of the smaller kind do.
+bool take_large(int32_t large_tiles) { return large_tiles >= device_cu_count() * 3 / 4; }
+
+template <int kProduct>
+void launch_product(const Place &end, const Mat *table, int32_t nmat, char *operands, int cur, float a, float b,
+                    float c, const Io &io, hipStream_t stream) {
+    constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
+    const int32_t small = kSym ? end.sym[0] : end.full[0], large = kSym ? end.sym[1] : end.full[1];
+    if (take_large(large))
+        muon_product_kernel<kProduct, Large><<<large, Large::kThreads, 0, stream>>>(table, nmat, operands, cur, a, b,
+                                                                                    c, io);
+    else
+        muon_product_kernel<kProduct, Small><<<small, Small::kThreads, 0, stream>>>(table, nmat, operands, cur, a, b,
+                                                                                    c, io);
+}
+
+void launch_lds(int kind, int32_t count, const GivenArray &given, bool batch, int64_t stride_in, int64_t stride_out,
+                const Io &io, int steps, const float *coeffs, hipStream_t stream) {
+    auto run = [&](auto kernel) {
+        kernel<<<count, kLdsBlock, 0, stream>>>(given, batch, stride_in, stride_out, io, steps, coeffs[0], coeffs[1],
+                                                coeffs[2]);
+    };
+    kind == 0 ? run(muon_lds_kernel<0>) : run(muon_lds_kernel<1>);
+}
+
+// The launches after the table.
+hipError_t launch_steps(const Place &end, int32_t nmat, char *ws, const Io &io, int steps, const float *coeffs,
+                        hipStream_t stream) {
+    const Layout l = layout_of(nmat, end);
+    const Mat *table = reinterpret_cast<const Mat *>(ws + l.table);
+    double *sums = reinterpret_cast<double *>(ws + l.sums);
+    char *operands = ws + l.operands;
+    muon_momentum_kernel<<<end.chunks, kSumBlock, 0, stream>>>(table, nmat, io, sums);
+    muon_pack_kernel<<<end.packs, kSumBlock, 0, stream>>>(table, nmat, io, sums, operands);
+    const float a = coeffs[0], b = coeffs[1], c = coeffs[2];
+    int cur = 0;
+    for (int s = 0; s < steps; ++s, cur ^= 1) {
+        launch_product<kGram>(end, table, nmat, operands, cur, a, b, c, io, stream);
+        launch_product<kPolynomial>(end, table, nmat, operands, cur, a, b, c, io, stream);
+        if (s + 1 < steps) launch_product<kApply>(end, table, nmat, operands, cur, a, b, c, io, stream);
+        else launch_product<kLast>(end, table, nmat, operands, cur, a, b, c, io, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool muon_workspace_size(int32_t nmat, const int32_t *rows, const int32_t *cols, int32_t next, size_t *bytes) {
+    Place end = {};
+    int64_t tiles = 0;
+    int32_t live = 0;
+    for (int32_t i = 0; i < nmat; ++i) {
+        if (rows[i * next] == 0 || cols[i * next] == 0 || lds_class(rows[i * next], cols[i * next]) >= 0) continue;
+        Place one = {};
+        advance(one, rows[i * next], cols[i * next]);
+        tiles += int64_t(one.packs) + one.full[0] + one.chunks + one.sym[0];
+        if (tiles > INT32_MAX) return false;
+        advance(end, rows[i * next], cols[i * next]);
+        ++live;
+    }
+    *bytes = size_t(layout_of(live, end).total);
+    return true;
+}
+
+hipError_t launch_muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, void *o, int64_t ld_o,
+                                     int64_t stride_o, bool bf16, int32_t batch, int32_t rows, int32_t cols,
+                                     int steps, const float *coeffs, float eps, void *workspace,
+                                     hipStream_t stream) {
+    Io io = {};
+    io.in = g;
+    io.out = o;
+    io.ld_in = ld_g;
+    io.ld_out = ld_o;
+    io.eps = eps;
+    io.bf16 = bf16;
+    GivenArray given = {};
+    given.mat[0] = Given{0, rows, cols};
+    const int kind = lds_class(rows, cols);
+    if (kind >= 0) {
+        launch_lds(kind, batch, given, true, stride_g, stride_o, io, steps, coeffs, stream);
+        return hipGetLastError();
+    }
+    Place end = {};
+    for (int32_t i = 0; i < batch; ++i) advance(end, rows, cols);
+    char *ws = static_cast<char *>(workspace);
+    const int32_t blocks = (batch + kSetupBlock) / kSetupBlock;
+    muon_setup_kernel<<<blocks < 64 ? blocks : 64, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, 0,
+                                                                             batch, 1, stride_g, stride_o);
+    return launch_steps(end, batch, ws, io, steps, coeffs, stream);
+}
+
+hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offsets, const int32_t *rows,
+                             const int32_t *cols, float *x, float *m, float beta, float gamma, float decay,
+                             bool nesterov, int steps, const float *coeffs, float eps, void *workspace,
+                             hipStream_t stream) {
+    Io io = {};
+    io.in = avg;
+    io.m = m;
+    io.out = x;
+    io.beta = beta;
+    io.gamma = gamma;
+    io.keep = float(1.0 - double(gamma) * double(decay));
+    io.eps = eps;
+    io.nesterov = nesterov;
+
+    // the matrices of each kind, as many as a launch's arguments hold at a time
+    char *ws = static_cast<char *>(workspace);
+    Place end = {};
+    int32_t live = 0;
+    for (int kind = -1; kind <= 1; ++kind) {
+        GivenArray given;
+        int32_t count = 0;
+        auto flush = [&]() {
+            if (count == 0) return;
+            if (kind >= 0)
+                launch_lds(kind, count, given, false, 0, 0, io, steps, coeffs, stream);
+            else
+                muon_setup_kernel<<<1, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, live - count,
+                                                                 count, 0, 0, 0);
+            count = 0;
+        };
+        for (int32_t i = 0; i < nmat; ++i) {
+            if (rows[i] == 0 || cols[i] == 0 || lds_class(rows[i], cols[i]) != kind) continue;
+            if (count == kGivenPerLaunch) flush();
+            given.mat[count++] = Given{offsets[i], rows[i], cols[i]};
+            if (kind < 0) {
+                advance(end, rows[i], cols[i]);
+                ++live;
+            }
+        }
+        flush();
+    }
+    if (live == 0) return hipGetLastError();
+    return launch_steps(end, live, ws, io, steps, coeffs, stream);
+}
+
+}  // namespace efs

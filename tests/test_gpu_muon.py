@@ -1,0 +1,261 @@
+"""Orthogonalised update (muon_orthogonalize, muon_apply) against its formula
+in 64 bits."""
+import numpy as np
+import pytest
+
+from tests import _dense
+from tests._checks import assert_bits_equal
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2108_00951_amd import binding as efs  # noqa: E402
+
+DEV = "cuda"
+SHAPES = [(1, 1), (1, 5), (7, 1), (2, 3), (31, 33), (32, 32), (33, 31), (64, 64), (65, 129), (129, 65), (128, 128),
+          (1, 4097), (4097, 3), (127, 1000), (1000, 127), (256, 300), (300, 257), (513, 520)]
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def ortho(g, **kw):
+    out = torch.full_like(g, 7.0, memory_format=torch.contiguous_format)
+    shapes = [tuple(g.shape[-2:])] * (g.shape[0] if g.dim() == 3 else 1)
+    ws = efs.new_muon_workspace(shapes, DEV)
+    ws.fill_(0xFF)
+    efs.muon_orthogonalize(g, out, ws, **kw)
+    return out
+
+
+@pytest.mark.parametrize("rows, cols", SHAPES)
+@pytest.mark.parametrize("kind", ["gauss", "lowrank"])
+def test_orthogonalize_fp32(rows, cols, kind):
+    say("ortho", rows, cols, kind)
+    g = _dense.matrix(np.random.default_rng(rows * 7919 + cols), kind, rows, cols)
+    got = ortho(torch.from_numpy(g).to(DEV)).cpu().numpy()
+    assert _dense.relative(got, _dense.newton_schulz(g)) <= _dense.ortho_limit(g)
+
+
+@pytest.mark.parametrize("kind", ["tiny", "huge", "one"])
+def test_orthogonalize_ranges(kind):
+    g = _dense.matrix(np.random.default_rng(5), kind, 70, 150)
+    got = ortho(torch.from_numpy(g).to(DEV)).cpu().numpy()
+    assert _dense.relative(got, _dense.newton_schulz(g)) <= _dense.ortho_limit(g)
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 3), (33, 70), (200, 64), (128, 256)])
+def test_orthogonalize_bf16(rows, cols):
+    g = torch.from_numpy(_dense.matrix(np.random.default_rng(rows + cols), "gauss", rows, cols)).to(torch.bfloat16)
+    want = _dense.newton_schulz(g.float().numpy())
+    got = ortho(g.to(DEV)).float().cpu().numpy()
+    # each value is rounded once, to 8 bits
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 1e-4 * np.abs(want).max())
+
+
+@pytest.mark.parametrize("steps, coeffs", [(1, None), (3, (2.0, -1.5, 0.5)), (10, (1.875, -1.25, 0.375))])
+def test_orthogonalize_steps_and_coefficients(steps, coeffs):
+    g = _dense.matrix(np.random.default_rng(9), "gauss", 48, 80)
+    kw = {"steps": steps, "coeffs": coeffs or _dense.COEFFS}
+    got = ortho(torch.from_numpy(g).to(DEV), steps=steps, coeffs=coeffs).cpu().numpy()
+    assert _dense.relative(got, _dense.newton_schulz(g, **kw)) <= _dense.ortho_limit(g, **kw)
+
+
+def test_orthogonalize_batch_of_strided_views():
+    rng = np.random.default_rng(11)
+    g = np.stack([_dense.matrix(rng, "gauss", 37, 90) for _ in range(6)])
+    # rows further apart than they are long, one element off any alignment
+    buf = torch.zeros(6 * 37 * 101 + 1, device=DEV)
+    view = buf[1:].view(6, 37, 101)[:, :, 3:93]
+    view.copy_(torch.from_numpy(g))
+    # matrices whose rows take turns
+    turns = torch.from_numpy(np.ascontiguousarray(g.transpose(1, 0, 2))).to(DEV).transpose(0, 1)
+    dense = ortho(torch.from_numpy(g).to(DEV))
+    for v in (view, turns):
+        assert_bits_equal(ortho(v).cpu().numpy(), dense.cpu().numpy(), "strided input")
+    out = torch.full((37, 6, 95), 5.0, device=DEV)
+    efs.muon_orthogonalize(view, out.transpose(0, 1)[:, :, :90], efs.new_muon_workspace([(37, 90)] * 6, DEV))
+    assert_bits_equal(out.transpose(0, 1)[:, :, :90].contiguous().cpu().numpy(), dense.cpu().numpy(), "strided output")
+    assert torch.all(out[:, :, 90:] == 5.0)
+    for i in range(6):
+        assert _dense.relative(dense[i].cpu().numpy(), _dense.newton_schulz(g[i])) <= _dense.ortho_limit(g[i])
+
+
+def test_orthogonalize_repeats_one_matrix_and_works_in_place():
+    g = torch.from_numpy(_dense.matrix(np.random.default_rng(12), "gauss", 40, 30)).to(DEV)
+    one = ortho(g)
+    three = ortho(g.expand(3, 40, 30))
+    for i in range(3):
+        assert torch.equal(three[i], one)
+    h = g.clone()
+    efs.muon_orthogonalize(h, h, efs.new_muon_workspace([(40, 30)], DEV))
+    assert torch.equal(h, one)
+
+
+def test_many_matrices_in_one_batch():
+    g = np.random.default_rng(13).standard_normal((700, 5, 9)).astype(np.float32)
+    got = ortho(torch.from_numpy(g).to(DEV)).cpu().numpy()
+    for i in range(0, 700, 23):
+        assert _dense.relative(got[i], _dense.newton_schulz(g[i])) <= _dense.ortho_limit(g[i])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_special_values_stay_in_their_matrix(bad):
+    g = np.random.default_rng(14).standard_normal((4, 34, 50)).astype(np.float32)
+    clean = ortho(torch.from_numpy(g).to(DEV))
+    g[2, 5, 7] = bad
+    g[3] = 0.0
+    got = ortho(torch.from_numpy(g).to(DEV))
+    assert torch.equal(got[:2], clean[:2])
+    assert torch.all(torch.isnan(got[2]))
+    assert torch.all(got[3] == 0.0)
+
+
+def test_zero_matrix_without_eps_is_nan():
+    assert torch.all(torch.isnan(ortho(torch.zeros(3, 4, device=DEV), eps=0.0)))
+
+
+def test_empty_calls_do_nothing():
+    for shape in ((0, 4, 5), (2, 0, 5), (2, 4, 0)):
+        ortho(torch.zeros(shape, device=DEV))
+    x = torch.ones(7, device=DEV)
+    efs.muon_apply(torch.ones(7, device=DEV), x, x.clone(), [(3, 0, 5)], efs.new_muon_workspace([(0, 5)], DEV), 0.9, 0.1)
+    assert torch.all(x == 1.0)
+
+
+@pytest.mark.parametrize("shape", [(1, 1100, 2300), (9, 530, 520)])
+def test_orthogonalize_large_tiles(shape):
+    """Enough tiles for the larger kind in some or all products."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    g = torch.randn(shape, generator=gen, device=DEV)
+    got = ortho(g)
+    for k in (0, shape[0] - 1):
+        x = g[k].double()
+        x = x / (x.norm() + 1e-7)
+        y = g[k] / (g[k].norm() + 1e-7)
+        for _ in range(5):
+            a, f = x @ x.T, y @ y.T
+            x = 3.4445 * x + (-4.7750 * a + 2.0315 * a @ a) @ x
+            y = 3.4445 * y + (-4.7750 * f + 2.0315 * f @ f) @ y
+        plain = float((y - x).norm() / x.norm())
+        assert float((got[k] - x).norm() / x.norm()) <= 3 * plain + _dense.SLACK
+
+
+def _model(seed, layers, d):
+    rng = np.random.default_rng(seed)
+    return [(rng.standard_normal(d) * s).astype(np.float32) for s in (1e-3, 0.05, 4e-3)]
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_apply(nesterov, shift):
+    layers, d = [(3, 40, 50), (2003, 50, 20), (3003, 1, 77), (3100, 64, 64), (7300, 0, 9), (7300, 130, 35)], 12000
+    say("apply", nesterov, shift)
+    avg, x, m = _model(21, layers, d)
+    dev = []
+    for v in (avg, x, m):
+        dev.append(torch.zeros(d + shift, device=DEV)[shift:])
+        dev[-1].copy_(torch.from_numpy(v))
+    beta, gamma, decay = np.float32(0.95), np.float32(0.02), np.float32(0.1)
+    ws = efs.new_muon_workspace([v[1:] for v in layers], DEV)
+    call = efs.prepare_muon_apply(dev[0], dev[1], dev[2], layers, ws, beta, gamma, decay, nesterov)
+    for step in range(2):
+        want_x, want_m = x.astype(np.float64), m.copy()
+        limit = np.zeros(d)
+        for at, r, c in layers:
+            s = slice(at, at + r * c)
+            if r * c == 0:
+                continue
+            want_m[s] = beta * m[s] + avg[s]
+            u = (avg[s] + beta * want_m[s] if nesterov else want_m[s]).reshape(r, c)
+            o = _dense.newton_schulz(u).reshape(-1)
+            scale = float(gamma) * np.sqrt(max(1.0, r / c))
+            keep = 1.0 - float(gamma) * float(decay)
+            want_x[s] = keep * x[s].astype(np.float64) - scale * o
+            # three roundings to 24 bits of x's and the update's size, and O's own error
+            limit[s] = 2.0 ** -23 * (np.abs(x[s]) + 2 * scale * np.abs(o)) + scale * _dense.ortho_limit(u) * np.abs(o).max() * 4
+        call()
+        got_x, got_m = dev[1].cpu().numpy(), dev[2].cpu().numpy()
+        assert_bits_equal(got_m, want_m, "m after step %d" % step)
+        assert np.all(np.abs(got_x - want_x) <= limit), step
+        outside = limit == 0.0
+        assert_bits_equal(got_x[outside], x[outside], "x outside the matrices")
+        assert_bits_equal(dev[0].cpu().numpy(), avg, "avg")
+        x, m = got_x.copy(), got_m.copy()
+
+
+def test_apply_many_layers_takes_several_tables():
+    """More layers than one launch of the table holds."""
+    rng = np.random.default_rng(31)
+    layers, at = [], 0
+    for _ in range(500):
+        r, c = int(rng.integers(1, 20)), int(rng.integers(1, 40))
+        layers.append((at, r, c))
+        at += r * c + int(rng.integers(0, 3))
+    avg, x, m = _model(32, layers, at + 5)
+    m[:] = 0.0
+    dx, dm = torch.from_numpy(x).to(DEV), torch.from_numpy(m).to(DEV)
+    ws = efs.new_muon_workspace([v[1:] for v in layers], DEV)
+    efs.muon_apply(torch.from_numpy(avg).to(DEV), dx, dm, layers, ws, 0.9, 1.0, nesterov=False)
+    got = dx.cpu().numpy()
+    for o, r, c in layers[::17] + layers[-3:]:
+        u = avg[o:o + r * c].reshape(r, c)
+        want = x[o:o + r * c].reshape(r, c).astype(np.float64) - np.sqrt(max(1.0, r / c)) * _dense.newton_schulz(u)
+        assert _dense.relative(got[o:o + r * c].reshape(r, c), want) <= _dense.ortho_limit(u) + 2.0 ** -22
+
+
+def test_apply_is_the_same_every_time_and_on_a_side_stream():
+    layers, d = [(0, 150, 300), (45000, 90, 64)], 60000
+    avg, x, m = (torch.from_numpy(v).to(DEV) for v in _model(41, layers, d))
+    results = []
+    for side in (False, False, True):
+        dx, dm = x.clone(), m.clone()
+        ws = efs.new_muon_workspace([v[1:] for v in layers], DEV)
+        s = torch.cuda.Stream() if side else None
+        torch.cuda.synchronize()
+        efs.muon_apply(avg, dx, dm, layers, ws, 0.9, 0.1, stream=s)
+        torch.cuda.synchronize()
+        results.append((dx, dm))
+    for dx, dm in results[1:]:
+        assert torch.equal(dx, results[0][0]) and torch.equal(dm, results[0][1])
+
+
+def test_apply_in_a_graph():
+    layers, d = [(0, 100, 60), (6000, 33, 65)], 8200
+    avg, x, m = (torch.from_numpy(v).to(DEV) for v in _model(51, layers, d))
+    ws = efs.new_muon_workspace([v[1:] for v in layers], DEV)
+    want_x, want_m = x.clone(), m.clone()
+    for _ in range(4):
+        efs.muon_apply(avg, want_x, want_m, layers, ws, 0.9, 0.1)
+    want = [want_x.clone(), want_m.clone()]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        efs.muon_apply(avg, x, m, layers, ws, 0.9, 0.1)
+    for _ in range(4):   # eager work between the replays
+        graph.replay()
+        torch.cuda.synchronize()
+        ws.fill_(0xFF)
+    assert torch.equal(x, want[0]) and torch.equal(m, want[1])
+
+
+def test_binding_refuses_what_the_kernels_do_not_take():
+    g = torch.zeros(4, 6, device=DEV)
+    ws = efs.new_muon_workspace([(4, 6)], DEV)
+    with pytest.raises(TypeError):
+        efs.muon_orthogonalize(g.double(), g.double(), ws)
+    with pytest.raises(TypeError):
+        efs.muon_orthogonalize(g, g.to(torch.bfloat16), ws)
+    with pytest.raises(TypeError):
+        efs.muon_orthogonalize(g.t(), torch.zeros(6, 4, device=DEV), ws)
+    with pytest.raises(ValueError):
+        efs.muon_orthogonalize(g, torch.zeros(4, 5, device=DEV), ws)
+    with pytest.raises(efs.EfsError):
+        efs.muon_orthogonalize(g, torch.zeros_like(g), ws[:16])
+    with pytest.raises(efs.EfsError):
+        efs.muon_apply(g.view(-1), g.view(-1), torch.zeros(24, device=DEV), [(0, 4, 6)], ws, 0.9, 0.1)
+    with pytest.raises(efs.EfsError):   # the second matrix starts inside the first
+        efs.muon_apply(torch.zeros(24, device=DEV), g.view(-1), torch.zeros(24, device=DEV), [(0, 2, 6), (11, 2, 6)],
+                       efs.new_muon_workspace([(2, 6)] * 2, DEV), 0.9, 0.1)
