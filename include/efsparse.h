@@ -375,6 +375,69 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
                       float gamma, float decay, int nesterov, int32_t steps, float eps,
                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* Softmax cross entropy of tokens against a vocabulary: the loss whose
+ * gradient a language model's largest matrix sends through the compression.
+ * The logits l = h w^T are never kept: tiles of them are formed, reduced and
+ * dropped.
+ *     lse[t]  = log(sum over v of exp(l[t, v]))
+ *     loss[t] = lse[t] - l[t, target[t]]
+ *
+ *   h          tokens x hidden hidden states, row t at h + t * ld_h elements.
+ *   w          vocab x hidden output head, row v at w + v * ld_w.
+ *   target     DEVICE int64[tokens], 8-byte aligned.  A token whose target is
+ *              ignore_index does not count: its loss and lse are 0, and its row
+ *              of h may hold anything.  So does, with EFS_XENT_BAD_TARGET in the
+ *              status word, one whose target is neither that nor in [0, vocab).
+ *   dtype      EFS_FP32 or EFS_BF16, of h and w.  fp32 products are held to
+ *              fp32's precision, relative to each tensor's largest finite
+ *              magnitude (elements below 2^-38 of that lose bits); bf16
+ *              products are summed in fp32.
+ *   tokens     0..EFS_XENT_MAX_TOKENS (0: nothing to do); vocab
+ *              1..EFS_XENT_MAX_VOCAB; hidden 1..EFS_XENT_MAX_HIDDEN; tokens x
+ *              vocab at most 2^44.
+ *   loss, lse  fp32[tokens], overwritten.
+ *   workspace  >= xent_workspace_bytes(tokens, vocab, hidden, dtype, 0) bytes,
+ *              16-byte aligned; contents need no initialisation.  bf16 rows
+ *              that are multiples of 64 long and 16-byte aligned are read where
+ *              they are; others, and fp32's, are laid out in the workspace
+ *              first.  Not shareable between concurrent calls.
+ * A row of h that holds NaN or infinities gives NaN, for its token alone. */
+#define EFS_XENT_MAX_TOKENS (1 << 22)
+#define EFS_XENT_MAX_VOCAB (1 << 24)
+#define EFS_XENT_MAX_HIDDEN (1 << 18)
+#define EFS_XENT_BAD_TARGET 1u
+/* Bytes for xent_forward (gradient = 0) or both calls (1); 0 if the arguments
+ * are out of range. */
+size_t xent_workspace_bytes(int32_t tokens, int32_t vocab, int32_t hidden, int dtype, int gradient);
+/* Byte offset, in that workspace, of a uint32 with the EFS_XENT_* bits of the
+ * last completed call (read it after the call has completed). */
+size_t xent_status_offset(void);
+efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,
+                        const int64_t *target, int dtype, int32_t tokens, int32_t vocab,
+                        int32_t hidden, int64_t ignore_index, float *loss, float *lse,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients of the sum over t of dloss[t] * loss[t]:
+ *     g[t, v] = dloss[t] * (exp(l[t, v] - lse[t]) - [v == target[t]])
+ *     dh = g w ;  dw = g^T h
+ * The logits are formed again, a piece of the vocabulary at a time.
+ *
+ *   h .. ignore_index   as for xent_forward.
+ *   lse        fp32[tokens] as xent_forward left it.
+ *   dloss      fp32[tokens]: 1 / (tokens that count) for their mean.  Not used
+ *              where the token does not count.
+ *   dh, dw     tokens x hidden and vocab x hidden of dtype, rows ld_dh and
+ *              ld_dw elements apart, overwritten (dh is 0 where a token does
+ *              not count; dw is 0 with no tokens).  Must not overlap h, w or
+ *              each other.  bf16: g is rounded to bf16 before it is
+ *              multiplied, and so is each result; sums are fp32.
+ *   workspace  >= xent_workspace_bytes(.., 1). */
+efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,
+                         const int64_t *target, int dtype, int32_t tokens, int32_t vocab,
+                         int32_t hidden, int64_t ignore_index, const float *lse,
+                         const float *dloss, void *dh, int64_t ld_dh, void *dw, int64_t ld_dw,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
 /* Streaming copy dst[0..n) = src[0..n) with the same 16-byte access pattern
  * and grid as the hard-threshold kernel: the reference transfer for
  * measurements, not part of the method.  src and dst 16-byte aligned,

@@ -99,6 +99,16 @@ def declare(lib):
                                ctypes.POINTER(i32), f32, f32, f32, ctypes.c_int, i32, f32, vp,
                                ctypes.c_size_t, vp]
     lib.muon_apply.restype = ctypes.c_int
+    lib.xent_workspace_bytes.argtypes = [i32, i32, i32, ctypes.c_int, ctypes.c_int]
+    lib.xent_workspace_bytes.restype = ctypes.c_size_t
+    lib.xent_status_offset.argtypes = []
+    lib.xent_status_offset.restype = ctypes.c_size_t
+    lib.xent_forward.argtypes = [vp, i64, vp, i64, vp, ctypes.c_int, i32, i32, i32, i64, vp, vp, vp,
+                                 ctypes.c_size_t, vp]
+    lib.xent_forward.restype = ctypes.c_int
+    lib.xent_backward.argtypes = [vp, i64, vp, i64, vp, ctypes.c_int, i32, i32, i32, i64, vp, vp, vp, i64,
+                                  vp, i64, vp, ctypes.c_size_t, vp]
+    lib.xent_backward.restype = ctypes.c_int
     lib.efs_copy_probe.argtypes = [vp, vp, i64, vp]
     lib.efs_copy_probe.restype = ctypes.c_int
     lib.efs_stream_probe.argtypes = [vp, vp, i64, ctypes.c_int, vp]
@@ -551,6 +561,82 @@ def muon_apply(avg, x, m, layers: Sequence[Tuple[int, int, int]], workspace, bet
     of each matrix, ascending; workspace from new_muon_workspace."""
     prepare_muon_apply(avg, x, m, layers, workspace, beta, gamma, weight_decay, nesterov, steps, eps,
                        stream)()
+
+
+def xent_workspace_bytes(tokens: int, vocab: int, hidden: int, dtype, gradient: bool = True) -> int:
+    import torch
+    code = {torch.float32: FP32, torch.bfloat16: BF16}[dtype]
+    return int(load_library().xent_workspace_bytes(int(tokens), int(vocab), int(hidden), code,
+                                                   int(bool(gradient))))
+
+
+def new_xent_workspace(tokens: int, vocab: int, hidden: int, dtype, device="cuda", gradient: bool = True):
+    """A workspace for xent_forward and, with gradient, xent_backward."""
+    import torch
+    return torch.empty(max(xent_workspace_bytes(tokens, vocab, hidden, dtype, gradient), 16),
+                       dtype=torch.uint8, device=device)
+
+
+XENT_BAD_TARGET = 1
+
+
+def xent_status(workspace) -> int:
+    """EFS_XENT_* bits of the last completed xent call on this workspace (synchronises)."""
+    off = int(load_library().xent_status_offset())
+    return int(workspace[off:off + 4].cpu().numpy().view("<u4")[0])
+
+
+def _xent_args(h, w, target):
+    """The arguments that both directions pass alike, checked."""
+    import torch
+    if h.dim() != 2 or w.dim() != 2 or h.shape[1] != w.shape[1] or target.shape != h.shape[:1]:
+        raise ValueError("h must be [tokens, hidden], w [vocab, hidden] and target [tokens]")
+    if h.dtype != w.dtype:
+        raise TypeError("h and w must have one dtype")
+    dtype = _dtype_code(h, "h")
+    _require_rows(h, "h")
+    _require_rows(w, "w")
+    _require(target, torch.int64, "target")
+    return (_ptr(h), _row_stride(h), _ptr(w), _row_stride(w), _ptr(target), dtype, h.shape[0], w.shape[0],
+            h.shape[1])
+
+
+def xent_forward(h, w, target, loss, lse, workspace, ignore_index: int = -100, stream=None) -> None:
+    """Softmax cross entropy of tokens h [tokens, hidden] against the head w
+    [vocab, hidden], fp32 or bf16: loss and lse, fp32 [tokens]; see
+    xent_forward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    args = _xent_args(h, w, target)
+    _require(loss, torch.float32, "loss")
+    _require(lse, torch.float32, "lse")
+    _require(workspace, torch.uint8, "workspace")
+    if loss.shape != target.shape or lse.shape != target.shape:
+        raise ValueError("loss and lse must be [tokens]")
+    _check(lib, lib.xent_forward(*args, int(ignore_index), _ptr(loss), _ptr(lse), _ptr(workspace),
+                                 workspace.numel(), _stream_handle(stream)))
+
+
+def xent_backward(h, w, target, lse, dloss, dh, dw, workspace, ignore_index: int = -100, stream=None) -> None:
+    """Gradients of sum(dloss * loss) into dh and dw (shapes and dtype of h and
+    w); lse as xent_forward left it; see xent_backward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    args = _xent_args(h, w, target)
+    _require(lse, torch.float32, "lse")
+    _require(dloss, torch.float32, "dloss")
+    _require(workspace, torch.uint8, "workspace")
+    if lse.shape != target.shape or dloss.shape != target.shape:
+        raise ValueError("lse and dloss must be [tokens]")
+    if dh.shape != h.shape or dw.shape != w.shape:
+        raise ValueError("dh and dw must have the shapes of h and w")
+    if dh.dtype != h.dtype or dw.dtype != h.dtype:
+        raise TypeError("dh and dw must have the dtype of h and w")
+    _require_rows(dh, "dh")
+    _require_rows(dw, "dw")
+    _check(lib, lib.xent_backward(*args, int(ignore_index), _ptr(lse), _ptr(dloss), _ptr(dh),
+                                  _row_stride(dh), _ptr(dw), _row_stride(dw), _ptr(workspace),
+                                  workspace.numel(), _stream_handle(stream)))
 
 
 def copy_probe(src, dst, stream=None) -> None:

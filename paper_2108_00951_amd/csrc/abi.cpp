@@ -19,6 +19,10 @@ static_assert(efs::kMaxSegments == EFS_SEG_MAX, "segment limit differs from the 
 static_assert(efs::kStaticScratchBytes == EFS_STATIC_SCRATCH_BYTES, "scratch size differs from the header");
 static_assert(efs::kMuonMaxMatrices == EFS_MUON_MAX_MATRICES, "matrix limit differs from the header");
 static_assert(efs::kMuonMaxSteps == EFS_MUON_MAX_STEPS, "step limit differs from the header");
+static_assert(efs::kXentMaxTokens == EFS_XENT_MAX_TOKENS, "token limit differs from the header");
+static_assert(efs::kXentMaxVocab == EFS_XENT_MAX_VOCAB, "vocabulary limit differs from the header");
+static_assert(efs::kXentMaxHidden == EFS_XENT_MAX_HIDDEN, "hidden limit differs from the header");
+static_assert(efs::kXentBadTarget == EFS_XENT_BAD_TARGET, "status bit differs from the header");
 static_assert(sizeof(efs::Telemetry) == EFS_TELEMETRY_BYTES, "telemetry layout differs from the header");
 
 namespace {
@@ -49,6 +53,14 @@ constexpr int64_t kMaxLen = INT32_MAX;
 bool overlap(const float *a, const float *b, int64_t d) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + uintptr_t(d) * 4 && y < x + uintptr_t(d) * 4;
+}
+
+// Whether the spans from the first to the last element of two row sets meet.
+bool rows_overlap(const void *a, int64_t rows_a, int64_t ld_a, const void *b, int64_t rows_b, int64_t ld_b,
+                  int64_t cols, int64_t size) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + uintptr_t(((rows_b - 1) * ld_b + cols) * size) &&
+           y < x + uintptr_t(((rows_a - 1) * ld_a + cols) * size);
 }
 
 int g_cu_count[64];  // per device; 0 = not queried yet
@@ -430,6 +442,89 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
     return check_launch(efs::launch_muon_apply(avg, nmat, offsets, rows, cols, x, m, beta, gamma, decay,
                                                nesterov != 0, steps, kCoeffs, eps, workspace,
                                                static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+static bool xent_sizes_ok(int32_t tokens, int32_t vocab, int32_t hidden, int dtype) {
+    return tokens >= 0 && tokens <= efs::kXentMaxTokens && vocab >= 1 && vocab <= efs::kXentMaxVocab &&
+           hidden >= 1 && hidden <= efs::kXentMaxHidden && int64_t(tokens) * vocab <= int64_t(1) << 44 &&
+           (dtype == EFS_FP32 || dtype == EFS_BF16);
+}
+
+size_t xent_workspace_bytes(int32_t tokens, int32_t vocab, int32_t hidden, int dtype, int gradient) {
+    if (!xent_sizes_ok(tokens, vocab, hidden, dtype) || gradient < 0 || gradient > 1) return 0;
+    return efs::xent_workspace_size(tokens, vocab, hidden, dtype == EFS_BF16, gradient != 0);
+}
+
+size_t xent_status_offset(void) { return 0; }
+
+// What both directions check alike.  Their rows: pointer, elements between them.
+static efs_status check_xent(const char *name, const void *h, int64_t ld_h, const void *w, int64_t ld_w,
+                             const int64_t *target, int dtype, int32_t tokens, int32_t vocab, int32_t hidden,
+                             bool gradient, const void *workspace, size_t workspace_bytes) {
+    if (dtype != EFS_FP32 && dtype != EFS_BF16)
+        return fail(EFS_EINVAL, "%s: dtype %d is neither EFS_FP32 nor EFS_BF16", name, dtype);
+    if (!xent_sizes_ok(tokens, vocab, hidden, dtype))
+        return fail(EFS_EINVAL, "%s: %d tokens, %d words or %d values a row are outside the limits", name, tokens,
+                    vocab, hidden);
+    if (tokens == 0) return EFS_OK;
+    const uintptr_t size = dtype == EFS_BF16 ? 2 : 4;
+    if (h == nullptr || w == nullptr || !aligned(h, size) || !aligned(w, size))
+        return fail(EFS_EINVAL, "%s: h and w must be non-NULL and aligned to their type", name);
+    if (ld_h < hidden || ld_w < hidden || ld_h > kMaxLen || ld_w > kMaxLen)
+        return fail(EFS_EINVAL, "%s: ld_h and ld_w must be in [hidden, 2^31-1]", name);
+    if (target == nullptr || !aligned(target, 8))
+        return fail(EFS_EINVAL, "%s: target must be non-NULL and 8-byte aligned", name);
+    if (workspace == nullptr || !aligned(workspace, 16))
+        return fail(EFS_EINVAL, "%s: workspace must be non-NULL and 16-byte aligned", name);
+    const size_t need = efs::xent_workspace_size(tokens, vocab, hidden, dtype == EFS_BF16, gradient);
+    if (workspace_bytes < need)
+        return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    return EFS_OK;
+}
+
+efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
+                        int dtype, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore_index,
+                        float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *name = "xent_forward";
+    const efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, false, workspace,
+                                    workspace_bytes);
+    if (s != EFS_OK || tokens == 0) return s;
+    if (loss == nullptr || lse == nullptr || !aligned(loss, 4) || !aligned(lse, 4))
+        return fail(EFS_EINVAL, "%s: loss and lse must be non-NULL and 4-byte aligned", name);
+    return check_launch(efs::launch_xent_forward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,
+                                                 hidden, ignore_index, loss, lse, workspace,
+                                                 static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
+                         int dtype, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore_index,
+                         const float *lse, const float *dloss, void *dh, int64_t ld_dh, void *dw, int64_t ld_dw,
+                         void *workspace, size_t workspace_bytes, void *stream) {
+    const char *name = "xent_backward";
+    const efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, true, workspace,
+                                    workspace_bytes);
+    if (s != EFS_OK) return s;
+    const uintptr_t size = dtype == EFS_BF16 ? 2 : 4;
+    if (dw == nullptr || !aligned(dw, size) || ld_dw < hidden || ld_dw > kMaxLen)
+        return fail(EFS_EINVAL, "%s: dw must be non-NULL and aligned to its type, ld_dw in [hidden, 2^31-1]", name);
+    if (tokens > 0) {
+        if (dh == nullptr || !aligned(dh, size) || ld_dh < hidden || ld_dh > kMaxLen)
+            return fail(EFS_EINVAL, "%s: dh must be non-NULL and aligned to its type, ld_dh in [hidden, 2^31-1]",
+                        name);
+        if (lse == nullptr || dloss == nullptr || !aligned(lse, 4) || !aligned(dloss, 4))
+            return fail(EFS_EINVAL, "%s: lse and dloss must be non-NULL and 4-byte aligned", name);
+        const void *given[4] = {h, w, dh, dw};
+        const int64_t rows[4] = {tokens, vocab, tokens, vocab}, ld[4] = {ld_h, ld_w, ld_dh, ld_dw};
+        for (int i = 2; i < 4; ++i)
+            for (int j = 0; j < i; ++j)
+                if (rows_overlap(given[i], rows[i], ld[i], given[j], rows[j], ld[j], hidden, size))
+                    return fail(EFS_EINVAL, "%s: dh and dw must not overlap h, w or each other", name);
+    }
+    return check_launch(efs::launch_xent_backward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,
+                                                  hidden, ignore_index, lse, dloss, dh, ld_dh, dw, ld_dw,
+                                                  workspace, static_cast<hipStream_t>(stream)),
                         name);
 }
 

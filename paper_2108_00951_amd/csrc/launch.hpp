@@ -62,6 +62,18 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
                              bool nesterov, int steps, const float *coeffs, float eps, void *workspace,
                              hipStream_t stream);
 
+// Softmax cross entropy over a vocabulary and its gradients (xent.hip).
+constexpr uint32_t kXentBadTarget = 1u;   // a target neither ignored nor in the vocabulary
+constexpr int32_t kXentMaxTokens = 1 << 22, kXentMaxVocab = 1 << 24, kXentMaxHidden = 1 << 18;
+size_t xent_workspace_size(int32_t tokens, int32_t vocab, int32_t hidden, bool bf16, bool gradient);
+hipError_t launch_xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
+                               bool bf16, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore, float *loss,
+                               float *lse, void *workspace, hipStream_t stream);
+hipError_t launch_xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
+                                bool bf16, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore,
+                                const float *lse, const float *dloss, void *dh, int64_t ld_dh, void *dw,
+                                int64_t ld_dw, void *workspace, hipStream_t stream);
+
 hipError_t launch_copy(const float *src, float *dst, int64_t n, bool per_tile, hipStream_t stream);
 hipError_t launch_stream_probe(const float *x, float *y, int64_t n, int mode, bool per_tile,
                                hipStream_t stream);

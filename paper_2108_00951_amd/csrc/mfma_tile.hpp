@@ -29,6 +29,7 @@
 #include <stdint.h>
 
 #include "device_common.hpp"
+#include "launch.hpp"
 
 namespace efs {
 
@@ -78,6 +79,21 @@ __device__ __forceinline__ void store_split(char *row, int32_t c, float y) {
     char *p = row + split_offset(c);
     *reinterpret_cast<_Float16 *>(p) = hi;
     *reinterpret_cast<_Float16 *>(p + 64) = lo;
+}
+
+// Four consecutive values of a split row, the first a multiple of four.
+__device__ __forceinline__ void store_split4(char *row, int32_t c, const float (&y)[4]) {
+    f16x4 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        _Float16 h, l;
+        split_value(y[k], h, l);
+        hi[k] = h;
+        lo[k] = l;
+    }
+    char *p = row + split_offset(c);
+    *reinterpret_cast<f16x4 *>(p) = hi;
+    *reinterpret_cast<f16x4 *>(p + 64) = lo;
 }
 
 __device__ __forceinline__ float load_split(const char *row, int32_t c) {
@@ -223,6 +239,10 @@ template <Prec P>
 using LargeTile = MfmaTile<P, 2, 4, 4, 2>;
 template <Prec P>
 using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
+
+// Tiles of the larger kind pay once they fill the compute units; until then
+// four times as many of the smaller kind do (measured above).
+inline bool take_large(int64_t large_tiles) { return large_tiles >= device_cu_count() * 3 / 4; }
 
 // The workgroup's place in a grid whose consecutive places should share an
 // XCD's cache: workgroups are dispatched to the eight XCDs in turn.

@@ -361,21 +361,6 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, 
     }
 }
 
-// Four consecutive values of a split row, the first a multiple of four.
-__device__ __forceinline__ void store_split4(char *row, int32_t c, const float (&y)[4]) {
-    f16x4 hi, lo;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        _Float16 h, l;
-        split_value(y[k], h, l);
-        hi[k] = h;
-        lo[k] = l;
-    }
-    char *p = row + split_offset(c);
-    *reinterpret_cast<f16x4 *>(p) = hi;
-    *reinterpret_cast<f16x4 *>(p + 64) = lo;
-}
-
 // One product of a step over all matrices, a tile a workgroup.
 //   kGram        A = X X^T             tiles on and below the diagonal
 //   kPolynomial  B = b A + c A A       the same
@@ -604,10 +589,6 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
         write_out(io, dst + r * ld_out + q, X[tall ? q * lx + r : r * lx + q], scale);
     }
 }
-
-// Tiles of the larger kind pay once they fill the compute units; until then
-// four times as many of the smaller kind do.
-bool take_large(int32_t large_tiles) { return large_tiles >= device_cu_count() * 3 / 4; }
 
 template <int kProduct>
 void launch_product(const Place &end, const Mat *table, int32_t nmat, char *operands, int cur, float a, float b,

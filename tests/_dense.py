@@ -47,3 +47,40 @@ def matrix(rng, kind, rows, cols):
         g = np.zeros((rows, cols))
         g[rows // 2, cols // 3] = -3.0
     return g.astype(np.float32)
+
+
+def xent(h, w, target, dloss, ignore=-100):
+    """loss, lse, dh, dw in 64 bits, and elementwise limits on what fp32 sums
+    (limits["fp32"]) or bf16 tensors (["bf16"]) may be off by.
+
+    A logit is a sum whose terms have 22 bits at least, and its own sum's
+    roundings: 2^-20 of the sum of the terms' magnitudes.  exp() turns that
+    into a relative error of p, twice it with lse's.  Each product's sum again
+    loses 2^-20 of its terms; bf16 rounds g and the result by 2^-8."""
+    h, w, dloss = (np.asarray(v, np.float64) for v in (h, w, dloss))
+    counts = (target != ignore) & (target >= 0) & (target < w.shape[0])
+    h = np.where(counts[:, None], h, 0.0)
+    at = np.where(counts, target, 0)
+    rows = np.arange(len(target))
+    l = h @ w.T
+    top = l.max(1, keepdims=True, initial=-np.inf)
+    lse = (top + np.log(np.exp(l - top).sum(1, keepdims=True)))[:, 0]
+    loss = np.where(counts, lse - l[rows, at], 0.0)
+    off = 2.0 ** -20 * (np.abs(h) @ np.abs(w).T).max(1, initial=0.0)
+    p = np.exp(l - lse[:, None])
+    weight = np.where(counts, dloss, 0.0)
+    g = p * weight[:, None]
+    g[rows, at] -= weight
+    dh, dw = g @ w, g.T @ h
+    out = {"loss": loss, "lse": np.where(counts, lse, 0.0), "dh": dh, "dw": dw}
+    limits = {}
+    for name, eps in (("fp32", 0.0), ("bf16", 2.0 ** -8)):
+        dg = (2.0 ** -20 + eps) * np.abs(g) + 2 * off[:, None] * p * np.abs(weight)[:, None]
+        # p - 1 at the target: rounded at the size of one
+        dg[rows, at] += 2.0 ** -22 * np.abs(weight)
+        limits[name] = {
+            "lse": off + 2.0 ** -21 * (1.0 + np.abs(lse)), "loss": 2 * off + 2.0 ** -20 * (1.0 + np.abs(lse)),
+            "dh": dg @ np.abs(w) + eps * np.abs(dh) + 2.0 ** -20 * (np.abs(g) @ np.abs(w)),
+            "dw": dg.T @ np.abs(h) + eps * np.abs(dw) + 2.0 ** -20 * (np.abs(g).T @ np.abs(h)),
+        }
+    return out, limits

@@ -1,0 +1,60 @@
+"""Argument checks of the cross entropy, before anything touches a device."""
+import ctypes
+import os
+
+import pytest
+
+from paper_2108_00951_amd import binding
+
+FAKE = 1 << 20   # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(binding.LIB_PATH):
+        pytest.fail("libefsparse.so is not built (run __graft_entry__.build())")
+    return binding.declare(ctypes.CDLL(binding.LIB_PATH))
+
+
+def test_workspace_bytes(lib):
+    forward = lib.xent_workspace_bytes(100, 5000, 64, 0, 0)
+    assert 0 < forward < lib.xent_workspace_bytes(100, 5000, 64, 0, 1)
+    assert lib.xent_workspace_bytes(0, 5000, 64, 1, 1) > 0
+    for bad in ((-1, 5000, 64, 0, 0), (2 ** 22 + 1, 5, 64, 0, 0), (100, 0, 64, 0, 0), (100, 2 ** 24 + 1, 64, 0, 0),
+                (100, 5000, 0, 0, 0), (100, 5000, 2 ** 18 + 1, 0, 0), (100, 5000, 64, 2, 0), (100, 5000, 64, 0, 2),
+                (2 ** 22, 2 ** 23, 64, 0, 0)):
+        assert lib.xent_workspace_bytes(*bad) == 0, bad
+    # the logits are not kept: a large vocabulary's pieces stay far below them
+    tokens, vocab = 65536, 131072
+    assert lib.xent_workspace_bytes(tokens, vocab, 64, 1, 1) < 2 * tokens * vocab / 4
+
+
+GOOD = dict(h=FAKE, ld_h=64, w=4 * FAKE, ld_w=64, target=FAKE, dtype=0, tokens=10, vocab=1000, hidden=64, ignore=-100)
+BAD = [dict(h=None), dict(w=None), dict(h=FAKE + 2), dict(dtype=1, w=FAKE + 1), dict(ld_h=63), dict(ld_w=63),
+       dict(ld_w=2 ** 31), dict(target=None), dict(target=FAKE + 4), dict(dtype=2), dict(tokens=-1), dict(vocab=0),
+       dict(hidden=0), dict(tokens=2 ** 23), dict(ws=None), dict(ws=FAKE + 8)]
+
+
+def test_forward_rejects_bad_arguments(lib):
+    need = lib.xent_workspace_bytes(10, 1000, 64, 0, 0)
+    good = dict(GOOD, loss=FAKE, lse=FAKE, ws=FAKE, nb=need)
+    for over in BAD + [dict(loss=None), dict(lse=None), dict(lse=FAKE + 2), dict(nb=need - 1)]:
+        a = dict(good, **over)
+        rc = lib.xent_forward(*(a[k] for k in GOOD), a["loss"], a["lse"], a["ws"], a["nb"], None)
+        assert rc == (binding.EFS_ESPACE if "nb" in over else binding.EFS_EINVAL), over
+        assert lib.efs_last_error_message()
+    assert lib.xent_forward(None, 64, None, 64, None, 0, 0, 1000, 64, -100, None, None, None, 0,
+                            None) == binding.EFS_OK
+
+
+def test_backward_rejects_bad_arguments(lib):
+    need = lib.xent_workspace_bytes(10, 1000, 64, 0, 1)
+    good = dict(GOOD, lse=FAKE, dloss=FAKE, dh=8 * FAKE, ld_dh=64, dw=16 * FAKE, ld_dw=64, ws=FAKE, nb=need)
+    more = [dict(lse=None), dict(dloss=None), dict(dh=None), dict(dw=None), dict(dh=8 * FAKE + 2), dict(ld_dh=63),
+            dict(ld_dw=63), dict(dh=FAKE), dict(dw=4 * FAKE), dict(dw=4 * FAKE + 255996), dict(dh=16 * FAKE + 512),
+            dict(nb=need - 1)]
+    for over in BAD + more:
+        a = dict(good, **over)
+        rc = lib.xent_backward(*(a[k] for k in GOOD), a["lse"], a["dloss"], a["dh"], a["ld_dh"], a["dw"], a["ld_dw"],
+                               a["ws"], a["nb"], None)
+        assert rc == (binding.EFS_ESPACE if "nb" in over else binding.EFS_EINVAL), over
