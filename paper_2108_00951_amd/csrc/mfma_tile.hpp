@@ -31,11 +31,13 @@
 #include "device_common.hpp"
 #include "launch.hpp"
 
+#include <math.h>
+#include <type_traits>
+
 namespace efs {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 enum class Prec { kBf16, kSplit };
@@ -73,33 +75,19 @@ __device__ __forceinline__ int64_t split_offset(int32_t c) {
     return int64_t(c >> 5) * kStepBytes + (c & 31) * 2;
 }
 
-__device__ __forceinline__ void store_split(char *row, int32_t c, float y) {
-    _Float16 hi, lo;
-    split_value(y, hi, lo);
-    char *p = row + split_offset(c);
-    *reinterpret_cast<_Float16 *>(p) = hi;
-    *reinterpret_cast<_Float16 *>(p + 64) = lo;
-}
-
-// Four consecutive values of a split row, the first a multiple of four.
-__device__ __forceinline__ void store_split4(char *row, int32_t c, const float (&y)[4]) {
-    f16x4 hi, lo;
+// Eight consecutive values of a split row, the first a multiple of eight.
+__device__ __forceinline__ void store_split8(char *row, int32_t c, const float (&y)[8]) {
+    f16x8 hi, lo;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 8; ++k) {
         _Float16 h, l;
         split_value(y[k], h, l);
         hi[k] = h;
         lo[k] = l;
     }
     char *p = row + split_offset(c);
-    *reinterpret_cast<f16x4 *>(p) = hi;
-    *reinterpret_cast<f16x4 *>(p + 64) = lo;
-}
-
-__device__ __forceinline__ float load_split(const char *row, int32_t c) {
-    const char *p = row + split_offset(c);
-    return __fadd_rn(float(*reinterpret_cast<const _Float16 *>(p)),
-                     float(*reinterpret_cast<const _Float16 *>(p + 64)));
+    *reinterpret_cast<f16x8 *>(p) = hi;
+    *reinterpret_cast<f16x8 *>(p + 64) = lo;
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -233,16 +221,120 @@ struct MfmaTile {
     }
 };
 
-// The two shapes in use: 256 x 256 by eight waves, one workgroup a compute
-// unit, and 128 x 128 by four, two a compute unit.
+// A finished tile on its way out, a band of WM x 32 rows at a time through LDS,
+// so that both a row's and a column's neighbours leave in 16-byte pieces.
+// Straight from the accumulators (a lane holds one column) a row leaves two
+// bytes a lane: 1024 x 4096 x 1024 then took 549 us for twelve matrices, with
+// the product itself 240 of them.
+template <class Tile>
+struct Band {
+    static constexpr int kRows = Tile::kRows / Tile::kTilesM;   // 32 of each row of waves
+    static constexpr int kStride = Tile::kCols + 4;
+    static constexpr int kGroups = Tile::kCols / 8;
+    static constexpr int kUnits = kRows * kGroups / Tile::kThreads;   // of eight values, a thread's
+    static_assert(kRows * kStride * 4 <= Tile::kLdsBytes, "a band fits");
+    static_assert(kUnits * Tile::kThreads == kRows * kGroups, "whole units");
+
+    float *lds;
+
+    // Row of the tile that row r of band i is.
+    static __device__ __forceinline__ int tile_row(int i, int r) {
+        return ((r >> 5) * Tile::kTilesM + i) * 32 + (r & 31);
+    }
+    // Unit k along the rows: eight columns from col() of row().
+    static __device__ __forceinline__ int row(int k) { return (k * Tile::kThreads + int(threadIdx.x)) / kGroups; }
+    static __device__ __forceinline__ int col(int k) { return (k * Tile::kThreads + int(threadIdx.x)) % kGroups * 8; }
+    // Unit k along the columns: eight rows of the band from turned_row() of
+    // column turned_col(); four neighbouring lanes have one column.
+    static __device__ __forceinline__ int turned_row(int k) {
+        const int u = k * Tile::kThreads + int(threadIdx.x);
+        return u / (4 * Tile::kCols) * 32 + u % 4 * 8;
+    }
+    static __device__ __forceinline__ int turned_col(int k) {
+        return (k * Tile::kThreads + int(threadIdx.x)) / 4 % Tile::kCols;
+    }
+
+    // acc[i][..] into LDS; a barrier on either side.
+    template <int i>
+    __device__ __forceinline__ void put(const Tile &tile) {
+        __syncthreads();
+        const int lane = threadIdx.x & (kWave - 1);
+        const int first = (Tile::row_of(0, 0) / (Tile::kTilesM * 32)) * 32 + (lane >> 5) * 4;
+#pragma unroll
+        for (int j = 0; j < Tile::kTilesN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                lds[(first + (e >> 2) * 8 + (e & 3)) * kStride + Tile::col_of(j)] = tile.acc[i][j][e];
+        __syncthreads();
+    }
+    __device__ __forceinline__ void get(int k, float (&v)[8]) const {
+        const f32x4 *p = reinterpret_cast<const f32x4 *>(lds + row(k) * kStride + col(k));
+        const f32x4 a = p[0], b = p[1];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            v[c] = a[c];
+            v[4 + c] = b[c];
+        }
+    }
+    __device__ __forceinline__ void set(int k, const float (&v)[8]) {
+        f32x4 *p = reinterpret_cast<f32x4 *>(lds + row(k) * kStride + col(k));
+        p[0] = f32x4{v[0], v[1], v[2], v[3]};
+        p[1] = f32x4{v[4], v[5], v[6], v[7]};
+    }
+    __device__ __forceinline__ void get_turned(int k, float (&v)[8]) const {
+        const float *p = lds + turned_row(k) * kStride + turned_col(k);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = p[c * kStride];
+    }
+};
+
+// Calls f(integral constant i) for i = 0 .. N-1: the accumulators' first index
+// has to be known to the compiler.
+template <int N, int i = 0, class F>
+__device__ __forceinline__ void each_band(F f) {
+    if constexpr (i < N) {
+        f(std::integral_constant<int, i>());
+        each_band<N, i + 1>(f);
+    }
+}
+
+// The shapes in use: 256 x 256 by eight waves (one workgroup a compute unit),
+// 128 x 128 by four (two), 64 x 64 by four (four).
 template <Prec P>
 using LargeTile = MfmaTile<P, 2, 4, 4, 2>;
 template <Prec P>
 using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
+template <Prec P>
+using TinyTile = MfmaTile<P, 2, 2, 1, 1>;
 
-// Tiles of the larger kind pay once they fill the compute units; until then
-// four times as many of the smaller kind do (measured above).
-inline bool take_large(int64_t large_tiles) { return large_tiles >= device_cu_count() * 3 / 4; }
+enum TileKind { kTiny, kSmall, kLarge };
+constexpr int kTileKinds = 3;
+constexpr int kTileSide[kTileKinds] = {64, 128, 256};
+
+// What a product over tiles of one kind takes: `work` tiles times steps in
+// all, `longest` steps of one tile, in microseconds.  Measured on kSplit
+// steps: a tile's step takes 0.32, 0.63 and 1.7 us on its own, and 0.25, 0.70
+// and 2.4 us of a compute unit where all are busy (270, 380 and 440 TFLOP/s),
+// so that 256 x 1024 x 512 is fastest with the smallest kind (13.6 against
+// 24.2 and 60 us), 2048 x 4096 x 1024 with the middle one (63.6, 49.3, 64.8) and
+// 4096 x 4096 x 4096 with the largest.
+inline TileKind best_tile(const int64_t (&work)[kTileKinds], int64_t longest) {
+    constexpr double kAlone[kTileKinds] = {0.32, 0.63, 1.7}, kBusy[kTileKinds] = {0.25, 0.70, 2.4};
+    const double cus = device_cu_count();
+    TileKind best = kTiny;
+    double least = 0.0;
+    for (int k = 0; k < kTileKinds; ++k) {
+        // whole rounds of the compute units, as far as a round can be told
+        const double rounds = longest > 0 ? double(work[k]) / double(longest) / cus : 0.0;
+        const double whole = rounds <= 1.0 || k == kTiny ? rounds : ceil(rounds * (k == kLarge ? 1.0 : 2.0)) / (k == kLarge ? 1.0 : 2.0);
+        const double t = longest * fmax(whole * kBusy[k], kAlone[k]);
+        if (k == 0 || t < least) {
+            least = t;
+            best = TileKind(k);
+        }
+    }
+    return best;
+}
 
 // The workgroup's place in a grid whose consecutive places should share an
 // XCD's cache: workgroups are dispatched to the eight XCDs in turn.

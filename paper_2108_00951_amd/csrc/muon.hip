@@ -45,17 +45,16 @@ constexpr int64_t kChunkMin = 4096;        // elements
 constexpr int kPackTile = 64;
 constexpr int kSetupBlock = 256;
 
-using Small = SmallTile<Prec::kSplit>;
-using Large = LargeTile<Prec::kSplit>;
-
 enum Product { kGram, kPolynomial, kApply, kLast };
+
+static_assert(kTileSide[kTiny] == 64 && kTileSide[kSmall] == 128 && kTileSide[kLarge] == 256, "64 << kind");
 
 // Running counts over the matrices before one: where its tiles, sums and
 // operands start.
 struct Place {
     int64_t bytes;      // operands
-    int32_t sym[2];     // tiles on and below the diagonal of m x m; [small, large]
-    int32_t full[2];    // tiles of m x n
+    int32_t sym[kTileKinds];    // tiles on and below the diagonal of m x m
+    int32_t full[kTileKinds];   // tiles of m x n
     int32_t chunks;     // partial sums
     int32_t packs;      // 64 x 64 tiles of the caller's matrix
 };
@@ -100,8 +99,8 @@ __host__ __device__ inline int64_t operand_bytes(int32_t rows, int32_t cols) {
 __host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols) {
     const int32_t m = int32_t(low(rows, cols)), n = int32_t(high(rows, cols));
     p.bytes += operand_bytes(rows, cols);
-    for (int k = 0; k < 2; ++k) {
-        const int32_t t = k == 0 ? Small::kRows : Large::kRows;
+    for (int k = 0; k < kTileKinds; ++k) {
+        const int32_t t = 64 << k;
         const int32_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
         p.sym[k] += tm * (tm + 1) / 2;
         p.full[k] += tm * tn;
@@ -112,7 +111,7 @@ __host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols) {
 
 __device__ inline void add(Place &p, const Place &q) {
     p.bytes += q.bytes;
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kTileKinds; ++k) {
         p.sym[k] += q.sym[k];
         p.full[k] += q.full[k];
     }
@@ -177,7 +176,7 @@ __global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, Giv
             t.rows = given.mat[0].rows;
             t.cols = given.mat[0].cols;
             t.at.bytes = one.bytes * i;
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kTileKinds; ++k) {
                 t.at.sym[k] = one.sym[k] * i;
                 t.at.full[k] = one.full[k] * i;
             }
@@ -246,6 +245,36 @@ __device__ __forceinline__ void write_out(const Io &io, int64_t at, float o, flo
     } else {
         static_cast<float *>(io.out)[at] = o;
     }
+}
+
+// Eight of a row's values, scaled by 2^14, of which `left` are the matrix's.
+__device__ __forceinline__ void write_out8(const Io &io, int64_t at, int32_t left, const float (&v)[8], float scale) {
+    typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+    if (left < 8) {
+        for (int e = 0; e < 8; ++e)
+            if (e < left) write_out(io, at + e, __fmul_rn(v[e], kUnscale), scale);
+        return;
+    }
+    if (io.bf16) {
+        bf16x8u o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __bf16(__fmul_rn(v[e], kUnscale));
+        *reinterpret_cast<bf16x8u *>(static_cast<__bf16 *>(io.out) + at) = o;
+        return;
+    }
+    f32x4u *p = reinterpret_cast<f32x4u *>(static_cast<float *>(io.out) + at);
+    f32x4u o[2];
+    if (io.m != nullptr) {
+        o[0] = p[0];
+        o[1] = p[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float u = __fmul_rn(v[e], kUnscale);
+        o[e / 4][e % 4] = io.m != nullptr ? __fsub_rn(__fmul_rn(io.keep, o[e / 4][e % 4]), __fmul_rn(scale, u)) : u;
+    }
+    p[0] = o[0];
+    p[1] = o[1];
 }
 
 // First pass: the momentum in place, and each chunk's sum of u^2 in binary64
@@ -372,19 +401,22 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void muon_product_kernel(const M
                                                                          char *operands, int cur, float a,
                                                                          float b, float c, Io io) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
-    constexpr int kSize = Tile::kRows == Small::kRows ? 0 : 1;
+    constexpr int kKind = Tile::kRows == kTileSide[kTiny] ? kTiny : Tile::kRows == kTileSide[kSmall] ? kSmall : kLarge;
     constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
     static_assert(Tile::kRows == Tile::kCols, "tiles of the diagonal are square");
-    const int32_t place = int32_t(xcd_place(blockIdx.x, gridDim.x));
-    const int32_t mi = matrix_of(table, nmat, place, [](const Place &p) { return kSym ? p.sym[kSize] : p.full[kSize]; });
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x,
+                                 [](const Place &p) { return kSym ? p.sym[kKind] : p.full[kKind]; });
     const Mat &mat = table[mi];
     const Operands op(operands, mat);
     const int32_t m = int32_t(op.m), n = int32_t(op.n);
     // the caller's orientation in the last product: its rows are X's columns
     // where the matrix is tall
     const bool turned = kProduct == kLast && mat.rows > mat.cols;
+    // a matrix's neighbouring tiles on one XCD; every XCD has a share of every matrix
+    const Place &end = table[mi + 1].at;
+    const int32_t begin = kSym ? mat.at.sym[kKind] : mat.at.full[kKind];
+    const uint32_t t = xcd_place(blockIdx.x - begin, (kSym ? end.sym[kKind] : end.full[kKind]) - begin);
     uint32_t tr, tc;
-    const uint32_t t = uint32_t(place - (kSym ? mat.at.sym[kSize] : mat.at.full[kSize]));
     if (kSym) {
         tr = uint32_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
         while (tr * (tr + 1) / 2 > t) --tr;
@@ -424,36 +456,58 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void muon_product_kernel(const M
     char *to = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.x(cur ^ 1);
     char *to_t = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.xt(cur ^ 1);
     const int64_t to_row = kSym ? op.t_row : op.x_row;
-    const bool mirror = !kSym || tr != tc;
+    const bool mirror = kProduct != kLast && (!kSym || tr != tc);
     const float scale = step_scale(io, mat.rows, mat.cols);
     const int64_t ld_out = io.ld_out ? io.ld_out : mat.cols;
+
+    using Out = Band<Tile>;
+    Out band{reinterpret_cast<float *>(lds)};
+    each_band<Tile::kTilesM>([&](auto index) {
+        constexpr int i = decltype(index)::value;
+        f16x8 hi[Out::kUnits], lo[Out::kUnits];   // on their way while the band is put
+        if (kProduct != kGram) {
 #pragma unroll
-    for (int i = 0; i < Tile::kTilesM; ++i)
-#pragma unroll
-        for (int j = 0; j < Tile::kTilesN; ++j) {
-            const int32_t col = col0 + Tile::col_of(j);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t row4 = row0 + Tile::row_of(i, 4 * q);
-                float y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int32_t row = row4 + k;
-                    const bool in = row < rows && col < cols;
-                    float v = __fmul_rn(tile.acc[i][j][4 * q + k], f_acc);
-                    if (kProduct != kGram && in)
-                        v = __fadd_rn(__fmul_rn(f_add, load_split(add + row * add_row, col)), v);
-                    y[k] = in ? v : 0.0f;
-                    if (kProduct == kLast) {
-                        if (in) write_out(io, mat.dst + row * ld_out + col, __fmul_rn(v, kUnscale), scale);
-                    } else if (row < rows && col < padded_cols) {
-                        store_split(to + row * to_row, col, y[k]);
-                    }
+            for (int k = 0; k < Out::kUnits; ++k) {
+                const int32_t row = row0 + Out::tile_row(i, Out::row(k)), col = col0 + Out::col(k);
+                if (row < rows && col < padded_cols) {
+                    const char *p = add + row * add_row + split_offset(col);
+                    hi[k] = *reinterpret_cast<const f16x8 *>(p);
+                    lo[k] = *reinterpret_cast<const f16x8 *>(p + 64);
                 }
-                if (kProduct != kLast && mirror && col < cols && row4 < padded_rows)
-                    store_split4(to_t + col * op.t_row, row4, y);
             }
         }
+        band.template put<i>(tile);
+#pragma unroll
+        for (int k = 0; k < Out::kUnits; ++k) {
+            const int32_t row = row0 + Out::tile_row(i, Out::row(k)), col = col0 + Out::col(k);
+            float v[8];
+            band.get(k, v);
+            const bool in = row < rows && col < padded_cols;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = __fmul_rn(v[e], f_acc);
+                if (kProduct != kGram)
+                    v[e] = __fadd_rn(__fmul_rn(f_add, __fadd_rn(float(hi[k][e]), float(lo[k][e]))), v[e]);
+                if (!in || col + e >= cols) v[e] = 0.0f;   // the padding of both results
+            }
+            if (kProduct == kLast) {
+                if (in) write_out8(io, mat.dst + row * ld_out + col, cols - col, v, scale);
+            } else {
+                if (mirror) band.set(k, v);
+                if (in) store_split8(to + row * to_row, col, v);
+            }
+        }
+        if (!mirror) return;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < Out::kUnits; ++k) {
+            const int32_t row = row0 + Out::tile_row(i, Out::turned_row(k)), col = col0 + Out::turned_col(k);
+            if (row >= padded_rows || col >= cols) continue;
+            float v[8];
+            band.get_turned(k, v);
+            store_split8(to_t + col * op.t_row, row, v);
+        }
+    });
 }
 
 // ---- small matrices -------------------------------------------------------
@@ -590,17 +644,39 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
     }
 }
 
+// What the products of all matrices come to: tiles times steps, and the most
+// steps that one tile takes; X X^T, A A, B X.
+struct Cost {
+    int64_t work[3][kTileKinds], longest[3];
+};
+
+void add_cost(Cost &cost, int32_t rows, int32_t cols) {
+    const int64_t steps_n = row_bytes<Prec::kSplit>(high(rows, cols)) / kStepBytes;
+    const int64_t steps_m = row_bytes<Prec::kSplit>(low(rows, cols)) / kStepBytes;
+    Place one = {};
+    advance(one, rows, cols);
+    for (int p = 0; p < 3; ++p) {
+        const int64_t steps = p == 0 ? steps_n : steps_m;
+        for (int k = 0; k < kTileKinds; ++k) cost.work[p][k] += steps * (p < 2 ? one.sym[k] : one.full[k]);
+        if (steps > cost.longest[p]) cost.longest[p] = steps;
+    }
+}
+
 template <int kProduct>
-void launch_product(const Place &end, const Mat *table, int32_t nmat, char *operands, int cur, float a, float b,
-                    float c, const Io &io, hipStream_t stream) {
+void launch_product(const Place &end, const Cost &cost, const Mat *table, int32_t nmat, char *operands, int cur,
+                    float a, float b, float c, const Io &io, hipStream_t stream) {
     constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
-    const int32_t small = kSym ? end.sym[0] : end.full[0], large = kSym ? end.sym[1] : end.full[1];
-    if (take_large(large))
-        muon_product_kernel<kProduct, Large><<<large, Large::kThreads, 0, stream>>>(table, nmat, operands, cur, a, b,
-                                                                                    c, io);
-    else
-        muon_product_kernel<kProduct, Small><<<small, Small::kThreads, 0, stream>>>(table, nmat, operands, cur, a, b,
-                                                                                    c, io);
+    constexpr int kCost = kProduct == kGram ? 0 : kProduct == kPolynomial ? 1 : 2;
+    auto run = [&](auto tile, int kind) {
+        using Tile = decltype(tile);
+        muon_product_kernel<kProduct, Tile><<<kSym ? end.sym[kind] : end.full[kind], Tile::kThreads, 0, stream>>>(
+            table, nmat, operands, cur, a, b, c, io);
+    };
+    switch (best_tile(cost.work[kCost], cost.longest[kCost])) {
+        case kTiny: return run(TinyTile<Prec::kSplit>(), kTiny);
+        case kSmall: return run(SmallTile<Prec::kSplit>(), kSmall);
+        case kLarge: return run(LargeTile<Prec::kSplit>(), kLarge);
+    }
 }
 
 void launch_lds(int kind, int32_t count, const GivenArray &given, bool batch, int64_t stride_in, int64_t stride_out,
@@ -613,7 +689,7 @@ void launch_lds(int kind, int32_t count, const GivenArray &given, bool batch, in
 }
 
 // The launches after the table.
-hipError_t launch_steps(const Place &end, int32_t nmat, char *ws, const Io &io, int steps, const float *coeffs,
+hipError_t launch_steps(const Place &end, const Cost &cost, int32_t nmat, char *ws, const Io &io, int steps, const float *coeffs,
                         hipStream_t stream) {
     const Layout l = layout_of(nmat, end);
     const Mat *table = reinterpret_cast<const Mat *>(ws + l.table);
@@ -624,10 +700,10 @@ hipError_t launch_steps(const Place &end, int32_t nmat, char *ws, const Io &io, 
     const float a = coeffs[0], b = coeffs[1], c = coeffs[2];
     int cur = 0;
     for (int s = 0; s < steps; ++s, cur ^= 1) {
-        launch_product<kGram>(end, table, nmat, operands, cur, a, b, c, io, stream);
-        launch_product<kPolynomial>(end, table, nmat, operands, cur, a, b, c, io, stream);
-        if (s + 1 < steps) launch_product<kApply>(end, table, nmat, operands, cur, a, b, c, io, stream);
-        else launch_product<kLast>(end, table, nmat, operands, cur, a, b, c, io, stream);
+        launch_product<kGram>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
+        launch_product<kPolynomial>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
+        if (s + 1 < steps) launch_product<kApply>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
+        else launch_product<kLast>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
     }
     return hipGetLastError();
 }
@@ -642,7 +718,7 @@ bool muon_workspace_size(int32_t nmat, const int32_t *rows, const int32_t *cols,
         if (rows[i * next] == 0 || cols[i * next] == 0 || lds_class(rows[i * next], cols[i * next]) >= 0) continue;
         Place one = {};
         advance(one, rows[i * next], cols[i * next]);
-        tiles += int64_t(one.packs) + one.full[0] + one.chunks + one.sym[0];
+        tiles += int64_t(one.packs) + one.full[kTiny] + one.chunks + one.sym[kTiny];
         if (tiles > INT32_MAX) return false;
         advance(end, rows[i * next], cols[i * next]);
         ++live;
@@ -670,12 +746,16 @@ hipError_t launch_muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride
         return hipGetLastError();
     }
     Place end = {};
-    for (int32_t i = 0; i < batch; ++i) advance(end, rows, cols);
+    Cost cost = {};
+    for (int32_t i = 0; i < batch; ++i) {
+        advance(end, rows, cols);
+        add_cost(cost, rows, cols);
+    }
     char *ws = static_cast<char *>(workspace);
     const int32_t blocks = (batch + kSetupBlock) / kSetupBlock;
     muon_setup_kernel<<<blocks < 64 ? blocks : 64, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, 0,
                                                                              batch, 1, stride_g, stride_o);
-    return launch_steps(end, batch, ws, io, steps, coeffs, stream);
+    return launch_steps(end, cost, batch, ws, io, steps, coeffs, stream);
 }
 
 hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offsets, const int32_t *rows,
@@ -695,6 +775,7 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
     // the matrices of each kind, as many as a launch's arguments hold at a time
     char *ws = static_cast<char *>(workspace);
     Place end = {};
+    Cost cost = {};
     int32_t live = 0;
     for (int kind = -1; kind <= 1; ++kind) {
         GivenArray given;
@@ -708,19 +789,25 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
                                                                  count, 0, 0, 0);
             count = 0;
         };
-        for (int32_t i = 0; i < nmat; ++i) {
-            if (rows[i] == 0 || cols[i] == 0 || lds_class(rows[i], cols[i]) != kind) continue;
-            if (count == kGivenPerLaunch) flush();
-            given.mat[count++] = Given{offsets[i], rows[i], cols[i]};
-            if (kind < 0) {
-                advance(end, rows[i], cols[i]);
-                ++live;
+        // the tiles that take longest first (X X^T sums over the longer axis):
+        // by the power of two of that axis
+        for (int bit = kind < 0 ? 30 : 0; bit >= 0; --bit) {
+            for (int32_t i = 0; i < nmat; ++i) {
+                if (rows[i] == 0 || cols[i] == 0 || lds_class(rows[i], cols[i]) != kind) continue;
+                if (kind < 0 && (high(rows[i], cols[i]) >> bit) != 1) continue;
+                if (count == kGivenPerLaunch) flush();
+                given.mat[count++] = Given{offsets[i], rows[i], cols[i]};
+                if (kind < 0) {
+                    advance(end, rows[i], cols[i]);
+                    add_cost(cost, rows[i], cols[i]);
+                    ++live;
+                }
             }
         }
         flush();
     }
     if (live == 0) return hipGetLastError();
-    return launch_steps(end, live, ws, io, steps, coeffs, stream);
+    return launch_steps(end, cost, live, ws, io, steps, coeffs, stream);
 }
 
 }  // namespace efs

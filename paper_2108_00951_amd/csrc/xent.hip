@@ -293,24 +293,17 @@ __global__ __launch_bounds__(kJoinTokens *kJoinSlices) void xent_join_kernel(Xen
     loss[t] = counts ? __fsub_rn(v, target_logit[t]) : 0.0f;
 }
 
-// Four consecutive values of an operand's row, the first a multiple of four.
+// Eight consecutive values of an operand's row, the first a multiple of eight.
 template <Prec P>
-__device__ __forceinline__ void store4(char *row, int32_t c, const float (&y)[4]) {
-    if constexpr (P == Prec::kBf16) {
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        bf16x4 v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = __bf16(y[k]);
-        *reinterpret_cast<bf16x4 *>(row + int64_t(c) * 2) = v;
+__device__ __forceinline__ void store8(char *row, int32_t c, const float (&y)[8]) {
+    if constexpr (P == Prec::kSplit) {
+        store_split8(row, c, y);
     } else {
-        store_split4(row, c, y);
+        bf16x8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __bf16(y[k]);
+        *reinterpret_cast<bf16x8 *>(row + int64_t(c) * 2) = v;
     }
-}
-
-template <Prec P>
-__device__ __forceinline__ void store1(char *row, int32_t c, float y) {
-    if constexpr (P == Prec::kBf16) *reinterpret_cast<__bf16 *>(row + int64_t(c) * 2) = __bf16(y);
-    else store_split(row, c, y);
 }
 
 // Backward: g of words [v0, v0 + words), as g [token][word] and gt [word][token].
@@ -340,24 +333,41 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
 #pragma unroll
         for (int i = 0; i < Tile::kTilesM; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t v4 = row0 + Tile::row_of(i, 4 * q);
-                float y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int32_t v = v4 + k;
-                    float p = 0.0f;
-                    if (target >= 0 && v < words) {
-                        p = expf(logit<P>(tile.acc[i][j][4 * q + k], exponent) - shift);
-                        if (v0 + v == target) p = __fsub_rn(p, 1.0f);
-                        p = __fmul_rn(p, weight);
-                    }
-                    y[k] = p;
-                    if (v < words && t < tokens_end) store1<P>(gt + v * gt_row, t, p);
+            for (int e = 0; e < 16; ++e) {
+                const int32_t v = row0 + Tile::row_of(i, e);
+                float p = 0.0f;   // tokens that do not count, and the padding
+                if (target >= 0 && v < words) {
+                    p = expf(logit<P>(tile.acc[i][j][e], exponent) - shift);
+                    if (v0 + v == target) p = __fsub_rn(p, 1.0f);
+                    p = __fmul_rn(p, weight);
                 }
-                if (t < x.tokens && v4 < words_end) store4<P>(g + t * g_row, v4, y);
+                tile.acc[i][j][e] = p;
             }
     }
+    using Out = Band<Tile>;
+    Out band{reinterpret_cast<float *>(lds)};
+    each_band<Tile::kTilesM>([&](auto index) {
+        constexpr int i = decltype(index)::value;
+        band.template put<i>(tile);
+#pragma unroll
+        for (int k = 0; k < Out::kUnits; ++k) {
+            float y[8];
+            const int32_t v = row0 + Out::tile_row(i, Out::row(k)), t = col0 + Out::col(k);
+            if (v < words && t < tokens_end) {
+                band.get(k, y);
+                store8<P>(gt + v * gt_row, t, y);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < Out::kUnits; ++k) {
+            float y[8];
+            const int32_t v = row0 + Out::tile_row(i, Out::turned_row(k)), t = col0 + Out::turned_col(k);
+            if (t < x.tokens && v < words_end) {
+                band.get_turned(k, y);
+                store8<P>(g + t * g_row, v, y);
+            }
+        }
+    });
 }
 
 // dw rows [v0, v0 + words) = g^T h.
@@ -455,16 +465,16 @@ struct Plan {
 
 template <Prec P>
 Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
-    constexpr int kSmall = SmallTile<P>::kRows, kLarge = LargeTile<P>::kRows;
+    constexpr int kTile = kTileSide[kLarge];
     Plan p;
     // whole large tiles of words, as many as the pieces' bytes allow
     if (tokens == 0) tokens = 1;   // (nothing is launched that reads them)
     const int64_t word = 2 * row_bytes<P>(tokens);
-    int64_t piece = kPieceBytes / word / kLarge * kLarge;
-    if (piece < 4 * kLarge) piece = 4 * kLarge;
+    int64_t piece = kPieceBytes / word / kTile * kTile;
+    if (piece < 4 * kTile) piece = 4 * kTile;
     p.piece = int32_t(piece < vocab ? piece : vocab);
     // enough workgroups for the compute units, with eight steps each at least
-    const int64_t dh_tiles = tiles(tokens, kSmall) * tiles(hidden, kSmall);
+    const int64_t dh_tiles = tiles(tokens, kTileSide[kSmall]) * tiles(hidden, kTileSide[kSmall]);
     const int64_t steps = row_bytes<P>(p.piece) / kStepBytes;
     int64_t splits = (512 + dh_tiles - 1) / dh_tiles;
     if (splits > steps / 8) splits = steps / 8;
@@ -477,7 +487,7 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
         return here;
     };
     p.target_logit = take(int64_t(tokens) * 4);
-    p.parts = take(int64_t(tokens) * tiles(vocab, kSmall) * 8);
+    p.parts = take(int64_t(tokens) * tiles(vocab, kTileSide[kTiny]) * 8);
     p.h_along = take(tokens * row_bytes<P>(hidden));
     p.w_along = take(vocab * row_bytes<P>(hidden));
     p.forward = at;
@@ -490,13 +500,20 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     return p;
 }
 
-// Calls run(tile) with the larger kind of tile where there are enough of
-// those for the compute units.
+// Calls run(tile, workgroups) with the kind of tile that rows x cols, `times`
+// over with `steps` each, is fastest with.
 template <Prec P, class F>
-void with_tile(int64_t rows, int64_t cols, int64_t times, F run) {
-    const int64_t large = tiles(rows, LargeTile<P>::kRows) * tiles(cols, LargeTile<P>::kCols) * times;
-    if (take_large(large)) run(LargeTile<P>(), large);
-    else run(SmallTile<P>(), tiles(rows, SmallTile<P>::kRows) * tiles(cols, SmallTile<P>::kCols) * times);
+void with_tile(int64_t rows, int64_t cols, int64_t times, int64_t steps, F run) {
+    int64_t n[kTileKinds], work[kTileKinds];
+    for (int k = 0; k < kTileKinds; ++k) {
+        n[k] = tiles(rows, kTileSide[k]) * tiles(cols, kTileSide[k]) * times;
+        work[k] = n[k] * steps;
+    }
+    switch (best_tile(work, steps)) {
+        case kTiny: return run(TinyTile<P>(), n[kTiny]);
+        case kSmall: return run(SmallTile<P>(), n[kSmall]);
+        case kLarge: return run(LargeTile<P>(), n[kLarge]);
+    }
 }
 
 // Whether the tensor can be multiplied where it is: whole steps along its
@@ -543,7 +560,7 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
     Operand h, w;
     pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
     int32_t nparts = 0;
-    with_tile<P>(x.vocab, x.tokens, 1, [&](auto tile, int64_t blocks) {
+    with_tile<P>(x.vocab, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
         using Tile = decltype(tile);
         nparts = int32_t(tiles(x.vocab, Tile::kRows));
         xent_forward_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
@@ -566,13 +583,13 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
     for (int64_t v0 = 0; v0 < x.vocab; v0 += plan.piece) {
         const int32_t words = int32_t(std::min<int64_t>(plan.piece, x.vocab - v0));
         const Operand w_piece{w.base + v0 * w.stride, w.stride, words};
-        with_tile<P>(words, x.tokens, 1, [&](auto tile, int64_t blocks) {
+        with_tile<P>(words, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_grad_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(
                 x, w_piece, h, int32_t(v0), words, lse, dloss, control, ws + plan.g, ws + plan.gt);
         });
         const Operand gt{ws + plan.gt, row_bytes<P>(x.tokens), words};
-        with_tile<P>(words, x.hidden, 1, [&](auto tile, int64_t blocks) {
+        with_tile<P>(words, x.hidden, 1, row_bytes<P>(x.tokens) / kStepBytes, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dw_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, gt, ht, int32_t(v0), control,
                                                                                      dw, ld_dw);
@@ -581,7 +598,7 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
         const Operand g{ws + plan.g, row_bytes<P>(words), x.tokens};
         const Operand wt{ws + plan.w_turned + row_bytes<P>(v0), row_bytes<P>(x.vocab), x.hidden};
         const int32_t steps = int32_t(row_bytes<P>(words) / kStepBytes);
-        with_tile<P>(x.tokens, x.hidden, plan.splits, [&](auto tile, int64_t blocks) {
+        with_tile<P>(x.tokens, x.hidden, plan.splits, steps / plan.splits, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dh_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, g, wt, steps, plan.splits,
                                                                                      v0 == 0, part);
