@@ -429,8 +429,8 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
  *   dh, dw     tokens x hidden and vocab x hidden of dtype, rows ld_dh and
  *              ld_dw elements apart, overwritten (dh is 0 where a token does
  *              not count; dw is 0 with no tokens).  Must not overlap h, w or
- *              each other.  bf16: g is rounded to bf16 before it is
- *              multiplied, and so is each result; sums are fp32.
+ *              each other.  bf16: g is rounded to 11 bits before it is
+ *              multiplied, each result to bf16; sums are fp32.
  *   workspace  >= xent_workspace_bytes(.., 1). */
 efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,
                          const int64_t *target, int dtype, int32_t tokens, int32_t vocab,

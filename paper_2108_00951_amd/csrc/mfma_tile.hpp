@@ -4,6 +4,10 @@
 // Both operands are stored along the summed axis: row r of A holds A[r, 0..K).
 // A row is read in steps of 128 bytes, which hold
 //   kBf16   64 bf16 values;
+//   kHalf   64 fp16 values, scaled by a power of two;
+//   kFp32   32 fp32 values as they are, for the fp32 matrix instructions
+//           (32 x 32 x 2; 157 TFLOP/s): where a product waits for memory and a
+//           pass that splits its operands would cost more than it saves;
 //   kSplit  32 fp32 values as 32 fp16 high parts and then their 32 low parts:
 //           v s = hi + lo with s a power of two, hi = fp16(v s),
 //           lo = fp16(v s - hi).  The product is hi hi + hi lo + lo hi, three
@@ -15,7 +19,8 @@
 // A workgroup of WM x WN waves computes WM TM 32 rows by WN TN 32 columns, a
 // wave TM x TN accumulators of the 32 x 32 x 16 instruction.  Steps go from
 // memory straight to LDS (16 bytes a lane, no registers), into one of two
-// buffers while the other one is multiplied.  In LDS a row's eight 16-byte
+// buffers while the other one is multiplied (kStages buffers, where a tile is so
+// narrow that one step in flight does not cover memory's latency).  In LDS a row's eight 16-byte
 // units are permuted by the row's low bits, so that the eight rows that a
 // quarter wave reads at once lie in different banks.  A step's reads from LDS
 // are spread between the products by scheduling groups.  Measured, 8192 x 8192
@@ -40,12 +45,12 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-enum class Prec { kBf16, kSplit };
+enum class Prec { kBf16, kHalf, kFp32, kSplit };
 
 constexpr int kStepBytes = 128;   // of one row, a step of the summed axis
 // values of a row in one step
 template <Prec P>
-constexpr int kStepValues = P == Prec::kSplit ? 32 : 64;
+constexpr int kStepValues = P == Prec::kSplit || P == Prec::kFp32 ? 32 : 64;
 
 // Bytes of a row of `len` values, padded with zeros to whole steps.
 template <Prec P>
@@ -93,16 +98,17 @@ __device__ __forceinline__ void store_split8(char *row, int32_t c, const float (
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-template <Prec P, int WM, int WN, int TM, int TN>
+template <Prec P, int WM, int WN, int TM, int TN, int kStages = 2>
 struct MfmaTile {
     static constexpr int kRows = WM * TM * 32;
     static constexpr int kCols = WN * TN * 32;
     static constexpr int kThreads = WM * WN * kWave;
     static constexpr int kBufferBytes = (kRows + kCols) * kStepBytes;
-    static constexpr int kLdsBytes = 2 * kBufferBytes;
+    static constexpr int kLdsBytes = kStages * kBufferBytes;
     static constexpr int kLoadsA = kRows / 8 / (WM * WN);   // a wave's, 8 rows each
     static constexpr int kLoadsB = kCols / 8 / (WM * WN);
     static constexpr int kTilesM = TM, kTilesN = TN;
+    static constexpr int kWavesPerSimd = kThreads >= 256 ? 2 : 1;   // asked of the compiler
 
     f32x16 acc[TM][TN];
 
@@ -118,11 +124,29 @@ struct MfmaTile {
     }
 
     static __device__ __forceinline__ f32x16 mfma(f16x8 a, f16x8 b, f32x16 c) {
-        if constexpr (P == Prec::kBf16)
+        if constexpr (P == Prec::kFp32) {
+            // a lane's four values are four values of k, the same for a and b
+            const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k], y[k], c, 0, 0, 0);
+            return c;
+        } else if constexpr (P == Prec::kBf16)
             return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                            __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
         else
             return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    }
+
+    // Waits until at most `stages` steps' loads of this wave are on their way.
+    static __device__ __forceinline__ void wait_loads(int stages) {
+        constexpr int kLoads = kLoadsA + kLoadsB;
+        static_assert(kStages >= 2 && kStages <= 4 && 2 * kLoads < 64, "counts that are written out below");
+        // the count's low four bits are bits 0..3 of the operand, its high two bits 14..15
+        constexpr int k1 = 0x0f70 | (kLoads & 15) | (kLoads >> 4 << 14);
+        constexpr int k2 = 0x0f70 | (2 * kLoads & 15) | (2 * kLoads >> 4 << 14);
+        if (kStages >= 4 && stages >= 2) __builtin_amdgcn_s_waitcnt(k2);
+        else if (kStages >= 3 && stages >= 1) __builtin_amdgcn_s_waitcnt(k1);
+        else __builtin_amdgcn_s_waitcnt(0x0f70);
     }
 
     // acc = A[row0.., step0..step0+steps) B[col0.., ...)^T, in the operands'
@@ -168,18 +192,24 @@ struct MfmaTile {
         };
 
         const int ra = wave / WN * TM * 32, rb = wave % WN * TN * 32;
-        if (steps > 0) load(0, step0);
+#pragma unroll
+        for (int k = 0; k < kStages - 1; ++k)
+            if (k < steps) load(k, step0 + k);
+        int buffer = 0;
         for (int32_t s = 0; s < steps; ++s) {
-            // this step is in LDS once every wave's loads have come back, and
-            // every wave has left the other buffer
-            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+            // this step is in LDS once every wave's loads for it have come back
+            // (those of later steps may be on their way), and every wave has
+            // left the buffer that is loaded next
+            wait_loads(min(kStages - 2, steps - 1 - s));
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (s + 1 < steps) load((s + 1) & 1, step0 + s + 1);
+            if (s + kStages - 1 < steps)
+                load(buffer == 0 ? kStages - 1 : buffer - 1, step0 + s + kStages - 1);
 
-            const char *la = lds + (s & 1) * kBufferBytes + ra * kStepBytes;
-            const char *lb = lds + (s & 1) * kBufferBytes + (kRows + rb) * kStepBytes;
+            const char *la = lds + buffer * kBufferBytes + ra * kStepBytes;
+            const char *lb = lds + buffer * kBufferBytes + (kRows + rb) * kStepBytes;
+            buffer = buffer + 1 == kStages ? 0 : buffer + 1;
             auto read = [&](const char *from, int tile, int q) {
                 const int r = tile * 32 + (lane & 31);
                 return *reinterpret_cast<const f16x8 *>(from + r * kStepBytes +
@@ -208,7 +238,7 @@ struct MfmaTile {
             }
             // the first quarter's reads, then one read for every few products
             constexpr int kReads = 4 * (TM + TN), kFirst = TM + TN + 1;
-            constexpr int kAll = kProducts * TM * TN;
+            constexpr int kAll = kProducts * TM * TN * (P == Prec::kFp32 ? 4 : 1);
             constexpr int kEach = kAll * 3 / 4 / (kReads - kFirst);
             __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
 #pragma unroll
@@ -306,6 +336,11 @@ template <Prec P>
 using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
 template <Prec P>
 using TinyTile = MfmaTile<P, 2, 2, 1, 1>;
+
+// For a few tokens against many rows: 64 x 32 TN by two waves, three steps on
+// their way in each of three or two workgroups a compute unit.
+template <Prec P, int TN>
+using NarrowTile = MfmaTile<P, 2, 1, 1, TN, 4>;
 
 enum TileKind { kTiny, kSmall, kLarge };
 constexpr int kTileKinds = 3;

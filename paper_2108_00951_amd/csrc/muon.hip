@@ -397,7 +397,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, 
 //   kLast        the same, into the caller's x or out
 // `cur`: which pair of buffers holds X.
 template <int kProduct, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, 2) void muon_product_kernel(const Mat *table, int32_t nmat,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_product_kernel(const Mat *table, int32_t nmat,
                                                                          char *operands, int cur, float a,
                                                                          float b, float c, Io io) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];

@@ -18,8 +18,18 @@
 // fp32 tensors are multiplied as split values (mfma_tile.hpp), scaled by a
 // power of two that brings the tensor's largest finite magnitude to 2^14; g by
 // 2^15 without dloss_t, which goes into h^T and into the last pass over dh.
-// bf16 tensors are multiplied as they are; g is then rounded to bf16 (2^-9 of
-// itself, as the results are when they are written).
+// bf16 tensors are multiplied as they are for the logits.  For the gradients
+// they are laid out as fp16, scaled in the same way (their 8 bits fit down to
+// 2^-31 of the largest), so that g can be rounded to fp16's 11 bits.  In bf16 g
+// would lose as much as the results do when they are written, and the same
+// way for every token where dloss is one value (dh of 4096 tokens: 2.8e-3 off
+// instead of 1.7e-3, the result's own rounding).
+//
+// Few tokens (64 at most; 128 forward, fp32): reading w is what counts.  Its
+// rows are multiplied where they are, fp32 by the fp32 matrix instructions
+// without the passes that split it; a second launch joins the parts.  Backward,
+// one launch leaves g in fp32, and one takes each block of w's rows to dh's
+// partial sums and writes the same rows of dw.
 //
 // Tokens whose target is ignored count nowhere: what their rows of h hold is
 // never used.
@@ -37,8 +47,59 @@ constexpr int kPackTile = 64;
 constexpr int kCheckBlock = 1024;
 constexpr int kJoinTokens = kWave;
 constexpr int kJoinSlices = 16;
-constexpr int kGradShift = 15;          // g's scale in split form
+constexpr int kGradShift = 15;          // g's scale
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // g along both axes, one piece
+
+// The form that the gradients' products take for tensors multiplied as P.
+template <Prec P>
+constexpr Prec kGradOf = P == Prec::kBf16 ? Prec::kHalf : P;
+
+// A tensor's element as it is stored.
+template <Prec P>
+__device__ __forceinline__ float element(const void *p, int64_t i) {
+    return P == Prec::kBf16 ? float(static_cast<const __bf16 *>(p)[i]) : static_cast<const float *>(p)[i];
+}
+
+// Eight consecutive elements, at any alignment.
+template <Prec P>
+__device__ __forceinline__ void load8(const void *p, int64_t i, float (&v)[8]) {
+    if constexpr (P != Prec::kBf16) {
+        const f32x4u *q = reinterpret_cast<const f32x4u *>(static_cast<const float *>(p) + i);
+        const f32x4u a = q[0], b = q[1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = a[k];
+            v[4 + k] = b[k];
+        }
+    } else {
+        typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+        const bf16x8u a = *reinterpret_cast<const bf16x8u *>(static_cast<const __bf16 *>(p) + i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = float(a[k]);
+    }
+}
+
+// Eight consecutive values of an operand's row, the first a multiple of eight.
+template <Prec P>
+__device__ __forceinline__ void store8(char *row, int32_t c, const float (&y)[8]) {
+    if constexpr (P == Prec::kSplit) {
+        store_split8(row, c, y);
+    } else if constexpr (P == Prec::kFp32) {
+        f32x4 *p = reinterpret_cast<f32x4 *>(row + int64_t(c) * 4);
+        p[0] = f32x4{y[0], y[1], y[2], y[3]};
+        p[1] = f32x4{y[4], y[5], y[6], y[7]};
+    } else if constexpr (P == Prec::kHalf) {
+        f16x8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = _Float16(y[k]);
+        *reinterpret_cast<f16x8 *>(row + int64_t(c) * 2) = v;
+    } else {
+        bf16x8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __bf16(y[k]);
+        *reinterpret_cast<bf16x8 *>(row + int64_t(c) * 2) = v;
+    }
+}
 
 // What a call knows of its tensors.
 struct Xent {
@@ -88,36 +149,38 @@ __global__ __launch_bounds__(kCheckBlock) void xent_check_kernel(Xent x, Control
     if (threadIdx.x < 3) control->top[threadIdx.x] = 0u;
 }
 
-// Largest finite magnitudes, fp32 tensors.  Workgroups [0, w_blocks) sweep w,
-// the others h (rows that count) and, with dloss, dloss h.  A wave takes a row
-// at a time.
+// Largest finite magnitudes.  Workgroups [0, w_blocks) sweep w, the others h
+// (rows that count) and, with dloss, dloss h.  A wave takes a row at a time,
+// eight elements a lane.
+template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const float *dloss, uint32_t w_blocks,
                                                               Control *control) {
     __shared__ uint32_t s_wave[kWaves];
     const bool of_w = blockIdx.x < w_blocks;
     const uint32_t block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
     const uint32_t blocks = of_w ? w_blocks : gridDim.x - w_blocks;
-    const float *base = static_cast<const float *>(of_w ? x.w : x.h);
+    const void *base = of_w ? x.w : x.h;
     const int64_t ld = of_w ? x.ld_w : x.ld_h;
     const int32_t rows = of_w ? x.vocab : x.tokens;
     const int lane = threadIdx.x & (kWave - 1);
     uint32_t top = 0u, weighted = 0u;
     for (int64_t r = int64_t(block) * kWaves + threadIdx.x / kWave; r < rows; r += int64_t(blocks) * kWaves) {
         if (!of_w && target_of(x, int32_t(r)) < 0) continue;
-        const float *row = base + r * ld;
         const float f = !of_w && dloss != nullptr ? dloss[r] : 0.0f;
-        int32_t c = lane * 4;
-        for (; c + 4 <= x.hidden; c += kWave * 4) {
-            const f32x4u v = *reinterpret_cast<const f32x4u *>(row + c);
+        int32_t c = lane * 8;
+        for (; c + 8 <= x.hidden; c += kWave * 8) {
+            float v[8];
+            load8<P>(base, r * ld + c, v);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) {
                 top = max(top, finite_bits(v[k]));
                 weighted = max(weighted, finite_bits(__fmul_rn(f, v[k])));
             }
         }
-        for (; c < x.hidden; ++c) {
-            top = max(top, finite_bits(row[c]));
-            weighted = max(weighted, finite_bits(__fmul_rn(f, row[c])));
+        for (; c < x.hidden; ++c) {   // the row's last elements, of one lane
+            const float v = element<P>(base, r * ld + c);
+            top = max(top, finite_bits(v));
+            weighted = max(weighted, finite_bits(__fmul_rn(f, v)));
         }
     }
     top = block_max(top, s_wave);
@@ -129,12 +192,13 @@ __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const floa
     }
 }
 
-// h or w as operands: `along` its rows, and `turned`, a row for each of its
-// columns; either may be null.  Rows of h that do not count are zeros.  In
-// split form the turned h holds dloss h.
+// h or w as operands: `along` its rows (for the logits), and `turned`, a row
+// for each of its columns (for the gradients); either may be null.  Rows of h
+// that do not count are zeros.  The turned h holds dloss h.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w, const float *dloss, char *along,
                                                                char *turned, const Control *control) {
+    constexpr Prec G = kGradOf<P>;
     __shared__ float tile[kPackTile][kPackTile + 1];
     __shared__ float s_weight[kPackTile];
     __shared__ bool s_counts[kPackTile];
@@ -146,55 +210,48 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
     if (tid < kPackTile) {
         const int32_t r = r0 + tid;
         s_counts[tid] = r < rows && (of_w || target_of(x, r) >= 0);
-        s_weight[tid] = P == Prec::kSplit && !of_w && dloss != nullptr && s_counts[tid] ? dloss[r] : 1.0f;
+        s_weight[tid] = !of_w && dloss != nullptr && s_counts[tid] ? dloss[r] : 1.0f;
     }
     __syncthreads();
-    for (int i = tid; i < kPackTile * kPackTile; i += kPackBlock) {
-        const int r = i / kPackTile, c = i % kPackTile;
-        float v = 0.0f;
-        if (s_counts[r] && c0 + c < cols) {
+    const void *base = of_w ? x.w : x.h;
+    for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
+        const int r = i / 8, c = i % 8 * 8;
+        float v[8] = {};
+        if (s_counts[r]) {
             const int64_t at = int64_t(r0 + r) * ld + c0 + c;
-            v = P == Prec::kBf16 ? float(static_cast<const __bf16 *>(of_w ? x.w : x.h)[at])
-                                 : static_cast<const float *>(of_w ? x.w : x.h)[at];
+            if (c0 + c + 8 <= cols) load8<P>(base, at, v);
+            else
+                for (int k = 0; k < 8; ++k)
+                    if (c0 + c + k < cols) v[k] = element<P>(base, at + k);
         }
-        tile[r][c] = v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tile[r][c + k] = v[k];
     }
     __syncthreads();
-    const int e_along = P == Prec::kSplit ? scale_exponent(control->top[of_w ? kTopW : kTopH]) : 0;
-    const int e_turned = P == Prec::kSplit ? scale_exponent(control->top[of_w ? kTopW : kTopWeighted]) : 0;
-    constexpr int kPad = kStepValues<P>;
-#pragma unroll
-    for (int turn = 0; turn < 2; ++turn) {
-        char *base = turn ? turned : along;
-        if (base == nullptr) continue;
-        const int64_t stride = row_bytes<P>(turn ? rows : cols);
-        const int32_t row_first = turn ? c0 : r0, col_first = turn ? r0 : c0;
-        const int32_t row_end = turn ? cols : rows;
-        const int32_t col_end = ((turn ? rows : cols) + kPad - 1) / kPad * kPad;
+    if (along != nullptr) {
+        const int exponent = P == Prec::kSplit ? scale_exponent(control->top[of_w ? kTopW : kTopH]) : 0;
+        const int64_t stride = row_bytes<P>(cols);
+        const int32_t end = int32_t(stride / kStepBytes) * kStepValues<P>;
         for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
-            const int r = turn ? i % kPackTile : i / 8, c = (turn ? i / kPackTile : i % 8) * 8;
-            if (row_first + r >= row_end || col_first + c >= col_end) continue;
-            char *row = base + int64_t(row_first + r) * stride;
-            if constexpr (P == Prec::kBf16) {
-                bf16x8 v;
+            const int r = i / 8, c = i % 8 * 8;
+            if (r0 + r >= rows || c0 + c >= end) continue;
+            float v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = __bf16(turn ? tile[c + k][r] : tile[r][c + k]);
-                *reinterpret_cast<bf16x8 *>(row + int64_t(col_first + c) * 2) = v;
-            } else {
-                f16x8 hi, lo;
+            for (int k = 0; k < 8; ++k) v[k] = P == Prec::kSplit ? ldexpf(tile[r][c + k], exponent) : tile[r][c + k];
+            store8<P>(along + int64_t(r0 + r) * stride, c0 + c, v);
+        }
+    }
+    if (turned != nullptr) {
+        const int exponent = scale_exponent(control->top[of_w ? kTopW : kTopWeighted]);
+        const int64_t stride = row_bytes<G>(rows);
+        const int32_t end = int32_t(stride / kStepBytes) * kStepValues<G>;
+        for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
+            const int r = i / 8, c = i % 8 * 8;   // of the turned tile
+            if (c0 + r >= cols || r0 + c >= end) continue;
+            float v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float v = turn ? tile[c + k][r] : tile[r][c + k];
-                    if (turn) v = __fmul_rn(s_weight[c + k], v);
-                    _Float16 a, b;
-                    split_value(ldexpf(v, turn ? e_turned : e_along), a, b);
-                    hi[k] = a;
-                    lo[k] = b;
-                }
-                char *p = row + split_offset(col_first + c);
-                *reinterpret_cast<f16x8 *>(p) = hi;
-                *reinterpret_cast<f16x8 *>(p + 64) = lo;
-            }
+            for (int k = 0; k < 8; ++k) v[k] = ldexpf(__fmul_rn(s_weight[c + k], tile[c + k][r]), exponent);
+            store8<G>(turned + int64_t(c0 + r) * stride, r0 + c, v);
         }
     }
 }
@@ -223,7 +280,7 @@ __device__ __forceinline__ float logit(float acc, int exponent) {
 
 // Forward: parts[tile row][token], and the targets' logits.
 template <Prec P, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, 2) void xent_forward_kernel(Xent x, Operand w, Operand h,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forward_kernel(Xent x, Operand w, Operand h,
                                                                          const Control *control, Part *parts,
                                                                          float *target_logit) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
@@ -293,25 +350,41 @@ __global__ __launch_bounds__(kJoinTokens *kJoinSlices) void xent_join_kernel(Xen
     loss[t] = counts ? __fsub_rn(v, target_logit[t]) : 0.0f;
 }
 
-// Eight consecutive values of an operand's row, the first a multiple of eight.
-template <Prec P>
-__device__ __forceinline__ void store8(char *row, int32_t c, const float (&y)[8]) {
-    if constexpr (P == Prec::kSplit) {
-        store_split8(row, c, y);
-    } else {
-        bf16x8 v;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = __bf16(y[k]);
-        *reinterpret_cast<bf16x8 *>(row + int64_t(c) * 2) = v;
+// The same for few tokens: a workgroup each; the first also sets the status word.
+__global__ __launch_bounds__(kPackBlock) void xent_join_few_kernel(Xent x, const Part *parts, int32_t nparts,
+                                                                   const float *target_logit, float *loss,
+                                                                   float *lse, Control *control) {
+    __shared__ Part s_part[kWaves];
+    __shared__ uint32_t s_wave[kWaves];
+    const int32_t t = int32_t(blockIdx.x);
+    if (t == 0) {
+        uint32_t bad = 0u;
+        if (threadIdx.x < x.tokens) {
+            const int64_t v = x.target[threadIdx.x];
+            bad = v != x.ignore && (v < 0 || v >= x.vocab) ? kXentBadTarget : 0u;
+        }
+        bad = block_max(bad, s_wave);
+        if (threadIdx.x == 0) control->status = bad;
     }
+    Part p = {-INFINITY, 0.0f};
+    for (int32_t i = threadIdx.x; i < nparts; i += kPackBlock) p = join(p, parts[int64_t(i) * x.tokens + t]);
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) p = join(p, Part{__shfl_xor(p.top, off), __shfl_xor(p.sum, off)});
+    if ((threadIdx.x & (kWave - 1)) == 0) s_part[threadIdx.x / kWave] = p;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < kWaves; ++w) p = join(p, s_part[w]);
+    const bool counts = target_of(x, t) >= 0;
+    const float v = __fadd_rn(p.top, logf(p.sum));
+    lse[t] = counts ? v : 0.0f;
+    loss[t] = counts ? __fsub_rn(v, target_logit[t]) : 0.0f;
 }
 
 // Backward: g of words [v0, v0 + words), as g [token][word] and gt [word][token].
 template <Prec P, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Operand w, Operand h, int32_t v0,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad_kernel(Xent x, Operand w, Operand h, int32_t v0,
                                                                       int32_t words, const float *lse,
-                                                                      const float *dloss, const Control *control,
-                                                                      char *g, char *gt) {
+                                                                      const Control *control, char *g, char *gt) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (words + Tile::kRows - 1) / Tile::kRows, tt = (x.tokens + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
@@ -320,16 +393,15 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
     Tile tile;
     tile.run(w, h, row0, col0, 0, int32_t(row_bytes<P>(x.hidden) / kStepBytes), lds);
     const int exponent = logit_exponent<P>(control);
-    const int64_t g_row = row_bytes<P>(words), gt_row = row_bytes<P>(x.tokens);
-    const int32_t words_end = int32_t(g_row / kStepBytes) * kStepValues<P>;
-    const int32_t tokens_end = int32_t(gt_row / kStepBytes) * kStepValues<P>;
+    constexpr Prec G = kGradOf<P>;
+    const int64_t g_row = row_bytes<G>(words), gt_row = row_bytes<G>(x.tokens);
+    const int32_t words_end = int32_t(g_row / kStepBytes) * kStepValues<G>;
+    const int32_t tokens_end = int32_t(gt_row / kStepBytes) * kStepValues<G>;
 #pragma unroll
     for (int j = 0; j < Tile::kTilesN; ++j) {
         const int32_t t = col0 + Tile::col_of(j);
         const int32_t target = t < x.tokens ? target_of(x, t) : -1;
         const float shift = target >= 0 ? lse[t] : 0.0f;
-        // bf16: dloss in g; split: in h^T and the last pass over dh
-        const float weight = P == Prec::kSplit ? float(1 << kGradShift) : target >= 0 ? dloss[t] : 0.0f;
 #pragma unroll
         for (int i = 0; i < Tile::kTilesM; ++i)
 #pragma unroll
@@ -339,7 +411,7 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
                 if (target >= 0 && v < words) {
                     p = expf(logit<P>(tile.acc[i][j][e], exponent) - shift);
                     if (v0 + v == target) p = __fsub_rn(p, 1.0f);
-                    p = __fmul_rn(p, weight);
+                    p = __fmul_rn(p, float(1 << kGradShift));   // dloss: in h^T, and in the last pass over dh
                 }
                 tile.acc[i][j][e] = p;
             }
@@ -355,7 +427,7 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
             const int32_t v = row0 + Out::tile_row(i, Out::row(k)), t = col0 + Out::col(k);
             if (v < words && t < tokens_end) {
                 band.get(k, y);
-                store8<P>(gt + v * gt_row, t, y);
+                store8<G>(gt + v * gt_row, t, y);
             }
         }
 #pragma unroll
@@ -364,7 +436,7 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
             const int32_t v = row0 + Out::tile_row(i, Out::turned_row(k)), t = col0 + Out::turned_col(k);
             if (t < x.tokens && v < words_end) {
                 band.get_turned(k, y);
-                store8<P>(g + t * g_row, v, y);
+                store8<G>(g + t * g_row, v, y);
             }
         }
     });
@@ -372,7 +444,7 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_grad_kernel(Xent x, Op
 
 // dw rows [v0, v0 + words) = g^T h.
 template <Prec P, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, 2) void xent_dw_kernel(Xent x, Operand gt, Operand ht, int32_t v0,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dw_kernel(Xent x, Operand gt, Operand ht, int32_t v0,
                                                                     const Control *control, void *dw, int64_t ld) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (gt.rows + Tile::kRows - 1) / Tile::kRows, th = (x.hidden + Tile::kCols - 1) / Tile::kCols;
@@ -380,8 +452,8 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_dw_kernel(Xent x, Oper
     banded(xcd_place(blockIdx.x, gridDim.x), tv, th, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
     Tile tile;
-    tile.run(gt, ht, row0, col0, 0, int32_t(row_bytes<P>(x.tokens) / kStepBytes), lds);
-    const int exponent = P == Prec::kSplit ? -(kGradShift + scale_exponent(control->top[kTopWeighted])) : 0;
+    tile.run(gt, ht, row0, col0, 0, int32_t(row_bytes<kGradOf<P>>(x.tokens) / kStepBytes), lds);
+    const int exponent = -(kGradShift + scale_exponent(control->top[kTopWeighted]));
 #pragma unroll
     for (int i = 0; i < Tile::kTilesM; ++i)
 #pragma unroll
@@ -391,15 +463,16 @@ __global__ __launch_bounds__(Tile::kThreads, 2) void xent_dw_kernel(Xent x, Oper
                 const int32_t v = row0 + Tile::row_of(i, e), k = col0 + Tile::col_of(j);
                 if (v >= gt.rows || k >= x.hidden) continue;
                 const int64_t at = (int64_t(v0) + v) * ld + k;
-                if constexpr (P == Prec::kSplit) static_cast<float *>(dw)[at] = ldexpf(tile.acc[i][j][e], exponent);
-                else static_cast<__bf16 *>(dw)[at] = __bf16(tile.acc[i][j][e]);
+                const float y = ldexpf(tile.acc[i][j][e], exponent);
+                if constexpr (P == Prec::kSplit) static_cast<float *>(dw)[at] = y;
+                else static_cast<__bf16 *>(dw)[at] = __bf16(y);
             }
 }
 
 // Partial sums of dh: split s adds its share of the piece's words to
 // part[s][token][hidden] (or starts it, with the first piece).
 template <Prec P, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, 2) void xent_dh_kernel(Xent x, Operand g, Operand wt, int32_t steps,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dh_kernel(Xent x, Operand g, Operand wt, int32_t steps,
                                                                     int32_t splits, bool first, float *part) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tt = (x.tokens + Tile::kRows - 1) / Tile::kRows, th = (x.hidden + Tile::kCols - 1) / Tile::kCols;
@@ -430,19 +503,223 @@ template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const float *part, int32_t splits,
                                                                   const float *dloss, const Control *control,
                                                                   void *dh, int64_t ld) {
-    const int exponent = P == Prec::kSplit ? -(kGradShift + scale_exponent(control->top[kTopW])) : 0;
+    const int exponent = -(kGradShift + scale_exponent(control->top[kTopW]));
     const int64_t size = int64_t(x.tokens) * x.hidden;
     for (int64_t i = int64_t(blockIdx.x) * kPackBlock + threadIdx.x; i < size; i += int64_t(gridDim.x) * kPackBlock) {
         const int32_t t = int32_t(i / x.hidden), k = int32_t(i - int64_t(t) * x.hidden);
         float v = 0.0f;
         if (target_of(x, t) >= 0) {
             for (int32_t s = 0; s < splits; ++s) v = __fadd_rn(v, part[s * size + i]);
-            if (P == Prec::kSplit) v = __fmul_rn(ldexpf(v, exponent), dloss[t]);
+            v = __fmul_rn(ldexpf(v, exponent), dloss[t]);
         }
         const int64_t at = t * ld + k;
         if constexpr (P == Prec::kSplit) static_cast<float *>(dh)[at] = v;
         else static_cast<__bf16 *>(dh)[at] = __bf16(v);
     }
+}
+
+// Few tokens: g as fp32 [token][word], rows `words_end` long (a multiple of 64;
+// zeros past the vocabulary and for tokens that do not count).
+template <Prec P, class Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_few_grad_kernel(Xent x, Operand w, Operand h, const float *lse,
+                                                                       const float *dloss, float *g,
+                                                                       int64_t words_end) {
+    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    const int32_t row0 = int32_t(blockIdx.x) * Tile::kRows;
+    Tile tile;
+    tile.run(w, h, row0, 0, 0, int32_t(row_bytes<P>(x.hidden) / kStepBytes), lds);
+#pragma unroll
+    for (int j = 0; j < Tile::kTilesN; ++j) {
+        const int32_t t = Tile::col_of(j);
+        if (t >= x.tokens) continue;
+        const int32_t target = target_of(x, t);
+        const float shift = target >= 0 ? lse[t] : 0.0f, weight = target >= 0 ? dloss[t] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < Tile::kTilesM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t v4 = row0 + Tile::row_of(i, 4 * q);
+                f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (target >= 0) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float p = expf(tile.acc[i][j][4 * q + k] - shift);
+                        if (v4 + k == target) p = __fsub_rn(p, 1.0f);
+                        y[k] = v4 + k < x.vocab ? __fmul_rn(p, weight) : 0.0f;
+                    }
+                }
+                *reinterpret_cast<f32x4 *>(g + t * words_end + v4) = y;
+            }
+    }
+}
+
+// Few tokens: dw, and dh's partial sums.  A workgroup takes 256 values of the
+// hidden axis (a wave 64, a lane four neighbours: column c of product j is
+// value 4 c + j) and every splits-th block of 32 words.  Both products run on
+// the 16 x 16 x 4 fp32 instruction, whose operands are one value a lane, so
+// that w's rows serve as they come from memory:
+//   dw[word][value]  = sum over tokens  g[word][token] h[token][value]
+//   dh[token][value] += sum over words  g[token][word] w[word][value]
+// with dh and h in registers throughout.  16 kTok tokens at most.
+constexpr int kFewHidden = 256, kFewWords = 32;
+
+template <Prec P, int kTok>
+__global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, const float *g, int64_t words_end,
+                                                                       int32_t splits, void *dw, int64_t ld_dw,
+                                                                       float *part) {
+    constexpr int kTokens = 16 * kTok, kStride = kFewWords + 1;
+    __shared__ float s_g[2][kTokens * kStride];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int col = lane & 15, four = lane >> 4;
+    const int32_t split = int32_t(blockIdx.x) % splits;
+    const int32_t k0 = int32_t(blockIdx.x) / splits * kFewHidden + wave * 64 + col * 4;   // this lane's values
+    const int32_t left = min(4, x.hidden - k0);   // of which exist
+
+    auto load4 = [&](const void *base, int64_t at, bool there) {
+        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (!there) return v;
+        if (left == 4) {
+            if constexpr (P == Prec::kBf16) {
+                typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+                const bf16x4u b = *reinterpret_cast<const bf16x4u *>(static_cast<const __bf16 *>(base) + at);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = float(b[k]);
+            } else {
+                v = *reinterpret_cast<const f32x4u *>(static_cast<const float *>(base) + at);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < left) v[k] = element<P>(base, at + k);
+        }
+        return v;
+    };
+    // g's block in LDS as [token][word]
+    constexpr int kLoads = kTokens * kFewWords / kPackBlock;
+    float next[kLoads];
+    auto fetch = [&](int32_t block) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int t = (i * kPackBlock + tid) / kFewWords, v = (i * kPackBlock + tid) % kFewWords;
+            next[i] = t < x.tokens ? g[t * words_end + int64_t(block) * kFewWords + v] : 0.0f;
+        }
+    };
+
+    f32x4 h[4 * kTok], dh[kTok][4];
+#pragma unroll
+    for (int s = 0; s < 4 * kTok; ++s) {
+        const int32_t t = 4 * s + four;
+        h[s] = load4(x.h, t * x.ld_h + k0, t < x.tokens && left > 0 && target_of(x, t) >= 0);
+    }
+#pragma unroll
+    for (int t = 0; t < kTok; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dh[t][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const int32_t blocks = (x.vocab + kFewWords - 1) / kFewWords;
+    int turn = 0;
+    if (split < blocks) fetch(split);
+    for (int32_t block = split; block < blocks; block += splits, turn ^= 1) {
+        float *sg = s_g[turn];   // the other one may still be read
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int t = (i * kPackBlock + tid) / kFewWords, v = (i * kPackBlock + tid) % kFewWords;
+            sg[t * kStride + v] = next[i];
+        }
+        const int32_t v0 = block * kFewWords;
+        f32x4 w[kFewWords / 4];
+#pragma unroll
+        for (int s = 0; s < kFewWords / 4; ++s) {
+            const int32_t v = v0 + 4 * s + four;
+            w[s] = load4(x.w, v * x.ld_w + k0, v < x.vocab && left > 0);
+        }
+        if (block + splits < blocks) fetch(block + splits);
+        __syncthreads();
+        // dw: two rows of 16 words, four columns of 16 values
+#pragma unroll
+        for (int r = 0; r < kFewWords / 16; ++r) {
+            f32x4 acc[4] = {};
+#pragma unroll
+            for (int s = 0; s < 4 * kTok; ++s) {
+                const float a = sg[(4 * s + four) * kStride + r * 16 + col];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, h[s][j], acc[j], 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int32_t v = v0 + r * 16 + four * 4 + e;
+                if (v >= x.vocab || left <= 0) continue;
+                const int64_t at = v * ld_dw + k0;
+                if constexpr (P == Prec::kBf16) {
+                    typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+                    __bf16 *p = static_cast<__bf16 *>(dw) + at;
+                    const bf16x4u y = {__bf16(acc[0][e]), __bf16(acc[1][e]), __bf16(acc[2][e]), __bf16(acc[3][e])};
+                    if (left == 4) *reinterpret_cast<bf16x4u *>(p) = y;
+                    else
+                        for (int j = 0; j < left; ++j) p[j] = __bf16(j == 0 ? acc[0][e] : j == 1 ? acc[1][e] : acc[2][e]);
+                } else {
+                    float *p = static_cast<float *>(dw) + at;
+                    if (left == 4) *reinterpret_cast<f32x4u *>(p) = f32x4u{acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+                    else
+                        for (int j = 0; j < left; ++j) p[j] = j == 0 ? acc[0][e] : j == 1 ? acc[1][e] : acc[2][e];
+                }
+            }
+        }
+        // dh
+#pragma unroll
+        for (int s = 0; s < kFewWords / 4; ++s)
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) {
+                const float a = sg[(t * 16 + col) * kStride + 4 * s + four];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    dh[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[s][j], dh[t][j], 0, 0, 0);
+            }
+    }
+    float *to = part + int64_t(split) * x.tokens * x.hidden;
+#pragma unroll
+    for (int t = 0; t < kTok; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int32_t token = t * 16 + four * 4 + e;
+            if (token >= x.tokens) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < left) to[int64_t(token) * x.hidden + k0 + j] = dh[t][j][e];
+        }
+}
+
+// dh of few tokens from its partial sums.
+template <Prec P>
+__global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const float *part, int32_t splits, void *dh,
+                                                                   int64_t ld, Control *control) {
+    __shared__ float s_sum[kWaves][kWave];
+    if (blockIdx.x == 0 && threadIdx.x < kWave) {   // the status word: 64 tokens at most
+        bool bad = false;
+        if (threadIdx.x < x.tokens) {
+            const int64_t v = x.target[threadIdx.x];
+            bad = v != x.ignore && (v < 0 || v >= x.vocab);
+        }
+        bad = __any(bad);
+        if (threadIdx.x == 0) control->status = bad ? kXentBadTarget : 0u;
+    }
+    // a wave takes every fourth split of 64 values
+    const int64_t size = int64_t(x.tokens) * x.hidden;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t i = int64_t(blockIdx.x) * kWave + lane;
+    float v = 0.0f;
+    if (i < size)
+        for (int32_t s = wave; s < splits; s += kWaves) v = __fadd_rn(v, part[s * size + i]);
+    s_sum[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || i >= size) return;
+    for (int k = 1; k < kWaves; ++k) v = __fadd_rn(v, s_sum[k][lane]);
+    const int32_t t = int32_t(i / x.hidden);
+    const int64_t at = t * ld + (i - int64_t(t) * x.hidden);
+    if (target_of(x, t) < 0) v = 0.0f;
+    if constexpr (P == Prec::kBf16) static_cast<__bf16 *>(dh)[at] = __bf16(v);
+    else static_cast<float *>(dh)[at] = v;
 }
 
 // dw of no tokens.
@@ -456,26 +733,36 @@ __global__ __launch_bounds__(kPackBlock) void xent_zero_kernel(T *dw, int64_t ld
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 
+// Few tokens: reading w takes longer than multiplying it.
+constexpr int32_t kFewTokens = 64;
+template <Prec P>
+constexpr int32_t kFewForward = P == Prec::kFp32 ? 128 : 64;
+
 // How a backward call is cut, and where everything is in the workspace.
 struct Plan {
     int32_t piece;    // words
     int32_t splits;   // of a piece, for dh
-    int64_t target_logit, parts, h_along, w_along, h_turned, w_turned, g, gt, dh, forward, total;
+    int32_t few_splits;
+    int64_t target_logit, parts, h_along, w_along, forward;
+    int64_t h_turned, w_turned, g, gt, dh;   // or, of few tokens,
+    int64_t few_g, few_dh;
+    int64_t total;
 };
 
 template <Prec P>
 Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
+    constexpr Prec G = kGradOf<P>;
     constexpr int kTile = kTileSide[kLarge];
-    Plan p;
+    Plan p = {};
     // whole large tiles of words, as many as the pieces' bytes allow
     if (tokens == 0) tokens = 1;   // (nothing is launched that reads them)
-    const int64_t word = 2 * row_bytes<P>(tokens);
+    const int64_t word = 2 * row_bytes<G>(tokens);
     int64_t piece = kPieceBytes / word / kTile * kTile;
     if (piece < 4 * kTile) piece = 4 * kTile;
     p.piece = int32_t(piece < vocab ? piece : vocab);
     // enough workgroups for the compute units, with eight steps each at least
     const int64_t dh_tiles = tiles(tokens, kTileSide[kSmall]) * tiles(hidden, kTileSide[kSmall]);
-    const int64_t steps = row_bytes<P>(p.piece) / kStepBytes;
+    const int64_t steps = row_bytes<G>(p.piece) / kStepBytes;
     int64_t splits = (512 + dh_tiles - 1) / dh_tiles;
     if (splits > steps / 8) splits = steps / 8;
     p.splits = int32_t(splits < 1 ? 1 : splits);
@@ -491,10 +778,21 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     p.h_along = take(tokens * row_bytes<P>(hidden));
     p.w_along = take(vocab * row_bytes<P>(hidden));
     p.forward = at;
-    p.h_turned = take(hidden * row_bytes<P>(tokens));
-    p.w_turned = take(hidden * row_bytes<P>(vocab));
-    p.g = take(tokens * row_bytes<P>(p.piece));
-    p.gt = take(p.piece * row_bytes<P>(tokens));
+    if (tokens <= kFewTokens) {
+        // two rounds of the three workgroups that a compute unit holds, with
+        // eight blocks of words each at least
+        int64_t n = tiles(1536, int(tiles(hidden, kFewHidden)));
+        n = std::min(n, tiles(vocab, kFewWords * 8));
+        p.few_splits = int32_t(n);
+        p.few_g = take(tokens * tiles(vocab, 64) * 64 * 4);
+        p.few_dh = take(n * tokens * hidden * 4);
+        p.total = at;
+        return p;
+    }
+    p.h_turned = take(hidden * row_bytes<G>(tokens));
+    p.w_turned = take(hidden * row_bytes<G>(vocab));
+    p.g = take(tokens * row_bytes<G>(p.piece));
+    p.gt = take(p.piece * row_bytes<G>(tokens));
     p.dh = take(int64_t(p.splits) * tokens * hidden * 4);
     p.total = at;
     return p;
@@ -520,35 +818,93 @@ void with_tile(int64_t rows, int64_t cols, int64_t times, int64_t steps, F run) 
 // rows, 16-byte aligned.
 template <Prec P>
 bool direct(const void *p, int64_t ld, int32_t hidden) {
-    return P == Prec::kBf16 && hidden % kStepValues<P> == 0 && ld % 8 == 0 &&
+    return P != Prec::kSplit && hidden % kStepValues<P> == 0 && ld % (P == Prec::kFp32 ? 4 : 8) == 0 &&
            reinterpret_cast<uintptr_t>(p) % 16 == 0;
 }
 
-// The operands of the logits, packed where they have to be.
+// The operands of the logits, laid out where they have to be; with `gradient`
+// those of the gradients' products too.
 template <Prec P>
 void pack_operands(const Xent &x, const float *dloss, bool gradient, const Plan &plan, char *ws, Operand *h,
                    Operand *w, hipStream_t stream) {
     Control *control = reinterpret_cast<Control *>(ws);
+    constexpr int kSize = P == Prec::kBf16 ? 2 : 4;
+    const int64_t row = row_bytes<P>(x.hidden);
+    auto pack = [&](bool of_w, const void *p, int64_t ld, int32_t rows, int64_t along, int64_t turned) {
+        const bool in_place = direct<P>(p, ld, x.hidden);
+        if (!in_place || gradient) {
+            const int64_t blocks = tiles(rows, kPackTile) * tiles(x.hidden, kPackTile);
+            xent_pack_kernel<P><<<uint32_t(blocks), kPackBlock, 0, stream>>>(
+                x, of_w, dloss, in_place ? nullptr : ws + along, gradient ? ws + turned : nullptr, control);
+        }
+        return in_place ? Operand{static_cast<const char *>(p), ld * kSize, rows} : Operand{ws + along, row, rows};
+    };
+    *h = pack(false, x.h, x.ld_h, x.tokens, plan.h_along, plan.h_turned);
+    *w = pack(true, x.w, x.ld_w, x.vocab, plan.w_along, plan.w_turned);
+}
+
+// The status word, and the largest magnitudes where a scale needs them.
+template <Prec P>
+void check_and_scale(const Xent &x, const float *dloss, bool gradient, char *ws, hipStream_t stream) {
+    Control *control = reinterpret_cast<Control *>(ws);
     xent_check_kernel<<<1, kCheckBlock, 0, stream>>>(x, control);
-    if (P == Prec::kSplit) {
+    if (P == Prec::kSplit || gradient) {
         const uint32_t w_blocks = uint32_t(std::min<int64_t>(tiles(x.vocab, kWaves), device_cu_count() * 8));
         const uint32_t h_blocks = uint32_t(std::min<int64_t>(tiles(x.tokens, kWaves), device_cu_count() * 2));
-        xent_top_kernel<<<w_blocks + h_blocks, kPackBlock, 0, stream>>>(x, dloss, w_blocks, control);
+        xent_top_kernel<P><<<w_blocks + h_blocks, kPackBlock, 0, stream>>>(x, dloss, w_blocks, control);
     }
-    const bool direct_h = direct<P>(x.h, x.ld_h, x.hidden), direct_w = direct<P>(x.w, x.ld_w, x.hidden);
-    auto pack = [&](bool of_w, bool in_place, int64_t along, int64_t turned) {
-        if (in_place && !gradient) return;
-        const int64_t blocks = tiles(of_w ? x.vocab : x.tokens, kPackTile) * tiles(x.hidden, kPackTile);
-        xent_pack_kernel<P><<<uint32_t(blocks), kPackBlock, 0, stream>>>(
-            x, of_w, dloss, in_place ? nullptr : ws + along, gradient ? ws + turned : nullptr, control);
+}
+
+template <Prec P, class F>
+void with_narrow_tile(int32_t tokens, F run) {
+    if (tokens <= 32) run(NarrowTile<P, 1>());
+    else if (tokens <= 64) run(NarrowTile<P, 2>());
+    else run(NarrowTile<P, 4>());
+}
+
+template <Prec P>
+hipError_t forward_few(const Xent &x, const Plan &plan, float *loss, float *lse, char *ws, hipStream_t stream) {
+    Control *control = reinterpret_cast<Control *>(ws);
+    Part *parts = reinterpret_cast<Part *>(ws + plan.parts);
+    float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
+    Operand h, w;
+    pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
+    int32_t nparts = 0;
+    with_narrow_tile<P>(x.tokens, [&](auto tile) {
+        using Tile = decltype(tile);
+        nparts = int32_t(tiles(x.vocab, Tile::kRows));
+        xent_forward_kernel<P, Tile><<<uint32_t(nparts), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
+                                                                                      target_logit);
+    });
+    xent_join_few_kernel<<<uint32_t(x.tokens), kPackBlock, 0, stream>>>(x, parts, nparts, target_logit, loss, lse,
+                                                                        control);
+    return hipGetLastError();
+}
+
+template <Prec P>
+hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const float *dloss, void *dh, int64_t ld_dh,
+                        void *dw, int64_t ld_dw, char *ws, hipStream_t stream) {
+    Operand h, w;
+    pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
+    float *g = reinterpret_cast<float *>(ws + plan.few_g), *part = reinterpret_cast<float *>(ws + plan.few_dh);
+    const int64_t words_end = tiles(x.vocab, 64) * 64;
+    with_narrow_tile<P>(x.tokens, [&](auto tile) {
+        using Tile = decltype(tile);
+        static_assert(Tile::kRows == 64, "g's rows end with the tiles");
+        if constexpr (Tile::kCols <= kFewTokens)
+            xent_few_grad_kernel<P, Tile><<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(
+                x, w, h, lse, dloss, g, words_end);
+    });
+    const uint32_t blocks = uint32_t(tiles(x.hidden, kFewHidden) * plan.few_splits);
+    auto run = [&](auto kernel) {
+        kernel<<<blocks, kPackBlock, 0, stream>>>(x, g, words_end, plan.few_splits, dw, ld_dw, part);
     };
-    pack(false, direct_h, plan.h_along, plan.h_turned);
-    pack(true, direct_w, plan.w_along, plan.w_turned);
-    const int64_t row = row_bytes<P>(x.hidden);
-    *h = direct_h ? Operand{static_cast<const char *>(x.h), x.ld_h * 2, x.tokens}
-                  : Operand{ws + plan.h_along, row, x.tokens};
-    *w = direct_w ? Operand{static_cast<const char *>(x.w), x.ld_w * 2, x.vocab}
-                  : Operand{ws + plan.w_along, row, x.vocab};
+    if (x.tokens <= 16) run(xent_few_products_kernel<P, 1>);
+    else if (x.tokens <= 32) run(xent_few_products_kernel<P, 2>);
+    else run(xent_few_products_kernel<P, 4>);
+    xent_few_join_kernel<P><<<uint32_t(tiles(int64_t(x.tokens) * x.hidden, kWave)), kPackBlock, 0, stream>>>(
+        x, part, plan.few_splits, dh, ld_dh, reinterpret_cast<Control *>(ws));
+    return hipGetLastError();
 }
 
 template <Prec P>
@@ -557,7 +913,10 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
     const Control *control = reinterpret_cast<const Control *>(ws);
     Part *parts = reinterpret_cast<Part *>(ws + plan.parts);
     float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
+    constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
+    if (x.tokens <= kFewForward<F>) return forward_few<F>(x, plan, loss, lse, ws, stream);
     Operand h, w;
+    check_and_scale<P>(x, nullptr, false, ws, stream);
     pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
     int32_t nparts = 0;
     with_tile<P>(x.vocab, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
@@ -574,11 +933,15 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
 template <Prec P>
 hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *dh, int64_t ld_dh, void *dw,
                     int64_t ld_dw, char *ws, hipStream_t stream) {
+    constexpr Prec G = kGradOf<P>;
     const Plan plan = plan_of<P>(x.tokens, x.vocab, x.hidden);
     const Control *control = reinterpret_cast<const Control *>(ws);
+    constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
+    if (x.tokens <= kFewTokens) return backward_few<F>(x, plan, lse, dloss, dh, ld_dh, dw, ld_dw, ws, stream);
     Operand h, w;
+    check_and_scale<P>(x, dloss, true, ws, stream);
     pack_operands<P>(x, dloss, true, plan, ws, &h, &w, stream);
-    const Operand ht{ws + plan.h_turned, row_bytes<P>(x.tokens), x.hidden};
+    const Operand ht{ws + plan.h_turned, row_bytes<G>(x.tokens), x.hidden};
     float *part = reinterpret_cast<float *>(ws + plan.dh);
     for (int64_t v0 = 0; v0 < x.vocab; v0 += plan.piece) {
         const int32_t words = int32_t(std::min<int64_t>(plan.piece, x.vocab - v0));
@@ -586,19 +949,19 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
         with_tile<P>(words, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_grad_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(
-                x, w_piece, h, int32_t(v0), words, lse, dloss, control, ws + plan.g, ws + plan.gt);
+                x, w_piece, h, int32_t(v0), words, lse, control, ws + plan.g, ws + plan.gt);
         });
-        const Operand gt{ws + plan.gt, row_bytes<P>(x.tokens), words};
-        with_tile<P>(words, x.hidden, 1, row_bytes<P>(x.tokens) / kStepBytes, [&](auto tile, int64_t blocks) {
+        const Operand gt{ws + plan.gt, row_bytes<G>(x.tokens), words};
+        with_tile<G>(words, x.hidden, 1, row_bytes<G>(x.tokens) / kStepBytes, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dw_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, gt, ht, int32_t(v0), control,
                                                                                      dw, ld_dw);
         });
         // a piece starts on a whole step of w^T: it is a multiple of 256 words
-        const Operand g{ws + plan.g, row_bytes<P>(words), x.tokens};
-        const Operand wt{ws + plan.w_turned + row_bytes<P>(v0), row_bytes<P>(x.vocab), x.hidden};
-        const int32_t steps = int32_t(row_bytes<P>(words) / kStepBytes);
-        with_tile<P>(x.tokens, x.hidden, plan.splits, steps / plan.splits, [&](auto tile, int64_t blocks) {
+        const Operand g{ws + plan.g, row_bytes<G>(words), x.tokens};
+        const Operand wt{ws + plan.w_turned + row_bytes<G>(v0), row_bytes<G>(x.vocab), x.hidden};
+        const int32_t steps = int32_t(row_bytes<G>(words) / kStepBytes);
+        with_tile<G>(x.tokens, x.hidden, plan.splits, steps / plan.splits, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dh_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, g, wt, steps, plan.splits,
                                                                                      v0 == 0, part);
