@@ -262,7 +262,8 @@ struct Band {
     static constexpr int kStride = Tile::kCols + 4;
     static constexpr int kGroups = Tile::kCols / 8;
     static constexpr int kUnits = kRows * kGroups / Tile::kThreads;   // of eight values, a thread's
-    static_assert(kRows * kStride * 4 <= Tile::kLdsBytes, "a band fits");
+    static constexpr int kBytes = kRows * kStride * 4;
+    static_assert(kBytes <= Tile::kLdsBytes, "a band fits");
     static_assert(kUnits * Tile::kThreads == kRows * kGroups, "whole units");
 
     float *lds;
@@ -329,13 +330,13 @@ __device__ __forceinline__ void each_band(F f) {
 }
 
 // The shapes in use: 256 x 256 by eight waves (one workgroup a compute unit),
-// 128 x 128 by four (two), 64 x 64 by four (four).
+// 128 x 128 by four (two), 64 x 64 by four with two steps on their way (three).
 template <Prec P>
 using LargeTile = MfmaTile<P, 2, 4, 4, 2>;
 template <Prec P>
 using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
 template <Prec P>
-using TinyTile = MfmaTile<P, 2, 2, 1, 1>;
+using TinyTile = MfmaTile<P, 2, 2, 1, 1, 3>;
 
 // For a few tokens against many rows: 64 x 32 TN by two waves, three steps on
 // their way in each of three or two workgroups a compute unit.
@@ -346,28 +347,28 @@ enum TileKind { kTiny, kSmall, kLarge };
 constexpr int kTileKinds = 3;
 constexpr int kTileSide[kTileKinds] = {64, 128, 256};
 
-// What a product over tiles of one kind takes: `work` tiles times steps in
-// all, `longest` steps of one tile, in microseconds.  Measured on kSplit
-// steps: a tile's step takes 0.32, 0.63 and 1.7 us on its own, and 0.25, 0.70
-// and 2.4 us of a compute unit where all are busy (270, 380 and 440 TFLOP/s),
-// so that 256 x 1024 x 512 is fastest with the smallest kind (13.6 against
-// 24.2 and 60 us), 2048 x 4096 x 1024 with the middle one (63.6, 49.3, 64.8) and
-// 4096 x 4096 x 4096 with the largest.
+// What a product over tiles of one kind takes, in microseconds: `work` tiles
+// times steps in all, `longest` steps of one tile.  Measured on kSplit steps:
+// a tile's step takes 0.32, 0.63 and 1.7 us on its own, and 0.25, 0.70 and 2.4
+// us of a compute unit where all are busy (270, 380 and 440 TFLOP/s), so that
+// 256 x 1024 x 512 is fastest with the smallest kind (13.6 against 24.2 and 60
+// us), 2048 x 4096 x 1024 with the middle one (63.6, 49.3, 64.8) and 4096 x
+// 4096 x 4096 with the largest.
+constexpr double kStepAlone[kTileKinds] = {0.32, 0.63, 1.7}, kStepBusy[kTileKinds] = {0.25, 0.70, 2.4};
+
+inline double product_time(int kind, int64_t work, int64_t longest) {
+    if (longest == 0) return 0.0;
+    // rounds of the compute units, whole where few tiles share one
+    double rounds = double(work) / double(longest) / device_cu_count();
+    if (kind == kLarge && rounds > 1.0) rounds = ceil(rounds);
+    if (kind == kSmall && rounds > 1.0) rounds = ceil(rounds * 2.0) / 2.0;
+    return longest * fmax(rounds * kStepBusy[kind], kStepAlone[kind]);
+}
+
 inline TileKind best_tile(const int64_t (&work)[kTileKinds], int64_t longest) {
-    constexpr double kAlone[kTileKinds] = {0.32, 0.63, 1.7}, kBusy[kTileKinds] = {0.25, 0.70, 2.4};
-    const double cus = device_cu_count();
     TileKind best = kTiny;
-    double least = 0.0;
-    for (int k = 0; k < kTileKinds; ++k) {
-        // whole rounds of the compute units, as far as a round can be told
-        const double rounds = longest > 0 ? double(work[k]) / double(longest) / cus : 0.0;
-        const double whole = rounds <= 1.0 || k == kTiny ? rounds : ceil(rounds * (k == kLarge ? 1.0 : 2.0)) / (k == kLarge ? 1.0 : 2.0);
-        const double t = longest * fmax(whole * kBusy[k], kAlone[k]);
-        if (k == 0 || t < least) {
-            least = t;
-            best = TileKind(k);
-        }
-    }
+    for (int k = kTiny + 1; k < kTileKinds; ++k)
+        if (product_time(k, work[k], longest) < product_time(best, work[best], longest)) best = TileKind(k);
     return best;
 }
 

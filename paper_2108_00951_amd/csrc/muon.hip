@@ -57,6 +57,8 @@ struct Place {
     int32_t full[kTileKinds];   // tiles of m x n
     int32_t chunks;     // partial sums
     int32_t packs;      // 64 x 64 tiles of the caller's matrix
+    int32_t units;      // workgroups of a split X X^T
+    int32_t parts;      // of which leave partial sums
 };
 
 struct Mat {
@@ -96,7 +98,15 @@ __host__ __device__ inline int64_t operand_bytes(int32_t rows, int32_t cols) {
     return 2 * x_bytes(m, n) + 2 * x_bytes(n, m) + 2 * x_bytes(m, m);
 }
 
-__host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols) {
+// How many workgroups share a tile of X X^T, with about `most` steps each.
+__host__ __device__ inline int32_t splits_of(int32_t rows, int32_t cols, int32_t most) {
+    const int64_t steps = row_bytes<Prec::kSplit>(high(rows, cols)) / kStepBytes;
+    const int64_t s = (steps + most / 2) / most;
+    return int32_t(s < 1 ? 1 : s);
+}
+
+// `most`: steps of X X^T in one workgroup.
+__host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols, int32_t most) {
     const int32_t m = int32_t(low(rows, cols)), n = int32_t(high(rows, cols));
     p.bytes += operand_bytes(rows, cols);
     for (int k = 0; k < kTileKinds; ++k) {
@@ -107,21 +117,27 @@ __host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols) {
     }
     p.chunks += chunks_of(int64_t(rows) * cols);
     p.packs += ((rows + kPackTile - 1) / kPackTile) * ((cols + kPackTile - 1) / kPackTile);
+    const int32_t tm = (m + kTileSide[kTiny] - 1) / kTileSide[kTiny], splits = splits_of(rows, cols, most);
+    p.units += tm * (tm + 1) / 2 * splits;
+    p.parts += splits > 1 ? tm * (tm + 1) / 2 * splits : 0;
 }
 
-__device__ inline void add(Place &p, const Place &q) {
-    p.bytes += q.bytes;
+__host__ __device__ inline void add(Place &p, const Place &q, int32_t times) {
+    p.bytes += q.bytes * times;
     for (int k = 0; k < kTileKinds; ++k) {
-        p.sym[k] += q.sym[k];
-        p.full[k] += q.full[k];
+        p.sym[k] += q.sym[k] * times;
+        p.full[k] += q.full[k] * times;
     }
-    p.chunks += q.chunks;
-    p.packs += q.packs;
+    p.chunks += q.chunks * times;
+    p.packs += q.packs * times;
+    p.units += q.units * times;
+    p.parts += q.parts * times;
 }
 
-// Workspace: the table, the partial sums, the operands.
+// Workspace: the table, the norms' partial sums, the operands, the partial
+// sums of X X^T.
 struct Layout {
-    int64_t table, sums, operands, total;
+    int64_t table, sums, operands, parts, total;
 };
 
 inline int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
@@ -131,7 +147,8 @@ inline Layout layout_of(int64_t nmat, const Place &end) {
     l.table = 0;
     l.sums = round256((nmat + 1) * int64_t(sizeof(Mat)));
     l.operands = l.sums + round256(int64_t(end.chunks) * 8);
-    l.total = l.operands + end.bytes;
+    l.parts = l.operands + round256(end.bytes);
+    l.total = l.parts + int64_t(end.parts) * kTileSide[kTiny] * kTileSide[kTiny] * 4;
     return l;
 }
 
@@ -164,24 +181,19 @@ struct Operands {
 // `given`, already in the table.  With `given.mat` unused (batch), the matrices
 // are alike and `stride` elements apart.
 __global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, GivenArray given, int32_t first,
-                                                                 int32_t count, int32_t batch,
+                                                                 int32_t count, int32_t batch, int32_t most,
                                                                  int64_t stride_in, int64_t stride_out) {
     if (batch) {   // alike: each place is a multiple
         for (int32_t i = blockIdx.x * kSetupBlock + threadIdx.x; i <= count; i += gridDim.x * kSetupBlock) {
             Place one = {};
-            advance(one, given.mat[0].rows, given.mat[0].cols);
+            advance(one, given.mat[0].rows, given.mat[0].cols, most);
             Mat &t = table[i];
             t.src = i * stride_in;
             t.dst = i * stride_out;
             t.rows = given.mat[0].rows;
             t.cols = given.mat[0].cols;
-            t.at.bytes = one.bytes * i;
-            for (int k = 0; k < kTileKinds; ++k) {
-                t.at.sym[k] = one.sym[k] * i;
-                t.at.full[k] = one.full[k] * i;
-            }
-            t.at.chunks = one.chunks * i;
-            t.at.packs = one.packs * i;
+            t.at = Place{};
+            add(t.at, one, i);
         }
         return;
     }
@@ -190,11 +202,11 @@ __global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, Giv
     const int32_t i = threadIdx.x;
     Place p = {};
     if (i == 0 && first > 0) p = table[first].at;
-    if (i > 0 && i <= count) advance(p, given.mat[i - 1].rows, given.mat[i - 1].cols);
+    if (i > 0 && i <= count) advance(p, given.mat[i - 1].rows, given.mat[i - 1].cols, most);
     for (int32_t d = 1; d <= count; d *= 2) {
         s_sum[i] = p;
         __syncthreads();
-        if (i >= d) add(p, s_sum[i - d]);
+        if (i >= d) add(p, s_sum[i - d], 1);
         __syncthreads();
     }
     if (i > count) return;
@@ -235,11 +247,16 @@ __device__ __forceinline__ float step_scale(const Io &io, int32_t rows, int32_t 
     return __fmul_rn(io.gamma, sqrtf(fmaxf(1.0f, __fdiv_rn(float(rows), float(cols)))));
 }
 
+// x after a step along o.
+__device__ __forceinline__ float step_of(const Io &io, float x, float o, float scale) {
+    return __fsub_rn(__fmul_rn(io.keep, x), __fmul_rn(scale, o));
+}
+
 // The orthogonalised value o of element `at`: into x, or out.
 __device__ __forceinline__ void write_out(const Io &io, int64_t at, float o, float scale) {
     if (io.m != nullptr) {
         float *x = static_cast<float *>(io.out) + at;
-        *x = __fsub_rn(__fmul_rn(io.keep, *x), __fmul_rn(scale, o));
+        *x = step_of(io, *x, o, scale);
     } else if (io.bf16) {
         static_cast<__bf16 *>(io.out)[at] = __bf16(o);   // the one rounding to 8 bits
     } else {
@@ -271,7 +288,7 @@ __device__ __forceinline__ void write_out8(const Io &io, int64_t at, int32_t lef
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float u = __fmul_rn(v[e], kUnscale);
-        o[e / 4][e % 4] = io.m != nullptr ? __fsub_rn(__fmul_rn(io.keep, o[e / 4][e % 4]), __fmul_rn(scale, u)) : u;
+        o[e / 4][e % 4] = io.m != nullptr ? step_of(io, o[e / 4][e % 4], u, scale) : u;
     }
     p[0] = o[0];
     p[1] = o[1];
@@ -390,61 +407,31 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, 
     }
 }
 
-// One product of a step over all matrices, a tile a workgroup.
-//   kGram        A = X X^T             tiles on and below the diagonal
-//   kPolynomial  B = b A + c A A       the same
-//   kApply       X' = a X + B X        into the other pair of buffers
-//   kLast        the same, into the caller's x or out
-// `cur`: which pair of buffers holds X.
+// Where a tile's result goes, and what is added to it.
+struct Target {
+    int32_t row0, col0;
+    bool diagonal;   // of a symmetric result: its other half is in the tile itself
+    bool turned;     // rows of the result are X's columns
+};
+
+// Tile t on or below the diagonal.
+template <class Tile>
+__device__ __forceinline__ Target symmetric_tile(uint32_t t) {
+    uint32_t r = uint32_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
+    while (r * (r + 1) / 2 > t) --r;
+    while ((r + 1) * (r + 2) / 2 <= t) ++r;
+    const uint32_t c = t - r * (r + 1) / 2;
+    return Target{int32_t(r) * Tile::kRows, int32_t(c) * Tile::kCols, r == c, false};
+}
+
+// A product's tile on its way out.
 template <int kProduct, class Tile>
-__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_product_kernel(const Mat *table, int32_t nmat,
-                                                                         char *operands, int cur, float a,
-                                                                         float b, float c, Io io) {
-    __shared__ __align__(16) char lds[Tile::kLdsBytes];
-    constexpr int kKind = Tile::kRows == kTileSide[kTiny] ? kTiny : Tile::kRows == kTileSide[kSmall] ? kSmall : kLarge;
+__device__ __forceinline__ void finish(const Tile &tile, const Target &target, const Mat &mat, const Operands &op,
+                                       int cur, float a, float b, float c, const Io &io, char *lds) {
     constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
-    static_assert(Tile::kRows == Tile::kCols, "tiles of the diagonal are square");
-    const int32_t mi = matrix_of(table, nmat, blockIdx.x,
-                                 [](const Place &p) { return kSym ? p.sym[kKind] : p.full[kKind]; });
-    const Mat &mat = table[mi];
-    const Operands op(operands, mat);
     const int32_t m = int32_t(op.m), n = int32_t(op.n);
-    // the caller's orientation in the last product: its rows are X's columns
-    // where the matrix is tall
-    const bool turned = kProduct == kLast && mat.rows > mat.cols;
-    // a matrix's neighbouring tiles on one XCD; every XCD has a share of every matrix
-    const Place &end = table[mi + 1].at;
-    const int32_t begin = kSym ? mat.at.sym[kKind] : mat.at.full[kKind];
-    const uint32_t t = xcd_place(blockIdx.x - begin, (kSym ? end.sym[kKind] : end.full[kKind]) - begin);
-    uint32_t tr, tc;
-    if (kSym) {
-        tr = uint32_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
-        while (tr * (tr + 1) / 2 > t) --tr;
-        while ((tr + 1) * (tr + 2) / 2 <= t) ++tr;
-        tc = t - tr * (tr + 1) / 2;
-    } else {
-        const uint32_t tm = (m + Tile::kRows - 1) / Tile::kRows, tn = (n + Tile::kCols - 1) / Tile::kCols;
-        if (turned) banded(t, tn, tm, tr, tc);
-        else banded(t, tm, tn, tr, tc);
-    }
-    const int32_t row0 = int32_t(tr) * Tile::kRows, col0 = int32_t(tc) * Tile::kCols;
-
-    const Operand x{op.x(cur), op.x_row, m}, xt{op.xt(cur), op.t_row, n};
-    const Operand oa{op.a(), op.t_row, m}, ob{op.b(), op.t_row, m};
-    Operand left, right;
-    int32_t steps = int32_t(op.t_row / kStepBytes);
-    if (kProduct == kGram) {
-        left = right = x;
-        steps = int32_t(op.x_row / kStepBytes);
-    } else if (kProduct == kPolynomial) {
-        left = right = oa;
-    } else {
-        left = turned ? xt : ob;
-        right = turned ? ob : xt;
-    }
-    Tile tile;
-    tile.run(left, right, row0, col0, 0, steps, lds);
-
+    const bool turned = kProduct == kLast && target.turned;
+    const int32_t row0 = target.row0, col0 = target.col0;
     const int32_t rows = turned ? n : m, cols = kSym ? m : turned ? m : n;
     const int32_t padded_cols = (cols + 31) & ~31, padded_rows = (rows + 31) & ~31;
     // what is added to the product: A, or X (turned: X^T)
@@ -456,7 +443,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_prod
     char *to = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.x(cur ^ 1);
     char *to_t = kProduct == kGram ? op.a() : kProduct == kPolynomial ? op.b() : op.xt(cur ^ 1);
     const int64_t to_row = kSym ? op.t_row : op.x_row;
-    const bool mirror = kProduct != kLast && (!kSym || tr != tc);
+    const bool mirror = kProduct != kLast && !target.diagonal;
     const float scale = step_scale(io, mat.rows, mat.cols);
     const int64_t ld_out = io.ld_out ? io.ld_out : mat.cols;
 
@@ -510,6 +497,120 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_prod
     });
 }
 
+// One product of a step over all matrices, a tile a workgroup.
+//   kGram        A = X X^T             tiles on and below the diagonal
+//   kPolynomial  B = b A + c A A       the same
+//   kApply       X' = a X + B X        into the other pair of buffers
+//   kLast        the same, into the caller's x or out
+// `cur`: which pair of buffers holds X.
+template <int kProduct, class Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_product_kernel(
+    const Mat *table, int32_t nmat, char *operands, int cur, float a, float b, float c, Io io) {
+    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    constexpr int kKind = Tile::kRows == kTileSide[kTiny] ? kTiny : Tile::kRows == kTileSide[kSmall] ? kSmall : kLarge;
+    constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
+    static_assert(Tile::kRows == Tile::kCols, "tiles of the diagonal are square");
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x,
+                                 [](const Place &p) { return kSym ? p.sym[kKind] : p.full[kKind]; });
+    const Mat &mat = table[mi];
+    const Operands op(operands, mat);
+    const int32_t m = int32_t(op.m), n = int32_t(op.n);
+    // a matrix's neighbouring tiles on one XCD; every XCD has a share of every matrix
+    const Place &end = table[mi + 1].at;
+    const int32_t begin = kSym ? mat.at.sym[kKind] : mat.at.full[kKind];
+    const uint32_t t = xcd_place(blockIdx.x - begin, (kSym ? end.sym[kKind] : end.full[kKind]) - begin);
+    Target target;
+    if (kSym) {
+        target = symmetric_tile<Tile>(t);
+    } else {
+        // the caller's orientation in the last product: its rows are X's
+        // columns where the matrix is tall
+        target.turned = kProduct == kLast && mat.rows > mat.cols;
+        target.diagonal = false;
+        const uint32_t tm = (m + Tile::kRows - 1) / Tile::kRows, tn = (n + Tile::kCols - 1) / Tile::kCols;
+        uint32_t r, q;
+        if (target.turned) banded(t, tn, tm, r, q);
+        else banded(t, tm, tn, r, q);
+        target.row0 = int32_t(r) * Tile::kRows;
+        target.col0 = int32_t(q) * Tile::kCols;
+    }
+
+    const Operand x{op.x(cur), op.x_row, m}, xt{op.xt(cur), op.t_row, n};
+    const Operand oa{op.a(), op.t_row, m}, ob{op.b(), op.t_row, m};
+    Operand left, right;
+    int32_t steps = int32_t(op.t_row / kStepBytes);
+    if (kProduct == kGram) {
+        left = right = x;
+        steps = int32_t(op.x_row / kStepBytes);
+    } else if (kProduct == kPolynomial) {
+        left = right = oa;
+    } else {
+        left = target.turned ? xt : ob;
+        right = target.turned ? ob : xt;
+    }
+    Tile tile;
+    tile.run(left, right, target.row0, target.col0, 0, steps, lds);
+    finish<kProduct>(tile, target, mat, op, cur, a, b, c, io, lds);
+}
+
+// X X^T of few tiles: several workgroups share a long tile's steps and leave
+// partial sums, as their registers hold them; the join adds them in order.
+template <class Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram_kernel(const Mat *table, int32_t nmat,
+                                                                                        char *operands, int cur,
+                                                                                        int32_t most, f32x4 *parts,
+                                                                                        Io io) {
+    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    static_assert(Tile::kRows == kTileSide[kTiny] && Tile::kTilesM == 1 && Tile::kTilesN == 1, "places count these");
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.units; });
+    const Mat &mat = table[mi];
+    const Operands op(operands, mat);
+    const uint32_t units = uint32_t(table[mi + 1].at.units - mat.at.units);
+    const uint32_t splits = uint32_t(splits_of(mat.rows, mat.cols, most)), tiles = units / splits;
+    const uint32_t u = xcd_place(blockIdx.x - mat.at.units, units);
+    const uint32_t t = u % tiles, split = u / tiles;
+    const Target target = symmetric_tile<Tile>(t);
+    const int64_t steps = op.x_row / kStepBytes;
+    const int32_t lo = int32_t(steps * split / splits), hi = int32_t(steps * (split + 1) / splits);
+    const Operand x{op.x(cur), op.x_row, int32_t(op.m)};
+    Tile tile;
+    tile.run(x, x, target.row0, target.col0, lo, hi - lo, lds);
+    if (splits == 1) {
+        finish<kGram>(tile, target, mat, op, cur, 0.0f, 0.0f, 0.0f, io, lds);
+        return;
+    }
+    f32x4 *to = parts + (int64_t(mat.at.parts) + t * splits + split) * (4 * Tile::kThreads);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f32x16 &v = tile.acc[0][0];
+        to[q * Tile::kThreads + threadIdx.x] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    }
+}
+
+template <class Tile>
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram_join_kernel(
+    const Mat *table, int32_t nmat, char *operands, int cur, int32_t most, const f32x4 *parts, Io io) {
+    __shared__ __align__(16) char lds[Band<Tile>::kBytes];
+    const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.sym[kTiny]; });
+    const Mat &mat = table[mi];
+    const int32_t splits = splits_of(mat.rows, mat.cols, most);
+    if (splits == 1) return;
+    const Operands op(operands, mat);
+    const uint32_t t = blockIdx.x - mat.at.sym[kTiny];
+    const f32x4 *from = parts + (int64_t(mat.at.parts) + int64_t(t) * splits) * (4 * Tile::kThreads) + threadIdx.x;
+    Tile tile;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) tile.acc[0][0][e] = 0.0f;
+    for (int32_t s = 0; s < splits; ++s)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 v = from[(s * 4 + q) * Tile::kThreads];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tile.acc[0][0][4 * q + e] = __fadd_rn(tile.acc[0][0][4 * q + e], v[e]);
+        }
+    finish<kGram>(tile, symmetric_tile<Tile>(t), mat, op, cur, 0.0f, 0.0f, 0.0f, io, lds);
+}
+
 // ---- small matrices -------------------------------------------------------
 // A matrix whose X fits in LDS as fp32 is one workgroup's from its gradient to
 // its update: one launch, nothing in the workspace, the fp32 matrix
@@ -536,16 +637,47 @@ __host__ inline int lds_class(int32_t rows, int32_t cols) {
     return f <= kLdsFloats[0] ? 0 : f <= kLdsFloats[1] ? 1 : -1;
 }
 
-// One 16 x 16 tile: sum over k < len of left(row, k) right(k, col).  Lane l
-// holds row l % 16 of the left, column l % 16 of the right, k = l / 16; of the
-// result column l % 16, rows l / 16 * 4 + e.
+// Two 16 x 16 tiles of one column of tiles: the sum over k < len (a multiple of
+// 16) of left(i, row, k) right(k, col).  Lane l holds row l % 16 of the left,
+// column l % 16 of the right, k = l / 16; of the result column l % 16, rows
+// l / 16 * 4 + e.  The next 16 values of k are on their way from LDS while the
+// present ones are multiplied.
 template <class L, class R>
-__device__ __forceinline__ f32x4 mfma_f32(int32_t len, L left, R right) {
-    const int lane = threadIdx.x & (kWave - 1);
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int32_t k = lane >> 4; k < len; k += 4)
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(left(lane & 15, k), right(k, lane & 15), acc, 0, 0, 0);
-    return acc;
+__device__ __forceinline__ void mfma_f32(int32_t len, f32x4 (&acc)[2], L left, R right) {
+    const int row = threadIdx.x & 15, four = (threadIdx.x & (kWave - 1)) >> 4;
+    float a[2][2][4], b[2][4];
+    auto load = [&](int turn, int32_t k0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int32_t k = k0 + 4 * q + four;
+            b[turn][q] = right(k, row);
+            a[turn][0][q] = left(0, row, k);
+            a[turn][1][q] = left(1, row, k);
+        }
+    };
+    auto multiply = [&](int turn) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[turn][i][q], b[turn][q], acc[i], 0, 0, 0);
+    };
+    acc[0] = acc[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    load(0, 0);
+    int32_t k = 16;
+    for (; k + 16 < len; k += 32) {
+        load(1, k);
+        multiply(0);
+        load(0, k + 16);
+        multiply(1);
+    }
+    if (k < len) {
+        load(1, k);
+        multiply(0);
+        multiply(1);
+    } else {
+        multiply(0);
+    }
 }
 
 template <int kClass>
@@ -563,22 +695,40 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
     const int32_t m = round16(low(mat.rows, mat.cols)), n = round16(high(mat.rows, mat.cols));
     const int32_t lx = n + 4, la = m + 4;
     float *X = lds, *A = X + m * lx, *B = A + m * la;
+    const int32_t size = mat.rows * mat.cols;
+    // element i of the matrix: where it is in memory and in X
+    auto place = [&](int32_t i, int64_t ld, int64_t &at, int32_t &to) {
+        const int32_t r = int32_t(uint32_t(i) / uint32_t(mat.cols)), q = i - r * mat.cols;
+        at = r * ld + q;
+        to = tall ? q * lx + r : r * lx + q;
+    };
 
     for (int32_t i = tid; i < m * lx; i += kLdsBlock) X[i] = 0.0f;
     __syncthreads();
-    const int32_t size = mat.rows * mat.cols;
     double sum = 0.0;
-    for (int32_t i = tid; i < size; i += kLdsBlock) {
-        const int32_t r = i / mat.cols, col = i - r * mat.cols;
-        const int64_t at = src + r * ld_in + col;
-        float u = read_in(io, at);
-        if (io.m != nullptr) {
-            const float v = __fadd_rn(__fmul_rn(io.beta, io.m[at]), u);
-            io.m[at] = v;
-            u = direction(io, u, v);
+    constexpr int kAhead = 4;   // elements of a thread on their way together
+    for (int32_t i0 = tid; i0 < size; i0 += kAhead * kLdsBlock) {
+        float u[kAhead], v[kAhead];
+        int64_t at[kAhead];
+        int32_t to[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int32_t i = min(i0 + k * kLdsBlock, size - 1);
+            place(i, ld_in, at[k], to[k]);
+            u[k] = read_in(io, src + at[k]);
+            v[k] = io.m != nullptr ? io.m[src + at[k]] : 0.0f;
         }
-        X[tall ? col * lx + r : r * lx + col] = u;
-        sum += double(u) * double(u);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + k * kLdsBlock >= size) continue;
+            if (io.m != nullptr) {
+                v[k] = __fadd_rn(__fmul_rn(io.beta, v[k]), u[k]);
+                io.m[src + at[k]] = v[k];
+                u[k] = direction(io, u[k], v[k]);
+            }
+            X[to[k]] = u[k];
+            sum += double(u[k]) * double(u[k]);
+        }
     }
 #pragma unroll
     for (int off = kWave / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
@@ -589,58 +739,85 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
     const float norm = __fadd_rn(float(sqrt(sum)), io.eps);
     // the padding stays zero, also where the norm is zero, infinite or NaN
     for (int32_t i = tid; i < size; i += kLdsBlock) {
-        const int32_t r = i / mat.cols, col = i - r * mat.cols;
-        float *p = X + (tall ? col * lx + r : r * lx + col);
-        *p = __fdiv_rn(*p, norm);
+        int64_t at;
+        int32_t to;
+        place(i, 0, at, to);
+        X[to] = __fdiv_rn(X[to], norm);
     }
     __syncthreads();
 
+    // A wave takes two tiles of a column: eight columns at a time, or four with
+    // both halves of their rows where there are more than two rows of tiles.
     const int32_t tm = m / 16, tn = n / 16;
+    const int halves = tm > 2 ? 2 : 1, columns = kLdsWaves / halves;
+    const int first = wave % halves * 2, column = wave / halves;
+    const int32_t last = (tm - 1) * 16;   // a second tile past the rows repeats the last
+    const int32_t r0 = min(first * 16, last), r1 = min(first * 16 + 16, last);
     const int32_t row4 = (lane >> 4) * 4, col = lane & 15;
     for (int s = 0; s < steps; ++s) {
-        for (int32_t t = wave; t < tm * tm; t += kLdsWaves) {
-            const int32_t r0 = t / tm * 16, c0 = t % tm * 16;
-            const f32x4 g = mfma_f32(n, [&](int r, int k) { return X[(r0 + r) * lx + k]; },
-                                     [&](int k, int q) { return X[(c0 + q) * lx + k]; });
+        f32x4 g[2];
+        if (column < tm) {
+            mfma_f32(n, g, [&](int i, int r, int k) { return X[((i ? r1 : r0) + r) * lx + k]; },
+                     [&](int k, int q) { return X[(column * 16 + q) * lx + k]; });
 #pragma unroll
-            for (int e = 0; e < 4; ++e) A[(r0 + row4 + e) * la + c0 + col] = g[e];
+            for (int i = 0; i < 2; ++i)
+                if (first + i < tm)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) A[((i ? r1 : r0) + row4 + e) * la + column * 16 + col] = g[i][e];
         }
         __syncthreads();
-        for (int32_t t = wave; t < tm * tm; t += kLdsWaves) {
-            const int32_t r0 = t / tm * 16, c0 = t % tm * 16;
-            const f32x4 g = mfma_f32(m, [&](int r, int k) { return A[(r0 + r) * la + k]; },
-                                     [&](int k, int q) { return A[k * la + c0 + q]; });
+        if (column < tm) {
+            mfma_f32(m, g, [&](int i, int r, int k) { return A[((i ? r1 : r0) + r) * la + k]; },
+                     [&](int k, int q) { return A[k * la + column * 16 + q]; });
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int32_t at = (r0 + row4 + e) * la + c0 + col;
-                B[at] = __fadd_rn(__fmul_rn(b, A[at]), __fmul_rn(c, g[e]));
-            }
-        }
-        __syncthreads();
-        // sixteen columns of X are one wave's, all rows, and replaced in place
-        for (int32_t t = wave; t < tn; t += kLdsWaves) {
-            f32x4 g[kLdsMaxM / 16];
-#pragma unroll
-            for (int i = 0; i < kLdsMaxM / 16; ++i)
-                if (i < tm)
-                    g[i] = mfma_f32(m, [&](int r, int k) { return B[(i * 16 + r) * la + k]; },
-                                    [&](int k, int q) { return X[k * lx + t * 16 + q]; });
-#pragma unroll
-            for (int i = 0; i < kLdsMaxM / 16; ++i)
-                if (i < tm) {
+            for (int i = 0; i < 2; ++i)
+                if (first + i < tm)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float *p = X + (i * 16 + row4 + e) * lx + t * 16 + col;
-                        *p = __fadd_rn(__fmul_rn(a, *p), g[i][e]);
+                        const int32_t at = ((i ? r1 : r0) + row4 + e) * la + column * 16 + col;
+                        B[at] = __fadd_rn(__fmul_rn(b, A[at]), __fmul_rn(c, g[i][e]));
                     }
-                }
+        }
+        __syncthreads();
+        for (int32_t t0 = 0; t0 < tn; t0 += columns) {
+            const int32_t t = t0 + column;
+            if (t < tn)
+                mfma_f32(m, g, [&](int i, int r, int k) { return B[((i ? r1 : r0) + r) * la + k]; },
+                         [&](int k, int q) { return X[k * lx + t * 16 + q]; });
+            // a column is replaced where it is, once both halves have read it
+            if (halves > 1) __syncthreads();
+            if (t < tn) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (first + i < tm)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float *p = X + ((i ? r1 : r0) + row4 + e) * lx + t * 16 + col;
+                            *p = __fadd_rn(__fmul_rn(a, *p), g[i][e]);
+                        }
+            }
         }
         __syncthreads();
     }
     const float scale = step_scale(io, mat.rows, mat.cols);
-    for (int32_t i = tid; i < size; i += kLdsBlock) {
-        const int32_t r = i / mat.cols, q = i - r * mat.cols;
-        write_out(io, dst + r * ld_out + q, X[tall ? q * lx + r : r * lx + q], scale);
+    for (int32_t i0 = tid; i0 < size; i0 += kAhead * kLdsBlock) {
+        float v[kAhead];
+        int64_t at[kAhead];
+        int32_t from[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            place(min(i0 + k * kLdsBlock, size - 1), ld_out, at[k], from[k]);
+            if (io.m != nullptr) v[k] = static_cast<const float *>(io.out)[dst + at[k]];
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (i0 + k * kLdsBlock >= size) continue;
+            const float o = X[from[k]];
+            if (io.m != nullptr)
+                static_cast<float *>(io.out)[dst + at[k]] = step_of(io, v[k], o, scale);
+            else
+                write_out(io, dst + at[k], o, scale);
+        }
     }
 }
 
@@ -650,29 +827,87 @@ struct Cost {
     int64_t work[3][kTileKinds], longest[3];
 };
 
-void add_cost(Cost &cost, int32_t rows, int32_t cols) {
+void add_cost(Cost &cost, int32_t rows, int32_t cols, int32_t times) {
     const int64_t steps_n = row_bytes<Prec::kSplit>(high(rows, cols)) / kStepBytes;
     const int64_t steps_m = row_bytes<Prec::kSplit>(low(rows, cols)) / kStepBytes;
     Place one = {};
-    advance(one, rows, cols);
+    advance(one, rows, cols, INT32_MAX);
     for (int p = 0; p < 3; ++p) {
         const int64_t steps = p == 0 ? steps_n : steps_m;
-        for (int k = 0; k < kTileKinds; ++k) cost.work[p][k] += steps * (p < 2 ? one.sym[k] : one.full[k]);
+        for (int k = 0; k < kTileKinds; ++k) cost.work[p][k] += steps * (p < 2 ? one.sym[k] : one.full[k]) * times;
         if (steps > cost.longest[p]) cost.longest[p] = steps;
     }
 }
 
+// The steps of X X^T that a workgroup takes where tiles are split, INT32_MAX
+// where they are not: for three workgroups a compute unit, but 24 at least.
+// Splitting costs a launch and the partial sums' way to memory and back, about
+// 10 us (LSTM-sized gates, 330 tiles of 82 to 157 steps: 87 -> 46 us).
+int32_t split_steps(const Cost &cost) {
+    const double whole = product_time(best_tile(cost.work[0], cost.longest[0]),
+                                      cost.work[0][best_tile(cost.work[0], cost.longest[0])], cost.longest[0]);
+    const int64_t share = cost.work[0][kTiny] / (3 * device_cu_count());
+    const int32_t most = int32_t(share < 24 ? 24 : share < (1 << 20) ? share : 1 << 20);
+    const double split = fmax(most * kStepAlone[kTiny], cost.work[0][kTiny] * kStepBusy[kTiny] / device_cu_count()) + 10.0;
+    return split < whole ? most : INT32_MAX;
+}
+
+// Everything that a call over these matrices is laid out by.
+struct Job {
+    Cost cost;
+    Place end;
+    int32_t nmat, most;
+};
+
+// Matrices that the workgroups of small ones do not take; `next` steps through
+// rows and cols.  False where they need more workgroups than a grid has.
+bool job_of(int32_t nmat, const int32_t *rows, const int32_t *cols, int32_t next, Job *job) {
+    *job = {};
+    auto each = [&](auto f) {
+        for (int32_t i = 0; i < (next == 0 && nmat > 0 ? 1 : nmat); ++i) {
+            const int32_t r = rows[i * next], c = cols[i * next];
+            if (r != 0 && c != 0 && lds_class(r, c) < 0) f(r, c);
+        }
+    };
+    const int32_t times = next == 0 ? nmat : 1;   // of each that is looked at
+    int64_t count = 0;
+    each([&](int32_t r, int32_t c) {
+        Place one = {};
+        advance(one, r, c, 8);   // no fewer workgroups than with any split
+        count += (int64_t(one.packs) + one.full[kTiny] + one.chunks + one.units) * times;
+        add_cost(job->cost, r, c, times);
+        job->nmat += times;
+    });
+    if (count > INT32_MAX) return false;
+    job->most = split_steps(job->cost);
+    each([&](int32_t r, int32_t c) {
+        Place one = {};
+        advance(one, r, c, job->most);
+        add(job->end, one, times);
+    });
+    return true;
+}
+
 template <int kProduct>
-void launch_product(const Place &end, const Cost &cost, const Mat *table, int32_t nmat, char *operands, int cur,
-                    float a, float b, float c, const Io &io, hipStream_t stream) {
+void launch_product(const Job &job, const Mat *table, char *operands, f32x4 *parts, int cur, float a, float b,
+                    float c, const Io &io, hipStream_t stream) {
+    if (kProduct == kGram && job.most != INT32_MAX) {
+        using Tile = TinyTile<Prec::kSplit>;
+        muon_gram_kernel<Tile><<<job.end.units, Tile::kThreads, 0, stream>>>(table, job.nmat, operands, cur, job.most,
+                                                                             parts, io);
+        if (job.end.parts > 0)
+            muon_gram_join_kernel<Tile><<<job.end.sym[kTiny], Tile::kThreads, 0, stream>>>(
+                table, job.nmat, operands, cur, job.most, parts, io);
+        return;
+    }
     constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
     constexpr int kCost = kProduct == kGram ? 0 : kProduct == kPolynomial ? 1 : 2;
     auto run = [&](auto tile, int kind) {
         using Tile = decltype(tile);
-        muon_product_kernel<kProduct, Tile><<<kSym ? end.sym[kind] : end.full[kind], Tile::kThreads, 0, stream>>>(
-            table, nmat, operands, cur, a, b, c, io);
+        muon_product_kernel<kProduct, Tile><<<kSym ? job.end.sym[kind] : job.end.full[kind], Tile::kThreads, 0, stream>>>(
+            table, job.nmat, operands, cur, a, b, c, io);
     };
-    switch (best_tile(cost.work[kCost], cost.longest[kCost])) {
+    switch (best_tile(job.cost.work[kCost], job.cost.longest[kCost])) {
         case kTiny: return run(TinyTile<Prec::kSplit>(), kTiny);
         case kSmall: return run(SmallTile<Prec::kSplit>(), kSmall);
         case kLarge: return run(LargeTile<Prec::kSplit>(), kLarge);
@@ -689,21 +924,21 @@ void launch_lds(int kind, int32_t count, const GivenArray &given, bool batch, in
 }
 
 // The launches after the table.
-hipError_t launch_steps(const Place &end, const Cost &cost, int32_t nmat, char *ws, const Io &io, int steps, const float *coeffs,
-                        hipStream_t stream) {
-    const Layout l = layout_of(nmat, end);
+hipError_t launch_steps(const Job &job, char *ws, const Io &io, int steps, const float *coeffs, hipStream_t stream) {
+    const Layout l = layout_of(job.nmat, job.end);
     const Mat *table = reinterpret_cast<const Mat *>(ws + l.table);
     double *sums = reinterpret_cast<double *>(ws + l.sums);
+    f32x4 *parts = reinterpret_cast<f32x4 *>(ws + l.parts);
     char *operands = ws + l.operands;
-    muon_momentum_kernel<<<end.chunks, kSumBlock, 0, stream>>>(table, nmat, io, sums);
-    muon_pack_kernel<<<end.packs, kSumBlock, 0, stream>>>(table, nmat, io, sums, operands);
+    muon_momentum_kernel<<<job.end.chunks, kSumBlock, 0, stream>>>(table, job.nmat, io, sums);
+    muon_pack_kernel<<<job.end.packs, kSumBlock, 0, stream>>>(table, job.nmat, io, sums, operands);
     const float a = coeffs[0], b = coeffs[1], c = coeffs[2];
     int cur = 0;
     for (int s = 0; s < steps; ++s, cur ^= 1) {
-        launch_product<kGram>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
-        launch_product<kPolynomial>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
-        if (s + 1 < steps) launch_product<kApply>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
-        else launch_product<kLast>(end, cost, table, nmat, operands, cur, a, b, c, io, stream);
+        launch_product<kGram>(job, table, operands, parts, cur, a, b, c, io, stream);
+        launch_product<kPolynomial>(job, table, operands, parts, cur, a, b, c, io, stream);
+        if (s + 1 < steps) launch_product<kApply>(job, table, operands, parts, cur, a, b, c, io, stream);
+        else launch_product<kLast>(job, table, operands, parts, cur, a, b, c, io, stream);
     }
     return hipGetLastError();
 }
@@ -711,19 +946,9 @@ hipError_t launch_steps(const Place &end, const Cost &cost, int32_t nmat, char *
 }  // namespace
 
 bool muon_workspace_size(int32_t nmat, const int32_t *rows, const int32_t *cols, int32_t next, size_t *bytes) {
-    Place end = {};
-    int64_t tiles = 0;
-    int32_t live = 0;
-    for (int32_t i = 0; i < nmat; ++i) {
-        if (rows[i * next] == 0 || cols[i * next] == 0 || lds_class(rows[i * next], cols[i * next]) >= 0) continue;
-        Place one = {};
-        advance(one, rows[i * next], cols[i * next]);
-        tiles += int64_t(one.packs) + one.full[kTiny] + one.chunks + one.sym[kTiny];
-        if (tiles > INT32_MAX) return false;
-        advance(end, rows[i * next], cols[i * next]);
-        ++live;
-    }
-    *bytes = size_t(layout_of(live, end).total);
+    Job job;
+    if (!job_of(nmat, rows, cols, next, &job)) return false;
+    *bytes = size_t(layout_of(job.nmat, job.end).total);
     return true;
 }
 
@@ -745,17 +970,13 @@ hipError_t launch_muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride
         launch_lds(kind, batch, given, true, stride_g, stride_o, io, steps, coeffs, stream);
         return hipGetLastError();
     }
-    Place end = {};
-    Cost cost = {};
-    for (int32_t i = 0; i < batch; ++i) {
-        advance(end, rows, cols);
-        add_cost(cost, rows, cols);
-    }
+    Job job;
+    job_of(batch, &rows, &cols, 0, &job);
     char *ws = static_cast<char *>(workspace);
     const int32_t blocks = (batch + kSetupBlock) / kSetupBlock;
-    muon_setup_kernel<<<blocks < 64 ? blocks : 64, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, 0,
-                                                                             batch, 1, stride_g, stride_o);
-    return launch_steps(end, cost, batch, ws, io, steps, coeffs, stream);
+    muon_setup_kernel<<<blocks < 64 ? blocks : 64, kSetupBlock, 0, stream>>>(
+        reinterpret_cast<Mat *>(ws), given, 0, batch, 1, job.most, stride_g, stride_o);
+    return launch_steps(job, ws, io, steps, coeffs, stream);
 }
 
 hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offsets, const int32_t *rows,
@@ -774,19 +995,19 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
 
     // the matrices of each kind, as many as a launch's arguments hold at a time
     char *ws = static_cast<char *>(workspace);
-    Place end = {};
-    Cost cost = {};
-    int32_t live = 0;
+    Job job;
+    job_of(nmat, rows, cols, 1, &job);
     for (int kind = -1; kind <= 1; ++kind) {
         GivenArray given;
-        int32_t count = 0;
+        int32_t count = 0, before = 0;
         auto flush = [&]() {
             if (count == 0) return;
             if (kind >= 0)
                 launch_lds(kind, count, given, false, 0, 0, io, steps, coeffs, stream);
             else
-                muon_setup_kernel<<<1, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, live - count,
-                                                                 count, 0, 0, 0);
+                muon_setup_kernel<<<1, kSetupBlock, 0, stream>>>(reinterpret_cast<Mat *>(ws), given, before, count, 0,
+                                                                 job.most, 0, 0);
+            before += count;
             count = 0;
         };
         // the tiles that take longest first (X X^T sums over the longer axis):
@@ -797,17 +1018,12 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
                 if (kind < 0 && (high(rows[i], cols[i]) >> bit) != 1) continue;
                 if (count == kGivenPerLaunch) flush();
                 given.mat[count++] = Given{offsets[i], rows[i], cols[i]};
-                if (kind < 0) {
-                    advance(end, rows[i], cols[i]);
-                    add_cost(cost, rows[i], cols[i]);
-                    ++live;
-                }
             }
         }
         flush();
     }
-    if (live == 0) return hipGetLastError();
-    return launch_steps(end, cost, live, ws, io, steps, coeffs, stream);
+    if (job.nmat == 0) return hipGetLastError();
+    return launch_steps(job, ws, io, steps, coeffs, stream);
 }
 
 }  // namespace efs
