@@ -2,7 +2,7 @@
 // orthogonalised update (muon.hip) and the cross entropy (xent.hip) share.
 //
 // Both operands are stored along the summed axis: row r of A holds A[r, 0..K).
-// A row is read in steps of 128 bytes, which hold
+// A step of 128 bytes of a row holds
 //   kBf16   64 bf16 values;
 //   kHalf   64 fp16 values, scaled by a power of two;
 //   kFp32   32 fp32 values as they are, for the fp32 matrix instructions
@@ -15,7 +15,8 @@
 //           the rounding of lo, is 2^-22 of a product at most, as much as an
 //           fp32 product's own sums lose.  It runs at a third of the 16-bit
 //           rate (2500 TFLOP/s), five times that of the fp32 matrix
-//           instructions (157).
+//           instructions.  (The parts in planes of their own, 64 bytes of each
+//           a step: 7 % slower.)
 // A workgroup of WM x WN waves computes WM TM 32 rows by WN TN 32 columns, a
 // wave TM x TN accumulators of the 32 x 32 x 16 instruction.  Steps go from
 // memory straight to LDS (16 bytes a lane, no registers), into one of two
@@ -52,10 +53,21 @@ constexpr int kStepBytes = 128;   // of one row, a step of the summed axis
 template <Prec P>
 constexpr int kStepValues = P == Prec::kSplit || P == Prec::kFp32 ? 32 : 64;
 
-// Bytes of a row of `len` values, padded with zeros to whole steps.
+// Steps that `len` values take.
+template <Prec P>
+__host__ __device__ constexpr int64_t steps_of(int64_t len) {
+    return (len + kStepValues<P> - 1) / kStepValues<P>;
+}
+
+// Bytes of a row of `len` values, padded with zeros to whole steps, and the
+// values that it then holds.
 template <Prec P>
 __host__ __device__ constexpr int64_t row_bytes(int64_t len) {
-    return (len + kStepValues<P> - 1) / kStepValues<P> * kStepBytes;
+    return steps_of<P>(len) * kStepBytes;
+}
+template <Prec P>
+__host__ __device__ constexpr int32_t row_values(int64_t len) {
+    return int32_t(steps_of<P>(len) * kStepValues<P>);
 }
 
 // `rows` >= 1 rows of `stride` bytes (a multiple of 16, as `base` is).  Rows
@@ -107,7 +119,17 @@ struct MfmaTile {
     static constexpr int kLdsBytes = kStages * kBufferBytes;
     static constexpr int kLoadsA = kRows / 8 / (WM * WN);   // a wave's, 8 rows each
     static constexpr int kLoadsB = kCols / 8 / (WM * WN);
+    static constexpr int kLoads = kLoadsA + kLoadsB;
     static constexpr int kTilesM = TM, kTilesN = TN;
+    // Waiting for all loads but those of the kStages - 2 later steps: the
+    // count's low four bits are bits 0..3 of the operand, its high two 14..15.
+    static constexpr int kLater = (kStages - 2) * kLoads;
+    static_assert(kStages >= 2 && kLater < 64, "six bits count the loads");
+    static constexpr int kWaitLoads = 0x0f70 | (kLater & 15) | (kLater >> 4 << 14);
+    // Loads between the products, where registers are left for it (64 x 64:
+    // 21.5 -> 19.6 us for 256 x 256 x 2048, 128 x 128: 381 -> 391 TFLOP/s; the
+    // largest kind loses 3 %).
+    static constexpr bool kSpread = TM * TN <= 4;
     static constexpr int kWavesPerSimd = kThreads >= 256 ? 2 : 1;   // asked of the compiler
 
     f32x16 acc[TM][TN];
@@ -137,18 +159,6 @@ struct MfmaTile {
             return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
     }
 
-    // Waits until at most `stages` steps' loads of this wave are on their way.
-    static __device__ __forceinline__ void wait_loads(int stages) {
-        constexpr int kLoads = kLoadsA + kLoadsB;
-        static_assert(kStages >= 2 && kStages <= 4 && 2 * kLoads < 64, "counts that are written out below");
-        // the count's low four bits are bits 0..3 of the operand, its high two bits 14..15
-        constexpr int k1 = 0x0f70 | (kLoads & 15) | (kLoads >> 4 << 14);
-        constexpr int k2 = 0x0f70 | (2 * kLoads & 15) | (2 * kLoads >> 4 << 14);
-        if (kStages >= 4 && stages >= 2) __builtin_amdgcn_s_waitcnt(k2);
-        else if (kStages >= 3 && stages >= 1) __builtin_amdgcn_s_waitcnt(k1);
-        else __builtin_amdgcn_s_waitcnt(0x0f70);
-    }
-
     // acc = A[row0.., step0..step0+steps) B[col0.., ...)^T, in the operands'
     // scaled units.  `lds` has kLdsBytes, 16-byte aligned; it is free again
     // after a barrier.  Called by every thread of the workgroup.
@@ -165,47 +175,45 @@ struct MfmaTile {
 
         // a load covers 8 rows of 128 bytes; lane l fills unit l % 8 of row
         // l / 8 in LDS, which holds unit (l % 8) ^ (row % 8) of memory
-        const char *pa[kLoadsA], *pb[kLoadsB];
+        const char *from[kLoads];
         const int unit = (lane & 7) ^ (lane >> 3);
 #pragma unroll
-        for (int i = 0; i < kLoadsA; ++i) {
-            const int r = (wave * kLoadsA + i) * 8 + (lane >> 3);
-            pa[i] = a.base + int64_t(min(row0 + r, a.rows - 1)) * a.stride + unit * 16;
-        }
-#pragma unroll
-        for (int i = 0; i < kLoadsB; ++i) {
-            const int r = (wave * kLoadsB + i) * 8 + (lane >> 3);
-            pb[i] = b.base + int64_t(min(col0 + r, b.rows - 1)) * b.stride + unit * 16;
+        for (int i = 0; i < kLoads; ++i) {
+            const Operand &o = i < kLoadsA ? a : b;
+            const int r = i < kLoadsA ? row0 + (wave * kLoadsA + i) * 8 + (lane >> 3)
+                                      : col0 + (wave * kLoadsB + i - kLoadsA) * 8 + (lane >> 3);
+            from[i] = o.base + int64_t(min(r, o.rows - 1)) * o.stride + unit * 16;
         }
         auto load = [&](int buffer, int32_t step) {
             char *to = lds + buffer * kBufferBytes;
-            const int64_t at = int64_t(step) * kStepBytes;
+            const int64_t off = int64_t(step) * kStepBytes;
 #pragma unroll
-            for (int i = 0; i < kLoadsA; ++i)
-                __builtin_amdgcn_global_load_lds((global_void *)(pa[i] + at),
-                                                 (lds_void *)(to + (wave * kLoadsA + i) * 1024), 16, 0, 0);
-#pragma unroll
-            for (int i = 0; i < kLoadsB; ++i)
+            for (int i = 0; i < kLoads; ++i)
                 __builtin_amdgcn_global_load_lds(
-                    (global_void *)(pb[i] + at),
-                    (lds_void *)(to + kRows * kStepBytes + (wave * kLoadsB + i) * 1024), 16, 0, 0);
+                    (global_void *)(from[i] + off),
+                    (lds_void *)(to + (i < kLoadsA ? wave * kLoadsA + i : kRows / 8 + wave * kLoadsB + i - kLoadsA) * 1024),
+                    16, 0, 0);
         };
 
         const int ra = wave / WN * TM * 32, rb = wave % WN * TN * 32;
+        if (steps <= 0) return;
+        // loads past the last step read the last again, into a buffer that
+        // nothing reads: the loop has no branch, and counts its loads
+        const int32_t last = step0 + steps - 1;
 #pragma unroll
-        for (int k = 0; k < kStages - 1; ++k)
-            if (k < steps) load(k, step0 + k);
+        for (int k = 0; k < kStages - 1; ++k) load(k, min(step0 + k, last));
         int buffer = 0;
         for (int32_t s = 0; s < steps; ++s) {
             // this step is in LDS once every wave's loads for it have come back
             // (those of later steps may be on their way), and every wave has
             // left the buffer that is loaded next
-            wait_loads(min(kStages - 2, steps - 1 - s));
+            __builtin_amdgcn_s_waitcnt(kWaitLoads);
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (s + kStages - 1 < steps)
-                load(buffer == 0 ? kStages - 1 : buffer - 1, step0 + s + kStages - 1);
+            const int next = buffer == 0 ? kStages - 1 : buffer - 1;
+            const int32_t next_step = min(step0 + s + kStages - 1, last);
+            if (!kSpread) load(next, next_step);
 
             const char *la = lds + buffer * kBufferBytes + ra * kStepBytes;
             const char *lb = lds + buffer * kBufferBytes + (kRows + rb) * kStepBytes;
@@ -226,6 +234,7 @@ struct MfmaTile {
 #pragma unroll
                 for (int i = 0; i < TM; ++i) fa[q][i] = read(la, i, at);
             }
+            if (kSpread) load(next, next_step);
             constexpr int kProducts = P == Prec::kSplit ? 6 : 4;
 #pragma unroll
             for (int p = 0; p < kProducts; ++p) {
@@ -236,18 +245,22 @@ struct MfmaTile {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fa[qa][i], fb[qb][j], acc[i][j]);
             }
-            // the first quarter's reads, then one read for every few products
+            // the first quarter's reads, then one read (and, spread, one load)
+            // for every few products
             constexpr int kReads = 4 * (TM + TN), kFirst = TM + TN + 1;
             constexpr int kAll = kProducts * TM * TN * (P == Prec::kFp32 ? 4 : 1);
-            constexpr int kEach = kAll * 3 / 4 / (kReads - kFirst);
+            constexpr int kSlots = kSpread && kLoads > kReads - kFirst ? kLoads : kReads - kFirst;
+            constexpr int kEach = kAll * 3 / 4 / kSlots;
             __builtin_amdgcn_sched_group_barrier(0x100, kFirst, 0);
 #pragma unroll
-            for (int x = 0; x < kReads - kFirst; ++x) {
+            for (int x = 0; x < kSlots; ++x) {
                 __builtin_amdgcn_sched_group_barrier(0x8, kEach > 0 ? kEach : 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (x < kReads - kFirst) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (kSpread && x < kLoads) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(0x8, kAll, 0);
         }
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // the loads that nothing reads
     }
 };
 

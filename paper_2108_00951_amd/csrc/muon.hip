@@ -90,8 +90,8 @@ __host__ __device__ inline int64_t chunk_of(int64_t size) {
     return ((size + c - 1) / c + 3) / 4 * 4;
 }
 
-// Bytes of one X and of one X^T, A and B.
-__host__ __device__ inline int64_t x_bytes(int64_t m, int64_t n) { return m * row_bytes<Prec::kSplit>(n); }
+// Bytes of one X, X^T, A or B.
+__host__ __device__ inline int64_t x_bytes(int64_t rows, int64_t len) { return rows * row_bytes<Prec::kSplit>(len); }
 
 __host__ __device__ inline int64_t operand_bytes(int32_t rows, int32_t cols) {
     const int64_t m = low(rows, cols), n = high(rows, cols);
@@ -100,7 +100,7 @@ __host__ __device__ inline int64_t operand_bytes(int32_t rows, int32_t cols) {
 
 // How many workgroups share a tile of X X^T, with about `most` steps each.
 __host__ __device__ inline int32_t splits_of(int32_t rows, int32_t cols, int32_t most) {
-    const int64_t steps = row_bytes<Prec::kSplit>(high(rows, cols)) / kStepBytes;
+    const int64_t steps = steps_of<Prec::kSplit>(high(rows, cols));
     const int64_t s = (steps + most / 2) / most;
     return int32_t(s < 1 ? 1 : s);
 }
@@ -175,6 +175,10 @@ struct Operands {
     __device__ char *xt(int k) const { return base + 2 * m * x_row + k * n * t_row; }
     __device__ char *a() const { return xt(2); }
     __device__ char *b() const { return a() + m * t_row; }
+    __device__ Operand x_operand(int k) const { return Operand{x(k), x_row, int32_t(m)}; }
+    __device__ Operand xt_operand(int k) const { return Operand{xt(k), t_row, int32_t(n)}; }
+    __device__ Operand a_operand() const { return Operand{a(), t_row, int32_t(m)}; }
+    __device__ Operand b_operand() const { return Operand{b(), t_row, int32_t(m)}; }
 };
 
 // The table.  Entry nmat holds the totals.  `first`: the matrices before
@@ -224,7 +228,7 @@ __global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, Giv
 // The last matrix whose count starts at or before `at`: none of them is
 // empty, so the starts differ.
 template <class F>
-__device__ __forceinline__ int32_t matrix_of(const Mat *table, int32_t nmat, int32_t at, F start) {
+__device__ __forceinline__ int32_t matrix_of(const Mat *__restrict__ table, int32_t nmat, int32_t at, F start) {
     int32_t lo = 0, hi = nmat;
     while (hi - lo > 1) {
         const int32_t mid = (lo + hi) / 2;
@@ -296,7 +300,7 @@ __device__ __forceinline__ void write_out8(const Io &io, int64_t at, int32_t lef
 
 // First pass: the momentum in place, and each chunk's sum of u^2 in binary64
 // (a fixed order: the same sum every time).
-__global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *table, int32_t nmat, Io io,
+__global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *__restrict__ table, int32_t nmat, Io io,
                                                                   double *sums) {
     __shared__ double s_f64[kWaves];
     const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.chunks; });
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *tab
 
 // Second pass: u / (||u|| + eps) as X and X^T, a 64 x 64 tile of the caller's
 // matrix at a time (turned in LDS).
-__global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, int32_t nmat, Io io,
+__global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restrict__ table, int32_t nmat, Io io,
                                                               const double *sums, char *operands) {
     __shared__ double s_f64[kWaves];
     __shared__ float s_norm;
@@ -378,31 +382,22 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *table, 
     const Operands op(operands, mat);
     const bool wide = mat.rows <= mat.cols;
     // along the caller's rows, then along its columns; a thread writes eight
-    // values of a row, both halves
-    char *along = wide ? op.x(0) : op.xt(0);
-    char *other = wide ? op.xt(0) : op.x(0);
-    const int64_t along_row = wide ? op.x_row : op.t_row, other_row = wide ? op.t_row : op.x_row;
+    // values of a row, both parts
 #pragma unroll
     for (int turn = 0; turn < 2; ++turn) {
-        char *base = turn ? other : along;
-        const int64_t stride = turn ? other_row : along_row;
+        const bool to_x = wide != bool(turn);
+        char *base = to_x ? op.x(0) : op.xt(0);
+        const int64_t stride = to_x ? op.x_row : op.t_row;
         const int32_t row_first = turn ? c0 : r0, col_first = turn ? r0 : c0;
         const int32_t row_end = turn ? mat.cols : mat.rows;
-        const int32_t col_end = (turn ? mat.rows : mat.cols) + 31 & ~31;
+        const int32_t col_end = row_values<Prec::kSplit>(turn ? mat.rows : mat.cols);
         for (int i = tid; i < kPackTile * 8; i += kSumBlock) {
             const int r = turn ? i % kPackTile : i / 8, c = (turn ? i / kPackTile : i % 8) * 8;
             if (row_first + r >= row_end || col_first + c >= col_end) continue;
-            f16x8 hi, lo;
+            float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                _Float16 h, l;
-                split_value(turn ? tile[c + k][r] : tile[r][c + k], h, l);
-                hi[k] = h;
-                lo[k] = l;
-            }
-            char *p = base + (row_first + r) * stride + split_offset(col_first + c);
-            *reinterpret_cast<f16x8 *>(p) = hi;
-            *reinterpret_cast<f16x8 *>(p + 64) = lo;
+            for (int k = 0; k < 8; ++k) v[k] = turn ? tile[c + k][r] : tile[r][c + k];
+            store_split8(base + (row_first + r) * stride, col_first + c, v);
         }
     }
 }
@@ -433,7 +428,7 @@ __device__ __forceinline__ void finish(const Tile &tile, const Target &target, c
     const bool turned = kProduct == kLast && target.turned;
     const int32_t row0 = target.row0, col0 = target.col0;
     const int32_t rows = turned ? n : m, cols = kSym ? m : turned ? m : n;
-    const int32_t padded_cols = (cols + 31) & ~31, padded_rows = (rows + 31) & ~31;
+    const int32_t padded_cols = row_values<Prec::kSplit>(cols), padded_rows = row_values<Prec::kSplit>(rows);
     // what is added to the product: A, or X (turned: X^T)
     const char *add = kProduct == kPolynomial ? op.a() : turned ? op.xt(cur) : op.x(cur);
     const int64_t add_row = kProduct == kPolynomial || turned ? op.t_row : op.x_row;
@@ -505,7 +500,7 @@ __device__ __forceinline__ void finish(const Tile &tile, const Target &target, c
 // `cur`: which pair of buffers holds X.
 template <int kProduct, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_product_kernel(
-    const Mat *table, int32_t nmat, char *operands, int cur, float a, float b, float c, Io io) {
+    const Mat *__restrict__ table, int32_t nmat, char *operands, int cur, float a, float b, float c, Io io) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     constexpr int kKind = Tile::kRows == kTileSide[kTiny] ? kTiny : Tile::kRows == kTileSide[kSmall] ? kSmall : kLarge;
     constexpr bool kSym = kProduct == kGram || kProduct == kPolynomial;
@@ -535,28 +530,26 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_prod
         target.col0 = int32_t(q) * Tile::kCols;
     }
 
-    const Operand x{op.x(cur), op.x_row, m}, xt{op.xt(cur), op.t_row, n};
-    const Operand oa{op.a(), op.t_row, m}, ob{op.b(), op.t_row, m};
     Operand left, right;
-    int32_t steps = int32_t(op.t_row / kStepBytes);
+    int64_t steps = steps_of<Prec::kSplit>(m);
     if (kProduct == kGram) {
-        left = right = x;
-        steps = int32_t(op.x_row / kStepBytes);
+        left = right = op.x_operand(cur);
+        steps = steps_of<Prec::kSplit>(n);
     } else if (kProduct == kPolynomial) {
-        left = right = oa;
+        left = right = op.a_operand();
     } else {
-        left = target.turned ? xt : ob;
-        right = target.turned ? ob : xt;
+        left = target.turned ? op.xt_operand(cur) : op.b_operand();
+        right = target.turned ? op.b_operand() : op.xt_operand(cur);
     }
     Tile tile;
-    tile.run(left, right, target.row0, target.col0, 0, steps, lds);
+    tile.run(left, right, target.row0, target.col0, 0, int32_t(steps), lds);
     finish<kProduct>(tile, target, mat, op, cur, a, b, c, io, lds);
 }
 
 // X X^T of few tiles: several workgroups share a long tile's steps and leave
 // partial sums, as their registers hold them; the join adds them in order.
 template <class Tile>
-__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram_kernel(const Mat *table, int32_t nmat,
+__global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram_kernel(const Mat *__restrict__ table, int32_t nmat,
                                                                                         char *operands, int cur,
                                                                                         int32_t most, f32x4 *parts,
                                                                                         Io io) {
@@ -570,9 +563,9 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram
     const uint32_t u = xcd_place(blockIdx.x - mat.at.units, units);
     const uint32_t t = u % tiles, split = u / tiles;
     const Target target = symmetric_tile<Tile>(t);
-    const int64_t steps = op.x_row / kStepBytes;
+    const int64_t steps = steps_of<Prec::kSplit>(op.n);
     const int32_t lo = int32_t(steps * split / splits), hi = int32_t(steps * (split + 1) / splits);
-    const Operand x{op.x(cur), op.x_row, int32_t(op.m)};
+    const Operand x = op.x_operand(cur);
     Tile tile;
     tile.run(x, x, target.row0, target.col0, lo, hi - lo, lds);
     if (splits == 1) {
@@ -589,7 +582,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram
 
 template <class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram_join_kernel(
-    const Mat *table, int32_t nmat, char *operands, int cur, int32_t most, const f32x4 *parts, Io io) {
+    const Mat *__restrict__ table, int32_t nmat, char *operands, int cur, int32_t most, const f32x4 *parts, Io io) {
     __shared__ __align__(16) char lds[Band<Tile>::kBytes];
     const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.sym[kTiny]; });
     const Mat &mat = table[mi];
@@ -828,8 +821,8 @@ struct Cost {
 };
 
 void add_cost(Cost &cost, int32_t rows, int32_t cols, int32_t times) {
-    const int64_t steps_n = row_bytes<Prec::kSplit>(high(rows, cols)) / kStepBytes;
-    const int64_t steps_m = row_bytes<Prec::kSplit>(low(rows, cols)) / kStepBytes;
+    const int64_t steps_n = steps_of<Prec::kSplit>(high(rows, cols));
+    const int64_t steps_m = steps_of<Prec::kSplit>(low(rows, cols));
     Place one = {};
     advance(one, rows, cols, INT32_MAX);
     for (int p = 0; p < 3; ++p) {
@@ -842,7 +835,7 @@ void add_cost(Cost &cost, int32_t rows, int32_t cols, int32_t times) {
 // The steps of X X^T that a workgroup takes where tiles are split, INT32_MAX
 // where they are not: for three workgroups a compute unit, but 24 at least.
 // Splitting costs a launch and the partial sums' way to memory and back, about
-// 10 us (LSTM-sized gates, 330 tiles of 82 to 157 steps: 87 -> 46 us).
+// 10 us (LSTM-sized gates, 330 tiles of 82 to 157 steps: 87 -> 59 us).
 int32_t split_steps(const Cost &cost) {
     const double whole = product_time(best_tile(cost.work[0], cost.longest[0]),
                                       cost.work[0][best_tile(cost.work[0], cost.longest[0])], cost.longest[0]);
@@ -904,8 +897,9 @@ void launch_product(const Job &job, const Mat *table, char *operands, f32x4 *par
     constexpr int kCost = kProduct == kGram ? 0 : kProduct == kPolynomial ? 1 : 2;
     auto run = [&](auto tile, int kind) {
         using Tile = decltype(tile);
-        muon_product_kernel<kProduct, Tile><<<kSym ? job.end.sym[kind] : job.end.full[kind], Tile::kThreads, 0, stream>>>(
-            table, job.nmat, operands, cur, a, b, c, io);
+        muon_product_kernel<kProduct, Tile>
+            <<<kSym ? job.end.sym[kind] : job.end.full[kind], Tile::kThreads, 0, stream>>>(table, job.nmat, operands,
+                                                                                           cur, a, b, c, io);
     };
     switch (best_tile(job.cost.work[kCost], job.cost.longest[kCost])) {
         case kTiny: return run(TinyTile<Prec::kSplit>(), kTiny);

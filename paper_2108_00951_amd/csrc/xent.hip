@@ -113,9 +113,13 @@ struct Xent {
 // Control words at the workspace's start.
 struct Control {
     uint32_t status;
-    uint32_t top[3];   // bits of the largest finite |h|, |w|, |dloss h|
+    // bits of the largest finite |h|, |w|, |dloss h|: the largest of 16 words
+    // each (2048 workgroups' atomics on one word took 27 us)
+    uint32_t top[3][16];
 };
 enum { kTopH, kTopW, kTopWeighted };
+constexpr int kControlBytes = 256;
+static_assert(sizeof(Control) <= kControlBytes, "control words");
 
 // -1: the token does not count.
 __device__ __forceinline__ int32_t target_of(const Xent &x, int32_t t) {
@@ -124,7 +128,10 @@ __device__ __forceinline__ int32_t target_of(const Xent &x, int32_t t) {
 }
 
 // Exponent that brings a tensor's largest magnitude to [2^14, 2^15).
-__device__ __forceinline__ int scale_exponent(uint32_t top) {
+__device__ __forceinline__ int scale_exponent(const uint32_t (&words)[16]) {
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, words[i]);
     return top == 0u ? 0 : 141 - max(int(top >> 23), 1);
 }
 
@@ -146,12 +153,12 @@ __global__ __launch_bounds__(kCheckBlock) void xent_check_kernel(Xent x, Control
     if (bad) s_bad = kXentBadTarget;
     __syncthreads();
     if (threadIdx.x == 0) control->status = s_bad;
-    if (threadIdx.x < 3) control->top[threadIdx.x] = 0u;
+    if (threadIdx.x < 48) control->top[threadIdx.x / 16][threadIdx.x % 16] = 0u;
 }
 
 // Largest finite magnitudes.  Workgroups [0, w_blocks) sweep w, the others h
-// (rows that count) and, with dloss, dloss h.  A wave takes a row at a time,
-// eight elements a lane.
+// (rows that count) and, with dloss, dloss h.  Eight elements a lane; rows with
+// gaps, and those of h, are a wave's each.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const float *dloss, uint32_t w_blocks,
                                                               Control *control) {
@@ -159,36 +166,58 @@ __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const floa
     const bool of_w = blockIdx.x < w_blocks;
     const uint32_t block = of_w ? blockIdx.x : blockIdx.x - w_blocks;
     const uint32_t blocks = of_w ? w_blocks : gridDim.x - w_blocks;
-    const void *base = of_w ? x.w : x.h;
-    const int64_t ld = of_w ? x.ld_w : x.ld_h;
-    const int32_t rows = of_w ? x.vocab : x.tokens;
-    const int lane = threadIdx.x & (kWave - 1);
     uint32_t top = 0u, weighted = 0u;
-    for (int64_t r = int64_t(block) * kWaves + threadIdx.x / kWave; r < rows; r += int64_t(blocks) * kWaves) {
-        if (!of_w && target_of(x, int32_t(r)) < 0) continue;
-        const float f = !of_w && dloss != nullptr ? dloss[r] : 0.0f;
-        int32_t c = lane * 8;
-        for (; c + 8 <= x.hidden; c += kWave * 8) {
-            float v[8];
-            load8<P>(base, r * ld + c, v);
+    if (of_w && x.ld_w == x.hidden) {   // without gaps: one vector
+        const int64_t size = int64_t(x.vocab) * x.hidden;
+        const int64_t step = int64_t(blocks) * kPackBlock * 8;
+        int64_t i = (int64_t(block) * kPackBlock + threadIdx.x) * 8;
+        for (; i + step + 8 <= size; i += 2 * step) {
+            float v[2][8];
+            load8<P>(x.w, i, v[0]);
+            load8<P>(x.w, i + step, v[1]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                top = max(top, finite_bits(v[k]));
-                weighted = max(weighted, finite_bits(__fmul_rn(f, v[k])));
-            }
+            for (int k = 0; k < 8; ++k) top = max(top, max(finite_bits(v[0][k]), finite_bits(v[1][k])));
         }
-        for (; c < x.hidden; ++c) {   // the row's last elements, of one lane
-            const float v = element<P>(base, r * ld + c);
-            top = max(top, finite_bits(v));
-            weighted = max(weighted, finite_bits(__fmul_rn(f, v)));
+        for (; i < size; i += step) {
+            float v[8] = {};
+            if (i + 8 <= size) load8<P>(x.w, i, v);
+            else
+                for (int k = 0; k < 8; ++k)
+                    if (i + k < size) v[k] = element<P>(x.w, i + k);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = max(top, finite_bits(v[k]));
+        }
+    } else {
+        const void *base = of_w ? x.w : x.h;
+        const int64_t ld = of_w ? x.ld_w : x.ld_h;
+        const int32_t rows = of_w ? x.vocab : x.tokens;
+        const int lane = threadIdx.x & (kWave - 1);
+        for (int64_t r = int64_t(block) * kWaves + threadIdx.x / kWave; r < rows; r += int64_t(blocks) * kWaves) {
+            if (!of_w && target_of(x, int32_t(r)) < 0) continue;
+            const float f = !of_w && dloss != nullptr ? dloss[r] : 0.0f;
+            int32_t c = lane * 8;
+            for (; c + 8 <= x.hidden; c += kWave * 8) {
+                float v[8];
+                load8<P>(base, r * ld + c, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    top = max(top, finite_bits(v[k]));
+                    weighted = max(weighted, finite_bits(__fmul_rn(f, v[k])));
+                }
+            }
+            for (; c < x.hidden; ++c) {   // the row's last elements, of one lane
+                const float v = element<P>(base, r * ld + c);
+                top = max(top, finite_bits(v));
+                weighted = max(weighted, finite_bits(__fmul_rn(f, v)));
+            }
         }
     }
     top = block_max(top, s_wave);
     __syncthreads();
     weighted = block_max(weighted, s_wave);
     if (threadIdx.x == 0) {
-        atomicMax(&control->top[of_w ? kTopW : kTopH], top);
-        if (!of_w) atomicMax(&control->top[kTopWeighted], weighted);
+        atomicMax(&control->top[of_w ? kTopW : kTopH][block % 16], top);
+        if (!of_w) atomicMax(&control->top[kTopWeighted][block % 16], weighted);
     }
 }
 
@@ -197,7 +226,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const floa
 // that do not count are zeros.  The turned h holds dloss h.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w, const float *dloss, char *along,
-                                                               char *turned, const Control *control) {
+                                                               char *turned, const Control *__restrict__ control) {
     constexpr Prec G = kGradOf<P>;
     __shared__ float tile[kPackTile][kPackTile + 1];
     __shared__ float s_weight[kPackTile];
@@ -231,7 +260,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
     if (along != nullptr) {
         const int exponent = P == Prec::kSplit ? scale_exponent(control->top[of_w ? kTopW : kTopH]) : 0;
         const int64_t stride = row_bytes<P>(cols);
-        const int32_t end = int32_t(stride / kStepBytes) * kStepValues<P>;
+        const int32_t end = row_values<P>(cols);
         for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
             const int r = i / 8, c = i % 8 * 8;
             if (r0 + r >= rows || c0 + c >= end) continue;
@@ -244,7 +273,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
     if (turned != nullptr) {
         const int exponent = scale_exponent(control->top[of_w ? kTopW : kTopWeighted]);
         const int64_t stride = row_bytes<G>(rows);
-        const int32_t end = int32_t(stride / kStepBytes) * kStepValues<G>;
+        const int32_t end = row_values<G>(rows);
         for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
             const int r = i / 8, c = i % 8 * 8;   // of the turned tile
             if (c0 + r >= cols || r0 + c >= end) continue;
@@ -269,7 +298,7 @@ __device__ __forceinline__ Part join(Part a, Part b) {
 
 // The logits of a tile: rows are words, columns tokens.
 template <Prec P>
-__device__ __forceinline__ int logit_exponent(const Control *control) {
+__device__ __forceinline__ int logit_exponent(const Control *__restrict__ control) {
     return P == Prec::kSplit ? -(scale_exponent(control->top[kTopH]) + scale_exponent(control->top[kTopW])) : 0;
 }
 
@@ -281,7 +310,7 @@ __device__ __forceinline__ float logit(float acc, int exponent) {
 // Forward: parts[tile row][token], and the targets' logits.
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forward_kernel(Xent x, Operand w, Operand h,
-                                                                         const Control *control, Part *parts,
+                                                                         const Control *__restrict__ control, Part *parts,
                                                                          float *target_logit) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (x.vocab + Tile::kRows - 1) / Tile::kRows, tt = (x.tokens + Tile::kCols - 1) / Tile::kCols;
@@ -289,7 +318,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forw
     banded(xcd_place(blockIdx.x, gridDim.x), tv, tt, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
     Tile tile;
-    tile.run(w, h, row0, col0, 0, int32_t(row_bytes<P>(x.hidden) / kStepBytes), lds);
+    tile.run(w, h, row0, col0, 0, int32_t(steps_of<P>(x.hidden)), lds);
     const int exponent = logit_exponent<P>(control);
     Part *s_part = reinterpret_cast<Part *>(lds);   // [rows of waves][columns]
     constexpr int kHigh = Tile::kRows / (Tile::kTilesM * 32);
@@ -384,19 +413,18 @@ __global__ __launch_bounds__(kPackBlock) void xent_join_few_kernel(Xent x, const
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad_kernel(Xent x, Operand w, Operand h, int32_t v0,
                                                                       int32_t words, const float *lse,
-                                                                      const Control *control, char *g, char *gt) {
+                                                                      const Control *__restrict__ control, char *g, char *gt) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (words + Tile::kRows - 1) / Tile::kRows, tt = (x.tokens + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
     banded(xcd_place(blockIdx.x, gridDim.x), tv, tt, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
     Tile tile;
-    tile.run(w, h, row0, col0, 0, int32_t(row_bytes<P>(x.hidden) / kStepBytes), lds);
+    tile.run(w, h, row0, col0, 0, int32_t(steps_of<P>(x.hidden)), lds);
     const int exponent = logit_exponent<P>(control);
     constexpr Prec G = kGradOf<P>;
     const int64_t g_row = row_bytes<G>(words), gt_row = row_bytes<G>(x.tokens);
-    const int32_t words_end = int32_t(g_row / kStepBytes) * kStepValues<G>;
-    const int32_t tokens_end = int32_t(gt_row / kStepBytes) * kStepValues<G>;
+    const int32_t words_end = row_values<G>(words), tokens_end = row_values<G>(x.tokens);
 #pragma unroll
     for (int j = 0; j < Tile::kTilesN; ++j) {
         const int32_t t = col0 + Tile::col_of(j);
@@ -445,14 +473,14 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad
 // dw rows [v0, v0 + words) = g^T h.
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dw_kernel(Xent x, Operand gt, Operand ht, int32_t v0,
-                                                                    const Control *control, void *dw, int64_t ld) {
+                                                                    const Control *__restrict__ control, void *dw, int64_t ld) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (gt.rows + Tile::kRows - 1) / Tile::kRows, th = (x.hidden + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
     banded(xcd_place(blockIdx.x, gridDim.x), tv, th, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
     Tile tile;
-    tile.run(gt, ht, row0, col0, 0, int32_t(row_bytes<kGradOf<P>>(x.tokens) / kStepBytes), lds);
+    tile.run(gt, ht, row0, col0, 0, int32_t(steps_of<kGradOf<P>>(x.tokens)), lds);
     const int exponent = -(kGradShift + scale_exponent(control->top[kTopWeighted]));
 #pragma unroll
     for (int i = 0; i < Tile::kTilesM; ++i)
@@ -501,7 +529,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dh_k
 // dh from its partial sums.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const float *part, int32_t splits,
-                                                                  const float *dloss, const Control *control,
+                                                                  const float *dloss, const Control *__restrict__ control,
                                                                   void *dh, int64_t ld) {
     const int exponent = -(kGradShift + scale_exponent(control->top[kTopW]));
     const int64_t size = int64_t(x.tokens) * x.hidden;
@@ -527,7 +555,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_few_
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const int32_t row0 = int32_t(blockIdx.x) * Tile::kRows;
     Tile tile;
-    tile.run(w, h, row0, 0, 0, int32_t(row_bytes<P>(x.hidden) / kStepBytes), lds);
+    tile.run(w, h, row0, 0, 0, int32_t(steps_of<P>(x.hidden)), lds);
 #pragma unroll
     for (int j = 0; j < Tile::kTilesN; ++j) {
         const int32_t t = Tile::col_of(j);
@@ -555,20 +583,36 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_few_
 
 // Few tokens: dw, and dh's partial sums.  A workgroup takes 256 values of the
 // hidden axis (a wave 64, a lane four neighbours: column c of product j is
-// value 4 c + j) and every splits-th block of 32 words.  Both products run on
-// the 16 x 16 x 4 fp32 instruction, whose operands are one value a lane, so
-// that w's rows serve as they come from memory:
+// value 4 c + j) and every splits-th block of 32 words.
 //   dw[word][value]  = sum over tokens  g[word][token] h[token][value]
 //   dh[token][value] += sum over words  g[token][word] w[word][value]
-// with dh and h in registers throughout.  16 kTok tokens at most.
+// with dh and h in registers throughout, 16 kTok tokens at most.  w's rows serve
+// as they come from memory: a lane loads four values of words four, four + 4,
+// .., four + 28 of the block (four = lane / 16), and that is what an
+// instruction takes of column 4 c + j, if the other operand's words are in the
+// same order.
+//   fp32: eight 16 x 16 x 4 instructions, a word of each lane each.
+//   bf16: one 16 x 16 x 32 instruction for g's high part and one for its low
+//   part (g = hi + lo in bf16, 16 bits of it); w and h are exact.  With the fp32
+//   instructions a step of 16 tokens took 92 us here, the matrix cores 42.
 constexpr int kFewHidden = 256, kFewWords = 32;
 
+__device__ __forceinline__ f32x4 mfma_16(bf16x8 a, bf16x8 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
 template <Prec P, int kTok>
-__global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, const float *g, int64_t words_end,
-                                                                       int32_t splits, void *dw, int64_t ld_dw,
-                                                                       float *part) {
+__global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, const float *__restrict__ g,
+                                                                       int64_t words_end, int32_t splits,
+                                                                       void *__restrict__ dw, int64_t ld_dw,
+                                                                       float *__restrict__ part) {
+    constexpr bool kWide = P == Prec::kBf16;
     constexpr int kTokens = 16 * kTok, kStride = kFewWords + 1;
+    // bf16: tokens in steps of the wide instruction's 32
+    constexpr int kSteps = kWide ? (kTokens + 31) / 32 : 4 * kTok;
     __shared__ float s_g[2][kTokens * kStride];
+    typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+    using Vec = std::conditional_t<kWide, bf16x4u, f32x4>;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int col = lane & 15, four = lane >> 4;
     const int32_t split = int32_t(blockIdx.x) % splits;
@@ -576,21 +620,22 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, c
     const int32_t left = min(4, x.hidden - k0);   // of which exist
 
     auto load4 = [&](const void *base, int64_t at, bool there) {
-        f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+        Vec v = {};
         if (!there) return v;
-        if (left == 4) {
-            if constexpr (P == Prec::kBf16) {
-                typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
-                const bf16x4u b = *reinterpret_cast<const bf16x4u *>(static_cast<const __bf16 *>(base) + at);
+        if constexpr (kWide) {
+            const __bf16 *p = static_cast<const __bf16 *>(base) + at;
+            if (left == 4) v = *reinterpret_cast<const bf16x4u *>(p);
+            else
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = float(b[k]);
-            } else {
-                v = *reinterpret_cast<const f32x4u *>(static_cast<const float *>(base) + at);
-            }
+                for (int k = 0; k < 3; ++k)
+                    if (k < left) v[k] = p[k];
         } else {
+            const float *p = static_cast<const float *>(base) + at;
+            if (left == 4) v = *reinterpret_cast<const f32x4u *>(p);
+            else
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k < left) v[k] = element<P>(base, at + k);
+                for (int k = 0; k < 3; ++k)
+                    if (k < left) v[k] = p[k];
         }
         return v;
     };
@@ -604,12 +649,39 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, c
             next[i] = t < x.tokens ? g[t * words_end + int64_t(block) * kFewWords + v] : 0.0f;
         }
     };
-
-    f32x4 h[4 * kTok], dh[kTok][4];
+    auto rows_of_w = [&](int32_t block, Vec (&w)[8]) {
 #pragma unroll
-    for (int s = 0; s < 4 * kTok; ++s) {
-        const int32_t t = 4 * s + four;
-        h[s] = load4(x.h, t * x.ld_h + k0, t < x.tokens && left > 0 && target_of(x, t) >= 0);
+        for (int s = 0; s < 8; ++s) {
+            const int32_t v = block * kFewWords + 4 * s + four;
+            w[s] = load4(x.w, v * x.ld_w + k0, v < x.vocab && left > 0);
+        }
+    };
+    // column j of eight rows, as the wide instruction takes it
+    auto column = [](const Vec (&v)[8], int j) {
+        bf16x8 b;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) b[s] = __bf16(v[s][j]);
+        return b;
+    };
+
+    // h, once: token 4 s + four of each step, or 32 step + 4 i + four
+    Vec h_narrow[kWide ? 1 : kSteps];
+    bf16x8 h_wide[kWide ? kSteps : 1][4];
+    f32x4 dh[kTok][4];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        auto row = [&](int32_t t) {
+            return load4(x.h, t * x.ld_h + k0, t < x.tokens && left > 0 && target_of(x, t) >= 0);
+        };
+        if constexpr (kWide) {
+            Vec v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = row(32 * s + 4 * i + four);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h_wide[s][j] = column(v, j);
+        } else {
+            h_narrow[s] = row(4 * s + four);
+        }
     }
 #pragma unroll
     for (int t = 0; t < kTok; ++t)
@@ -618,7 +690,11 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, c
 
     const int32_t blocks = (x.vocab + kFewWords - 1) / kFewWords;
     int turn = 0;
-    if (split < blocks) fetch(split);
+    Vec w[8];
+    if (split < blocks) {
+        fetch(split);
+        rows_of_w(split, w);
+    }
     for (int32_t block = split; block < blocks; block += splits, turn ^= 1) {
         float *sg = s_g[turn];   // the other one may still be read
 #pragma unroll
@@ -627,55 +703,90 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, c
             sg[t * kStride + v] = next[i];
         }
         const int32_t v0 = block * kFewWords;
-        f32x4 w[kFewWords / 4];
-#pragma unroll
-        for (int s = 0; s < kFewWords / 4; ++s) {
-            const int32_t v = v0 + 4 * s + four;
-            w[s] = load4(x.w, v * x.ld_w + k0, v < x.vocab && left > 0);
-        }
-        if (block + splits < blocks) fetch(block + splits);
         __syncthreads();
+        // dh first: its rows of w make room for the next block's
+        if constexpr (kWide) {
+            bf16x8 b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = column(w, j);
+            if (block + splits < blocks) {
+                fetch(block + splits);
+                rows_of_w(block + splits, w);
+            }
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) {
+                bf16x8 hi, lo;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = sg[(t * 16 + col) * kStride + 4 * i + four];
+                    hi[i] = __bf16(v);
+                    lo[i] = __bf16(__fsub_rn(v, float(hi[i])));
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) dh[t][j] = mfma_16(lo, b[j], mfma_16(hi, b[j], dh[t][j]));
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int t = 0; t < kTok; ++t) {
+                    const float a = sg[(t * 16 + col) * kStride + 4 * s + four];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        dh[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[s][j], dh[t][j], 0, 0, 0);
+                }
+            if (block + splits < blocks) {
+                fetch(block + splits);
+                rows_of_w(block + splits, w);
+            }
+        }
         // dw: two rows of 16 words, four columns of 16 values
 #pragma unroll
         for (int r = 0; r < kFewWords / 16; ++r) {
             f32x4 acc[4] = {};
 #pragma unroll
-            for (int s = 0; s < 4 * kTok; ++s) {
-                const float a = sg[(4 * s + four) * kStride + r * 16 + col];
+            for (int s = 0; s < kSteps; ++s) {
+                if constexpr (kWide) {
+                    bf16x8 hi, lo;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, h[s][j], acc[j], 0, 0, 0);
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = 32 * s + 4 * i + four;
+                        const float v = t < kTokens ? sg[t * kStride + r * 16 + col] : 0.0f;
+                        hi[i] = __bf16(v);
+                        lo[i] = __bf16(__fsub_rn(v, float(hi[i])));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[j] = mfma_16(lo, h_wide[s][j], mfma_16(hi, h_wide[s][j], acc[j]));
+                } else {
+                    const float a = sg[(4 * s + four) * kStride + r * 16 + col];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, h_narrow[s][j], acc[j], 0, 0, 0);
+                }
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int32_t v = v0 + r * 16 + four * 4 + e;
                 if (v >= x.vocab || left <= 0) continue;
                 const int64_t at = v * ld_dw + k0;
-                if constexpr (P == Prec::kBf16) {
-                    typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(2)));
+                if constexpr (kWide) {
                     __bf16 *p = static_cast<__bf16 *>(dw) + at;
                     const bf16x4u y = {__bf16(acc[0][e]), __bf16(acc[1][e]), __bf16(acc[2][e]), __bf16(acc[3][e])};
                     if (left == 4) *reinterpret_cast<bf16x4u *>(p) = y;
                     else
-                        for (int j = 0; j < left; ++j) p[j] = __bf16(j == 0 ? acc[0][e] : j == 1 ? acc[1][e] : acc[2][e]);
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (j < left) p[j] = y[j];
                 } else {
                     float *p = static_cast<float *>(dw) + at;
                     if (left == 4) *reinterpret_cast<f32x4u *>(p) = f32x4u{acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
                     else
-                        for (int j = 0; j < left; ++j) p[j] = j == 0 ? acc[0][e] : j == 1 ? acc[1][e] : acc[2][e];
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (j < left) p[j] = acc[j][e];
                 }
             }
         }
-        // dh
-#pragma unroll
-        for (int s = 0; s < kFewWords / 4; ++s)
-#pragma unroll
-            for (int t = 0; t < kTok; ++t) {
-                const float a = sg[(t * 16 + col) * kStride + 4 * s + four];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    dh[t][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, w[s][j], dh[t][j], 0, 0, 0);
-            }
     }
     float *to = part + int64_t(split) * x.tokens * x.hidden;
 #pragma unroll
@@ -692,7 +803,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_products_kernel(Xent x, c
 
 // dh of few tokens from its partial sums.
 template <Prec P>
-__global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const float *part, int32_t splits, void *dh,
+__global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const float *__restrict__ part, int32_t splits, void *__restrict__ dh,
                                                                    int64_t ld, Control *control) {
     __shared__ float s_sum[kWaves][kWave];
     if (blockIdx.x == 0 && threadIdx.x < kWave) {   // the status word: 64 tokens at most
@@ -710,6 +821,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const
     const int64_t i = int64_t(blockIdx.x) * kWave + lane;
     float v = 0.0f;
     if (i < size)
+#pragma unroll 8
         for (int32_t s = wave; s < splits; s += kWaves) v = __fadd_rn(v, part[s * size + i]);
     s_sum[wave][lane] = v;
     __syncthreads();
@@ -760,14 +872,15 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     int64_t piece = kPieceBytes / word / kTile * kTile;
     if (piece < 4 * kTile) piece = 4 * kTile;
     p.piece = int32_t(piece < vocab ? piece : vocab);
-    // enough workgroups for the compute units, with eight steps each at least
+    // as many as two workgroups a compute unit take in one round, with eight
+    // steps each at least
     const int64_t dh_tiles = tiles(tokens, kTileSide[kSmall]) * tiles(hidden, kTileSide[kSmall]);
-    const int64_t steps = row_bytes<G>(p.piece) / kStepBytes;
-    int64_t splits = (512 + dh_tiles - 1) / dh_tiles;
+    const int64_t steps = steps_of<G>(p.piece);
+    int64_t splits = 512 / dh_tiles;
     if (splits > steps / 8) splits = steps / 8;
     p.splits = int32_t(splits < 1 ? 1 : splits);
 
-    int64_t at = 256;
+    int64_t at = kControlBytes;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += round256(bytes);
@@ -779,9 +892,9 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     p.w_along = take(vocab * row_bytes<P>(hidden));
     p.forward = at;
     if (tokens <= kFewTokens) {
-        // two rounds of the three workgroups that a compute unit holds, with
-        // eight blocks of words each at least
-        int64_t n = tiles(1536, int(tiles(hidden, kFewHidden)));
+        // the workgroups that three to a compute unit make, with eight blocks of
+        // words each at least
+        int64_t n = tiles(768, int(tiles(hidden, kFewHidden)));
         n = std::min(n, tiles(vocab, kFewWords * 8));
         p.few_splits = int32_t(n);
         p.few_g = take(tokens * tiles(vocab, 64) * 64 * 4);
@@ -837,7 +950,8 @@ void pack_operands(const Xent &x, const float *dloss, bool gradient, const Plan 
             xent_pack_kernel<P><<<uint32_t(blocks), kPackBlock, 0, stream>>>(
                 x, of_w, dloss, in_place ? nullptr : ws + along, gradient ? ws + turned : nullptr, control);
         }
-        return in_place ? Operand{static_cast<const char *>(p), ld * kSize, rows} : Operand{ws + along, row, rows};
+        return in_place ? Operand{static_cast<const char *>(p), ld * kSize, rows}
+                        : Operand{ws + along, row, rows};
     };
     *h = pack(false, x.h, x.ld_h, x.tokens, plan.h_along, plan.h_turned);
     *w = pack(true, x.w, x.ld_w, x.vocab, plan.w_along, plan.w_turned);
@@ -910,7 +1024,7 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
 template <Prec P>
 hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t stream) {
     const Plan plan = plan_of<P>(x.tokens, x.vocab, x.hidden);
-    const Control *control = reinterpret_cast<const Control *>(ws);
+    const Control *__restrict__ control = reinterpret_cast<const Control *>(ws);
     Part *parts = reinterpret_cast<Part *>(ws + plan.parts);
     float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
     constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
@@ -919,7 +1033,7 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
     check_and_scale<P>(x, nullptr, false, ws, stream);
     pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
     int32_t nparts = 0;
-    with_tile<P>(x.vocab, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
+    with_tile<P>(x.vocab, x.tokens, 1, steps_of<P>(x.hidden), [&](auto tile, int64_t blocks) {
         using Tile = decltype(tile);
         nparts = int32_t(tiles(x.vocab, Tile::kRows));
         xent_forward_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
@@ -935,32 +1049,34 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
                     int64_t ld_dw, char *ws, hipStream_t stream) {
     constexpr Prec G = kGradOf<P>;
     const Plan plan = plan_of<P>(x.tokens, x.vocab, x.hidden);
-    const Control *control = reinterpret_cast<const Control *>(ws);
+    const Control *__restrict__ control = reinterpret_cast<const Control *>(ws);
     constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
     if (x.tokens <= kFewTokens) return backward_few<F>(x, plan, lse, dloss, dh, ld_dh, dw, ld_dw, ws, stream);
     Operand h, w;
     check_and_scale<P>(x, dloss, true, ws, stream);
     pack_operands<P>(x, dloss, true, plan, ws, &h, &w, stream);
-    const Operand ht{ws + plan.h_turned, row_bytes<G>(x.tokens), x.hidden};
+    const int64_t t_row = row_bytes<G>(x.tokens), v_row = row_bytes<G>(x.vocab);
+    const Operand ht{ws + plan.h_turned, t_row, x.hidden};
     float *part = reinterpret_cast<float *>(ws + plan.dh);
     for (int64_t v0 = 0; v0 < x.vocab; v0 += plan.piece) {
         const int32_t words = int32_t(std::min<int64_t>(plan.piece, x.vocab - v0));
         const Operand w_piece{w.base + v0 * w.stride, w.stride, words};
-        with_tile<P>(words, x.tokens, 1, row_bytes<P>(x.hidden) / kStepBytes, [&](auto tile, int64_t blocks) {
+        with_tile<P>(words, x.tokens, 1, steps_of<P>(x.hidden), [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_grad_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(
                 x, w_piece, h, int32_t(v0), words, lse, control, ws + plan.g, ws + plan.gt);
         });
-        const Operand gt{ws + plan.gt, row_bytes<G>(x.tokens), words};
-        with_tile<G>(words, x.hidden, 1, row_bytes<G>(x.tokens) / kStepBytes, [&](auto tile, int64_t blocks) {
+        const Operand gt{ws + plan.gt, t_row, words};
+        with_tile<G>(words, x.hidden, 1, steps_of<G>(x.tokens), [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dw_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, gt, ht, int32_t(v0), control,
                                                                                      dw, ld_dw);
         });
         // a piece starts on a whole step of w^T: it is a multiple of 256 words
-        const Operand g{ws + plan.g, row_bytes<G>(words), x.tokens};
-        const Operand wt{ws + plan.w_turned + row_bytes<G>(v0), row_bytes<G>(x.vocab), x.hidden};
-        const int32_t steps = int32_t(row_bytes<G>(words) / kStepBytes);
+        const int64_t g_row = row_bytes<G>(words);
+        const Operand g{ws + plan.g, g_row, x.tokens};
+        const Operand wt{ws + plan.w_turned + row_bytes<G>(v0), v_row, x.hidden};
+        const int32_t steps = int32_t(steps_of<G>(words));
         with_tile<G>(x.tokens, x.hidden, plan.splits, steps / plan.splits, [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dh_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, g, wt, steps, plan.splits,
