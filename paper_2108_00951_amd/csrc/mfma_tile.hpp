@@ -362,12 +362,12 @@ constexpr int kTileSide[kTileKinds] = {64, 128, 256};
 
 // What a product over tiles of one kind takes, in microseconds: `work` tiles
 // times steps in all, `longest` steps of one tile.  Measured on kSplit steps:
-// a tile's step takes 0.32, 0.63 and 1.7 us on its own, and 0.25, 0.70 and 2.4
-// us of a compute unit where all are busy (270, 380 and 440 TFLOP/s), so that
+// a tile's step takes 0.32, 0.63 and 1.7 us on its own, and 0.25, 0.76 and 2.4
+// us of a compute unit where all are busy (270, 350 and 440 TFLOP/s), so that
 // 256 x 1024 x 512 is fastest with the smallest kind (13.6 against 24.2 and 60
 // us), 2048 x 4096 x 1024 with the middle one (63.6, 49.3, 64.8) and 4096 x
 // 4096 x 4096 with the largest.
-constexpr double kStepAlone[kTileKinds] = {0.32, 0.63, 1.7}, kStepBusy[kTileKinds] = {0.25, 0.70, 2.4};
+constexpr double kStepAlone[kTileKinds] = {0.32, 0.63, 1.7}, kStepBusy[kTileKinds] = {0.25, 0.76, 2.4};
 
 inline double product_time(int kind, int64_t work, int64_t longest) {
     if (longest == 0) return 0.0;
