@@ -351,10 +351,10 @@ using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
 template <Prec P>
 using TinyTile = MfmaTile<P, 2, 2, 1, 1, 3>;
 
-// For a few tokens against many rows: 64 x 32 TN by two waves, three steps on
-// their way in each of three or two workgroups a compute unit.
+// For a few tokens against many rows: 64 x 32 TN by two waves, two steps on
+// their way in each of four workgroups a compute unit (TN = 1).
 template <Prec P, int TN>
-using NarrowTile = MfmaTile<P, 2, 1, 1, TN, 4>;
+using NarrowTile = MfmaTile<P, 2, 1, 1, TN, 3>;
 
 enum TileKind { kTiny, kSmall, kLarge };
 constexpr int kTileKinds = 3;

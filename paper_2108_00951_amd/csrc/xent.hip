@@ -44,7 +44,6 @@ namespace {
 
 constexpr int kPackBlock = 256;
 constexpr int kPackTile = 64;
-constexpr int kCheckBlock = 1024;
 constexpr int kJoinTokens = kWave;
 constexpr int kJoinSlices = 16;
 constexpr int kGradShift = 15;          // g's scale
@@ -111,14 +110,18 @@ struct Xent {
 };
 
 // Control words at the workspace's start.
+constexpr int kTopBlocksW = 768, kTopBlocksH = 128;   // workgroups that look for magnitudes, at most
 struct Control {
     uint32_t status;
-    // bits of the largest finite |h|, |w|, |dloss h|: the largest of 16 words
-    // each (2048 workgroups' atomics on one word took 27 us)
-    uint32_t top[3][16];
+    // bits of the largest finite |w|, |h| and |dloss h| that each of those
+    // found; a tensor's magnitude is the largest of them (atomics on one word
+    // would take 13 ns each, one after the other)
+    uint32_t w[kTopBlocksW], h[kTopBlocksH], weighted[kTopBlocksH];
+    // and that (from the pass that lays the tensors out on)
+    uint32_t top[3];
 };
 enum { kTopH, kTopW, kTopWeighted };
-constexpr int kControlBytes = 256;
+constexpr int kControlBytes = 8192;
 static_assert(sizeof(Control) <= kControlBytes, "control words");
 
 // -1: the token does not count.
@@ -128,10 +131,7 @@ __device__ __forceinline__ int32_t target_of(const Xent &x, int32_t t) {
 }
 
 // Exponent that brings a tensor's largest magnitude to [2^14, 2^15).
-__device__ __forceinline__ int scale_exponent(const uint32_t (&words)[16]) {
-    uint32_t top = 0u;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, words[i]);
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
     return top == 0u ? 0 : 141 - max(int(top >> 23), 1);
 }
 
@@ -140,20 +140,15 @@ __device__ __forceinline__ uint32_t finite_bits(float v) {
     return b < 0x7f800000u ? b : 0u;
 }
 
-// One workgroup: the status word, and zeros for the magnitudes.
-__global__ __launch_bounds__(kCheckBlock) void xent_check_kernel(Xent x, Control *control) {
-    __shared__ uint32_t s_bad;
-    if (threadIdx.x == 0) s_bad = 0u;
-    __syncthreads();
+// The status word, by one workgroup.
+__device__ __forceinline__ void write_status(const Xent &x, Control *control) {
     bool bad = false;
-    for (int32_t t = threadIdx.x; t < x.tokens; t += kCheckBlock) {
+    for (int32_t t = threadIdx.x; t < x.tokens; t += blockDim.x) {
         const int64_t v = x.target[t];
         bad |= v != x.ignore && (v < 0 || v >= x.vocab);
     }
-    if (bad) s_bad = kXentBadTarget;
-    __syncthreads();
-    if (threadIdx.x == 0) control->status = s_bad;
-    if (threadIdx.x < 48) control->top[threadIdx.x / 16][threadIdx.x % 16] = 0u;
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) control->status = bad ? kXentBadTarget : 0u;
 }
 
 // Largest finite magnitudes.  Workgroups [0, w_blocks) sweep w, the others h
@@ -168,24 +163,23 @@ __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const floa
     const uint32_t blocks = of_w ? w_blocks : gridDim.x - w_blocks;
     uint32_t top = 0u, weighted = 0u;
     if (of_w && x.ld_w == x.hidden) {   // without gaps: one vector
+        constexpr int kAhead = 4;
         const int64_t size = int64_t(x.vocab) * x.hidden;
         const int64_t step = int64_t(blocks) * kPackBlock * 8;
-        int64_t i = (int64_t(block) * kPackBlock + threadIdx.x) * 8;
-        for (; i + step + 8 <= size; i += 2 * step) {
-            float v[2][8];
-            load8<P>(x.w, i, v[0]);
-            load8<P>(x.w, i + step, v[1]);
+        for (int64_t i = (int64_t(block) * kPackBlock + threadIdx.x) * 8; i < size; i += kAhead * step) {
+            float v[kAhead][8] = {};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = max(top, max(finite_bits(v[0][k]), finite_bits(v[1][k])));
-        }
-        for (; i < size; i += step) {
-            float v[8] = {};
-            if (i + 8 <= size) load8<P>(x.w, i, v);
-            else
-                for (int k = 0; k < 8; ++k)
-                    if (i + k < size) v[k] = element<P>(x.w, i + k);
+            for (int q = 0; q < kAhead; ++q) {
+                const int64_t at = i + q * step;
+                if (at + 8 <= size) load8<P>(x.w, at, v[q]);
+                else
+                    for (int k = 0; k < 8; ++k)
+                        if (at + k < size) v[q][k] = element<P>(x.w, at + k);
+            }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = max(top, finite_bits(v[k]));
+            for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = max(top, finite_bits(v[q][k]));
         }
     } else {
         const void *base = of_w ? x.w : x.h;
@@ -216,21 +210,35 @@ __global__ __launch_bounds__(kPackBlock) void xent_top_kernel(Xent x, const floa
     __syncthreads();
     weighted = block_max(weighted, s_wave);
     if (threadIdx.x == 0) {
-        atomicMax(&control->top[of_w ? kTopW : kTopH][block % 16], top);
-        if (!of_w) atomicMax(&control->top[kTopWeighted][block % 16], weighted);
+        (of_w ? control->w : control->h)[block] = top;
+        if (!of_w) control->weighted[block] = weighted;
     }
+}
+
+// What that found, to every thread of a workgroup.
+template <int kFrom>
+__device__ __forceinline__ uint32_t largest_of(const uint32_t *words, int32_t n, uint32_t *s_wave) {
+    uint32_t top = 0u;
+#pragma unroll
+    for (int i = 0; i < kFrom; i += kPackBlock)
+        if (i + int(threadIdx.x) < n) top = max(top, words[i + threadIdx.x]);
+    top = block_max(top, s_wave);
+    __syncthreads();
+    return top;
 }
 
 // h or w as operands: `along` its rows (for the logits), and `turned`, a row
 // for each of its columns (for the gradients); either may be null.  Rows of h
-// that do not count are zeros.  The turned h holds dloss h.
+// that do not count are zeros.  The turned h holds dloss h.  `found`: the
+// magnitudes of this tensor that the control words hold.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w, const float *dloss, char *along,
-                                                               char *turned, const Control *__restrict__ control) {
+                                                               char *turned, int32_t found, Control *control) {
     constexpr Prec G = kGradOf<P>;
     __shared__ float tile[kPackTile][kPackTile + 1];
     __shared__ float s_weight[kPackTile];
     __shared__ bool s_counts[kPackTile];
+    __shared__ uint32_t s_wave[kWaves];
     const int tid = threadIdx.x;
     const int32_t rows = of_w ? x.vocab : x.tokens, cols = x.hidden;
     const int64_t ld = of_w ? x.ld_w : x.ld_h;
@@ -242,6 +250,15 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
         s_weight[tid] = !of_w && dloss != nullptr && s_counts[tid] ? dloss[r] : 1.0f;
     }
     __syncthreads();
+    uint32_t top = 0u, weighted = 0u;
+    if (found > 0) {
+        top = of_w ? largest_of<kTopBlocksW>(control->w, found, s_wave) : largest_of<kTopBlocksH>(control->h, found, s_wave);
+        weighted = of_w ? top : largest_of<kTopBlocksH>(control->weighted, found, s_wave);
+        if (blockIdx.x == 0 && tid == 0) {   // for the products
+            control->top[of_w ? kTopW : kTopH] = top;
+            if (!of_w) control->top[kTopWeighted] = weighted;
+        }
+    }
     const void *base = of_w ? x.w : x.h;
     for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
         const int r = i / 8, c = i % 8 * 8;
@@ -258,7 +275,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
     }
     __syncthreads();
     if (along != nullptr) {
-        const int exponent = P == Prec::kSplit ? scale_exponent(control->top[of_w ? kTopW : kTopH]) : 0;
+        const int exponent = P == Prec::kSplit ? scale_exponent(top) : 0;
         const int64_t stride = row_bytes<P>(cols);
         const int32_t end = row_values<P>(cols);
         for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
@@ -271,7 +288,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_pack_kernel(Xent x, bool of_w
         }
     }
     if (turned != nullptr) {
-        const int exponent = scale_exponent(control->top[of_w ? kTopW : kTopWeighted]);
+        const int exponent = scale_exponent(weighted);
         const int64_t stride = row_bytes<G>(rows);
         const int32_t end = row_values<G>(rows);
         for (int i = tid; i < kPackTile * 8; i += kPackBlock) {
@@ -362,8 +379,9 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forw
 // A token's parts joined: lanes are tokens, waves take every 16th part.
 __global__ __launch_bounds__(kJoinTokens *kJoinSlices) void xent_join_kernel(Xent x, const Part *parts, int32_t nparts,
                                                                              const float *target_logit, float *loss,
-                                                                             float *lse) {
+                                                                             float *lse, Control *control) {
     __shared__ Part s_part[kJoinSlices][kJoinTokens];
+    if (blockIdx.x == 0) write_status(x, control);
     const int lane = threadIdx.x % kJoinTokens, slice = threadIdx.x / kJoinTokens;
     const int32_t t = int32_t(blockIdx.x) * kJoinTokens + lane;
     Part p = {-INFINITY, 0.0f};
@@ -379,22 +397,13 @@ __global__ __launch_bounds__(kJoinTokens *kJoinSlices) void xent_join_kernel(Xen
     loss[t] = counts ? __fsub_rn(v, target_logit[t]) : 0.0f;
 }
 
-// The same for few tokens: a workgroup each; the first also sets the status word.
+// The same for few tokens: a workgroup each.
 __global__ __launch_bounds__(kPackBlock) void xent_join_few_kernel(Xent x, const Part *parts, int32_t nparts,
                                                                    const float *target_logit, float *loss,
                                                                    float *lse, Control *control) {
     __shared__ Part s_part[kWaves];
-    __shared__ uint32_t s_wave[kWaves];
     const int32_t t = int32_t(blockIdx.x);
-    if (t == 0) {
-        uint32_t bad = 0u;
-        if (threadIdx.x < x.tokens) {
-            const int64_t v = x.target[threadIdx.x];
-            bad = v != x.ignore && (v < 0 || v >= x.vocab) ? kXentBadTarget : 0u;
-        }
-        bad = block_max(bad, s_wave);
-        if (threadIdx.x == 0) control->status = bad;
-    }
+    if (t == 0) write_status(x, control);
     Part p = {-INFINITY, 0.0f};
     for (int32_t i = threadIdx.x; i < nparts; i += kPackBlock) p = join(p, parts[int64_t(i) * x.tokens + t]);
 #pragma unroll
@@ -529,8 +538,9 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dh_k
 // dh from its partial sums.
 template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const float *part, int32_t splits,
-                                                                  const float *dloss, const Control *__restrict__ control,
-                                                                  void *dh, int64_t ld) {
+                                                                  const float *dloss, Control *control, void *dh,
+                                                                  int64_t ld) {
+    if (blockIdx.x == 0) write_status(x, control);
     const int exponent = -(kGradShift + scale_exponent(control->top[kTopW]));
     const int64_t size = int64_t(x.tokens) * x.hidden;
     for (int64_t i = int64_t(blockIdx.x) * kPackBlock + threadIdx.x; i < size; i += int64_t(gridDim.x) * kPackBlock) {
@@ -806,15 +816,7 @@ template <Prec P>
 __global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const float *__restrict__ part, int32_t splits, void *__restrict__ dh,
                                                                    int64_t ld, Control *control) {
     __shared__ float s_sum[kWaves][kWave];
-    if (blockIdx.x == 0 && threadIdx.x < kWave) {   // the status word: 64 tokens at most
-        bool bad = false;
-        if (threadIdx.x < x.tokens) {
-            const int64_t v = x.target[threadIdx.x];
-            bad = v != x.ignore && (v < 0 || v >= x.vocab);
-        }
-        bad = __any(bad);
-        if (threadIdx.x == 0) control->status = bad ? kXentBadTarget : 0u;
-    }
+    if (blockIdx.x == 0) write_status(x, control);
     // a wave takes every fourth split of 64 values
     const int64_t size = int64_t(x.tokens) * x.hidden;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -943,30 +945,25 @@ void pack_operands(const Xent &x, const float *dloss, bool gradient, const Plan 
     Control *control = reinterpret_cast<Control *>(ws);
     constexpr int kSize = P == Prec::kBf16 ? 2 : 4;
     const int64_t row = row_bytes<P>(x.hidden);
+    // the largest magnitudes, where a scale needs them
+    uint32_t w_blocks = 0, h_blocks = 0;
+    if (P == Prec::kSplit || gradient) {
+        w_blocks = uint32_t(std::min<int64_t>(tiles(x.vocab, kWaves), kTopBlocksW));
+        h_blocks = uint32_t(std::min<int64_t>(tiles(x.tokens, kWaves), kTopBlocksH));
+        xent_top_kernel<P><<<w_blocks + h_blocks, kPackBlock, 0, stream>>>(x, dloss, w_blocks, control);
+    }
     auto pack = [&](bool of_w, const void *p, int64_t ld, int32_t rows, int64_t along, int64_t turned) {
         const bool in_place = direct<P>(p, ld, x.hidden);
         if (!in_place || gradient) {
             const int64_t blocks = tiles(rows, kPackTile) * tiles(x.hidden, kPackTile);
             xent_pack_kernel<P><<<uint32_t(blocks), kPackBlock, 0, stream>>>(
-                x, of_w, dloss, in_place ? nullptr : ws + along, gradient ? ws + turned : nullptr, control);
+                x, of_w, dloss, in_place ? nullptr : ws + along, gradient ? ws + turned : nullptr,
+                int32_t(of_w ? w_blocks : h_blocks), control);
         }
-        return in_place ? Operand{static_cast<const char *>(p), ld * kSize, rows}
-                        : Operand{ws + along, row, rows};
+        return in_place ? Operand{static_cast<const char *>(p), ld * kSize, rows} : Operand{ws + along, row, rows};
     };
     *h = pack(false, x.h, x.ld_h, x.tokens, plan.h_along, plan.h_turned);
     *w = pack(true, x.w, x.ld_w, x.vocab, plan.w_along, plan.w_turned);
-}
-
-// The status word, and the largest magnitudes where a scale needs them.
-template <Prec P>
-void check_and_scale(const Xent &x, const float *dloss, bool gradient, char *ws, hipStream_t stream) {
-    Control *control = reinterpret_cast<Control *>(ws);
-    xent_check_kernel<<<1, kCheckBlock, 0, stream>>>(x, control);
-    if (P == Prec::kSplit || gradient) {
-        const uint32_t w_blocks = uint32_t(std::min<int64_t>(tiles(x.vocab, kWaves), device_cu_count() * 8));
-        const uint32_t h_blocks = uint32_t(std::min<int64_t>(tiles(x.tokens, kWaves), device_cu_count() * 2));
-        xent_top_kernel<P><<<w_blocks + h_blocks, kPackBlock, 0, stream>>>(x, dloss, w_blocks, control);
-    }
 }
 
 template <Prec P, class F>
@@ -1024,13 +1021,12 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
 template <Prec P>
 hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t stream) {
     const Plan plan = plan_of<P>(x.tokens, x.vocab, x.hidden);
-    const Control *__restrict__ control = reinterpret_cast<const Control *>(ws);
+    Control *control = reinterpret_cast<Control *>(ws);
     Part *parts = reinterpret_cast<Part *>(ws + plan.parts);
     float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
     constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
     if (x.tokens <= kFewForward<F>) return forward_few<F>(x, plan, loss, lse, ws, stream);
     Operand h, w;
-    check_and_scale<P>(x, nullptr, false, ws, stream);
     pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
     int32_t nparts = 0;
     with_tile<P>(x.vocab, x.tokens, 1, steps_of<P>(x.hidden), [&](auto tile, int64_t blocks) {
@@ -1040,7 +1036,7 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
                                                                                       target_logit);
     });
     xent_join_kernel<<<uint32_t(tiles(x.tokens, kJoinTokens)), kJoinTokens * kJoinSlices, 0, stream>>>(
-        x, parts, nparts, target_logit, loss, lse);
+        x, parts, nparts, target_logit, loss, lse, control);
     return hipGetLastError();
 }
 
@@ -1049,11 +1045,10 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
                     int64_t ld_dw, char *ws, hipStream_t stream) {
     constexpr Prec G = kGradOf<P>;
     const Plan plan = plan_of<P>(x.tokens, x.vocab, x.hidden);
-    const Control *__restrict__ control = reinterpret_cast<const Control *>(ws);
+    Control *control = reinterpret_cast<Control *>(ws);
     constexpr Prec F = P == Prec::kSplit ? Prec::kFp32 : P;
     if (x.tokens <= kFewTokens) return backward_few<F>(x, plan, lse, dloss, dh, ld_dh, dw, ld_dw, ws, stream);
     Operand h, w;
-    check_and_scale<P>(x, dloss, true, ws, stream);
     pack_operands<P>(x, dloss, true, plan, ws, &h, &w, stream);
     const int64_t t_row = row_bytes<G>(x.tokens), v_row = row_bytes<G>(x.vocab);
     const Operand ht{ws + plan.h_turned, t_row, x.hidden};
