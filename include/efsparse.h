@@ -394,7 +394,7 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              products are summed in fp32.
  *   tokens     0..EFS_XENT_MAX_TOKENS (0: nothing to do); vocab
  *              1..EFS_XENT_MAX_VOCAB; hidden 1..EFS_XENT_MAX_HIDDEN; tokens x
- *              vocab at most 2^44.
+ *              vocab at most 2^38.
  *   loss, lse  fp32[tokens], overwritten.
  *   workspace  >= xent_workspace_bytes(tokens, vocab, hidden, dtype, 0) bytes,
  *              16-byte aligned; contents need no initialisation.  bf16 rows

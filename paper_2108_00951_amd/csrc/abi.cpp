@@ -447,7 +447,7 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
 
 static bool xent_sizes_ok(int32_t tokens, int32_t vocab, int32_t hidden, int dtype) {
     return tokens >= 0 && tokens <= efs::kXentMaxTokens && vocab >= 1 && vocab <= efs::kXentMaxVocab &&
-           hidden >= 1 && hidden <= efs::kXentMaxHidden && int64_t(tokens) * vocab <= int64_t(1) << 44 &&
+           hidden >= 1 && hidden <= efs::kXentMaxHidden && int64_t(tokens) * vocab <= int64_t(1) << 38 &&
            (dtype == EFS_FP32 || dtype == EFS_BF16);
 }
 

@@ -107,6 +107,9 @@ __device__ __forceinline__ void store_split8(char *row, int32_t c, const float (
     *reinterpret_cast<f16x8 *>(p + 64) = lo;
 }
 
+typedef uint16_t u16x8_at2 __attribute__((ext_vector_type(8), aligned(2)));
+typedef uint16_t u16x8_at4 __attribute__((ext_vector_type(8), aligned(4)));
+
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
@@ -261,6 +264,77 @@ struct MfmaTile {
             __builtin_amdgcn_sched_group_barrier(0x8, kAll, 0);
         }
         __builtin_amdgcn_s_waitcnt(0x0f70);   // the loads that nothing reads
+    }
+
+    // The same of rows that are not laid out in steps: element (r, k) is
+    // a[r * lda + k], k < len, at any alignment of the element type.  A lane
+    // loads its own rows' values into registers, half of a step's 128 bytes of a
+    // row, with zeros for values past len: the same values in the same order as
+    // run's, and so the same sums.
+    __device__ __forceinline__ void run_rows(const void *a, int64_t lda, int32_t rows_a, const void *b, int64_t ldb,
+                                             int32_t rows_b, int32_t row0, int32_t col0, int32_t len) {
+        static_assert(P == Prec::kBf16 || P == Prec::kFp32, "elements as they are stored");
+        constexpr int kEach = P == Prec::kBf16 ? 8 : 4, kSize = 16 / kEach;   // elements of a load, bytes of one
+        const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+        const char *from[TM + TN];
+#pragma unroll
+        for (int i = 0; i < TM + TN; ++i) {
+            const int r = (lane & 31) + (i < TM ? row0 + (wave / WN * TM + i) * 32 : col0 + (wave % WN * TN + i - TM) * 32);
+            from[i] = i < TM ? static_cast<const char *>(a) + min(r, rows_a - 1) * lda * kSize
+                             : static_cast<const char *>(b) + min(r, rows_b - 1) * ldb * kSize;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (i < TM)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j][e] = 0.0f;
+        }
+        using u16x8u = std::conditional_t<P == Prec::kBf16, u16x8_at2, u16x8_at4>;
+        f16x8 f[2][4][TM + TN];
+        auto load = [&](f16x8 (&to)[4][TM + TN], int32_t k0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < TM + TN; ++i)
+                    to[q][i] = __builtin_bit_cast(
+                        f16x8, *reinterpret_cast<const u16x8u *>(from[i] + int64_t(k0 + (2 * q + (lane >> 5)) * kEach) * kSize));
+        };
+        auto load_last = [&](f16x8 (&to)[4][TM + TN], int32_t k0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int32_t k = k0 + (2 * q + (lane >> 5)) * kEach;
+#pragma unroll
+                for (int i = 0; i < TM + TN; ++i) {
+                    u16x8u v = {};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k + e * 2 / kSize < len)
+                            v[e] = reinterpret_cast<const uint16_t *>(from[i] + int64_t(k) * kSize)[e];
+                    to[q][i] = __builtin_bit_cast(f16x8, v);
+                }
+            }
+        };
+        auto multiply = [&](const f16x8 (&of)[4][TM + TN]) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma(of[q][i], of[q][TM + j], acc[i][j]);
+        };
+        constexpr int kStep = 8 * kEach;
+        const int32_t whole = len / kStep;
+        if (whole > 0) load(f[0], 0);
+        for (int32_t s = 0; s < whole; s += 2) {   // past the last, that one again
+            load(f[1], min(s + 1, whole - 1) * kStep);
+            multiply(f[0]);
+            if (s + 1 == whole) break;
+            load(f[0], min(s + 2, whole - 1) * kStep);
+            multiply(f[1]);
+        }
+        if (whole * kStep < len) {
+            load_last(f[0], whole * kStep);
+            multiply(f[0]);
+        }
     }
 };
 

@@ -27,7 +27,8 @@
 //
 // Few tokens (64 at most; 128 forward, fp32): reading w is what counts.  Its
 // rows are multiplied where they are, fp32 by the fp32 matrix instructions
-// without the passes that split it; a second launch joins the parts.  Backward,
+// without the passes that split it (through LDS where they are whole steps,
+// else straight into registers); a second launch joins the parts.  Backward,
 // one launch leaves g in fp32, and one takes each block of w's rows to dh's
 // partial sums and writes the same rows of dw.
 //
@@ -324,18 +325,20 @@ __device__ __forceinline__ float logit(float acc, int exponent) {
     return P == Prec::kSplit ? ldexpf(acc, exponent) : acc;
 }
 
-// Forward: parts[tile row][token], and the targets' logits.
-template <Prec P, class Tile>
+// Forward: parts[tile row][token], and the targets' logits.  kRows: from h and w
+// as they are, whatever their alignment, and not from operands.
+template <Prec P, class Tile, bool kRows>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forward_kernel(Xent x, Operand w, Operand h,
                                                                          const Control *__restrict__ control, Part *parts,
                                                                          float *target_logit) {
-    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    __shared__ __align__(16) char lds[kRows ? Tile::kRows / 32 * Tile::kCols * sizeof(Part) : Tile::kLdsBytes];
     const uint32_t tv = (x.vocab + Tile::kRows - 1) / Tile::kRows, tt = (x.tokens + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
     banded(xcd_place(blockIdx.x, gridDim.x), tv, tt, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
     Tile tile;
-    tile.run(w, h, row0, col0, 0, int32_t(steps_of<P>(x.hidden)), lds);
+    if constexpr (kRows) tile.run_rows(x.w, x.ld_w, x.vocab, x.h, x.ld_h, x.tokens, row0, col0, x.hidden);
+    else tile.run(w, h, row0, col0, 0, int32_t(steps_of<P>(x.hidden)), lds);
     const int exponent = logit_exponent<P>(control);
     Part *s_part = reinterpret_cast<Part *>(lds);   // [rows of waves][columns]
     constexpr int kHigh = Tile::kRows / (Tile::kTilesM * 32);
@@ -558,14 +561,15 @@ __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const 
 
 // Few tokens: g as fp32 [token][word], rows `words_end` long (a multiple of 64;
 // zeros past the vocabulary and for tokens that do not count).
-template <Prec P, class Tile>
+template <Prec P, class Tile, bool kRows>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_few_grad_kernel(Xent x, Operand w, Operand h, const float *lse,
                                                                        const float *dloss, float *g,
                                                                        int64_t words_end) {
-    __shared__ __align__(16) char lds[Tile::kLdsBytes];
+    __shared__ __align__(16) char lds[kRows ? 16 : Tile::kLdsBytes];
     const int32_t row0 = int32_t(blockIdx.x) * Tile::kRows;
     Tile tile;
-    tile.run(w, h, row0, 0, 0, int32_t(steps_of<P>(x.hidden)), lds);
+    if constexpr (kRows) tile.run_rows(x.w, x.ld_w, x.vocab, x.h, x.ld_h, x.tokens, row0, 0, x.hidden);
+    else tile.run(w, h, row0, 0, 0, int32_t(steps_of<P>(x.hidden)), lds);
 #pragma unroll
     for (int j = 0; j < Tile::kTilesN; ++j) {
         const int32_t t = Tile::col_of(j);
@@ -863,6 +867,36 @@ struct Plan {
     int64_t total;
 };
 
+// The kind of tile that rows x cols, `times` over with `steps` each, is fastest
+// with, and how many there are of each.
+TileKind tile_kind(int64_t rows, int64_t cols, int64_t times, int64_t steps, int64_t (&n)[kTileKinds]) {
+    int64_t work[kTileKinds];
+    for (int k = 0; k < kTileKinds; ++k) {
+        n[k] = tiles(rows, kTileSide[k]) * tiles(cols, kTileSide[k]) * times;
+        work[k] = n[k] * steps;
+    }
+    return best_tile(work, steps);
+}
+
+// Calls run(tile, workgroups) with it.
+template <Prec P, class F>
+void with_tile(int64_t rows, int64_t cols, int64_t times, int64_t steps, F run) {
+    int64_t n[kTileKinds];
+    switch (tile_kind(rows, cols, times, steps, n)) {
+        case kTiny: return run(TinyTile<P>(), n[kTiny]);
+        case kSmall: return run(SmallTile<P>(), n[kSmall]);
+        case kLarge: return run(LargeTile<P>(), n[kLarge]);
+    }
+}
+
+// The forward product's (few tokens: tiles of 64 words).
+template <Prec P>
+TileKind forward_tile(int32_t tokens, int32_t vocab, int32_t hidden) {
+    int64_t n[kTileKinds];
+    return tokens <= kFewForward<P == Prec::kSplit ? Prec::kFp32 : P> ? kTiny
+                                                                     : tile_kind(vocab, tokens, 1, steps_of<P>(hidden), n);
+}
+
 template <Prec P>
 Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     constexpr Prec G = kGradOf<P>;
@@ -889,7 +923,7 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
         return here;
     };
     p.target_logit = take(int64_t(tokens) * 4);
-    p.parts = take(int64_t(tokens) * tiles(vocab, kTileSide[kTiny]) * 8);
+    p.parts = take(int64_t(tokens) * tiles(vocab, kTileSide[forward_tile<P>(tokens, vocab, hidden)]) * 8);
     p.h_along = take(tokens * row_bytes<P>(hidden));
     p.w_along = take(vocab * row_bytes<P>(hidden));
     p.forward = at;
@@ -911,22 +945,6 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     p.dh = take(int64_t(p.splits) * tokens * hidden * 4);
     p.total = at;
     return p;
-}
-
-// Calls run(tile, workgroups) with the kind of tile that rows x cols, `times`
-// over with `steps` each, is fastest with.
-template <Prec P, class F>
-void with_tile(int64_t rows, int64_t cols, int64_t times, int64_t steps, F run) {
-    int64_t n[kTileKinds], work[kTileKinds];
-    for (int k = 0; k < kTileKinds; ++k) {
-        n[k] = tiles(rows, kTileSide[k]) * tiles(cols, kTileSide[k]) * times;
-        work[k] = n[k] * steps;
-    }
-    switch (best_tile(work, steps)) {
-        case kTiny: return run(TinyTile<P>(), n[kTiny]);
-        case kSmall: return run(SmallTile<P>(), n[kSmall]);
-        case kLarge: return run(LargeTile<P>(), n[kLarge]);
-    }
 }
 
 // Whether the tensor can be multiplied where it is: whole steps along its
@@ -973,19 +991,27 @@ void with_narrow_tile(int32_t tokens, F run) {
     else run(NarrowTile<P, 4>());
 }
 
+// Few tokens: the operands are the tensors themselves.
+template <Prec P>
+Operand operand_of(const void *p, int64_t ld, int32_t rows) {
+    return Operand{static_cast<const char *>(p), ld * (P == Prec::kBf16 ? 2 : 4), rows};
+}
+
 template <Prec P>
 hipError_t forward_few(const Xent &x, const Plan &plan, float *loss, float *lse, char *ws, hipStream_t stream) {
     Control *control = reinterpret_cast<Control *>(ws);
     Part *parts = reinterpret_cast<Part *>(ws + plan.parts);
     float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
-    Operand h, w;
-    pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
+    const bool in_steps = direct<P>(x.w, x.ld_w, x.hidden) && direct<P>(x.h, x.ld_h, x.hidden);
+    const Operand h = operand_of<P>(x.h, x.ld_h, x.tokens), w = operand_of<P>(x.w, x.ld_w, x.vocab);
     int32_t nparts = 0;
     with_narrow_tile<P>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
         nparts = int32_t(tiles(x.vocab, Tile::kRows));
-        xent_forward_kernel<P, Tile><<<uint32_t(nparts), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
-                                                                                      target_logit);
+        auto run = [&](auto kernel) {
+            kernel<<<uint32_t(nparts), Tile::kThreads, 0, stream>>>(x, w, h, control, parts, target_logit);
+        };
+        in_steps ? run(xent_forward_kernel<P, Tile, false>) : run(xent_forward_kernel<P, Tile, true>);
     });
     xent_join_few_kernel<<<uint32_t(x.tokens), kPackBlock, 0, stream>>>(x, parts, nparts, target_logit, loss, lse,
                                                                         control);
@@ -995,16 +1021,20 @@ hipError_t forward_few(const Xent &x, const Plan &plan, float *loss, float *lse,
 template <Prec P>
 hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const float *dloss, void *dh, int64_t ld_dh,
                         void *dw, int64_t ld_dw, char *ws, hipStream_t stream) {
-    Operand h, w;
-    pack_operands<P>(x, nullptr, false, plan, ws, &h, &w, stream);
+    const bool in_steps = direct<P>(x.w, x.ld_w, x.hidden) && direct<P>(x.h, x.ld_h, x.hidden);
+    const Operand h = operand_of<P>(x.h, x.ld_h, x.tokens), w = operand_of<P>(x.w, x.ld_w, x.vocab);
     float *g = reinterpret_cast<float *>(ws + plan.few_g), *part = reinterpret_cast<float *>(ws + plan.few_dh);
     const int64_t words_end = tiles(x.vocab, 64) * 64;
     with_narrow_tile<P>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
         static_assert(Tile::kRows == 64, "g's rows end with the tiles");
-        if constexpr (Tile::kCols <= kFewTokens)
-            xent_few_grad_kernel<P, Tile><<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(
-                x, w, h, lse, dloss, g, words_end);
+        if constexpr (Tile::kCols <= kFewTokens) {
+            auto run = [&](auto kernel) {
+                kernel<<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(x, w, h, lse, dloss, g,
+                                                                                             words_end);
+            };
+            in_steps ? run(xent_few_grad_kernel<P, Tile, false>) : run(xent_few_grad_kernel<P, Tile, true>);
+        }
     });
     const uint32_t blocks = uint32_t(tiles(x.hidden, kFewHidden) * plan.few_splits);
     auto run = [&](auto kernel) {
@@ -1032,8 +1062,8 @@ hipError_t forward(const Xent &x, float *loss, float *lse, char *ws, hipStream_t
     with_tile<P>(x.vocab, x.tokens, 1, steps_of<P>(x.hidden), [&](auto tile, int64_t blocks) {
         using Tile = decltype(tile);
         nparts = int32_t(tiles(x.vocab, Tile::kRows));
-        xent_forward_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
-                                                                                      target_logit);
+        xent_forward_kernel<P, Tile, false><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, w, h, control, parts,
+                                                                                             target_logit);
     });
     xent_join_kernel<<<uint32_t(tiles(x.tokens, kJoinTokens)), kJoinTokens * kJoinSlices, 0, stream>>>(
         x, parts, nparts, target_logit, loss, lse, control);

@@ -111,6 +111,28 @@ def test_strides_and_alignment(dtype, pad, shift):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens, hidden", [(5, 128), (20, 65), (50, 200), (100, 129)])
+@pytest.mark.parametrize("pad, shift", [(0, 1), (8, 0), (5, 3)])
+def test_strides_and_alignment_of_few_tokens(dtype, tokens, hidden, pad, shift):
+    """The path that reads the head where it is, aligned to whole steps or not."""
+    h, w, target, dloss = inputs(tokens, 700, hidden, dtype)
+
+    def view(x):
+        rows, cols = x.shape
+        buf = torch.full((rows * (cols + pad) + shift,), float("nan"), dtype=x.dtype, device=DEV)
+        return buf[shift:].view(rows, cols + pad)[:, :cols]
+    hv, wv, dh, dw = view(h), view(w), view(h), view(w)
+    hv.copy_(h)
+    wv.copy_(w)
+    target, dloss = target.to(DEV), dloss.to(DEV)
+    ws = efs.new_xent_workspace(tokens, 700, hidden, h.dtype, DEV)
+    got = {"loss": torch.empty(tokens, device=DEV), "lse": torch.empty(tokens, device=DEV), "dh": dh, "dw": dw}
+    efs.xent_forward(hv, wv, target, got["loss"], got["lse"], ws)
+    efs.xent_backward(hv, wv, target, got["lse"], dloss, dh, dw, ws)
+    check(got, h, w, target, dloss, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -3.3e38])
 @pytest.mark.parametrize("hidden", [64, 70])
 def test_ignored_tokens_hold_anything(dtype, bad, hidden):
