@@ -425,10 +425,11 @@ using SmallTile = MfmaTile<P, 2, 2, 2, 2>;
 template <Prec P>
 using TinyTile = MfmaTile<P, 2, 2, 1, 1, 3>;
 
-// For a few tokens against many rows: 64 x 32 TN by two waves, two steps on
-// their way in each of four workgroups a compute unit (TN = 1).
+// For a few tokens against many rows: 64 x 32 TN by two waves, with two steps on
+// their way in each of four workgroups a compute unit (TN = 1), or one in each
+// of six where the fp32 instructions take longer than the loads.
 template <Prec P, int TN>
-using NarrowTile = MfmaTile<P, 2, 1, 1, TN, 3>;
+using NarrowTile = MfmaTile<P, 2, 1, 1, TN, P == Prec::kFp32 ? 2 : 3>;
 
 enum TileKind { kTiny, kSmall, kLarge };
 constexpr int kTileKinds = 3;

@@ -28,7 +28,8 @@
 // Few tokens (64 at most; 128 forward, fp32): reading w is what counts.  Its
 // rows are multiplied where they are, fp32 by the fp32 matrix instructions
 // without the passes that split it (through LDS where they are whole steps,
-// else straight into registers); a second launch joins the parts.  Backward,
+// else straight into registers), and by the vector units for four tokens or
+// fewer; a second launch joins the parts.  Backward,
 // one launch leaves g in fp32, and one takes each block of w's rows to dh's
 // partial sums and writes the same rows of dw.
 //
@@ -559,6 +560,135 @@ __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const 
     }
 }
 
+// One to four tokens: a wave takes rows of w, its lanes 16 bytes each along
+// them, so that rows of any alignment come in whole lines, and multiplies on
+// the vector units (kTok operations an element).  kGrad: g as
+// xent_few_grad_kernel leaves it; else parts and target logits as
+// xent_forward_kernel does.  A workgroup covers 64 words, a wave 16 of them, in
+// one group or (more tokens: registers) two.  fp32, 56,852 x 2,758 words: 146 us
+// for three tokens, 289 through the matrix cores; for eight, 256 against 205.
+// bf16 rows in whole steps are faster through the matrix cores at any count (one
+// token x 33,278 x 1,024: 15 against 18 us).
+constexpr int kDotTokens = 4, kDotWords = 64;
+template <Prec P>
+bool take_dot(int32_t tokens, bool in_steps) {
+    return tokens <= kDotTokens && (P == Prec::kFp32 || !in_steps);
+}
+
+// Sums of N (a power of two) values over the wave's lanes; lane l gets that of
+// value l / (64 / N).  A stage halves the values: each lane keeps one half and
+// sends the other.
+template <int N, int kBit = kWave / 2, int M>
+__device__ __forceinline__ float sum_scattered(float (&v)[M]) {
+    if constexpr (N > 1) {
+        const bool upper = (threadIdx.x & kBit) != 0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            const float keep = upper ? v[i + N / 2] : v[i], send = upper ? v[i] : v[i + N / 2];
+            v[i] = __fadd_rn(keep, __shfl_xor(send, kBit));
+        }
+        return sum_scattered<N / 2, kBit / 2>(v);
+    } else if constexpr (kBit > 0) {
+        v[0] = __fadd_rn(v[0], __shfl_xor(v[0], kBit));
+        return sum_scattered<1, kBit / 2>(v);
+    } else {
+        return v[0];
+    }
+}
+
+// 16 bytes of elements, at any alignment.
+template <Prec P>
+constexpr int kVec = P == Prec::kBf16 ? 8 : 4;
+template <Prec P>
+__device__ __forceinline__ void load_vec(const void *p, int64_t i, float (&v)[kVec<P>]) {
+    if constexpr (P == Prec::kBf16) {
+        load8<P>(p, i, v);
+    } else {
+        const f32x4u a = *reinterpret_cast<const f32x4u *>(static_cast<const float *>(p) + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = a[k];
+    }
+}
+
+template <Prec P, int kTok, bool kGrad>
+__global__ __launch_bounds__(kPackBlock) void xent_dot_kernel(Xent x, Part *__restrict__ parts,
+                                                              float *__restrict__ target_logit,
+                                                              const float *__restrict__ lse,
+                                                              const float *__restrict__ dloss, float *__restrict__ g,
+                                                              int64_t words_end) {
+    constexpr int kRows = kTok <= 2 ? 16 : 8, kGroups = kDotWords / kWaves / kRows;
+    constexpr int kSums = kRows * kTok, kSame = kWave / kSums;   // lanes that get one sum
+    constexpr int kEach = kVec<P>;
+    __shared__ Part s_part[kWaves][kTok];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int token = lane / kSame / kRows;   // of this lane's sum
+    const bool there = token < x.tokens;
+    const int32_t target = there ? target_of(x, token) : -1;
+    const float shift = kGrad && target >= 0 ? lse[token] : 0.0f, weight = kGrad && target >= 0 ? dloss[token] : 0.0f;
+    Part part = {-INFINITY, 0.0f};
+    for (int group = 0; group < kGroups; ++group) {
+        const int32_t v0 = int32_t(blockIdx.x) * kDotWords + (wave * kGroups + group) * kRows;
+        float sum[kSums];   // [token][row]
+#pragma unroll
+        for (int i = 0; i < kSums; ++i) sum[i] = 0.0f;
+        int32_t k = lane * kEach;
+        for (; k + kEach <= x.hidden; k += kWave * kEach) {
+            float w[kRows][kEach], h[kTok][kEach];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) load_vec<P>(x.w, min(v0 + r, x.vocab - 1) * x.ld_w + k, w[r]);
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) load_vec<P>(x.h, min(t, x.tokens - 1) * x.ld_h + k, h[t]);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+#pragma unroll
+                for (int t = 0; t < kTok; ++t)
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) sum[t * kRows + r] = fmaf(w[r][e], h[t][e], sum[t * kRows + r]);
+        }
+        for (; k < x.hidden; ++k) {   // the rows' last values, of one lane
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float w = element<P>(x.w, min(v0 + r, x.vocab - 1) * x.ld_w + k);
+#pragma unroll
+                for (int t = 0; t < kTok; ++t)
+                    sum[t * kRows + r] = fmaf(w, element<P>(x.h, min(t, x.tokens - 1) * x.ld_h + k), sum[t * kRows + r]);
+            }
+        }
+        float l = sum_scattered<kSums>(sum);
+        const int32_t v = v0 + lane / kSame % kRows;
+        if constexpr (kGrad) {
+            if (there && lane % kSame == 0) {
+                float p = 0.0f;
+                if (target >= 0 && v < x.vocab) {
+                    p = expf(l - shift);
+                    if (v == target) p = __fsub_rn(p, 1.0f);
+                    p = __fmul_rn(p, weight);
+                }
+                g[token * words_end + v] = p;
+            }
+        } else {
+            if (v >= x.vocab) l = -INFINITY;
+            if (v == target && lane % kSame == 0) target_logit[token] = l;
+            // (a NaN has no maximum; it goes into the sum)
+            part = join(part, l != l ? Part{-INFINITY, l} : Part{l, l == -INFINITY ? 0.0f : 1.0f});
+        }
+    }
+    if constexpr (!kGrad) {
+        // over the rows of a token, which are neighbouring lanes
+#pragma unroll
+        for (int bit = kSame; bit < kSame * kRows; bit *= 2)
+            part = join(part, Part{__shfl_xor(part.top, bit), __shfl_xor(part.sum, bit)});
+        if (lane % (kSame * kRows) == 0) s_part[wave][token] = part;
+        __syncthreads();
+        if (threadIdx.x < kTok && int(threadIdx.x) < x.tokens) {
+            Part p = s_part[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) p = join(p, s_part[w][threadIdx.x]);
+            parts[int64_t(blockIdx.x) * x.tokens + threadIdx.x] = p;
+        }
+    }
+}
+
 // Few tokens: g as fp32 [token][word], rows `words_end` long (a multiple of 64;
 // zeros past the vocabulary and for tokens that do not count).
 template <Prec P, class Tile, bool kRows>
@@ -1004,10 +1134,17 @@ hipError_t forward_few(const Xent &x, const Plan &plan, float *loss, float *lse,
     float *target_logit = reinterpret_cast<float *>(ws + plan.target_logit);
     const bool in_steps = direct<P>(x.w, x.ld_w, x.hidden) && direct<P>(x.h, x.ld_h, x.hidden);
     const Operand h = operand_of<P>(x.h, x.ld_h, x.tokens), w = operand_of<P>(x.w, x.ld_w, x.vocab);
-    int32_t nparts = 0;
-    with_narrow_tile<P>(x.tokens, [&](auto tile) {
+    int32_t nparts = int32_t(tiles(x.vocab, kDotWords));
+    auto dot = [&](auto kernel) {
+        kernel<<<uint32_t(nparts), kPackBlock, 0, stream>>>(x, parts, target_logit, nullptr, nullptr, nullptr, 0);
+    };
+    if (take_dot<P>(x.tokens, in_steps))
+        x.tokens == 1   ? dot(xent_dot_kernel<P, 1, false>)
+        : x.tokens == 2 ? dot(xent_dot_kernel<P, 2, false>)
+                        : dot(xent_dot_kernel<P, 4, false>);
+    else with_narrow_tile<P>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
-        nparts = int32_t(tiles(x.vocab, Tile::kRows));
+        static_assert(Tile::kRows == kDotWords, "parts of as many words");
         auto run = [&](auto kernel) {
             kernel<<<uint32_t(nparts), Tile::kThreads, 0, stream>>>(x, w, h, control, parts, target_logit);
         };
@@ -1024,10 +1161,17 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
     const bool in_steps = direct<P>(x.w, x.ld_w, x.hidden) && direct<P>(x.h, x.ld_h, x.hidden);
     const Operand h = operand_of<P>(x.h, x.ld_h, x.tokens), w = operand_of<P>(x.w, x.ld_w, x.vocab);
     float *g = reinterpret_cast<float *>(ws + plan.few_g), *part = reinterpret_cast<float *>(ws + plan.few_dh);
-    const int64_t words_end = tiles(x.vocab, 64) * 64;
-    with_narrow_tile<P>(x.tokens, [&](auto tile) {
+    const int64_t words_end = tiles(x.vocab, kDotWords) * kDotWords;
+    auto dot = [&](auto kernel) {
+        kernel<<<uint32_t(words_end / kDotWords), kPackBlock, 0, stream>>>(x, nullptr, nullptr, lse, dloss, g, words_end);
+    };
+    if (take_dot<P>(x.tokens, in_steps))
+        x.tokens == 1   ? dot(xent_dot_kernel<P, 1, true>)
+        : x.tokens == 2 ? dot(xent_dot_kernel<P, 2, true>)
+                        : dot(xent_dot_kernel<P, 4, true>);
+    else with_narrow_tile<P>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
-        static_assert(Tile::kRows == 64, "g's rows end with the tiles");
+        static_assert(Tile::kRows == kDotWords, "g's rows end with the tiles");
         if constexpr (Tile::kCols <= kFewTokens) {
             auto run = [&](auto kernel) {
                 kernel<<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(x, w, h, lse, dloss, g,
