@@ -321,8 +321,10 @@ enum { EFS_FP32 = 0, EFS_BF16 = 1 };
  *              g[i * stride_g + r * ld_g + c] (in elements; ld_g >= cols).  Read
  *              only; matrices may overlap (stride_g = 0 repeats one).
  *   out        the same with ld_out, stride_out; matrices must not overlap
- *              each other.  May be g itself: g is not read any more when out is
- *              written.
+ *              each other.  May be g itself (the same pointer, ld and stride):
+ *              a matrix of g is not read any more when its result is written.
+ *              A batch must not overlap g in any other way; other columns of
+ *              the same rows are no overlap.
  *   dtype      EFS_FP32 or EFS_BF16, of g and out.
  *   batch, rows, cols   >= 0; rows * cols <= INT32_MAX, batch <=
  *              EFS_MUON_MAX_MATRICES.  0 of any: a call that does nothing.
@@ -429,7 +431,8 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
  *   dh, dw     tokens x hidden and vocab x hidden of dtype, rows ld_dh and
  *              ld_dw elements apart, overwritten (dh is 0 where a token does
  *              not count; dw is 0 with no tokens).  Must not overlap h, w or
- *              each other.  bf16: g is rounded to 11 bits before it is
+ *              each other (other columns of the same rows are no overlap).
+ *              bf16: g is rounded to 11 bits before it is
  *              multiplied, each result to bf16; sums are fp32.
  *   workspace  >= xent_workspace_bytes(.., 1). */
 efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,

@@ -55,12 +55,22 @@ bool overlap(const float *a, const float *b, int64_t d) {
     return x < y + uintptr_t(d) * 4 && y < x + uintptr_t(d) * 4;
 }
 
-// Whether the spans from the first to the last element of two row sets meet.
+// Whether two sets of rows of `cols` elements, in memory from x and y on over
+// span_a and span_b elements, can meet: their spans do, unless the rows of both
+// are `ld` elements apart throughout (0: they are not) and take different
+// columns of it.
+bool spans_meet(uintptr_t x, int64_t span_a, uintptr_t y, int64_t span_b, int64_t ld, int64_t cols, uintptr_t size) {
+    if (x >= y + uintptr_t(span_b) * size || y >= x + uintptr_t(span_a) * size) return false;
+    if (ld == 0) return true;
+    const uintptr_t row = uintptr_t(ld) * size, apart = x < y ? (y - x) % row : (row - (x - y) % row) % row;
+    return apart < uintptr_t(cols) * size || apart > row - uintptr_t(cols) * size;
+}
+
+// Whether two sets of rows can share an element.
 bool rows_overlap(const void *a, int64_t rows_a, int64_t ld_a, const void *b, int64_t rows_b, int64_t ld_b,
                   int64_t cols, int64_t size) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + uintptr_t(((rows_b - 1) * ld_b + cols) * size) &&
-           y < x + uintptr_t(((rows_a - 1) * ld_a + cols) * size);
+    return spans_meet(reinterpret_cast<uintptr_t>(a), (rows_a - 1) * ld_a + cols, reinterpret_cast<uintptr_t>(b),
+                      (rows_b - 1) * ld_b + cols, ld_a == ld_b ? ld_a : 0, cols, uintptr_t(size));
 }
 
 int g_cu_count[64];  // per device; 0 = not queried yet
@@ -398,6 +408,13 @@ efs_status muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, voi
     if (batch > 1 && stride_out < (int64_t(rows) - 1) * ld_out + cols &&
         (stride_out < cols || ld_out < (int64_t(batch) - 1) * stride_out + cols))
         return fail(EFS_EINVAL, "%s: the matrices of out overlap", name);
+    // a matrix is written when it has been read, but others may not have been
+    const int64_t span_g = (int64_t(rows) - 1) * ld_g + cols + (batch - 1) * stride_g;
+    const int64_t span_out = (int64_t(rows) - 1) * ld_out + cols + (batch - 1) * stride_out;
+    const int64_t ld = ld_g == ld_out && stride_g % ld_g == 0 && stride_out % ld_out == 0 ? ld_g : 0;
+    if (batch > 1 && (g != out || ld_g != ld_out || stride_g != stride_out) &&
+        spans_meet(reinterpret_cast<uintptr_t>(g), span_g, reinterpret_cast<uintptr_t>(out), span_out, ld, cols, size))
+        return fail(EFS_EINVAL, "%s: out overlaps g and is not g itself", name);
     const efs_status s = check_muon(name, batch, &rows, &cols, 0, steps, eps, workspace, workspace_bytes);
     if (s != EFS_OK) return s;
     return check_launch(efs::launch_muon_orthogonalize(g, ld_g, stride_g, out, ld_out, stride_out,

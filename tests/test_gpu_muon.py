@@ -259,3 +259,18 @@ def test_binding_refuses_what_the_kernels_do_not_take():
     with pytest.raises(efs.EfsError):   # the second matrix starts inside the first
         efs.muon_apply(torch.zeros(24, device=DEV), g.view(-1), torch.zeros(24, device=DEV), [(0, 2, 6), (11, 2, 6)],
                        efs.new_muon_workspace([(2, 6)] * 2, DEV), 0.9, 0.1)
+
+
+@pytest.mark.parametrize("rows, cols", [(30, 40), (70, 90)])
+def test_orthogonalize_a_batch_in_place_and_beside_itself(rows, cols):
+    g = torch.from_numpy(np.random.default_rng(14).standard_normal((20, rows, cols)).astype(np.float32)).to(DEV)
+    want = ortho(g)
+    ws = efs.new_muon_workspace([(rows, cols)] * 20, DEV)
+    both = torch.cat((g, g), 2)
+    efs.muon_orthogonalize(both[:, :, :cols], both[:, :, cols:], ws)
+    assert torch.equal(both[:, :, cols:], want)
+    assert torch.equal(both[:, :, :cols], g)
+    efs.muon_orthogonalize(g, g, ws)
+    assert torch.equal(g, want)
+    with pytest.raises(Exception, match="overlaps g"):
+        efs.muon_orthogonalize(g[:-1], g[1:], ws)

@@ -294,3 +294,16 @@ def test_binding_refuses_what_the_kernels_do_not_take():
         efs.xent_backward(h, w, target, f, dloss, h, torch.empty_like(w), ws)
     with pytest.raises(ValueError):
         efs.xent_backward(h, w, target, f, dloss, torch.empty_like(w), torch.empty_like(w), ws)
+
+
+@pytest.mark.parametrize("tokens", [9, 150])
+def test_gradients_beside_their_tensors(tokens):
+    """dh and dw in other columns of the rows that hold h and w."""
+    h, w, target, dloss = (x.to(DEV) for x in inputs(tokens, 700, 70, "fp32"))
+    want = call(h, w, target, dloss)
+    both_h, both_w = torch.cat((h, h), 1), torch.cat((w, w), 1)
+    ws = efs.new_xent_workspace(tokens, 700, 70, h.dtype, DEV)
+    efs.xent_backward(both_h[:, :70], both_w[:, :70], target, want["lse"], dloss, both_h[:, 70:], both_w[:, 70:], ws)
+    for k, both, x in (("dh", both_h, h), ("dw", both_w, w)):
+        assert torch.equal(both[:, 70:], want[k]), k
+        assert torch.equal(both[:, :70], x), k

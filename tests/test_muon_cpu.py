@@ -77,3 +77,20 @@ def test_apply_rejects_bad_arguments(lib):
         assert rc == (binding.EFS_ESPACE if "nb" in over else binding.EFS_EINVAL), over
     assert lib.muon_apply(None, None, None, 0, 0, None, None, None, 0.9, 0.1, 0.0, 1, 5, 1e-7, None, 0,
                           None) == binding.EFS_OK
+
+
+def test_orthogonalize_takes_g_itself_and_no_other_overlap(lib):
+    def call(g, ldg, sg, o, ldo, so, batch=3):
+        return lib.muon_orthogonalize(g, ldg, sg, o, ldo, so, 0, batch, 80, 100, 5, None, 1e-7, FAKE, 0, None)
+    # accepted: only the workspace is refused
+    for good in ((FAKE, 100, 8000, FAKE, 100, 8000), (FAKE, 100, 8000, FAKE + 96000, 100, 8000),
+                 (FAKE, 100, 0, FAKE + 32000, 100, 8000),
+                 (FAKE, 250, 20000, FAKE + 400, 250, 20000), (FAKE + 400, 250, 20000, FAKE, 250, 40000),
+                 (FAKE, 100, 8000, FAKE + 4, 100, 8000, 1)):
+        assert call(*good) == binding.EFS_ESPACE, good
+    for bad in ((FAKE, 100, 0, FAKE, 100, 8000), (FAKE, 100, 8000, FAKE + 32000, 100, 8000),
+                (FAKE + 95996, 100, 8000, FAKE, 100, 8000), (FAKE, 100, 8000, FAKE, 100, 16000),
+                (FAKE, 250, 20000, FAKE + 396, 250, 20000), (FAKE + 604, 250, 20000, FAKE, 250, 20000),
+                (FAKE, 250, 20100, FAKE + 400, 250, 20100)):
+        assert call(*bad) == binding.EFS_EINVAL, bad
+        assert b"overlaps g" in lib.efs_last_error_message()

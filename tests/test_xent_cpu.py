@@ -58,3 +58,13 @@ def test_backward_rejects_bad_arguments(lib):
         rc = lib.xent_backward(*(a[k] for k in GOOD), a["lse"], a["dloss"], a["dh"], a["ld_dh"], a["dw"], a["ld_dw"],
                                a["ws"], a["nb"], None)
         assert rc == (binding.EFS_ESPACE if "nb" in over else binding.EFS_EINVAL), over
+
+
+def test_backward_refuses_shared_elements_of_the_same_rows(lib):
+    need = lib.xent_workspace_bytes(10, 1000, 64, 0, 1)
+    args = dict(GOOD, ld_h=128, ld_w=128)
+    h, w = args["h"], args["w"]
+    for dh, dw in ((h + 252, w + 256), (h + 256, w + 260), (h + 256, w - 252), (h + 256 + 512 * 9 + 4, w + 256 + 512 * 9 + 4)):
+        rc = lib.xent_backward(*(args[k] for k in GOOD), FAKE, FAKE, dh, 128, dw, 128, FAKE, need, None)
+        assert rc == binding.EFS_EINVAL, (dh - h, dw - w)
+        assert b"must not overlap" in lib.efs_last_error_message()
