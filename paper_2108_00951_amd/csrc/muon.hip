@@ -87,10 +87,10 @@ __host__ __device__ inline int32_t chunks_of(int64_t size) {
     return int32_t(c < kMaxChunks ? c : kMaxChunks);
 }
 
-// Elements of one partial sum: whole 16-byte vectors.
+// Elements of one partial sum: whole pieces of eight.
 __host__ __device__ inline int64_t chunk_of(int64_t size) {
     const int64_t c = chunks_of(size);
-    return ((size + c - 1) / c + 3) / 4 * 4;
+    return ((size + c - 1) / c + 7) / 8 * 8;
 }
 
 // Bytes of one X, X^T, A or B.
@@ -229,16 +229,20 @@ __global__ __launch_bounds__(kSetupBlock) void muon_setup_kernel(Mat *table, Giv
 }
 
 // The last matrix whose count starts at or before `at`: none of them is
-// empty, so the starts differ.
+// empty, so the starts differ.  A wave looks at 64 of them at a time (every
+// look is a way to memory and back before the kernel can start).
 template <class F>
 __device__ __forceinline__ int32_t matrix_of(const Mat *__restrict__ table, int32_t nmat, int32_t at, F start) {
-    int32_t lo = 0, hi = nmat;
-    while (hi - lo > 1) {
-        const int32_t mid = (lo + hi) / 2;
-        if (start(table[mid].at) <= at) lo = mid;
-        else hi = mid;
+    const int32_t lane = threadIdx.x & (kWave - 1);
+    int32_t lo = 0, left = nmat;
+    while (left > 1) {
+        const int32_t step = (left + kWave - 1) / kWave, mine = lane * step;
+        const bool before = mine < left && start(table[lo + mine].at) <= at;
+        const int32_t passed = (__popcll(__ballot(before)) - 1) * step;
+        lo += passed;
+        left = min(step, left - passed);
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
 __device__ __forceinline__ float direction(const Io &io, float avg, float m) {
@@ -247,6 +251,29 @@ __device__ __forceinline__ float direction(const Io &io, float avg, float m) {
 
 __device__ __forceinline__ float read_in(const Io &io, int64_t i) {
     return io.bf16 ? float(static_cast<const __bf16 *>(io.in)[i]) : static_cast<const float *>(io.in)[i];
+}
+
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+
+// Eight neighbours, at any alignment.
+__device__ __forceinline__ void load8(const float *from, float (&v)[8]) {
+    const f32x4u *p = reinterpret_cast<const f32x4u *>(from);
+    const f32x4u a = p[0], b = p[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        v[k] = a[k];
+        v[4 + k] = b[k];
+    }
+}
+
+__device__ __forceinline__ void read_in8(const Io &io, int64_t i, float (&v)[8]) {
+    if (io.bf16) {
+        const bf16x8u a = *reinterpret_cast<const bf16x8u *>(static_cast<const __bf16 *>(io.in) + i);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = float(a[k]);
+    } else {
+        load8(static_cast<const float *>(io.in) + i, v);
+    }
 }
 
 // gamma sqrt(max(1, rows / cols))
@@ -273,7 +300,6 @@ __device__ __forceinline__ void write_out(const Io &io, int64_t at, float o, flo
 
 // Eight of a row's values, scaled by 2^14, of which `left` are the matrix's.
 __device__ __forceinline__ void write_out8(const Io &io, int64_t at, int32_t left, const float (&v)[8], float scale) {
-    typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
     if (left < 8) {
         for (int e = 0; e < 8; ++e)
             if (e < left) write_out(io, at + e, __fmul_rn(v[e], kUnscale), scale);
@@ -338,10 +364,24 @@ __global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *__r
         }
     } else {
         const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
-        for (int64_t i = lo + threadIdx.x; i < hi; i += kSumBlock) {
-            const uint32_t r = uint32_t(i) / uint32_t(mat.cols), c = uint32_t(i) - r * uint32_t(mat.cols);
-            const double u = read_in(io, mat.src + r * ld + c);
-            sum += u * u;
+#pragma unroll 2
+        for (int64_t i = lo + int64_t(threadIdx.x) * 8; i < hi; i += kSumBlock * 8) {
+            uint32_t r = uint32_t(i) / uint32_t(mat.cols), c = uint32_t(i) - r * uint32_t(mat.cols);
+            float v[8] = {};
+            if (c + 8 <= uint32_t(mat.cols)) {
+                read_in8(io, mat.src + r * ld + c, v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {   // from one row into the next
+                    if (i + k < hi) v[k] = read_in(io, mat.src + r * ld + c);
+                    if (++c == uint32_t(mat.cols)) {
+                        c = 0;
+                        ++r;
+                    }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += double(v[k]) * double(v[k]);
         }
     }
     sum = block_sum_f64(sum, s_f64);
@@ -349,8 +389,11 @@ __global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *__r
 }
 
 // Second pass: u / (||u|| + eps) as X and X^T, a 64 x 64 tile of the caller's
-// matrix at a time (turned in LDS).  Bound by HBM: 563 us for 134 M elements
-// (16 bytes each, with momentum: 3.8 TB/s).
+// matrix at a time (turned in LDS; its values are on their way while the norm's
+// sums are added).  Bound by HBM: 441 us for 134 M elements
+// (16 bytes each, with momentum: 4.9 TB/s).  Eight neighbouring lanes write two
+// whole lines of a row, turned or not; with a row a lane the turned half took the
+// whole to 563 us.
 __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restrict__ table, int32_t nmat, Io io,
                                                               const double *sums, char *operands) {
     __shared__ double s_f64[kWaves];
@@ -359,6 +402,32 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
     const int tid = threadIdx.x;
     const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.packs; });
     const Mat &mat = table[mi];
+    const int32_t across = (mat.cols + kPackTile - 1) / kPackTile;
+    const int32_t t = int32_t(blockIdx.x) - mat.at.packs;
+    const int32_t r0 = t / across * kPackTile, c0 = t % across * kPackTile;
+    const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
+    constexpr int kPieces = kPackTile * kPackTile / 8 / kSumBlock;   // of a thread, eight values each
+    float in[kPieces][8], mom[kPieces][8];
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        const int i = q * kSumBlock + tid;
+        const int32_t r = r0 + i / 8, c = c0 + i % 8 * 8;
+        const int64_t at = mat.src + r * ld + c;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) in[q][k] = mom[q][k] = 0.0f;
+        if (r >= mat.rows) continue;
+        if (c + 8 <= mat.cols) {
+            read_in8(io, at, in[q]);
+            if (io.m != nullptr) load8(io.m + at, mom[q]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (c + k >= mat.cols) continue;
+                in[q][k] = read_in(io, at + k);
+                if (io.m != nullptr) mom[q][k] = io.m[at + k];
+            }
+        }
+    }
     const int32_t nsums = chunks_of(int64_t(mat.rows) * mat.cols);
     double sum = 0.0;
     for (int32_t i = tid; i < nsums; i += kSumBlock) sum += sums[mat.at.chunks + i];
@@ -366,21 +435,15 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
     if (tid == 0) s_norm = __fadd_rn(float(sqrt(sum)), io.eps);
     __syncthreads();
     const float norm = s_norm;
-
-    const int32_t across = (mat.cols + kPackTile - 1) / kPackTile;
-    const int32_t t = int32_t(blockIdx.x) - mat.at.packs;
-    const int32_t r0 = t / across * kPackTile, c0 = t % across * kPackTile;
-    const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
-    for (int i = tid; i < kPackTile * kPackTile; i += kSumBlock) {
-        const int32_t r = r0 + i / kPackTile, c = c0 + i % kPackTile;
-        float v = 0.0f;
-        if (r < mat.rows && c < mat.cols) {
-            const int64_t at = mat.src + r * ld + c;
-            const float in = read_in(io, at);
-            v = io.m != nullptr ? direction(io, in, io.m[at]) : in;
-            v = __fmul_rn(__fdiv_rn(v, norm), kScale);
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        const int i = q * kSumBlock + tid;
+        const int32_t r = r0 + i / 8, c = c0 + i % 8 * 8;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float v = io.m != nullptr ? direction(io, in[q][k], mom[q][k]) : in[q][k];
+            tile[i / 8][i % 8 * 8 + k] = r < mat.rows && c + k < mat.cols ? __fmul_rn(__fdiv_rn(v, norm), kScale) : 0.0f;
         }
-        tile[i / kPackTile][i % kPackTile] = v;
     }
     __syncthreads();
 
@@ -397,7 +460,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
         const int32_t row_end = turn ? mat.cols : mat.rows;
         const int32_t col_end = row_values<Prec::kSplit>(turn ? mat.rows : mat.cols);
         for (int i = tid; i < kPackTile * 8; i += kSumBlock) {
-            const int r = turn ? i % kPackTile : i / 8, c = (turn ? i / kPackTile : i % 8) * 8;
+            const int r = i / 8, c = i % 8 * 8;
             if (row_first + r >= row_end || col_first + c >= col_end) continue;
             float v[8];
 #pragma unroll
