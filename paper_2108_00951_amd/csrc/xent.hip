@@ -31,7 +31,8 @@
 // else straight into registers), and by the vector units for four tokens or
 // fewer; a second launch joins the parts.  Backward,
 // one launch leaves g in fp32, and one takes each block of w's rows to dh's
-// partial sums and writes the same rows of dw.
+// partial sums and writes the same rows of dw; four tokens of fp32 or fewer take
+// w's rows once for both.
 //
 // Tokens whose target is ignored count nowhere: what their rows of h hold is
 // never used.
@@ -701,6 +702,126 @@ __global__ __launch_bounds__(kPackBlock) void xent_dot_kernel(Xent x, Part *__re
     }
 }
 
+// One to four tokens, backward in one pass over w: a workgroup takes four words
+// at a time with the whole hidden axis in its registers, 4 kSlots values a
+// thread; the logits' sums meet in LDS, and the same registers serve
+// dh += g w and dw = g h.  h and this workgroup's share of dh stay in registers
+// throughout.  Bound by reading w and writing dw (three tokens x 56,852 x 2,758:
+// forward and this take 403 us, 4.7 TB/s over both).
+constexpr int kOnceWords = 4;
+
+template <int kTok, int kSlots>
+__global__ __launch_bounds__(kPackBlock, 2) void xent_once_kernel(Xent x, const float *__restrict__ lse,
+                                                                  const float *__restrict__ dloss,
+                                                                  float *__restrict__ dw, int64_t ld_dw,
+                                                                  float *__restrict__ part) {
+    constexpr int kSums = kOnceWords * kTok, kSame = kWave / kSums;   // lanes that get one sum
+    __shared__ float s_sum[2][kWaves][kSums], s_g[2][kSums];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    auto place = [&](int slot) { return (slot * kPackBlock + tid) * 4; };
+    auto load = [&](const void *base, int64_t row, int slot, float (&v)[4]) {
+        const int32_t k = place(slot);
+        const float *p = static_cast<const float *>(base) + row + k;
+        if (k + 4 <= x.hidden) {
+            const f32x4u a = *reinterpret_cast<const f32x4u *>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = k + e < x.hidden ? p[e] : 0.0f;
+        }
+    };
+    auto store = [&](float *row, int slot, const float (&v)[4]) {
+        const int32_t k = place(slot);
+        if (k + 4 <= x.hidden) {
+            *reinterpret_cast<f32x4u *>(row + k) = f32x4u{v[0], v[1], v[2], v[3]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (k + e < x.hidden) row[k + e] = v[e];
+        }
+    };
+    // h; zeros where a token does not count, whatever its row holds
+    float h[kTok][kSlots][4], dh[kTok][kSlots][4];
+#pragma unroll
+    for (int t = 0; t < kTok; ++t) {
+        const bool counts = t < x.tokens && target_of(x, t) >= 0;
+#pragma unroll
+        for (int q = 0; q < kSlots; ++q) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[t][q][e] = dh[t][q][e] = 0.0f;
+            if (counts) load(x.h, t * x.ld_h, q, h[t][q]);
+        }
+    }
+    // thread i < kSums: the sum of token i / 4 and word i % 4
+    const int token = tid / kOnceWords;
+    const int32_t target = tid < kSums && token < x.tokens ? target_of(x, token) : -1;
+    const float shift = target >= 0 ? lse[token] : 0.0f, weight = target >= 0 ? dloss[token] : 0.0f;
+    const int32_t groups = (x.vocab + kOnceWords - 1) / kOnceWords;
+    int turn = 0;   // the other half of LDS may still be read
+    for (int32_t group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+        const int32_t v0 = group * kOnceWords;
+        float w[kOnceWords][kSlots][4], sum[kSums];
+#pragma unroll
+        for (int r = 0; r < kOnceWords; ++r)
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) load(x.w, min(v0 + r, x.vocab - 1) * x.ld_w, q, w[r][q]);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t)
+#pragma unroll
+            for (int r = 0; r < kOnceWords; ++r) {
+                float l = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kSlots; ++q)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) l = fmaf(w[r][q][e], h[t][q][e], l);
+                sum[t * kOnceWords + r] = l;
+            }
+        const float mine = sum_scattered<kSums>(sum);
+        if (lane % kSame == 0) s_sum[turn][wave][lane / kSame] = mine;
+        __syncthreads();
+        if (tid < kSums) {
+            float l = s_sum[turn][0][tid], p = 0.0f;
+#pragma unroll
+            for (int k = 1; k < kWaves; ++k) l = __fadd_rn(l, s_sum[turn][k][tid]);
+            const int32_t v = v0 + tid % kOnceWords;
+            if (target >= 0 && v < x.vocab) {
+                p = expf(l - shift);
+                if (v == target) p = __fsub_rn(p, 1.0f);
+                p = __fmul_rn(p, weight);
+            }
+            s_g[turn][tid] = p;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOnceWords; ++r) {
+            float g[kTok];
+#pragma unroll
+            for (int t = 0; t < kTok; ++t) g[t] = s_g[turn][t * kOnceWords + r];
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) {
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = 0.0f;
+#pragma unroll
+                    for (int t = 0; t < kTok; ++t) {
+                        y[e] = fmaf(g[t], h[t][q][e], y[e]);
+                        dh[t][q][e] = fmaf(g[t], w[r][q][e], dh[t][q][e]);
+                    }
+                }
+                if (v0 + r < x.vocab) store(dw + (v0 + r) * ld_dw, q, y);
+            }
+        }
+    }
+    float *to = part + int64_t(blockIdx.x) * x.tokens * x.hidden;
+#pragma unroll
+    for (int t = 0; t < kTok; ++t)
+        if (t < x.tokens)
+#pragma unroll
+            for (int q = 0; q < kSlots; ++q) store(to + int64_t(t) * x.hidden, q, dh[t][q]);
+}
+
 // Few tokens: g as fp32 [token][word], rows `words_end` long (a multiple of 64;
 // zeros past the vocabulary and for tokens that do not count).  Bound by reading
 // w: 16 tokens x 50,001 x 1,024, bf16: 20.7 us, 5.0 TB/s.
@@ -1000,6 +1121,21 @@ constexpr int32_t kFewTokens = 64;
 template <Prec P>
 constexpr int32_t kFewForward = P == Prec::kFp32 ? 128 : 64;
 
+// Whether backward takes w in one pass, and by how many workgroups: fp32, and
+// rows that fill a workgroup's registers (half of them, of the shortest) but no
+// more.  A step of three tokens x 56,852 x 2,758: 403 us against 620 in two
+// passes, of 1 x 1,000 x 512 31 against 41, of 4 x 100,000 x 512 135 against 162.
+constexpr int32_t kOnceHidden = 4096, kOnceLeast = 512;
+bool take_once(int32_t tokens, int32_t hidden, bool fp32) {
+    return fp32 && tokens <= kDotTokens && hidden >= kOnceLeast && hidden <= kOnceHidden;
+}
+// Two to a compute unit, or four where rows are short and leave lanes idle (3 x
+// 33,278 x 700: 85 -> 77 us; 2 x 50,001 x 1,024 would take 136 for 128); with eight
+// groups of words each at least.
+int32_t once_blocks(int32_t vocab, int32_t hidden) {
+    return int32_t(std::min<int64_t>(tiles(vocab, kOnceWords * 8), hidden <= kPackBlock * 3 ? 1024 : 512));
+}
+
 // How a backward call is cut, and where everything is in the workspace.
 struct Plan {
     int32_t piece;    // words
@@ -1076,6 +1212,7 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
         // words each at least
         int64_t n = tiles(768, int(tiles(hidden, kFewHidden)));
         n = std::min(n, tiles(vocab, kFewWords * 8));
+        if (take_once(tokens, hidden, P == Prec::kSplit || P == Prec::kFp32)) n = once_blocks(vocab, hidden);
         p.few_splits = int32_t(n);
         p.few_g = take(tokens * tiles(vocab, 64) * 64 * 4);
         p.few_dh = take(n * tokens * hidden * 4);
@@ -1175,6 +1312,31 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
     const bool in_steps = direct<P>(x.w, x.ld_w, x.hidden) && direct<P>(x.h, x.ld_h, x.hidden);
     const Operand h = operand_of<P>(x.h, x.ld_h, x.tokens), w = operand_of<P>(x.w, x.ld_w, x.vocab);
     float *g = reinterpret_cast<float *>(ws + plan.few_g), *part = reinterpret_cast<float *>(ws + plan.few_dh);
+    auto finish = [&]() {
+        xent_few_join_kernel<P><<<uint32_t(tiles(int64_t(x.tokens) * x.hidden, kWave)), kPackBlock, 0, stream>>>(
+            x, part, plan.few_splits, dh, ld_dh, reinterpret_cast<Control *>(ws));
+        return hipGetLastError();
+    };
+    if constexpr (P == Prec::kFp32)
+        if (take_once(x.tokens, x.hidden, true)) {
+            auto once = [&](auto kernel) {
+                kernel<<<uint32_t(plan.few_splits), kPackBlock, 0, stream>>>(x, lse, dloss, static_cast<float *>(dw), ld_dw,
+                                                                             part);
+            };
+            auto with_slots = [&](auto slots) {
+                constexpr int n = decltype(slots)::value;
+                x.tokens == 1   ? once(xent_once_kernel<1, n>)
+                : x.tokens == 2 ? once(xent_once_kernel<2, n>)
+                                : once(xent_once_kernel<4, n>);
+            };
+            switch (tiles(x.hidden, kPackBlock * 4)) {
+                case 1: with_slots(std::integral_constant<int, 1>()); break;
+                case 2: with_slots(std::integral_constant<int, 2>()); break;
+                case 3: with_slots(std::integral_constant<int, 3>()); break;
+                case 4: with_slots(std::integral_constant<int, 4>()); break;
+            }
+            return finish();
+        }
     const int64_t words_end = tiles(x.vocab, kDotWords) * kDotWords;
     auto dot = [&](auto kernel) {
         kernel<<<uint32_t(words_end / kDotWords), kPackBlock, 0, stream>>>(x, nullptr, nullptr, lse, dloss, g, words_end);
@@ -1201,9 +1363,7 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
     if (x.tokens <= 16) run(xent_few_products_kernel<P, 1>);
     else if (x.tokens <= 32) run(xent_few_products_kernel<P, 2>);
     else run(xent_few_products_kernel<P, 4>);
-    xent_few_join_kernel<P><<<uint32_t(tiles(int64_t(x.tokens) * x.hidden, kWave)), kPackBlock, 0, stream>>>(
-        x, part, plan.few_splits, dh, ld_dh, reinterpret_cast<Control *>(ws));
-    return hipGetLastError();
+    return finish();
 }
 
 template <Prec P>

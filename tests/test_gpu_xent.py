@@ -307,3 +307,28 @@ def test_gradients_beside_their_tensors(tokens):
     for k, both, x in (("dh", both_h, h), ("dw", both_w, w)):
         assert torch.equal(both[:, 70:], want[k]), k
         assert torch.equal(both[:, :70], x), k
+
+
+@pytest.mark.parametrize("hidden, pad, shift", [(511, 0, 0), (512, 0, 0), (513, 2, 1), (1024, 0, 0), (1027, 0, 3), (2500, 4, 0),
+                                                (4095, 1, 0), (4096, 0, 1), (4097, 0, 0)])
+@pytest.mark.parametrize("tokens", [1, 2, 3, 4])
+def test_one_to_four_tokens_of_long_rows(tokens, hidden, pad, shift):
+    """Rows that a workgroup holds whole, of any length and alignment, and just
+    shorter and longer ones; a vocabulary of 331 is no multiple of anything."""
+    h, w, target, dloss = inputs(tokens, 331, hidden, "fp32", ignored=0.3)
+    buf = torch.zeros(331 * (hidden + pad) + shift, device=DEV)
+    rows = buf[shift:].view(331, hidden + pad)[:, :hidden]
+    rows.copy_(w)
+    got = call(h.to(DEV), rows, target.to(DEV), dloss.to(DEV))
+    check(got, h, w, target, dloss, "fp32")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_an_ignored_token_of_a_long_row_holds_anything(bad):
+    h, w, target, dloss = (x.to(DEV) for x in inputs(3, 90, 700, "fp32", ignored=0.0))
+    target[1] = -100
+    want = call(h, w, target, dloss)
+    h[1], dloss[1] = bad, bad
+    got = call(h, w, target, dloss)
+    for k in ("loss", "lse", "dh", "dw"):
+        assert torch.equal(got[k], want[k]), k
