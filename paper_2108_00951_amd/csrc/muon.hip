@@ -690,7 +690,8 @@ constexpr int kLdsWaves = kLdsBlock / kWave;
 constexpr int kLdsMaxM = 64;
 constexpr int kLdsFloats[2] = {8 << 10, 39 << 10};   // 32 KB: four a compute unit; 156 KB
 
-__host__ __device__ inline int32_t round16(int64_t v) { return int32_t((v + 15) / 16 * 16); }
+// (past 32 bits for the longest axes, which no workgroup takes)
+__host__ __device__ inline int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
 
 // LDS of a matrix: X, A, B.
 __host__ __device__ inline int64_t lds_floats(int32_t rows, int32_t cols) {
@@ -760,7 +761,7 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
     const int64_t dst = batch ? blockIdx.x * stride_out : mat.offset;
     const int64_t ld_in = io.ld_in ? io.ld_in : mat.cols, ld_out = io.ld_out ? io.ld_out : mat.cols;
     const bool tall = mat.rows > mat.cols;
-    const int32_t m = round16(low(mat.rows, mat.cols)), n = round16(high(mat.rows, mat.cols));
+    const int32_t m = int32_t(round16(low(mat.rows, mat.cols))), n = int32_t(round16(high(mat.rows, mat.cols)));
     const int32_t lx = n + 4, la = m + 4;
     float *X = lds, *A = X + m * lx, *B = A + m * la;
     const int32_t size = mat.rows * mat.cols;

@@ -94,3 +94,16 @@ def test_orthogonalize_takes_g_itself_and_no_other_overlap(lib):
                 (FAKE, 250, 20100, FAKE + 400, 250, 20100)):
         assert call(*bad) == binding.EFS_EINVAL, bad
         assert b"overlaps g" in lib.efs_last_error_message()
+
+
+def test_workspace_of_the_longest_axes(lib):
+    """Where the padded axis passes 32 bits a matrix is still one of the large
+    ones: two X of four bytes a value, and two X^T of 128 bytes a row."""
+    for n in (2 ** 31 - 17, 2 ** 31 - 16, 2 ** 31 - 15, 2 ** 31 - 2, 2 ** 31 - 1):
+        for rows, cols in ((1, n), (n, 1)):
+            assert lib.muon_workspace_bytes(1, i32(rows), i32(cols)) > 2 * (4 + 128) * n, (rows, cols)
+        # and a call with less is refused before it reaches a device
+        assert lib.muon_orthogonalize(FAKE, n, 0, FAKE, n, 0, 0, 1, 1, n, 5, None, 1e-7, FAKE, 2 ** 20,
+                                      None) == binding.EFS_ESPACE
+        assert lib.muon_apply(FAKE, 2 ** 34, 2 ** 35, n, 1, i64(0), i32(1), i32(n), 0.9, 0.1, 0.0, 1, 5, 1e-7, FAKE,
+                              2 ** 20, None) == binding.EFS_ESPACE
