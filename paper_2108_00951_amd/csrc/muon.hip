@@ -50,8 +50,6 @@ constexpr int kSetupBlock = 256;
 
 enum Product { kGram, kPolynomial, kApply, kLast };
 
-static_assert(kTileSide[kTiny] == 64 && kTileSide[kSmall] == 128 && kTileSide[kLarge] == 256, "64 << kind");
-
 // Running counts over the matrices before one: where its tiles, sums and
 // operands start.
 struct Place {
@@ -108,19 +106,21 @@ __host__ __device__ inline int32_t splits_of(int32_t rows, int32_t cols, int32_t
     return int32_t(s < 1 ? 1 : s);
 }
 
+// Tiles along an axis (len + side can pass 32 bits).
+__host__ __device__ inline int32_t tiles_along(int64_t len, int32_t side) { return int32_t((len + side - 1) / side); }
+
 // `most`: steps of X X^T in one workgroup.
 __host__ __device__ inline void advance(Place &p, int32_t rows, int32_t cols, int32_t most) {
     const int32_t m = int32_t(low(rows, cols)), n = int32_t(high(rows, cols));
     p.bytes += operand_bytes(rows, cols);
     for (int k = 0; k < kTileKinds; ++k) {
-        const int32_t t = 64 << k;
-        const int32_t tm = (m + t - 1) / t, tn = (n + t - 1) / t;
+        const int32_t tm = tiles_along(m, kTileSide[k]), tn = tiles_along(n, kTileSide[k]);
         p.sym[k] += tm * (tm + 1) / 2;
         p.full[k] += tm * tn;
     }
     p.chunks += chunks_of(int64_t(rows) * cols);
-    p.packs += ((rows + kPackTile - 1) / kPackTile) * ((cols + kPackTile - 1) / kPackTile);
-    const int32_t tm = (m + kTileSide[kTiny] - 1) / kTileSide[kTiny], splits = splits_of(rows, cols, most);
+    p.packs += tiles_along(rows, kPackTile) * tiles_along(cols, kPackTile);
+    const int32_t tm = tiles_along(m, kTileSide[kTiny]), splits = splits_of(rows, cols, most);
     p.units += tm * (tm + 1) / 2 * splits;
     p.parts += splits > 1 ? tm * (tm + 1) / 2 * splits : 0;
 }
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
     const int tid = threadIdx.x;
     const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.packs; });
     const Mat &mat = table[mi];
-    const int32_t across = (mat.cols + kPackTile - 1) / kPackTile;
+    const int32_t across = tiles_along(mat.cols, kPackTile);
     const int32_t t = int32_t(blockIdx.x) - mat.at.packs;
     const int32_t r0 = t / across * kPackTile, c0 = t % across * kPackTile;
     const int64_t ld = io.ld_in ? io.ld_in : mat.cols;
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_prod
         // columns where the matrix is tall
         target.turned = kProduct == kLast && mat.rows > mat.cols;
         target.diagonal = false;
-        const uint32_t tm = (m + Tile::kRows - 1) / Tile::kRows, tn = (n + Tile::kCols - 1) / Tile::kCols;
+        const uint32_t tm = tiles_along(m, Tile::kRows), tn = tiles_along(n, Tile::kCols);
         uint32_t r, q;
         if (target.turned) banded(t, tn, tm, r, q);
         else banded(t, tm, tn, r, q);

@@ -107,3 +107,12 @@ def test_workspace_of_the_longest_axes(lib):
                                       None) == binding.EFS_ESPACE
         assert lib.muon_apply(FAKE, 2 ** 34, 2 ** 35, n, 1, i64(0), i32(1), i32(n), 0.9, 0.1, 0.0, 1, 5, 1e-7, FAKE,
                               2 ** 20, None) == binding.EFS_ESPACE
+
+
+def test_workgroups_of_the_longest_axes_are_counted(lib):
+    """A 1 x n of about 2^31 values takes 33.5 M tiles of 64 values, twice: more
+    than a grid has in a batch of 200, at every n."""
+    for n in (2 ** 31 - 1024, 2 ** 31 - 256, 2 ** 31 - 60, 2 ** 31 - 1):
+        for rows, cols in ((1, n), (n, 1)):
+            assert lib.muon_workspace_bytes(200, i32(*[rows] * 200), i32(*[cols] * 200)) == 0, (rows, cols)
+            assert lib.muon_workspace_bytes(20, i32(*[rows] * 20), i32(*[cols] * 20)) > 20 * 264 * n, (rows, cols)
