@@ -422,7 +422,11 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
 /* Gradients of the sum over t of dloss[t] * loss[t]:
  *     g[t, v] = dloss[t] * (exp(l[t, v] - lse[t]) - [v == target[t]])
  *     dh = g w ;  dw = g^T h
- * The logits are formed again, a piece of the vocabulary at a time.
+ * The logits are formed again, a piece of the vocabulary at a time.  Up to 64
+ * tokens g is held in fp32 (bf16: in 16 bits).  Above, g / dloss is held in 22
+ * bits (bf16: 11), of small elements to 2^-32 of the largest of the word for
+ * dw, whatever its size, and to 2^-40 for dh, of which p - 1 at the target loses
+ * more.
  *
  *   h .. ignore_index   as for xent_forward.
  *   lse        fp32[tokens] as xent_forward left it.
@@ -432,8 +436,7 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
  *              ld_dw elements apart, overwritten (dh is 0 where a token does
  *              not count; dw is 0 with no tokens).  Must not overlap h, w or
  *              each other (other columns of the same rows are no overlap).
- *              bf16: g is rounded to 11 bits before it is
- *              multiplied, each result to bf16; sums are fp32.
+ *              Sums are fp32; bf16: each result is rounded once more.
  *   workspace  >= xent_workspace_bytes(.., 1). */
 efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,
                          const int64_t *target, int dtype, int32_t tokens, int32_t vocab,

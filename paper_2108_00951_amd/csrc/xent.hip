@@ -16,8 +16,11 @@
 // that the order of every addition is fixed.
 //
 // fp32 tensors are multiplied as split values (mfma_tile.hpp), scaled by a
-// power of two that brings the tensor's largest finite magnitude to 2^14; g by
-// 2^15 without dloss_t, which goes into h^T and into the last pass over dh.
+// power of two that brings the tensor's largest finite magnitude to 2^14; g without
+// dloss_t, which goes into h^T and into the last pass over dh.  Along the words, for
+// dh, g is scaled by 2^15: what that loses is below p - 1's own rounding at the
+// target.  Along the tokens, for dw, every word has a scale of its own, since a word
+// that is no token's target has small p alone (xent_align_kernel).
 // bf16 tensors are multiplied as they are for the logits.  For the gradients
 // they are laid out as fp16, scaled in the same way (their 8 bits fit down to
 // 2^-31 of the largest), so that g can be rounded to fp16's 11 bits.  In bf16 g
@@ -49,7 +52,8 @@ constexpr int kPackBlock = 256;
 constexpr int kPackTile = 64;
 constexpr int kJoinTokens = kWave;
 constexpr int kJoinSlices = 16;
-constexpr int kGradShift = 15;          // g's scale
+constexpr int kGradShift = 15;          // g's scale, and of a word's g beyond it:
+constexpr int kWordShift = 8, kWordShiftMost = 136;   // a multiple, the largest
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // g along both axes, one piece
 
 // The form that the gradients' products take for tensors multiplied as P.
@@ -430,14 +434,24 @@ __global__ __launch_bounds__(kPackBlock) void xent_join_few_kernel(Xent x, const
     loss[t] = counts ? __fsub_rn(v, target_logit[t]) : 0.0f;
 }
 
-// Backward: g of words [v0, v0 + words), as g [token][word] and gt [word][token].
+// A word's scale beyond 2^15 in one tile, from the largest |g| 2^15 of its tokens
+// there: a multiple of kWordShift, so that most tiles of a word agree, which still
+// leaves that value 2^7 or more.
+__device__ __forceinline__ int word_shift(uint32_t top) {
+    const int most = top == 0u ? kWordShiftMost : scale_exponent(top);   // -1 at |g| = 1
+    return min(max(most, 0) / kWordShift * kWordShift, kWordShiftMost);
+}
+
+// Backward: g of words [v0, v0 + words), as g [token][word] and gt [word][token],
+// and the words' shifts in this tile's tokens, shift [word][tile].
 // Both are written from the tile, turned in LDS, so that no pass turns g; bound
 // by the matrix cores (a piece of 8,192 words for 4,096 tokens of 4,096: 670 us in
 // fp32, 410 TFLOP/s; of 16,384 in bf16 526 us, 1045).
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad_kernel(Xent x, Operand w, Operand h, int32_t v0,
                                                                       int32_t words, const float *lse,
-                                                                      const Control *__restrict__ control, char *g, char *gt) {
+                                                                      const Control *__restrict__ control, char *g, char *gt,
+                                                                      uint8_t *shifts) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (words + Tile::kRows - 1) / Tile::kRows, tt = (x.tokens + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
@@ -473,14 +487,32 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad
     each_band<Tile::kTilesM>([&](auto index) {
         constexpr int i = decltype(index)::value;
         band.template put<i>(tile);
+        float top[Out::kUnits];
+#pragma unroll
+        for (int k = 0; k < Out::kUnits; ++k) {
+            float y[8];
+            band.get(k, y);
+            top[k] = 0.0f;   // (NaN has no part in it)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top[k] = fmaxf(top[k], fabsf(y[e]));
+        }
+        // of the word: neighbouring lanes have its tokens
+#pragma unroll
+        for (int bit = 1; bit < Out::kGroups; bit *= 2)
+#pragma unroll
+            for (int k = 0; k < Out::kUnits; ++k) top[k] = fmaxf(top[k], __shfl_xor(top[k], bit));
 #pragma unroll
         for (int k = 0; k < Out::kUnits; ++k) {
             float y[8];
             const int32_t v = row0 + Out::tile_row(i, Out::row(k)), t = col0 + Out::col(k);
+            const int more = word_shift(__float_as_uint(top[k]));
             if (v < words && t < tokens_end) {
                 band.get(k, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = ldexpf(y[e], more);
                 store8<G>(gt + v * gt_row, t, y);
             }
+            if (v < words && t == col0) shifts[int64_t(v) * tt + c] = uint8_t(more);
         }
 #pragma unroll
         for (int k = 0; k < Out::kUnits; ++k) {
@@ -494,32 +526,80 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad
     });
 }
 
+// Brings all tiles of a word in gt to the smallest of their shifts, row_shift [word].
+// A wave takes a word; values whose tile has that shift already are not touched.
+template <Prec G>
+__global__ __launch_bounds__(kPackBlock) void xent_align_kernel(char *gt, int64_t gt_row, int32_t words,
+                                                                int32_t tokens_end, int32_t width, int32_t tiles,
+                                                                const uint8_t *__restrict__ shifts,
+                                                                uint8_t *__restrict__ row_shift) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int32_t v = int32_t(blockIdx.x) * kWaves + threadIdx.x / kWave;
+    if (v >= words) return;
+    const uint8_t *mine = shifts + int64_t(v) * tiles;
+    int least = kWordShiftMost;
+    for (int32_t i = lane; i < tiles; i += kWave) least = min(least, int(mine[i]));
+#pragma unroll
+    for (int bit = 1; bit < kWave; bit *= 2) least = min(least, __shfl_xor(least, bit));
+    if (lane == 0) row_shift[v] = uint8_t(least);
+    char *row = gt + v * gt_row;
+#pragma unroll 4
+    for (int32_t t = lane * 8; t < tokens_end; t += kWave * 8) {
+        const int down = least - int(mine[t / width]);
+        if (down == 0) continue;
+        float y[8];
+        if constexpr (G == Prec::kSplit) {
+            const char *p = row + split_offset(t);
+            const f16x8 hi = *reinterpret_cast<const f16x8 *>(p), lo = *reinterpret_cast<const f16x8 *>(p + 64);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = ldexpf(__fadd_rn(float(hi[e]), float(lo[e])), down);
+        } else {
+            const f16x8 hi = *reinterpret_cast<const f16x8 *>(row + int64_t(t) * 2);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = ldexpf(float(hi[e]), down);
+        }
+        store8<G>(row, t, y);
+    }
+}
+
 // dw rows [v0, v0 + words) = g^T h.  Bound by the matrix cores (the same pieces:
 // 621 and 487 us, 442 and 1130 TFLOP/s).
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dw_kernel(Xent x, Operand gt, Operand ht, int32_t v0,
-                                                                    const Control *__restrict__ control, void *dw, int64_t ld) {
+                                                                    const Control *__restrict__ control,
+                                                                    const uint8_t *__restrict__ row_shift, void *dw,
+                                                                    int64_t ld) {
     __shared__ __align__(16) char lds[Tile::kLdsBytes];
     const uint32_t tv = (gt.rows + Tile::kRows - 1) / Tile::kRows, th = (x.hidden + Tile::kCols - 1) / Tile::kCols;
     uint32_t r, c;
     banded(xcd_place(blockIdx.x, gridDim.x), tv, th, r, c);
     const int32_t row0 = int32_t(r) * Tile::kRows, col0 = int32_t(c) * Tile::kCols;
+    uint32_t four[Tile::kTilesM][4];   // shifts of four neighbouring rows
+#pragma unroll
+    for (int i = 0; i < Tile::kTilesM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            four[i][q] = reinterpret_cast<const uint32_t *>(row_shift)[min(row0 + Tile::row_of(i, 4 * q), gt.rows - 1) / 4];
     Tile tile;
     tile.run(gt, ht, row0, col0, 0, int32_t(steps_of<kGradOf<P>>(x.tokens)), lds);
     const int exponent = -(kGradShift + scale_exponent(control->top[kTopWeighted]));
 #pragma unroll
     for (int i = 0; i < Tile::kTilesM; ++i)
 #pragma unroll
-        for (int j = 0; j < Tile::kTilesN; ++j)
+        for (int e = 0; e < 16; ++e) {
+            const int32_t v = row0 + Tile::row_of(i, e);
+            if (v >= gt.rows) continue;
+            const int of_word = exponent - int(four[i][e >> 2] >> 8 * (e & 3) & 255u);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int32_t v = row0 + Tile::row_of(i, e), k = col0 + Tile::col_of(j);
-                if (v >= gt.rows || k >= x.hidden) continue;
+            for (int j = 0; j < Tile::kTilesN; ++j) {
+                const int32_t k = col0 + Tile::col_of(j);
+                if (k >= x.hidden) continue;
                 const int64_t at = (int64_t(v0) + v) * ld + k;
-                const float y = ldexpf(tile.acc[i][j][e], exponent);
+                const float y = ldexpf(tile.acc[i][j][e], of_word);
                 if constexpr (P == Prec::kSplit) static_cast<float *>(dw)[at] = y;
                 else static_cast<__bf16 *>(dw)[at] = __bf16(y);
             }
+        }
 }
 
 // Partial sums of dh: split s adds its share of the piece's words to
@@ -1142,7 +1222,7 @@ struct Plan {
     int32_t splits;   // of a piece, for dh
     int32_t few_splits;
     int64_t target_logit, parts, h_along, w_along, forward;
-    int64_t h_turned, w_turned, g, gt, dh;   // or, of few tokens,
+    int64_t h_turned, w_turned, g, gt, shifts, row_shift, dh;   // or, of few tokens,
     int64_t few_g, few_dh;
     int64_t total;
 };
@@ -1223,6 +1303,8 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     p.w_turned = take(hidden * row_bytes<G>(vocab));
     p.g = take(tokens * row_bytes<G>(p.piece));
     p.gt = take(p.piece * row_bytes<G>(tokens));
+    p.shifts = take(p.piece * tiles(tokens, kTileSide[kTiny]));   // of the smallest tiles
+    p.row_shift = take(p.piece);
     p.dh = take(int64_t(p.splits) * tokens * hidden * 4);
     p.total = at;
     return p;
@@ -1404,16 +1486,22 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
     for (int64_t v0 = 0; v0 < x.vocab; v0 += plan.piece) {
         const int32_t words = int32_t(std::min<int64_t>(plan.piece, x.vocab - v0));
         const Operand w_piece{w.base + v0 * w.stride, w.stride, words};
+        uint8_t *shifts = reinterpret_cast<uint8_t *>(ws + plan.shifts), *row_shift = shifts;
         with_tile<P>(words, x.tokens, 1, steps_of<P>(x.hidden), [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_grad_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(
-                x, w_piece, h, int32_t(v0), words, lse, control, ws + plan.g, ws + plan.gt);
+                x, w_piece, h, int32_t(v0), words, lse, control, ws + plan.g, ws + plan.gt, shifts);
+            const int32_t across = int32_t(tiles(x.tokens, Tile::kCols));
+            if (across == 1) return;   // a word's only shift
+            row_shift = reinterpret_cast<uint8_t *>(ws + plan.row_shift);
+            xent_align_kernel<G><<<uint32_t(tiles(words, kWaves)), kPackBlock, 0, stream>>>(
+                ws + plan.gt, t_row, words, row_values<G>(x.tokens), Tile::kCols, across, shifts, row_shift);
         });
         const Operand gt{ws + plan.gt, t_row, words};
         with_tile<G>(words, x.hidden, 1, steps_of<G>(x.tokens), [&](auto tile, int64_t blocks) {
             using Tile = decltype(tile);
             xent_dw_kernel<P, Tile><<<uint32_t(blocks), Tile::kThreads, 0, stream>>>(x, gt, ht, int32_t(v0), control,
-                                                                                     dw, ld_dw);
+                                                                                     row_shift, dw, ld_dw);
         });
         // a piece starts on a whole step of w^T: it is a multiple of 256 words
         const int64_t g_row = row_bytes<G>(words);

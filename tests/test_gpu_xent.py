@@ -332,3 +332,20 @@ def test_an_ignored_token_of_a_long_row_holds_anything(bad):
     got = call(h, w, target, dloss)
     for k in ("loss", "lse", "dh", "dw"):
         assert torch.equal(got[k], want[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens, vocab, hidden", [(40, 2000, 256), (65, 500, 64), (150, 2000, 256), (700, 8000, 64)])
+@pytest.mark.parametrize("gap, spread", [(30.0, 1.0), (40.0, 1.0), (0.0, 6.0)])
+def test_words_that_no_token_finds_likely(dtype, tokens, vocab, hidden, gap, spread):
+    """Targets' logits far above the others', or logits of a standard deviation
+    of 12: the rows of dw of words with tiny probabilities alone are as near,
+    each for itself, as those of the targets."""
+    say("xent", tokens, vocab, hidden, dtype, gap, spread)
+    h, w, target, dloss = inputs(tokens, vocab, hidden, dtype, seed=3)
+    counts = target >= 0
+    h = h.float() * spread
+    h[counts] += w[target[counts]].float() * (gap / 4.0)   # |w|^2 is about 4
+    h = h.to(DTYPES[dtype])
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, h, w, target, dloss, dtype)
