@@ -276,6 +276,20 @@ __device__ __forceinline__ void read_in8(const Io &io, int64_t i, float (&v)[8])
     }
 }
 
+// What a matrix's values are divided by, from the sum of their squares.  Where 32
+// bits do not reach to it (finite values near the largest), both are taken in
+// units of 2^64.
+struct Norm {
+    float unit, norm;
+    __device__ __forceinline__ float divide(float v) const { return __fdiv_rn(__fmul_rn(v, unit), norm); }
+};
+
+__device__ __forceinline__ Norm norm_of(double sum, float eps) {
+    const float norm = __fadd_rn(float(sqrt(sum)), eps);
+    if (norm == INFINITY && sum < INFINITY) return Norm{0x1p-64f, float((sqrt(sum) + double(eps)) * 0x1p-64)};
+    return Norm{1.0f, norm};
+}
+
 // gamma sqrt(max(1, rows / cols))
 __device__ __forceinline__ float step_scale(const Io &io, int32_t rows, int32_t cols) {
     return __fmul_rn(io.gamma, sqrtf(fmaxf(1.0f, __fdiv_rn(float(rows), float(cols)))));
@@ -397,7 +411,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_momentum_kernel(const Mat *__r
 __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restrict__ table, int32_t nmat, Io io,
                                                               const double *sums, char *operands) {
     __shared__ double s_f64[kWaves];
-    __shared__ float s_norm;
+    __shared__ Norm s_norm;
     __shared__ float tile[kPackTile][kPackTile + 1];
     const int tid = threadIdx.x;
     const int32_t mi = matrix_of(table, nmat, blockIdx.x, [](const Place &p) { return p.packs; });
@@ -432,9 +446,9 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
     double sum = 0.0;
     for (int32_t i = tid; i < nsums; i += kSumBlock) sum += sums[mat.at.chunks + i];
     sum = block_sum_f64(sum, s_f64);
-    if (tid == 0) s_norm = __fadd_rn(float(sqrt(sum)), io.eps);
+    if (tid == 0) s_norm = norm_of(sum, io.eps);
     __syncthreads();
-    const float norm = s_norm;
+    const Norm norm = s_norm;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
         const int i = q * kSumBlock + tid;
@@ -442,7 +456,7 @@ __global__ __launch_bounds__(kSumBlock) void muon_pack_kernel(const Mat *__restr
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const float v = io.m != nullptr ? direction(io, in[q][k], mom[q][k]) : in[q][k];
-            tile[i / 8][i % 8 * 8 + k] = r < mat.rows && c + k < mat.cols ? __fmul_rn(__fdiv_rn(v, norm), kScale) : 0.0f;
+            tile[i / 8][i % 8 * 8 + k] = r < mat.rows && c + k < mat.cols ? __fmul_rn(norm.divide(v), kScale) : 0.0f;
         }
     }
     __syncthreads();
@@ -805,13 +819,13 @@ __global__ __launch_bounds__(kLdsBlock) void muon_lds_kernel(GivenArray given, b
     __syncthreads();
     sum = 0.0;
     for (int w = 0; w < kLdsWaves; ++w) sum += s_sum[w];
-    const float norm = __fadd_rn(float(sqrt(sum)), io.eps);
+    const Norm norm = norm_of(sum, io.eps);
     // the padding stays zero, also where the norm is zero, infinite or NaN
     for (int32_t i = tid; i < size; i += kLdsBlock) {
         int64_t at;
         int32_t to;
         place(i, 0, at, to);
-        X[to] = __fdiv_rn(X[to], norm);
+        X[to] = norm.divide(X[to]);
     }
     __syncthreads();
 

@@ -274,3 +274,26 @@ def test_orthogonalize_a_batch_in_place_and_beside_itself(rows, cols):
     assert torch.equal(g, want)
     with pytest.raises(Exception, match="overlaps g"):
         efs.muon_orthogonalize(g[:-1], g[1:], ws)
+
+
+@pytest.mark.parametrize("rows, cols", [(40, 30), (150, 70)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_norm_past_32_bits(rows, cols, dtype):
+    """Finite values whose norm fp32 does not hold: the result of the same
+    matrix in smaller units."""
+    g = torch.from_numpy(np.random.default_rng(17).standard_normal((2, rows, cols)).astype(np.float32) * np.float32(5e37))
+    g[1, 3, 4] = 3e38
+    g = g.to(dtype)
+    assert torch.isfinite(g.float()).all() and float(g.double().norm()) > 2.0 ** 128
+    got = ortho(g.to(DEV)).float().cpu().numpy()
+    for i in range(2):
+        small = g[i].float().numpy() * np.float32(2.0 ** -64)
+        rounding = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+        assert _dense.relative(got[i], _dense.newton_schulz(small)) <= _dense.ortho_limit(small) + rounding
+    x, m = torch.zeros(rows * cols, device=DEV), torch.zeros(rows * cols, device=DEV)
+    u = g[0].float()
+    efs.muon_apply(u.view(-1).to(DEV), x, m, [(0, rows, cols)], efs.new_muon_workspace([(rows, cols)], DEV), 0.0, 1.0,
+                   nesterov=False)
+    small = u.numpy() * np.float32(2.0 ** -64)
+    want = -np.sqrt(max(1.0, rows / cols)) * _dense.newton_schulz(small)
+    assert _dense.relative(x.cpu().numpy().reshape(rows, cols), want) <= _dense.ortho_limit(small) + 2.0 ** -22
