@@ -394,7 +394,8 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              fp32's precision, relative to each tensor's largest finite
  *              magnitude (elements below 2^-38 of that lose bits); bf16
  *              products are summed in fp32.
- *   tokens     0..EFS_XENT_MAX_TOKENS (0: nothing to do); vocab
+ *   tokens     0..EFS_XENT_MAX_TOKENS (0: nothing to do but to clear the status
+ *              word, where a workspace is given); vocab
  *              1..EFS_XENT_MAX_VOCAB; hidden 1..EFS_XENT_MAX_HIDDEN; tokens x
  *              vocab at most 2^38.
  *   loss, lse  fp32[tokens], overwritten.

@@ -500,13 +500,20 @@ static efs_status check_xent(const char *name, const void *h, int64_t ld_h, cons
     return EFS_OK;
 }
 
+// A call without tokens: the status word is cleared where there is one.
+static efs_status clear_xent_status(const char *name, void *workspace, size_t workspace_bytes, void *stream) {
+    if (workspace == nullptr || workspace_bytes < sizeof(uint32_t) || !aligned(workspace, 4)) return EFS_OK;
+    return check_launch(efs::launch_xent_clear(workspace, static_cast<hipStream_t>(stream)), name);
+}
+
 efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
                         int dtype, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore_index,
                         float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     const char *name = "xent_forward";
     const efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, false, workspace,
                                     workspace_bytes);
-    if (s != EFS_OK || tokens == 0) return s;
+    if (s != EFS_OK) return s;
+    if (tokens == 0) return clear_xent_status(name, workspace, workspace_bytes, stream);
     if (loss == nullptr || lse == nullptr || !aligned(loss, 4) || !aligned(lse, 4))
         return fail(EFS_EINVAL, "%s: loss and lse must be non-NULL and 4-byte aligned", name);
     return check_launch(efs::launch_xent_forward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,
@@ -526,7 +533,10 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
     const uintptr_t size = dtype == EFS_BF16 ? 2 : 4;
     if (dw == nullptr || !aligned(dw, size) || ld_dw < hidden || ld_dw > kMaxLen)
         return fail(EFS_EINVAL, "%s: dw must be non-NULL and aligned to its type, ld_dw in [hidden, 2^31-1]", name);
-    if (tokens > 0) {
+    if (tokens == 0) {
+        const efs_status cleared = clear_xent_status(name, workspace, workspace_bytes, stream);
+        if (cleared != EFS_OK) return cleared;
+    } else {
         if (dh == nullptr || !aligned(dh, size) || ld_dh < hidden || ld_dh > kMaxLen)
             return fail(EFS_EINVAL, "%s: dh must be non-NULL and aligned to its type, ld_dh in [hidden, 2^31-1]",
                         name);

@@ -66,6 +66,7 @@ hipError_t launch_muon_apply(const float *avg, int32_t nmat, const int64_t *offs
 constexpr uint32_t kXentBadTarget = 1u;   // a target neither ignored nor in the vocabulary
 constexpr int32_t kXentMaxTokens = 1 << 22, kXentMaxVocab = 1 << 24, kXentMaxHidden = 1 << 18;
 size_t xent_workspace_size(int32_t tokens, int32_t vocab, int32_t hidden, bool bf16, bool gradient);
+hipError_t launch_xent_clear(void *workspace, hipStream_t stream);
 hipError_t launch_xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,
                                bool bf16, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore, float *loss,
                                float *lse, void *workspace, hipStream_t stream);

@@ -1185,6 +1185,9 @@ __global__ __launch_bounds__(kPackBlock) void xent_few_join_kernel(Xent x, const
     else static_cast<float *>(dh)[at] = v;
 }
 
+// The status word of a call without tokens.
+__global__ void xent_clear_kernel(Control *control) { control->status = 0u; }
+
 // dw of no tokens.
 template <class T>
 __global__ __launch_bounds__(kPackBlock) void xent_zero_kernel(T *dw, int64_t ld, int32_t rows, int32_t cols) {
@@ -1525,6 +1528,11 @@ hipError_t backward(const Xent &x, const float *lse, const float *dloss, void *d
 size_t xent_workspace_size(int32_t tokens, int32_t vocab, int32_t hidden, bool bf16, bool gradient) {
     const Plan p = bf16 ? plan_of<Prec::kBf16>(tokens, vocab, hidden) : plan_of<Prec::kSplit>(tokens, vocab, hidden);
     return size_t(gradient ? p.total : p.forward);
+}
+
+hipError_t launch_xent_clear(void *workspace, hipStream_t stream) {
+    xent_clear_kernel<<<1, 1, 0, stream>>>(static_cast<Control *>(workspace));
+    return hipGetLastError();
 }
 
 hipError_t launch_xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w, const int64_t *target,

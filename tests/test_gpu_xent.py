@@ -349,3 +349,17 @@ def test_words_that_no_token_finds_likely(dtype, tokens, vocab, hidden, gap, spr
     h = h.to(DTYPES[dtype])
     got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
     check(got, h, w, target, dloss, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_no_tokens_have_no_bad_target(dtype):
+    w = torch.ones((30, 20), dtype=DTYPES[dtype], device=DEV)
+    h = torch.empty((0, 20), dtype=DTYPES[dtype], device=DEV)
+    none, target = torch.empty(0, device=DEV), torch.empty(0, dtype=torch.int64, device=DEV)
+    ws = efs.new_xent_workspace(0, 30, 20, h.dtype, DEV)
+    ws.fill_(0xFF)
+    efs.xent_forward(h, w, target, none, none, ws)
+    assert efs.xent_status(ws) == 0
+    ws.fill_(0xFF)
+    efs.xent_backward(h, w, target, none, none, h, torch.empty_like(w), ws)
+    assert efs.xent_status(ws) == 0
