@@ -400,10 +400,11 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              vocab at most 2^38.
  *   loss, lse  fp32[tokens], overwritten.
  *   workspace  >= xent_workspace_bytes(tokens, vocab, hidden, dtype, 0) bytes,
- *              16-byte aligned; contents need no initialisation.  bf16 rows
- *              that are multiples of 64 long and 16-byte aligned are read where
- *              they are; others, and fp32's, are laid out in the workspace
- *              first.  Not shareable between concurrent calls.
+ *              16-byte aligned; contents need no initialisation.  Up to 64
+ *              tokens (xent_forward of fp32: 128) h and w are read where they
+ *              are.  With more, the bytes hold a copy of both, which bf16 rows
+ *              that are multiples of 64 long and 16-byte aligned do without.
+ *              Not shareable between concurrent calls.
  * A row of h that holds NaN or infinities gives NaN, for its token alone. */
 #define EFS_XENT_MAX_TOKENS (1 << 22)
 #define EFS_XENT_MAX_VOCAB (1 << 24)

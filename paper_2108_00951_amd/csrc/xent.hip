@@ -1287,8 +1287,13 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
     };
     p.target_logit = take(int64_t(tokens) * 4);
     p.parts = take(int64_t(tokens) * tiles(vocab, kTileSide[forward_tile<P>(tokens, vocab, hidden)]) * 8);
-    p.h_along = take(tokens * row_bytes<P>(hidden));
-    p.w_along = take(vocab * row_bytes<P>(hidden));
+    // few tokens read h and w where they are
+    const bool laid_out = tokens > kFewForward<P == Prec::kSplit ? Prec::kFp32 : P>;
+    auto take_along = [&]() {
+        p.h_along = take(tokens * row_bytes<P>(hidden));
+        p.w_along = take(vocab * row_bytes<P>(hidden));
+    };
+    if (laid_out) take_along();
     p.forward = at;
     if (tokens <= kFewTokens) {
         // the workgroups that three to a compute unit make, with eight blocks of
@@ -1302,6 +1307,7 @@ Plan plan_of(int32_t tokens, int32_t vocab, int32_t hidden) {
         p.total = at;
         return p;
     }
+    if (!laid_out) take_along();
     p.h_turned = take(hidden * row_bytes<G>(tokens));
     p.w_turned = take(hidden * row_bytes<G>(vocab));
     p.g = take(tokens * row_bytes<G>(p.piece));

@@ -68,3 +68,17 @@ def test_backward_refuses_shared_elements_of_the_same_rows(lib):
         rc = lib.xent_backward(*(args[k] for k in GOOD), FAKE, FAKE, dh, 128, dw, 128, FAKE, need, None)
         assert rc == binding.EFS_EINVAL, (dh - h, dw - w)
         assert b"must not overlap" in lib.efs_last_error_message()
+
+
+def test_few_tokens_need_no_copy_of_the_head(lib):
+    vocab, hidden = 131072, 4096
+    for dtype, head in ((0, vocab * hidden * 4), (1, vocab * hidden * 2)):
+        assert lib.xent_workspace_bytes(1, vocab, hidden, dtype, 0) < 2 ** 20
+        assert lib.xent_workspace_bytes(64, vocab, hidden, dtype, 0) < head / 100
+        assert lib.xent_workspace_bytes(1, vocab, hidden, dtype, 1) < head / 50
+        assert lib.xent_workspace_bytes(64, vocab, hidden, dtype, 1) < head / 8
+        # more tokens: a copy along the rows, and for the gradients one along the columns
+        assert lib.xent_workspace_bytes(129, vocab, hidden, dtype, 0) > head
+        assert lib.xent_workspace_bytes(65, vocab, hidden, dtype, 1) > 2 * head
+    assert lib.xent_workspace_bytes(128, vocab, hidden, 0, 0) < vocab * hidden / 50
+    assert lib.xent_workspace_bytes(65, vocab, hidden, 1, 0) > vocab * hidden * 2
