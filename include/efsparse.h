@@ -324,7 +324,8 @@ enum { EFS_FP32 = 0, EFS_BF16 = 1 };
  *              each other.  May be g itself (the same pointer, ld and stride):
  *              a matrix of g is not read any more when its result is written.
  *              A batch must not overlap g in any other way; other columns of
- *              the same rows are no overlap.
+ *              the same rows are no overlap (of rows that take turns, past all of
+ *              them).
  *   dtype      EFS_FP32 or EFS_BF16, of g and out.
  *   batch, rows, cols   >= 0; rows * cols <= INT32_MAX, batch <=
  *              EFS_MUON_MAX_MATRICES.  0 of any: a call that does nothing.

@@ -55,22 +55,40 @@ bool overlap(const float *a, const float *b, int64_t d) {
     return x < y + uintptr_t(d) * 4 && y < x + uintptr_t(d) * 4;
 }
 
-// Whether two sets of rows of `cols` elements, in memory from x and y on over
-// span_a and span_b elements, can meet: their spans do, unless the rows of both
-// are `ld` elements apart throughout (0: they are not) and take different
-// columns of it.
-bool spans_meet(uintptr_t x, int64_t span_a, uintptr_t y, int64_t span_b, int64_t ld, int64_t cols, uintptr_t size) {
-    if (x >= y + uintptr_t(span_b) * size || y >= x + uintptr_t(span_a) * size) return false;
-    if (ld == 0) return true;
-    const uintptr_t row = uintptr_t(ld) * size, apart = x < y ? (y - x) % row : (row - (x - y) % row) % row;
-    return apart < uintptr_t(cols) * size || apart > row - uintptr_t(cols) * size;
+// Memory that a tensor takes, in bytes: rows of `width`, `ld` apart (0: not so
+// regular), over `span` from the first's start to the last's end.
+struct Rows {
+    uintptr_t at;
+    int64_t ld, width, span;
+};
+
+Rows rows_of(const void *p, int64_t rows, int64_t ld, int64_t cols, int64_t size) {
+    return Rows{reinterpret_cast<uintptr_t>(p), ld * size, cols * size, ((rows - 1) * ld + cols) * size};
 }
 
-// Whether two sets of rows can share an element.
-bool rows_overlap(const void *a, int64_t rows_a, int64_t ld_a, const void *b, int64_t rows_b, int64_t ld_b,
-                  int64_t cols, int64_t size) {
-    return spans_meet(reinterpret_cast<uintptr_t>(a), (rows_a - 1) * ld_a + cols, reinterpret_cast<uintptr_t>(b),
-                      (rows_b - 1) * ld_b + cols, ld_a == ld_b ? ld_a : 0, cols, uintptr_t(size));
+// A batch of matrices: their rows, where the matrices are whole rows apart; where
+// their rows take turns, as wide as all of them.
+Rows rows_of_batch(const void *p, int64_t batch, int64_t stride, int64_t rows, int64_t ld, int64_t cols, int64_t size) {
+    if (rows == 1) ld = batch > 1 && stride >= cols ? stride : cols;   // a row each
+    const int64_t wide = (batch - 1) * stride + cols;
+    Rows r = rows_of(p, rows, ld, cols, size);
+    r.span += (batch - 1) * stride * size;
+    if (batch > 1 && stride % ld != 0) {
+        r.width = wide * size;
+        if (wide > ld) r.ld = 0;
+    }
+    return r;
+}
+
+// Whether two tensors can share a byte: their spans do, unless the rows of both
+// are as far apart throughout and take different columns of that.
+bool meet(const Rows &a, const Rows &b) {
+    if (a.at >= b.at + uintptr_t(b.span) || b.at >= a.at + uintptr_t(a.span)) return false;
+    // a single row fits the other's
+    const int64_t ld = a.span == a.width ? b.ld : b.span == b.width || a.ld == b.ld ? a.ld : 0;
+    if (ld == 0) return true;
+    const uintptr_t row = uintptr_t(ld), apart = a.at < b.at ? (b.at - a.at) % row : (row - (a.at - b.at) % row) % row;
+    return apart < uintptr_t(a.width) || apart + uintptr_t(b.width) > row;
 }
 
 int g_cu_count[64];  // per device; 0 = not queried yet
@@ -409,11 +427,9 @@ efs_status muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, voi
         (stride_out < cols || ld_out < (int64_t(batch) - 1) * stride_out + cols))
         return fail(EFS_EINVAL, "%s: the matrices of out overlap", name);
     // a matrix is written when it has been read, but others may not have been
-    const int64_t span_g = (int64_t(rows) - 1) * ld_g + cols + (batch - 1) * stride_g;
-    const int64_t span_out = (int64_t(rows) - 1) * ld_out + cols + (batch - 1) * stride_out;
-    const int64_t ld = ld_g == ld_out && stride_g % ld_g == 0 && stride_out % ld_out == 0 ? ld_g : 0;
     if (batch > 1 && (g != out || ld_g != ld_out || stride_g != stride_out) &&
-        spans_meet(reinterpret_cast<uintptr_t>(g), span_g, reinterpret_cast<uintptr_t>(out), span_out, ld, cols, size))
+        meet(rows_of_batch(g, batch, stride_g, rows, ld_g, cols, size),
+             rows_of_batch(out, batch, stride_out, rows, ld_out, cols, size)))
         return fail(EFS_EINVAL, "%s: out overlaps g and is not g itself", name);
     const efs_status s = check_muon(name, batch, &rows, &cols, 0, steps, eps, workspace, workspace_bytes);
     if (s != EFS_OK) return s;
@@ -542,11 +558,11 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
                         name);
         if (lse == nullptr || dloss == nullptr || !aligned(lse, 4) || !aligned(dloss, 4))
             return fail(EFS_EINVAL, "%s: lse and dloss must be non-NULL and 4-byte aligned", name);
-        const void *given[4] = {h, w, dh, dw};
-        const int64_t rows[4] = {tokens, vocab, tokens, vocab}, ld[4] = {ld_h, ld_w, ld_dh, ld_dw};
+        const Rows given[4] = {rows_of(h, tokens, ld_h, hidden, size), rows_of(w, vocab, ld_w, hidden, size),
+                               rows_of(dh, tokens, ld_dh, hidden, size), rows_of(dw, vocab, ld_dw, hidden, size)};
         for (int i = 2; i < 4; ++i)
             for (int j = 0; j < i; ++j)
-                if (rows_overlap(given[i], rows[i], ld[i], given[j], rows[j], ld[j], hidden, size))
+                if (meet(given[i], given[j]))
                     return fail(EFS_EINVAL, "%s: dh and dw must not overlap h, w or each other", name);
     }
     return check_launch(efs::launch_xent_backward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,

@@ -363,3 +363,16 @@ def test_no_tokens_have_no_bad_target(dtype):
     ws.fill_(0xFF)
     efs.xent_backward(h, w, target, none, none, h, torch.empty_like(w), ws)
     assert efs.xent_status(ws) == 0
+
+
+def test_a_token_between_the_rows_of_a_gradient():
+    h, w, target, dloss = (x.to(DEV) for x in inputs(1, 300, 64, "fp32", ignored=0.0))
+    want = call(h, w, target, dloss)
+    both = torch.full((300, 192), 5.0, device=DEV)
+    both[7, 64:128], both[9, 128:] = h[0], 9.0
+    ws = efs.new_xent_workspace(1, 300, 64, h.dtype, DEV)
+    efs.xent_backward(both[7:8, 64:128], w, target, want["lse"], dloss, both[9:10, 128:], both[:, :64], ws)
+    assert torch.equal(both[:, :64], want["dw"]) and torch.equal(both[9:10, 128:], want["dh"])
+    assert torch.equal(both[7, 64:128], h[0]) and torch.all(both[10:, 64:] == 5.0)
+    with pytest.raises(efs.EfsError, match="must not overlap"):
+        efs.xent_backward(both[7:8, 63:127], w, target, want["lse"], dloss, both[9:10, 128:], both[:, :64], ws)

@@ -116,3 +116,17 @@ def test_workgroups_of_the_longest_axes_are_counted(lib):
         for rows, cols in ((1, n), (n, 1)):
             assert lib.muon_workspace_bytes(200, i32(*[rows] * 200), i32(*[cols] * 200)) == 0, (rows, cols)
             assert lib.muon_workspace_bytes(20, i32(*[rows] * 20), i32(*[cols] * 20)) > 20 * 264 * n, (rows, cols)
+
+
+def test_orthogonalize_into_other_columns_of_the_same_rows(lib):
+    def call(rows, ldg, sg, o, ldo, so):
+        return lib.muon_orthogonalize(FAKE, ldg, sg, o, ldo, so, 0, 3, rows, 100, 5, None, 1e-7, FAKE, 0, None)
+    # accepted (only the workspace is refused): matrices whose rows take turns, matrices of one row
+    for good in ((80, 600, 100, FAKE + 1200, 600, 100), (1, 100, 200, FAKE + 400, 100, 200),
+                 (1, 200, 200, FAKE + 400, 100, 200), (1, 100, 0, FAKE + 400, 100, 100)):
+        assert call(*good) == binding.EFS_ESPACE, good
+    for bad in ((80, 600, 100, FAKE + 1196, 600, 100), (80, 600, 100, FAKE + 1204, 600, 100),
+                (80, 600, 100, FAKE + 1200, 500, 100), (1, 100, 200, FAKE + 396, 100, 200),
+                (1, 100, 200, FAKE + 404, 100, 200), (1, 100, 50, FAKE + 400, 100, 200)):
+        assert call(*bad) == binding.EFS_EINVAL, bad
+        assert b"overlaps g" in lib.efs_last_error_message()
