@@ -338,8 +338,8 @@ enum { EFS_FP32 = 0, EFS_BF16 = 1 };
  *   eps        added to the norm (finite, >= 0): a matrix of zeros gives zeros
  *              (with eps = 0 NaN, as 0 / 0).
  *   workspace  >= muon_workspace_bytes for these matrices, 16-byte aligned;
- *              contents need no initialisation and are not kept.  Not
- *              shareable between concurrent calls.
+ *              contents need no initialisation and are not kept.  Must not
+ *              overlap the matrices.  Not shareable between concurrent calls.
  * A matrix that holds NaN or infinities gives NaN; the others of the batch
  * are not affected. */
 #define EFS_MUON_MAX_MATRICES 65536
@@ -399,7 +399,8 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              word, where a workspace is given); vocab
  *              1..EFS_XENT_MAX_VOCAB; hidden 1..EFS_XENT_MAX_HIDDEN; tokens x
  *              vocab at most 2^38.
- *   loss, lse  fp32[tokens], overwritten.
+ *   loss, lse  fp32[tokens], overwritten.  They and the workspace must not
+ *              overlap each other or an input.
  *   workspace  >= xent_workspace_bytes(tokens, vocab, hidden, dtype, 0) bytes,
  *              16-byte aligned; contents need no initialisation.  Up to 64
  *              tokens (xent_forward of fp32: 128) h and w are read where they
@@ -437,8 +438,9 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
  *              where the token does not count.
  *   dh, dw     tokens x hidden and vocab x hidden of dtype, rows ld_dh and
  *              ld_dw elements apart, overwritten (dh is 0 where a token does
- *              not count; dw is 0 with no tokens).  Must not overlap h, w or
- *              each other (other columns of the same rows are no overlap).
+ *              not count; dw is 0 with no tokens).  They and the workspace must
+ *              not overlap each other or an input (other columns of the same rows
+ *              are no overlap).
  *              Sums are fp32; bf16: each result is rounded once more.
  *   workspace  >= xent_workspace_bytes(.., 1). */
 efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,

@@ -91,6 +91,26 @@ bool meet(const Rows &a, const Rows &b) {
     return apart < uintptr_t(a.width) || apart + uintptr_t(b.width) > row;
 }
 
+// A tensor of a call, under its name; what is written meets no other one.
+struct Given {
+    const char *name;
+    Rows rows;
+    bool written;
+};
+
+Given flat(const char *name, const void *p, int64_t bytes, bool written) {
+    return Given{name, Rows{reinterpret_cast<uintptr_t>(p), bytes, bytes, bytes}, written};
+}
+
+template <int N>
+efs_status check_apart(const char *name, const Given (&given)[N]) {
+    for (int i = 0; i < N; ++i)
+        for (int j = 0; j < i; ++j)
+            if ((given[i].written || given[j].written) && meet(given[i].rows, given[j].rows))
+                return fail(EFS_EINVAL, "%s: %s and %s must not overlap", name, given[j].name, given[i].name);
+    return EFS_OK;
+}
+
 int g_cu_count[64];  // per device; 0 = not queried yet
 
 }  // namespace
@@ -376,7 +396,8 @@ efs_status sparse_apply(const int32_t *const *idx, const float *const *val,
 // What the two orthogonalising calls check alike.  next: from one matrix's
 // entry of rows and cols to the next's (0: all alike).
 static efs_status check_muon(const char *name, int32_t nmat, const int32_t *rows, const int32_t *cols,
-                             int32_t next, int32_t steps, float eps, const void *workspace, size_t workspace_bytes) {
+                             int32_t next, int32_t steps, float eps, const void *workspace, size_t workspace_bytes,
+                             int64_t *used) {
     if (steps < 1 || steps > efs::kMuonMaxSteps)
         return fail(EFS_EINVAL, "%s: steps=%d outside [1, %d]", name, steps, efs::kMuonMaxSteps);
     if (!std::isfinite(eps) || eps < 0.0f) return fail(EFS_EINVAL, "%s: eps must be finite and >= 0", name);
@@ -387,6 +408,7 @@ static efs_status check_muon(const char *name, int32_t nmat, const int32_t *rows
         return fail(EFS_EINVAL, "%s: workspace must be non-NULL and 16-byte aligned", name);
     if (workspace_bytes < need)
         return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    *used = int64_t(need);
     return EFS_OK;
 }
 
@@ -431,7 +453,13 @@ efs_status muon_orthogonalize(const void *g, int64_t ld_g, int64_t stride_g, voi
         meet(rows_of_batch(g, batch, stride_g, rows, ld_g, cols, size),
              rows_of_batch(out, batch, stride_out, rows, ld_out, cols, size)))
         return fail(EFS_EINVAL, "%s: out overlaps g and is not g itself", name);
-    const efs_status s = check_muon(name, batch, &rows, &cols, 0, steps, eps, workspace, workspace_bytes);
+    int64_t used = 0;
+    efs_status s = check_muon(name, batch, &rows, &cols, 0, steps, eps, workspace, workspace_bytes, &used);
+    if (s != EFS_OK) return s;
+    const Given given[3] = {{"g", rows_of_batch(g, batch, stride_g, rows, ld_g, cols, size), false},
+                            {"out", rows_of_batch(out, batch, stride_out, rows, ld_out, cols, size), false},
+                            flat("workspace", workspace, used, true)};   // (g and out: above)
+    s = check_apart(name, given);
     if (s != EFS_OK) return s;
     return check_launch(efs::launch_muon_orthogonalize(g, ld_g, stride_g, out, ld_out, stride_out,
                                                        dtype == EFS_BF16, batch, rows, cols, steps, coeffs,
@@ -470,7 +498,12 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
         return fail(EFS_EINVAL, "%s: avg, x and m must be non-NULL and 4-byte aligned", name);
     if (overlap(avg, x, d) || overlap(avg, m, d) || overlap(x, m, d))
         return fail(EFS_EINVAL, "%s: avg, x and m must not overlap", name);
-    const efs_status s = check_muon(name, nmat, rows, cols, 1, steps, eps, workspace, workspace_bytes);
+    int64_t used = 0;
+    efs_status s = check_muon(name, nmat, rows, cols, 1, steps, eps, workspace, workspace_bytes, &used);
+    if (s != EFS_OK) return s;
+    const Given given[4] = {flat("avg", avg, d * 4, false), flat("x", x, d * 4, true), flat("m", m, d * 4, true),
+                            flat("workspace", workspace, used, true)};
+    s = check_apart(name, given);
     if (s != EFS_OK) return s;
     return check_launch(efs::launch_muon_apply(avg, nmat, offsets, rows, cols, x, m, beta, gamma, decay,
                                                nesterov != 0, steps, kCoeffs, eps, workspace,
@@ -494,7 +527,7 @@ size_t xent_status_offset(void) { return 0; }
 // What both directions check alike.  Their rows: pointer, elements between them.
 static efs_status check_xent(const char *name, const void *h, int64_t ld_h, const void *w, int64_t ld_w,
                              const int64_t *target, int dtype, int32_t tokens, int32_t vocab, int32_t hidden,
-                             bool gradient, const void *workspace, size_t workspace_bytes) {
+                             bool gradient, const void *workspace, size_t workspace_bytes, int64_t *used) {
     if (dtype != EFS_FP32 && dtype != EFS_BF16)
         return fail(EFS_EINVAL, "%s: dtype %d is neither EFS_FP32 nor EFS_BF16", name, dtype);
     if (!xent_sizes_ok(tokens, vocab, hidden, dtype))
@@ -513,6 +546,7 @@ static efs_status check_xent(const char *name, const void *h, int64_t ld_h, cons
     const size_t need = efs::xent_workspace_size(tokens, vocab, hidden, dtype == EFS_BF16, gradient);
     if (workspace_bytes < need)
         return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    *used = int64_t(need);
     return EFS_OK;
 }
 
@@ -526,12 +560,20 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
                         int dtype, int32_t tokens, int32_t vocab, int32_t hidden, int64_t ignore_index,
                         float *loss, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
     const char *name = "xent_forward";
-    const efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, false, workspace,
-                                    workspace_bytes);
+    int64_t used = 0;
+    efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, false, workspace,
+                              workspace_bytes, &used);
     if (s != EFS_OK) return s;
     if (tokens == 0) return clear_xent_status(name, workspace, workspace_bytes, stream);
     if (loss == nullptr || lse == nullptr || !aligned(loss, 4) || !aligned(lse, 4))
         return fail(EFS_EINVAL, "%s: loss and lse must be non-NULL and 4-byte aligned", name);
+    const int64_t size = dtype == EFS_BF16 ? 2 : 4, t = tokens;
+    const Given given[6] = {{"h", rows_of(h, t, ld_h, hidden, size), false},
+                            {"w", rows_of(w, vocab, ld_w, hidden, size), false},
+                            flat("target", target, t * 8, false), flat("loss", loss, t * 4, true),
+                            flat("lse", lse, t * 4, true), flat("workspace", workspace, used, true)};
+    s = check_apart(name, given);
+    if (s != EFS_OK) return s;
     return check_launch(efs::launch_xent_forward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,
                                                  hidden, ignore_index, loss, lse, workspace,
                                                  static_cast<hipStream_t>(stream)),
@@ -543,8 +585,9 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
                          const float *lse, const float *dloss, void *dh, int64_t ld_dh, void *dw, int64_t ld_dw,
                          void *workspace, size_t workspace_bytes, void *stream) {
     const char *name = "xent_backward";
-    const efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, true, workspace,
-                                    workspace_bytes);
+    int64_t used = 0;
+    efs_status s = check_xent(name, h, ld_h, w, ld_w, target, dtype, tokens, vocab, hidden, true, workspace,
+                              workspace_bytes, &used);
     if (s != EFS_OK) return s;
     const uintptr_t size = dtype == EFS_BF16 ? 2 : 4;
     if (dw == nullptr || !aligned(dw, size) || ld_dw < hidden || ld_dw > kMaxLen)
@@ -558,12 +601,15 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
                         name);
         if (lse == nullptr || dloss == nullptr || !aligned(lse, 4) || !aligned(dloss, 4))
             return fail(EFS_EINVAL, "%s: lse and dloss must be non-NULL and 4-byte aligned", name);
-        const Rows given[4] = {rows_of(h, tokens, ld_h, hidden, size), rows_of(w, vocab, ld_w, hidden, size),
-                               rows_of(dh, tokens, ld_dh, hidden, size), rows_of(dw, vocab, ld_dw, hidden, size)};
-        for (int i = 2; i < 4; ++i)
-            for (int j = 0; j < i; ++j)
-                if (meet(given[i], given[j]))
-                    return fail(EFS_EINVAL, "%s: dh and dw must not overlap h, w or each other", name);
+        const int64_t t = tokens;
+        const Given given[8] = {{"h", rows_of(h, t, ld_h, hidden, size), false},
+                                {"w", rows_of(w, vocab, ld_w, hidden, size), false},
+                                {"dh", rows_of(dh, t, ld_dh, hidden, size), true},
+                                {"dw", rows_of(dw, vocab, ld_dw, hidden, size), true},
+                                flat("target", target, t * 8, false), flat("lse", lse, t * 4, false),
+                                flat("dloss", dloss, t * 4, false), flat("workspace", workspace, used, true)};
+        s = check_apart(name, given);
+        if (s != EFS_OK) return s;
     }
     return check_launch(efs::launch_xent_backward(h, ld_h, w, ld_w, target, dtype == EFS_BF16, tokens, vocab,
                                                   hidden, ignore_index, lse, dloss, dh, ld_dh, dw, ld_dw,

@@ -130,3 +130,15 @@ def test_orthogonalize_into_other_columns_of_the_same_rows(lib):
                 (1, 100, 200, FAKE + 404, 100, 200), (1, 100, 50, FAKE + 400, 100, 200)):
         assert call(*bad) == binding.EFS_EINVAL, bad
         assert b"overlaps g" in lib.efs_last_error_message()
+
+
+def test_the_workspace_meets_nothing_else(lib):
+    need = lib.muon_workspace_bytes(2, i32(80, 80), i32(100, 100))
+    for g, out, ws in ((FAKE, 2 ** 24, FAKE + 63984), (2 ** 24, FAKE, FAKE), (FAKE, 2 ** 24, 2 ** 24 - need // 16 * 16 + 16)):
+        rc = lib.muon_orthogonalize(g, 100, 8000, out, 100, 8000, 0, 2, 80, 100, 5, None, 1e-7, ws, need, None)
+        assert rc == binding.EFS_EINVAL and b"must not overlap" in lib.efs_last_error_message()
+    need = lib.muon_workspace_bytes(1, i32(80), i32(100))
+    for k in range(3):
+        at = [2 ** 24, 2 ** 25, 2 ** 26]
+        rc = lib.muon_apply(*at, 8000, 1, i64(0), i32(80), i32(100), 0.9, 0.1, 0.0, 1, 5, 1e-7, at[k] + 31984, need, None)
+        assert rc == binding.EFS_EINVAL and b"must not overlap" in lib.efs_last_error_message()

@@ -82,3 +82,28 @@ def test_few_tokens_need_no_copy_of_the_head(lib):
         assert lib.xent_workspace_bytes(65, vocab, hidden, dtype, 1) > 2 * head
     assert lib.xent_workspace_bytes(128, vocab, hidden, 0, 0) < vocab * hidden / 50
     assert lib.xent_workspace_bytes(65, vocab, hidden, 1, 0) > vocab * hidden * 2
+
+
+def test_what_is_written_meets_nothing_else(lib):
+    """h 2,560 bytes, w 256,000, the vectors 40 and 80, at places of their own;
+    one of them moved into another by an element."""
+    at = dict(h=FAKE, w=4 * FAKE, target=5 * FAKE, loss=6 * FAKE, lse=7 * FAKE, dloss=8 * FAKE, dh=9 * FAKE, dw=10 * FAKE,
+              ws=12 * FAKE)
+
+    def call(gradient, **over):
+        a = dict(at, **over)
+        head = (a["h"], 64, a["w"], 64, a["target"], 0, 10, 1000, 64, -100)
+        need = lib.xent_workspace_bytes(10, 1000, 64, 0, int(gradient))
+        if gradient:
+            return lib.xent_backward(*head, a["lse"], a["dloss"], a["dh"], 64, a["dw"], 64, a["ws"], need, None)
+        return lib.xent_forward(*head, a["loss"], a["lse"], a["ws"], need, None)
+    forward = [dict(loss=at["lse"]), dict(loss=at["lse"] + 36), dict(lse=at["loss"] - 36), dict(loss=at["h"] + 2556),
+               dict(lse=at["w"] - 36), dict(lse=at["w"] + 255996), dict(loss=at["target"] + 76), dict(loss=at["ws"]),
+               dict(lse=at["ws"] - 36), dict(ws=at["h"]), dict(ws=at["w"] + 16), dict(ws=at["target"])]
+    backward = [dict(lse=at["dh"]), dict(dloss=at["dh"] + 2556), dict(lse=at["dw"] - 36), dict(dloss=at["dw"] + 255996),
+                dict(target=at["dw"]), dict(target=at["dh"] - 72), dict(dloss=at["ws"]), dict(lse=at["ws"] - 36),
+                dict(ws=at["dw"]), dict(ws=at["dh"]), dict(ws=at["h"] + 2544), dict(dh=at["dw"]), dict(dw=at["w"])]
+    for gradient, cases in ((False, forward), (True, backward)):
+        for over in cases:
+            assert call(gradient, **over) == binding.EFS_EINVAL, over
+            assert b"must not overlap" in lib.efs_last_error_message(), over
