@@ -483,11 +483,19 @@ def _row_stride(t) -> int:
     return t.stride(-2) if t.shape[-2] > 1 else t.shape[-1]
 
 
+def _int32(v, name) -> int:
+    """ctypes would pass the low 32 bits of a larger value."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s does not fit 32 bits: %d" % (name, v))
+    return v
+
+
 def _shape_arrays(shapes: Sequence[Tuple[int, int]]):
     n = max(len(shapes), 1)
     rows, cols = (ctypes.c_int32 * n)(), (ctypes.c_int32 * n)()
     for i, (r, c) in enumerate(shapes):
-        rows[i], cols[i] = int(r), int(c)
+        rows[i], cols[i] = _int32(r, "rows"), _int32(c, "cols")
     return rows, cols
 
 
@@ -522,8 +530,9 @@ def muon_orthogonalize(g, out, workspace, steps: int = 5, coeffs=None, eps: floa
     rows, cols = g.shape[-2:]
     co = None if coeffs is None else (ctypes.c_float * 3)(*(float(v) for v in coeffs))
     rc = lib.muon_orthogonalize(_ptr(g), _row_stride(g), g.stride(0) if batch > 1 else 0, _ptr(out),
-                                _row_stride(out), out.stride(0) if batch > 1 else 0, dtype, batch, rows, cols,
-                                int(steps), co, float(eps), _ptr(workspace), workspace.numel(),
+                                _row_stride(out), out.stride(0) if batch > 1 else 0, dtype,
+                                _int32(batch, "batch"), _int32(rows, "rows"), _int32(cols, "cols"),
+                                _int32(steps, "steps"), co, float(eps), _ptr(workspace), workspace.numel(),
                                 _stream_handle(stream))
     _check(lib, rc)
 
@@ -543,7 +552,7 @@ def prepare_muon_apply(avg, x, m, layers: Sequence[Tuple[int, int, int]], worksp
     offsets = (ctypes.c_int64 * max(len(layers), 1))(*(int(v[0]) for v in layers))
     rows, cols = _shape_arrays([v[1:] for v in layers])
     args = (_ptr(avg), _ptr(x), _ptr(m), x.numel(), len(layers), offsets, rows, cols, float(beta),
-            float(gamma), float(weight_decay), int(bool(nesterov)), int(steps), float(eps),
+            float(gamma), float(weight_decay), int(bool(nesterov)), _int32(steps, "steps"), float(eps),
             _ptr(workspace), workspace.numel(), _stream_handle(stream))
     fn = lib.muon_apply
 
@@ -566,8 +575,8 @@ def muon_apply(avg, x, m, layers: Sequence[Tuple[int, int, int]], workspace, bet
 def xent_workspace_bytes(tokens: int, vocab: int, hidden: int, dtype, gradient: bool = True) -> int:
     import torch
     code = {torch.float32: FP32, torch.bfloat16: BF16}[dtype]
-    return int(load_library().xent_workspace_bytes(int(tokens), int(vocab), int(hidden), code,
-                                                   int(bool(gradient))))
+    return int(load_library().xent_workspace_bytes(_int32(tokens, "tokens"), _int32(vocab, "vocab"),
+                                                   _int32(hidden, "hidden"), code, int(bool(gradient))))
 
 
 def new_xent_workspace(tokens: int, vocab: int, hidden: int, dtype, device="cuda", gradient: bool = True):
@@ -597,8 +606,8 @@ def _xent_args(h, w, target):
     _require_rows(h, "h")
     _require_rows(w, "w")
     _require(target, torch.int64, "target")
-    return (_ptr(h), _row_stride(h), _ptr(w), _row_stride(w), _ptr(target), dtype, h.shape[0], w.shape[0],
-            h.shape[1])
+    return (_ptr(h), _row_stride(h), _ptr(w), _row_stride(w), _ptr(target), dtype, _int32(h.shape[0], "tokens"),
+            _int32(w.shape[0], "vocab"), _int32(h.shape[1], "hidden"))
 
 
 def xent_forward(h, w, target, loss, lse, workspace, ignore_index: int = -100, stream=None) -> None:

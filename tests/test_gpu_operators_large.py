@@ -85,3 +85,23 @@ def test_prepared_update_keeps_its_tensors():
     del call
     gc.collect()
     assert all(r() is None for r in alive)
+
+
+def test_tensors_of_more_rows_than_32_bits_count_are_refused():
+    """Their low 32 bits would pass for a size."""
+    many = torch.empty((2 ** 32 + 8, 1), dtype=torch.bfloat16, device=DEV)
+    ws = efs.new_muon_workspace([(8, 1)], DEV)
+    with pytest.raises(ValueError, match="32 bits"):
+        efs.muon_orthogonalize(many, many, ws)
+    with pytest.raises(ValueError, match="32 bits"):
+        efs.muon_orthogonalize(many.t(), many.t(), ws)
+    with pytest.raises(ValueError, match="32 bits"):
+        efs.muon_orthogonalize(torch.ones((8, 1), device=DEV), torch.ones((8, 1), device=DEV), ws, steps=2 ** 32 + 5)
+    h = torch.ones((2, 1), dtype=torch.bfloat16, device=DEV)
+    target, f = torch.zeros(2, dtype=torch.int64, device=DEV), torch.empty(2, device=DEV)
+    ws = efs.new_xent_workspace(2, 8, 1, h.dtype, DEV)
+    with pytest.raises(ValueError, match="32 bits"):
+        efs.xent_forward(h, many, target, f, torch.empty_like(f), ws)
+    flat = torch.zeros(40, device=DEV)
+    with pytest.raises(ValueError, match="32 bits"):
+        efs.muon_apply(flat, flat.clone(), flat.clone(), [(0, 2 ** 32 + 4, 5)], ws, 0.9, 0.1)

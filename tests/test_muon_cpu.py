@@ -142,3 +142,11 @@ def test_the_workspace_meets_nothing_else(lib):
         at = [2 ** 24, 2 ** 25, 2 ** 26]
         rc = lib.muon_apply(*at, 8000, 1, i64(0), i32(80), i32(100), 0.9, 0.1, 0.0, 1, 5, 1e-7, at[k] + 31984, need, None)
         assert rc == binding.EFS_EINVAL and b"must not overlap" in lib.efs_last_error_message()
+
+
+def test_sizes_past_32_bits_do_not_wrap():
+    for shape in ((2 ** 32 + 3, 5), (5, 2 ** 32 + 3), (2 ** 31, 1), (-2 ** 32 + 3, 5)):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.muon_workspace_bytes([(4, 4), shape])
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.new_muon_workspace([shape], "cpu")

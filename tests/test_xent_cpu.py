@@ -107,3 +107,10 @@ def test_what_is_written_meets_nothing_else(lib):
         for over in cases:
             assert call(gradient, **over) == binding.EFS_EINVAL, over
             assert b"must not overlap" in lib.efs_last_error_message(), over
+
+
+def test_sizes_past_32_bits_do_not_wrap():
+    import torch
+    for sizes in ((2 ** 32 + 3, 50, 8), (3, 2 ** 32 + 50, 8), (3, 50, 2 ** 31)):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.xent_workspace_bytes(*sizes, torch.float32)
