@@ -508,7 +508,10 @@ def new_muon_workspace(shapes: Sequence[Tuple[int, int]], device="cuda"):
     """A workspace for muon_orthogonalize or muon_apply over matrices of these
     (rows, cols)."""
     import torch
-    return torch.empty(max(muon_workspace_bytes(shapes), 16), dtype=torch.uint8, device=device)
+    nbytes = muon_workspace_bytes(shapes)
+    if nbytes == 0:
+        raise ValueError("the matrices are out of range (sizes, or too many for one call)")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def muon_orthogonalize(g, out, workspace, steps: int = 5, coeffs=None, eps: float = 1e-7,
@@ -582,8 +585,10 @@ def xent_workspace_bytes(tokens: int, vocab: int, hidden: int, dtype, gradient: 
 def new_xent_workspace(tokens: int, vocab: int, hidden: int, dtype, device="cuda", gradient: bool = True):
     """A workspace for xent_forward and, with gradient, xent_backward."""
     import torch
-    return torch.empty(max(xent_workspace_bytes(tokens, vocab, hidden, dtype, gradient), 16),
-                       dtype=torch.uint8, device=device)
+    nbytes = xent_workspace_bytes(tokens, vocab, hidden, dtype, gradient)
+    if nbytes == 0:
+        raise ValueError("%d tokens, %d words or %d values a row are out of range" % (tokens, vocab, hidden))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 XENT_BAD_TARGET = 1

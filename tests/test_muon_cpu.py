@@ -150,3 +150,12 @@ def test_sizes_past_32_bits_do_not_wrap():
             binding.muon_workspace_bytes([(4, 4), shape])
         with pytest.raises(ValueError, match="32 bits"):
             binding.new_muon_workspace([shape], "cpu")
+
+
+def test_no_workspace_for_matrices_that_no_call_takes():
+    for shapes in ([(65536, 65536)], [(-1, 4)], [(2, 2)] * 65537):
+        assert binding.muon_workspace_bytes(shapes) == 0
+        with pytest.raises(ValueError, match="out of range"):
+            binding.new_muon_workspace(shapes, "cpu")
+    assert binding.new_muon_workspace([], "cpu").numel() >= 16
+    assert binding.new_muon_workspace([(0, 5)], "cpu").numel() >= 16

@@ -114,3 +114,11 @@ def test_sizes_past_32_bits_do_not_wrap():
     for sizes in ((2 ** 32 + 3, 50, 8), (3, 2 ** 32 + 50, 8), (3, 50, 2 ** 31)):
         with pytest.raises(ValueError, match="32 bits"):
             binding.xent_workspace_bytes(*sizes, torch.float32)
+
+
+def test_no_workspace_for_sizes_that_no_call_takes():
+    import torch
+    for sizes in ((-1, 50, 8), (3, 0, 8), (3, 50, 2 ** 18 + 1)):
+        with pytest.raises(ValueError, match="out of range"):
+            binding.new_xent_workspace(*sizes, torch.float32, "cpu")
+    assert binding.new_xent_workspace(0, 50, 8, torch.float32, "cpu").numel() >= 16
