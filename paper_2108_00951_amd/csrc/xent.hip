@@ -90,16 +90,13 @@ template <Prec P>
 __device__ __forceinline__ void store8(char *row, int32_t c, const float (&y)[8]) {
     if constexpr (P == Prec::kSplit) {
         store_split8(row, c, y);
-    } else if constexpr (P == Prec::kFp32) {
-        f32x4 *p = reinterpret_cast<f32x4 *>(row + int64_t(c) * 4);
-        p[0] = f32x4{y[0], y[1], y[2], y[3]};
-        p[1] = f32x4{y[4], y[5], y[6], y[7]};
     } else if constexpr (P == Prec::kHalf) {
         f16x8 v;
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = _Float16(y[k]);
         *reinterpret_cast<f16x8 *>(row + int64_t(c) * 2) = v;
     } else {
+        static_assert(P == Prec::kBf16, "fp32 operands are not laid out as they are");
         bf16x8 v;
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = __bf16(y[k]);
@@ -1356,11 +1353,13 @@ void pack_operands(const Xent &x, const float *dloss, bool gradient, const Plan 
     *w = pack(true, x.w, x.ld_w, x.vocab, plan.w_along, plan.w_turned);
 }
 
-template <Prec P, class F>
+// Calls run with the narrow tile of `tokens`, kMost at most.
+template <Prec P, int32_t kMost, class F>
 void with_narrow_tile(int32_t tokens, F run) {
+    static_assert(kMost == 64 || kMost == 128, "whole tiles");
     if (tokens <= 32) run(NarrowTile<P, 1>());
-    else if (tokens <= 64) run(NarrowTile<P, 2>());
-    else run(NarrowTile<P, 4>());
+    else if (kMost == 64 || tokens <= 64) run(NarrowTile<P, 2>());
+    else if constexpr (kMost == 128) run(NarrowTile<P, 4>());
 }
 
 // Few tokens: the operands are the tensors themselves.
@@ -1384,7 +1383,7 @@ hipError_t forward_few(const Xent &x, const Plan &plan, float *loss, float *lse,
         x.tokens == 1   ? dot(xent_dot_kernel<P, 1, false>)
         : x.tokens == 2 ? dot(xent_dot_kernel<P, 2, false>)
                         : dot(xent_dot_kernel<P, 4, false>);
-    else with_narrow_tile<P>(x.tokens, [&](auto tile) {
+    else with_narrow_tile<P, kFewForward<P>>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
         static_assert(Tile::kRows == kDotWords, "parts of as many words");
         auto run = [&](auto kernel) {
@@ -1436,16 +1435,14 @@ hipError_t backward_few(const Xent &x, const Plan &plan, const float *lse, const
         x.tokens == 1   ? dot(xent_dot_kernel<P, 1, true>)
         : x.tokens == 2 ? dot(xent_dot_kernel<P, 2, true>)
                         : dot(xent_dot_kernel<P, 4, true>);
-    else with_narrow_tile<P>(x.tokens, [&](auto tile) {
+    else with_narrow_tile<P, kFewTokens>(x.tokens, [&](auto tile) {
         using Tile = decltype(tile);
         static_assert(Tile::kRows == kDotWords, "g's rows end with the tiles");
-        if constexpr (Tile::kCols <= kFewTokens) {
-            auto run = [&](auto kernel) {
-                kernel<<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(x, w, h, lse, dloss, g,
-                                                                                             words_end);
-            };
-            in_steps ? run(xent_few_grad_kernel<P, Tile, false>) : run(xent_few_grad_kernel<P, Tile, true>);
-        }
+        auto run = [&](auto kernel) {
+            kernel<<<uint32_t(tiles(x.vocab, Tile::kRows)), Tile::kThreads, 0, stream>>>(x, w, h, lse, dloss, g,
+                                                                                         words_end);
+        };
+        in_steps ? run(xent_few_grad_kernel<P, Tile, false>) : run(xent_few_grad_kernel<P, Tile, true>);
     });
     const uint32_t blocks = uint32_t(tiles(x.hidden, kFewHidden) * plan.few_splits);
     auto run = [&](auto kernel) {
