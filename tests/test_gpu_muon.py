@@ -297,3 +297,102 @@ def test_a_norm_past_32_bits(rows, cols, dtype):
     small = u.numpy() * np.float32(2.0 ** -64)
     want = -np.sqrt(max(1.0, rows / cols)) * _dense.newton_schulz(small)
     assert _dense.relative(x.cpu().numpy().reshape(rows, cols), want) <= _dense.ortho_limit(small) + 2.0 ** -22
+
+
+def _iterated(g, dtype):
+    """A batch through the formula by torch's products in `dtype`."""
+    tall = g.shape[-2] > g.shape[-1]
+    x = (g.transpose(-2, -1) if tall else g).to(dtype).contiguous()
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + 1e-7)
+    for _ in range(5):
+        a = torch.matmul(x, x.transpose(-2, -1).contiguous())
+        x = 3.4445 * x + torch.matmul(-4.7750 * a + 2.0315 * torch.matmul(a, a), x)
+    return x.transpose(-2, -1) if tall else x
+
+
+# By the rule for tiles on 256 compute units (X X^T, b A + c A A, a X + B X): 256 each;
+# 256 each, turned at the end; 128 each; 128 each, turned; 128, 128, 256; 64, 64, 256.
+@pytest.mark.parametrize("batch, rows, cols", [(200, 250, 500), (200, 500, 250), (256, 250, 300), (256, 300, 250),
+                                               (4, 1500, 1490), (40, 512, 520)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_product_with_every_tile(dtype, batch, rows, cols):
+    say("ortho", batch, rows, cols, dtype)
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    g = torch.randn((batch, rows, cols), generator=gen, device=DEV).to(dtype)
+    got = ortho(g).double()
+    want = _iterated(g.double(), torch.float64)
+    size = want.square().sum((-2, -1)).sqrt()
+    plain = ((_iterated(g.float(), torch.float32).double() - want).square().sum((-2, -1)).sqrt() / size)
+    off = (got - want).square().sum((-2, -1)).sqrt() / size
+    rounding = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+    assert torch.all(off <= 3 * plain + _dense.SLACK + rounding)
+
+
+def test_apply_of_layers_that_take_three_tables():
+    """More matrices above the small ones' size than two launches of the table
+    hold, with longer axes on both sides of 128 and small ones between."""
+    rng = np.random.default_rng(33)
+    layers, at = [], 0
+    for i in range(600):
+        r, c = int(rng.integers(65, 81)), int(rng.integers(66, 91))
+        if i % 7 == 3:
+            c = int(rng.integers(120, 140))
+        if i % 4 == 1:
+            r, c = c, r
+        if i % 5 == 2:
+            r, c = int(rng.integers(1, 20)), int(rng.integers(1, 40))
+        layers.append((at, r, c))
+        at += r * c + int(rng.integers(0, 3))
+    assert sum(min(r, c) > 64 for _, r, c in layers) > 2 * 192 + 64
+    d = at + 5
+    avg, x, m = _model(34, layers, d)
+    m[:] = 0.0
+    dx, dm = torch.from_numpy(x).to(DEV), torch.from_numpy(m).to(DEV)
+    ws = efs.new_muon_workspace([v[1:] for v in layers], DEV)
+    ws.fill_(0xFF)
+    efs.muon_apply(torch.from_numpy(avg).to(DEV), dx, dm, layers, ws, 0.9, 1.0, nesterov=False)
+    got, got_m = dx.cpu().numpy(), dm.cpu().numpy()
+    outside = np.ones(d, bool)
+    for o, r, c in layers:
+        s = slice(o, o + r * c)
+        outside[s] = False
+        u = avg[s].reshape(r, c)
+        want = x[s].reshape(r, c).astype(np.float64) - np.sqrt(max(1.0, r / c)) * _dense.newton_schulz(u)
+        assert _dense.relative(got[s].reshape(r, c), want) <= _dense.ortho_limit(u) + 2.0 ** -22, (o, r, c)
+        assert_bits_equal(got_m[s], avg[s], "m")
+    assert_bits_equal(got[outside], x[outside], "x outside the matrices")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("rows, cols", [(70, 90), (150, 66)])
+def test_special_values_stay_in_their_matrix_of_tiles(bad, rows, cols):
+    g = np.random.default_rng(14).standard_normal((4, rows, cols)).astype(np.float32)
+    clean = ortho(torch.from_numpy(g).to(DEV))
+    g[2, 5, 7] = bad
+    g[3] = 0.0
+    got = ortho(torch.from_numpy(g).to(DEV))
+    assert torch.equal(got[:2], clean[:2])
+    assert torch.all(torch.isnan(got[2]))
+    assert torch.all(got[3] == 0.0)
+    assert torch.all(torch.isnan(ortho(torch.zeros(rows, cols, device=DEV), eps=0.0)))
+
+
+@pytest.mark.parametrize("steps, coeffs", [(1, None), (2, None), (3, (2.0, -1.5, 0.5)), (10, (1.875, -1.25, 0.375))])
+@pytest.mark.parametrize("rows, cols", [(130, 80), (66, 300)])
+def test_steps_and_coefficients_of_tiles(steps, coeffs, rows, cols):
+    g = _dense.matrix(np.random.default_rng(9), "gauss", rows, cols)
+    kw = {"steps": steps, "coeffs": coeffs or _dense.COEFFS}
+    got = ortho(torch.from_numpy(g).to(DEV), steps=steps, coeffs=coeffs).cpu().numpy()
+    assert _dense.relative(got, _dense.newton_schulz(g, **kw)) <= _dense.ortho_limit(g, **kw)
+
+
+@pytest.mark.parametrize("rows, cols", [(70, 66), (90, 200)])
+def test_one_matrix_repeated_and_in_place_of_tiles(rows, cols):
+    g = torch.from_numpy(_dense.matrix(np.random.default_rng(12), "gauss", rows, cols)).to(DEV)
+    one = ortho(g)
+    three = ortho(g.expand(3, rows, cols))
+    for i in range(3):
+        assert torch.equal(three[i], one)
+    h = g.clone()
+    efs.muon_orthogonalize(h, h, efs.new_muon_workspace([(rows, cols)], DEV))
+    assert torch.equal(h, one)

@@ -376,3 +376,139 @@ def test_a_token_between_the_rows_of_a_gradient():
     assert torch.equal(both[7, 64:128], h[0]) and torch.all(both[10:, 64:] == 5.0)
     with pytest.raises(efs.EfsError, match="must not overlap"):
         efs.xent_backward(both[7:8, 63:127], w, target, want["lse"], dloss, both[9:10, 128:], both[:, :64], ws)
+
+
+# Above 128 tokens everything is laid out first, in both directions and types.
+PACKED = 150
+
+
+@pytest.mark.parametrize("scale", [1e-15, 1e-6, 1e6, 1e15])
+def test_tensors_of_any_magnitude_laid_out(scale):
+    """The split form is scaled to each tensor."""
+    h, w, target, dloss = inputs(PACKED, 400, 96, "fp32", scale=scale)
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, h, w, target, dloss, "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens", [40, PACKED])
+def test_tokens_and_weights_of_many_magnitudes(dtype, tokens):
+    """Within one call: rows of h from 2^-10 to 1, weights from 2^-10 to 1."""
+    h, w, target, dloss = inputs(tokens, 400, 96, dtype)
+    rng = np.random.default_rng(2)
+    h = (h.float() * torch.from_numpy(2.0 ** rng.integers(-10, 1, (tokens, 1))).float()).to(DTYPES[dtype])
+    dloss = dloss * torch.from_numpy(2.0 ** rng.integers(-10, 1, tokens)).float()
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, h, w, target, dloss, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -3.3e38])
+@pytest.mark.parametrize("hidden", [64, 70])
+def test_ignored_tokens_hold_anything_laid_out(dtype, bad, hidden):
+    h, w, target, dloss = inputs(PACKED, 500, hidden, dtype)
+    target[::3] = -100
+    clean = h.clone()
+    clean[::3] = 0.0
+    h[::3] = bad
+    dloss[::3] = bad
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, clean, w, target, torch.where(target == -100, torch.zeros(()), dloss), dtype)
+    for k in ("loss", "lse", "dh"):
+        assert torch.all(got[k][::3] == 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_every_token_ignored_laid_out(dtype):
+    h, w, target, dloss = (x.to(DEV) for x in inputs(PACKED, 300, 64, dtype))
+    got = call(torch.full_like(h, float("nan")), w, torch.full_like(target, -100), torch.full_like(dloss, float("inf")))
+    for k in ("loss", "lse", "dh", "dw"):
+        assert torch.all(got[k] == 0.0), k
+    assert not got["status"].any()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_targets_outside_the_vocabulary_are_reported_laid_out(dtype):
+    h, w, target, dloss = inputs(PACKED, 500, 64, dtype)
+    target[3], target[17], target[130] = 500, -1, 2 ** 40
+    dev = [x.to(DEV) for x in (h, w, target, dloss)]
+    got = call(*dev)
+    check(got, h, w, target, dloss, dtype)
+    assert int(got["status"].cpu().numpy().view("<u4")[0]) == efs.XENT_BAD_TARGET
+    ws = efs.new_xent_workspace(PACKED, 500, 64, h.dtype, DEV)
+    ws.fill_(0xFF)
+    efs.xent_backward(*dev[:3], got["lse"], dev[3], torch.empty_like(dev[0]), torch.empty_like(dev[1]), ws)
+    assert efs.xent_status(ws) == efs.XENT_BAD_TARGET
+    # another ignore_index: -100 is then bad as well, 500 is not
+    target[:] = 7
+    target[5] = 500
+    loss, lse = torch.empty(PACKED, device=DEV), torch.empty(PACKED, device=DEV)
+    efs.xent_forward(dev[0], dev[1], target.to(DEV), loss, lse, ws, ignore_index=500)
+    assert efs.xent_status(ws) == 0 and float(loss[5]) == 0.0 and float(loss[6]) > 0.0
+    efs.xent_forward(dev[0], dev[1], target.to(DEV), loss, lse, ws)
+    assert efs.xent_status(ws) == efs.XENT_BAD_TARGET
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_special_values_stay_with_their_token_laid_out(dtype):
+    h, w, target, dloss = (x.to(DEV) for x in inputs(PACKED, 500, 64, dtype, ignored=0.0))
+    want = call(h, w, target, dloss)
+    h[11, 5] = float("inf")
+    h[112, 6] = float("nan")
+    got = call(h, w, target, dloss)
+    rest = torch.ones(PACKED, dtype=torch.bool, device=DEV)
+    rest[11] = rest[112] = False
+    for k in ("loss", "lse", "dh"):
+        assert torch.equal(got[k][rest], want[k][rest]), k
+        assert torch.all(torch.isnan(got[k][112])), k
+        assert not torch.isfinite(got[k][11]).any(), k
+    assert torch.isnan(got["dw"]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_logits_far_apart_laid_out(dtype):
+    """Probabilities of exactly one and zero: maxima in the first and the last
+    tile, logits thousands apart."""
+    h, w, target, dloss = inputs(PACKED, 1000, 64, dtype, ignored=0.0)
+    w[0] *= 200.0
+    w[999] *= 300.0
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, h, w, target, dloss, dtype)
+
+
+def test_gradients_against_differences_laid_out():
+    """As above, with more tokens."""
+    h, w, target, dloss = inputs(PACKED, 200, 40, "fp32", ignored=0.1)
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    hn, wn, tn, dn = (x.numpy().astype(np.float64) if x.is_floating_point() else x.numpy() for x in (h, w, target, dloss))
+    rng = np.random.default_rng(1)
+    step = 1e-4
+
+    def total(a, b):
+        return float((_dense.xent(a, b, tn, dn)[0]["loss"] * dn).sum())
+    for _ in range(5):
+        dh, dw = rng.standard_normal(hn.shape), rng.standard_normal(wn.shape)
+        slope = (total(hn + step * dh, wn + step * dw) - total(hn - step * dh, wn - step * dw)) / (2 * step)
+        mine = float((got["dh"].double().cpu().numpy() * dh).sum() + (got["dw"].double().cpu().numpy() * dw).sum())
+        size = np.linalg.norm(got["dh"].cpu().numpy()) * np.linalg.norm(dh) + \
+            np.linalg.norm(got["dw"].cpu().numpy()) * np.linalg.norm(dw)
+        assert abs(mine - slope) <= 1e-5 * size
+
+
+# By the rule for tiles on 256 compute units: dh of 256 x 256; the logits and g of
+# 256 x 256, dh of 128 x 128; dw of 256 x 256; dw of 128 x 128; the logits and g of
+# 128 x 128; dh of 128 x 128.
+@pytest.mark.parametrize("tokens, vocab, hidden", [(3999, 301, 4001), (4001, 3990, 70), (150, 4001, 3999),
+                                                   (150, 2800, 2900), (2040, 2040, 130), (1500, 260, 2000)])
+@pytest.mark.parametrize("gap", [0.0, 30.0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_every_product_with_every_tile(dtype, gap, tokens, vocab, hidden):
+    say("xent", tokens, vocab, hidden, dtype, gap)
+    h, w, target, dloss = inputs(tokens, vocab, hidden, dtype, seed=5)
+    if gap:   # the targets' logits above the others'; |w|^2 is about 4
+        counts = target >= 0
+        h = h.float()
+        h[counts] += w[target[counts]].float() * (gap / 4.0)
+        h = h.to(DTYPES[dtype])
+    got = call(*(x.to(DEV) for x in (h, w, target, dloss)))
+    check(got, h, w, target, dloss, dtype)
