@@ -314,8 +314,12 @@ enum { EFS_FP32 = 0, EFS_BF16 = 1 };
  * muon_apply).  With X = G / (||G||_F + eps), transposed where it has more
  * rows than columns, `steps` times
  *     A = X X^T ;  B = b A + c A A ;  X = a X + B X
- * and the last X, transposed back.  Everything between reading g and writing
- * out is held to binary32's precision or better, whatever the type.
+ * and the last X, transposed back.  The norm is summed in binary64.  Whatever the
+ * type, matrices of up to 64 rows or columns whose X fits one workgroup's LDS are
+ * iterated in binary32.  Others keep 22 bits of every entry of X, A and B, of
+ * small entries to 2^-39 (no singular value of X is above 1.99): where eps
+ * outweighs the norm so far that the entries of G / (||G||_F + eps) are below
+ * 2^-38 they vanish.
  *
  *   g          batch matrices of rows x cols; element (i, r, c) is
  *              g[i * stride_g + r * ld_g + c] (in elements; ld_g >= cols).  Read
@@ -337,7 +341,9 @@ enum { EFS_FP32 = 0, EFS_BF16 = 1 };
  *              beyond it they become infinite.
  *   eps        added to the norm (finite, >= 0): a matrix of zeros gives zeros
  *              (with eps = 0 NaN, as 0 / 0).
- *   workspace  >= muon_workspace_bytes for these matrices, 16-byte aligned;
+ *   workspace  >= muon_workspace_bytes for these matrices (16 to 24 bytes an
+ *              element, more where an axis is short, since both are padded to 32
+ *              values: 1 x 100,000 takes 285), 16-byte aligned;
  *              contents need no initialisation and are not kept.  Must not
  *              overlap the matrices.  Not shareable between concurrent calls.
  * A matrix that holds NaN or infinities gives NaN; the others of the batch
@@ -391,10 +397,12 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              ignore_index does not count: its loss and lse are 0, and its row
  *              of h may hold anything.  So does, with EFS_XENT_BAD_TARGET in the
  *              status word, one whose target is neither that nor in [0, vocab).
- *   dtype      EFS_FP32 or EFS_BF16, of h and w.  fp32 products are held to
- *              fp32's precision, relative to each tensor's largest finite
- *              magnitude (elements below 2^-38 of that lose bits); bf16
- *              products are summed in fp32.
+ *   dtype      EFS_FP32 or EFS_BF16, of h and w.  fp32: up to 64 tokens
+ *              (xent_forward: 128) products of fp32.  With more, 22 bits of every
+ *              element count, of those below 2^-17 of the tensor's largest finite
+ *              magnitude to 2^-39 of that.  bf16: the logits are exact products;
+ *              above 64 tokens the gradients take w and dloss h in 11 bits, of
+ *              small elements to 2^-39 of the largest.  All sums are fp32.
  *   tokens     0..EFS_XENT_MAX_TOKENS (0: nothing to do but to clear the status
  *              word, where a workspace is given); vocab
  *              1..EFS_XENT_MAX_VOCAB; hidden 1..EFS_XENT_MAX_HIDDEN; tokens x
@@ -407,7 +415,8 @@ efs_status muon_apply(const float *avg, float *x, float *m, int64_t d, int32_t n
  *              are.  With more, the bytes hold a copy of both, which bf16 rows
  *              that are multiples of 64 long and 16-byte aligned do without.
  *              Not shareable between concurrent calls.
- * A row of h that holds NaN or infinities gives NaN, for its token alone. */
+ * A row of h that holds NaN or infinities gives NaN or infinities for its token
+ * alone (and NaN in all of dw); w has to be finite. */
 #define EFS_XENT_MAX_TOKENS (1 << 22)
 #define EFS_XENT_MAX_VOCAB (1 << 24)
 #define EFS_XENT_MAX_HIDDEN (1 << 18)
@@ -440,8 +449,7 @@ efs_status xent_forward(const void *h, int64_t ld_h, const void *w, int64_t ld_w
  *              ld_dw elements apart, overwritten (dh is 0 where a token does
  *              not count; dw is 0 with no tokens).  They and the workspace must
  *              not overlap each other or an input (other columns of the same rows
- *              are no overlap).
- *              Sums are fp32; bf16: each result is rounded once more.
+ *              are no overlap).  bf16: each result is rounded once more.
  *   workspace  >= xent_workspace_bytes(.., 1). */
 efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_w,
                          const int64_t *target, int dtype, int32_t tokens, int32_t vocab,

@@ -22,8 +22,9 @@
 // memory straight to LDS (16 bytes a lane, no registers), into one of two
 // buffers while the other one is multiplied (kStages buffers, where a tile is so
 // narrow that one step in flight does not cover memory's latency).  In LDS a row's eight 16-byte
-// units are permuted by the row's low bits, so that the eight rows that a
-// quarter wave reads at once lie in different banks.  A step's reads from LDS
+// units are permuted by the row's low bits, so that eight neighbouring rows
+// lie in different banks; rows eight apart share theirs, and half of the cycles
+// that LDS is busy count as conflicts.  A step's reads from LDS
 // are spread between the products by scheduling groups.  Measured, 8192 x 8192
 // x 4096, 256 x 256 tile: kSplit 441 TFLOP/s (1322 of fp16 products), kBf16
 // 1124; without the groups 396 and 1056.  With 128 x 128 tiles 380 and 948,

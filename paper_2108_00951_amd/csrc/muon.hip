@@ -698,7 +698,9 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void muon_gram
 // instructions (16 x 16 x 4).  Rows are padded with zeros to 16 values and lie
 // 4 values further apart, so that the 16 rows x 4 values that an instruction
 // takes are in 64 different banks.  Bound by that one workgroup's instructions and
-// round trips through LDS: 64 x 64 in 28.6 us, by tiles 90 and more.
+// round trips through LDS.  us, against tiles: 64 x 64 30 and 62, 256 of them 33 and
+// 88; 2,048 of 32 x 32 68 and 201; 256 of 64 x 300 96 and 183; but one of 64 x 300 90
+// and 80, of 64 x 450 129 and 86, of 16 x 2000 148 and 99.
 constexpr int kLdsBlock = 512;
 constexpr int kLdsWaves = kLdsBlock / kWave;
 constexpr int kLdsMaxM = 64;

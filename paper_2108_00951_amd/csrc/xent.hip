@@ -334,8 +334,8 @@ __device__ __forceinline__ float logit(float acc, int exponent) {
 // Forward: parts[tile row][token], and the targets' logits.  kRows: from h and w
 // as they are, whatever their alignment, and not from operands.
 // Bound by the matrix cores for many tokens (2,048 x 131,072 x 4,096, bf16: 1.95
-// ms, 1130 TFLOP/s; 4,096 x 131,072 x 4,096, fp32: 10.4 ms, 423), by reading w for
-// few (a token x 33,278 x 1,024, bf16: 14.5 us, 4.7 TB/s).
+// ms, 1130 TFLOP/s; 4,096 x 131,072 x 4,096, fp32: 10.5 ms, 418), by reading w for
+// few (a token x 33,278 x 1,024, bf16: 14.9 us, 4.6 TB/s).
 template <Prec P, class Tile, bool kRows>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_forward_kernel(Xent x, Operand w, Operand h,
                                                                          const Control *__restrict__ control, Part *parts,
@@ -442,8 +442,8 @@ __device__ __forceinline__ int word_shift(uint32_t top) {
 // Backward: g of words [v0, v0 + words), as g [token][word] and gt [word][token],
 // and the words' shifts in this tile's tokens, shift [word][tile].
 // Both are written from the tile, turned in LDS, so that no pass turns g; bound
-// by the matrix cores (a piece of 8,192 words for 4,096 tokens of 4,096: 670 us in
-// fp32, 410 TFLOP/s; of 16,384 in bf16 526 us, 1045).
+// by the matrix cores (a piece of 8,192 words for 4,096 tokens of 4,096: 679 us in
+// fp32, 405 TFLOP/s; of 16,384 in bf16 534 us, 1030).
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad_kernel(Xent x, Operand w, Operand h, int32_t v0,
                                                                       int32_t words, const float *lse,
@@ -525,6 +525,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_grad
 
 // Brings all tiles of a word in gt to the smallest of their shifts, row_shift [word].
 // A wave takes a word; values whose tile has that shift already are not touched.
+// Bound by the way to memory and back (11 and 16 us for those pieces, of which 2 to
+// 4 MB are rewritten).
 template <Prec G>
 __global__ __launch_bounds__(kPackBlock) void xent_align_kernel(char *gt, int64_t gt_row, int32_t words,
                                                                 int32_t tokens_end, int32_t width, int32_t tiles,
@@ -560,7 +562,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_align_kernel(char *gt, int64_
 }
 
 // dw rows [v0, v0 + words) = g^T h.  Bound by the matrix cores (the same pieces:
-// 621 and 487 us, 442 and 1130 TFLOP/s).
+// 635 and 492 us, 433 and 1118 TFLOP/s).
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dw_kernel(Xent x, Operand gt, Operand ht, int32_t v0,
                                                                     const Control *__restrict__ control,
@@ -600,8 +602,8 @@ __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dw_k
 }
 
 // Partial sums of dh: split s adds its share of the piece's words to
-// part[s][token][hidden] (or starts it, with the first piece).  As dw (673 and 502
-// us, 408 and 1095 TFLOP/s).
+// part[s][token][hidden] (or starts it, with the first piece).  As dw (680 and 502
+// us, 404 and 1095 TFLOP/s).
 template <Prec P, class Tile>
 __global__ __launch_bounds__(Tile::kThreads, Tile::kWavesPerSimd) void xent_dh_kernel(Xent x, Operand g, Operand wt, int32_t steps,
                                                                     int32_t splits, bool first, float *part) {
@@ -655,10 +657,12 @@ __global__ __launch_bounds__(kPackBlock) void xent_dh_join_kernel(Xent x, const 
 // the vector units (kTok operations an element).  kGrad: g as
 // xent_few_grad_kernel leaves it; else parts and target logits as
 // xent_forward_kernel does.  A workgroup covers 64 words, a wave 16 of them, in
-// one group or (more tokens: registers) two.  fp32, 56,852 x 2,758 words: 146 us
-// for three tokens, 289 through the matrix cores; for eight, 256 against 205.
-// bf16 rows in whole steps are faster through the matrix cores at any count (one
-// token x 33,278 x 1,024: 15 against 18 us).
+// one group or (more tokens: registers) two.  A call of 56,852 words x 2,758 (in
+// brackets 2,752, whole steps), us, against the matrix cores: fp32, three tokens
+// 126 and 268 (145, 155); eight, by a variant of this, 232 and 278 (240, 155); bf16,
+// three tokens 76 and 110, eight 94 and 119.  bf16 rows in whole steps are as fast
+// or faster through the matrix cores at any count (three tokens 61 either way, one
+// token x 33,278 x 1,024 15 against 18).
 constexpr int kDotTokens = 4, kDotWords = 64;
 template <Prec P>
 bool take_dot(int32_t tokens, bool in_steps) {
@@ -784,7 +788,7 @@ __global__ __launch_bounds__(kPackBlock) void xent_dot_kernel(Xent x, Part *__re
 // thread; the logits' sums meet in LDS, and the same registers serve
 // dh += g w and dw = g h.  h and this workgroup's share of dh stay in registers
 // throughout.  Bound by reading w and writing dw (three tokens x 56,852 x 2,758:
-// forward and this take 403 us, 4.7 TB/s over both).
+// 239 us, 5.2 TB/s; with the forward call 405).
 constexpr int kOnceWords = 4;
 
 template <int kTok, int kSlots>
@@ -1196,7 +1200,13 @@ __global__ __launch_bounds__(kPackBlock) void xent_zero_kernel(T *dw, int64_t ld
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
 int64_t tiles(int64_t len, int tile) { return (len + tile - 1) / tile; }
 
-// Few tokens: reading w takes longer than multiplying it.
+// Few tokens: reading w takes longer than multiplying it.  65,536 words x 2,048, us,
+// where they are against laid out first: a step of fp32 with 16 tokens 499 and 1283,
+// with 64 864 and 1306; of bf16 225 and 526, 344 and 532.  (dh of more than 64 does
+// not fit xent_few_products_kernel's registers.)  Forward of fp32 with 64: 221 and
+// 449; with 65, 96 and 128 the two are near each other (491 and 453, 517 and 449, 489
+// and 448), and a call of loss alone does without a copy of the head.  Forward of
+// bf16 with 64: 53 and 77; with 65 and 128, 58 and 66, 64 and 69.
 constexpr int32_t kFewTokens = 64;
 template <Prec P>
 constexpr int32_t kFewForward = P == Prec::kFp32 ? 128 : 64;
