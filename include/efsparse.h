@@ -457,6 +457,166 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
                          const float *dloss, void *dh, int64_t ld_dh, void *dw, int64_t ld_dw,
                          void *workspace, size_t workspace_bytes, void *stream);
 
+/* Words' vectors: out[t] = scale * table[ids[t]], the start of a language model.
+ *
+ *   table      vocab x width, row v at table + v * ld_table elements, read only.
+ *   ids        DEVICE int64[tokens], 8-byte aligned.  A token whose id is
+ *              ignore_index does not count: its row of out is 0.  So is, with
+ *              EFS_EMBED_BAD_ID in the status word, that of an id which is
+ *              neither ignore_index nor in [0, vocab).
+ *   out        tokens x width, rows ld_out elements apart, overwritten; must not
+ *              overlap table, ids or status.
+ *   dtype, table_dtype   EFS_FP32 or EFS_BF16, of out and of table.
+ *   tokens     0..EFS_EMBED_MAX_TOKENS; vocab 1..EFS_EMBED_MAX_VOCAB; width
+ *              1..EFS_EMBED_MAX_WIDTH.
+ *   scale      finite; the product is one fp32 operation, rounded once more for
+ *              bf16.
+ *   status     DEVICE uint32, 4-byte aligned, zero-filled by the caller before its
+ *              first use, or NULL: calls that meet a bad id set bits in it, and
+ *              no call clears it. */
+#define EFS_EMBED_MAX_TOKENS (1 << 22)
+#define EFS_EMBED_MAX_VOCAB (1 << 24)
+#define EFS_EMBED_MAX_WIDTH (1 << 18)
+#define EFS_EMBED_BAD_ID 1u
+efs_status embed_forward(const void *table, int64_t ld_table, int table_dtype, const int64_t *ids, void *out,
+                         int64_t ld_out, int dtype, int32_t tokens, int32_t vocab, int32_t width, float scale,
+                         int64_t ignore_index, uint32_t *status, void *stream);
+
+/* Gradient of the table:
+ *     dtable[v] = scale * sum over the tokens t with ids[t] = v of dout[t]
+ * and 0 for words without a token that counts.  The sums are fp32, always in
+ * the same order: a call on the same inputs gives the same bits.
+ *
+ *   dout       tokens x width of dtype, rows ld_dout elements apart, read only.
+ *              Rows of tokens that do not count are not read.
+ *   dtable     vocab x width of table_dtype, rows ld_dtable elements apart: a
+ *              layer of the flat gradient vector, say.
+ *   accumulate 0: every row is overwritten.  1: the rows of words with a token
+ *              have their sum added (one fp32 addition, rounded once more for
+ *              bf16), others keep what they hold: an output head that shares its
+ *              weights, after xent_backward.
+ *   ids, status, scale, ignore_index, limits   as for embed_forward; tokens x
+ *              vocab at most 2^38.
+ *   workspace  >= embed_workspace_bytes(tokens, vocab, width) bytes, 16-byte
+ *              aligned; contents need no initialisation and are not kept.  Not
+ *              shareable between concurrent calls.
+ * dtable, status and the workspace must not overlap each other or an input
+ * (other columns of the same rows are no overlap). */
+/* Bytes; 0 if the arguments are out of range. */
+size_t embed_workspace_bytes(int32_t tokens, int32_t vocab, int32_t width);
+efs_status embed_backward(const void *dout, int64_t ld_dout, int dtype, const int64_t *ids, void *dtable,
+                          int64_t ld_dtable, int table_dtype, int32_t tokens, int32_t vocab, int32_t width,
+                          float scale, int64_t ignore_index, int accumulate, uint32_t *status, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Layer norm of every row of x:
+ *     mean = sum(x) / width ;  rstd = 1 / sqrt(sum((x - mean)^2) / width + eps)
+ *     y = (x - mean) * rstd * weight + bias
+ * in fp32; bf16 results are rounded once.
+ *
+ *   x, y       rows x width of dtype, rows ld_x and ld_y elements apart.  y may be
+ *              x itself (the same pointer and ld); it must not overlap x in any
+ *              other way (other columns of the same rows are no overlap), nor
+ *              anything else.
+ *   weight, bias   [width] of weight_dtype, aligned to it; NULL: 1 and 0.
+ *   dtype, weight_dtype   EFS_FP32 or EFS_BF16.
+ *   rows       0..INT32_MAX; width 1..EFS_NORM_MAX_WIDTH.
+ *   eps        finite, >= 0 (a constant row gives bias; with eps = 0 NaN).
+ *   mean, rstd fp32[rows], overwritten, for the gradients; each may be NULL.
+ * A row that holds NaN or infinities, or whose sum or sum of squares passes
+ * fp32's range, gives NaN or zeros; the others are not affected. */
+#define EFS_NORM_MAX_WIDTH (1 << 18)
+efs_status layernorm_forward(const void *x, int64_t ld_x, const void *weight, const void *bias, void *y,
+                             int64_t ld_y, int dtype, int weight_dtype, int32_t rows, int32_t width, float eps,
+                             float *mean, float *rstd, void *stream);
+
+/* Its gradients, with g = dy * weight and h = (x - mean) * rstd:
+ *     dx = rstd * (g - sum(g) / width - h * sum(g * h) / width)     (of its row)
+ *     dweight = sum over the rows of dy * h ;  dbias = sum over the rows of dy
+ * Sums are fp32, always in the same order.
+ *
+ *   x, weight, dtype, weight_dtype, rows, width   as for layernorm_forward.
+ *   mean, rstd fp32[rows] as layernorm_forward left them.
+ *   dy         rows x width of dtype, rows ld_dy elements apart.
+ *   dx         the same with ld_dx, overwritten.  May be dy or x itself (the
+ *              same pointer and ld).
+ *   dweight, dbias   [width] of weight_dtype, overwritten (0 with no rows); each may
+ *              be NULL.
+ *   workspace  >= layernorm_workspace_bytes(rows, width) bytes, 16-byte aligned;
+ *              contents need no initialisation and are not kept.  Not shareable
+ *              between concurrent calls.
+ * What is written must not overlap anything else. */
+/* Bytes; 0 if the arguments are out of range. */
+size_t layernorm_workspace_bytes(int32_t rows, int32_t width);
+efs_status layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean, const float *rstd,
+                              const void *dy, int64_t ld_dy, void *dx, int64_t ld_dx, int dtype, int weight_dtype,
+                              int32_t rows, int32_t width, void *dweight, void *dbias, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* AdamW over many tensors at once: the update of the parameters that muon_apply
+ * leaves as they are (norms, biases, embeddings, output heads), from the averaged
+ * gradient.  With t the number of the step, from 1 on,
+ *     m = beta1 * m + (1 - beta1) * g
+ *     v = beta2 * v + ((1 - beta2) * g) * g
+ *     x = (1 - gamma * decay) * x - alpha * (m / (root * sqrt(v) + eps))
+ *     alpha = gamma / (1 - beta1^t) ;  root = 1 / sqrt(1 - beta2^t)
+ * each a separately rounded fp32 operation in the order written; 1 - beta1, 1 -
+ * beta2, 1 - gamma * decay, alpha and root are computed in binary64 and rounded.
+ *
+ *   g, x, m, v, sizes   HOST arrays of `count` device pointers (and lengths, 0 to
+ *              INT32_MAX elements): tensors of their own or layers of flat vectors.
+ *              g: of grad_dtype, read only; x: fp32, in place; m, v: in place, of
+ *              state.  Aligned to their type; states of 8 bits to 16 bytes.
+ *   copies     HOST array of device pointers to bf16 that receive the new x
+ *              rounded, or NULL (in which entries may be NULL).
+ *   decays     HOST float[count] (finite), or NULL for 0.
+ *   count      0..EFS_ADAMW_MAX_TENSORS, of which those of length 0 are skipped
+ *              (their pointers are not looked at).
+ *   state      EFS_STATE_32: m[i] and v[i] are fp32[sizes[i]], zero before the
+ *              first step.  EFS_STATE_8: adamw_state_bytes(sizes[i]) bytes each,
+ *              zero-filled before the first step; see below.
+ *   gamma, beta1, beta2, eps   finite; 0 <= beta < 1, eps >= 0 (with eps = 0 an
+ *              element that never had a gradient becomes NaN, as 0 / 0).
+ *   step       t >= 1, where step_device is NULL.
+ *   step_device   DEVICE int64, 8-byte aligned, with t in it (below 1: as 1), or
+ *              NULL: for calls in a captured graph, which the caller advances
+ *              between them.
+ *   factors    DEVICE float[2], 4-byte aligned, or NULL for 1, 1: gamma is
+ *              multiplied by the first (a schedule), every element of g by the
+ *              second (one over a loss scale, a clipped norm's factor).
+ *   seed       of the random rounding of states of 8 bits.
+ * A tensor that is written, its states among them, must not overlap any other.
+ * NaN or infinities in g spoil their own elements alone.
+ *
+ * States of 8 bits.  256 consecutive elements share a power of two s for m and one
+ * for r = sqrt(v): the largest finite magnitude lies in [2^7, 2^8) * s (s is
+ * 2^-102 where it is below 2^-95).  m is kept as a sign and a value of 3 bits
+ * below its leading one, from 2^-6 s on (smaller: in steps of 2^-9 s); r as one
+ * of 4 bits (steps of 2^-10 s), of which no r > 0 becomes 0.  A value between two
+ * others is rounded up with the share of its distance from the lower one, by a
+ * hash of (seed, the tensor's place in the list, t, element): the same call
+ * gives the same bits.  A magnitude that is infinite or NaN is kept as NaN.  x is
+ * computed from m and v before they are rounded.  The state of n elements is
+ * ceil(n / 256) * 256 bytes (a byte an element, zeros behind the last), then a
+ * float s for each 256. */
+#define EFS_ADAMW_MAX_TENSORS 65536
+enum { EFS_STATE_32 = 0, EFS_STATE_8 = 1 };
+/* Bytes of m (or of v) of `size` elements in 8 bits; 0 if size is out of range. */
+size_t adamw_state_bytes(int64_t size);
+efs_status adamw_apply(const void *const *g, int grad_dtype, float *const *x, void *const *copies, void *const *m,
+                       void *const *v, int state, const int64_t *sizes, const float *decays, int32_t count,
+                       float gamma, float beta1, float beta2, float eps, int64_t step, const int64_t *step_device,
+                       const float *factors, uint32_t seed, void *stream);
+
+/* States of 8 bits as values and back, for checkpoints: adamw_read_state writes
+ * the m and v that m8 and v8 stand for; adamw_write_state is its inverse, rounding
+ * to nearest (ties up).  HOST arrays of device pointers as for adamw_apply; m and
+ * v fp32.  What is written must not overlap anything else. */
+efs_status adamw_read_state(void *const *m8, void *const *v8, float *const *m, float *const *v, const int64_t *sizes,
+                            int32_t count, void *stream);
+efs_status adamw_write_state(float *const *m, float *const *v, void *const *m8, void *const *v8, const int64_t *sizes,
+                             int32_t count, void *stream);
+
 /* Streaming copy dst[0..n) = src[0..n) with the same 16-byte access pattern
  * and grid as the hard-threshold kernel: the reference transfer for
  * measurements, not part of the method.  src and dst 16-byte aligned,

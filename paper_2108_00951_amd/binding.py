@@ -109,6 +109,30 @@ def declare(lib):
     lib.xent_backward.argtypes = [vp, i64, vp, i64, vp, ctypes.c_int, i32, i32, i32, i64, vp, vp, vp, i64,
                                   vp, i64, vp, ctypes.c_size_t, vp]
     lib.xent_backward.restype = ctypes.c_int
+    lib.embed_forward.argtypes = [vp, i64, ctypes.c_int, vp, vp, i64, ctypes.c_int, i32, i32, i32, f32, i64, vp, vp]
+    lib.embed_forward.restype = ctypes.c_int
+    lib.embed_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.embed_workspace_bytes.restype = ctypes.c_size_t
+    lib.embed_backward.argtypes = [vp, i64, ctypes.c_int, vp, vp, i64, ctypes.c_int, i32, i32, i32, f32, i64,
+                                   ctypes.c_int, vp, vp, ctypes.c_size_t, vp]
+    lib.embed_backward.restype = ctypes.c_int
+    lib.layernorm_forward.argtypes = [vp, i64, vp, vp, vp, i64, ctypes.c_int, ctypes.c_int, i32, i32, f32, vp, vp, vp]
+    lib.layernorm_forward.restype = ctypes.c_int
+    lib.layernorm_workspace_bytes.argtypes = [i32, i32]
+    lib.layernorm_workspace_bytes.restype = ctypes.c_size_t
+    lib.layernorm_backward.argtypes = [vp, i64, vp, vp, vp, vp, i64, vp, i64, ctypes.c_int, ctypes.c_int, i32, i32,
+                                       vp, vp, vp, ctypes.c_size_t, vp]
+    lib.layernorm_backward.restype = ctypes.c_int
+    vps, i64s = ctypes.POINTER(vp), ctypes.POINTER(i64)
+    lib.adamw_state_bytes.argtypes = [i64]
+    lib.adamw_state_bytes.restype = ctypes.c_size_t
+    lib.adamw_apply.argtypes = [vps, ctypes.c_int, vps, vps, vps, vps, ctypes.c_int, i64s, ctypes.POINTER(f32), i32, f32,
+                                f32, f32, f32, i64, vp, vp, ctypes.c_uint32, vp]
+    lib.adamw_apply.restype = ctypes.c_int
+    lib.adamw_read_state.argtypes = [vps, vps, vps, vps, i64s, i32, vp]
+    lib.adamw_read_state.restype = ctypes.c_int
+    lib.adamw_write_state.argtypes = [vps, vps, vps, vps, i64s, i32, vp]
+    lib.adamw_write_state.restype = ctypes.c_int
     lib.efs_copy_probe.argtypes = [vp, vp, i64, vp]
     lib.efs_copy_probe.restype = ctypes.c_int
     lib.efs_stream_probe.argtypes = [vp, vp, i64, ctypes.c_int, vp]
@@ -651,6 +675,336 @@ def xent_backward(h, w, target, lse, dloss, dh, dw, workspace, ignore_index: int
     _check(lib, lib.xent_backward(*args, int(ignore_index), _ptr(lse), _ptr(dloss), _ptr(dh),
                                   _row_stride(dh), _ptr(dw), _row_stride(dw), _ptr(workspace),
                                   workspace.numel(), _stream_handle(stream)))
+
+
+def _on_current_device(**tensors) -> None:
+    """The call's stream is one of the current device: the tensors must be too."""
+    import torch
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.device.index != here:
+            raise ValueError("%s is on %s, and the current device is cuda:%d" % (name, t.device, here))
+
+
+def _require_status(status):
+    import torch
+    if status is not None:
+        _require(status, torch.int32, "status")
+        if status.numel() < 1:
+            raise ValueError("status must have an element")
+
+
+EMBED_BAD_ID = 1
+
+
+def new_embed_status(device="cuda"):
+    """A zero-filled status word for embed_forward and embed_backward."""
+    import torch
+    return torch.zeros(1, dtype=torch.int32, device=device)
+
+
+def embed_status(status) -> int:
+    """EFS_EMBED_* bits that calls have set since the word was filled with zeros (synchronises)."""
+    return int(status[0].item()) & 0xFFFFFFFF
+
+
+def embed_forward(table, ids, out, scale: float = 1.0, ignore_index: int = -100, status=None, stream=None) -> None:
+    """out [tokens, width] = scale * table [vocab, width] at ids [tokens], each fp32
+    or bf16; see embed_forward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    if table.dim() != 2 or ids.dim() != 1 or out.shape != (ids.shape[0], table.shape[1]):
+        raise ValueError("table must be [vocab, width], ids [tokens] and out [tokens, width]")
+    table_dtype, dtype = _dtype_code(table, "table"), _dtype_code(out, "out")
+    _require_rows(table, "table")
+    _require(ids, torch.int64, "ids")
+    _require_rows(out, "out")
+    _require_status(status)
+    _on_current_device(table=table, ids=ids, out=out, status=status)
+    _check(lib, lib.embed_forward(_ptr(table), _row_stride(table), table_dtype, _ptr(ids), _ptr(out), _row_stride(out),
+                                  dtype, _int32(ids.shape[0], "tokens"), _int32(table.shape[0], "vocab"),
+                                  _int32(table.shape[1], "width"), float(scale), int(ignore_index),
+                                  None if status is None else status.data_ptr(), _stream_handle(stream)))
+
+
+def embed_workspace_bytes(tokens: int, vocab: int, width: int) -> int:
+    return int(load_library().embed_workspace_bytes(_int32(tokens, "tokens"), _int32(vocab, "vocab"),
+                                                    _int32(width, "width")))
+
+
+def new_embed_workspace(tokens: int, vocab: int, width: int, device="cuda"):
+    """A workspace for embed_backward, of any types."""
+    import torch
+    nbytes = embed_workspace_bytes(tokens, vocab, width)
+    if nbytes == 0:
+        raise ValueError("%d tokens, %d words or %d values a row are out of range" % (tokens, vocab, width))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def embed_backward(dout, ids, dtable, workspace, scale: float = 1.0, ignore_index: int = -100,
+                   accumulate: bool = False, status=None, stream=None) -> None:
+    """The table's gradient dtable [vocab, width] from dout [tokens, width] at ids
+    [tokens], written whole or added to; see embed_backward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    if dtable.dim() != 2 or ids.dim() != 1 or dout.shape != (ids.shape[0], dtable.shape[1]):
+        raise ValueError("dtable must be [vocab, width], ids [tokens] and dout [tokens, width]")
+    table_dtype, dtype = _dtype_code(dtable, "dtable"), _dtype_code(dout, "dout")
+    _require_rows(dout, "dout")
+    _require(ids, torch.int64, "ids")
+    _require_rows(dtable, "dtable")
+    _require(workspace, torch.uint8, "workspace")
+    _require_status(status)
+    _on_current_device(dout=dout, ids=ids, dtable=dtable, workspace=workspace, status=status)
+    _check(lib, lib.embed_backward(_ptr(dout), _row_stride(dout), dtype, _ptr(ids), _ptr(dtable), _row_stride(dtable),
+                                   table_dtype, _int32(ids.shape[0], "tokens"), _int32(dtable.shape[0], "vocab"),
+                                   _int32(dtable.shape[1], "width"), float(scale), int(ignore_index),
+                                   int(bool(accumulate)), None if status is None else status.data_ptr(),
+                                   _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+
+
+def _weight_args(width, **weights):
+    """The code of the dtype that the given weights share (of None: fp32)."""
+    code = None
+    for name, t in weights.items():
+        if t is None:
+            continue
+        if t.shape != (width,):
+            raise ValueError("%s must be [width]" % name)
+        one = _dtype_code(t, name)
+        if code is not None and one != code:
+            raise TypeError("%s must have one dtype" % " and ".join(weights))
+        if t.device.type != "cuda" or not t.is_contiguous():
+            raise TypeError("%s must be a contiguous device tensor" % name)
+        code = one
+    return FP32 if code is None else code
+
+
+def _norm_sizes(x):
+    return _int32(x.shape[0], "rows"), _int32(x.shape[1], "width")
+
+
+def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
+    """Layer norm of the rows of x [rows, width] into y, fp32 or bf16; weight and
+    bias [width] of their own dtype, or None; mean and rstd fp32 [rows] for the
+    gradients, or None; see layernorm_forward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    if x.dim() != 2 or y.shape != x.shape:
+        raise ValueError("x and y must be [rows, width]")
+    if x.dtype != y.dtype:
+        raise TypeError("x and y must have one dtype")
+    dtype = _dtype_code(x, "x")
+    _require_rows(x, "x")
+    _require_rows(y, "y")
+    rows, width = _norm_sizes(x)
+    weight_dtype = _weight_args(width, weight=weight, bias=bias)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _require(t, torch.float32, name)
+            if t.shape != x.shape[:1]:
+                raise ValueError("%s must be [rows]" % name)
+    _on_current_device(x=x, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd)
+    _check(lib, lib.layernorm_forward(_ptr(x), _row_stride(x), _ptr(weight), _ptr(bias), _ptr(y), _row_stride(y), dtype,
+                                      weight_dtype, rows, width, float(eps), _ptr(mean), _ptr(rstd),
+                                      _stream_handle(stream)))
+
+
+def layernorm_workspace_bytes(rows: int, width: int) -> int:
+    return int(load_library().layernorm_workspace_bytes(_int32(rows, "rows"), _int32(width, "width")))
+
+
+def new_layernorm_workspace(rows: int, width: int, device="cuda"):
+    """A workspace for layernorm_backward, of any types."""
+    import torch
+    nbytes = layernorm_workspace_bytes(rows, width)
+    if nbytes == 0:
+        raise ValueError("%d rows of %d values are out of range" % (rows, width))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def layernorm_backward(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, stream=None) -> None:
+    """Gradients of layernorm_forward: dx [rows, width], dweight and dbias [width]
+    (or None); see layernorm_backward in include/efsparse.h."""
+    import torch
+    lib = load_library()
+    if x.dim() != 2 or dy.shape != x.shape or dx.shape != x.shape:
+        raise ValueError("x, dy and dx must be [rows, width]")
+    if x.dtype != dy.dtype or x.dtype != dx.dtype:
+        raise TypeError("x, dy and dx must have one dtype")
+    dtype = _dtype_code(x, "x")
+    _require_rows(x, "x")
+    _require_rows(dy, "dy")
+    _require_rows(dx, "dx")
+    rows, width = _norm_sizes(x)
+    weight_dtype = _weight_args(width, weight=weight, dweight=dweight, dbias=dbias)
+    _require(mean, torch.float32, "mean")
+    _require(rstd, torch.float32, "rstd")
+    _require(workspace, torch.uint8, "workspace")
+    if mean.shape != x.shape[:1] or rstd.shape != x.shape[:1]:
+        raise ValueError("mean and rstd must be [rows]")
+    _on_current_device(x=x, weight=weight, mean=mean, rstd=rstd, dy=dy, dx=dx, dweight=dweight, dbias=dbias,
+                       workspace=workspace)
+    _check(lib, lib.layernorm_backward(_ptr(x), _row_stride(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dy),
+                                       _row_stride(dy), _ptr(dx), _row_stride(dx), dtype, weight_dtype, rows, width,
+                                       _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace.numel(),
+                                       _stream_handle(stream)))
+
+
+STATE_32, STATE_8 = 0, 1
+
+
+def adamw_state_bytes(size: int) -> int:
+    """Bytes of one moment of `size` elements in 8 bits."""
+    return int(load_library().adamw_state_bytes(int(size)))
+
+
+def new_adamw_state(sizes: Sequence[int], device="cuda"):
+    """The moments (m, v) of tensors of these sizes in 8 bits, before the first
+    step: two lists of uint8 tensors, each list in one allocation."""
+    import torch
+    spans = []
+    for n in sizes:
+        nbytes = adamw_state_bytes(n)
+        if nbytes == 0 and n != 0:
+            raise ValueError("a tensor of %d elements is out of range" % n)
+        spans.append(nbytes)
+
+    def one():
+        at, out = 0, []
+        flat = torch.zeros(sum(-(-b // 16) * 16 for b in spans), dtype=torch.uint8, device=device)
+        for nbytes in spans:
+            out.append(flat[at:at + nbytes])
+            at += -(-nbytes // 16) * 16
+        return out
+    return one(), one()
+
+
+def _tensor_list(tensors, name, dtypes, sizes, optional=False):
+    """A host array of the pointers of a list's tensors, of which each has its
+    size; optional: some may be None."""
+    import torch
+    if len(tensors) != len(sizes):
+        raise ValueError("%s must have as many tensors as the other lists" % name)
+    arr = (ctypes.c_void_p * max(len(tensors), 1))()
+    here = torch.cuda.current_device() if tensors else 0
+    kind = None
+    for i, t in enumerate(tensors):
+        if t is None:
+            if not optional:
+                raise TypeError("%s[%d] is None" % (name, i))
+            continue
+        if t.dtype not in dtypes or (kind is not None and t.dtype != kind):
+            raise TypeError("%s must be %s, all alike; %s[%d] is %s"
+                            % (name, " or ".join(str(d) for d in dtypes), name, i, t.dtype))
+        kind = t.dtype
+        if not t.is_cuda or not t.is_contiguous():
+            raise TypeError("%s[%d] must be a contiguous device tensor" % (name, i))
+        if t.device.index != here:
+            raise ValueError("%s[%d] is on %s, and the current device is cuda:%d" % (name, i, t.device, here))
+        if t.numel() != sizes[i]:
+            raise ValueError("%s[%d] must have %d elements, has %d" % (name, i, sizes[i], t.numel()))
+        arr[i] = _ptr(t)
+    return arr
+
+
+def _size_array(sizes):
+    return (ctypes.c_int64 * max(len(sizes), 1))(*sizes)
+
+
+def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                        weight_decay=0.01, copy=None, factors=None, seed: int = 0, stream=None):
+    """adamw_apply with its arguments marshalled once (see prepare_sparse_apply):
+    a callable that takes the step."""
+    import torch
+    lib = load_library()
+    g, x, m, v = list(g), list(x), list(m), list(v)
+    copy = None if copy is None else list(copy)
+    sizes = [t.numel() for t in x]
+    state = STATE_8 if m and m[0] is not None and m[0].dtype == torch.uint8 else STATE_32
+    held = [adamw_state_bytes(n) for n in sizes] if state == STATE_8 else sizes
+    kinds = (torch.uint8,) if state == STATE_8 else (torch.float32,)
+    gp = _tensor_list(g, "g", (torch.float32, torch.bfloat16), sizes)
+    xp = _tensor_list(x, "x", (torch.float32,), sizes)
+    mp = _tensor_list(m, "m", kinds, held)
+    vp = _tensor_list(v, "v", kinds, held)
+    cp = None if copy is None else _tensor_list(copy, "copy", (torch.bfloat16,), sizes, optional=True)
+    if hasattr(weight_decay, "__len__"):
+        if len(weight_decay) != len(sizes):
+            raise ValueError("weight_decay must be one number or one for each tensor")
+        decays = [float(w) for w in weight_decay]
+    else:
+        decays = [float(weight_decay)] * len(sizes)
+    dp = (ctypes.c_float * max(len(sizes), 1))(*decays)
+    if factors is not None:
+        _require(factors, torch.float32, "factors")
+        if factors.numel() != 2:
+            raise ValueError("factors must have two elements")
+        _on_current_device(factors=factors)
+    if not 0 <= int(seed) < 2 ** 32:
+        raise ValueError("seed must fit 32 bits")
+    grad = _dtype_code(g[0], "g") if g else FP32
+    head = (gp, grad, xp, cp, mp, vp, state, _size_array(sizes), dp, len(sizes), float(lr), float(beta1), float(beta2),
+            float(eps))
+    tail = (None if factors is None else factors.data_ptr(), int(seed), _stream_handle(stream))
+    fn = lib.adamw_apply
+
+    def call(step):
+        if isinstance(step, torch.Tensor):
+            _require(step, torch.int64, "step")
+            if step.numel() != 1:
+                raise ValueError("step must have one element")
+            _on_current_device(step=step)
+            call.step = step   # alive as long as a graph that this call was captured in
+            _check(lib, fn(*head, 1, step.data_ptr(), *tail))
+        else:
+            _check(lib, fn(*head, int(step), None, *tail))
+    call.tensors = (tuple(g), tuple(x), tuple(m), tuple(v), copy and tuple(copy), factors)
+    return call
+
+
+def adamw_apply(g, x, m, v, step, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                weight_decay=0.01, copy=None, factors=None, seed: int = 0, stream=None) -> None:
+    """One AdamW step over lists of tensors; see adamw_apply in include/efsparse.h.
+    g: fp32 or bf16; x: fp32; m, v: fp32, or uint8 from new_adamw_state; copy: bf16
+    tensors (or None) that receive the new x; step: the number of the step, or an
+    int64 device tensor that holds it; weight_decay: one number, or one for each
+    tensor; factors: fp32 device tensor of two, of lr and of g."""
+    prepare_adamw_apply(g, x, m, v, lr, beta1, beta2, eps, weight_decay, copy, factors, seed, stream)(step)
+
+
+def _prepare_state(name, m8, v8, m, v, stream):
+    import torch
+    lib = load_library()
+    m8, v8, m, v = list(m8), list(v8), list(m), list(v)
+    sizes = [t.numel() for t in m]
+    held = [adamw_state_bytes(n) for n in sizes]
+    lists = {"m8": _tensor_list(m8, "m8", (torch.uint8,), held), "v8": _tensor_list(v8, "v8", (torch.uint8,), held),
+             "m": _tensor_list(m, "m", (torch.float32,), sizes), "v": _tensor_list(v, "v", (torch.float32,), sizes)}
+    order = ("m8", "v8", "m", "v") if name == "adamw_read_state" else ("m", "v", "m8", "v8")
+    args = tuple(lists[k] for k in order) + (_size_array(sizes), len(sizes), _stream_handle(stream))
+    fn = getattr(lib, name)
+
+    def call():
+        _check(lib, fn(*args))
+    call.tensors = (tuple(m8), tuple(v8), tuple(m), tuple(v))   # alive as long as the pointers in args
+    return call
+
+
+def prepare_adamw_read_state(m8, v8, m, v, stream=None):
+    """adamw_read_state with its arguments marshalled once (see prepare_sparse_apply)."""
+    return _prepare_state("adamw_read_state", m8, v8, m, v, stream)
+
+
+def adamw_read_state(m8, v8, m, v, stream=None) -> None:
+    """The values that states of 8 bits stand for, into fp32 tensors m and v; see
+    adamw_read_state in include/efsparse.h."""
+    prepare_adamw_read_state(m8, v8, m, v, stream)()
+
+
+def adamw_write_state(m, v, m8, v8, stream=None) -> None:
+    """States of 8 bits from fp32 tensors m and v; see adamw_write_state in include/efsparse.h."""
+    _prepare_state("adamw_write_state", m8, v8, m, v, stream)()
 
 
 def copy_probe(src, dst, stream=None) -> None:

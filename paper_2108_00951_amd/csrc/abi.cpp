@@ -3,10 +3,12 @@
 // every argument has been checked; nothing here allocates or synchronises.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <cstdlib>
 
 #include "../../include/efsparse.h"
 #include "launch.hpp"
@@ -23,6 +25,12 @@ static_assert(efs::kXentMaxTokens == EFS_XENT_MAX_TOKENS, "token limit differs f
 static_assert(efs::kXentMaxVocab == EFS_XENT_MAX_VOCAB, "vocabulary limit differs from the header");
 static_assert(efs::kXentMaxHidden == EFS_XENT_MAX_HIDDEN, "hidden limit differs from the header");
 static_assert(efs::kXentBadTarget == EFS_XENT_BAD_TARGET, "status bit differs from the header");
+static_assert(efs::kEmbedMaxTokens == EFS_EMBED_MAX_TOKENS, "token limit differs from the header");
+static_assert(efs::kEmbedMaxVocab == EFS_EMBED_MAX_VOCAB, "vocabulary limit differs from the header");
+static_assert(efs::kEmbedMaxWidth == EFS_EMBED_MAX_WIDTH, "width limit differs from the header");
+static_assert(efs::kEmbedBadId == EFS_EMBED_BAD_ID, "status bit differs from the header");
+static_assert(efs::kNormMaxWidth == EFS_NORM_MAX_WIDTH, "width limit differs from the header");
+static_assert(efs::kAdamwMaxTensors == EFS_ADAMW_MAX_TENSORS, "tensor limit differs from the header");
 static_assert(sizeof(efs::Telemetry) == EFS_TELEMETRY_BYTES, "telemetry layout differs from the header");
 
 namespace {
@@ -99,7 +107,7 @@ struct Given {
 };
 
 Given flat(const char *name, const void *p, int64_t bytes, bool written) {
-    return Given{name, Rows{reinterpret_cast<uintptr_t>(p), bytes, bytes, bytes}, written};
+    return Given{name, Rows{bytes == 0 ? 0 : reinterpret_cast<uintptr_t>(p), bytes, bytes, bytes}, written};
 }
 
 template <int N>
@@ -109,6 +117,93 @@ efs_status check_apart(const char *name, const Given (&given)[N]) {
             if ((given[i].written || given[j].written) && meet(given[i].rows, given[j].rows))
                 return fail(EFS_EINVAL, "%s: %s and %s must not overlap", name, given[j].name, given[i].name);
     return EFS_OK;
+}
+
+// Memory of a list of tensors, of which each is a run of bytes.
+struct Span {
+    uintptr_t at, end;
+    const char *name;
+    bool written;
+};
+
+// Sees spans in ascending order and says which two share a byte that one of them writes.
+struct SpanSweep {
+    Span last = {0, 0, "", false}, last_written = {0, 0, "", false};   // those that reach furthest
+
+    const char *add(const Span &s) {
+        const char *met = nullptr;
+        if (s.at < last_written.end) met = last_written.name;
+        else if (s.written && s.at < last.end) met = last.name;
+        if (s.end > last.end) last = s;
+        if (s.written && s.end > last_written.end) last_written = s;
+        return met;
+    }
+};
+
+// One array of a call's list of tensors: pointers, bytes of each element (of the
+// states of 8 bits: 0).
+struct Column {
+    const char *name;
+    const void *const *at;   // NULL: none; entries may be NULL
+    int64_t size;
+    bool written;
+};
+
+Span span_of(const Column &c, const int64_t *sizes, int32_t i) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(c.at[i]);
+    const uintptr_t bytes = c.size == 0 ? uintptr_t(efs::adamw_state_size(sizes[i])) : uintptr_t(sizes[i] * c.size);
+    return Span{at, at + bytes, c.name, c.written};
+}
+
+// Whether what is written meets anything else, over all tensors of all columns.
+// Layers of flat vectors come in ascending order and are merged as they are;
+// others are sorted.
+template <int N>
+efs_status check_lists(const char *name, const Column (&columns)[N], const int64_t *sizes, int32_t count) {
+    const auto there = [&](int c, int32_t i) {
+        return columns[c].at != nullptr && columns[c].at[i] != nullptr && sizes[i] > 0;
+    };
+    bool ascending = true;
+    int64_t spans = 0;
+    for (int c = 0; c < N && columns[c].at != nullptr; ++c) {
+        uintptr_t before = 0;
+        for (int32_t i = 0; i < count; ++i)
+            if (there(c, i)) {
+                const uintptr_t at = reinterpret_cast<uintptr_t>(columns[c].at[i]);
+                ascending = ascending && at >= before;
+                before = at;
+                ++spans;
+            }
+    }
+    SpanSweep sweep;
+    if (ascending) {
+        int32_t next[N] = {};
+        for (;;) {
+            int least = -1;
+            for (int c = 0; c < N; ++c) {
+                if (columns[c].at == nullptr) continue;
+                while (next[c] < count && !there(c, next[c])) ++next[c];
+                if (next[c] < count && (least < 0 || columns[c].at[next[c]] < columns[least].at[next[least]])) least = c;
+            }
+            if (least < 0) return EFS_OK;
+            const Span s = span_of(columns[least], sizes, next[least]++);
+            if (const char *met = sweep.add(s))
+                return fail(EFS_EINVAL, "%s: tensors of %s and %s must not overlap", name, met, s.name);
+        }
+    }
+    Span *all = static_cast<Span *>(std::malloc(size_t(spans) * sizeof(Span)));
+    if (all == nullptr) return fail(EFS_ESPACE, "%s: no host memory to check %lld tensors", name, (long long)spans);
+    int64_t n = 0;
+    for (int c = 0; c < N; ++c)
+        for (int32_t i = 0; i < count; ++i)
+            if (there(c, i)) all[n++] = span_of(columns[c], sizes, i);
+    std::sort(all, all + n, [](const Span &a, const Span &b) { return a.at < b.at; });
+    efs_status s = EFS_OK;
+    for (int64_t i = 0; i < n && s == EFS_OK; ++i)
+        if (const char *met = sweep.add(all[i]))
+            s = fail(EFS_EINVAL, "%s: tensors of %s and %s must not overlap", name, met, all[i].name);
+    std::free(all);
+    return s;
 }
 
 int g_cu_count[64];  // per device; 0 = not queried yet
@@ -615,6 +710,274 @@ efs_status xent_backward(const void *h, int64_t ld_h, const void *w, int64_t ld_
                                                   hidden, ignore_index, lse, dloss, dh, ld_dh, dw, ld_dw,
                                                   workspace, static_cast<hipStream_t>(stream)),
                         name);
+}
+
+static bool dtype_ok(int dtype) { return dtype == EFS_FP32 || dtype == EFS_BF16; }
+
+static int64_t dtype_size(int dtype) { return dtype == EFS_BF16 ? 2 : 4; }
+
+// A matrix of a call: non-NULL, aligned to its type, its rows no closer than they are long.
+static efs_status check_rows(const char *name, const char *what, const void *p, int64_t ld, int32_t cols, int dtype) {
+    if (p == nullptr || !aligned(p, uintptr_t(dtype_size(dtype))))
+        return fail(EFS_EINVAL, "%s: %s must be non-NULL and aligned to its type", name, what);
+    if (ld < cols || ld > kMaxLen) return fail(EFS_EINVAL, "%s: ld_%s must be in [%d, 2^31-1]", name, what, cols);
+    return EFS_OK;
+}
+
+// What both directions of the lookup check alike.
+static efs_status check_embed(const char *name, int table_dtype, const int64_t *ids, int dtype, int32_t tokens,
+                              int32_t vocab, int32_t width, float scale, const uint32_t *status) {
+    if (!dtype_ok(dtype) || !dtype_ok(table_dtype))
+        return fail(EFS_EINVAL, "%s: a dtype is neither EFS_FP32 nor EFS_BF16", name);
+    if (tokens < 0 || tokens > efs::kEmbedMaxTokens || vocab < 1 || vocab > efs::kEmbedMaxVocab || width < 1 ||
+        width > efs::kEmbedMaxWidth)
+        return fail(EFS_EINVAL, "%s: %d tokens, %d words or %d values a row are outside the limits", name, tokens,
+                    vocab, width);
+    if (!std::isfinite(scale)) return fail(EFS_EINVAL, "%s: scale must be finite", name);
+    if (tokens > 0 && (ids == nullptr || !aligned(ids, 8)))
+        return fail(EFS_EINVAL, "%s: ids must be non-NULL and 8-byte aligned", name);
+    if (!aligned(status, 4)) return fail(EFS_EINVAL, "%s: status must be 4-byte aligned", name);
+    return EFS_OK;
+}
+
+efs_status embed_forward(const void *table, int64_t ld_table, int table_dtype, const int64_t *ids, void *out,
+                         int64_t ld_out, int dtype, int32_t tokens, int32_t vocab, int32_t width, float scale,
+                         int64_t ignore_index, uint32_t *status, void *stream) {
+    const char *name = "embed_forward";
+    efs_status s = check_embed(name, table_dtype, ids, dtype, tokens, vocab, width, scale, status);
+    if (s != EFS_OK || tokens == 0) return s;
+    if ((s = check_rows(name, "table", table, ld_table, width, table_dtype)) != EFS_OK) return s;
+    if ((s = check_rows(name, "out", out, ld_out, width, dtype)) != EFS_OK) return s;
+    const Given given[4] = {{"table", rows_of(table, vocab, ld_table, width, dtype_size(table_dtype)), false},
+                            {"out", rows_of(out, tokens, ld_out, width, dtype_size(dtype)), true},
+                            flat("ids", ids, int64_t(tokens) * 8, false),
+                            flat("status", status, status != nullptr ? 4 : 0, true)};
+    if ((s = check_apart(name, given)) != EFS_OK) return s;
+    return check_launch(efs::launch_embed_forward(table, ld_table, table_dtype == EFS_BF16, ids, out, ld_out,
+                                                  dtype == EFS_BF16, tokens, vocab, width, scale, ignore_index, status,
+                                                  static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+size_t embed_workspace_bytes(int32_t tokens, int32_t vocab, int32_t width) {
+    if (tokens < 0 || tokens > efs::kEmbedMaxTokens || vocab < 1 || vocab > efs::kEmbedMaxVocab || width < 1 ||
+        width > efs::kEmbedMaxWidth || int64_t(tokens) * vocab > int64_t(1) << 38)
+        return 0;
+    return efs::embed_workspace_size(tokens, width);
+}
+
+efs_status embed_backward(const void *dout, int64_t ld_dout, int dtype, const int64_t *ids, void *dtable,
+                          int64_t ld_dtable, int table_dtype, int32_t tokens, int32_t vocab, int32_t width,
+                          float scale, int64_t ignore_index, int accumulate, uint32_t *status, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    const char *name = "embed_backward";
+    efs_status s = check_embed(name, table_dtype, ids, dtype, tokens, vocab, width, scale, status);
+    if (s != EFS_OK) return s;
+    const size_t need = embed_workspace_bytes(tokens, vocab, width);
+    if (need == 0) return fail(EFS_EINVAL, "%s: %d tokens x %d words are more than 2^38", name, tokens, vocab);
+    if (accumulate != 0 && accumulate != 1) return fail(EFS_EINVAL, "%s: accumulate must be 0 or 1", name);
+    if ((s = check_rows(name, "dtable", dtable, ld_dtable, width, table_dtype)) != EFS_OK) return s;
+    if (tokens > 0 && (s = check_rows(name, "dout", dout, ld_dout, width, dtype)) != EFS_OK) return s;
+    if (workspace == nullptr || !aligned(workspace, 16))
+        return fail(EFS_EINVAL, "%s: workspace must be non-NULL and 16-byte aligned", name);
+    if (workspace_bytes < need)
+        return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    const Given given[5] = {{"dtable", rows_of(dtable, vocab, ld_dtable, width, dtype_size(table_dtype)), true},
+                            tokens > 0 ? Given{"dout", rows_of(dout, tokens, ld_dout, width, dtype_size(dtype)), false}
+                                       : flat("dout", nullptr, 0, false),
+                            flat("ids", ids, int64_t(tokens) * 8, false),
+                            flat("status", status, status != nullptr ? 4 : 0, true),
+                            flat("workspace", workspace, int64_t(need), true)};
+    if ((s = check_apart(name, given)) != EFS_OK) return s;
+    if (tokens == 0 && accumulate) return EFS_OK;
+    return check_launch(efs::launch_embed_backward(dout, ld_dout, dtype == EFS_BF16, ids, dtable, ld_dtable,
+                                                   table_dtype == EFS_BF16, tokens, vocab, width, scale, ignore_index,
+                                                   accumulate != 0, status, workspace,
+                                                   static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+// What both directions of the norm check alike.
+static efs_status check_norm(const char *name, const void *x, int64_t ld_x, const void *weight, int dtype,
+                             int weight_dtype, int32_t rows, int32_t width) {
+    if (!dtype_ok(dtype) || !dtype_ok(weight_dtype))
+        return fail(EFS_EINVAL, "%s: a dtype is neither EFS_FP32 nor EFS_BF16", name);
+    if (rows < 0 || width < 1 || width > efs::kNormMaxWidth)
+        return fail(EFS_EINVAL, "%s: %d rows of %d values are outside the limits", name, rows, width);
+    if (!aligned(weight, uintptr_t(dtype_size(weight_dtype))))
+        return fail(EFS_EINVAL, "%s: weight must be aligned to its type", name);
+    return rows == 0 ? EFS_OK : check_rows(name, "x", x, ld_x, width, dtype);
+}
+
+// Rows that are written: they may be those of an input itself, and then meet nothing of it.
+static Given given_rows(const char *name, const void *p, int64_t rows, int64_t ld, int64_t width, int dtype, bool written) {
+    if (rows == 0) return flat(name, nullptr, 0, written);
+    return Given{name, rows_of(p, rows, ld, width, dtype_size(dtype)), written};
+}
+
+efs_status layernorm_forward(const void *x, int64_t ld_x, const void *weight, const void *bias, void *y, int64_t ld_y,
+                             int dtype, int weight_dtype, int32_t rows, int32_t width, float eps, float *mean,
+                             float *rstd, void *stream) {
+    const char *name = "layernorm_forward";
+    efs_status s = check_norm(name, x, ld_x, weight, dtype, weight_dtype, rows, width);
+    if (s != EFS_OK) return s;
+    if (!aligned(bias, uintptr_t(dtype_size(weight_dtype))))
+        return fail(EFS_EINVAL, "%s: bias must be aligned to its type", name);
+    if (!std::isfinite(eps) || eps < 0.0f) return fail(EFS_EINVAL, "%s: eps must be finite and >= 0", name);
+    if (!aligned(mean, 4) || !aligned(rstd, 4)) return fail(EFS_EINVAL, "%s: mean and rstd must be 4-byte aligned", name);
+    if (rows == 0) return EFS_OK;
+    if ((s = check_rows(name, "y", y, ld_y, width, dtype)) != EFS_OK) return s;
+    const bool itself = y == x && (ld_y == ld_x || rows == 1);
+    const int64_t row = int64_t(width) * dtype_size(weight_dtype);
+    const Given given[6] = {given_rows("x", x, itself ? 0 : rows, ld_x, width, dtype, false),
+                            given_rows("y", y, rows, ld_y, width, dtype, true),
+                            flat("weight", weight, weight != nullptr ? row : 0, false),
+                            flat("bias", bias, bias != nullptr ? row : 0, false),
+                            flat("mean", mean, mean != nullptr ? int64_t(rows) * 4 : 0, true),
+                            flat("rstd", rstd, rstd != nullptr ? int64_t(rows) * 4 : 0, true)};
+    if ((s = check_apart(name, given)) != EFS_OK) return s;
+    return check_launch(efs::launch_layernorm_forward(x, ld_x, weight, bias, y, ld_y, dtype == EFS_BF16,
+                                                      weight_dtype == EFS_BF16, rows, width, eps, mean, rstd,
+                                                      static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+size_t layernorm_workspace_bytes(int32_t rows, int32_t width) {
+    if (rows < 0 || width < 1 || width > efs::kNormMaxWidth) return 0;
+    return efs::layernorm_workspace_size(rows, width);
+}
+
+efs_status layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean, const float *rstd,
+                              const void *dy, int64_t ld_dy, void *dx, int64_t ld_dx, int dtype, int weight_dtype,
+                              int32_t rows, int32_t width, void *dweight, void *dbias, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    const char *name = "layernorm_backward";
+    efs_status s = check_norm(name, x, ld_x, weight, dtype, weight_dtype, rows, width);
+    if (s != EFS_OK) return s;
+    const uintptr_t size = uintptr_t(dtype_size(weight_dtype));
+    if (!aligned(dweight, size) || !aligned(dbias, size))
+        return fail(EFS_EINVAL, "%s: dweight and dbias must be aligned to their type", name);
+    if (rows > 0) {
+        if ((s = check_rows(name, "dy", dy, ld_dy, width, dtype)) != EFS_OK) return s;
+        if ((s = check_rows(name, "dx", dx, ld_dx, width, dtype)) != EFS_OK) return s;
+        if (mean == nullptr || rstd == nullptr || !aligned(mean, 4) || !aligned(rstd, 4))
+            return fail(EFS_EINVAL, "%s: mean and rstd must be non-NULL and 4-byte aligned", name);
+    }
+    if (workspace == nullptr || !aligned(workspace, 16))
+        return fail(EFS_EINVAL, "%s: workspace must be non-NULL and 16-byte aligned", name);
+    const size_t need = efs::layernorm_workspace_size(rows, width);
+    if (workspace_bytes < need)
+        return fail(EFS_ESPACE, "%s: workspace has %zu bytes, needs %zu", name, workspace_bytes, need);
+    const bool is_x = dx == x && (ld_dx == ld_x || rows == 1), is_dy = dx == dy && (ld_dx == ld_dy || rows == 1);
+    const int64_t row = int64_t(width) * int64_t(size), each = int64_t(rows) * 4;
+    const Given given[9] = {given_rows("x", x, is_x ? 0 : rows, ld_x, width, dtype, false),
+                            given_rows("dy", dy, is_dy ? 0 : rows, ld_dy, width, dtype, false),
+                            given_rows("dx", dx, rows, ld_dx, width, dtype, true),
+                            flat("weight", weight, weight != nullptr ? row : 0, false),
+                            flat("mean", mean, each, false),
+                            flat("rstd", rstd, each, false),
+                            flat("dweight", dweight, dweight != nullptr ? row : 0, true),
+                            flat("dbias", dbias, dbias != nullptr ? row : 0, true),
+                            flat("workspace", workspace, int64_t(need), true)};
+    if ((s = check_apart(name, given)) != EFS_OK) return s;
+    if (rows == 0 && dweight == nullptr && dbias == nullptr) return EFS_OK;
+    return check_launch(efs::launch_layernorm_backward(x, ld_x, weight, mean, rstd, dy, ld_dy, dx, ld_dx,
+                                                       dtype == EFS_BF16, weight_dtype == EFS_BF16, rows, width,
+                                                       dweight, dbias, workspace, static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+size_t adamw_state_bytes(int64_t size) {
+    if (size < 0 || size > kMaxLen) return 0;
+    return efs::adamw_state_size(size);
+}
+
+// One array of tensors: there, and every tensor that is not empty aligned.
+static efs_status check_list(const char *name, const char *what, const void *const *list, const int64_t *sizes,
+                             int32_t count, uintptr_t align, bool optional) {
+    if (list == nullptr) return fail(EFS_EINVAL, "%s: %s must be a host array", name, what);
+    for (int32_t i = 0; i < count; ++i)
+        if (sizes[i] > 0 && ((list[i] == nullptr && !optional) || !aligned(list[i], align)))
+            return fail(EFS_EINVAL, "%s: tensor %d of %s must be non-NULL and %d-byte aligned", name, i, what,
+                        int(align));
+    return EFS_OK;
+}
+
+static efs_status check_sizes(const char *name, const int64_t *sizes, int32_t count) {
+    if (count < 0 || count > efs::kAdamwMaxTensors)
+        return fail(EFS_EINVAL, "%s: count=%d outside [0, %d]", name, count, efs::kAdamwMaxTensors);
+    if (count > 0 && sizes == nullptr) return fail(EFS_EINVAL, "%s: sizes must be a host array", name);
+    for (int32_t i = 0; i < count; ++i)
+        if (sizes[i] < 0 || sizes[i] > kMaxLen)
+            return fail(EFS_EINVAL, "%s: tensor %d has %lld elements, not 0 to 2^31-1", name, i, (long long)sizes[i]);
+    return EFS_OK;
+}
+
+static const void *const *as_list(const void *list) { return static_cast<const void *const *>(list); }
+
+efs_status adamw_apply(const void *const *g, int grad_dtype, float *const *x, void *const *copies, void *const *m,
+                       void *const *v, int state, const int64_t *sizes, const float *decays, int32_t count,
+                       float gamma, float beta1, float beta2, float eps, int64_t step, const int64_t *step_device,
+                       const float *factors, uint32_t seed, void *stream) {
+    const char *name = "adamw_apply";
+    if (!dtype_ok(grad_dtype)) return fail(EFS_EINVAL, "%s: grad_dtype is neither EFS_FP32 nor EFS_BF16", name);
+    if (state != EFS_STATE_32 && state != EFS_STATE_8)
+        return fail(EFS_EINVAL, "%s: state is neither EFS_STATE_32 nor EFS_STATE_8", name);
+    efs_status s = check_sizes(name, sizes, count);
+    if (s != EFS_OK) return s;
+    if (!std::isfinite(gamma) || !std::isfinite(eps) || eps < 0.0f)
+        return fail(EFS_EINVAL, "%s: gamma and eps must be finite, eps >= 0", name);
+    if (!(beta1 >= 0.0f && beta1 < 1.0f && beta2 >= 0.0f && beta2 < 1.0f))
+        return fail(EFS_EINVAL, "%s: beta1 and beta2 must be in [0, 1)", name);
+    if (step_device == nullptr && step < 1) return fail(EFS_EINVAL, "%s: step must be >= 1", name);
+    if (!aligned(step_device, 8) || !aligned(factors, 4))
+        return fail(EFS_EINVAL, "%s: step_device must be 8-byte and factors 4-byte aligned", name);
+    if (count == 0) return EFS_OK;
+    const bool bytes = state == EFS_STATE_8;
+    const uintptr_t held = bytes ? 16 : 4;
+    if ((s = check_list(name, "g", g, sizes, count, uintptr_t(dtype_size(grad_dtype)), false)) != EFS_OK) return s;
+    if ((s = check_list(name, "x", as_list(x), sizes, count, 4, false)) != EFS_OK) return s;
+    if ((s = check_list(name, "m", as_list(m), sizes, count, held, false)) != EFS_OK) return s;
+    if ((s = check_list(name, "v", as_list(v), sizes, count, held, false)) != EFS_OK) return s;
+    if (copies != nullptr && (s = check_list(name, "copies", as_list(copies), sizes, count, 2, true)) != EFS_OK) return s;
+    for (int32_t i = 0; decays != nullptr && i < count; ++i)
+        if (!std::isfinite(decays[i])) return fail(EFS_EINVAL, "%s: decays must be finite", name);
+    const Column columns[5] = {{"g", g, dtype_size(grad_dtype), false},
+                               {"x", as_list(x), 4, true},
+                               {"m", as_list(m), bytes ? 0 : 4, true},
+                               {"v", as_list(v), bytes ? 0 : 4, true},
+                               {"copies", as_list(copies), 2, true}};
+    if ((s = check_lists(name, columns, sizes, count)) != EFS_OK) return s;
+    const efs::AdamwArgs args{g,    x,     m,     v,   copies, sizes,       decays,  count, grad_dtype == EFS_BF16, bytes,
+                              gamma, beta1, beta2, eps, step,   step_device, factors, seed};
+    return check_launch(efs::launch_adamw(args, static_cast<hipStream_t>(stream)), name);
+}
+
+static efs_status state_call(const char *name, bool write, float *const *m, float *const *v, void *const *m8,
+                             void *const *v8, const int64_t *sizes, int32_t count, void *stream) {
+    efs_status s = check_sizes(name, sizes, count);
+    if (s != EFS_OK || count == 0) return s;
+    if ((s = check_list(name, "m", as_list(m), sizes, count, 4, false)) != EFS_OK) return s;
+    if ((s = check_list(name, "v", as_list(v), sizes, count, 4, false)) != EFS_OK) return s;
+    if ((s = check_list(name, "m8", as_list(m8), sizes, count, 16, false)) != EFS_OK) return s;
+    if ((s = check_list(name, "v8", as_list(v8), sizes, count, 16, false)) != EFS_OK) return s;
+    const Column columns[4] = {{"m", as_list(m), 4, !write},
+                               {"v", as_list(v), 4, !write},
+                               {"m8", as_list(m8), 0, write},
+                               {"v8", as_list(v8), 0, write}};
+    if ((s = check_lists(name, columns, sizes, count)) != EFS_OK) return s;
+    return check_launch(efs::launch_adamw_state(write, m, v, m8, v8, sizes, count, static_cast<hipStream_t>(stream)),
+                        name);
+}
+
+efs_status adamw_read_state(void *const *m8, void *const *v8, float *const *m, float *const *v, const int64_t *sizes,
+                            int32_t count, void *stream) {
+    return state_call("adamw_read_state", false, m, v, m8, v8, sizes, count, stream);
+}
+
+efs_status adamw_write_state(float *const *m, float *const *v, void *const *m8, void *const *v8, const int64_t *sizes,
+                             int32_t count, void *stream) {
+    return state_call("adamw_write_state", true, m, v, m8, v8, sizes, count, stream);
 }
 
 // The probes address at most INT32_MAX tiles (one workgroup each in the

@@ -75,6 +75,53 @@ hipError_t launch_xent_backward(const void *h, int64_t ld_h, const void *w, int6
                                 const float *lse, const float *dloss, void *dh, int64_t ld_dh, void *dw,
                                 int64_t ld_dw, void *workspace, hipStream_t stream);
 
+// Words looked up and the gradient of their table (embed.hip).
+constexpr uint32_t kEmbedBadId = 1u;   // an id neither ignored nor in the table
+constexpr int32_t kEmbedMaxTokens = 1 << 22, kEmbedMaxVocab = 1 << 24, kEmbedMaxWidth = 1 << 18;
+hipError_t launch_embed_forward(const void *table, int64_t ld_table, bool table_bf16, const int64_t *ids, void *out,
+                                int64_t ld_out, bool bf16, int32_t tokens, int32_t vocab, int32_t width, float scale,
+                                int64_t ignore, uint32_t *status, hipStream_t stream);
+size_t embed_workspace_size(int32_t tokens, int32_t width);
+hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, const int64_t *ids, void *dtable,
+                                 int64_t ld_dtable, bool table_bf16, int32_t tokens, int32_t vocab, int32_t width,
+                                 float scale, int64_t ignore, bool accumulate, uint32_t *status, void *workspace,
+                                 hipStream_t stream);
+
+// Layer norm and its gradients (norm.hip).  weight, bias, dweight, dbias, mean
+// and rstd of the forward call may be NULL.
+constexpr int32_t kNormMaxWidth = 1 << 18;
+hipError_t launch_layernorm_forward(const void *x, int64_t ld_x, const void *weight, const void *bias, void *y,
+                                    int64_t ld_y, bool bf16, bool weight_bf16, int32_t rows, int32_t width, float eps,
+                                    float *mean, float *rstd, hipStream_t stream);
+size_t layernorm_workspace_size(int32_t rows, int32_t width);
+hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean,
+                                     const float *rstd, const void *dy, int64_t ld_dy, void *dx, int64_t ld_dx, bool bf16,
+                                     bool weight_bf16, int32_t rows, int32_t width, void *dweight, void *dbias,
+                                     void *workspace, hipStream_t stream);
+
+// AdamW over a list of tensors (adamw.hip).  Arrays of `count` on the host.
+constexpr int32_t kAdamwMaxTensors = 1 << 16;
+constexpr int kAdamwBlock = 256;   // elements of an 8-bit state with one scale
+struct AdamwArgs {
+    const void *const *g;
+    float *const *x;
+    void *const *m, *const *v, *const *copy;   // copy: may be NULL
+    const int64_t *size;
+    const float *decay;                        // may be NULL
+    int32_t count;
+    bool bf16, bytes;                          // of g; states in 8 bits
+    float gamma, beta1, beta2, eps;
+    int64_t step;
+    const int64_t *step_device;                // may be NULL
+    const float *factors;                      // may be NULL
+    uint32_t seed;
+};
+hipError_t launch_adamw(const AdamwArgs &args, hipStream_t stream);
+size_t adamw_state_size(int64_t size);
+// write: the states of 8 bits from m and v; else these from the states.
+hipError_t launch_adamw_state(bool write, float *const *m, float *const *v, void *const *m8, void *const *v8,
+                              const int64_t *size, int32_t count, hipStream_t stream);
+
 hipError_t launch_copy(const float *src, float *dst, int64_t n, bool per_tile, hipStream_t stream);
 hipError_t launch_stream_probe(const float *x, float *y, int64_t n, int mode, bool per_tile,
                                hipStream_t stream);

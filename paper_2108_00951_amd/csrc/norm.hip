@@ -1,0 +1,511 @@
+// Layer norm and its gradients.
+//
+//   y  = (x - mean) rstd w + b                     rows of x; mean, rstd of a row
+//   g  = dy w ;  h = (x - mean) rstd
+//   dx = rstd (g - mean(g) - h mean(g h))
+//   dw = sum over the rows of dy h ;  db = sum over the rows of dy
+//
+// Bytes bound it: x in and y out, x and dy in and dx out.  A row is read once and
+// stays in the registers of one wave, 256 or 1,024 threads, which are left with
+// the same columns row after row, so that the weights are read once too and the
+// sums of dw and db stay in registers until the workgroup ends.  These partial
+// sums go to the workspace and a second launch adds them in order: no atomics,
+// and the same bits each time.
+//
+// The mean is taken first and the squares of x - mean after it: a row whose mean
+// is large against its spread loses nothing by them.  What the rounding of the
+// mean itself leaves, the sum of x - mean, is taken off again (it is also what
+// makes x - mean right in the backward pass, from the mean as it was stored).
+#include "rows.hpp"
+#include "launch.hpp"
+
+#include <math.h>
+
+namespace efs {
+
+namespace {
+
+struct Norm {
+    const void *x, *weight, *bias, *dy;
+    void *out;              // y or dx
+    float *mean, *rstd;     // forward: may be NULL
+    float *partial;         // backward: [gridDim.x][2][width], NULL: no gradients of weight and bias
+    float *sums;            // backward of long rows: [rows][4]
+    int64_t ld_x, ld_dy, ld_out;
+    int32_t rows, width;
+    float eps;
+};
+
+template <typename T>
+constexpr int kRowPack = 16 / sizeof(T);
+
+// The sums of M values over the kThreads threads that hold a row, in each of
+// them.  One barrier: the next call takes another buffer, and the one after it
+// comes behind that one's barrier.
+template <int kThreads, int M>
+__device__ __forceinline__ void row_sums(float (&v)[M], float (*buffer)[M]) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) v[m] = wave_sum(v[m]);
+    if (kThreads > kWave) {
+        constexpr int kRowWaves = kThreads / kWave;
+        const int wave = threadIdx.x / kWave, first = wave / kRowWaves * kRowWaves;
+        if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+            for (int m = 0; m < M; ++m) buffer[wave][m] = v[m];
+        __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M; ++m) v[m] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w)
+#pragma unroll
+            for (int m = 0; m < M; ++m) v[m] += buffer[first + w][m];
+    }
+}
+
+// This thread's columns of a row of weights; `absent` where there are none.
+template <typename F, int N, int kPacks, int kThreads>
+__device__ __forceinline__ void load_columns(const void *row, int width, float absent, float (&v)[kPacks][N]) {
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+        const int at = (k * kThreads + threadIdx.x % kThreads) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[k][i] = absent;
+        if (row != nullptr && at < width) load_pack<N>(static_cast<const F *>(row) + at, width - at, v[k]);
+    }
+}
+
+struct Moments {
+    float mean, rstd, rest;   // rest: mean of x - (the mean that was subtracted)
+};
+
+// From the sums of x - m and of its squares.
+__device__ __forceinline__ Moments moments(float m, float sum, float squares, int width, float eps) {
+    const float n = float(width), rest = sum / n;
+    const float var = (squares - sum * rest) / n;
+    // a constant row's sums can leave less than 0; NaN stays.  Where the spread is
+    // larger than the mean, the differences are rounded more coarsely than the sum was
+    return Moments{m * m > var ? m + rest : m, 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps), rest};
+}
+
+template <typename T, typename F, int kThreads, int kPacks>
+__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void norm_forward_kernel(const Norm a) {
+    constexpr int N = kRowPack<T>, kSize = kThreads < kBlock ? kBlock : kThreads, kGroups = kSize / kThreads;
+    __shared__ float s_sum[kSize / kWave][1], s_squares[kSize / kWave][2];
+    const int lane = threadIdx.x % kThreads, group = threadIdx.x / kThreads;
+    float w[kPacks][N], b[kPacks][N];
+    load_columns<F, N, kPacks, kThreads>(a.weight, a.width, 1.0f, w);
+    load_columns<F, N, kPacks, kThreads>(a.bias, a.width, 0.0f, b);
+    for (int64_t first = int64_t(blockIdx.x) * kGroups; first < a.rows; first += int64_t(gridDim.x) * kGroups) {
+        const int64_t row = first + group;
+        if (kThreads <= kWave && row >= a.rows) break;   // (a row of the workgroup's own is there)
+        const T *from = static_cast<const T *>(a.x) + row * a.ld_x;
+        float x[kPacks][N];
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[k][i] = 0.0f;
+            if (at < a.width) load_pack<N>(from + at, a.width - at, x[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[0] += x[k][i];
+        row_sums<kThreads>(sum, s_sum);
+        const float m = sum[0] / float(a.width);
+        float rest[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[k][i] = at + i < a.width ? x[k][i] - m : 0.0f;
+                rest[0] += x[k][i];
+                rest[1] = fmaf(x[k][i], x[k][i], rest[1]);
+            }
+        }
+        row_sums<kThreads>(rest, s_squares);
+        const Moments s = moments(m, rest[0], rest[1], a.width, a.eps);
+        if (lane == 0 && a.mean != nullptr) a.mean[row] = s.mean;
+        if (lane == 0 && a.rstd != nullptr) a.rstd[row] = s.rstd;
+        T *to = static_cast<T *>(a.out) + row * a.ld_out;
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+            if (at >= a.width) break;
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[k][i] = fmaf((x[k][i] - s.rest) * s.rstd, w[k][i], b[k][i]);
+            store_pack<N>(to + at, a.width - at, x[k]);
+        }
+    }
+}
+
+// Rows too long for registers, one workgroup each, read three times.
+constexpr int kLong = 1024;
+
+template <typename T, typename F>
+__global__ __launch_bounds__(kLong) void norm_forward_long_kernel(const Norm a) {
+    constexpr int N = kRowPack<T>;
+    __shared__ float s_sum[kLong / kWave][1], s_squares[kLong / kWave][2];
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *from = static_cast<const T *>(a.x) + row * a.ld_x;
+        float sum[1] = {0.0f}, rest[2] = {0.0f, 0.0f};
+        for (int at = threadIdx.x * N; at < a.width; at += kLong * N) {
+            float x[N];
+            load_pack<N>(from + at, a.width - at, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[0] += x[i];
+        }
+        row_sums<kLong>(sum, s_sum);
+        const float m = sum[0] / float(a.width);
+        for (int at = threadIdx.x * N; at < a.width; at += kLong * N) {
+            float x[N];
+            load_pack<N>(from + at, a.width - at, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float c = at + i < a.width ? x[i] - m : 0.0f;
+                rest[0] += c;
+                rest[1] = fmaf(c, c, rest[1]);
+            }
+        }
+        row_sums<kLong>(rest, s_squares);
+        const Moments s = moments(m, rest[0], rest[1], a.width, a.eps);
+        if (threadIdx.x == 0 && a.mean != nullptr) a.mean[row] = s.mean;
+        if (threadIdx.x == 0 && a.rstd != nullptr) a.rstd[row] = s.rstd;
+        T *to = static_cast<T *>(a.out) + row * a.ld_out;
+        for (int at = threadIdx.x * N; at < a.width; at += kLong * N) {
+            float x[N], w[N], b[N];
+            load_pack<N>(from + at, a.width - at, x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = 1.0f, b[i] = 0.0f;
+            if (a.weight != nullptr) load_pack<N>(static_cast<const F *>(a.weight) + at, a.width - at, w);
+            if (a.bias != nullptr) load_pack<N>(static_cast<const F *>(a.bias) + at, a.width - at, b);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - m - s.rest) * s.rstd, w[i], b[i]);
+            store_pack<N>(to + at, a.width - at, x);
+        }
+    }
+}
+
+// What a row's gradient needs of its sums: dx = rstd g - even - slope (x - mean - rest).
+struct Slopes {
+    float rest, even, slope;
+};
+
+// From the sums of x - mean, of g and of g (x - mean).
+__device__ __forceinline__ Slopes slopes(const float (&s)[3], float rstd, int width) {
+    const float n = float(width), rest = s[0] / n, along = (s[2] - rest * s[1]) * rstd;
+    return Slopes{rest, rstd * (s[1] / n), rstd * rstd * (along / n)};
+}
+
+template <typename T, typename F, int kThreads, int kPacks, int kSize>
+__global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
+    constexpr int N = kRowPack<T>, kGroups = kSize / kThreads;
+    __shared__ float s_sums[2][kSize / kWave][3];
+    __shared__ float s_join[kGroups > 1 ? (kGroups - 1) * kThreads * N : 1];
+    const int lane = threadIdx.x % kThreads, group = threadIdx.x / kThreads;
+    float w[kPacks][N], dw[kPacks][N], db[kPacks][N];
+    load_columns<F, N, kPacks, kThreads>(a.weight, a.width, 1.0f, w);
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) dw[k][i] = db[k][i] = 0.0f;
+    int turn = 0;
+    for (int64_t first = int64_t(blockIdx.x) * kGroups; first < a.rows; first += int64_t(gridDim.x) * kGroups) {
+        const int64_t row = first + group;
+        const bool there = row < a.rows;   // (all groups meet at the barrier)
+        const float mean = there ? a.mean[row] : 0.0f, rstd = there ? a.rstd[row] : 0.0f;
+        float x[kPacks][N], dy[kPacks][N];
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[k][i] = dy[k][i] = 0.0f;
+            if (there && at < a.width) {
+                load_pack<N>(static_cast<const T *>(a.x) + row * a.ld_x + at, a.width - at, x[k]);
+                load_pack<N>(static_cast<const T *>(a.dy) + row * a.ld_dy + at, a.width - at, dy[k]);
+            }
+        }
+        float s[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[k][i] = at + i < a.width ? x[k][i] - mean : 0.0f;
+                db[k][i] += dy[k][i];
+                const float g = dy[k][i] * w[k][i];
+                s[0] += x[k][i];
+                s[1] += g;
+                s[2] = fmaf(g, x[k][i], s[2]);
+            }
+        }
+        row_sums<kThreads>(s, s_sums[turn]);
+        turn ^= 1;
+        const Slopes p = slopes(s, rstd, a.width);
+        T *to = static_cast<T *>(a.out) + row * a.ld_out;
+#pragma unroll
+        for (int k = 0; k < kPacks; ++k) {
+            const int at = (k * kThreads + lane) * N;
+            float dx[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float c = x[k][i] - p.rest;
+                dw[k][i] = fmaf(dy[k][i], c * rstd, dw[k][i]);
+                dx[i] = fmaf(rstd, dy[k][i] * w[k][i], -p.even) - p.slope * c;
+            }
+            if (there && at < a.width) store_pack<N>(to + at, a.width - at, dx);
+        }
+    }
+    if (a.partial == nullptr) return;
+    // the groups' sums in order, then this workgroup's to the workspace
+    float *to = a.partial + int64_t(blockIdx.x) * 2 * a.width;
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+        const int at = (k * kThreads + lane) * N;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = which == 0 ? dw[k][i] : db[k][i];
+            if (kGroups > 1) {
+                __syncthreads();
+                if (group > 0)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s_join[((group - 1) * N + i) * kThreads + lane] = v[i];
+                __syncthreads();
+                if (group == 0)
+                    for (int o = 0; o < kGroups - 1; ++o)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) v[i] += s_join[(o * N + i) * kThreads + lane];
+            }
+            if (group == 0 && at < a.width) store_pack<N>(to + which * int64_t(a.width) + at, a.width - at, v);
+        }
+    }
+}
+
+// Long rows: their sums first, a workgroup a row ...
+template <typename T, typename F>
+__global__ __launch_bounds__(kLong) void norm_sums_kernel(const Norm a) {
+    constexpr int N = kRowPack<T>;
+    __shared__ float s_sums[2][kLong / kWave][3];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const float mean = a.mean[row];
+        float s[3] = {0.0f, 0.0f, 0.0f};
+        for (int at = threadIdx.x * N; at < a.width; at += kLong * N) {
+            float x[N], dy[N], w[N];
+            load_pack<N>(static_cast<const T *>(a.x) + row * a.ld_x + at, a.width - at, x);
+            load_pack<N>(static_cast<const T *>(a.dy) + row * a.ld_dy + at, a.width - at, dy);
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = 1.0f;
+            if (a.weight != nullptr) load_pack<N>(static_cast<const F *>(a.weight) + at, a.width - at, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float c = at + i < a.width ? x[i] - mean : 0.0f, g = dy[i] * w[i];
+                s[0] += c;
+                s[1] += g;
+                s[2] = fmaf(g, c, s[2]);
+            }
+        }
+        row_sums<kLong>(s, s_sums[turn]);
+        turn ^= 1;
+        if (threadIdx.x < 3) a.sums[row * 4 + threadIdx.x] = s[threadIdx.x];
+    }
+}
+
+// ... then columns of some rows, each thread the same ones.
+template <typename T, typename F>
+__global__ __launch_bounds__(kBlock) void norm_backward_long_kernel(const Norm a, int32_t rows_each) {
+    constexpr int N = kRowPack<T>;
+    const int at = (blockIdx.x * kBlock + threadIdx.x) * N;
+    if (at >= a.width) return;
+    float w[N], dw[N], db[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = 1.0f, dw[i] = db[i] = 0.0f;
+    if (a.weight != nullptr) load_pack<N>(static_cast<const F *>(a.weight) + at, a.width - at, w);
+    const int64_t lo = int64_t(blockIdx.y) * rows_each, hi = min(lo + rows_each, int64_t(a.rows));
+    for (int64_t row = lo; row < hi; ++row) {
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        const float s[3] = {a.sums[row * 4], a.sums[row * 4 + 1], a.sums[row * 4 + 2]};
+        const Slopes p = slopes(s, rstd, a.width);
+        float x[N], dy[N], dx[N];
+        load_pack<N>(static_cast<const T *>(a.x) + row * a.ld_x + at, a.width - at, x);
+        load_pack<N>(static_cast<const T *>(a.dy) + row * a.ld_dy + at, a.width - at, dy);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float c = x[i] - mean - p.rest;
+            db[i] += dy[i];
+            dw[i] = fmaf(dy[i], c * rstd, dw[i]);
+            dx[i] = fmaf(rstd, dy[i] * w[i], -p.even) - p.slope * c;
+        }
+        store_pack<N>(static_cast<T *>(a.out) + row * a.ld_out + at, a.width - at, dx);
+    }
+    if (a.partial == nullptr) return;
+    float *to = a.partial + int64_t(blockIdx.y) * 2 * a.width + at;
+    store_pack<N>(to, a.width - at, dw);
+    store_pack<N>(to + a.width, a.width - at, db);
+}
+
+// dw and db: the workgroups' sums in order, each wave a run of them.
+constexpr int kJoin = 1024, kJoinWaves = kJoin / kWave;
+
+template <typename F>
+__global__ __launch_bounds__(kJoin) void norm_join_kernel(const float *__restrict__ partial, int32_t parts, int32_t width,
+                                                          F *dweight, F *dbias) {
+    __shared__ float s_sum[kJoinWaves][kWave];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t column = int64_t(blockIdx.x) * kWave + lane, columns = 2 * int64_t(width);
+    const int each = (parts + kJoinWaves - 1) / kJoinWaves, lo = min(wave * each, parts), hi = min(lo + each, parts);
+    float sum = 0.0f;
+    if (column < columns) {
+#pragma unroll 8
+        for (int p = lo; p < hi; ++p) sum += partial[p * columns + column];
+    }
+    s_sum[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && column < columns) {
+#pragma unroll
+        for (int w = 1; w < kJoinWaves; ++w) sum += s_sum[w][lane];
+        if (column < width) {
+            if (dweight != nullptr) dweight[column] = F(sum);
+        } else if (dbias != nullptr) {
+            dbias[column - width] = F(sum);
+        }
+    }
+}
+
+// How a row is held: threads and packs of each.
+struct Hold {
+    int threads, packs;   // 0: too long for registers
+};
+
+constexpr int kMaxHeld = 16384;   // elements of a row; beyond them, the registers of 1,024 threads
+
+Hold hold_of(int32_t width, int pack) {
+    const int packs = (width + pack - 1) / pack;
+    if (width > kMaxHeld) return Hold{0, 0};
+    for (int threads = kWave; threads <= kLong; threads *= 4)
+        for (int k = 1; k <= 4; k *= 2)
+            if (packs <= threads * k) return Hold{threads, k};
+    return Hold{0, 0};
+}
+
+// Workgroups of the backward pass, whose partial sums the workspace holds: one
+// for each row held by one, no more than some a compute unit.
+constexpr int kBackwardGroups = 512;
+
+int backward_groups(int32_t rows, int32_t width, int pack) {
+    const Hold h = hold_of(width, pack);
+    const int64_t each = h.threads == 0 ? 8 : h.threads < kBlock ? kBlock / h.threads : 1;
+    const int64_t groups = (rows + each - 1) / each;
+    return int(groups < kBackwardGroups ? groups : kBackwardGroups);
+}
+
+template <typename T, typename F, int kThreads, int kPacks>
+void forward(const Norm &a, hipStream_t stream) {
+    constexpr int kSize = kThreads < kBlock ? kBlock : kThreads, kGroups = kSize / kThreads;
+    const int64_t groups = (int64_t(a.rows) + kGroups - 1) / kGroups, most = int64_t(device_cu_count()) * (2048 / kSize);
+    norm_forward_kernel<T, F, kThreads, kPacks><<<uint32_t(groups < most ? groups : most), kSize, 0, stream>>>(a);
+}
+
+template <typename T, typename F, int kThreads, int kPacks>
+void backward(const Norm &a, int groups, hipStream_t stream) {
+    norm_backward_kernel<T, F, kThreads, kPacks, (kThreads < kBlock ? kBlock : kThreads)>
+        <<<groups, kThreads < kBlock ? kBlock : kThreads, 0, stream>>>(a);
+}
+
+template <typename T, typename F>
+hipError_t run_forward(const Norm &a, hipStream_t stream) {
+    const Hold h = hold_of(a.width, kRowPack<T>);
+    switch (h.threads * 8 + h.packs) {
+        case 64 * 8 + 1: forward<T, F, 64, 1>(a, stream); break;
+        case 64 * 8 + 2: forward<T, F, 64, 2>(a, stream); break;
+        case 64 * 8 + 4: forward<T, F, 64, 4>(a, stream); break;
+        case 256 * 8 + 2: forward<T, F, 256, 2>(a, stream); break;
+        case 256 * 8 + 4: forward<T, F, 256, 4>(a, stream); break;
+        case 1024 * 8 + 2: forward<T, F, 1024, 2>(a, stream); break;
+        case 1024 * 8 + 4:   // (bf16's rows of that length end in registers of two packs)
+            if constexpr (sizeof(T) == 4) forward<T, F, 1024, 4>(a, stream);
+            break;
+        default: {
+            const int64_t most = int64_t(device_cu_count()) * 2;
+            norm_forward_long_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
+        }
+    }
+    return hipGetLastError();
+}
+
+template <typename T, typename F>
+hipError_t run_backward(const Norm &a, F *dweight, F *dbias, hipStream_t stream) {
+    const Hold h = hold_of(a.width, kRowPack<T>);
+    const int groups = backward_groups(a.rows, a.width, kRowPack<T>);
+    int parts = groups;
+    if (a.rows > 0) switch (h.threads * 8 + h.packs) {
+        case 64 * 8 + 1: backward<T, F, 64, 1>(a, groups, stream); break;
+        case 64 * 8 + 2: backward<T, F, 64, 2>(a, groups, stream); break;
+        case 64 * 8 + 4: backward<T, F, 64, 4>(a, groups, stream); break;
+        case 256 * 8 + 2: backward<T, F, 256, 2>(a, groups, stream); break;
+        case 256 * 8 + 4: backward<T, F, 256, 4>(a, groups, stream); break;
+        case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, groups, stream); break;
+        case 1024 * 8 + 4:
+            if constexpr (sizeof(T) == 4) backward<T, F, 1024, 4>(a, groups, stream);
+            break;
+        default: {
+            const int64_t most = int64_t(device_cu_count()) * 2;
+            norm_sums_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
+            const int each = (a.rows + groups - 1) / groups;
+            parts = (a.rows + each - 1) / each;
+            const int across = (a.width + kBlock * kRowPack<T> - 1) / (kBlock * kRowPack<T>);
+            norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, each);
+        }
+    }
+    if (a.partial != nullptr)
+        norm_join_kernel<F><<<uint32_t((2 * int64_t(a.width) + kWave - 1) / kWave), kJoin, 0, stream>>>(
+            a.partial, parts, a.width, dweight, dbias);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_layernorm_forward(const void *x, int64_t ld_x, const void *weight, const void *bias, void *y,
+                                    int64_t ld_y, bool bf16, bool weight_bf16, int32_t rows, int32_t width, float eps,
+                                    float *mean, float *rstd, hipStream_t stream) {
+    Norm a{};
+    a.x = x, a.weight = weight, a.bias = bias, a.out = y, a.mean = mean, a.rstd = rstd;
+    a.ld_x = ld_x, a.ld_out = ld_y, a.rows = rows, a.width = width, a.eps = eps;
+    if (bf16 && weight_bf16) return run_forward<__bf16, __bf16>(a, stream);
+    if (bf16) return run_forward<__bf16, float>(a, stream);
+    if (weight_bf16) return run_forward<float, __bf16>(a, stream);
+    return run_forward<float, float>(a, stream);
+}
+
+// [partial sums of dw and db][sums of long rows], for either type of x
+size_t layernorm_workspace_size(int32_t rows, int32_t width) {
+    const int wide = backward_groups(rows, width, 4), narrow = backward_groups(rows, width, 8);
+    const size_t groups = size_t(wide > narrow ? wide : narrow);
+    return 16 + groups * 2 * size_t(width) * sizeof(float) + (width > kMaxHeld ? size_t(rows) * 4 * sizeof(float) : 0);
+}
+
+hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean,
+                                     const float *rstd, const void *dy, int64_t ld_dy, void *dx, int64_t ld_dx, bool bf16,
+                                     bool weight_bf16, int32_t rows, int32_t width, void *dweight, void *dbias,
+                                     void *workspace, hipStream_t stream) {
+    Norm a{};
+    a.x = x, a.weight = weight, a.dy = dy, a.out = dx;
+    a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
+    a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx, a.rows = rows, a.width = width;
+    a.sums = static_cast<float *>(workspace);
+    const bool long_rows = width > kMaxHeld;
+    if (dweight != nullptr || dbias != nullptr)
+        a.partial = static_cast<float *>(workspace) + (long_rows ? int64_t(rows) * 4 : 0);
+    if (bf16 && weight_bf16)
+        return run_backward<__bf16, __bf16>(a, static_cast<__bf16 *>(dweight), static_cast<__bf16 *>(dbias), stream);
+    if (bf16) return run_backward<__bf16, float>(a, static_cast<float *>(dweight), static_cast<float *>(dbias), stream);
+    if (weight_bf16)
+        return run_backward<float, __bf16>(a, static_cast<__bf16 *>(dweight), static_cast<__bf16 *>(dbias), stream);
+    return run_backward<float, float>(a, static_cast<float *>(dweight), static_cast<float *>(dbias), stream);
+}
+
+}  // namespace efs

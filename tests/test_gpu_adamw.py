@@ -1,0 +1,220 @@
+"""AdamW over lists of tensors, with states in 32 and in 8 bits, against the step
+done one rounded operation at a time, bit for bit."""
+import numpy as np
+import pytest
+
+from tests import _step
+from tests._checks import assert_bits_equal
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2108_00951_amd import binding as efs  # noqa: E402
+
+DEV = "cuda"
+SIZES = [1, 3, 255, 256, 257, 4095, 4096, 4097, 10007, 0, 64]
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+class Model:
+    """Tensors on the device and the same ones on the host."""
+
+    def __init__(self, sizes, bits=32, grad=torch.float32, copy=False, offset=0, seed=0):
+        self.rng, self.bits, self.grad, self.offset = np.random.default_rng(seed), bits, grad, offset
+        self.sizes = sizes
+        self.x = [self.rng.standard_normal(n).astype(np.float32) for n in sizes]
+        self.m = [np.zeros(n, np.float32) for n in sizes]
+        self.v = [np.zeros(n, np.float32) for n in sizes]
+        self.dx = [self.device(v) for v in self.x]
+        if bits == 8:
+            self.dm, self.dv = efs.new_adamw_state(sizes, DEV)
+        else:
+            self.dm, self.dv = ([self.device(v) for v in vs] for vs in (self.m, self.v))
+        self.copy = [torch.full((n,), 7.0, dtype=torch.bfloat16, device=DEV) for n in sizes] if copy else None
+
+    def device(self, v, dtype=torch.float32):
+        """A view `offset` elements off its allocation's alignment."""
+        t = torch.zeros(v.size + self.offset, dtype=dtype, device=DEV)[self.offset:]
+        t.copy_(torch.from_numpy(v))
+        return t
+
+    def gradients(self, scale=1e-3):
+        g = [torch.from_numpy((self.rng.standard_normal(n) * np.exp(2 * self.rng.standard_normal(n)) * scale).astype(np.float32))
+             .to(self.grad) for n in self.sizes]
+        return [v.float().numpy() for v in g], [self.device(v.float().numpy(), self.grad) for v in g]
+
+    def states(self):
+        if self.bits == 32:
+            return [t.cpu().numpy() for t in self.dm], [t.cpu().numpy() for t in self.dv]
+        m, v = ([torch.full((n,), 7.0, device=DEV) for n in self.sizes] for _ in range(2))
+        efs.adamw_read_state(self.dm, self.dv, m, v)
+        return [t.cpu().numpy() for t in m], [t.cpu().numpy() for t in v]
+
+    def expect(self, plain, t, g, decays, **kw):
+        for i in range(len(self.sizes)):
+            self.x[i], self.m[i], self.v[i] = plain.step(t, i, g[i], self.x[i], self.m[i], self.v[i], decays[i], **kw)
+
+    def check(self, what):
+        m, v = self.states()
+        for i, n in enumerate(self.sizes):
+            # (values: a state of 8 bits has one zero)
+            np.testing.assert_array_equal(m[i], self.m[i], "%s m[%d] of %d" % (what, i, n))
+            np.testing.assert_array_equal(v[i], self.v[i], "%s v[%d] of %d" % (what, i, n))
+            assert_bits_equal(self.dx[i].cpu().numpy(), self.x[i], "%s x[%d] of %d" % (what, i, n))
+            if self.copy is not None:
+                assert torch.equal(self.copy[i].cpu(), torch.from_numpy(self.x[i]).to(torch.bfloat16))
+
+
+def decays_of(sizes):
+    return [0.1 * (i % 3) for i in range(len(sizes))]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("copy, offset", [(False, 0), (True, 0), (True, 1)])
+def test_steps(bits, grad, copy, offset):
+    say("adamw", bits, grad, copy, offset)
+    model = Model(SIZES, bits, grad, copy, offset)
+    plain = _step.Adamw(3e-3, 0.9, 0.99, 1e-8, seed=77, bits=bits)
+    for t in range(1, 6):
+        g, dg = model.gradients()
+        efs.adamw_apply(dg, model.dx, model.dm, model.dv, t, lr=3e-3, beta1=0.9, beta2=0.99, eps=1e-8,
+                        weight_decay=decays_of(SIZES), copy=model.copy, seed=77)
+        model.expect(plain, t, g, decays_of(SIZES))
+        model.check("step %d" % t)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_tensors_than_a_launch_takes(bits):
+    sizes = [1 + (i * 37) % 300 for i in range(200)] + [0, 5000]
+    model = Model(sizes, bits)
+    plain = _step.Adamw(1e-2, bits=bits)
+    for t in (1, 1000):
+        g, dg = model.gradients()
+        efs.adamw_apply(dg, model.dx, model.dm, model.dv, t, lr=1e-2, weight_decay=0.3)
+        model.expect(plain, t, g, [0.3] * len(sizes))
+        model.check("step %d" % t)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_layers_of_flat_vectors(bits):
+    """Neighbouring views, any of which is off 16 bytes, are tensors like others."""
+    sizes = [5, 1000, 3, 257, 4099]
+    model = Model(sizes, bits)
+    d = sum(sizes)
+    x = torch.from_numpy(np.concatenate(model.x)).to(DEV)
+    model.dx = list(torch.split(x, sizes))
+    if bits == 32:
+        model.dm, model.dv = (list(torch.split(torch.zeros(d, device=DEV), sizes)) for _ in range(2))
+    plain = _step.Adamw(1e-2, bits=bits)
+    g, _ = model.gradients()
+    dg = torch.split(torch.from_numpy(np.concatenate(g)).to(DEV), sizes)
+    efs.adamw_apply(dg, model.dx, model.dm, model.dv, 3, lr=1e-2, weight_decay=0.0)
+    model.expect(plain, 3, g, [0.0] * len(sizes))
+    model.check("flat")
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("given", ["step", "factors", "both"])
+def test_rates_from_the_device(bits, given):
+    model = Model(SIZES, bits)
+    plain = _step.Adamw(3e-3, bits=bits, seed=5)
+    step = torch.zeros((), dtype=torch.int64, device=DEV)
+    factors = torch.tensor([1.0, 1.0], device=DEV) if given != "step" else None
+    call = None
+    for t in (1, 2, 7, 100000):
+        g, dg = model.gradients()
+        kw = {}
+        if factors is not None:
+            factors[0], factors[1] = 0.3 * t, 0.7
+            kw = {"lr_factor": float(factors[0]), "gain": float(factors[1])}
+        step.fill_(t)
+        call = efs.prepare_adamw_apply(dg, model.dx, model.dm, model.dv, lr=3e-3, weight_decay=0.1, factors=factors, seed=5)
+        call(t if given == "factors" else step)
+        model.expect(plain, t, g, [0.1] * len(SIZES), **kw)
+        model.check("step %d" % t)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_special_gradients_spoil_their_element_alone(bits, bad):
+    model = Model([1000], bits)
+    plain = _step.Adamw(1e-2, bits=bits)
+    for t in (1, 2):
+        g, dg = model.gradients()
+        if t == 1:
+            g[0][300] = bad
+            dg[0][300] = bad
+        efs.adamw_apply(dg, model.dx, model.dm, model.dv, t, lr=1e-2, weight_decay=0.0)
+        model.expect(plain, t, g, [0.0])
+        m, v = model.states()
+        others = np.arange(1000) != 300
+        for got, want in ((m[0], model.m[0]), (v[0], model.v[0]), (model.dx[0].cpu().numpy(), model.x[0])):
+            np.testing.assert_array_equal(got[others], want[others])
+        assert not np.isfinite(m[0][300]) and not np.isfinite(v[0][300])
+        assert np.isnan(model.dx[0][300].item())
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-14, 1e12])
+def test_states_of_8_bits_over_the_range_of_gradients(scale):
+    model = Model([3000], 8)
+    plain = _step.Adamw(1e-2, eps=1e-30, bits=8)
+    for t in (1, 2):
+        g, dg = model.gradients(scale)
+        efs.adamw_apply(dg, model.dx, model.dm, model.dv, t, lr=1e-2, eps=1e-30, weight_decay=0.0)
+        model.expect(plain, t, g, [0.0])
+        model.check("scale %g step %d" % (scale, t))
+
+
+def test_a_state_of_8_bits_decays_without_gradients():
+    """Rounded to nearest, sqrt(v) would stay where it is for good; at random it
+    falls as often as it should: 4,000 steps of sqrt(0.999) are a factor 0.135."""
+    n = 4096
+    x, g = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    m8, v8 = efs.new_adamw_state([n], DEV)
+    m, v = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    start = 1e-4 * (1.0 + torch.rand(n, device=DEV))
+    efs.adamw_write_state([m], [start.square()], m8, v8)
+    call = efs.prepare_adamw_apply([g], [x], m8, v8, lr=1e-3)
+    for t in range(1, 4001):
+        call(t)
+    efs.adamw_read_state(m8, v8, [m], [v])
+    left = float(v.sqrt().mean() / start.mean())
+    # every rounding moves a value by up to 2^-4 of it, at random: over 4,000 steps and
+    # 4,096 elements the mean's spread is below 2^-4 * sqrt(4000) / 64 = 0.06 of it
+    assert abs(left / 0.999 ** 2000 - 1.0) < 0.25
+    assert torch.all(x == 0.0)
+
+
+def test_write_and_read_state():
+    rng = np.random.default_rng(3)
+    sizes = [1, 256, 1000, 5]
+    m = [(rng.standard_normal(n) * np.exp(4 * rng.standard_normal(n))).astype(np.float32) for n in sizes]
+    v = [np.square(rng.standard_normal(n) * np.exp(4 * rng.standard_normal(n))).astype(np.float32) for n in sizes]
+    m[3][:] = 0.0
+    v[3][:] = 0.0
+    m8, v8 = efs.new_adamw_state(sizes, DEV)
+    efs.adamw_write_state([torch.from_numpy(t).to(DEV) for t in m], [torch.from_numpy(t).to(DEV) for t in v], m8, v8)
+    gm, gv = ([torch.empty(n, device=DEV) for n in sizes] for _ in range(2))
+    efs.adamw_read_state(m8, v8, gm, gv)
+    for i in range(len(sizes)):
+        want_m = np.copysign(_step.in_8_bits(np.abs(m[i]), 3, 0, np.float32(0.5)), m[i])
+        want_r = _step.in_8_bits(np.sqrt(v[i]), 4, 1, np.float32(0.5))
+        np.testing.assert_array_equal(gm[i].cpu().numpy(), want_m)
+        np.testing.assert_array_equal(gv[i].cpu().numpy(), want_r * want_r)
+        # half a step of 3 and of 4 bits, or of the smallest values' steps
+        top_m, top_r = np.abs(m[i]).max(), np.sqrt(v[i]).max()
+        assert np.all(np.abs(want_m - m[i]) <= np.maximum(2.0 ** -4 * np.abs(m[i]), 2.0 ** -17 * top_m))
+        assert np.all(np.abs(want_r - np.sqrt(v[i])) <= np.maximum(2.0 ** -5 * np.sqrt(v[i]), 2.0 ** -17 * top_r) + 1e-30)
+
+
+def test_empty_lists_do_nothing():
+    efs.adamw_apply([], [], [], [], 1, lr=1e-3)
+    none = torch.empty(0, device=DEV)
+    efs.adamw_apply([none], [none], [none], [none], 1, lr=1e-3)
+    m8, v8 = efs.new_adamw_state([0], DEV)
+    efs.adamw_apply([none], [none], m8, v8, 1, lr=1e-3)
+    efs.adamw_read_state(m8, v8, [none], [none.clone()])
