@@ -763,7 +763,7 @@ size_t embed_workspace_bytes(int32_t tokens, int32_t vocab, int32_t width) {
     if (tokens < 0 || tokens > efs::kEmbedMaxTokens || vocab < 1 || vocab > efs::kEmbedMaxVocab || width < 1 ||
         width > efs::kEmbedMaxWidth || int64_t(tokens) * vocab > int64_t(1) << 38)
         return 0;
-    return efs::embed_workspace_size(tokens, width);
+    return efs::embed_workspace_size(tokens, vocab, width);
 }
 
 efs_status embed_backward(const void *dout, int64_t ld_dout, int dtype, const int64_t *ids, void *dtable,

@@ -86,76 +86,110 @@ __device__ __forceinline__ uint32_t mixed(uint32_t z) {
     return z ^ (z >> 16);
 }
 
-// kMantissa bits below the leading one, 4 of exponent.
-template <int kMantissa>
-__device__ __forceinline__ uint32_t encode(float y, uint32_t dither) {   // 0 <= y < 2^8, dither of 16 bits
-    const uint32_t normal = ((__float_as_uint(y) + (dither << (7 - kMantissa))) >> (23 - kMantissa)) - (120u << kMantissa);
-    const float low = 0x1p6f * float(1 << kMantissa);
-    const uint32_t small = uint32_t(__fadd_rn(__fmul_rn(y, low), __fmul_rn(float(dither), 0x1p-16f)));
-    return y < 0x1p-6f ? small : normal;
-}
-
-template <int kMantissa>
-__device__ __forceinline__ float decode(uint32_t code) {
-    const float normal = __uint_as_float((code + (120u << kMantissa)) << (23 - kMantissa));
-    const float small = float(code) * (0x1p-6f / float(1 << kMantissa));
-    return code < (1u << kMantissa) ? small : normal;
-}
-
+constexpr uint32_t kInfinity = 0x7f800000u, kMagnitude = 0x7fffffffu;
 constexpr uint32_t kNanM = 0x7fu, kNanR = 0xffu;
 
-// The exponent of a block's scale from its largest finite magnitude; those below
-// 2^-95 are small beside the scale.
-__device__ __forceinline__ int scale_exponent(float largest) {
-    const int e = int(__float_as_uint(largest) >> 23) - 127;
-    return e < -95 ? -95 : e;
+// The code of a magnitude, of kMantissa bits below the leading one and 4 of
+// exponent, rounded up with the share `dither` / 2^16; e: the block's exponent,
+// magnitudes are below 2^(e + 1).  In full: fp32's own bits, moved and cut ...
+template <int kMantissa>
+__device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t dither, int e) {
+    return (bits + (dither << (7 - kMantissa)) - (uint32_t(113 + e) << 23)) >> (23 - kMantissa);
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off));
-    return v;
-}
+// ... and below 2^-6 of the scale in steps of its last bit there.
+__device__ __forceinline__ uint32_t least_in_full(int e) { return uint32_t(114 + e) << 23; }
 
-__device__ __forceinline__ float finite_or_zero(float v) { return fabsf(v) < INFINITY ? v : 0.0f; }
+template <int kMantissa>
+__device__ __forceinline__ uint32_t encode_small(float y, uint32_t dither, float up) {
+    return uint32_t(__fadd_rn(__fmul_rn(__fmul_rn(y, up), 0x1p6f * float(1 << kMantissa)), __fmul_rn(float(dither), 0x1p-16f)));
+}
 
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }
 
-// One lane's four elements of a block: its m and r >= 0 into codes; the block's scales.
+// The exponent of a block's scale from its largest finite magnitude; those below
+// 2^-95 are small beside the scale.
+__device__ __forceinline__ int scale_exponent(uint32_t largest) { return max(int(largest >> 23) - 127, -95); }
+
+// The largest finite magnitude of a block.
+__device__ __forceinline__ uint32_t top_of(const uint32_t (&bits)[4], bool &whole) {
+    uint32_t top = wave_max(max(max(bits[0], bits[1]), max(bits[2], bits[3])));
+    whole = top < kInfinity;
+    if (!whole) {   // (the same for the wave)
+        top = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = max(top, bits[i] < kInfinity ? bits[i] : 0u);
+        top = wave_max(top);
+    }
+    return top;
+}
+
+// One lane's four elements of a block: its m and r >= 0 into codes; the block's
+// scales.  What few blocks have (NaN, infinities, values that are small beside the
+// scale) is left to branches that the whole wave takes or not.
 __device__ __forceinline__ void pack_block(const float (&m)[4], const float (&r)[4], const uint32_t (&random)[4],
                                            uint32_t &m_codes, uint32_t &r_codes, float &m_scale, float &r_scale) {
-    float top_m = 0.0f, top_r = 0.0f;
+    uint32_t mb[4], rb[4], c[4], d[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mb[i] = __float_as_uint(m[i]) & kMagnitude, rb[i] = __float_as_uint(r[i]);
+    bool whole_m, whole_r;
+    const int em = scale_exponent(top_of(mb, whole_m)), er = scale_exponent(top_of(rb, whole_r));
+    m_scale = two_to(em - 7), r_scale = two_to(er - 7);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        top_m = fmaxf(top_m, fabsf(finite_or_zero(m[i])));
-        top_r = fmaxf(top_r, finite_or_zero(r[i]));
+        c[i] = encode<3>(mb[i], random[i] & 0xffffu, em);
+        d[i] = encode<4>(rb[i], random[i] >> 16, er);
     }
-    const int em = scale_exponent(wave_max(top_m)), er = scale_exponent(wave_max(top_r));
-    const float up_m = two_to(7 - em), up_r = two_to(7 - er);
-    m_scale = two_to(em - 7), r_scale = two_to(er - 7);
+    const uint32_t least_m = least_in_full(em), least_r = least_in_full(er);
+    if (__any(min(min(mb[0], mb[1]), min(mb[2], mb[3])) < least_m)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t small = encode_small<3>(fabsf(m[i]), random[i] & 0xffffu, two_to(7 - em));
+            c[i] = mb[i] < least_m ? small : c[i];
+        }
+    }
+    if (__any(min(min(rb[0], rb[1]), min(rb[2], rb[3])) < least_r)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t small = max(encode_small<4>(r[i], random[i] >> 16, two_to(7 - er)), rb[i] != 0u ? 1u : 0u);
+            d[i] = rb[i] < least_r ? small : d[i];
+        }
+    }
+    if (!whole_m || !whole_r) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = mb[i] < kInfinity ? c[i] : kNanM;
+            d[i] = rb[i] < kInfinity ? d[i] : kNanR;
+        }
+    }
     m_codes = r_codes = 0u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t c = encode<3>(__fmul_rn(fabsf(m[i]), up_m), random[i] & 0xffffu);
-        if (!(fabsf(m[i]) < INFINITY)) c = kNanM;
-        c |= (__float_as_uint(m[i]) >> 24) & 0x80u;
-        uint32_t d = encode<4>(__fmul_rn(r[i], up_r), random[i] >> 16);
-        if (r[i] > 0.0f && d == 0u) d = 1u;
-        if (!(r[i] < INFINITY)) d = kNanR;
-        m_codes |= c << (8 * i);
-        r_codes |= d << (8 * i);
+        m_codes |= (c[i] | ((__float_as_uint(m[i]) >> 24) & 0x80u)) << (8 * i);
+        r_codes |= d[i] << (8 * i);
     }
 }
 
-__device__ __forceinline__ float value_of_m(uint32_t codes, int i, float scale) {
-    const uint32_t c = (codes >> (8 * i)) & 0xffu;
-    const float v = (c & 0x7fu) == kNanM ? NAN : __fmul_rn(decode<3>(c & 0x7fu), scale);
-    return c & 0x80u ? -v : v;
+// The values of a lane's four codes.  Those of m are the 8-bit floats of 4 and 3
+// bits that the hardware knows.
+__device__ __forceinline__ void values_of_m(uint32_t codes, float scale, float (&m)[4]) {
+    m[0] = __builtin_amdgcn_cvt_f32_fp8(int(codes), 0);
+    m[1] = __builtin_amdgcn_cvt_f32_fp8(int(codes), 1);
+    m[2] = __builtin_amdgcn_cvt_f32_fp8(int(codes), 2);
+    m[3] = __builtin_amdgcn_cvt_f32_fp8(int(codes), 3);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = __fmul_rn(m[i], scale);
 }
 
-__device__ __forceinline__ float value_of_r(uint32_t codes, int i, float scale) {
-    const uint32_t c = (codes >> (8 * i)) & 0xffu;
-    return c == kNanR ? NAN : __fmul_rn(decode<4>(c), scale);
+// Those of r as fp32's own exponent and mantissa bits, 2^120 too small; there also
+// the small ones are right, as subnormals.
+__device__ __forceinline__ void values_of_r(uint32_t codes, float scale, float (&r)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t bits = (i < 3 ? codes << (19 - 8 * i) : codes >> 5) & (0xffu << 19);
+        const float v = __fmul_rn(__uint_as_float(bits), 0x1p120f);
+        r[i] = __fmul_rn(v > 256.0f ? NAN : v, scale);   // (kNanR; no other code is above 256)
+    }
 }
 
 // The step of one element; returns the new x.
@@ -199,14 +233,10 @@ __global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
         if (kBytes && block < blocks) {
             const uint8_t *m8 = static_cast<const uint8_t *>(t.m), *r8 = static_cast<const uint8_t *>(t.v);
             const uint32_t mc = *reinterpret_cast<const uint32_t *>(m8 + at), rc = *reinterpret_cast<const uint32_t *>(r8 + at);
-            const float ms = reinterpret_cast<const float *>(m8 + int64_t(blocks) * kStateBlock)[block];
-            const float rs = reinterpret_cast<const float *>(r8 + int64_t(blocks) * kStateBlock)[block];
+            values_of_m(mc, reinterpret_cast<const float *>(m8 + int64_t(blocks) * kStateBlock)[block], mv[k]);
+            values_of_r(rc, reinterpret_cast<const float *>(r8 + int64_t(blocks) * kStateBlock)[block], vv[k]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                mv[k][i] = value_of_m(mc, i, ms);
-                const float r = value_of_r(rc, i, rs);
-                vv[k][i] = __fmul_rn(r, r);
-            }
+            for (int i = 0; i < 4; ++i) vv[k][i] = __fmul_rn(vv[k][i], vv[k][i]);
         }
         if (left[k] > 0) {
             load_pack<4>(g + at, left[k], gv[k]);
@@ -317,14 +347,11 @@ __global__ __launch_bounds__(kBlock) void adamw_state_kernel(const States a) {
             if (lane == 0) m_scale[block] = ms, r_scale[block] = rs;
         } else if (left > 0) {
             const uint32_t mc = *reinterpret_cast<const uint32_t *>(m8 + at), rc = *reinterpret_cast<const uint32_t *>(r8 + at);
-            const float ms = m_scale[block], rs = r_scale[block];
             float m[4], v[4];
+            values_of_m(mc, m_scale[block], m);
+            values_of_r(rc, r_scale[block], v);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m[i] = value_of_m(mc, i, ms);
-                const float r = value_of_r(rc, i, rs);
-                v[i] = __fmul_rn(r, r);
-            }
+            for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], v[i]);
             store_pack<4>(t.m + at, left, m);
             store_pack<4>(t.v + at, left, v);
         }

@@ -6,31 +6,40 @@
 // Nothing but bytes: the rows that are looked up in, out; dout in, the table's
 // gradient out, whole, since words without a token get zeros.
 //
-// The gradient sorts the tokens by word without a pass that has to wait for
-// another: a workgroup owns some consecutive words, looks through all ids twice
-// (they stay in L2: 16,384 of them are 128 KiB) and so knows by itself how many
-// tokens the words before its own have, and which tokens, in their order, each
-// of its own has.  The same workgroup then writes its words' rows: zeros, or
-// the sum of a word's few rows.  A word of kHot tokens or more is left to two
-// more launches that cut the sorted tokens into pieces of kHot whatever their
-// words, sum each piece, and join the pieces of a word in order: no word is
-// summed by one wave, and nothing depends on which workgroup comes first.
+// The gradient of up to kFew tokens is one launch: a workgroup for each token
+// looks through all ids, ends if an earlier token has the same, and else sums the
+// rows of its word's tokens; others write the zeros of words without a token.
+//
+// More tokens are sorted by word, without a pass that has to wait for another:
+// a workgroup owns some consecutive words, looks through all ids twice (they stay
+// in L2: 16,384 of them are 128 KiB) and so knows by itself how many tokens the
+// words before its own have, and which tokens, in their order, each of its own
+// has.  A second launch writes the rows of words with fewer than kHot tokens and
+// of those without, and cuts the sorted tokens into pieces of kHot, of which it
+// sums what belongs to words of more; a third joins the pieces of a word in order.
+// So no word is summed by one wave, and nothing depends on which workgroup comes
+// first.
 #include "rows.hpp"
 #include "launch.hpp"
 
-#include <math.h>
+#include <type_traits>
 
 namespace efs {
 
 namespace {
 
-constexpr int kGradBlock = 512;
-constexpr int kGradWaves = kGradBlock / kWave;
-constexpr int kMaxWords = 1024;        // of one workgroup
+constexpr int kFew = 1024;             // tokens that need no sorting
+constexpr int kFewRounds = kFew / kBlock;
+constexpr int kFewAlone = 16;          // rows that one wave sums
+constexpr int kSortBlock = 1024;
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kMaxWords = 768;         // of one sorting workgroup: 54 KiB of LDS
 constexpr int kHot = 32;               // tokens; a lane of a half wave each
 constexpr int kAhead = 8;              // loads of a lane on their way at once
 constexpr int kJoinBlock = 512;
 constexpr int kJoinWaves = kJoinBlock / kWave;
+constexpr int64_t kFillBytes = 32768;  // of the table's rows that a workgroup writes
+constexpr int kMaxRows = 1024;         // of one such workgroup
 
 // Flags beside a sorted token.
 constexpr uint32_t kIsHot = 1u << 31, kIsFirst = 1u << 30, kTokenMask = kIsFirst - 1;
@@ -94,11 +103,13 @@ struct Spread {
     void *dtable;
     const int64_t *ids;
     int64_t ld_dout, ld_dtable, ignore;
-    int32_t tokens, vocab, width, words;   // words: of one workgroup
+    int32_t tokens, vocab, width;
+    int32_t words, rows;  // of one workgroup that sorts, that writes rows
+    int32_t first;        // workgroups before those that write rows
     float scale;
     int accumulate;
     uint32_t *status;
-    int32_t *count;       // tokens that count, all words together
+    int32_t *start;       // [vocab + 1] in the sorted list
     Sorted *list;         // [tokens]
     int32_t *lengths;     // [pieces] tokens of the word that starts in a piece
     float *partial;       // [pieces][2][width]
@@ -119,43 +130,139 @@ __device__ __forceinline__ void put_row(const Spread &a, int64_t word, int at, f
     store_pack<N>(to, a.width - at, sum);
 }
 
-// Sum of the rows of dout whose numbers are token(0..n-1), at one lane's
-// columns, in that order; kAhead loads on their way.
-template <typename T, int N, typename Token>
-__device__ __forceinline__ void sum_rows(const Spread &a, int at, int n, Token token, float (&sum)[N]) {
-    const T *rows = static_cast<const T *>(a.dout) + at;
+// Sum of the rows row(0..n-1) at one lane's columns (at < width), in that order.
+template <int N, int kLoads, typename Row>
+__device__ __forceinline__ void sum_rows(int left, int n, Row row, float (&sum)[N]) {
+    typedef typename std::remove_cv<typename std::remove_pointer<decltype(row(0))>::type>::type T;
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] = 0.0f;
-    for (int j = 0; j < n; j += kAhead) {
-        float v[kAhead][N];
+    for (int j = 0; j < n; j += kLoads) {
+        Pack<T, N> v[kLoads];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (j + k < n) load_pack<N>(rows + int64_t(token(j + k)) * a.ld_dout, a.width - at, v[k]);
+        for (int k = 0; k < kLoads; ++k)
+            if (j + k < n) v[k] = load_raw<N>(row(j + k), left);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
+        for (int k = 0; k < kLoads; ++k)
             if (j + k < n) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], v[k][i]);
+                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], float(v[k][i]));
             }
     }
 }
 
+// Zeros into the rows of [first, first + rows) that empty(r) says.
+template <typename F, typename Empty>
+__device__ __forceinline__ void clear_rows(const Spread &a, int64_t first, int rows, Empty empty) {
+    constexpr int N = 16 / sizeof(F);
+    const uint32_t packs = uint32_t(a.width + N - 1) / N;
+    const float zero[N] = {};
+    for (uint32_t u = threadIdx.x; u < uint32_t(rows) * packs; u += blockDim.x) {
+        const uint32_t r = u / packs;
+        const int at = int(u - r * packs) * N;
+        if (empty(int(r))) store_pack<N>(static_cast<F *>(a.dtable) + (first + r) * a.ld_dtable + at, a.width - at, zero);
+    }
+}
+
+__device__ __forceinline__ bool counts(const Spread &a, int64_t id) { return id != a.ignore && id >= 0 && id < a.vocab; }
+
+// Up to kFew tokens.  Workgroups below a.first: a token's word, at four waves'
+// columns; the others: rows of words without a token.
 template <typename T, typename F>
-__global__ __launch_bounds__(kGradBlock) void embed_grad_kernel(const Spread a) {
+__global__ __launch_bounds__(kBlock) void embed_few_kernel(const Spread a) {
     constexpr int N = kPack<T, F>;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (int(blockIdx.x) >= a.first) {
+        __shared__ uint8_t s_there[kMaxRows];
+        const int64_t first = int64_t(blockIdx.x - a.first) * a.rows;
+        const int rows = int(min(int64_t(a.rows), a.vocab - first));
+        for (int r = threadIdx.x; r < rows; r += kBlock) s_there[r] = 0;
+        __syncthreads();
+        for (int t = threadIdx.x; t < a.tokens; t += kBlock) {
+            const int64_t id = a.ids[t];
+            if (id != a.ignore && id >= first && id < first + rows) s_there[id - first] = 1;
+        }
+        __syncthreads();
+        clear_rows<F>(a, first, rows, [&](int r) { return s_there[r] == 0; });
+        return;
+    }
+
+    __shared__ uint64_t s_same[kFewRounds * kWaves];
+    __shared__ int32_t s_token[kFew];
+    __shared__ float s_sum[kWaves][kWave * N];
+    const int across = (a.width + kBlock * N - 1) / (kBlock * N);
+    const int token = int(blockIdx.x) / across, part0 = int(blockIdx.x) % across * kWaves;
+    const int64_t word = a.ids[token];
+    if (!counts(a, word)) {
+        if (word != a.ignore && part0 == 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
+        return;
+    }
+    // the tokens of the same word, a bit each
+    uint64_t mine[kFewRounds];
+#pragma unroll
+    for (int k = 0; k < kFewRounds; ++k) {
+        const int t = k * kBlock + threadIdx.x;
+        mine[k] = __ballot(t < a.tokens && a.ids[t] == word);
+        if (lane == 0) s_same[k * kWaves + wave] = mine[k];
+    }
+    __syncthreads();
+    int n = 0, before[kFewRounds] = {}, first = -1;
+#pragma unroll
+    for (int i = 0; i < kFewRounds * kWaves; ++i) {
+        const uint64_t same = s_same[i];
+        if (i % kWaves == wave) before[i / kWaves] = n;
+        if (same != 0 && first < 0) first = i * kWave + __ffsll((unsigned long long)same) - 1;
+        n += __popcll(same);
+    }
+    if (first != token) return;   // that one's workgroup sums them
+#pragma unroll
+    for (int k = 0; k < kFewRounds; ++k)
+        if ((mine[k] >> lane) & 1u) s_token[before[k] + int(lanes_below(mine[k]))] = k * kBlock + int(threadIdx.x);
+    __syncthreads();
+    const T *dout = static_cast<const T *>(a.dout);
+    if (n <= kFewAlone) {
+        const int at = ((part0 + wave) * kWave + lane) * N;
+        if (at >= a.width) return;
+        float sum[N];
+        sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(s_token[j]) * a.ld_dout + at; }, sum);
+        put_row<F, N>(a, word, at, sum);
+        return;
+    }
+    const int each = (n + kWaves - 1) / kWaves, lo = min(wave * each, n), hi = min(lo + each, n);
+    for (int part = part0; part < part0 + kWaves; ++part) {
+        const int at = (part * kWave + lane) * N;
+        float sum[N] = {};
+        if (at < a.width)
+            sum_rows<N, kAhead>(a.width - at, hi - lo,
+                                [&](int j) { return dout + int64_t(s_token[lo + j]) * a.ld_dout + at; }, sum);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) s_sum[wave][i * kWave + lane] = sum[i];
+        __syncthreads();
+        if (wave == 0 && at < a.width) {
+            for (int w = 1; w < kWaves; ++w)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], s_sum[w][i * kWave + lane]);
+            put_row<F, N>(a, word, at, sum);
+        }
+    }
+}
+
+// The tokens by word: the list, and where each word's start in it.
+__global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) {
     extern __shared__ uint32_t s_mem[];
-    uint32_t *s_at = s_mem;                              // [kGradWaves][words]
-    uint32_t *s_start = s_mem + kGradWaves * a.words;    // [words] in the sorted list
+    uint32_t *s_at = s_mem;                              // [kSortWaves][words]
+    uint32_t *s_start = s_mem + kSortWaves * a.words;    // [words]
     uint32_t *s_total = s_start + a.words;               // [words]
-    __shared__ uint32_t s_wave[kGradWaves];
+    __shared__ uint32_t s_wave[kSortWaves];
+    static_assert(kMaxWords <= kSortBlock, "a thread a word");
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t first = int64_t(blockIdx.x) * a.words;
     const int words = int(min(int64_t(a.words), a.vocab - first));
-    for (int i = threadIdx.x; i < kGradWaves * a.words; i += kGradBlock) s_at[i] = 0u;
+    for (int i = threadIdx.x; i < kSortWaves * a.words; i += kSortBlock) s_at[i] = 0u;
     __syncthreads();
 
     // each wave counts its share of the tokens, and all that come before this workgroup's words
-    const int share = (a.tokens + kGradBlock - 1) / kGradBlock * kWave;   // whole rounds
+    const int share = (a.tokens + kSortBlock - 1) / kSortBlock * kWave;   // whole rounds
     const int lo = min(wave * share, a.tokens), hi = min(lo + share, a.tokens);
     uint32_t before = 0;
     bool bad = false;
@@ -179,39 +286,35 @@ __global__ __launch_bounds__(kGradBlock) void embed_grad_kernel(const Spread a) 
     __syncthreads();
     uint32_t base = 0;
 #pragma unroll
-    for (int w = 0; w < kGradWaves; ++w) base += s_wave[w];
+    for (int w = 0; w < kSortWaves; ++w) base += s_wave[w];
 
-    // where each word's tokens start, and each wave's among them
-    for (int r0 = 0; r0 < words; r0 += kGradBlock) {
-        const int r = r0 + threadIdx.x;
-        uint32_t total = 0;
-        if (r < words)
-            for (int w = 0; w < kGradWaves; ++w) total += s_at[w * a.words + r];
-        uint32_t upto = total;   // inclusive, over the wave and then the workgroup
+    // where each word's tokens start, and each wave's among them (a thread a word)
+    const int r = threadIdx.x;
+    uint32_t total = 0;
+    if (r < words)
+        for (int w = 0; w < kSortWaves; ++w) total += s_at[w * a.words + r];
+    uint32_t upto = total;   // inclusive, over the wave and then the workgroup
 #pragma unroll
-        for (int off = 1; off < kWave; off <<= 1) {
-            const uint32_t left = __shfl_up(upto, off);
-            if (lane >= off) upto += left;
-        }
-        __syncthreads();
-        if (lane == kWave - 1) s_wave[wave] = upto;
-        __syncthreads();
-        uint32_t start = base + upto - total;
-        for (int w = 0; w < kGradWaves; ++w) {
-            if (w < wave) start += s_wave[w];
-            base += s_wave[w];
-        }
-        if (r < words) {
-            s_start[r] = start;
-            s_total[r] = total;
-            for (int w = 0; w < kGradWaves; ++w) {
-                const uint32_t n = s_at[w * a.words + r];
-                s_at[w * a.words + r] = start;
-                start += n;
-            }
+    for (int off = 1; off < kWave; off <<= 1) {
+        const uint32_t left = __shfl_up(upto, off);
+        if (lane >= off) upto += left;
+    }
+    __syncthreads();
+    if (lane == kWave - 1) s_wave[wave] = upto;
+    __syncthreads();
+    uint32_t start = base + upto - total;
+    for (int w = 0; w < wave; ++w) start += s_wave[w];
+    if (r < words) {
+        s_start[r] = start;
+        s_total[r] = total;
+        a.start[first + r] = int32_t(start);
+        if (first + r == a.vocab - 1) a.start[a.vocab] = int32_t(start + total);
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t n = s_at[w * a.words + r];
+            s_at[w * a.words + r] = start;
+            start += n;
         }
     }
-    if (first + words >= a.vocab && threadIdx.x == 0) *a.count = int32_t(base);
     __syncthreads();
 
     // the tokens into their places, in order: a wave takes them as they come, and
@@ -223,14 +326,14 @@ __global__ __launch_bounds__(kGradBlock) void embed_grad_kernel(const Spread a) 
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const bool in = id[k] != a.ignore && id[k] >= first && id[k] < first + words;
-            const int r = int(id[k] - first);
+            const int own = int(id[k] - first);
             uint64_t left = __ballot(in);
             while (left != 0) {
                 const int leader = __ffsll((unsigned long long)left) - 1;
-                const int word = __shfl(r, leader);
-                const uint64_t same = __ballot(in && r == word);
-                if (in && r == word) {
-                    const uint32_t start = mine[word], at = start + lanes_below(same), n = s_total[word];
+                const int word = __shfl(own, leader);
+                const uint64_t same = __ballot(in && own == word);
+                if (in && own == word) {
+                    const uint32_t from = mine[word], at = from + lanes_below(same), n = s_total[word];
                     uint32_t token = uint32_t(t + k * kWave + lane);
                     if (n >= uint32_t(kHot)) {
                         token |= kIsHot;
@@ -240,30 +343,10 @@ __global__ __launch_bounds__(kGradBlock) void embed_grad_kernel(const Spread a) 
                         }
                     }
                     a.list[at] = Sorted{token, int32_t(first) + word};
-                    if (lane == leader) mine[word] = start + uint32_t(__popcll(same));
+                    if (lane == leader) mine[word] = from + uint32_t(__popcll(same));
                 }
                 left &= ~same;
             }
-        }
-    }
-    __syncthreads();
-
-    // the rows: a wave takes a word's 64 packs of columns
-    const int parts = (a.width + kWave * N - 1) / (kWave * N);
-    for (int u = wave; u < words * parts; u += kGradWaves) {
-        const int r = u / parts, at = (u % parts * kWave + lane) * N;
-        const int n = int(s_total[r]);
-        if (n >= kHot || (n == 0 && a.accumulate)) continue;
-        if (at >= a.width) continue;
-        float sum[N];
-        const Sorted *list = a.list + s_start[r];
-        if (n == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) sum[i] = 0.0f;
-            store_pack<N>(static_cast<F *>(a.dtable) + (first + r) * a.ld_dtable + at, a.width - at, sum);
-        } else {
-            sum_rows<T, N>(a, at, n, [&](int j) { return list[j].token; }, sum);
-            put_row<F, N>(a, first + r, at, sum);
         }
     }
 }
@@ -272,34 +355,59 @@ __global__ __launch_bounds__(kGradBlock) void embed_grad_kernel(const Spread a) 
 // or more: at most two such words meet a piece, one that is there at its first
 // token (slot 0) and one that starts behind it (slot 1).
 template <typename T, typename F>
-__global__ __launch_bounds__(kBlock) void embed_pieces_kernel(const Spread a) {
+__device__ __forceinline__ void sum_piece(const Spread &a, int64_t piece, int at) {
     constexpr int N = kPack<T, F>;
     const int lane = threadIdx.x & (kWave - 1);
+    const int64_t begin = piece * kHot;
+    const int n = int(min(int64_t(kHot), a.start[a.vocab] - begin));
+    Sorted s{0u, -1};
+    if (lane < n) s = a.list[begin + lane];
+    const uint64_t hot = __ballot((s.token & kIsHot) != 0u);
+    if (hot == 0) return;
+    const int token = int(s.token & kTokenMask);
+    const uint64_t head = hot & 1u ? __ballot(s.word == __shfl(s.word, 0) && lane < n) : 0;
+    const T *rows = static_cast<const T *>(a.dout) + min(at, a.width - 1);
+#pragma unroll
+    for (int slot = 0; slot < 2; ++slot) {
+        const uint64_t lanes = slot == 0 ? head : hot & ~head;
+        if (lanes == 0) continue;
+        const int from = __ffsll((unsigned long long)lanes) - 1, many = int(__popcll(lanes));
+        float sum[N];
+        sum_rows<N, 2 * kAhead>(max(a.width - at, 1), many, [&](int j) {
+            return rows + int64_t(__builtin_amdgcn_readlane(token, from + j)) * a.ld_dout;
+        }, sum);
+        if (at < a.width)
+            store_pack<N>(a.partial + (piece * 2 + slot) * int64_t(a.width) + at, a.width - at, sum);
+    }
+}
+
+// Workgroups below a.first: a piece's columns a wave; the others: rows of words.
+template <typename T, typename F>
+__global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
+    constexpr int N = kPack<T, F>;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int parts = (a.width + kWave * N - 1) / (kWave * N);
-    const int64_t units = ((*a.count + int64_t(kHot) - 1) / kHot) * parts;
-    for (int64_t unit = int64_t(blockIdx.x) * kWaves + threadIdx.x / kWave; unit < units;
-         unit += int64_t(gridDim.x) * kWaves) {
-        const int64_t piece = unit / parts, begin = piece * kHot;
-        const int at = (int(unit % parts) * kWave + lane) * N;
-        const int n = int(min(int64_t(kHot), *a.count - begin));
-        Sorted s{0u, -1};
-        if (lane < n) s = a.list[begin + lane];
-        const uint64_t hot = __ballot((s.token & kIsHot) != 0u);
-        if (hot == 0) continue;
-        const uint32_t token = s.token & kTokenMask;
-        const uint64_t head = hot & 1u ? __ballot(s.word == __shfl(s.word, 0) && lane < n) : 0;
-    #pragma unroll
-        for (int slot = 0; slot < 2; ++slot) {
-            const uint64_t lanes = slot == 0 ? head : hot & ~head;
-            if (lanes == 0) continue;
-            const int from = __ffsll((unsigned long long)lanes) - 1, many = int(__popcll(lanes));
-            float sum[N];
-            sum_rows<T, N>(a, min(at, a.width - 1), many, [&](int j) { return __builtin_amdgcn_readlane(token, from + j); }, sum);
-            if (at < a.width) {
-                float *to = a.partial + (piece * 2 + slot) * int64_t(a.width) + at;
-                store_pack<N>(to, a.width - at, sum);
-            }
-        }
+    if (int(blockIdx.x) < a.first) {
+        const int64_t units = ((a.start[a.vocab] + int64_t(kHot) - 1) / kHot) * parts;
+        for (int64_t u = int64_t(blockIdx.x) * kWaves + wave; u < units; u += int64_t(a.first) * kWaves)
+            sum_piece<T, F>(a, u / parts, (int(u % parts) * kWave + lane) * N);
+        return;
+    }
+    __shared__ int32_t s_start[kMaxRows + 1];
+    const int64_t first = int64_t(blockIdx.x - a.first) * a.rows;
+    const int rows = int(min(int64_t(a.rows), a.vocab - first));
+    for (int r = threadIdx.x; r <= rows; r += kBlock) s_start[r] = a.start[first + r];
+    __syncthreads();
+    if (!a.accumulate) clear_rows<F>(a, first, rows, [&](int r) { return s_start[r] == s_start[r + 1]; });
+    const T *dout = static_cast<const T *>(a.dout);
+    for (int u = wave; u < rows * parts; u += kWaves) {
+        const int r = u / parts, at = (u % parts * kWave + lane) * N;
+        const int n = s_start[r + 1] - s_start[r];
+        if (n == 0 || n >= kHot || at >= a.width) continue;
+        const Sorted *list = a.list + s_start[r];
+        float sum[N];
+        sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
+        put_row<F, N>(a, first + r, at, sum);
     }
 }
 
@@ -311,7 +419,7 @@ __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) 
     __shared__ float s_sum[kJoinWaves][kWave * N];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t piece = blockIdx.x, begin = piece * kHot;
-    const int n = int(min(int64_t(kHot), *a.count - begin));
+    const int n = int(min(int64_t(kHot), a.start[a.vocab] - begin));
     if (n <= 0) return;
     Sorted s{0u, -1};
     if (lane < n) s = a.list[begin + lane];
@@ -325,24 +433,12 @@ __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) 
     const int parts = (a.width + kWave * N - 1) / (kWave * N);
     for (int part = blockIdx.y; part < parts; part += gridDim.y) {
         const int at = (part * kWave + lane) * N;
-        float sum[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+        float sum[N] = {};
         if (at < a.width)
-            for (int64_t j = lo; j < hi; j += kAhead) {
-                float v[kAhead][N];
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    const int64_t slot = (piece + j + k) * 2 + (j + k == 0 && from != 0);
-                    if (j + k < hi) load_pack<N>(a.partial + slot * a.width + at, a.width - at, v[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k)
-                    if (j + k < hi) {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], v[k][i]);
-                    }
-            }
+            sum_rows<N, kAhead>(a.width - at, int(hi - lo), [&](int j) {
+                const int64_t slot = (piece + lo + j) * 2 + (lo + j == 0 && from != 0);
+                return static_cast<const float *>(a.partial) + slot * a.width + at;
+            }, sum);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) s_sum[wave][i * kWave + lane] = sum[i];
@@ -356,36 +452,33 @@ __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) 
     }
 }
 
-int64_t pieces_of(int32_t tokens) { return tokens < kHot ? 0 : (int64_t(tokens) + kHot - 1) / kHot; }
+int64_t pieces_of(int32_t tokens) { return (int64_t(tokens) + kHot - 1) / kHot; }
 
 // A grid's threads are counted in 32 bits; the kernels step on where it ends.
 uint32_t grid_of(int64_t groups) { return uint32_t(groups < (1 << 20) ? groups : 1 << 20); }
 
 size_t up16(size_t bytes) { return (bytes + 15) & ~size_t(15); }
 
-// Words of one workgroup: enough of them that looking through the ids (16 bytes
-// a token at the rate of L2) stays below a tenth of writing their rows, and few
-// enough that there are some workgroups for every compute unit.
-int words_per_workgroup(int32_t tokens, int32_t vocab, int64_t row_bytes) {
-    const int64_t scan = 24 * int64_t(tokens) / row_bytes;
-    int64_t words = vocab / (8 * int64_t(device_cu_count()));
-    if (words < scan) words = scan;
-    return int(words < 1 ? 1 : words > kMaxWords ? kMaxWords : words);
-}
-
 template <typename T, typename F>
 hipError_t spread(Spread a, hipStream_t stream) {
     constexpr int N = kPack<T, F>;
-    a.words = words_per_workgroup(a.tokens, a.vocab, int64_t(a.width) * int(sizeof(F)));
-    const uint32_t groups = uint32_t((a.vocab + a.words - 1) / a.words);
-    const size_t lds = size_t(a.words) * (kGradWaves + 2) * sizeof(uint32_t);
-    embed_grad_kernel<T, F><<<groups, kGradBlock, lds, stream>>>(a);
-    const int64_t pieces = pieces_of(a.tokens);
-    if (pieces > 0) {
-        const int64_t parts = (a.width + kWave * N - 1) / (kWave * N);
-        embed_pieces_kernel<T, F><<<grid_of((pieces * parts + kWaves - 1) / kWaves), kBlock, 0, stream>>>(a);
-        embed_join_kernel<T, F><<<dim3(uint32_t(pieces), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0, stream>>>(a);
+    const int64_t rows = kFillBytes / (int64_t(a.width) * int(sizeof(F)));
+    a.rows = int32_t(rows < 1 ? 1 : rows > kMaxRows ? kMaxRows : rows);
+    const uint32_t fills = uint32_t((a.vocab + a.rows - 1) / a.rows);
+    if (a.tokens <= kFew) {
+        a.first = a.tokens * ((a.width + kBlock * N - 1) / (kBlock * N));
+        const uint32_t groups = uint32_t(a.first) + (a.accumulate ? 0 : fills);
+        embed_few_kernel<T, F><<<groups, kBlock, 0, stream>>>(a);
+        return hipGetLastError();
     }
+    const int each = (a.vocab + device_cu_count() - 1) / device_cu_count();
+    a.words = each > kMaxWords ? kMaxWords : each;
+    const size_t lds = size_t(a.words) * (kSortWaves + 2) * sizeof(uint32_t);
+    embed_sort_kernel<<<uint32_t((a.vocab + a.words - 1) / a.words), kSortBlock, lds, stream>>>(a);
+    const int64_t pieces = pieces_of(a.tokens), parts = (a.width + kWave * N - 1) / (kWave * N);
+    a.first = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
+    embed_rows_kernel<T, F><<<uint32_t(a.first) + fills, kBlock, 0, stream>>>(a);
+    embed_join_kernel<T, F><<<dim3(uint32_t(pieces), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -408,11 +501,12 @@ hipError_t launch_embed_forward(const void *table, int64_t ld_table, bool table_
     return hipGetLastError();
 }
 
-// [16 bytes: tokens that count][list][lengths][partial sums]
-size_t embed_workspace_size(int32_t tokens, int32_t width) {
+// [list][where words start][lengths][partial sums]; up to kFew tokens need none
+size_t embed_workspace_size(int32_t tokens, int32_t vocab, int32_t width) {
+    if (tokens <= kFew) return 16;
     const size_t pieces = size_t(pieces_of(tokens));
-    return 16 + up16(size_t(tokens) * sizeof(Sorted)) + up16(pieces * sizeof(int32_t)) +
-           up16(pieces * 2 * size_t(width) * sizeof(float));
+    return up16(size_t(tokens) * sizeof(Sorted)) + up16((size_t(vocab) + 1) * sizeof(int32_t)) +
+           up16(pieces * sizeof(int32_t)) + up16(pieces * 2 * size_t(width) * sizeof(float));
 }
 
 hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, const int64_t *ids, void *dtable,
@@ -425,10 +519,10 @@ hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, c
     a.ld_dout = ld_dout, a.ld_dtable = ld_dtable, a.ignore = ignore;
     a.tokens = tokens, a.vocab = vocab, a.width = width;
     a.scale = scale, a.accumulate = accumulate, a.status = status;
-    a.count = reinterpret_cast<int32_t *>(ws);
-    ws += 16;
     a.list = reinterpret_cast<Sorted *>(ws);
     ws += up16(size_t(tokens) * sizeof(Sorted));
+    a.start = reinterpret_cast<int32_t *>(ws);
+    ws += up16((size_t(vocab) + 1) * sizeof(int32_t));
     a.lengths = reinterpret_cast<int32_t *>(ws);
     ws += up16(size_t(pieces_of(tokens)) * sizeof(int32_t));
     a.partial = reinterpret_cast<float *>(ws);

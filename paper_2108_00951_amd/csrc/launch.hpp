@@ -81,7 +81,7 @@ constexpr int32_t kEmbedMaxTokens = 1 << 22, kEmbedMaxVocab = 1 << 24, kEmbedMax
 hipError_t launch_embed_forward(const void *table, int64_t ld_table, bool table_bf16, const int64_t *ids, void *out,
                                 int64_t ld_out, bool bf16, int32_t tokens, int32_t vocab, int32_t width, float scale,
                                 int64_t ignore, uint32_t *status, hipStream_t stream);
-size_t embed_workspace_size(int32_t tokens, int32_t width);
+size_t embed_workspace_size(int32_t tokens, int32_t vocab, int32_t width);
 hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, const int64_t *ids, void *dtable,
                                  int64_t ld_dtable, bool table_bf16, int32_t tokens, int32_t vocab, int32_t width,
                                  float scale, int64_t ignore, bool accumulate, uint32_t *status, void *workspace,

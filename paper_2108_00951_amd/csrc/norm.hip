@@ -39,6 +39,8 @@ struct Norm {
 template <typename T>
 constexpr int kRowPack = 16 / sizeof(T);
 
+constexpr int kLong = 1024;   // threads of the longest rows
+
 // The sums of M values over the kThreads threads that hold a row, in each of
 // them.  One barrier: the next call takes another buffer, and the one after it
 // comes behind that one's barrier.
@@ -74,6 +76,18 @@ __device__ __forceinline__ void load_columns(const void *row, int width, float a
     }
 }
 
+// This thread's packs of a row of `width` elements (0: none there).
+template <int N, int kPacks, int kThreads, typename T>
+__device__ __forceinline__ void load_row(const T *row, int lane, int width, Pack<T, N> (&v)[kPacks]) {
+#pragma unroll
+    for (int k = 0; k < kPacks; ++k) {
+        const int at = (k * kThreads + lane) * N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[k][i] = T(0.0f);
+        if (at < width) v[k] = load_raw<N>(row + at, width - at);
+    }
+}
+
 struct Moments {
     float mean, rstd, rest;   // rest: mean of x - (the mean that was subtracted)
 };
@@ -95,23 +109,23 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void norm_fo
     float w[kPacks][N], b[kPacks][N];
     load_columns<F, N, kPacks, kThreads>(a.weight, a.width, 1.0f, w);
     load_columns<F, N, kPacks, kThreads>(a.bias, a.width, 0.0f, b);
-    for (int64_t first = int64_t(blockIdx.x) * kGroups; first < a.rows; first += int64_t(gridDim.x) * kGroups) {
-        const int64_t row = first + group;
-        if (kThreads <= kWave && row >= a.rows) break;   // (a row of the workgroup's own is there)
-        const T *from = static_cast<const T *>(a.x) + row * a.ld_x;
+    const int64_t step = int64_t(gridDim.x) * kGroups;
+    const T *const rows = static_cast<const T *>(a.x);
+    int64_t row = int64_t(blockIdx.x) * kGroups + group;
+    Pack<T, N> next[kPacks];   // a row on its way while the one before it is worked on
+    load_row<N, kPacks, kThreads>(rows + row * a.ld_x, lane, row < a.rows ? a.width : 0, next);
+    // (a wave's own rows end where it likes; groups of waves are one to a workgroup)
+    for (; row < a.rows; row += step) {
         float x[kPacks][N];
         float sum[1] = {0.0f};
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const int at = (k * kThreads + lane) * N;
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[k][i] = 0.0f;
-            if (at < a.width) load_pack<N>(from + at, a.width - at, x[k]);
-        }
-#pragma unroll
         for (int k = 0; k < kPacks; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum[0] += x[k][i];
+            for (int i = 0; i < N; ++i) {
+                x[k][i] = float(next[k][i]);
+                sum[0] += x[k][i];
+            }
+        load_row<N, kPacks, kThreads>(rows + (row + step) * a.ld_x, lane, row + step < a.rows ? a.width : 0, next);
         row_sums<kThreads>(sum, s_sum);
         const float m = sum[0] / float(a.width);
         float rest[2] = {0.0f, 0.0f};
@@ -142,7 +156,6 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void norm_fo
 }
 
 // Rows too long for registers, one workgroup each, read three times.
-constexpr int kLong = 1024;
 
 template <typename T, typename F>
 __global__ __launch_bounds__(kLong) void norm_forward_long_kernel(const Norm a) {
@@ -212,21 +225,30 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) dw[k][i] = db[k][i] = 0.0f;
     int turn = 0;
-    for (int64_t first = int64_t(blockIdx.x) * kGroups; first < a.rows; first += int64_t(gridDim.x) * kGroups) {
+    const int64_t step = int64_t(gridDim.x) * kGroups;
+    const T *const xs = static_cast<const T *>(a.x), *const dys = static_cast<const T *>(a.dy);
+    Pack<T, N> next_x[kPacks], next_dy[kPacks];   // a row on its way while the one before it is worked on
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    const auto fetch = [&](int64_t row) {
+        const bool there = row < a.rows;
+        load_row<N, kPacks, kThreads>(xs + row * a.ld_x, lane, there ? a.width : 0, next_x);
+        load_row<N, kPacks, kThreads>(dys + row * a.ld_dy, lane, there ? a.width : 0, next_dy);
+        next_mean = there ? a.mean[row] : 0.0f, next_rstd = there ? a.rstd[row] : 0.0f;
+    };
+    // (16 waves' registers do not hold two rows)
+    constexpr bool kFetchAhead = kThreads < kLong;
+    if (kFetchAhead) fetch(int64_t(blockIdx.x) * kGroups + group);
+    for (int64_t first = int64_t(blockIdx.x) * kGroups; first < a.rows; first += step) {
         const int64_t row = first + group;
         const bool there = row < a.rows;   // (all groups meet at the barrier)
-        const float mean = there ? a.mean[row] : 0.0f, rstd = there ? a.rstd[row] : 0.0f;
+        if (!kFetchAhead) fetch(row);
+        const float mean = next_mean, rstd = next_rstd;
         float x[kPacks][N], dy[kPacks][N];
 #pragma unroll
-        for (int k = 0; k < kPacks; ++k) {
-            const int at = (k * kThreads + lane) * N;
+        for (int k = 0; k < kPacks; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[k][i] = dy[k][i] = 0.0f;
-            if (there && at < a.width) {
-                load_pack<N>(static_cast<const T *>(a.x) + row * a.ld_x + at, a.width - at, x[k]);
-                load_pack<N>(static_cast<const T *>(a.dy) + row * a.ld_dy + at, a.width - at, dy[k]);
-            }
-        }
+            for (int i = 0; i < N; ++i) x[k][i] = float(next_x[k][i]), dy[k][i] = float(next_dy[k][i]);
+        if (kFetchAhead) fetch(row + step);
         float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
@@ -381,26 +403,31 @@ struct Hold {
     int threads, packs;   // 0: too long for registers
 };
 
-constexpr int kMaxHeld = 16384;   // elements of a row; beyond them, the registers of 1,024 threads
-
-Hold hold_of(int32_t width, int pack) {
+// Forward: up to four packs of 8 bf16 or 4 fp32 values a thread, 16,384 values.
+Hold forward_hold(int32_t width, int pack) {
     const int packs = (width + pack - 1) / pack;
-    if (width > kMaxHeld) return Hold{0, 0};
+    if (width > kLong * 16) return Hold{0, 0};
     for (int threads = kWave; threads <= kLong; threads *= 4)
         for (int k = 1; k <= 4; k *= 2)
             if (packs <= threads * k) return Hold{threads, k};
     return Hold{0, 0};
 }
 
-// Workgroups of the backward pass, whose partial sums the workspace holds: one
-// for each row held by one, no more than some a compute unit.
-constexpr int kBackwardGroups = 512;
+// Backward: two packs, beside which a thread holds those of dy, the weights and both sums.
+Hold backward_hold(int32_t width, int pack) {
+    const int packs = (width + pack - 1) / pack;
+    for (int threads = kWave; threads <= kLong; threads *= 4)
+        for (int k = 1; k <= 2; k *= 2)
+            if (packs <= threads * k) return Hold{threads, k};
+    return Hold{0, 0};
+}
 
-int backward_groups(int32_t rows, int32_t width, int pack) {
-    const Hold h = hold_of(width, pack);
+// Workgroups of the backward pass, whose partial sums the workspace holds: no
+// more than run at once.
+int backward_groups(int32_t rows, Hold h) {
     const int64_t each = h.threads == 0 ? 8 : h.threads < kBlock ? kBlock / h.threads : 1;
-    const int64_t groups = (rows + each - 1) / each;
-    return int(groups < kBackwardGroups ? groups : kBackwardGroups);
+    const int64_t groups = (rows + each - 1) / each, most = h.threads == kLong ? 256 : 768;
+    return int(groups < most ? groups : most);
 }
 
 template <typename T, typename F, int kThreads, int kPacks>
@@ -418,7 +445,7 @@ void backward(const Norm &a, int groups, hipStream_t stream) {
 
 template <typename T, typename F>
 hipError_t run_forward(const Norm &a, hipStream_t stream) {
-    const Hold h = hold_of(a.width, kRowPack<T>);
+    const Hold h = forward_hold(a.width, kRowPack<T>);
     switch (h.threads * 8 + h.packs) {
         case 64 * 8 + 1: forward<T, F, 64, 1>(a, stream); break;
         case 64 * 8 + 2: forward<T, F, 64, 2>(a, stream); break;
@@ -426,7 +453,7 @@ hipError_t run_forward(const Norm &a, hipStream_t stream) {
         case 256 * 8 + 2: forward<T, F, 256, 2>(a, stream); break;
         case 256 * 8 + 4: forward<T, F, 256, 4>(a, stream); break;
         case 1024 * 8 + 2: forward<T, F, 1024, 2>(a, stream); break;
-        case 1024 * 8 + 4:   // (bf16's rows of that length end in registers of two packs)
+        case 1024 * 8 + 4:   // (16,384 bf16 values are two packs)
             if constexpr (sizeof(T) == 4) forward<T, F, 1024, 4>(a, stream);
             break;
         default: {
@@ -439,19 +466,16 @@ hipError_t run_forward(const Norm &a, hipStream_t stream) {
 
 template <typename T, typename F>
 hipError_t run_backward(const Norm &a, F *dweight, F *dbias, hipStream_t stream) {
-    const Hold h = hold_of(a.width, kRowPack<T>);
-    const int groups = backward_groups(a.rows, a.width, kRowPack<T>);
+    const Hold h = backward_hold(a.width, kRowPack<T>);
+    const int groups = backward_groups(a.rows, h);
     int parts = groups;
     if (a.rows > 0) switch (h.threads * 8 + h.packs) {
         case 64 * 8 + 1: backward<T, F, 64, 1>(a, groups, stream); break;
         case 64 * 8 + 2: backward<T, F, 64, 2>(a, groups, stream); break;
-        case 64 * 8 + 4: backward<T, F, 64, 4>(a, groups, stream); break;
+        case 256 * 8 + 1: backward<T, F, 256, 1>(a, groups, stream); break;
         case 256 * 8 + 2: backward<T, F, 256, 2>(a, groups, stream); break;
-        case 256 * 8 + 4: backward<T, F, 256, 4>(a, groups, stream); break;
+        case 1024 * 8 + 1: backward<T, F, 1024, 1>(a, groups, stream); break;
         case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, groups, stream); break;
-        case 1024 * 8 + 4:
-            if constexpr (sizeof(T) == 4) backward<T, F, 1024, 4>(a, groups, stream);
-            break;
         default: {
             const int64_t most = int64_t(device_cu_count()) * 2;
             norm_sums_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
@@ -481,11 +505,16 @@ hipError_t launch_layernorm_forward(const void *x, int64_t ld_x, const void *wei
     return run_forward<float, float>(a, stream);
 }
 
-// [partial sums of dw and db][sums of long rows], for either type of x
+// [sums of long rows][partial sums of dw and db], as much as either type of x takes
 size_t layernorm_workspace_size(int32_t rows, int32_t width) {
-    const int wide = backward_groups(rows, width, 4), narrow = backward_groups(rows, width, 8);
-    const size_t groups = size_t(wide > narrow ? wide : narrow);
-    return 16 + groups * 2 * size_t(width) * sizeof(float) + (width > kMaxHeld ? size_t(rows) * 4 * sizeof(float) : 0);
+    size_t most = 0;
+    for (int pack = kRowPack<float>; pack <= kRowPack<__bf16>; pack *= 2) {
+        const Hold h = backward_hold(width, pack);
+        const size_t bytes = size_t(backward_groups(rows, h)) * 2 * size_t(width) * sizeof(float) +
+                             (h.threads == 0 ? size_t(rows) * 4 * sizeof(float) : 0);
+        most = bytes > most ? bytes : most;
+    }
+    return 16 + most;
 }
 
 hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean,
@@ -497,7 +526,7 @@ hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *we
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx, a.rows = rows, a.width = width;
     a.sums = static_cast<float *>(workspace);
-    const bool long_rows = width > kMaxHeld;
+    const bool long_rows = backward_hold(width, bf16 ? kRowPack<__bf16> : kRowPack<float>).threads == 0;
     if (dweight != nullptr || dbias != nullptr)
         a.partial = static_cast<float *>(workspace) + (long_rows ? int64_t(rows) * 4 : 0);
     if (bf16 && weight_bf16)

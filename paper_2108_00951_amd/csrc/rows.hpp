@@ -10,37 +10,43 @@ namespace efs {
 // wide as they are, since the hardware asks for no more alignment than that.
 template <typename T, int N>
 struct PackOf {
-    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    typedef T type __attribute__((ext_vector_type(N)));
+    typedef T loose __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 };
+template <typename T, int N>
+using Pack = typename PackOf<T, N>::type;
 
 // Elements a lane takes at once from a row of T where it also handles rows of
 // F: 16 bytes of the wider type.
 template <typename T, typename F>
 constexpr int kPack = sizeof(T) == 2 && sizeof(F) == 2 ? 8 : 4;
 
+// The first `left` (at least 1) elements from p on, zeros behind; a whole pack if
+// left >= N.
 template <int N, typename T>
-__device__ __forceinline__ void load_pack(const T *p, float (&v)[N]) {
-    const typename PackOf<T, N>::type a = *reinterpret_cast<const typename PackOf<T, N>::type *>(p);
+__device__ __forceinline__ Pack<T, N> load_raw(const T *p, int left) {
+    Pack<T, N> v;
+    if (left >= N) return *reinterpret_cast<const typename PackOf<T, N>::loose *>(p);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = float(a[i]);
+    for (int i = 0; i < N; ++i) v[i] = i < left ? p[i] : T(0.0f);
+    return v;
 }
 
-// The first `left` (at least 1) of them, zeros behind; a whole pack if left >= N.
 template <int N, typename T>
 __device__ __forceinline__ void load_pack(const T *p, int left, float (&v)[N]) {
-    if (left >= N) return load_pack(p, v);
+    const Pack<T, N> a = load_raw<N>(p, left);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = i < left ? float(p[i]) : 0.0f;
+    for (int i = 0; i < N; ++i) v[i] = float(a[i]);
 }
 
 // bf16 results are rounded here, to nearest even.
 template <int N, typename T>
 __device__ __forceinline__ void store_pack(T *p, int left, const float (&v)[N]) {
     if (left >= N) {
-        typename PackOf<T, N>::type a;
+        Pack<T, N> a;
 #pragma unroll
         for (int i = 0; i < N; ++i) a[i] = T(v[i]);
-        *reinterpret_cast<typename PackOf<T, N>::type *>(p) = a;
+        *reinterpret_cast<typename PackOf<T, N>::loose *>(p) = a;
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -48,11 +54,41 @@ __device__ __forceinline__ void store_pack(T *p, int left, const float (&v)[N]) 
     }
 }
 
+// Lane permutations within the wave without LDS: pairs, fours, eights, sixteens
+// mirrored, and the last lane of a row of 16 (of 32) to the next (to the upper half).
+constexpr int kDppPairs = 0xB1, kDppFours = 0x4E, kDppEights = 0x141, kDppSixteens = 0x140, kDppNextRow = 0x142,
+              kDppUpperHalf = 0x143;
+
+template <int kControl, int kRows = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), kControl, kRows, 0xf, false));
+}
+
+template <int kControl, int kRows = 0xf>
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(dpp<kControl, kRows>(__float_as_uint(v)));
+}
+
 // Sum over the wave, in every lane.
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
-    return v;
+    v += dpp<kDppPairs>(v);
+    v += dpp<kDppFours>(v);
+    v += dpp<kDppEights>(v);
+    v += dpp<kDppSixteens>(v);
+    v += dpp<kDppNextRow, 0xa>(v);
+    v += dpp<kDppUpperHalf, 0xc>(v);
+    return __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(v)), kWave - 1)));
+}
+
+// Largest over the wave, in every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max(v, dpp<kDppPairs>(v));
+    v = max(v, dpp<kDppFours>(v));
+    v = max(v, dpp<kDppEights>(v));
+    v = max(v, dpp<kDppSixteens>(v));
+    v = max(v, dpp<kDppNextRow, 0xa>(v));
+    v = max(v, dpp<kDppUpperHalf, 0xc>(v));
+    return uint32_t(__builtin_amdgcn_readlane(int(v), kWave - 1));
 }
 
 }  // namespace efs
