@@ -677,21 +677,52 @@ def xent_backward(h, w, target, lse, dloss, dh, dw, workspace, ignore_index: int
                                   workspace.numel(), _stream_handle(stream)))
 
 
-def _on_current_device(**tensors) -> None:
-    """The call's stream is one of the current device: the tensors must be too."""
+def _device_of(t, name) -> int:
+    """The device of a call's first tensor: the current one, whose stream the call takes."""
+    here = t.get_device()
+    if here < 0:
+        raise TypeError("%s must be a device tensor" % name)
     import torch
-    here = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if t is not None and t.device.index != here:
-            raise ValueError("%s is on %s, and the current device is cuda:%d" % (name, t.device, here))
+    if here != torch._C._cuda_getDevice():
+        raise ValueError("%s is on %s, and the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    return here
 
 
-def _require_status(status):
+def _elsewhere(t, name, here):
+    if t.get_device() < 0:
+        raise TypeError("%s must be a device tensor" % name)
+    raise ValueError("%s is on %s, and the current device is cuda:%d" % (name, t.device, here))
+
+
+def _matrix(t, name, here):
+    """Pointer and elements between the rows of a matrix of contiguous rows."""
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if t.get_device() != here:
+        _elsewhere(t, name, here)
+    if step != 1 and cols > 1 and rows > 0:
+        raise TypeError("%s must have contiguous rows" % name)
+    return _ptr(t), ld if rows > 1 else cols
+
+
+def _vector(t, name, dtype, here):
+    """Pointer of a contiguous tensor of this dtype."""
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.get_device() != here:
+        _elsewhere(t, name, here)
+    if not t.is_contiguous():
+        raise TypeError("%s must be contiguous" % name)
+    return _ptr(t)
+
+
+def _status_pointer(status, here):
+    if status is None:
+        return None
     import torch
-    if status is not None:
-        _require(status, torch.int32, "status")
-        if status.numel() < 1:
-            raise ValueError("status must have an element")
+    if status.numel() < 1:
+        raise ValueError("status must have an element")
+    return _vector(status, "status", torch.int32, here)
 
 
 EMBED_BAD_ID = 1
@@ -716,15 +747,11 @@ def embed_forward(table, ids, out, scale: float = 1.0, ignore_index: int = -100,
     if table.dim() != 2 or ids.dim() != 1 or out.shape != (ids.shape[0], table.shape[1]):
         raise ValueError("table must be [vocab, width], ids [tokens] and out [tokens, width]")
     table_dtype, dtype = _dtype_code(table, "table"), _dtype_code(out, "out")
-    _require_rows(table, "table")
-    _require(ids, torch.int64, "ids")
-    _require_rows(out, "out")
-    _require_status(status)
-    _on_current_device(table=table, ids=ids, out=out, status=status)
-    _check(lib, lib.embed_forward(_ptr(table), _row_stride(table), table_dtype, _ptr(ids), _ptr(out), _row_stride(out),
-                                  dtype, _int32(ids.shape[0], "tokens"), _int32(table.shape[0], "vocab"),
-                                  _int32(table.shape[1], "width"), float(scale), int(ignore_index),
-                                  None if status is None else status.data_ptr(), _stream_handle(stream)))
+    here = _device_of(table, "table")
+    _check(lib, lib.embed_forward(*_matrix(table, "table", here), table_dtype, _vector(ids, "ids", torch.int64, here),
+                                  *_matrix(out, "out", here), dtype, _int32(ids.shape[0], "tokens"),
+                                  _int32(table.shape[0], "vocab"), _int32(table.shape[1], "width"), float(scale),
+                                  int(ignore_index), _status_pointer(status, here), _stream_handle(stream)))
 
 
 def embed_workspace_bytes(tokens: int, vocab: int, width: int) -> int:
@@ -750,63 +777,58 @@ def embed_backward(dout, ids, dtable, workspace, scale: float = 1.0, ignore_inde
     if dtable.dim() != 2 or ids.dim() != 1 or dout.shape != (ids.shape[0], dtable.shape[1]):
         raise ValueError("dtable must be [vocab, width], ids [tokens] and dout [tokens, width]")
     table_dtype, dtype = _dtype_code(dtable, "dtable"), _dtype_code(dout, "dout")
-    _require_rows(dout, "dout")
-    _require(ids, torch.int64, "ids")
-    _require_rows(dtable, "dtable")
-    _require(workspace, torch.uint8, "workspace")
-    _require_status(status)
-    _on_current_device(dout=dout, ids=ids, dtable=dtable, workspace=workspace, status=status)
-    _check(lib, lib.embed_backward(_ptr(dout), _row_stride(dout), dtype, _ptr(ids), _ptr(dtable), _row_stride(dtable),
-                                   table_dtype, _int32(ids.shape[0], "tokens"), _int32(dtable.shape[0], "vocab"),
-                                   _int32(dtable.shape[1], "width"), float(scale), int(ignore_index),
-                                   int(bool(accumulate)), None if status is None else status.data_ptr(),
-                                   _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+    here = _device_of(dtable, "dtable")
+    _check(lib, lib.embed_backward(*_matrix(dout, "dout", here), dtype, _vector(ids, "ids", torch.int64, here),
+                                   *_matrix(dtable, "dtable", here), table_dtype, _int32(ids.shape[0], "tokens"),
+                                   _int32(dtable.shape[0], "vocab"), _int32(dtable.shape[1], "width"), float(scale),
+                                   int(ignore_index), int(bool(accumulate)), _status_pointer(status, here),
+                                   _vector(workspace, "workspace", torch.uint8, here), workspace.numel(),
+                                   _stream_handle(stream)))
 
 
-def _weight_args(width, **weights):
-    """The code of the dtype that the given weights share (of None: fp32)."""
-    code = None
+def _weights(width, here, **weights):
+    """The code of the dtype that the given weights share (of None: fp32), and their pointers."""
+    kind, pointers = None, []
     for name, t in weights.items():
         if t is None:
+            pointers.append(None)
             continue
-        if t.shape != (width,):
+        if t.dim() != 1 or t.shape[0] != width:
             raise ValueError("%s must be [width]" % name)
-        one = _dtype_code(t, name)
-        if code is not None and one != code:
+        if kind is not None and t.dtype is not kind:
             raise TypeError("%s must have one dtype" % " and ".join(weights))
-        if t.device.type != "cuda" or not t.is_contiguous():
-            raise TypeError("%s must be a contiguous device tensor" % name)
-        code = one
-    return FP32 if code is None else code
+        kind = t.dtype
+        pointers.append(_vector(t, name, kind, here))
+        code = _dtype_code(t, name)
+    return FP32 if kind is None else code, pointers
 
 
-def _norm_sizes(x):
-    return _int32(x.shape[0], "rows"), _int32(x.shape[1], "width")
+def _row_values(t, name, rows, here):
+    """Pointer of fp32 values, one a row, or None."""
+    import torch
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != rows:
+        raise ValueError("%s must be [rows]" % name)
+    return _vector(t, name, torch.float32, here)
 
 
 def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
     """Layer norm of the rows of x [rows, width] into y, fp32 or bf16; weight and
     bias [width] of their own dtype, or None; mean and rstd fp32 [rows] for the
     gradients, or None; see layernorm_forward in include/efsparse.h."""
-    import torch
     lib = load_library()
     if x.dim() != 2 or y.shape != x.shape:
         raise ValueError("x and y must be [rows, width]")
-    if x.dtype != y.dtype:
+    if x.dtype is not y.dtype:
         raise TypeError("x and y must have one dtype")
     dtype = _dtype_code(x, "x")
-    _require_rows(x, "x")
-    _require_rows(y, "y")
-    rows, width = _norm_sizes(x)
-    weight_dtype = _weight_args(width, weight=weight, bias=bias)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is not None:
-            _require(t, torch.float32, name)
-            if t.shape != x.shape[:1]:
-                raise ValueError("%s must be [rows]" % name)
-    _on_current_device(x=x, weight=weight, bias=bias, y=y, mean=mean, rstd=rstd)
-    _check(lib, lib.layernorm_forward(_ptr(x), _row_stride(x), _ptr(weight), _ptr(bias), _ptr(y), _row_stride(y), dtype,
-                                      weight_dtype, rows, width, float(eps), _ptr(mean), _ptr(rstd),
+    here = _device_of(x, "x")
+    rows, width = x.shape
+    weight_dtype, (w, b) = _weights(width, here, weight=weight, bias=bias)
+    _check(lib, lib.layernorm_forward(*_matrix(x, "x", here), w, b, *_matrix(y, "y", here), dtype, weight_dtype,
+                                      _int32(rows, "rows"), _int32(width, "width"), float(eps),
+                                      _row_values(mean, "mean", rows, here), _row_values(rstd, "rstd", rows, here),
                                       _stream_handle(stream)))
 
 
@@ -830,24 +852,19 @@ def layernorm_backward(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace,
     lib = load_library()
     if x.dim() != 2 or dy.shape != x.shape or dx.shape != x.shape:
         raise ValueError("x, dy and dx must be [rows, width]")
-    if x.dtype != dy.dtype or x.dtype != dx.dtype:
+    if x.dtype is not dy.dtype or x.dtype is not dx.dtype:
         raise TypeError("x, dy and dx must have one dtype")
+    if mean is None or rstd is None:
+        raise TypeError("mean and rstd must be tensors")
     dtype = _dtype_code(x, "x")
-    _require_rows(x, "x")
-    _require_rows(dy, "dy")
-    _require_rows(dx, "dx")
-    rows, width = _norm_sizes(x)
-    weight_dtype = _weight_args(width, weight=weight, dweight=dweight, dbias=dbias)
-    _require(mean, torch.float32, "mean")
-    _require(rstd, torch.float32, "rstd")
-    _require(workspace, torch.uint8, "workspace")
-    if mean.shape != x.shape[:1] or rstd.shape != x.shape[:1]:
-        raise ValueError("mean and rstd must be [rows]")
-    _on_current_device(x=x, weight=weight, mean=mean, rstd=rstd, dy=dy, dx=dx, dweight=dweight, dbias=dbias,
-                       workspace=workspace)
-    _check(lib, lib.layernorm_backward(_ptr(x), _row_stride(x), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dy),
-                                       _row_stride(dy), _ptr(dx), _row_stride(dx), dtype, weight_dtype, rows, width,
-                                       _ptr(dweight), _ptr(dbias), _ptr(workspace), workspace.numel(),
+    here = _device_of(x, "x")
+    rows, width = x.shape
+    weight_dtype, (w, dw, db) = _weights(width, here, weight=weight, dweight=dweight, dbias=dbias)
+    _check(lib, lib.layernorm_backward(*_matrix(x, "x", here), w, _row_values(mean, "mean", rows, here),
+                                       _row_values(rstd, "rstd", rows, here), *_matrix(dy, "dy", here),
+                                       *_matrix(dx, "dx", here), dtype, weight_dtype, _int32(rows, "rows"),
+                                       _int32(width, "width"), dw, db,
+                                       _vector(workspace, "workspace", torch.uint8, here), workspace.numel(),
                                        _stream_handle(stream)))
 
 
@@ -937,10 +954,9 @@ def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float 
         decays = [float(weight_decay)] * len(sizes)
     dp = (ctypes.c_float * max(len(sizes), 1))(*decays)
     if factors is not None:
-        _require(factors, torch.float32, "factors")
         if factors.numel() != 2:
             raise ValueError("factors must have two elements")
-        _on_current_device(factors=factors)
+        _vector(factors, "factors", torch.float32, _device_of(factors, "factors"))
     if not 0 <= int(seed) < 2 ** 32:
         raise ValueError("seed must fit 32 bits")
     grad = _dtype_code(g[0], "g") if g else FP32
@@ -951,10 +967,9 @@ def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float 
 
     def call(step):
         if isinstance(step, torch.Tensor):
-            _require(step, torch.int64, "step")
             if step.numel() != 1:
                 raise ValueError("step must have one element")
-            _on_current_device(step=step)
+            _vector(step, "step", torch.int64, _device_of(step, "step"))
             call.step = step   # alive as long as a graph that this call was captured in
             _check(lib, fn(*head, 1, step.data_ptr(), *tail))
         else:

@@ -7,7 +7,7 @@
 // each operation rounded to fp32 by itself.  Bytes bound it: 28 of an element
 // with states of 32 bits (g, x, m, v in; x, m, v out), 16 with states of 8.
 // A launch takes the tensors of its arguments, kTensors at most, one tile of
-// kTile elements a workgroup, whichever tensor it lies in.
+// kStepTile elements a workgroup, whichever tensor it lies in.
 //
 // States of 8 bits.  A block of kStateBlock elements shares a scale for m and one
 // for r = sqrt(v), powers of two that put the block's largest in [2^7, 2^8).
@@ -28,21 +28,50 @@ namespace efs {
 
 namespace {
 
-constexpr int kTensors = 64;           // of one launch: 3.6 KB of arguments
-constexpr int kTiles = kTile / (kBlock * 4);
+constexpr int kTensors = 112;          // of one launch: 3.9 KB of arguments
 constexpr int kStateBlock = kAdamwBlock;
 static_assert(kStateBlock == kWave * 4, "a wave holds a block of a state");
+// Four times as much a workgroup (217 instead of 204 us for 37 M elements of 161
+// tensors, 680 instead of 597 for 134 M with states of 8 bits) leaves each wave
+// more registers to wait for and the chip fewer waves.
+constexpr int kStepTile = kBlock * 4;
 
-struct Tensor {
-    const void *g;
-    float *x;
-    void *m, *v;
-    __bf16 *copy;
-    int32_t size;
-    float decay;
-    uint32_t ordinal;     // in the caller's list
-    uint32_t first;       // tile
+constexpr uint32_t kMaxTiles = 1u << 23;   // of one launch, whose threads are counted in 32 bits
+
+// What a step writes is read again a step later, after all else has passed the caches.
+constexpr bool kPast = true;
+
+constexpr int32_t kNone = INT32_MIN;   // no tensor of an optional list
+
+// The tensors of a launch: list l's tensor i starts at[l][i] units of unit[l] bytes
+// behind (or before) its first one at base[l], so that a launch holds many.
+template <int kLists>
+struct Tensors {
+    char *base[kLists];
+    int32_t unit[kLists];
+    int32_t at[kLists][kTensors];
+    int32_t size[kTensors];
+    uint32_t first[kTensors];     // tile
+    int32_t count;
+    uint32_t ordinal;             // of the first in the caller's list
+
+    template <typename T>
+    __device__ __forceinline__ T *pointer(int list, int i) const {
+        return reinterpret_cast<T *>(base[list] + int64_t(at[list][i]) * unit[list]);
+    }
 };
+
+// The tensor in which a tile lies: the last whose first tile is at or before it
+// (one that is empty starts where the next one does).
+template <int kLists>
+__device__ __forceinline__ int tensor_of(const Tensors<kLists> &a, uint32_t tile) {
+    static_assert(kTensors <= 2 * kWave, "two tensors a lane");
+    const int lane = threadIdx.x & (kWave - 1);
+    int before = int(__popcll(__ballot(lane < a.count && a.first[min(lane, kTensors - 1)] <= tile)));
+    if (a.count > kWave)
+        before += int(__popcll(__ballot(lane + kWave < a.count && a.first[min(lane + kWave, kTensors - 1)] <= tile)));
+    return __builtin_amdgcn_readfirstlane(before - 1);
+}
 
 // What a step multiplies by.
 struct Rates {
@@ -51,16 +80,19 @@ struct Rates {
     uint32_t key;                                   // of the random bits, before the tensor's ordinal
 };
 
+enum { kG, kX, kM, kV, kCopy, kStepLists };
+
 struct Step {
-    Tensor tensor[kTensors];
+    Tensors<kStepLists> tensors;
+    float decay[kTensors];
     Rates rates;
     const int64_t *step;      // on the device, NULL: rates are complete
     const float *factors;     // on the device, may be NULL
     int64_t given;            // the step where it is not on the device
     float gamma;
     uint32_t seed;
-    int32_t count;
 };
+static_assert(sizeof(Step) <= 4096, "a launch's arguments");
 
 // b^t by squaring, in binary64.
 __host__ __device__ inline double power(double b, int64_t t) {
@@ -200,51 +232,35 @@ __device__ __forceinline__ float advance(const Rates &c, float keep, float g, fl
     return __fsub_rn(__fmul_rn(x, keep), __fmul_rn(c.alpha, m / den));
 }
 
-// The tensor in which a tile lies, of those of the arguments.
-template <typename List>
-__device__ __forceinline__ int tensor_of(const List &a, uint32_t tile) {
-    int lo = 0, hi = a.count;   // the last whose first tile is at or before it
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.tensor[mid].first <= tile) lo = mid;
-        else hi = mid;
-    }
-    return lo;
-}
-
 template <typename G, bool kBytes, bool kDevice>
 __global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
-    const Tensor t = a.tensor[tensor_of(a, blockIdx.x)];
-    const int64_t tile0 = int64_t(blockIdx.x - t.first) * kTile;
+    const int which = tensor_of(a.tensors, blockIdx.x);
+    const int32_t size = a.tensors.size[which], blocks = (size + kStateBlock - 1) / kStateBlock;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int blocks = (t.size + kStateBlock - 1) / kStateBlock;
-    const G *g = static_cast<const G *>(t.g);
+    // a wave's block of 256 elements, four of a lane's each
+    const int block = int(blockIdx.x - a.tensors.first[which]) * kWaves + wave;
+    const int64_t at = int64_t(block) * kStateBlock + lane * 4;
+    const int left = int(min(int64_t(4), size - at));
+    const G *g = a.tensors.template pointer<const G>(kG, which) + at;
+    float *x = a.tensors.template pointer<float>(kX, which) + at;
+    float *m32 = a.tensors.template pointer<float>(kM, which) + at, *v32 = a.tensors.template pointer<float>(kV, which) + at;
+    uint8_t *m8 = a.tensors.template pointer<uint8_t>(kM, which), *r8 = a.tensors.template pointer<uint8_t>(kV, which);
+    float *m_scale = reinterpret_cast<float *>(m8 + int64_t(blocks) * kStateBlock) + block;
+    float *r_scale = reinterpret_cast<float *>(r8 + int64_t(blocks) * kStateBlock) + block;
 
-    // a wave's share is kTiles blocks of 256 elements, four of a lane's each
-    float gv[kTiles][4], xv[kTiles][4], mv[kTiles][4], vv[kTiles][4];
-    int left[kTiles];
+    float gv[4] = {}, xv[4] = {}, mv[4] = {}, vv[4] = {};
+    if (kBytes && block < blocks) {
+        values_of_m(*reinterpret_cast<const uint32_t *>(m8 + at), *m_scale, mv);
+        values_of_r(*reinterpret_cast<const uint32_t *>(r8 + at), *r_scale, vv);
 #pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-        const int block = int(tile0 / kStateBlock) + wave * kTiles + k;
-        const int64_t at = int64_t(block) * kStateBlock + lane * 4;
-        left[k] = int(min(int64_t(4), t.size - at));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) gv[k][i] = xv[k][i] = mv[k][i] = vv[k][i] = 0.0f;
-        if (kBytes && block < blocks) {
-            const uint8_t *m8 = static_cast<const uint8_t *>(t.m), *r8 = static_cast<const uint8_t *>(t.v);
-            const uint32_t mc = *reinterpret_cast<const uint32_t *>(m8 + at), rc = *reinterpret_cast<const uint32_t *>(r8 + at);
-            values_of_m(mc, reinterpret_cast<const float *>(m8 + int64_t(blocks) * kStateBlock)[block], mv[k]);
-            values_of_r(rc, reinterpret_cast<const float *>(r8 + int64_t(blocks) * kStateBlock)[block], vv[k]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vv[k][i] = __fmul_rn(vv[k][i], vv[k][i]);
-        }
-        if (left[k] > 0) {
-            load_pack<4>(g + at, left[k], gv[k]);
-            load_pack<4>(t.x + at, left[k], xv[k]);
-            if (!kBytes) {
-                load_pack<4>(static_cast<const float *>(t.m) + at, left[k], mv[k]);
-                load_pack<4>(static_cast<const float *>(t.v) + at, left[k], vv[k]);
-            }
+        for (int i = 0; i < 4; ++i) vv[i] = __fmul_rn(vv[i], vv[i]);
+    }
+    if (left > 0) {
+        load_pack<4>(g, left, gv);
+        load_pack<4>(x, left, xv);
+        if (!kBytes) {
+            load_pack<4>(m32, left, mv);
+            load_pack<4>(v32, left, vv);
         }
     }
 
@@ -260,105 +276,113 @@ __global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
         __syncthreads();
         c = s_rates;
     }
-    const float keep = float(1.0 - c.gamma * double(t.decay));
-    const uint32_t key = mixed(c.key + t.ordinal * 0x3C6EF373u);
-
+    if (block >= blocks) return;
+    const float keep = float(1.0 - c.gamma * double(a.decay[which]));
+    const uint32_t key = mixed(c.key + (a.tensors.ordinal + uint32_t(which)) * 0x3C6EF373u);
 #pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-        const int block = int(tile0 / kStateBlock) + wave * kTiles + k;
-        const int64_t at = int64_t(block) * kStateBlock + lane * 4;
-        if (block >= blocks) break;   // the whole wave's
+    for (int i = 0; i < 4; ++i) {
+        if (kDevice) gv[i] = __fmul_rn(gv[i], c.gain);
+        xv[i] = advance(c, keep, gv[i], xv[i], mv[i], vv[i]);
+    }
+    if (kBytes) {
+        uint32_t random[4], mc, rc;
+        float r[4], ms, rs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (kDevice) gv[k][i] = __fmul_rn(gv[k][i], c.gain);
-            xv[k][i] = advance(c, keep, gv[k][i], xv[k][i], mv[k][i], vv[k][i]);
+            random[i] = mixed((uint32_t(at + i) * 0x9E3779B1u) ^ key);
+            const bool in = i < left;   // what lies behind the tensor is zero
+            mv[i] = in ? mv[i] : 0.0f;
+            r[i] = in ? sqrtf(vv[i]) : 0.0f;
         }
-        if (kBytes) {
-            uint32_t random[4], mc, rc;
-            float r[4], ms, rs;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                random[i] = mixed((uint32_t(at + i) * 0x9E3779B1u) ^ key);
-                const bool in = i < left[k];   // what lies behind the tensor is zero
-                mv[k][i] = in ? mv[k][i] : 0.0f;
-                r[i] = in ? sqrtf(vv[k][i]) : 0.0f;
-            }
-            pack_block(mv[k], r, random, mc, rc, ms, rs);
-            uint8_t *m8 = static_cast<uint8_t *>(t.m), *r8 = static_cast<uint8_t *>(t.v);
-            *reinterpret_cast<uint32_t *>(m8 + at) = mc;
-            *reinterpret_cast<uint32_t *>(r8 + at) = rc;
-            if (lane == 0) {
-                reinterpret_cast<float *>(m8 + int64_t(blocks) * kStateBlock)[block] = ms;
-                reinterpret_cast<float *>(r8 + int64_t(blocks) * kStateBlock)[block] = rs;
-            }
-        }
-        if (left[k] <= 0) continue;
-        store_pack<4>(t.x + at, left[k], xv[k]);
-        if (t.copy != nullptr) store_pack<4>(t.copy + at, left[k], xv[k]);
-        if (!kBytes) {
-            store_pack<4>(static_cast<float *>(t.m) + at, left[k], mv[k]);
-            store_pack<4>(static_cast<float *>(t.v) + at, left[k], vv[k]);
-        }
+        pack_block(mv, r, random, mc, rc, ms, rs);
+        *reinterpret_cast<uint32_t *>(m8 + at) = mc;
+        *reinterpret_cast<uint32_t *>(r8 + at) = rc;
+        if (lane == 0) *m_scale = ms, *r_scale = rs;
+    }
+    if (left <= 0) return;
+    store_pack<4>(x, left, xv, kPast);
+    if (a.tensors.at[kCopy][which] != kNone)
+        store_pack<4>(a.tensors.template pointer<__bf16>(kCopy, which) + at, left, xv, kPast);
+    if (!kBytes) {
+        store_pack<4>(m32, left, mv, kPast);
+        store_pack<4>(v32, left, vv, kPast);
     }
 }
 
 // States of 8 bits from values of 32 and back: what a program does when it saves
 // or loads them.
-struct StateTensor {
-    float *m, *v;
-    void *m8, *v8;
-    int32_t size;
-    uint32_t first;
-};
+enum { kM32, kV32, kM8, kV8, kStateLists };
 
 struct States {
-    StateTensor tensor[kTensors];
-    int32_t count;
+    Tensors<kStateLists> tensors;
 };
 
 template <bool kWrite>
 __global__ __launch_bounds__(kBlock) void adamw_state_kernel(const States a) {
-    const StateTensor t = a.tensor[tensor_of(a, blockIdx.x)];
-    const int64_t tile0 = int64_t(blockIdx.x - t.first) * kTile;
+    const int which = tensor_of(a.tensors, blockIdx.x);
+    const int32_t size = a.tensors.size[which], blocks = (size + kStateBlock - 1) / kStateBlock;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int blocks = (t.size + kStateBlock - 1) / kStateBlock;
-    uint8_t *m8 = static_cast<uint8_t *>(t.m8), *r8 = static_cast<uint8_t *>(t.v8);
-    float *m_scale = reinterpret_cast<float *>(m8 + int64_t(blocks) * kStateBlock);
-    float *r_scale = reinterpret_cast<float *>(r8 + int64_t(blocks) * kStateBlock);
-#pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-        const int block = int(tile0 / kStateBlock) + wave * kTiles + k;
-        const int64_t at = int64_t(block) * kStateBlock + lane * 4;
-        const int left = int(min(int64_t(4), t.size - at));
-        if (block >= blocks) break;
-        if (kWrite) {   // rounded to nearest, ties up
-            const uint32_t half[4] = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-            float m[4] = {0.0f, 0.0f, 0.0f, 0.0f}, r[4] = {0.0f, 0.0f, 0.0f, 0.0f}, ms, rs;
-            uint32_t mc, rc;
-            if (left > 0) {
-                load_pack<4>(t.m + at, left, m);
-                load_pack<4>(t.v + at, left, r);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = sqrtf(r[i]);
-            pack_block(m, r, half, mc, rc, ms, rs);
-            *reinterpret_cast<uint32_t *>(m8 + at) = mc;
-            *reinterpret_cast<uint32_t *>(r8 + at) = rc;
-            if (lane == 0) m_scale[block] = ms, r_scale[block] = rs;
-        } else if (left > 0) {
-            const uint32_t mc = *reinterpret_cast<const uint32_t *>(m8 + at), rc = *reinterpret_cast<const uint32_t *>(r8 + at);
-            float m[4], v[4];
-            values_of_m(mc, m_scale[block], m);
-            values_of_r(rc, r_scale[block], v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], v[i]);
-            store_pack<4>(t.m + at, left, m);
-            store_pack<4>(t.v + at, left, v);
+    const int block = int(blockIdx.x - a.tensors.first[which]) * kWaves + wave;
+    if (block >= blocks) return;
+    const int64_t at = int64_t(block) * kStateBlock + lane * 4;
+    const int left = int(min(int64_t(4), size - at));
+    float *m32 = a.tensors.template pointer<float>(kM32, which) + at, *v32 = a.tensors.template pointer<float>(kV32, which) + at;
+    uint8_t *m8 = a.tensors.template pointer<uint8_t>(kM8, which), *r8 = a.tensors.template pointer<uint8_t>(kV8, which);
+    float *m_scale = reinterpret_cast<float *>(m8 + int64_t(blocks) * kStateBlock) + block;
+    float *r_scale = reinterpret_cast<float *>(r8 + int64_t(blocks) * kStateBlock) + block;
+    if (kWrite) {   // rounded to nearest, ties up
+        const uint32_t half[4] = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        float m[4] = {}, r[4] = {}, ms, rs;
+        uint32_t mc, rc;
+        if (left > 0) {
+            load_pack<4>(m32, left, m);
+            load_pack<4>(v32, left, r);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = sqrtf(r[i]);
+        pack_block(m, r, half, mc, rc, ms, rs);
+        *reinterpret_cast<uint32_t *>(m8 + at) = mc;
+        *reinterpret_cast<uint32_t *>(r8 + at) = rc;
+        if (lane == 0) *m_scale = ms, *r_scale = rs;
+    } else if (left > 0) {
+        float m[4], v[4];
+        values_of_m(*reinterpret_cast<const uint32_t *>(m8 + at), *m_scale, m);
+        values_of_r(*reinterpret_cast<const uint32_t *>(r8 + at), *r_scale, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __fmul_rn(v[i], v[i]);
+        store_pack<4>(m32, left, m, kPast);
+        store_pack<4>(v32, left, v, kPast);
     }
 }
 
-uint32_t tiles_of(int64_t size) { return uint32_t((size + kTile - 1) / kTile); }
+const void *const *list_of(const void *list) { return static_cast<const void *const *>(list); }
+
+// The next launch's tensors, from tensor i on: as many as fit.  Returns their tiles.
+template <int kLists>
+uint32_t take(Tensors<kLists> &a, const void *const *const (&lists)[kLists], const int64_t *size, int32_t count, int32_t &i) {
+    uint32_t tiles = 0;
+    a.ordinal = uint32_t(i);
+    for (int l = 0; l < kLists; ++l) a.base[l] = nullptr;
+    for (a.count = 0; i < count && a.count < kTensors; ++i, ++a.count) {
+        bool fits = true;
+        for (int l = 0; l < kLists; ++l) {
+            char *p = size[i] > 0 && lists[l] != nullptr ? static_cast<char *>(const_cast<void *>(lists[l][i])) : nullptr;
+            a.at[l][a.count] = kNone;
+            if (p == nullptr) continue;
+            if (a.base[l] == nullptr) a.base[l] = p;
+            // (of whole elements: a list is aligned to its type)
+            const int64_t far = (p - a.base[l]) / a.unit[l];
+            fits = fits && far > INT32_MIN && far <= INT32_MAX && far * a.unit[l] == p - a.base[l];
+            a.at[l][a.count] = int32_t(far);
+        }
+        const uint32_t more = uint32_t((size[i] + kStepTile - 1) / kStepTile);
+        if (!fits || (a.count > 0 && tiles + more > kMaxTiles)) break;
+        a.size[a.count] = int32_t(size[i]);
+        a.first[a.count] = tiles;
+        tiles += more;
+    }
+    return tiles;
+}
 
 template <typename G>
 void step(const Step &a, uint32_t tiles, bool bytes, bool device, hipStream_t stream) {
@@ -379,18 +403,14 @@ hipError_t launch_adamw(const AdamwArgs &c, hipStream_t stream) {
     a.given = c.step;
     const bool device = c.step_device != nullptr || c.factors != nullptr;
     set_step(a.rates, c.gamma, 1.0f, c.step, c.seed);
+    const int units[kStepLists] = {c.bf16 ? 2 : 4, 4, c.bytes ? 16 : 4, c.bytes ? 16 : 4, 2};
+    for (int l = 0; l < kStepLists; ++l) a.tensors.unit[l] = units[l];
+    const void *const *const lists[kStepLists] = {c.g, list_of(c.x), list_of(c.m), list_of(c.v), list_of(c.copy)};
     for (int32_t i = 0; i < c.count;) {
-        uint32_t tiles = 0;
-        for (a.count = 0; i < c.count && a.count < kTensors; ++i) {
-            if (c.size[i] == 0) continue;
-            Tensor &t = a.tensor[a.count++];
-            t.g = c.g[i], t.x = c.x[i], t.m = c.m[i], t.v = c.v[i];
-            t.copy = c.copy != nullptr ? static_cast<__bf16 *>(c.copy[i]) : nullptr;
-            t.size = int32_t(c.size[i]), t.decay = c.decay != nullptr ? c.decay[i] : 0.0f;
-            t.ordinal = uint32_t(i), t.first = tiles;
-            tiles += tiles_of(t.size);
-        }
-        if (a.count == 0) break;
+        const int32_t from = i;
+        const uint32_t tiles = take(a.tensors, lists, c.size, c.count, i);
+        for (int32_t k = from; k < i; ++k) a.decay[k - from] = c.decay != nullptr ? c.decay[k] : 0.0f;
+        if (tiles == 0) continue;
         if (c.bf16) step<__bf16>(a, tiles, c.bytes, device, stream);
         else step<float>(a, tiles, c.bytes, device, stream);
         const hipError_t err = hipGetLastError();
@@ -407,14 +427,11 @@ size_t adamw_state_size(int64_t size) {
 hipError_t launch_adamw_state(bool write, float *const *m, float *const *v, void *const *m8, void *const *v8,
                               const int64_t *size, int32_t count, hipStream_t stream) {
     States a;
+    for (int l = 0; l < kStateLists; ++l) a.tensors.unit[l] = l == kM32 || l == kV32 ? 4 : 16;
+    const void *const *const lists[kStateLists] = {list_of(m), list_of(v), list_of(m8), list_of(v8)};
     for (int32_t i = 0; i < count;) {
-        uint32_t tiles = 0;
-        for (a.count = 0; i < count && a.count < kTensors; ++i) {
-            if (size[i] == 0) continue;
-            a.tensor[a.count++] = StateTensor{m[i], v[i], m8[i], v8[i], int32_t(size[i]), tiles};
-            tiles += tiles_of(size[i]);
-        }
-        if (a.count == 0) break;
+        const uint32_t tiles = take(a.tensors, lists, size, count, i);
+        if (tiles == 0) continue;
         if (write) adamw_state_kernel<true><<<tiles, kBlock, 0, stream>>>(a);
         else adamw_state_kernel<false><<<tiles, kBlock, 0, stream>>>(a);
         const hipError_t err = hipGetLastError();

@@ -33,12 +33,13 @@ constexpr int kFewRounds = kFew / kBlock;
 constexpr int kFewAlone = 16;          // rows that one wave sums
 constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kSortAhead = 16;         // rounds of ids that a wave keeps
 constexpr int kMaxWords = 768;         // of one sorting workgroup: 54 KiB of LDS
 constexpr int kHot = 32;               // tokens; a lane of a half wave each
 constexpr int kAhead = 8;              // loads of a lane on their way at once
 constexpr int kJoinBlock = 512;
 constexpr int kJoinWaves = kJoinBlock / kWave;
-constexpr int64_t kFillBytes = 32768;  // of the table's rows that a workgroup writes
+constexpr int64_t kFewBytes = 32768, kSortedBytes = 16384;   // of the table's rows that a workgroup writes
 constexpr int kMaxRows = 1024;         // of one such workgroup
 
 // Flags beside a sorted token.
@@ -51,6 +52,7 @@ struct Lookup {
     int64_t ld_table, ld_out, ignore;
     int32_t tokens, vocab, width, parts, lanes_log2;
     float scale;
+    bool past;            // the results go past the caches
     uint32_t *status;
 };
 
@@ -88,7 +90,7 @@ __global__ __launch_bounds__(kBlock) void embed_forward_kernel(const Lookup a) {
     #pragma unroll
                 for (int i = 0; i < N; ++i) v[k][i] = __fmul_rn(v[k][i], a.scale);
             }
-            store_pack<N>(to + at, a.width - at, v[k]);
+            store_pack<N>(to + at, a.width - at, v[k], a.past);
         }
     }
 }
@@ -107,7 +109,7 @@ struct Spread {
     int32_t words, rows;  // of one workgroup that sorts, that writes rows
     int32_t first;        // workgroups before those that write rows
     float scale;
-    int accumulate;
+    bool accumulate, past;
     uint32_t *status;
     int32_t *start;       // [vocab + 1] in the sorted list
     Sorted *list;         // [tokens]
@@ -127,7 +129,7 @@ __device__ __forceinline__ void put_row(const Spread &a, int64_t word, int at, f
 #pragma unroll
         for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(old[i], sum[i]);
     }
-    store_pack<N>(to, a.width - at, sum);
+    store_pack<N>(to, a.width - at, sum, a.past);
 }
 
 // Sum of the rows row(0..n-1) at one lane's columns (at < width), in that order.
@@ -159,7 +161,7 @@ __device__ __forceinline__ void clear_rows(const Spread &a, int64_t first, int r
     for (uint32_t u = threadIdx.x; u < uint32_t(rows) * packs; u += blockDim.x) {
         const uint32_t r = u / packs;
         const int at = int(u - r * packs) * N;
-        if (empty(int(r))) store_pack<N>(static_cast<F *>(a.dtable) + (first + r) * a.ld_dtable + at, a.width - at, zero);
+        if (empty(int(r))) store_pack<N>(static_cast<F *>(a.dtable) + (first + r) * a.ld_dtable + at, a.width - at, zero, a.past);
     }
 }
 
@@ -264,19 +266,27 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
     // each wave counts its share of the tokens, and all that come before this workgroup's words
     const int share = (a.tokens + kSortBlock - 1) / kSortBlock * kWave;   // whole rounds
     const int lo = min(wave * share, a.tokens), hi = min(lo + share, a.tokens);
+    int32_t id[kSortAhead];   // -1: does not count, -2: nor is it a word
+    const auto fetch = [&](int t) {
+        int64_t wide[kSortAhead];
+#pragma unroll
+        for (int k = 0; k < kSortAhead; ++k)
+            wide[k] = t + k * kWave + lane < hi ? a.ids[t + k * kWave + lane] : a.ignore;
+#pragma unroll
+        for (int k = 0; k < kSortAhead; ++k)
+            id[k] = wide[k] == a.ignore ? -1 : wide[k] < 0 || wide[k] >= a.vocab ? -2 : int32_t(wide[k]);
+    };
     uint32_t before = 0;
     bool bad = false;
     uint32_t *mine = s_at + wave * a.words;
-    for (int t = lo; t < hi; t += kAhead * kWave) {
-        int64_t id[kAhead];
+    for (int t = lo; t < hi; t += kSortAhead * kWave) {
+        fetch(t);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) id[k] = t + k * kWave + lane < hi ? a.ids[t + k * kWave + lane] : a.ignore;
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (id[k] == a.ignore) continue;
-            if (id[k] < 0 || id[k] >= a.vocab) bad = true;
-            else if (id[k] < first) ++before;
-            else if (id[k] < first + words) atomicAdd(&mine[id[k] - first], 1u);
+        for (int k = 0; k < kSortAhead; ++k) {
+            const uint32_t own = uint32_t(id[k]) - uint32_t(first);
+            bad = bad || id[k] == -2;
+            before += uint32_t(id[k]) < uint32_t(first);
+            if (own < uint32_t(words)) atomicAdd(&mine[own], 1u);
         }
     }
     if (bad && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
@@ -319,14 +329,12 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
 
     // the tokens into their places, in order: a wave takes them as they come, and
     // lanes with the same word count those below them
-    for (int t = lo; t < hi; t += kAhead * kWave) {
-        int64_t id[kAhead];
+    for (int t = lo; t < hi; t += kSortAhead * kWave) {
+        if (hi - lo > kSortAhead * kWave) fetch(t);   // (else they are there)
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) id[k] = t + k * kWave + lane < hi ? a.ids[t + k * kWave + lane] : a.ignore;
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const bool in = id[k] != a.ignore && id[k] >= first && id[k] < first + words;
-            const int own = int(id[k] - first);
+        for (int k = 0; k < kSortAhead; ++k) {
+            const int own = id[k] - int(first);
+            const bool in = uint32_t(own) < uint32_t(words);
             uint64_t left = __ballot(in);
             while (left != 0) {
                 const int leader = __ffsll((unsigned long long)left) - 1;
@@ -462,7 +470,7 @@ size_t up16(size_t bytes) { return (bytes + 15) & ~size_t(15); }
 template <typename T, typename F>
 hipError_t spread(Spread a, hipStream_t stream) {
     constexpr int N = kPack<T, F>;
-    const int64_t rows = kFillBytes / (int64_t(a.width) * int(sizeof(F)));
+    const int64_t rows = (a.tokens <= kFew ? kFewBytes : kSortedBytes) / (int64_t(a.width) * int(sizeof(F)));
     a.rows = int32_t(rows < 1 ? 1 : rows > kMaxRows ? kMaxRows : rows);
     const uint32_t fills = uint32_t((a.vocab + a.rows - 1) / a.rows);
     if (a.tokens <= kFew) {
@@ -487,7 +495,8 @@ hipError_t spread(Spread a, hipStream_t stream) {
 hipError_t launch_embed_forward(const void *table, int64_t ld_table, bool table_bf16, const int64_t *ids, void *out,
                                 int64_t ld_out, bool bf16, int32_t tokens, int32_t vocab, int32_t width, float scale,
                                 int64_t ignore, uint32_t *status, hipStream_t stream) {
-    Lookup a{table, out, ids, ld_table, ld_out, ignore, tokens, vocab, width, 0, 0, scale, status};
+    Lookup a{table, out, ids, ld_table, ld_out, ignore, tokens, vocab, width, 0, 0, scale, false, status};
+    a.past = int64_t(tokens) * width * (bf16 ? 2 : 4) >= kPastCaches;
     const int pack = bf16 && table_bf16 ? 8 : 4, packs = (width + pack - 1) / pack;
     while ((1 << a.lanes_log2) < kWave && (1 << a.lanes_log2) < packs) ++a.lanes_log2;
     const int each = kLookAhead << a.lanes_log2;
@@ -519,6 +528,7 @@ hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, c
     a.ld_dout = ld_dout, a.ld_dtable = ld_dtable, a.ignore = ignore;
     a.tokens = tokens, a.vocab = vocab, a.width = width;
     a.scale = scale, a.accumulate = accumulate, a.status = status;
+    a.past = !accumulate && int64_t(vocab) * width * (table_bf16 ? 2 : 4) >= kPastCaches;
     a.list = reinterpret_cast<Sorted *>(ws);
     ws += up16(size_t(tokens) * sizeof(Sorted));
     a.start = reinterpret_cast<int32_t *>(ws);

@@ -34,6 +34,7 @@ struct Norm {
     int64_t ld_x, ld_dy, ld_out;
     int32_t rows, width;
     float eps;
+    bool past;              // y or dx goes past the caches
 };
 
 template <typename T>
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void norm_fo
             if (at >= a.width) break;
 #pragma unroll
             for (int i = 0; i < N; ++i) x[k][i] = fmaf((x[k][i] - s.rest) * s.rstd, w[k][i], b[k][i]);
-            store_pack<N>(to + at, a.width - at, x[k]);
+            store_pack<N>(to + at, a.width - at, x[k], a.past);
         }
     }
 }
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(kLong) void norm_forward_long_kernel(const Norm a) 
             if (a.bias != nullptr) load_pack<N>(static_cast<const F *>(a.bias) + at, a.width - at, b);
 #pragma unroll
             for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - m - s.rest) * s.rstd, w[i], b[i]);
-            store_pack<N>(to + at, a.width - at, x);
+            store_pack<N>(to + at, a.width - at, x, a.past);
         }
     }
 }
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
                 dw[k][i] = fmaf(dy[k][i], c * rstd, dw[k][i]);
                 dx[i] = fmaf(rstd, dy[k][i] * w[k][i], -p.even) - p.slope * c;
             }
-            if (there && at < a.width) store_pack<N>(to + at, a.width - at, dx);
+            if (there && at < a.width) store_pack<N>(to + at, a.width - at, dx, a.past);
         }
     }
     if (a.partial == nullptr) return;
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(kBlock) void norm_backward_long_kernel(const Norm a
             dw[i] = fmaf(dy[i], c * rstd, dw[i]);
             dx[i] = fmaf(rstd, dy[i] * w[i], -p.even) - p.slope * c;
         }
-        store_pack<N>(static_cast<T *>(a.out) + row * a.ld_out + at, a.width - at, dx);
+        store_pack<N>(static_cast<T *>(a.out) + row * a.ld_out + at, a.width - at, dx, a.past);
     }
     if (a.partial == nullptr) return;
     float *to = a.partial + int64_t(blockIdx.y) * 2 * a.width + at;
@@ -499,6 +500,7 @@ hipError_t launch_layernorm_forward(const void *x, int64_t ld_x, const void *wei
     Norm a{};
     a.x = x, a.weight = weight, a.bias = bias, a.out = y, a.mean = mean, a.rstd = rstd;
     a.ld_x = ld_x, a.ld_out = ld_y, a.rows = rows, a.width = width, a.eps = eps;
+    a.past = int64_t(rows) * width * (bf16 ? 2 : 4) >= kPastCaches;
     if (bf16 && weight_bf16) return run_forward<__bf16, __bf16>(a, stream);
     if (bf16) return run_forward<__bf16, float>(a, stream);
     if (weight_bf16) return run_forward<float, __bf16>(a, stream);
@@ -525,6 +527,7 @@ hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *we
     a.x = x, a.weight = weight, a.dy = dy, a.out = dx;
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx, a.rows = rows, a.width = width;
+    a.past = int64_t(rows) * width * (bf16 ? 2 : 4) >= kPastCaches;
     a.sums = static_cast<float *>(workspace);
     const bool long_rows = backward_hold(width, bf16 ? kRowPack<__bf16> : kRowPack<float>).threads == 0;
     if (dweight != nullptr || dbias != nullptr)

@@ -39,14 +39,25 @@ __device__ __forceinline__ void load_pack(const T *p, int left, float (&v)[N]) {
     for (int i = 0; i < N; ++i) v[i] = float(a[i]);
 }
 
+// What a call writes from here on does not stay in the 256 MB of the Infinity Cache
+// until it is read: it is stored past the caches.
+constexpr int64_t kPastCaches = int64_t(128) << 20;
+
 // bf16 results are rounded here, to nearest even.
 template <int N, typename T>
-__device__ __forceinline__ void store_pack(T *p, int left, const float (&v)[N]) {
+__device__ __forceinline__ void store_pack(T *p, int left, const float (&v)[N], bool past = false) {
     if (left >= N) {
         Pack<T, N> a;
 #pragma unroll
         for (int i = 0; i < N; ++i) a[i] = T(v[i]);
-        *reinterpret_cast<typename PackOf<T, N>::loose *>(p) = a;
+        typename PackOf<T, N>::loose *to = reinterpret_cast<typename PackOf<T, N>::loose *>(p);
+        if (past) {
+            asm volatile("");   // (both keep the two stores from becoming one)
+            __builtin_nontemporal_store(a, to);
+            asm volatile("");
+        } else {
+            *to = a;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
