@@ -266,32 +266,32 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
     // each wave counts its share of the tokens, and all that come before this workgroup's words
     const int share = (a.tokens + kSortBlock - 1) / kSortBlock * kWave;   // whole rounds
     const int lo = min(wave * share, a.tokens), hi = min(lo + share, a.tokens);
-    int32_t id[kSortAhead];   // -1: does not count, -2: nor is it a word
+    int32_t id[kSortAhead];      // -1: does not count
+    uint64_t in[kSortAhead];     // the lanes whose token is one of this workgroup's words
+    const uint32_t from = uint32_t(first), vocab = uint32_t(a.vocab);
     const auto fetch = [&](int t) {
         int64_t wide[kSortAhead];
 #pragma unroll
         for (int k = 0; k < kSortAhead; ++k)
             wide[k] = t + k * kWave + lane < hi ? a.ids[t + k * kWave + lane] : a.ignore;
 #pragma unroll
-        for (int k = 0; k < kSortAhead; ++k)
-            id[k] = wide[k] == a.ignore ? -1 : wide[k] < 0 || wide[k] >= a.vocab ? -2 : int32_t(wide[k]);
+        for (int k = 0; k < kSortAhead; ++k) {
+            const bool word = uint32_t(wide[k] >> 32) == 0u && uint32_t(wide[k]) < vocab;
+            id[k] = word && wide[k] != a.ignore ? int32_t(wide[k]) : -1;
+            in[k] = __ballot(uint32_t(id[k]) - from < uint32_t(words));
+            if (blockIdx.x == 0 && !word && wide[k] != a.ignore && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
+        }
     };
-    uint32_t before = 0;
-    bool bad = false;
+    uint32_t before = 0;   // of the wave
     uint32_t *mine = s_at + wave * a.words;
     for (int t = lo; t < hi; t += kSortAhead * kWave) {
         fetch(t);
 #pragma unroll
         for (int k = 0; k < kSortAhead; ++k) {
-            const uint32_t own = uint32_t(id[k]) - uint32_t(first);
-            bad = bad || id[k] == -2;
-            before += uint32_t(id[k]) < uint32_t(first);
-            if (own < uint32_t(words)) atomicAdd(&mine[own], 1u);
+            before += uint32_t(__popcll(__ballot(uint32_t(id[k]) < from)));
+            if (in[k] != 0 && uint32_t(id[k]) - from < uint32_t(words)) atomicAdd(&mine[uint32_t(id[k]) - from], 1u);
         }
     }
-    if (bad && blockIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) before += __shfl_xor(before, off);
     if (lane == 0) s_wave[wave] = before;
     __syncthreads();
     uint32_t base = 0;
@@ -334,26 +334,27 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
 #pragma unroll
         for (int k = 0; k < kSortAhead; ++k) {
             const int own = id[k] - int(first);
-            const bool in = uint32_t(own) < uint32_t(words);
-            uint64_t left = __ballot(in);
-            while (left != 0) {
-                const int leader = __ffsll((unsigned long long)left) - 1;
-                const int word = __shfl(own, leader);
-                const uint64_t same = __ballot(in && own == word);
-                if (in && own == word) {
-                    const uint32_t from = mine[word], at = from + lanes_below(same), n = s_total[word];
-                    uint32_t token = uint32_t(t + k * kWave + lane);
-                    if (n >= uint32_t(kHot)) {
-                        token |= kIsHot;
-                        if (at == s_start[word]) {
-                            token |= kIsFirst;
-                            a.lengths[at / kHot] = int32_t(n);
-                        }
+            uint64_t left = in[k], same = 0;
+            if (left == 0) continue;
+            while (left != 0) {   // a word at a time: the lanes that have it
+                const int word = __builtin_amdgcn_readlane(own, __ffsll((unsigned long long)left) - 1);
+                const uint64_t its = __ballot(own == word);
+                same = own == word ? its : same;
+                left &= ~its;
+            }
+            if ((in[k] >> lane) & 1u) {
+                const uint32_t next = mine[own], below = lanes_below(same), n = s_total[own];
+                const uint32_t at = next + below;
+                uint32_t token = uint32_t(t + k * kWave + lane);
+                if (n >= uint32_t(kHot)) {
+                    token |= kIsHot;
+                    if (at == s_start[own]) {
+                        token |= kIsFirst;
+                        a.lengths[at / kHot] = int32_t(n);
                     }
-                    a.list[at] = Sorted{token, int32_t(first) + word};
-                    if (lane == leader) mine[word] = from + uint32_t(__popcll(same));
                 }
-                left &= ~same;
+                a.list[at] = Sorted{token, int32_t(first) + own};
+                if (below == 0u) mine[own] = next + uint32_t(__popcll(same));
             }
         }
     }
@@ -420,42 +421,54 @@ __global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
 }
 
 // The pieces of a word, in order, from the piece in which it starts: each wave
-// sums a run of them, and the first joins the waves' sums.
+// sums a run of them, and the first joins the waves' sums.  A workgroup looks for
+// words in as many pieces as it has waves.
 template <typename T, typename F>
 __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) {
     constexpr int N = kPack<T, F>;
     __shared__ float s_sum[kJoinWaves][kWave * N];
+    __shared__ int32_t s_word[kJoinWaves], s_from[kJoinWaves], s_length[kJoinWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t piece = blockIdx.x, begin = piece * kHot;
-    const int n = int(min(int64_t(kHot), a.start[a.vocab] - begin));
-    if (n <= 0) return;
-    Sorted s{0u, -1};
-    if (lane < n) s = a.list[begin + lane];
-    const uint64_t starts = __ballot((s.token & kIsFirst) != 0u);
-    if (starts == 0) return;   // the same for every wave
-    const int from = __ffsll((unsigned long long)starts) - 1;
-    const int word = __shfl(s.word, from);
-    const int64_t pieces = (begin + from + a.lengths[piece] - 1) / kHot - piece + 1;
-    const int64_t each = (pieces + kJoinWaves - 1) / kJoinWaves;
-    const int64_t lo = min(wave * each, pieces), hi = min(lo + each, pieces);
+    const int64_t piece0 = int64_t(blockIdx.x) * kJoinWaves;
+    {
+        const int64_t piece = piece0 + wave;
+        Sorted s{0u, -1};
+        if (lane < kHot && piece * kHot + lane < a.start[a.vocab]) s = a.list[piece * kHot + lane];
+        const uint64_t starts = __ballot((s.token & kIsFirst) != 0u);
+        const int from = starts != 0 ? __ffsll((unsigned long long)starts) - 1 : 0;
+        const int word = __shfl(s.word, from);
+        if (lane == 0) {
+            s_word[wave] = starts != 0 ? word : -1;
+            s_from[wave] = from;
+            s_length[wave] = starts != 0 ? a.lengths[piece] : 0;
+        }
+    }
+    __syncthreads();
     const int parts = (a.width + kWave * N - 1) / (kWave * N);
-    for (int part = blockIdx.y; part < parts; part += gridDim.y) {
-        const int at = (part * kWave + lane) * N;
-        float sum[N] = {};
-        if (at < a.width)
-            sum_rows<N, kAhead>(a.width - at, int(hi - lo), [&](int j) {
-                const int64_t slot = (piece + lo + j) * 2 + (lo + j == 0 && from != 0);
-                return static_cast<const float *>(a.partial) + slot * a.width + at;
-            }, sum);
-        __syncthreads();
+    for (int i = 0; i < kJoinWaves; ++i) {
+        const int word = s_word[i], from = s_from[i];
+        if (word < 0) continue;   // the same for every wave
+        const int64_t piece = piece0 + i, pieces = (int64_t(from) + s_length[i] - 1) / kHot + 1;
+        const int64_t each = (pieces + kJoinWaves - 1) / kJoinWaves;
+        const int64_t lo = min(wave * each, pieces), hi = min(lo + each, pieces);
+        for (int part = blockIdx.y; part < parts; part += gridDim.y) {
+            const int at = (part * kWave + lane) * N;
+            float sum[N] = {};
+            if (at < a.width)
+                sum_rows<N, kAhead>(a.width - at, int(hi - lo), [&](int j) {
+                    const int64_t slot = (piece + lo + j) * 2 + (lo + j == 0 && from != 0);
+                    return static_cast<const float *>(a.partial) + slot * a.width + at;
+                }, sum);
+            __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) s_sum[wave][i * kWave + lane] = sum[i];
-        __syncthreads();
-        if (wave == 0 && at < a.width) {
-            for (int w = 1; w < kJoinWaves; ++w)
+            for (int k = 0; k < N; ++k) s_sum[wave][k * kWave + lane] = sum[k];
+            __syncthreads();
+            if (wave == 0 && at < a.width) {
+                for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], s_sum[w][i * kWave + lane]);
-            put_row<F, N>(a, word, at, sum);
+                    for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], s_sum[w][k * kWave + lane]);
+                put_row<F, N>(a, word, at, sum);
+            }
         }
     }
 }
@@ -486,7 +499,8 @@ hipError_t spread(Spread a, hipStream_t stream) {
     const int64_t pieces = pieces_of(a.tokens), parts = (a.width + kWave * N - 1) / (kWave * N);
     a.first = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
     embed_rows_kernel<T, F><<<uint32_t(a.first) + fills, kBlock, 0, stream>>>(a);
-    embed_join_kernel<T, F><<<dim3(uint32_t(pieces), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0, stream>>>(a);
+    embed_join_kernel<T, F><<<dim3(uint32_t((pieces + kJoinWaves - 1) / kJoinWaves), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0,
+                              stream>>>(a);
     return hipGetLastError();
 }
 
