@@ -6,7 +6,7 @@
 // Nothing but bytes: the rows that are looked up in, out; dout in, the table's
 // gradient out, whole, since words without a token get zeros.
 //
-// The gradient of up to kFew tokens is one launch: a workgroup for each token
+// The gradient of few tokens is one launch: a workgroup for each token
 // looks through all ids, ends if an earlier token has the same, and else sums the
 // rows of its word's tokens; others write the zeros of words without a token.
 //
@@ -28,22 +28,20 @@ namespace efs {
 
 namespace {
 
-constexpr int kFew = 1024;             // tokens that need no sorting
+constexpr int kFew = 4096;             // tokens that need no sorting, with short rows
+constexpr int kFewAny = 1024;          // with rows of any length
 constexpr int kFewRounds = kFew / kBlock;
 constexpr int kFewAlone = 16;          // rows that one wave sums
 constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kSortAhead = 16;         // rounds of ids that a wave keeps
-constexpr int kMaxWords = 768;         // of one sorting workgroup: 54 KiB of LDS
+constexpr int kMaxWords = 960;         // of one sorting workgroup: 60 KiB of LDS
 constexpr int kHot = 32;               // tokens; a lane of a half wave each
 constexpr int kAhead = 8;              // loads of a lane on their way at once
 constexpr int kJoinBlock = 512;
 constexpr int kJoinWaves = kJoinBlock / kWave;
 constexpr int64_t kFewBytes = 32768, kSortedBytes = 16384;   // of the table's rows that a workgroup writes
 constexpr int kMaxRows = 1024;         // of one such workgroup
-
-// Flags beside a sorted token.
-constexpr uint32_t kIsHot = 1u << 31, kIsFirst = 1u << 30, kTokenMask = kIsFirst - 1;
 
 struct Lookup {
     const void *table;
@@ -64,9 +62,9 @@ template <typename T, typename F>
 __global__ __launch_bounds__(kBlock) void embed_forward_kernel(const Lookup a) {
     constexpr int N = kPack<T, F>;
     const int lanes = 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int64_t units = int64_t(a.tokens) * a.parts, step = (int64_t(gridDim.x) * kBlock) >> a.lanes_log2;
-    for (int64_t unit = (int64_t(blockIdx.x) * kBlock + threadIdx.x) >> a.lanes_log2; unit < units; unit += step) {
-        const int32_t token = int32_t(unit / a.parts), part = int32_t(unit % a.parts);
+    const uint32_t units = uint32_t(a.tokens) * uint32_t(a.parts), step = (gridDim.x * kBlock) >> a.lanes_log2;
+    for (uint32_t unit = (blockIdx.x * kBlock + threadIdx.x) >> a.lanes_log2; unit < units; unit += step) {
+        const int32_t token = int32_t(unit / uint32_t(a.parts)), part = int32_t(unit % uint32_t(a.parts));
         const int64_t id = a.ids[token];
         const bool known = id >= 0 && id < a.vocab, counts = known && id != a.ignore;
         if (!known && id != a.ignore && lane == 0 && part == 0 && a.status != nullptr)
@@ -96,8 +94,7 @@ __global__ __launch_bounds__(kBlock) void embed_forward_kernel(const Lookup a) {
 }
 
 struct Sorted {
-    uint32_t token;   // with flags
-    int32_t word;
+    int32_t token, word;
 };
 
 struct Spread {
@@ -107,13 +104,13 @@ struct Spread {
     int64_t ld_dout, ld_dtable, ignore;
     int32_t tokens, vocab, width;
     int32_t words, rows;  // of one workgroup that sorts, that writes rows
-    int32_t first;        // workgroups before those that write rows
+    int32_t pieces, sums, clears;   // workgroups that sum pieces, that sum rows (these among them), that clear rows
+    uint64_t share;       // of the workgroups that sum, times 2^32
     float scale;
     bool accumulate, past;
     uint32_t *status;
     int32_t *start;       // [vocab + 1] in the sorted list
     Sorted *list;         // [tokens]
-    int32_t *lengths;     // [pieces] tokens of the word that starts in a piece
     float *partial;       // [pieces][2][width]
 };
 
@@ -167,15 +164,25 @@ __device__ __forceinline__ void clear_rows(const Spread &a, int64_t first, int r
 
 __device__ __forceinline__ bool counts(const Spread &a, int64_t id) { return id != a.ignore && id >= 0 && id < a.vocab; }
 
-// Up to kFew tokens.  Workgroups below a.first: a token's word, at four waves'
-// columns; the others: rows of words without a token.
+// The workgroups that sum (which >= 0: the how manieth) among those that clear
+// (which < 0: -1 - the how manieth), evenly spread: the ones wait for what they
+// read, the others fill the memory's time.
+__device__ __forceinline__ int dealt(const Spread &a) {
+    const uint64_t b = blockIdx.x;
+    const int before = int((b * a.share) >> 32), upto = int(((b + 1) * a.share) >> 32);
+    return upto > before ? before : -1 - (int(b) - before);
+}
+
+// Up to kFew tokens: a token's word, a workgroup for 64 packs of columns; or rows of
+// words without a token.
 template <typename T, typename F>
 __global__ __launch_bounds__(kBlock) void embed_few_kernel(const Spread a) {
     constexpr int N = kPack<T, F>;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    if (int(blockIdx.x) >= a.first) {
+    const int group = dealt(a);
+    if (group < 0) {
         __shared__ uint8_t s_there[kMaxRows];
-        const int64_t first = int64_t(blockIdx.x - a.first) * a.rows;
+        const int64_t first = int64_t(-1 - group) * a.rows;
         const int rows = int(min(int64_t(a.rows), a.vocab - first));
         for (int r = threadIdx.x; r < rows; r += kBlock) s_there[r] = 0;
         __syncthreads();
@@ -188,64 +195,72 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(const Spread a) {
         return;
     }
 
-    __shared__ uint64_t s_same[kFewRounds * kWaves];
+    __shared__ int32_t s_count[kFewRounds * kWaves];
     __shared__ int32_t s_token[kFew];
     __shared__ float s_sum[kWaves][kWave * N];
-    const int across = (a.width + kBlock * N - 1) / (kBlock * N);
-    const int token = int(blockIdx.x) / across, part0 = int(blockIdx.x) % across * kWaves;
+    const int parts = (a.width + kWave * N - 1) / (kWave * N), token = group / parts, part = group % parts;
     const int64_t word = a.ids[token];
     if (!counts(a, word)) {
-        if (word != a.ignore && part0 == 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
+        if (word != a.ignore && part == 0 && threadIdx.x == 0 && a.status != nullptr) atomicOr(a.status, kEmbedBadId);
         return;
     }
-    // the tokens of the same word, a bit each
+    // the tokens of the same word, a bit each; an earlier one's workgroup sums them
+    const int rounds = (a.tokens + kBlock - 1) / kBlock;
     uint64_t mine[kFewRounds];
+    bool earlier = false;
 #pragma unroll
     for (int k = 0; k < kFewRounds; ++k) {
-        const int t = k * kBlock + threadIdx.x;
-        mine[k] = __ballot(t < a.tokens && a.ids[t] == word);
-        if (lane == 0) s_same[k * kWaves + wave] = mine[k];
+        mine[k] = 0;
+        if (k >= rounds) continue;
+        const int t = k * kBlock + int(threadIdx.x);
+        const bool same = t < a.tokens && a.ids[t] == word;
+        earlier = earlier || (same && t < token);
+        mine[k] = __ballot(same);
+        if (lane == 0) s_count[k * kWaves + wave] = int(__popcll(mine[k]));
     }
-    __syncthreads();
-    int n = 0, before[kFewRounds] = {}, first = -1;
+    if (__syncthreads_or(earlier)) return;
+    int n = 0;
+    for (int k = 0; k < rounds; ++k)   // in the order of the tokens: round by round, wave by wave
 #pragma unroll
-    for (int i = 0; i < kFewRounds * kWaves; ++i) {
-        const uint64_t same = s_same[i];
-        if (i % kWaves == wave) before[i / kWaves] = n;
-        if (same != 0 && first < 0) first = i * kWave + __ffsll((unsigned long long)same) - 1;
-        n += __popcll(same);
+        for (int w = 0; w < kWaves; ++w) n += s_count[k * kWaves + w];
+    int before = 0, next = 0;
+#pragma unroll
+    for (int k = 0; k < kFewRounds; ++k) {
+        if (k >= rounds) continue;
+        before = next;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const int c = s_count[k * kWaves + w];
+            before += w < wave ? c : 0;
+            next += c;
+        }
+        if ((mine[k] >> lane) & 1u) s_token[before + int(lanes_below(mine[k]))] = k * kBlock + int(threadIdx.x);
     }
-    if (first != token) return;   // that one's workgroup sums them
-#pragma unroll
-    for (int k = 0; k < kFewRounds; ++k)
-        if ((mine[k] >> lane) & 1u) s_token[before[k] + int(lanes_below(mine[k]))] = k * kBlock + int(threadIdx.x);
     __syncthreads();
     const T *dout = static_cast<const T *>(a.dout);
-    if (n <= kFewAlone) {
-        const int at = ((part0 + wave) * kWave + lane) * N;
-        if (at >= a.width) return;
+    if (n <= kFewAlone) {   // a wave's columns each, in one of four workgroups
+        const int at = ((part + wave) * kWave + lane) * N;
+        if (part % kWaves != 0 || at >= a.width) return;
         float sum[N];
         sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(s_token[j]) * a.ld_dout + at; }, sum);
         put_row<F, N>(a, word, at, sum);
         return;
     }
+    // a wave's tokens each
     const int each = (n + kWaves - 1) / kWaves, lo = min(wave * each, n), hi = min(lo + each, n);
-    for (int part = part0; part < part0 + kWaves; ++part) {
-        const int at = (part * kWave + lane) * N;
-        float sum[N] = {};
-        if (at < a.width)
-            sum_rows<N, kAhead>(a.width - at, hi - lo,
+    const int at = (part * kWave + lane) * N;
+    float sum[N] = {};
+    if (at < a.width)
+        sum_rows<N, 2 * kAhead>(a.width - at, hi - lo,
                                 [&](int j) { return dout + int64_t(s_token[lo + j]) * a.ld_dout + at; }, sum);
-        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) s_sum[wave][i * kWave + lane] = sum[i];
-        __syncthreads();
-        if (wave == 0 && at < a.width) {
-            for (int w = 1; w < kWaves; ++w)
+    for (int i = 0; i < N; ++i) s_sum[wave][i * kWave + lane] = sum[i];
+    __syncthreads();
+    if (wave == 0 && at < a.width) {
+        for (int w = 1; w < kWaves; ++w)
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], s_sum[w][i * kWave + lane]);
-            put_row<F, N>(a, word, at, sum);
-        }
+            for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], s_sum[w][i * kWave + lane]);
+        put_row<F, N>(a, word, at, sum);
     }
 }
 
@@ -253,8 +268,6 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(const Spread a) {
 __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) {
     extern __shared__ uint32_t s_mem[];
     uint32_t *s_at = s_mem;                              // [kSortWaves][words]
-    uint32_t *s_start = s_mem + kSortWaves * a.words;    // [words]
-    uint32_t *s_total = s_start + a.words;               // [words]
     __shared__ uint32_t s_wave[kSortWaves];
     static_assert(kMaxWords <= kSortBlock, "a thread a word");
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -315,8 +328,6 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
     uint32_t start = base + upto - total;
     for (int w = 0; w < wave; ++w) start += s_wave[w];
     if (r < words) {
-        s_start[r] = start;
-        s_total[r] = total;
         a.start[first + r] = int32_t(start);
         if (first + r == a.vocab - 1) a.start[a.vocab] = int32_t(start + total);
         for (int w = 0; w < kSortWaves; ++w) {
@@ -343,22 +354,16 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
                 left &= ~its;
             }
             if ((in[k] >> lane) & 1u) {
-                const uint32_t next = mine[own], below = lanes_below(same), n = s_total[own];
-                const uint32_t at = next + below;
-                uint32_t token = uint32_t(t + k * kWave + lane);
-                if (n >= uint32_t(kHot)) {
-                    token |= kIsHot;
-                    if (at == s_start[own]) {
-                        token |= kIsFirst;
-                        a.lengths[at / kHot] = int32_t(n);
-                    }
-                }
-                a.list[at] = Sorted{token, int32_t(first) + own};
-                if (below == 0u) mine[own] = next + uint32_t(__popcll(same));
+                const uint32_t at = mine[own], below = lanes_below(same);
+                a.list[at + below] = Sorted{t + k * kWave + lane, int32_t(first) + own};
+                if (below == 0u) mine[own] = at + uint32_t(__popcll(same));
             }
         }
     }
 }
+
+// How many tokens a word has.
+__device__ __forceinline__ int tokens_of(const Spread &a, int word) { return a.start[word + 1] - a.start[word]; }
 
 // Sums of one piece of kHot sorted tokens, of those whose word has kHot tokens
 // or more: at most two such words meet a piece, one that is there at its first
@@ -369,11 +374,11 @@ __device__ __forceinline__ void sum_piece(const Spread &a, int64_t piece, int at
     const int lane = threadIdx.x & (kWave - 1);
     const int64_t begin = piece * kHot;
     const int n = int(min(int64_t(kHot), a.start[a.vocab] - begin));
-    Sorted s{0u, -1};
+    Sorted s{0, -1};
     if (lane < n) s = a.list[begin + lane];
-    const uint64_t hot = __ballot((s.token & kIsHot) != 0u);
+    const uint64_t hot = __ballot(lane < n && tokens_of(a, s.word) >= kHot);
     if (hot == 0) return;
-    const int token = int(s.token & kTokenMask);
+    const int token = s.token;
     const uint64_t head = hot & 1u ? __ballot(s.word == __shfl(s.word, 0) && lane < n) : 0;
     const T *rows = static_cast<const T *>(a.dout) + min(at, a.width - 1);
 #pragma unroll
@@ -390,34 +395,42 @@ __device__ __forceinline__ void sum_piece(const Spread &a, int64_t piece, int at
     }
 }
 
-// Workgroups below a.first: a piece's columns a wave; the others: rows of words.
+// Workgroups below a.pieces: a piece's columns a wave; other sums: a token's, if it
+// is the first of a word with fewer than kHot; or rows without a token.
 template <typename T, typename F>
 __global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
     constexpr int N = kPack<T, F>;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int parts = (a.width + kWave * N - 1) / (kWave * N);
-    if (int(blockIdx.x) < a.first) {
-        const int64_t units = ((a.start[a.vocab] + int64_t(kHot) - 1) / kHot) * parts;
-        for (int64_t u = int64_t(blockIdx.x) * kWaves + wave; u < units; u += int64_t(a.first) * kWaves)
-            sum_piece<T, F>(a, u / parts, (int(u % parts) * kWave + lane) * N);
+    const int group = dealt(a);
+    if (group >= 0 && group < a.pieces) {
+        const uint32_t units = (uint32_t(a.start[a.vocab]) + kHot - 1) / kHot * uint32_t(parts);
+        for (uint32_t u = uint32_t(group * kWaves + wave); u < units; u += uint32_t(a.pieces) * kWaves)
+            sum_piece<T, F>(a, int64_t(u / uint32_t(parts)), (int(u % uint32_t(parts)) * kWave + lane) * N);
+        return;
+    }
+    if (group >= 0) {
+        const uint32_t units = uint32_t(a.start[a.vocab]) * uint32_t(parts);
+        const T *dout = static_cast<const T *>(a.dout);
+        for (uint32_t u = uint32_t((group - a.pieces) * kWaves + wave); u < units; u += uint32_t(a.sums - a.pieces) * kWaves) {
+            const int32_t place = int32_t(u / uint32_t(parts));
+            const int at = (int(u % uint32_t(parts)) * kWave + lane) * N;
+            const Sorted *list = a.list + place;
+            const int32_t word = list[0].word;
+            const int n = tokens_of(a, word);
+            if (a.start[word] != place || n >= kHot || at >= a.width) continue;
+            float sum[N];
+            sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
+            put_row<F, N>(a, word, at, sum);
+        }
         return;
     }
     __shared__ int32_t s_start[kMaxRows + 1];
-    const int64_t first = int64_t(blockIdx.x - a.first) * a.rows;
+    const int64_t first = int64_t(-1 - group) * a.rows;
     const int rows = int(min(int64_t(a.rows), a.vocab - first));
     for (int r = threadIdx.x; r <= rows; r += kBlock) s_start[r] = a.start[first + r];
     __syncthreads();
-    if (!a.accumulate) clear_rows<F>(a, first, rows, [&](int r) { return s_start[r] == s_start[r + 1]; });
-    const T *dout = static_cast<const T *>(a.dout);
-    for (int u = wave; u < rows * parts; u += kWaves) {
-        const int r = u / parts, at = (u % parts * kWave + lane) * N;
-        const int n = s_start[r + 1] - s_start[r];
-        if (n == 0 || n >= kHot || at >= a.width) continue;
-        const Sorted *list = a.list + s_start[r];
-        float sum[N];
-        sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
-        put_row<F, N>(a, first + r, at, sum);
-    }
+    clear_rows<F>(a, first, rows, [&](int r) { return s_start[r] == s_start[r + 1]; });
 }
 
 // The pieces of a word, in order, from the piece in which it starts: each wave
@@ -432,15 +445,15 @@ __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) 
     const int64_t piece0 = int64_t(blockIdx.x) * kJoinWaves;
     {
         const int64_t piece = piece0 + wave;
-        Sorted s{0u, -1};
-        if (lane < kHot && piece * kHot + lane < a.start[a.vocab]) s = a.list[piece * kHot + lane];
-        const uint64_t starts = __ballot((s.token & kIsFirst) != 0u);
-        const int from = starts != 0 ? __ffsll((unsigned long long)starts) - 1 : 0;
-        const int word = __shfl(s.word, from);
-        if (lane == 0) {
-            s_word[wave] = starts != 0 ? word : -1;
-            s_from[wave] = from;
-            s_length[wave] = starts != 0 ? a.lengths[piece] : 0;
+        const int64_t place = piece * kHot + lane;
+        const bool there = lane < kHot && place < a.start[a.vocab];
+        const int word = there ? a.list[place].word : 0;
+        const int n = there ? tokens_of(a, word) : 0;
+        if (lane == 0) s_word[wave] = -1;
+        if (n >= kHot && a.start[word] == place) {   // one lane at most
+            s_word[wave] = word;
+            s_from[wave] = lane;
+            s_length[wave] = n;
         }
     }
     __syncthreads();
@@ -478,27 +491,35 @@ int64_t pieces_of(int32_t tokens) { return (int64_t(tokens) + kHot - 1) / kHot; 
 // A grid's threads are counted in 32 bits; the kernels step on where it ends.
 uint32_t grid_of(int64_t groups) { return uint32_t(groups < (1 << 20) ? groups : 1 << 20); }
 
+// Whether all ids are looked through for every token and 64 packs of its columns.
+bool few(int32_t tokens, int64_t parts) { return tokens <= kFewAny || tokens * parts <= kFew; }
+
 size_t up16(size_t bytes) { return (bytes + 15) & ~size_t(15); }
 
 template <typename T, typename F>
 hipError_t spread(Spread a, hipStream_t stream) {
     constexpr int N = kPack<T, F>;
-    const int64_t rows = (a.tokens <= kFew ? kFewBytes : kSortedBytes) / (int64_t(a.width) * int(sizeof(F)));
-    a.rows = int32_t(rows < 1 ? 1 : rows > kMaxRows ? kMaxRows : rows);
-    const uint32_t fills = uint32_t((a.vocab + a.rows - 1) / a.rows);
-    if (a.tokens <= kFew) {
-        a.first = a.tokens * ((a.width + kBlock * N - 1) / (kBlock * N));
-        const uint32_t groups = uint32_t(a.first) + (a.accumulate ? 0 : fills);
-        embed_few_kernel<T, F><<<groups, kBlock, 0, stream>>>(a);
+    const int64_t parts = (a.width + kWave * N - 1) / (kWave * N);
+    const int64_t rows = (few(a.tokens, parts) ? kFewBytes : kSortedBytes) / (int64_t(a.width) * int(sizeof(F)));
+    a.rows = int32_t(rows > kMaxRows ? kMaxRows : rows);
+    if (a.rows <= a.vocab >> 22) a.rows = (a.vocab >> 22) + 1;   // (a grid's threads again)
+    a.clears = a.accumulate ? 0 : (a.vocab + a.rows - 1) / a.rows;
+    const auto share = [&] { return ((uint64_t(a.sums) << 32) + uint64_t(a.sums + a.clears) - 1) / uint64_t(a.sums + a.clears); };
+    if (few(a.tokens, parts)) {
+        a.sums = int32_t(a.tokens * parts);
+        a.share = share();
+        embed_few_kernel<T, F><<<uint32_t(a.sums) + uint32_t(a.clears), kBlock, 0, stream>>>(a);
         return hipGetLastError();
     }
     const int each = (a.vocab + device_cu_count() - 1) / device_cu_count();
     a.words = each > kMaxWords ? kMaxWords : each;
-    const size_t lds = size_t(a.words) * (kSortWaves + 2) * sizeof(uint32_t);
+    const size_t lds = size_t(a.words) * kSortWaves * sizeof(uint32_t);
     embed_sort_kernel<<<uint32_t((a.vocab + a.words - 1) / a.words), kSortBlock, lds, stream>>>(a);
-    const int64_t pieces = pieces_of(a.tokens), parts = (a.width + kWave * N - 1) / (kWave * N);
-    a.first = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
-    embed_rows_kernel<T, F><<<uint32_t(a.first) + fills, kBlock, 0, stream>>>(a);
+    const int64_t pieces = pieces_of(a.tokens);
+    a.pieces = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
+    a.sums = a.pieces + int32_t(grid_of((int64_t(a.tokens) * parts + kWaves - 1) / kWaves));
+    a.share = share();
+    embed_rows_kernel<T, F><<<uint32_t(a.sums) + uint32_t(a.clears), kBlock, 0, stream>>>(a);
     embed_join_kernel<T, F><<<dim3(uint32_t((pieces + kJoinWaves - 1) / kJoinWaves), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0,
                               stream>>>(a);
     return hipGetLastError();
@@ -524,12 +545,12 @@ hipError_t launch_embed_forward(const void *table, int64_t ld_table, bool table_
     return hipGetLastError();
 }
 
-// [list][where words start][lengths][partial sums]; up to kFew tokens need none
+// [list][where words start][partial sums]; few tokens need none.  (Types whose
+// packs are longer are few no later.)
 size_t embed_workspace_size(int32_t tokens, int32_t vocab, int32_t width) {
-    if (tokens <= kFew) return 16;
-    const size_t pieces = size_t(pieces_of(tokens));
+    if (few(tokens, (int64_t(width) + kWave * 4 - 1) / (kWave * 4))) return 16;
     return up16(size_t(tokens) * sizeof(Sorted)) + up16((size_t(vocab) + 1) * sizeof(int32_t)) +
-           up16(pieces * sizeof(int32_t)) + up16(pieces * 2 * size_t(width) * sizeof(float));
+           up16(size_t(pieces_of(tokens)) * 2 * size_t(width) * sizeof(float));
 }
 
 hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, const int64_t *ids, void *dtable,
@@ -547,8 +568,6 @@ hipError_t launch_embed_backward(const void *dout, int64_t ld_dout, bool bf16, c
     ws += up16(size_t(tokens) * sizeof(Sorted));
     a.start = reinterpret_cast<int32_t *>(ws);
     ws += up16((size_t(vocab) + 1) * sizeof(int32_t));
-    a.lengths = reinterpret_cast<int32_t *>(ws);
-    ws += up16(size_t(pieces_of(tokens)) * sizeof(int32_t));
     a.partial = reinterpret_cast<float *>(ws);
     if (bf16 && table_bf16) return spread<__bf16, __bf16>(a, stream);
     if (bf16) return spread<__bf16, float>(a, stream);

@@ -31,6 +31,7 @@ struct Norm {
     float *mean, *rstd;     // forward: may be NULL
     float *partial;         // backward: [gridDim.x][2][width], NULL: no gradients of weight and bias
     float *sums;            // backward of long rows: [rows][4]
+    void *dweight, *dbias;  // backward by one workgroup, which writes them itself
     int64_t ld_x, ld_dy, ld_out;
     int32_t rows, width;
     float eps;
@@ -282,7 +283,8 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
         }
     }
     if (a.partial == nullptr) return;
-    // the groups' sums in order, then this workgroup's to the workspace
+    // the groups' sums in order, then this workgroup's to the workspace; one alone is done
+    const bool alone = gridDim.x == 1;
     float *to = a.partial + int64_t(blockIdx.x) * 2 * a.width;
 #pragma unroll
     for (int k = 0; k < kPacks; ++k) {
@@ -303,7 +305,10 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
 #pragma unroll
                         for (int i = 0; i < N; ++i) v[i] += s_join[(o * N + i) * kThreads + lane];
             }
-            if (group == 0 && at < a.width) store_pack<N>(to + which * int64_t(a.width) + at, a.width - at, v);
+            if (group > 0 || at >= a.width) continue;
+            F *result = static_cast<F *>(which == 0 ? a.dweight : a.dbias);
+            if (!alone) store_pack<N>(to + which * int64_t(a.width) + at, a.width - at, v);
+            else if (result != nullptr) store_pack<N>(result + at, a.width - at, v);
         }
     }
 }
@@ -423,11 +428,15 @@ Hold backward_hold(int32_t width, int pack) {
     return Hold{0, 0};
 }
 
+// Rounds of rows after which a workgroup alone, without a join, is as fast as many.
+constexpr int kAlone = 4;
+
 // Workgroups of the backward pass, whose partial sums the workspace holds: no
 // more than run at once.
 int backward_groups(int32_t rows, Hold h) {
     const int64_t each = h.threads == 0 ? 8 : h.threads < kBlock ? kBlock / h.threads : 1;
     const int64_t groups = (rows + each - 1) / each, most = h.threads == kLong ? 256 : 768;
+    if (h.threads != 0 && groups <= kAlone) return rows > 0;
     return int(groups < most ? groups : most);
 }
 
@@ -486,7 +495,7 @@ hipError_t run_backward(const Norm &a, F *dweight, F *dbias, hipStream_t stream)
             norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, each);
         }
     }
-    if (a.partial != nullptr)
+    if (a.partial != nullptr && (groups != 1 || h.threads == 0))
         norm_join_kernel<F><<<uint32_t((2 * int64_t(a.width) + kWave - 1) / kWave), kJoin, 0, stream>>>(
             a.partial, parts, a.width, dweight, dbias);
     return hipGetLastError();
@@ -529,6 +538,7 @@ hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *we
     a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx, a.rows = rows, a.width = width;
     a.past = int64_t(rows) * width * (bf16 ? 2 : 4) >= kPastCaches;
     a.sums = static_cast<float *>(workspace);
+    a.dweight = dweight, a.dbias = dbias;
     const bool long_rows = backward_hold(width, bf16 ? kRowPack<__bf16> : kRowPack<float>).threads == 0;
     if (dweight != nullptr || dbias != nullptr)
         a.partial = static_cast<float *>(workspace) + (long_rows ? int64_t(rows) * 4 : 0);

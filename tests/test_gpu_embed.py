@@ -102,7 +102,7 @@ def test_an_ignored_word_may_lie_in_the_table():
 
 @pytest.mark.parametrize("kind", ["uniform", "same", "zipf", "runs", "holes"])
 @pytest.mark.parametrize("tokens, vocab, width", [(1, 1, 1), (1, 40, 70), (31, 7, 33), (32, 7, 64), (33, 1, 129), (64, 3, 8),
-                                                  (700, 1000, 65), (3000, 97, 257), (5000, 20000, 16), (9999, 1500, 33)])
+                                                  (700, 1000, 65), (3000, 97, 257), (5000, 20000, 16), (9999, 1500, 33), (4096, 60, 40), (4097, 60, 40)])
 def test_backward(tokens, vocab, width, kind):
     say("embed_backward", tokens, vocab, width, kind)
     rng = np.random.default_rng(tokens * 31 + vocab)
@@ -113,30 +113,35 @@ def test_backward(tokens, vocab, width, kind):
 @pytest.mark.parametrize("add", [False, True])
 def test_backward_types(dtype, to, add):
     rng = np.random.default_rng(4)
-    for tokens, vocab, width in ((20, 50, 70), (600, 90, 523)):
+    for tokens, vocab, width in ((20, 50, 70), (600, 90, 523), (4500, 700, 267)):
         before = draw(rng, (vocab, width), to) if add else None
         check_backward(draw(rng, (tokens, width), dtype), words(rng, tokens, vocab, "zipf"), vocab, to, 8.0, before)
 
 
-def test_added_rows_without_a_token_keep_their_bits():
+# few tokens, and more than are handled without sorting
+@pytest.mark.parametrize("tokens", [400, 5000])
+def test_added_rows_without_a_token_keep_their_bits(tokens):
     rng = np.random.default_rng(5)
-    before = draw(rng, (500, 30), "fp32")
+    vocab = 5 * tokens // 4
+    before = draw(rng, (vocab, 30), "fp32")
     before[7] = float("nan")
-    ids = words(rng, 400, 500, "holes")
+    ids = words(rng, tokens, vocab, "holes")
     ids[ids == 7] = 8
-    got = gradient(draw(rng, (400, 30), "fp32"), ids, 500, before=before).cpu()
-    left = torch.from_numpy(np.setdiff1d(np.arange(500), ids))
+    got = gradient(draw(rng, (tokens, 30), "fp32"), ids, vocab, before=before).cpu()
+    left = torch.from_numpy(np.setdiff1d(np.arange(vocab), ids))
     assert_bits_equal(got[left].numpy(), before[left].numpy(), "rows without a token")
 
 
-def test_backward_of_strided_rows_leaves_what_lies_between():
+@pytest.mark.parametrize("tokens", [300, 6000])
+def test_backward_of_strided_rows_leaves_what_lies_between(tokens):
     rng = np.random.default_rng(6)
-    ids = torch.from_numpy(words(rng, 300, 40, "zipf")).to(DEV)
-    dout = draw(rng, (300, 77), "fp32").to(DEV)
-    wide = torch.full((40, 99), 5.0, device=DEV)
-    ws = efs.new_embed_workspace(300, 40, 60, DEV)
+    vocab = 40 if tokens < 1000 else 2000
+    ids = torch.from_numpy(words(rng, tokens, vocab, "zipf")).to(DEV)
+    dout = draw(rng, (tokens, 77), "fp32").to(DEV)
+    wide = torch.full((vocab, 99), 5.0, device=DEV)
+    ws = efs.new_embed_workspace(tokens, vocab, 60, DEV)
     efs.embed_backward(dout[:, 9:69], ids, wide[:, 1:61], ws)
-    dense = gradient(dout[:, 9:69].contiguous(), ids.cpu().numpy(), 40)
+    dense = gradient(dout[:, 9:69].contiguous(), ids.cpu().numpy(), vocab)
     assert torch.equal(wide[:, 1:61], dense)
     assert torch.all(wide[:, :1] == 5.0) and torch.all(wide[:, 61:] == 5.0)
 
@@ -163,23 +168,25 @@ def test_no_tokens():
 
 def test_no_token_that_counts():
     rng = np.random.default_rng(8)
-    for tokens in (5, 500):
+    for tokens in (5, 500, 5000):
         assert torch.all(check_backward(draw(rng, (tokens, 40), "fp32"), np.full(tokens, -100), 60) == 0.0)
 
 
-def test_rows_that_do_not_count_may_hold_anything():
+@pytest.mark.parametrize("tokens", [300, 5000])
+def test_rows_that_do_not_count_may_hold_anything(tokens):
     rng = np.random.default_rng(9)
-    ids = words(rng, 300, 50, "holes")
-    dout = draw(rng, (300, 20), "fp32")
+    ids = words(rng, tokens, 50, "holes")
+    dout = draw(rng, (tokens, 20), "fp32")
     clean = gradient(dout, ids, 50)
     dout[torch.from_numpy((ids < 0) | (ids >= 50))] = float("nan")
     assert torch.equal(gradient(dout, ids, 50), clean)
 
 
-def test_nan_stays_in_its_word():
+@pytest.mark.parametrize("tokens", [900, 5000])
+def test_nan_stays_in_its_word(tokens):
     rng = np.random.default_rng(10)
-    ids = words(rng, 900, 20, "zipf")
-    dout = draw(rng, (900, 70), "fp32")
+    ids = words(rng, tokens, 20, "zipf")
+    dout = draw(rng, (tokens, 70), "fp32")
     clean = gradient(dout, ids, 20)
     dout[450, 33] = float("nan")
     got = gradient(dout, ids, 20)
@@ -204,6 +211,13 @@ def test_status_word():
     status.zero_()
     gradient(dout, np.array([1, -1, 2, 3]), 10, status=status)
     assert efs.embed_status(status) == efs.EMBED_BAD_ID
+    many = np.full(5000, 3)
+    for at, want in ((None, 0), (4999, efs.EMBED_BAD_ID)):
+        status.zero_()
+        if at is not None:
+            many[at] = 10
+        gradient(draw(rng, (5000, 6), "fp32"), many, 10, status=status)
+        assert efs.embed_status(status) == want
 
 
 def test_gradient_against_differences():
