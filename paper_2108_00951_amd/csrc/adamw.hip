@@ -235,7 +235,7 @@ __device__ __forceinline__ float advance(const Rates &c, float keep, float g, fl
 template <typename G, bool kBytes, bool kDevice>
 __global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
     const int which = tensor_of(a.tensors, blockIdx.x);
-    const int32_t size = a.tensors.size[which], blocks = (size + kStateBlock - 1) / kStateBlock;
+    const int32_t size = a.tensors.size[which], blocks = (size - 1) / kStateBlock + 1;   // (a size may be the largest)
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     // a wave's block of 256 elements, four of a lane's each
     const int block = int(blockIdx.x - a.tensors.first[which]) * kWaves + wave;
@@ -320,7 +320,7 @@ struct States {
 template <bool kWrite>
 __global__ __launch_bounds__(kBlock) void adamw_state_kernel(const States a) {
     const int which = tensor_of(a.tensors, blockIdx.x);
-    const int32_t size = a.tensors.size[which], blocks = (size + kStateBlock - 1) / kStateBlock;
+    const int32_t size = a.tensors.size[which], blocks = (size - 1) / kStateBlock + 1;   // (a size may be the largest)
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int block = int(blockIdx.x - a.tensors.first[which]) * kWaves + wave;
     if (block >= blocks) return;

@@ -489,10 +489,10 @@ hipError_t run_backward(const Norm &a, F *dweight, F *dbias, hipStream_t stream)
         default: {
             const int64_t most = int64_t(device_cu_count()) * 2;
             norm_sums_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
-            const int each = (a.rows + groups - 1) / groups;
-            parts = (a.rows + each - 1) / each;
+            const int64_t each = (int64_t(a.rows) + groups - 1) / groups;
+            parts = int((a.rows + each - 1) / each);
             const int across = (a.width + kBlock * kRowPack<T> - 1) / (kBlock * kRowPack<T>);
-            norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, each);
+            norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, int32_t(each));
         }
     }
     if (a.partial != nullptr && (groups != 1 || h.threads == 0))

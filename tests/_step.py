@@ -97,8 +97,9 @@ class Adamw:
             t >>= 1
         return p
 
-    def step(self, t, ordinal, g, x, m, v, decay, lr_factor=1.0, gain=None):
-        """New x, m, v (as the state holds them)."""
+    def step(self, t, ordinal, g, x, m, v, decay, lr_factor=1.0, gain=None, start=0):
+        """New x, m, v (as the state holds them) of the elements from `start` on
+        (a multiple of 256)."""
         with np.errstate(all="ignore"):
             lr = float(self.lr) * float(np.float32(lr_factor))
             alpha = np.float32(lr / (1.0 - self.power(self.b1, t)))
@@ -111,14 +112,14 @@ class Adamw:
             v = self.b2 * v + (np.float32(1.0 - float(self.b2)) * g) * g
             x = x * keep - alpha * (m / (np.sqrt(v) * root + self.eps))
             if self.bits == 8:
-                dm, dr = dither(g.size, ordinal, t, self.seed)
+                dm, dr = dither(g.size, ordinal, t, self.seed, start)
                 m = np.copysign(in_8_bits(np.abs(m), 3, 0, dm), m)
                 r = in_8_bits(np.sqrt(v), 4, 1, dr)
                 v = r * r
         return x, m, v
 
 
-def dither(n, ordinal, step, seed):
+def dither(n, ordinal, step, seed, start=0):
     """Random numbers below 1 in steps of 2^-16 for m and for r."""
     mask = np.uint64(0xFFFFFFFF)
 
@@ -129,7 +130,7 @@ def dither(n, ordinal, step, seed):
         z = (z * np.uint64(0xBB67AE85)) & mask
         return z ^ (z >> np.uint64(16))
     key = mixed(np.uint64((seed + ordinal * 0x3C6EF373 + step * 0xA54FF53B) & 0xFFFFFFFF))
-    z = mixed(((np.arange(n, dtype=np.uint64) * np.uint64(0x9E3779B1)) & mask) ^ key)
+    z = mixed(((np.arange(start, start + n, dtype=np.uint64) * np.uint64(0x9E3779B1)) & mask) ^ key)
     return (z & np.uint64(0xFFFF)).astype(np.float64) / 65536, (z >> np.uint64(16)).astype(np.float64) / 65536
 
 

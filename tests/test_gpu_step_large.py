@@ -1,0 +1,163 @@
+"""The lookup, the layer norm and the AdamW step where offsets pass 32 bits and
+where results go past the caches."""
+import gc
+
+import numpy as np
+import pytest
+
+from tests import _step
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2108_00951_amd import binding as efs  # noqa: E402
+
+DEV = "cuda"
+PAST = 128 << 20   # bytes from which results are stored past the caches
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+@pytest.fixture(autouse=True)
+def give_back():
+    yield
+    gc.collect()
+    torch.cuda.empty_cache()
+
+
+def rand(shape, seed, dtype=torch.float32):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    out = torch.empty(shape, dtype=dtype, device=DEV)
+    for part in out.split(max(1, (1 << 28) // max(1, out[0].numel()))):
+        part.copy_(torch.randn(part.shape, generator=gen, device=DEV))
+    return out
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_results_past_the_caches(dtype):
+    """Sizes that are no multiple of anything; parts of each call, small enough to
+    stay in the caches, give the same bits."""
+    width = 1999
+    tokens = PAST // (width * dtype.itemsize) + 50
+    table = rand((3001, width), 1, dtype)
+    ids = torch.randint(0, 3001, (tokens,), device=DEV)
+    out, part = torch.empty(tokens, width, dtype=dtype, device=DEV), torch.empty(500, width, dtype=dtype, device=DEV)
+    efs.embed_forward(table, ids, out, scale=0.7)
+    for at in (0, tokens // 2, tokens - 500):
+        efs.embed_forward(table, ids[at:at + 500], part, scale=0.7)
+        assert torch.equal(part, out[at:at + 500])
+    w, b = rand((width,), 2), rand((width,), 3)
+    y, mean, rstd = torch.empty_like(out), torch.empty(tokens, device=DEV), torch.empty(tokens, device=DEV)
+    efs.layernorm_forward(out, w, b, y, mean, rstd)
+    dx = torch.empty_like(out)
+    ws = efs.new_layernorm_workspace(tokens, width, DEV)
+    efs.layernorm_backward(out, w, mean, rstd, y, dx, None, None, ws)
+    for at in (0, tokens // 2, tokens - 500):
+        s = slice(at, at + 500)
+        efs.layernorm_forward(out[s], w, b, part)
+        assert torch.equal(part, y[s])
+        efs.layernorm_backward(out[s], w, mean[s], rstd[s], y[s], part, None, None, ws)
+        assert torch.equal(part, dx[s])
+    # the table's gradient, against the same sums added to zeros, which stay in the caches
+    for count in (900, 15000):
+        vocab = PAST // (width * dtype.itemsize) + 50
+        ids = torch.randint(0, vocab, (count,), device=DEV)
+        ids[: count // 3] = 77
+        ws = efs.new_embed_workspace(count, vocab, width, DEV)
+        whole, added = torch.full((vocab, width), 3.0, dtype=dtype, device=DEV), torch.zeros((vocab, width), dtype=dtype, device=DEV)
+        efs.embed_backward(out[:count], ids, whole, ws, scale=0.7)
+        efs.embed_backward(out[:count], ids, added, ws, scale=0.7, accumulate=True)
+        assert torch.equal(whole, added)
+
+
+def test_tables_past_2_31_elements():
+    vocab, width = 530_000, 4099
+    say("table of", vocab * width)
+    table = rand((vocab, width), 4, torch.bfloat16)
+    ids = torch.tensor([vocab - 1, 0, 524_000, vocab - 2, 524_000], device=DEV)
+    out = torch.empty(5, width, dtype=torch.bfloat16, device=DEV)
+    efs.embed_forward(table, ids, out)
+    assert torch.equal(out, table[ids])
+    for count in (5, 5000):
+        where = ids.repeat(count // 5)
+        dout = rand((count, width), 5, torch.bfloat16)
+        dtable = table
+        dtable.fill_(7.0)
+        efs.embed_backward(dout, where, dtable, efs.new_embed_workspace(count, vocab, width, DEV))
+        # the same words in a small table
+        small = torch.empty(4, width, dtype=torch.bfloat16, device=DEV)
+        order = torch.tensor([0, 524_000, vocab - 2, vocab - 1], device=DEV)
+        efs.embed_backward(dout, torch.searchsorted(order, where), small, efs.new_embed_workspace(count, 4, width, DEV))
+        assert torch.equal(dtable[order], small)
+        dtable[order] = 0.0
+        assert not dtable.view(torch.int16).any()
+
+
+def test_tokens_past_2_31_elements():
+    tokens, width = 530_000, 4099
+    table = rand((40, width), 6, torch.bfloat16)
+    ids = torch.arange(tokens, device=DEV) % 40
+    out = torch.empty(tokens, width, dtype=torch.bfloat16, device=DEV)
+    efs.embed_forward(table, ids, out)
+    for at in (0, 524_000, tokens - 80):
+        assert torch.equal(out[at:at + 80], table[ids[at:at + 80]])
+    # 13,250 rows each of the same 40: small whole numbers, whose sums are exact
+    out.copy_(ids[:, None].expand(-1, width))
+    dtable = torch.empty(40, width, device=DEV)
+    efs.embed_backward(out, ids, dtable, efs.new_embed_workspace(tokens, 40, width, DEV))
+    assert torch.equal(dtable, (torch.arange(40.0, device=DEV) * (tokens // 40))[:, None].expand(-1, width))
+
+
+@pytest.mark.parametrize("rows, width", [(530_000, 4099), (33_000, 66_001)])
+def test_norms_past_2_31_elements(rows, width):
+    """The last rows give what they give alone."""
+    say("norm of", rows * width)
+    x, w, b = rand((rows, width), 7, torch.bfloat16), rand((width,), 8), rand((width,), 9)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    ws = efs.new_layernorm_workspace(rows, width, DEV)
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    efs.layernorm_forward(x, w, b, y, mean, rstd)
+    last = slice(rows - 300, rows)
+    alone = torch.empty(300, width, dtype=torch.bfloat16, device=DEV)
+    efs.layernorm_forward(x[last], w, b, alone)
+    assert torch.equal(alone, y[last])
+    dx = y.clone() if rows * width * 6 < 150e9 else y
+    efs.layernorm_backward(x, w, mean, rstd, y, dx, dw, db, ws)
+    efs.layernorm_backward(x[last], w, mean[last], rstd[last], alone, alone, None, None, ws)
+    assert torch.equal(alone, dx[last])
+    # sums of some columns, in 64 bits
+    for c in (0, width // 2, width - 1):
+        h = (x[:, c].double() - mean.double()) * rstd.double()
+        v = y[:, c].double()
+        for got, terms in ((dw[c], v * h), (db[c], v)):
+            # an addition for every row of a workgroup, in order, and the join's
+            assert abs(float(got) - float(terms.sum())) <= 2.0 ** -24 * (rows / 256 + 1000) * float(terms.abs().sum())
+
+
+def test_more_elements_than_2_31_in_one_step():
+    """Two tensors, one of the largest size; windows against the plain step."""
+    n = 2 ** 31 - 1
+    sizes = [n, 1000]
+    x = [torch.full((k,), 0.5, device=DEV) for k in sizes]
+    g = [torch.empty(k, dtype=torch.bfloat16, device=DEV) for k in sizes]
+    g[0].fill_(1e-3)
+    spots = [0, 2 ** 30, n - 511 - (n - 511) % 256]
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for at in spots:
+        part = g[0][at:at + 512]
+        part.copy_(torch.randn(part.shape, generator=gen, device=DEV))
+    g[1].copy_(torch.randn(1000, generator=gen, device=DEV))
+    m8, v8 = efs.new_adamw_state(sizes, DEV)
+    efs.adamw_apply(g, x, m8, v8, 1, lr=1e-2, weight_decay=0.1, seed=9)
+    m, v = ([torch.empty(k, device=DEV) for k in sizes] for _ in range(2))
+    efs.adamw_read_state(m8, v8, m, v)
+    plain = _step.Adamw(1e-2, seed=9, bits=8)
+    for tensor, at in [(0, s) for s in spots] + [(1, 0)]:
+        w = slice(at, min(at + 512, sizes[tensor]))
+        host = g[tensor][w].float().cpu().numpy()
+        zero = np.zeros_like(host)
+        want = plain.step(1, tensor, host, np.full_like(host, 0.5), zero, zero, 0.1, start=at)
+        for got, t in zip(want, (x[tensor], m[tensor], v[tensor])):
+            np.testing.assert_array_equal(t[w].cpu().numpy(), got, "tensor %d from %d" % (tensor, at))
