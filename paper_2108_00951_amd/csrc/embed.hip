@@ -56,7 +56,7 @@ struct Lookup {
 
 // A row's packs are dealt to 1..64 lanes, kLookAhead to each; longer rows are
 // several units.
-constexpr int kLookAhead = 4;
+constexpr int kLookAhead = 2;
 
 template <typename T, typename F>
 __global__ __launch_bounds__(kBlock) void embed_forward_kernel(const Lookup a) {
