@@ -524,7 +524,8 @@ efs_status embed_backward(const void *dout, int64_t ld_dout, int dtype, const in
  *   eps        finite, >= 0 (a constant row gives bias; with eps = 0 NaN).
  *   mean, rstd fp32[rows], overwritten, for the gradients; each may be NULL.
  * A row that holds NaN or infinities, or whose sum or sum of squares passes
- * fp32's range, gives NaN or zeros; the others are not affected. */
+ * fp32's range, gives NaN or zeros; the others are not affected (in the gradients:
+ * dweight and dbias take it in). */
 #define EFS_NORM_MAX_WIDTH (1 << 18)
 efs_status layernorm_forward(const void *x, int64_t ld_x, const void *weight, const void *bias, void *y,
                              int64_t ld_y, int dtype, int weight_dtype, int32_t rows, int32_t width, float eps,
@@ -585,7 +586,8 @@ efs_status layernorm_backward(const void *x, int64_t ld_x, const void *weight, c
  *              multiplied by the first (a schedule), every element of g by the
  *              second (one over a loss scale, a clipped norm's factor).
  *   seed       of the random rounding of states of 8 bits.
- * A tensor that is written, its states among them, must not overlap any other.
+ * A tensor that is written, its states among them, must not overlap any other,
+ * step_device or factors.
  * NaN or infinities in g spoil their own elements alone.
  *
  * States of 8 bits.  256 consecutive elements share a power of two s for m and one

@@ -900,28 +900,29 @@ def new_adamw_state(sizes: Sequence[int], device="cuda"):
 def _tensor_list(tensors, name, dtypes, sizes, optional=False):
     """A host array of the pointers of a list's tensors, of which each has its
     size; optional: some may be None."""
-    import torch
     if len(tensors) != len(sizes):
         raise ValueError("%s must have as many tensors as the other lists" % name)
     arr = (ctypes.c_void_p * max(len(tensors), 1))()
-    here = torch.cuda.current_device() if tensors else 0
-    kind = None
+    here, kind = None, None
     for i, t in enumerate(tensors):
         if t is None:
             if not optional:
                 raise TypeError("%s[%d] is None" % (name, i))
             continue
-        if t.dtype not in dtypes or (kind is not None and t.dtype != kind):
-            raise TypeError("%s must be %s, all alike; %s[%d] is %s"
-                            % (name, " or ".join(str(d) for d in dtypes), name, i, t.dtype))
-        kind = t.dtype
-        if not t.is_cuda or not t.is_contiguous():
-            raise TypeError("%s[%d] must be a contiguous device tensor" % (name, i))
-        if t.device.index != here:
-            raise ValueError("%s[%d] is on %s, and the current device is cuda:%d" % (name, i, t.device, here))
-        if t.numel() != sizes[i]:
-            raise ValueError("%s[%d] must have %d elements, has %d" % (name, i, sizes[i], t.numel()))
-        arr[i] = _ptr(t)
+        if t.dtype is not kind:
+            if kind is not None or t.dtype not in dtypes:
+                raise TypeError("%s must be %s, all alike; %s[%d] is %s"
+                                % (name, " or ".join(str(d) for d in dtypes), name, i, t.dtype))
+            kind, here = t.dtype, _device_of(t, "%s[%d]" % (name, i))
+        if t.get_device() != here:
+            _elsewhere(t, "%s[%d]" % (name, i), here)
+        if not t.is_contiguous():
+            raise TypeError("%s[%d] must be contiguous" % (name, i))
+        n = t.numel()
+        if n != sizes[i]:
+            raise ValueError("%s[%d] must have %d elements, has %d" % (name, i, sizes[i], n))
+        if n:
+            arr[i] = t.data_ptr()
     return arr
 
 

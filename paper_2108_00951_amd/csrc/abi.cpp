@@ -155,6 +155,12 @@ Span span_of(const Column &c, const int64_t *sizes, int32_t i) {
     return Span{at, at + bytes, c.name, c.written};
 }
 
+// Something that is read beside the lists (NULL: nothing).
+Span span_at(const char *name, const void *p, uintptr_t bytes) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return Span{at, p == nullptr ? at : at + bytes, name, false};
+}
+
 // Whether what is written meets anything else, over all tensors of all columns.
 // Layers of flat vectors come in ascending order and are merged as they are;
 // others are sorted.
@@ -948,6 +954,15 @@ efs_status adamw_apply(const void *const *g, int grad_dtype, float *const *x, vo
                                {"v", as_list(v), bytes ? 0 : 4, true},
                                {"copies", as_list(copies), 2, true}};
     if ((s = check_lists(name, columns, sizes, count)) != EFS_OK) return s;
+    const Span read[2] = {span_at("step_device", step_device, 8), span_at("factors", factors, 8)};
+    for (const Column &c : columns)
+        for (int32_t i = 0; c.written && c.at != nullptr && i < count; ++i)
+            for (const Span &r : read) {
+                if (c.at[i] == nullptr || sizes[i] == 0) continue;
+                const Span t = span_of(c, sizes, i);
+                if (t.at < r.end && r.at < t.end)
+                    return fail(EFS_EINVAL, "%s: tensors of %s and %s must not overlap", name, c.name, r.name);
+            }
     const efs::AdamwArgs args{g,    x,     m,     v,   copies, sizes,       decays,  count, grad_dtype == EFS_BF16, bytes,
                               gamma, beta1, beta2, eps, step,   step_device, factors, seed};
     return check_launch(efs::launch_adamw(args, static_cast<hipStream_t>(stream)), name);

@@ -163,7 +163,7 @@ __device__ __forceinline__ void pack_block(const float (&m)[4], const float (&r)
                                            uint32_t &m_codes, uint32_t &r_codes, float &m_scale, float &r_scale) {
     uint32_t mb[4], rb[4], c[4], d[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) mb[i] = __float_as_uint(m[i]) & kMagnitude, rb[i] = __float_as_uint(r[i]);
+    for (int i = 0; i < 4; ++i) mb[i] = __float_as_uint(m[i]) & kMagnitude, rb[i] = __float_as_uint(r[i]) & kMagnitude;
     bool whole_m, whole_r;
     const int em = scale_exponent(top_of(mb, whole_m)), er = scale_exponent(top_of(rb, whole_r));
     m_scale = two_to(em - 7), r_scale = two_to(er - 7);

@@ -73,19 +73,19 @@ __global__ __launch_bounds__(kBlock) void embed_forward_kernel(const Lookup a) {
         T *to = static_cast<T *>(a.out) + int64_t(token) * a.ld_out;
         const int first = (part * kLookAhead * lanes + lane) * N;
         float v[kLookAhead][N];
-    #pragma unroll
+#pragma unroll
         for (int k = 0; k < kLookAhead; ++k) {
             const int at = first + k * lanes * N;
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < N; ++i) v[k][i] = 0.0f;
             if (counts && at < a.width) load_pack<N>(from + at, a.width - at, v[k]);
         }
-    #pragma unroll
+#pragma unroll
         for (int k = 0; k < kLookAhead; ++k) {
             const int at = first + k * lanes * N;
             if (at >= a.width) break;
             if (counts) {   // (a row that does not count is +0 whatever the scale)
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < N; ++i) v[k][i] = __fmul_rn(v[k][i], a.scale);
             }
             store_pack<N>(to + at, a.width - at, v[k], a.past);

@@ -1,5 +1,8 @@
 """AdamW over lists of tensors, with states in 32 and in 8 bits, against the step
 done one rounded operation at a time, bit for bit."""
+import gc
+import weakref
+
 import numpy as np
 import pytest
 
@@ -195,7 +198,7 @@ def test_write_and_read_state():
     m = [(rng.standard_normal(n) * np.exp(4 * rng.standard_normal(n))).astype(np.float32) for n in sizes]
     v = [np.square(rng.standard_normal(n) * np.exp(4 * rng.standard_normal(n))).astype(np.float32) for n in sizes]
     m[3][:] = 0.0
-    v[3][:] = 0.0
+    v[3][:] = [0.0, -0.0, 0.0, -0.0, 0.0]
     m8, v8 = efs.new_adamw_state(sizes, DEV)
     efs.adamw_write_state([torch.from_numpy(t).to(DEV) for t in m], [torch.from_numpy(t).to(DEV) for t in v], m8, v8)
     gm, gv = ([torch.empty(n, device=DEV) for n in sizes] for _ in range(2))
@@ -209,6 +212,26 @@ def test_write_and_read_state():
         top_m, top_r = np.abs(m[i]).max(), np.sqrt(v[i]).max()
         assert np.all(np.abs(want_m - m[i]) <= np.maximum(2.0 ** -4 * np.abs(m[i]), 2.0 ** -17 * top_m))
         assert np.all(np.abs(want_r - np.sqrt(v[i])) <= np.maximum(2.0 ** -5 * np.sqrt(v[i]), 2.0 ** -17 * top_r) + 1e-30)
+
+
+def test_a_prepared_call_keeps_its_tensors():
+    model = Model([300, 5], 8, copy=True)
+    _, g = model.gradients()
+    lists = [g, model.dx, model.dm, model.dv, model.copy]
+    alive = [weakref.ref(t) for ts in lists for t in ts]
+    factors = torch.ones(2, device=DEV)
+    alive.append(weakref.ref(factors))
+    call = efs.prepare_adamw_apply(*lists[:4], lr=1e-3, copy=lists[4], factors=factors)
+    for ts in lists:
+        ts.clear()   # the caller's own lists, put to another use
+    del g, factors, lists, ts
+    gc.collect()
+    call(1)
+    torch.cuda.synchronize()
+    assert all(r() is not None for r in alive)
+    del call
+    gc.collect()
+    assert all(r() is None for r in alive)
 
 
 def test_empty_lists_do_nothing():

@@ -159,6 +159,16 @@ def test_adamw_refuses_what_overlaps(lib, descending):
                     assert b"must not overlap" in lib.efs_last_error_message()
 
 
+def test_adamw_refuses_rates_among_what_it_writes(lib):
+    c = Lists(lib)
+    for k in "xmvc":
+        for n in range(3):
+            for at in (c.at[k][n], c.at[k][n] + 592):
+                for what in ("step_device", "factors"):
+                    assert c.call(**{what: at}) == EINVAL
+                    assert b"must not overlap" in lib.efs_last_error_message()
+
+
 def test_reading_states_rejects_bad_arguments(lib):
     at = {k: [(i + 1) * 100 * FAKE + n * 8192 for n in range(2)] for i, k in enumerate(("m8", "v8", "m", "v"))}
 
@@ -226,3 +236,14 @@ def test_tensors_off_the_device_or_of_another_type_are_refused():
         binding.layernorm_forward(f, None, None, f.bfloat16())
     with pytest.raises(ValueError, match="width"):
         binding.layernorm_backward(f, None, f[:, 0], f[:, 0], f[:, :7], f, None, None, None)
+
+
+def test_lists_of_other_tensors_are_refused():
+    import torch
+    f = torch.zeros(3)
+    for lists, error, match in ((([f], [f], [f], [f]), TypeError, "device tensor"), (([f.half()], [f], [f], [f]), TypeError, "must be"),
+                                (([f], [f, f], [f], [f]), ValueError, "as many"), (([None], [f], [f], [f]), TypeError, "None")):
+        with pytest.raises(error, match=match):
+            binding.prepare_adamw_apply(*lists, lr=1e-3)
+    with pytest.raises(ValueError, match="as many"):
+        binding.adamw_read_state([], [], [f], [f])
