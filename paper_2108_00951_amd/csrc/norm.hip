@@ -29,9 +29,10 @@ struct Norm {
     const void *x, *weight, *bias, *dy;
     void *out;              // y or dx
     float *mean, *rstd;     // forward: may be NULL
-    float *partial;         // backward: [gridDim.x][2][width], NULL: no gradients of weight and bias
+    float *partial;         // backward: [groups][2][width], NULL: no partial sums of dw and db
     float *sums;            // backward of long rows: [rows][4]
-    void *dweight, *dbias;  // backward by one workgroup, which writes them itself
+    void *dweight, *dbias;  // backward of few rows: written by workgroups of columns
+    int32_t groups;         // backward: workgroups that take rows, before those of columns
     int64_t ld_x, ld_dy, ld_out;
     int32_t rows, width;
     float eps;
@@ -214,11 +215,46 @@ __device__ __forceinline__ Slopes slopes(const float (&s)[3], float rstd, int wi
     return Slopes{rest, rstd * (s[1] / n), rstd * rstd * (along / n)};
 }
 
+// Few rows: dw and db of kColumns columns from all rows, which stay in L2, with the
+// mean as it was stored; beside the workgroups that take rows, and no join.
+constexpr int kColumns = 8;
+
+template <typename T, typename F, int kSize>
+__device__ __forceinline__ void norm_columns(const Norm &a, int64_t first) {
+    __shared__ float s_part[kSize / kWave][2][kColumns];
+    constexpr int kSlots = kSize / kColumns;   // a thread's rows: its slot's, every kSlots
+    const int64_t column = first + threadIdx.x % kColumns;
+    const int slot = threadIdx.x / kColumns;
+    const T *x = static_cast<const T *>(a.x) + column, *dy = static_cast<const T *>(a.dy) + column;
+    float dw = 0.0f, db = 0.0f;
+    if (column < a.width) {
+#pragma unroll 8
+        for (int row = slot; row < a.rows; row += kSlots) {
+            const float v = float(dy[row * a.ld_dy]);
+            dw = fmaf(v, (float(x[row * a.ld_x]) - a.mean[row]) * a.rstd[row], dw);
+            db += v;
+        }
+    }
+#pragma unroll
+    for (int off = kColumns; off < kWave; off <<= 1) dw += __shfl_xor(dw, off), db += __shfl_xor(db, off);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (lane < kColumns) s_part[wave][0][lane] = dw, s_part[wave][1][lane] = db;
+    __syncthreads();
+    if (threadIdx.x >= 2 * kColumns || first + threadIdx.x % kColumns >= a.width) return;
+    const int which = threadIdx.x / kColumns;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kSize / kWave; ++w) sum += s_part[w][which][threadIdx.x % kColumns];
+    F *to = static_cast<F *>(which == 0 ? a.dweight : a.dbias);
+    if (to != nullptr) to[column] = F(sum);
+}
+
 template <typename T, typename F, int kThreads, int kPacks, int kSize>
 __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
     constexpr int N = kRowPack<T>, kGroups = kSize / kThreads;
     __shared__ float s_sums[2][kSize / kWave][3];
     __shared__ float s_join[kGroups > 1 ? (kGroups - 1) * kThreads * N : 1];
+    if (int(blockIdx.x) >= a.groups) return norm_columns<T, F, kSize>(a, int64_t(int(blockIdx.x) - a.groups) * kColumns);
     const int lane = threadIdx.x % kThreads, group = threadIdx.x / kThreads;
     float w[kPacks][N], dw[kPacks][N], db[kPacks][N];
     load_columns<F, N, kPacks, kThreads>(a.weight, a.width, 1.0f, w);
@@ -227,7 +263,7 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
 #pragma unroll
         for (int i = 0; i < N; ++i) dw[k][i] = db[k][i] = 0.0f;
     int turn = 0;
-    const int64_t step = int64_t(gridDim.x) * kGroups;
+    const int64_t step = int64_t(a.groups) * kGroups;
     const T *const xs = static_cast<const T *>(a.x), *const dys = static_cast<const T *>(a.dy);
     Pack<T, N> next_x[kPacks], next_dy[kPacks];   // a row on its way while the one before it is worked on
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -283,8 +319,7 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
         }
     }
     if (a.partial == nullptr) return;
-    // the groups' sums in order, then this workgroup's to the workspace; one alone is done
-    const bool alone = gridDim.x == 1;
+    // the groups' sums in order, then this workgroup's to the workspace
     float *to = a.partial + int64_t(blockIdx.x) * 2 * a.width;
 #pragma unroll
     for (int k = 0; k < kPacks; ++k) {
@@ -305,10 +340,7 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
 #pragma unroll
                         for (int i = 0; i < N; ++i) v[i] += s_join[(o * N + i) * kThreads + lane];
             }
-            if (group > 0 || at >= a.width) continue;
-            F *result = static_cast<F *>(which == 0 ? a.dweight : a.dbias);
-            if (!alone) store_pack<N>(to + which * int64_t(a.width) + at, a.width - at, v);
-            else if (result != nullptr) store_pack<N>(result + at, a.width - at, v);
+            if (group == 0 && at < a.width) store_pack<N>(to + which * int64_t(a.width) + at, a.width - at, v);
         }
     }
 }
@@ -428,15 +460,23 @@ Hold backward_hold(int32_t width, int pack) {
     return Hold{0, 0};
 }
 
-// Rounds of rows after which a workgroup alone, without a join, is as fast as many.
-constexpr int kAlone = 4;
+// Whether dw and db are summed over columns of all rows, which are read a second
+// time for that, from L2, instead of by rows with a join.  us, against the join:
+// 700 x 650 fp32 4.5 and 10.6, 1 x 1,024 bf16 3.3 and 7.0, 300 x 4,096 8.8 and 14.0,
+// 1,024 x 1,500 fp32 12.2 and 15.4; beyond: 1,500 x 1,024 bf16 12.3 and 10.9, 250 x
+// 8,000 fp32 17.0 and 15.6, 4,000 x 1,024 bf16 45 and 15.
+constexpr int kFewRows = 1024;
+constexpr int64_t kFewElements = 3 << 19;
+
+bool few_rows(int32_t rows, int32_t width, Hold h) {
+    return h.threads != 0 && rows <= kFewRows && int64_t(rows) * width <= kFewElements;
+}
 
 // Workgroups of the backward pass, whose partial sums the workspace holds: no
 // more than run at once.
 int backward_groups(int32_t rows, Hold h) {
     const int64_t each = h.threads == 0 ? 8 : h.threads < kBlock ? kBlock / h.threads : 1;
     const int64_t groups = (rows + each - 1) / each, most = h.threads == kLong ? 256 : 768;
-    if (h.threads != 0 && groups <= kAlone) return rows > 0;
     return int(groups < most ? groups : most);
 }
 
@@ -448,9 +488,9 @@ void forward(const Norm &a, hipStream_t stream) {
 }
 
 template <typename T, typename F, int kThreads, int kPacks>
-void backward(const Norm &a, int groups, hipStream_t stream) {
-    norm_backward_kernel<T, F, kThreads, kPacks, (kThreads < kBlock ? kBlock : kThreads)>
-        <<<groups, kThreads < kBlock ? kBlock : kThreads, 0, stream>>>(a);
+void backward(const Norm &a, int columns, hipStream_t stream) {
+    constexpr int kSize = kThreads < kBlock ? kBlock : kThreads;
+    norm_backward_kernel<T, F, kThreads, kPacks, kSize><<<uint32_t(a.groups + columns), kSize, 0, stream>>>(a);
 }
 
 template <typename T, typename F>
@@ -475,29 +515,37 @@ hipError_t run_forward(const Norm &a, hipStream_t stream) {
 }
 
 template <typename T, typename F>
-hipError_t run_backward(const Norm &a, F *dweight, F *dbias, hipStream_t stream) {
+hipError_t run_backward(Norm a, void *workspace, hipStream_t stream) {
     const Hold h = backward_hold(a.width, kRowPack<T>);
-    const int groups = backward_groups(a.rows, h);
-    int parts = groups;
-    if (a.rows > 0) switch (h.threads * 8 + h.packs) {
-        case 64 * 8 + 1: backward<T, F, 64, 1>(a, groups, stream); break;
-        case 64 * 8 + 2: backward<T, F, 64, 2>(a, groups, stream); break;
-        case 256 * 8 + 1: backward<T, F, 256, 1>(a, groups, stream); break;
-        case 256 * 8 + 2: backward<T, F, 256, 2>(a, groups, stream); break;
-        case 1024 * 8 + 1: backward<T, F, 1024, 1>(a, groups, stream); break;
-        case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, groups, stream); break;
+    a.groups = backward_groups(a.rows, h);
+    int parts = a.groups, columns = 0;
+    const bool gradients = a.dweight != nullptr || a.dbias != nullptr;
+    // (rows that are overwritten in place are not there for the columns)
+    if (gradients && a.out != a.x && a.out != a.dy && few_rows(a.rows, a.width, h)) {
+        columns = (a.width + kColumns - 1) / kColumns;
+    } else if (gradients) {
+        a.partial = static_cast<float *>(workspace) + (h.threads == 0 ? int64_t(a.rows) * 4 : 0);
+    }
+    a.sums = static_cast<float *>(workspace);
+    if (a.rows > 0 || columns > 0) switch (h.threads * 8 + h.packs) {
+        case 64 * 8 + 1: backward<T, F, 64, 1>(a, columns, stream); break;
+        case 64 * 8 + 2: backward<T, F, 64, 2>(a, columns, stream); break;
+        case 256 * 8 + 1: backward<T, F, 256, 1>(a, columns, stream); break;
+        case 256 * 8 + 2: backward<T, F, 256, 2>(a, columns, stream); break;
+        case 1024 * 8 + 1: backward<T, F, 1024, 1>(a, columns, stream); break;
+        case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, columns, stream); break;
         default: {
             const int64_t most = int64_t(device_cu_count()) * 2;
             norm_sums_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
-            const int64_t each = (int64_t(a.rows) + groups - 1) / groups;
+            const int64_t each = (int64_t(a.rows) + a.groups - 1) / a.groups;
             parts = int((a.rows + each - 1) / each);
             const int across = (a.width + kBlock * kRowPack<T> - 1) / (kBlock * kRowPack<T>);
             norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, int32_t(each));
         }
     }
-    if (a.partial != nullptr && (groups != 1 || h.threads == 0))
+    if (a.partial != nullptr)
         norm_join_kernel<F><<<uint32_t((2 * int64_t(a.width) + kWave - 1) / kWave), kJoin, 0, stream>>>(
-            a.partial, parts, a.width, dweight, dbias);
+            a.partial, parts, a.width, static_cast<F *>(a.dweight), static_cast<F *>(a.dbias));
     return hipGetLastError();
 }
 
@@ -537,17 +585,11 @@ hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *we
     a.mean = const_cast<float *>(mean), a.rstd = const_cast<float *>(rstd);
     a.ld_x = ld_x, a.ld_dy = ld_dy, a.ld_out = ld_dx, a.rows = rows, a.width = width;
     a.past = int64_t(rows) * width * (bf16 ? 2 : 4) >= kPastCaches;
-    a.sums = static_cast<float *>(workspace);
     a.dweight = dweight, a.dbias = dbias;
-    const bool long_rows = backward_hold(width, bf16 ? kRowPack<__bf16> : kRowPack<float>).threads == 0;
-    if (dweight != nullptr || dbias != nullptr)
-        a.partial = static_cast<float *>(workspace) + (long_rows ? int64_t(rows) * 4 : 0);
-    if (bf16 && weight_bf16)
-        return run_backward<__bf16, __bf16>(a, static_cast<__bf16 *>(dweight), static_cast<__bf16 *>(dbias), stream);
-    if (bf16) return run_backward<__bf16, float>(a, static_cast<float *>(dweight), static_cast<float *>(dbias), stream);
-    if (weight_bf16)
-        return run_backward<float, __bf16>(a, static_cast<__bf16 *>(dweight), static_cast<__bf16 *>(dbias), stream);
-    return run_backward<float, float>(a, static_cast<float *>(dweight), static_cast<float *>(dbias), stream);
+    if (bf16 && weight_bf16) return run_backward<__bf16, __bf16>(a, workspace, stream);
+    if (bf16) return run_backward<__bf16, float>(a, workspace, stream);
+    if (weight_bf16) return run_backward<float, __bf16>(a, workspace, stream);
+    return run_backward<float, float>(a, workspace, stream);
 }
 
 }  // namespace efs

@@ -119,7 +119,24 @@ def test_in_place(k):
     x = c.x.clone()
     dw, db = torch.empty_like(c.w), torch.empty_like(c.w)
     efs.layernorm_backward(x, c.w, c.mean, c.rstd, c.dy, x, dw, db, ws)
-    assert torch.equal(x, c.dx) and torch.equal(dw, c.dweight) and torch.equal(db, c.dbias)
+    assert torch.equal(x, c.dx)
+    # (the sums over the rows may be in another order)
+    c.out = {"dweight": dw, "dbias": db}
+    c.check()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 31, 33, 1024, 1025])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_weights_gradients_of_few_rows(rows, dtype):
+    """By columns of all rows, up to 1,024 of them; in place and with more, by rows."""
+    for k in (7, 8, 65, 1000):
+        c = make(rows, k, dtype, kind="columns")
+        c.check()
+        dx, dw, db = c.dy.clone(), torch.empty_like(c.w), torch.empty_like(c.w)
+        efs.layernorm_backward(c.x, c.w, c.mean, c.rstd, dx, dx, dw, db, efs.new_layernorm_workspace(rows, k, DEV))
+        assert torch.equal(dx, c.dx)
+        c.out = {"dweight": dw, "dbias": db}
+        c.check()
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
