@@ -40,8 +40,9 @@ constexpr int kHot = 32;               // tokens; a lane of a half wave each
 constexpr int kAhead = 8;              // loads of a lane on their way at once
 constexpr int kJoinBlock = 512;
 constexpr int kJoinWaves = kJoinBlock / kWave;
-constexpr int64_t kFewBytes = 32768, kSortedBytes = 16384;   // of the table's rows that a workgroup writes
+constexpr int64_t kFewBytes = 32768;   // of the table's rows that a workgroup of few tokens writes
 constexpr int kMaxRows = 1024;         // of one such workgroup
+constexpr int64_t kTileBytes = kSortBlock * 16, kRowTile = kBlock * 16;   // cleared by one, 16 bytes a thread
 
 struct Lookup {
     const void *table;
@@ -105,6 +106,8 @@ struct Spread {
     int32_t tokens, vocab, width;
     int32_t words, rows;  // of one workgroup that sorts, that writes rows
     int32_t pieces, sums, clears;   // workgroups that sum pieces, that sum rows (these among them), that clear rows
+    int32_t sorts;        // workgroups that sort, before those that clear
+    int64_t tiles;        // that these clear
     uint64_t share;       // of the workgroups that sum, times 2^32
     float scale;
     bool accumulate, past;
@@ -264,8 +267,33 @@ __global__ __launch_bounds__(kBlock) void embed_few_kernel(const Spread a) {
     }
 }
 
-// The tokens by word: the list, and where each word's start in it.
+// Zeros into a tile of the table, words with tokens or not: the rows of those, no more
+// than there are tokens, are written again.
+template <typename F>
+__device__ __forceinline__ void clear_table(const Spread &a, int64_t tile) {
+    constexpr int N = 16 / sizeof(F);
+    const float zero[N] = {};
+    if (a.ld_dtable == a.width) {   // without gaps: whole lines, whatever the rows
+        F *const table = static_cast<F *>(a.dtable);
+        const int64_t ahead = int64_t(reinterpret_cast<uintptr_t>(table) % 128 / sizeof(F)), all = int64_t(a.vocab) * a.width;
+        const int64_t e = (tile * kSortBlock + threadIdx.x) * N - ahead;
+        if (e >= 0 && e + N <= all) return store_pack<N>(table + e, N, zero, a.past);
+        for (int i = 0; i < N; ++i)
+            if (e + i >= 0 && e + i < all) table[e + i] = F(0.0f);
+        return;
+    }
+    const int64_t first = tile * a.rows;
+    clear_rows<F>(a, first, int(min(int64_t(a.rows), a.vocab - first)), [](int) { return true; });
+}
+
+// The tokens by word: the list, and where each word's start in it.  Workgroups behind
+// a.sorts clear the table meanwhile.
+template <typename F>
 __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) {
+    if (int(blockIdx.x) >= a.sorts) {
+        for (int64_t tile = int64_t(blockIdx.x) - a.sorts; tile < a.tiles; tile += a.clears) clear_table<F>(a, tile);
+        return;
+    }
     extern __shared__ uint32_t s_mem[];
     uint32_t *s_at = s_mem;                              // [kSortWaves][words]
     __shared__ uint32_t s_wave[kSortWaves];
@@ -395,42 +423,45 @@ __device__ __forceinline__ void sum_piece(const Spread &a, int64_t piece, int at
     }
 }
 
-// Workgroups below a.pieces: a piece's columns a wave; other sums: a token's, if it
-// is the first of a word with fewer than kHot; or rows without a token.
-template <typename T, typename F>
+// Workgroups below a.pieces: a piece's columns a wave; others: a token's, if it is the
+// first of a word with fewer than kHot.  kClear: among them, those that clear rows
+// without a token, whose bytes are whole tiles.
+template <typename T, typename F, bool kClear>
 __global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
     constexpr int N = kPack<T, F>;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int parts = (a.width + kWave * N - 1) / (kWave * N);
-    const int group = dealt(a);
-    if (group >= 0 && group < a.pieces) {
+    const int group = kClear ? dealt(a) : int(blockIdx.x);
+    if (kClear && group < 0) {
+        constexpr int kZeros = 16 / sizeof(F), kElements = kRowTile / sizeof(F);
+        const uint32_t across = uint32_t(a.width) / kElements;
+        const float zero[kZeros] = {};
+        for (uint32_t tile = uint32_t(-1 - group); tile < uint32_t(a.tiles); tile += uint32_t(a.clears)) {
+            const int32_t word = int32_t(tile / across);
+            F *to = static_cast<F *>(a.dtable) + word * a.ld_dtable + int64_t(tile % across) * kElements;
+            if (tokens_of(a, word) == 0) store_pack<kZeros>(to + threadIdx.x * kZeros, kZeros, zero, true);
+        }
+        return;
+    }
+    if (group < a.pieces) {
         const uint32_t units = (uint32_t(a.start[a.vocab]) + kHot - 1) / kHot * uint32_t(parts);
         for (uint32_t u = uint32_t(group * kWaves + wave); u < units; u += uint32_t(a.pieces) * kWaves)
             sum_piece<T, F>(a, int64_t(u / uint32_t(parts)), (int(u % uint32_t(parts)) * kWave + lane) * N);
         return;
     }
-    if (group >= 0) {
-        const uint32_t units = uint32_t(a.start[a.vocab]) * uint32_t(parts);
-        const T *dout = static_cast<const T *>(a.dout);
-        for (uint32_t u = uint32_t((group - a.pieces) * kWaves + wave); u < units; u += uint32_t(a.sums - a.pieces) * kWaves) {
-            const int32_t place = int32_t(u / uint32_t(parts));
-            const int at = (int(u % uint32_t(parts)) * kWave + lane) * N;
-            const Sorted *list = a.list + place;
-            const int32_t word = list[0].word;
-            const int n = tokens_of(a, word);
-            if (a.start[word] != place || n >= kHot || at >= a.width) continue;
-            float sum[N];
-            sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
-            put_row<F, N>(a, word, at, sum);
-        }
-        return;
+    const uint32_t units = uint32_t(a.start[a.vocab]) * uint32_t(parts);
+    const T *dout = static_cast<const T *>(a.dout);
+    for (uint32_t u = uint32_t((group - a.pieces) * kWaves + wave); u < units; u += uint32_t(a.sums - a.pieces) * kWaves) {
+        const int32_t place = int32_t(u / uint32_t(parts));
+        const int at = (int(u % uint32_t(parts)) * kWave + lane) * N;
+        const Sorted *list = a.list + place;
+        const int32_t word = list[0].word;
+        const int n = tokens_of(a, word);
+        if (a.start[word] != place || n >= kHot || at >= a.width) continue;
+        float sum[N];
+        sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
+        put_row<F, N>(a, word, at, sum);
     }
-    __shared__ int32_t s_start[kMaxRows + 1];
-    const int64_t first = int64_t(-1 - group) * a.rows;
-    const int rows = int(min(int64_t(a.rows), a.vocab - first));
-    for (int r = threadIdx.x; r <= rows; r += kBlock) s_start[r] = a.start[first + r];
-    __syncthreads();
-    clear_rows<F>(a, first, rows, [&](int r) { return s_start[r] == s_start[r + 1]; });
 }
 
 // The pieces of a word, in order, from the piece in which it starts: each wave
@@ -496,30 +527,55 @@ bool few(int32_t tokens, int64_t parts) { return tokens <= kFewAny || tokens * p
 
 size_t up16(size_t bytes) { return (bytes + 15) & ~size_t(15); }
 
+// The workgroups that sum among all (dealt()), rounded up: as many as there are come out.
+uint64_t share_of(const Spread &a) {
+    const uint64_t all = uint64_t(a.sums) + uint64_t(a.clears);
+    return all == 0 ? 0 : ((uint64_t(a.sums) << 32) + all - 1) / all;
+}
+
 template <typename T, typename F>
 hipError_t spread(Spread a, hipStream_t stream) {
     constexpr int N = kPack<T, F>;
     const int64_t parts = (a.width + kWave * N - 1) / (kWave * N);
-    const int64_t rows = (few(a.tokens, parts) ? kFewBytes : kSortedBytes) / (int64_t(a.width) * int(sizeof(F)));
-    a.rows = int32_t(rows > kMaxRows ? kMaxRows : rows);
-    if (a.rows <= a.vocab >> 22) a.rows = (a.vocab >> 22) + 1;   // (a grid's threads again)
-    a.clears = a.accumulate ? 0 : (a.vocab + a.rows - 1) / a.rows;
-    const auto share = [&] { return ((uint64_t(a.sums) << 32) + uint64_t(a.sums + a.clears) - 1) / uint64_t(a.sums + a.clears); };
+    const int64_t row_bytes = int64_t(a.width) * int(sizeof(F));
     if (few(a.tokens, parts)) {
+        const int64_t rows = kFewBytes / row_bytes;
+        a.rows = int32_t(rows > kMaxRows ? kMaxRows : rows);
+        if (a.rows <= a.vocab >> 22) a.rows = (a.vocab >> 22) + 1;   // (a grid's threads again)
+        a.clears = a.accumulate ? 0 : (a.vocab + a.rows - 1) / a.rows;
         a.sums = int32_t(a.tokens * parts);
-        a.share = share();
+        a.share = share_of(a);
         embed_few_kernel<T, F><<<uint32_t(a.sums) + uint32_t(a.clears), kBlock, 0, stream>>>(a);
         return hipGetLastError();
     }
+    // How rows without a token are cleared.  Large tables whose rows are whole tiles of 4
+    // KiB: by the second launch, which knows those rows, and in the order of the table.
+    // Others, all of the table while the tokens are sorted.  us, against the second for all:
+    // 16,384 tokens x 131,072 x 2,048 fp32 183 and 212; the second, against the first with
+    // tiles that meet several rows: 131,072 x 1,056 fp32 116 and 130, 1,055 bf16 75 and 91,
+    // 1,000,000 x 64 76 and 96.
+    const bool whole = !a.accumulate && a.past && row_bytes % kRowTile == 0 && a.ld_dtable * int(sizeof(F)) % 128 == 0 &&
+                       reinterpret_cast<uintptr_t>(a.dtable) % 128 == 0;
+    a.rows = int32_t(kTileBytes / row_bytes < 1 ? 1 : kTileBytes / row_bytes);
+    a.tiles = a.accumulate || whole ? 0 : a.ld_dtable != a.width ? (a.vocab + a.rows - 1) / a.rows :
+              (a.vocab * row_bytes + 127 + kTileBytes - 1) / kTileBytes;
+    a.clears = int32_t(grid_of(a.tiles));
     const int each = (a.vocab + device_cu_count() - 1) / device_cu_count();
     a.words = each > kMaxWords ? kMaxWords : each;
+    a.sorts = (a.vocab + a.words - 1) / a.words;
     const size_t lds = size_t(a.words) * kSortWaves * sizeof(uint32_t);
-    embed_sort_kernel<<<uint32_t((a.vocab + a.words - 1) / a.words), kSortBlock, lds, stream>>>(a);
+    embed_sort_kernel<F><<<uint32_t(a.sorts + a.clears), kSortBlock, lds, stream>>>(a);
     const int64_t pieces = pieces_of(a.tokens);
     a.pieces = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
     a.sums = a.pieces + int32_t(grid_of((int64_t(a.tokens) * parts + kWaves - 1) / kWaves));
-    a.share = share();
-    embed_rows_kernel<T, F><<<uint32_t(a.sums) + uint32_t(a.clears), kBlock, 0, stream>>>(a);
+    if (whole) {
+        a.tiles = a.vocab * (row_bytes / kRowTile);
+        a.clears = int32_t(a.tiles < 1 << 23 ? a.tiles : 1 << 23);
+        a.share = share_of(a);
+        embed_rows_kernel<T, F, true><<<uint32_t(a.sums) + uint32_t(a.clears), kBlock, 0, stream>>>(a);
+    } else {
+        embed_rows_kernel<T, F, false><<<uint32_t(a.sums), kBlock, 0, stream>>>(a);
+    }
     embed_join_kernel<T, F><<<dim3(uint32_t((pieces + kJoinWaves - 1) / kJoinWaves), uint32_t(parts < 64 ? parts : 64)), kJoinBlock, 0,
                               stream>>>(a);
     return hipGetLastError();

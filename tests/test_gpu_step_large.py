@@ -70,6 +70,34 @@ def test_results_past_the_caches(dtype):
         efs.embed_backward(out[:count], ids, whole, ws, scale=0.7)
         efs.embed_backward(out[:count], ids, added, ws, scale=0.7, accumulate=True)
         assert torch.equal(whole, added)
+        # a layer of a flat vector, off every alignment
+        flat = torch.full((vocab * width + 9,), 3.0, dtype=dtype, device=DEV)
+        layer = flat[5:-4].view(vocab, width)
+        efs.embed_backward(out[:count], ids, layer, ws, scale=0.7)
+        assert torch.equal(layer, added)
+        assert torch.all(flat[:5] == 3.0) and torch.all(flat[-4:] == 3.0)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("width", [8, 13, 250, 1024, 2048, 4100])
+def test_tables_cleared_past_the_caches(width, dtype):
+    """Rows shorter and longer than what a workgroup clears, words that have tokens
+    at the table's ends and next to each other."""
+    vocab = PAST // (width * dtype.itemsize) + 7
+    count = 5000
+    gen = torch.Generator(device=DEV).manual_seed(width)
+    ids = torch.randint(0, vocab, (count,), generator=gen, device=DEV)
+    ids[:4] = torch.tensor([0, vocab - 1, 5, 6], device=DEV)
+    dout = rand((count, width), 3)
+    for offset in (0, 3):
+        flat = torch.full((vocab * width + offset + 2,), 3.0, dtype=dtype, device=DEV)
+        layer = flat[offset:-2].view(vocab, width)
+        ws = efs.new_embed_workspace(count, vocab, width, DEV)
+        efs.embed_backward(dout, ids, layer, ws)
+        added = torch.zeros(vocab, width, dtype=dtype, device=DEV)
+        efs.embed_backward(dout, ids, added, ws, accumulate=True)
+        assert torch.equal(layer, added)
+        assert torch.all(flat[:offset] == 3.0) and torch.all(flat[-2:] == 3.0)
 
 
 def test_tables_past_2_31_elements():
