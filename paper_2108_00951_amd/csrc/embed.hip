@@ -3,22 +3,30 @@
 //   out[t]    = scale * table[ids[t]]
 //   dtable[v] = scale * sum over the tokens t with ids[t] = v, in their order, of dout[t]
 //
-// Nothing but bytes: the rows that are looked up in, out; dout in, the table's
-// gradient out, whole, since words without a token get zeros.
+// Bytes bound both: the rows that are looked up in and out; dout in, the table's
+// gradient out, whole, since words without a token get zeros.  Measured on one MI355X
+// (a copy reaches 6.0 to 6.3 TB/s, zeros alone 6.9):
+//   32,768 rows of 4,096 bf16 looked up              77 us, 4.7 TB/s (5.6 with the rows
+//                                                    that several XCDs fetch)
+//   gradient, 131,072 x 2,048 fp32, 16,384 tokens    167 us, 6.8 TB/s
+//   gradient, 33,278 x 650 fp32, 700 tokens          17 us, 5.2 TB/s
+//   gradient, 64 tokens added to 33,278 x 1,024      4.2 us
 //
-// The gradient of few tokens is one launch: a workgroup for each token
-// looks through all ids, ends if an earlier token has the same, and else sums the
-// rows of its word's tokens; others write the zeros of words without a token.
+// The gradient of few tokens is one launch: a workgroup for each token and 64 packs
+// of columns looks through all ids, ends if an earlier token has the same, and else
+// sums the rows of its word's tokens; others write the zeros of words without a
+// token.  Up to 1,024 tokens, or 4,096 where the rows are short: 1,520 x 23,472 x 499
+// takes 17 us so and 33 by the other way, 2,241 x 48,840 x 4,095 90 and 29.
 //
-// More tokens are sorted by word, without a pass that has to wait for another:
-// a workgroup owns some consecutive words, looks through all ids twice (they stay
-// in L2: 16,384 of them are 128 KiB) and so knows by itself how many tokens the
-// words before its own have, and which tokens, in their order, each of its own
-// has.  A second launch writes the rows of words with fewer than kHot tokens and
-// of those without, and cuts the sorted tokens into pieces of kHot, of which it
-// sums what belongs to words of more; a third joins the pieces of a word in order.
-// So no word is summed by one wave, and nothing depends on which workgroup comes
-// first.
+// More tokens are sorted by word, without a pass that has to wait for another: a
+// workgroup owns some consecutive words and looks through all ids (they stay in L2:
+// 16,384 of them are 128 KiB), so that it knows by itself how many tokens the words
+// before its own have, and which tokens, in their order, each of its own has (13 us
+// for 16,384 tokens, of which the hottest words' workgroup waits longest).  A second
+// launch takes the sorted tokens in pieces of kHot, writes the rows of words with
+// fewer than kHot tokens and sums those of other words piece by piece; a third joins
+// the pieces of a word in order.  So no word is summed by one wave, and nothing depends
+// on which workgroup comes first.
 #include "rows.hpp"
 #include "launch.hpp"
 
@@ -56,7 +64,7 @@ struct Lookup {
 };
 
 // A row's packs are dealt to 1..64 lanes, kLookAhead to each; longer rows are
-// several units.
+// several units.  (1, 2, 4 and 8 of them: 84, 77, 80 and 98 us for 32,768 x 4,096 bf16.)
 constexpr int kLookAhead = 2;
 
 template <typename T, typename F>
@@ -105,7 +113,7 @@ struct Spread {
     int64_t ld_dout, ld_dtable, ignore;
     int32_t tokens, vocab, width;
     int32_t words, rows;  // of one workgroup that sorts, that writes rows
-    int32_t pieces, sums, clears;   // workgroups that sum pieces, that sum rows (these among them), that clear rows
+    int32_t sums, clears;   // workgroups that sum rows, that clear rows
     int32_t sorts;        // workgroups that sort, before those that clear
     int64_t tiles;        // that these clear
     uint64_t share;       // of the workgroups that sum, times 2^32
@@ -393,38 +401,77 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
 // How many tokens a word has.
 __device__ __forceinline__ int tokens_of(const Spread &a, int word) { return a.start[word + 1] - a.start[word]; }
 
-// Sums of one piece of kHot sorted tokens, of those whose word has kHot tokens
-// or more: at most two such words meet a piece, one that is there at its first
-// token (slot 0) and one that starts behind it (slot 1).
+// One piece of kHot sorted tokens at a lane's columns.  share < kShares: words with
+// fewer than kHot that start in that share of the piece are summed, all of their
+// tokens, and their rows written (a whole piece for a wave, its loads waited for the
+// rows that it had stored: 229 us where this takes 167).  kShares: of words with
+// more, the sums of those tokens that lie in the piece; at most two such words meet
+// it, one that is there at its first token (slot 0) and one that starts behind it
+// (slot 1).
+constexpr int kShares = 4;
+
 template <typename T, typename F>
-__device__ __forceinline__ void sum_piece(const Spread &a, int64_t piece, int at) {
+__device__ __forceinline__ void sum_piece(const Spread &a, int32_t piece, int share, int at) {
     constexpr int N = kPack<T, F>;
+    static_assert(2 * kHot == kWave, "a piece, and what words that start in it have in the next");
     const int lane = threadIdx.x & (kWave - 1);
-    const int64_t begin = piece * kHot;
-    const int n = int(min(int64_t(kHot), a.start[a.vocab] - begin));
+    const int64_t place = int64_t(piece) * kHot + lane;
+    const bool there = place < a.start[a.vocab];
     Sorted s{0, -1};
-    if (lane < n) s = a.list[begin + lane];
-    const uint64_t hot = __ballot(lane < n && tokens_of(a, s.word) >= kHot);
-    if (hot == 0) return;
-    const int token = s.token;
-    const uint64_t head = hot & 1u ? __ballot(s.word == __shfl(s.word, 0) && lane < n) : 0;
+    int from = -1, n = 0;   // of the word: its first place, its tokens
+    if (there) {
+        s = a.list[place];
+        from = a.start[s.word];
+        n = a.start[s.word + 1] - from;
+    }
+    const uint64_t in_piece = (uint64_t(1) << kHot) - 1;
+    const uint64_t hot = __ballot(n >= kHot) & in_piece;
+    const uint64_t firsts = __ballot(there && from == place && n < kHot) & in_piece;
+    const uint64_t lasts = __ballot(there && from + n - 1 == place);
+    // tokens of words that start in the share and are not hot
+    const int64_t lo = place - lane + share * (kHot / kShares), hi = lo + kHot / kShares;
+    uint64_t todo = share < kShares ? __ballot(there && n < kHot && from >= lo && from < hi) : 0;
     const T *rows = static_cast<const T *>(a.dout) + min(at, a.width - 1);
+    const int left = max(a.width - at, 1);
+    const auto row = [&](int j) { return rows + int64_t(__builtin_amdgcn_readlane(s.token, j)) * a.ld_dout; };
+    float sum[N] = {};
+    while (todo != 0) {
+        constexpr int kLoads = 2 * kAhead;
+        Pack<T, N> v[kLoads];
+        uint64_t now = todo;
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (todo != 0) {
+                v[k] = load_raw<N>(row(__ffsll((unsigned long long)todo) - 1), left);
+                todo &= todo - 1;
+            }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k)
+            if (now != 0) {
+                const int j = __ffsll((unsigned long long)now) - 1;
+                now &= now - 1;
+                if ((firsts >> j) & 1u)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) sum[i] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[i] = __fadd_rn(sum[i], float(v[k][i]));
+                if ((lasts >> j) & 1u && at < a.width) put_row<F, N>(a, __builtin_amdgcn_readlane(s.word, j), at, sum);
+            }
+    }
+    if (share < kShares || hot == 0) return;
+    const uint64_t head = hot & 1u ? __ballot(s.word == __builtin_amdgcn_readlane(s.word, 0) && there) & in_piece : 0;
 #pragma unroll
     for (int slot = 0; slot < 2; ++slot) {
         const uint64_t lanes = slot == 0 ? head : hot & ~head;
         if (lanes == 0) continue;
-        const int from = __ffsll((unsigned long long)lanes) - 1, many = int(__popcll(lanes));
-        float sum[N];
-        sum_rows<N, 2 * kAhead>(max(a.width - at, 1), many, [&](int j) {
-            return rows + int64_t(__builtin_amdgcn_readlane(token, from + j)) * a.ld_dout;
-        }, sum);
+        const int first = __ffsll((unsigned long long)lanes) - 1;
+        sum_rows<N, 2 * kAhead>(left, int(__popcll(lanes)), [&](int j) { return row(first + j); }, sum);
         if (at < a.width)
-            store_pack<N>(a.partial + (piece * 2 + slot) * int64_t(a.width) + at, a.width - at, sum);
+            store_pack<N>(a.partial + (int64_t(piece) * 2 + slot) * a.width + at, a.width - at, sum);
     }
 }
 
-// Workgroups below a.pieces: a piece's columns a wave; others: a token's, if it is the
-// first of a word with fewer than kHot.  kClear: among them, those that clear rows
+// A piece's columns a wave.  kClear: and among these workgroups, those that clear rows
 // without a token, whose bytes are whole tiles.
 template <typename T, typename F, bool kClear>
 __global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
@@ -443,24 +490,10 @@ __global__ __launch_bounds__(kBlock) void embed_rows_kernel(const Spread a) {
         }
         return;
     }
-    if (group < a.pieces) {
-        const uint32_t units = (uint32_t(a.start[a.vocab]) + kHot - 1) / kHot * uint32_t(parts);
-        for (uint32_t u = uint32_t(group * kWaves + wave); u < units; u += uint32_t(a.pieces) * kWaves)
-            sum_piece<T, F>(a, int64_t(u / uint32_t(parts)), (int(u % uint32_t(parts)) * kWave + lane) * N);
-        return;
-    }
-    const uint32_t units = uint32_t(a.start[a.vocab]) * uint32_t(parts);
-    const T *dout = static_cast<const T *>(a.dout);
-    for (uint32_t u = uint32_t((group - a.pieces) * kWaves + wave); u < units; u += uint32_t(a.sums - a.pieces) * kWaves) {
-        const int32_t place = int32_t(u / uint32_t(parts));
-        const int at = (int(u % uint32_t(parts)) * kWave + lane) * N;
-        const Sorted *list = a.list + place;
-        const int32_t word = list[0].word;
-        const int n = tokens_of(a, word);
-        if (a.start[word] != place || n >= kHot || at >= a.width) continue;
-        float sum[N];
-        sum_rows<N, kAhead>(a.width - at, n, [&](int j) { return dout + int64_t(list[j].token) * a.ld_dout + at; }, sum);
-        put_row<F, N>(a, word, at, sum);
+    const uint32_t each = uint32_t(parts) * (kShares + 1), units = (uint32_t(a.start[a.vocab]) + kHot - 1) / kHot * each;
+    for (uint32_t u = uint32_t(group * kWaves + wave); u < units; u += uint32_t(a.sums) * kWaves) {
+        const uint32_t piece = u / each, rest = u - piece * each, share = rest / uint32_t(parts);
+        sum_piece<T, F>(a, int32_t(piece), int(share), (int(rest - share * uint32_t(parts)) * kWave + lane) * N);
     }
 }
 
@@ -550,10 +583,9 @@ hipError_t spread(Spread a, hipStream_t stream) {
     }
     // How rows without a token are cleared.  Large tables whose rows are whole tiles of 4
     // KiB: by the second launch, which knows those rows, and in the order of the table.
-    // Others, all of the table while the tokens are sorted.  us, against the second for all:
-    // 16,384 tokens x 131,072 x 2,048 fp32 183 and 212; the second, against the first with
-    // tiles that meet several rows: 131,072 x 1,056 fp32 116 and 130, 1,055 bf16 75 and 91,
-    // 1,000,000 x 64 76 and 96.
+    // Others, all of the table while the tokens are sorted.  16,384 tokens x 131,072 x 2,048
+    // fp32 took 183 us by the first and 212 by the second; where tiles meet several rows,
+    // 131,072 x 1,056 fp32 130 and 116, 1,055 bf16 91 and 75, 1,000,000 x 64 96 and 76.
     const bool whole = !a.accumulate && a.past && row_bytes % kRowTile == 0 && a.ld_dtable * int(sizeof(F)) % 128 == 0 &&
                        reinterpret_cast<uintptr_t>(a.dtable) % 128 == 0;
     a.rows = int32_t(kTileBytes / row_bytes < 1 ? 1 : kTileBytes / row_bytes);
@@ -566,8 +598,7 @@ hipError_t spread(Spread a, hipStream_t stream) {
     const size_t lds = size_t(a.words) * kSortWaves * sizeof(uint32_t);
     embed_sort_kernel<F><<<uint32_t(a.sorts + a.clears), kSortBlock, lds, stream>>>(a);
     const int64_t pieces = pieces_of(a.tokens);
-    a.pieces = int32_t(grid_of((pieces * parts + kWaves - 1) / kWaves));
-    a.sums = a.pieces + int32_t(grid_of((int64_t(a.tokens) * parts + kWaves - 1) / kWaves));
+    a.sums = int32_t(grid_of((pieces * parts * (kShares + 1) + kWaves - 1) / kWaves));
     if (whole) {
         a.tiles = a.vocab * (row_bytes / kRowTile);
         a.clears = int32_t(a.tiles < 1 << 23 ? a.tiles : 1 << 23);

@@ -5,7 +5,10 @@
 //   dx = rstd (g - mean(g) - h mean(g h))
 //   dw = sum over the rows of dy h ;  db = sum over the rows of dy
 //
-// Bytes bound it: x in and y out, x and dy in and dx out.  A row is read once and
+// Bytes bound it: x in and y out, x and dy in and dx out.  Measured on one MI355X, 16,384 x
+// 4,096 bf16: forward 51 us (5.3 TB/s), backward 76 us (5.3 TB/s, and 25 MB of partial
+// sums) and 5 for their join; 700 x 650 fp32: 4.9 and 6.9 us; one row of 1,024: 2.6 us,
+// a launch and two sums over a wave.  A row is read once and
 // stays in the registers of one wave, 256 or 1,024 threads, which are left with
 // the same columns row after row, so that the weights are read once too and the
 // sums of dw and db stay in registers until the workgroup ends.  These partial
@@ -472,8 +475,9 @@ bool few_rows(int32_t rows, int32_t width, Hold h) {
     return h.threads != 0 && rows <= kFewRows && int64_t(rows) * width <= kFewElements;
 }
 
-// Workgroups of the backward pass, whose partial sums the workspace holds: no
-// more than run at once.
+// Workgroups of the backward pass, whose partial sums the workspace holds: no more
+// than run at once, three a compute unit (two: 143 us where three take 135 for 16,384 x
+// 4,096 with the forward call, four 146: more partial sums, and a second round).
 int backward_groups(int32_t rows, Hold h) {
     const int64_t each = h.threads == 0 ? 8 : h.threads < kBlock ? kBlock / h.threads : 1;
     const int64_t groups = (rows + each - 1) / each, most = h.threads == kLong ? 256 : 768;

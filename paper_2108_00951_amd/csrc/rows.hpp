@@ -40,7 +40,9 @@ __device__ __forceinline__ void load_pack(const T *p, int left, float (&v)[N]) {
 }
 
 // What a call writes from here on does not stay in the 256 MB of the Infinity Cache
-// until it is read: it is stored past the caches.
+// until it is read: it is stored past the caches (norm of 16,384 x 4,096 bf16 and its
+// gradients 144 -> 134 us, gradient of 131,072 x 2,048 266 -> 236; below, 33,278 x 650
+// in 16 us through them and 23 past them).
 constexpr int64_t kPastCaches = int64_t(128) << 20;
 
 // bf16 results are rounded here, to nearest even.
