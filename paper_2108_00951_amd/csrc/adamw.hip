@@ -139,7 +139,8 @@ __device__ __forceinline__ uint32_t least_in_full(int e) { return uint32_t(114 +
 
 template <int kMantissa>
 __device__ __forceinline__ uint32_t encode_small(float y, uint32_t dither, float up) {
-    return uint32_t(__fadd_rn(__fmul_rn(__fmul_rn(y, up), 0x1p6f * float(1 << kMantissa)), __fmul_rn(float(dither), 0x1p-16f)));
+    // (the products are exact: the scale and the share are powers of two)
+    return uint32_t(fmaf(float(dither), 0x1p-16f, __fmul_rn(y, up * (0x1p6f * float(1 << kMantissa)))));
 }
 
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float(uint32_t(e + 127) << 23); }
@@ -237,81 +238,94 @@ __device__ __forceinline__ float advance(const Rates &c, float keep, float g, fl
     return __fsub_rn(__fmul_rn(x, keep), __fmul_rn(c.alpha, m / den));
 }
 
-template <typename G, bool kBytes, bool kDevice>
-__global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
-    const int which = tensor_of(a.tensors, blockIdx.x);
-    const int32_t size = a.tensors.size[which], blocks = (size - 1) / kStateBlock + 1;   // (a size may be the largest)
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    // a wave's block of 256 elements, four of a lane's each
-    const int block = int(blockIdx.x - a.tensors.first[which]) * kWaves + wave;
-    const int64_t at = int64_t(block) * kStateBlock + lane * 4;
-    const int left = int(min(int64_t(4), size - at));
-    const G *g = a.tensors.template pointer<const G>(kG, which) + at;
-    float *x = a.tensors.template pointer<float>(kX, which) + at;
-    float *m32 = a.tensors.template pointer<float>(kM, which) + at, *v32 = a.tensors.template pointer<float>(kV, which) + at;
-    uint8_t *m8 = a.tensors.template pointer<uint8_t>(kM, which), *r8 = a.tensors.template pointer<uint8_t>(kV, which);
-    float *m_scale = reinterpret_cast<float *>(m8 + int64_t(blocks) * kStateBlock) + block;
-    float *r_scale = reinterpret_cast<float *>(r8 + int64_t(blocks) * kStateBlock) + block;
+// A wave's block of 256 elements of a tensor, four of a lane's each, `left` of which
+// are there (kWhole: all of the wave's).
+template <typename G, bool kBytes, bool kDevice, bool kWhole>
+__device__ __forceinline__ void step_block(const Step &a, const Rates &c, int which, int64_t tile0, int left) {
+    const Tensors<kStepLists> &t = a.tensors;
+    const int lane = threadIdx.x & (kWave - 1), off = threadIdx.x * 4, count = kWhole ? 4 : left;
+    const int block = int(tile0 / kStateBlock) + int(threadIdx.x) / kWave;
+    const G *g = t.template pointer<const G>(kG, which) + tile0;   // (of the workgroup; off is a thread's)
+    float *x = t.template pointer<float>(kX, which) + tile0;
+    float *m32 = t.template pointer<float>(kM, which) + tile0, *v32 = t.template pointer<float>(kV, which) + tile0;
+    uint8_t *m8 = t.template pointer<uint8_t>(kM, which) + tile0, *r8 = t.template pointer<uint8_t>(kV, which) + tile0;
+    // the scales lie behind the codes
+    const int64_t scales = (int64_t(t.size[which] - 1) / kStateBlock + 1) * kStateBlock - tile0;
+    float *m_scale = reinterpret_cast<float *>(m8 + scales) + block, *r_scale = reinterpret_cast<float *>(r8 + scales) + block;
 
-    float gv[4] = {}, xv[4] = {}, mv[4] = {}, vv[4] = {};
-    if (kBytes && block < blocks) {
-        values_of_m(*reinterpret_cast<const uint32_t *>(m8 + at), *m_scale, mv);
-        values_of_r(*reinterpret_cast<const uint32_t *>(r8 + at), *r_scale, vv);
+    float gv[4], xv[4], mv[4], vv[4];
+    if (!kWhole)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gv[i] = xv[i] = mv[i] = vv[i] = 0.0f;
+    if (kBytes) {
+        values_of_m(*reinterpret_cast<const uint32_t *>(m8 + off), *m_scale, mv);
+        values_of_r(*reinterpret_cast<const uint32_t *>(r8 + off), *r_scale, vv);
 #pragma unroll
         for (int i = 0; i < 4; ++i) vv[i] = __fmul_rn(vv[i], vv[i]);
     }
-    if (left > 0) {
-        load_pack<4>(g, left, gv);
-        load_pack<4>(x, left, xv);
+    if (kWhole || left > 0) {
+        load_pack<4>(g + off, count, gv);
+        load_pack<4>(x + off, count, xv);
         if (!kBytes) {
-            load_pack<4>(m32, left, mv);
-            load_pack<4>(v32, left, vv);
+            load_pack<4>(m32 + off, count, mv);
+            load_pack<4>(v32 + off, count, vv);
         }
     }
-
-    Rates c = a.rates;
-    if (kDevice) {   // the step's rates are computed by one wave, beside the loads
-        __shared__ Rates s_rates;
-        if (wave == 0) {
-            const int64_t step = a.step != nullptr ? *a.step : a.given;
-            if (a.factors != nullptr) c.gain = a.factors[1];
-            set_step(c, a.gamma, a.factors != nullptr ? a.factors[0] : 1.0f, step < 1 ? 1 : step, a.seed);
-            if (lane == 0) s_rates = c;
-        }
-        __syncthreads();
-        c = s_rates;
-    }
-    if (block >= blocks) return;
     const float keep = float(1.0 - c.gamma * double(a.decay[which]));
-    const uint32_t key = mixed(c.key + (a.tensors.ordinal + uint32_t(which)) * 0x3C6EF373u);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (kDevice) gv[i] = __fmul_rn(gv[i], c.gain);
         xv[i] = advance(c, keep, gv[i], xv[i], mv[i], vv[i]);
     }
     if (kBytes) {
+        const uint32_t key = mixed(c.key + (t.ordinal + uint32_t(which)) * 0x3C6EF373u);
+        const uint32_t index = (uint32_t(tile0) + uint32_t(off)) * 0x9E3779B1u;
         uint32_t random[4], mc, rc;
         float r[4], ms, rs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            random[i] = mixed((uint32_t(at + i) * 0x9E3779B1u) ^ key);
-            const bool in = i < left;   // what lies behind the tensor is zero
+            random[i] = mixed((index + uint32_t(i) * 0x9E3779B1u) ^ key);
+            const bool in = kWhole || i < left;   // what lies behind the tensor is zero
             mv[i] = in ? mv[i] : 0.0f;
             r[i] = in ? sqrtf(vv[i]) : 0.0f;
         }
         pack_block(mv, r, random, mc, rc, ms, rs);
-        *reinterpret_cast<uint32_t *>(m8 + at) = mc;
-        *reinterpret_cast<uint32_t *>(r8 + at) = rc;
+        *reinterpret_cast<uint32_t *>(m8 + off) = mc;
+        *reinterpret_cast<uint32_t *>(r8 + off) = rc;
         if (lane == 0) *m_scale = ms, *r_scale = rs;
     }
-    if (left <= 0) return;
-    store_pack<4>(x, left, xv, kPast);
-    if (a.tensors.at[kCopy][which] != kNone)
-        store_pack<4>(a.tensors.template pointer<__bf16>(kCopy, which) + at, left, xv, kPast);
+    if (!kWhole && left <= 0) return;
+    store_pack<4>(x + off, count, xv, kPast);
+    if (t.at[kCopy][which] != kNone)
+        store_pack<4>(t.template pointer<__bf16>(kCopy, which) + tile0 + off, count, xv, kPast);
     if (!kBytes) {
-        store_pack<4>(m32, left, mv, kPast);
-        store_pack<4>(v32, left, vv, kPast);
+        store_pack<4>(m32 + off, count, mv, kPast);
+        store_pack<4>(v32 + off, count, vv, kPast);
     }
+}
+
+template <typename G, bool kBytes, bool kDevice>
+__global__ __launch_bounds__(kBlock) void adamw_kernel(const Step a) {
+    Rates c = a.rates;
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
+    if (kDevice) {   // the step's rates, by one wave
+        __shared__ Rates s_rates;
+        if (wave == 0) {
+            const int64_t step = a.step != nullptr ? *a.step : a.given;
+            if (a.factors != nullptr) c.gain = a.factors[1];
+            set_step(c, a.gamma, a.factors != nullptr ? a.factors[0] : 1.0f, step < 1 ? 1 : step, a.seed);
+            if (threadIdx.x == 0) s_rates = c;
+        }
+        __syncthreads();
+        c = s_rates;
+    }
+    const int which = tensor_of(a.tensors, blockIdx.x);
+    const int64_t tile0 = int64_t(blockIdx.x - a.tensors.first[which]) * kStepTile;
+    const int rest = int(min(int64_t(kStepTile), a.tensors.size[which] - tile0));   // of the workgroup's elements
+    if (rest >= (wave + 1) * kStateBlock)
+        step_block<G, kBytes, kDevice, true>(a, c, which, tile0, 4);
+    else if (rest > wave * kStateBlock)
+        step_block<G, kBytes, kDevice, false>(a, c, which, tile0, rest - int(threadIdx.x) * 4);
 }
 
 // States of 8 bits from values of 32 and back: what a program does when it saves

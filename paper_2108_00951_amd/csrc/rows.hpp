@@ -72,9 +72,10 @@ __device__ __forceinline__ void store_pack(T *p, int left, const float (&v)[N], 
 constexpr int kDppPairs = 0xB1, kDppFours = 0x4E, kDppEights = 0x141, kDppSixteens = 0x140, kDppNextRow = 0x142,
               kDppUpperHalf = 0x143;
 
+// (lanes of rows that are left out get 0)
 template <int kControl, int kRows = 0xf>
 __device__ __forceinline__ uint32_t dpp(uint32_t v) {
-    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), kControl, kRows, 0xf, false));
+    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), kControl, kRows, 0xf, kRows == 0xf));
 }
 
 template <int kControl, int kRows = 0xf>
