@@ -103,6 +103,49 @@ def test_more_tensors_than_a_launch_takes(bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_lists_in_any_order(bits):
+    """Tensors whose addresses fall, and a copy of some of them."""
+    sizes = [300, 0, 4097, 5, 1000]
+    model = Model(sizes, bits)
+    model.copy = [torch.full((n,), 7.0, dtype=torch.bfloat16, device=DEV) for n in sizes]
+    plain = _step.Adamw(1e-2, bits=bits)
+    g, dg = model.gradients()
+    some = [model.copy[0], None, None, model.copy[3], None][::-1]
+    # (the order in the list is the tensors' place: the random rounding goes by it)
+    efs.adamw_apply(dg[::-1], model.dx[::-1], model.dm[::-1], model.dv[::-1], 2, lr=1e-2, weight_decay=0.0, copy=some)
+    for i, n in enumerate(sizes):
+        model.x[i], model.m[i], model.v[i] = plain.step(2, len(sizes) - 1 - i, g[i], model.x[i], model.m[i], model.v[i], 0.0)
+    for i, n in enumerate(sizes):
+        want = torch.from_numpy(model.x[i]).to(torch.bfloat16)
+        assert torch.equal(model.copy[i].cpu(), want) if i in (0, 3) else torch.all(model.copy[i] == 7.0)
+    model.copy = None
+    model.check("reversed")
+
+
+def test_the_most_tensors():
+    sizes = [1 + i % 3 for i in range(65536)]
+    flat = torch.arange(float(sum(sizes)), device=DEV)
+    x, g, m, v = (list(t.split(sizes)) for t in (flat.clone(), flat * 1e-3, torch.zeros_like(flat), torch.zeros_like(flat)))
+    efs.adamw_apply(g, x, m, v, 1, lr=0.5, weight_decay=0.0)
+    moved = flat - torch.cat(x)   # a first step is lr, but for eps and a rounding of x
+    assert torch.all((moved[1:] - 0.5).abs() <= 0.5 * 1e-4 + 2.0 ** -24 * flat[1:])
+    assert moved[0] == 0.0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_below_one_is_one(bits):
+    outs = []
+    for step in (1, torch.zeros(1, dtype=torch.int64, device=DEV), torch.full((), -5, dtype=torch.int64, device=DEV)):
+        model = Model([1000], bits)
+        _, dg = model.gradients()
+        efs.adamw_apply(dg, model.dx, model.dm, model.dv, step, lr=1e-2)
+        outs.append([model.dx[0]] + [t[0].clone() for t in (model.dm, model.dv)])
+    for other in outs[1:]:
+        for a, b in zip(other, outs[0]):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_layers_of_flat_vectors(bits):
     """Neighbouring views, any of which is off 16 bytes, are tensors like others."""
     sizes = [5, 1000, 3, 257, 4099]

@@ -138,6 +138,46 @@ def test_tokens_past_2_31_elements():
     assert torch.equal(dtable, (torch.arange(40.0, device=DEV) * (tokens // 40))[:, None].expand(-1, width))
 
 
+@pytest.mark.parametrize("tokens, vocab, width", [(1 << 22, 1 << 16, 3), (1 << 14, 1 << 24, 5), (5000, 1 << 24, 1), (1000, 1 << 24, 2)])
+def test_the_most_tokens_and_words(tokens, vocab, width):
+    """Whole numbers, whose sums are exact in any order."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    ids = torch.randint(0, vocab, (tokens,), generator=gen, device=DEV)
+    ids[: tokens // 4] = vocab - 1
+    ids[-3:] = torch.tensor([0, -100, vocab], device=DEV)
+    dout = torch.randint(-8, 9, (tokens, width), generator=gen, device=DEV).float()
+    status = efs.new_embed_status(DEV)
+    got = torch.full((vocab, width), 3.0, device=DEV)
+    efs.embed_backward(dout, ids, got, efs.new_embed_workspace(tokens, vocab, width, DEV), status=status)
+    want = torch.zeros(vocab, width, device=DEV).index_add_(0, ids[:-2], dout[:-2])
+    assert torch.equal(got, want)
+    assert efs.embed_status(status) == efs.EMBED_BAD_ID
+    out = torch.empty(tokens, width, device=DEV)
+    efs.embed_forward(got, ids, out)
+    assert torch.equal(out[:-2], got[ids[:-2]]) and not out[-2:].any()
+
+
+@pytest.mark.parametrize("rows, width", [((1 << 23) + 3, 2), (100_003, 9), (40, 1 << 18), (2, 8193)])
+def test_many_and_long_rows(rows, width):
+    """Some rows give what they give alone; the sums over all of them are those of
+    other pieces of the same rows."""
+    x, dy, w = rand((rows, width), 1), rand((rows, width), 2), rand((width,), 3)
+    y, dx, mean, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    efs.layernorm_forward(x, w, None, y, mean, rstd)
+    efs.layernorm_backward(x, w, mean, rstd, dy, dx, dw, db, efs.new_layernorm_workspace(rows, width, DEV))
+    for at in (0, rows // 2, max(0, rows - 20)):
+        s = slice(at, min(at + 20, rows))
+        want = _step.norm(x[s].cpu().numpy(), w.cpu().numpy(), None, dy[s].cpu().numpy())
+        for name, got in (("y", y), ("dx", dx), ("mean", mean), ("rstd", rstd)):
+            _step.within(got[s].cpu().numpy(), want[name], name)
+    for c in {0, width // 2, width - 1}:
+        h = (x[:, c].double() - mean.double()) * rstd.double()
+        for got, terms in ((dw[c], dy[:, c].double() * h), (db[c], dy[:, c].double())):
+            # an addition for every row of a workgroup, in order, and the join's; h's own rounding
+            assert abs(float(got) - float(terms.sum())) <= 2.0 ** -24 * (rows / 64 + 1000) * float(terms.abs().sum())
+
+
 @pytest.mark.parametrize("rows, width", [(530_000, 4099), (33_000, 66_001)])
 def test_norms_past_2_31_elements(rows, width):
     """The last rows give what they give alone."""
