@@ -20,6 +20,8 @@ COUNTER_WORDS = 4
 MAX_WORKERS = 64
 
 _lib = None
+_torch = None     # once the library is loaded
+_current = None   # once the device is initialised: its stream's handle, its number
 
 
 class EfsError(RuntimeError):
@@ -36,16 +38,16 @@ def load_library(path: str = LIB_PATH):
     torch is imported first so that the library binds to the HIP runtime
     torch already loaded (one runtime per process, shared streams).
     """
-    global _lib
+    global _lib, _torch
     if _lib is not None:
         return _lib
-    import torch  # noqa: F401  (binds the HIP runtime before the library loads)
+    import torch  # (binds the HIP runtime before the library loads)
     if not os.path.exists(path):
         raise ImportError("libefsparse.so not built at %s; run python -m paper_2108_00951_amd.build"
                           % path)
     lib = ctypes.CDLL(path)
     declare(lib)
-    _lib = lib
+    _lib, _torch = lib, torch
     return lib
 
 
@@ -152,13 +154,17 @@ def _check(lib, rc: int):
 
 
 def _stream_handle(stream) -> int:
+    global _current
     if stream is None:
+        if _current is not None:
+            return _current[0](_current[1]())
         import torch
         # the current stream's handle itself, without a Stream object around it
         # (with the checks' short way, a hard-threshold step over 5,000
         # elements 14.1 -> 11.2 us: two launches bound by the host)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None and torch.cuda.is_initialized():
+            _current = raw, torch._C._cuda_getDevice
             return raw(torch._C._cuda_getDevice())
         stream = torch.cuda.current_stream()
     return int(getattr(stream, "cuda_stream", stream))
@@ -485,13 +491,18 @@ def sparse_accumulate_static(payloads: Sequence[Tuple], d: int, out, stream=None
 FP32, BF16 = 0, 1
 
 
+_codes = {}   # of torch's dtypes
+
+
 def _dtype_code(t, name) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return FP32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+    code = _codes.get(t.dtype)
+    if code is None:
+        import torch
+        _codes.update({torch.float32: FP32, torch.bfloat16: BF16})
+        if t.dtype not in _codes:
+            raise TypeError("%s must be float32 or bfloat16, got %s" % (name, t.dtype))
+        code = _codes[t.dtype]
+    return code
 
 
 def _require_rows(t, name):
@@ -682,9 +693,9 @@ def _device_of(t, name) -> int:
     here = t.get_device()
     if here < 0:
         raise TypeError("%s must be a device tensor" % name)
-    import torch
-    if here != torch._C._cuda_getDevice():
-        raise ValueError("%s is on %s, and the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    if here != _torch._C._cuda_getDevice():
+        raise ValueError("%s is on %s, and the current device is cuda:%d"
+                         % (name, t.device, _torch.cuda.current_device()))
     return here
 
 
@@ -702,7 +713,7 @@ def _matrix(t, name, here):
         _elsewhere(t, name, here)
     if step != 1 and cols > 1 and rows > 0:
         raise TypeError("%s must have contiguous rows" % name)
-    return _ptr(t), ld if rows > 1 else cols
+    return t.data_ptr() if rows and cols else None, ld if rows > 1 else cols
 
 
 def _vector(t, name, dtype, here):
@@ -719,10 +730,9 @@ def _vector(t, name, dtype, here):
 def _status_pointer(status, here):
     if status is None:
         return None
-    import torch
     if status.numel() < 1:
         raise ValueError("status must have an element")
-    return _vector(status, "status", torch.int32, here)
+    return _vector(status, "status", _torch.int32, here)
 
 
 EMBED_BAD_ID = 1
@@ -742,13 +752,12 @@ def embed_status(status) -> int:
 def embed_forward(table, ids, out, scale: float = 1.0, ignore_index: int = -100, status=None, stream=None) -> None:
     """out [tokens, width] = scale * table [vocab, width] at ids [tokens], each fp32
     or bf16; see embed_forward in include/efsparse.h."""
-    import torch
     lib = load_library()
     if table.dim() != 2 or ids.dim() != 1 or out.shape != (ids.shape[0], table.shape[1]):
         raise ValueError("table must be [vocab, width], ids [tokens] and out [tokens, width]")
     table_dtype, dtype = _dtype_code(table, "table"), _dtype_code(out, "out")
     here = _device_of(table, "table")
-    _check(lib, lib.embed_forward(*_matrix(table, "table", here), table_dtype, _vector(ids, "ids", torch.int64, here),
+    _check(lib, lib.embed_forward(*_matrix(table, "table", here), table_dtype, _vector(ids, "ids", _torch.int64, here),
                                   *_matrix(out, "out", here), dtype, _int32(ids.shape[0], "tokens"),
                                   _int32(table.shape[0], "vocab"), _int32(table.shape[1], "width"), float(scale),
                                   int(ignore_index), _status_pointer(status, here), _stream_handle(stream)))
@@ -772,17 +781,16 @@ def embed_backward(dout, ids, dtable, workspace, scale: float = 1.0, ignore_inde
                    accumulate: bool = False, status=None, stream=None) -> None:
     """The table's gradient dtable [vocab, width] from dout [tokens, width] at ids
     [tokens], written whole or added to; see embed_backward in include/efsparse.h."""
-    import torch
     lib = load_library()
     if dtable.dim() != 2 or ids.dim() != 1 or dout.shape != (ids.shape[0], dtable.shape[1]):
         raise ValueError("dtable must be [vocab, width], ids [tokens] and dout [tokens, width]")
     table_dtype, dtype = _dtype_code(dtable, "dtable"), _dtype_code(dout, "dout")
     here = _device_of(dtable, "dtable")
-    _check(lib, lib.embed_backward(*_matrix(dout, "dout", here), dtype, _vector(ids, "ids", torch.int64, here),
+    _check(lib, lib.embed_backward(*_matrix(dout, "dout", here), dtype, _vector(ids, "ids", _torch.int64, here),
                                    *_matrix(dtable, "dtable", here), table_dtype, _int32(ids.shape[0], "tokens"),
                                    _int32(dtable.shape[0], "vocab"), _int32(dtable.shape[1], "width"), float(scale),
                                    int(ignore_index), int(bool(accumulate)), _status_pointer(status, here),
-                                   _vector(workspace, "workspace", torch.uint8, here), workspace.numel(),
+                                   _vector(workspace, "workspace", _torch.uint8, here), workspace.numel(),
                                    _stream_handle(stream)))
 
 
@@ -805,12 +813,11 @@ def _weights(width, here, **weights):
 
 def _row_values(t, name, rows, here):
     """Pointer of fp32 values, one a row, or None."""
-    import torch
     if t is None:
         return None
     if t.dim() != 1 or t.shape[0] != rows:
         raise ValueError("%s must be [rows]" % name)
-    return _vector(t, name, torch.float32, here)
+    return _vector(t, name, _torch.float32, here)
 
 
 def layernorm_forward(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5, stream=None) -> None:
@@ -848,7 +855,6 @@ def new_layernorm_workspace(rows: int, width: int, device="cuda"):
 def layernorm_backward(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace, stream=None) -> None:
     """Gradients of layernorm_forward: dx [rows, width], dweight and dbias [width]
     (or None); see layernorm_backward in include/efsparse.h."""
-    import torch
     lib = load_library()
     if x.dim() != 2 or dy.shape != x.shape or dx.shape != x.shape:
         raise ValueError("x, dy and dx must be [rows, width]")
@@ -864,7 +870,7 @@ def layernorm_backward(x, weight, mean, rstd, dy, dx, dweight, dbias, workspace,
                                        _row_values(rstd, "rstd", rows, here), *_matrix(dy, "dy", here),
                                        *_matrix(dx, "dx", here), dtype, weight_dtype, _int32(rows, "rows"),
                                        _int32(width, "width"), dw, db,
-                                       _vector(workspace, "workspace", torch.uint8, here), workspace.numel(),
+                                       _vector(workspace, "workspace", _torch.uint8, here), workspace.numel(),
                                        _stream_handle(stream)))
 
 
