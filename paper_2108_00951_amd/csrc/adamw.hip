@@ -7,8 +7,8 @@
 // each operation rounded to fp32 by itself.  Bytes bound it: 28 of an element
 // with states of 32 bits (g, x, m, v in; x, m, v out), 16 with states of 8.  Measured
 // on one MI355X: 37 M elements of 161 tensors, 32 bits, 198 us (5.3 TB/s, two
-// launches); 134 M, 8 bits, bf16 g and copy (16 bytes an element too) 375 to 420 us
-// (5.7 to 5.1 TB/s), where the vector units are busy throughout: 90 instructions an
+// launches); 134 M, 8 bits, bf16 g and copy (16 bytes an element too) 371 to 431 us
+// (5.8 to 5.0 TB/s), where the vector units are busy throughout: 90 instructions an
 // element, of which the square root, the division and the hash are half; 97 short
 // vectors 5.0 us.
 // A launch takes the tensors of its arguments, kTensors at most, one tile of
