@@ -212,12 +212,13 @@ efs_status topk_segmented_compress(const float *g, float *e, int64_t d, float lr
  *              Both give the same bits.  (sparse_apply's EFS_APPLY_SGD with
  *              one payload uses neither: one launch, and words of the control
  *              block with an epoch of their own.)  Contents need no
- *              initialisation: each counter carries the 40-bit epoch of the
- *              call that wrote it (the control block's epoch, advanced by
+ *              initialisation: each counter carries a 40-bit tag of the epoch
+ *              of the call that wrote it (the control block's epoch, advanced by
  *              every call that uses the counters), so a counter of an earlier
- *              call reads as zero, as does arbitrary content except when its
- *              epoch bits equal the current epoch (probability 2^-40 per
- *              counter for random bytes).  Calls on one workspace must be
+ *              call reads as zero, also where a call of another layout or other
+ *              sizes has overwritten half of it since, as does arbitrary content
+ *              except when its tag bits equal the current tag (probability 2^-40
+ *              per counter for random bytes).  Calls on one workspace must be
  *              ordered (one stream, or synchronised streams); concurrent
  *              calls on one workspace race.
  * Payload entries with an index outside [0, d) are skipped and reported in

@@ -73,17 +73,27 @@ struct Payloads {
 
 // Counter words: a tag in the bits above kEpochShift, the count below (a
 // segment holds at most a range's worth of pairs of one worker, whose
-// indices are distinct).  The tag of counter e in the call of epoch E is E xor a
-// multiplicative hash of e, so that neither a counter of an earlier call
-// nor a workspace filled with any one byte value carries the current tag (a
-// constant fill would otherwise give every counter the control block's
-// epoch bits).
+// indices are distinct).  The tag of counter e in the call of epoch E is a
+// multiple of E xor a multiplicative hash of e, so that neither a counter of
+// an earlier call nor a workspace filled with any one byte value carries the
+// current tag (a constant fill would otherwise give every counter the control
+// block's epoch bits).
+//   A multiple, since another call's layout may have written half of a word: a
+// 4-byte segment start in the low half, over the count and the tag's low 8
+// bits, beside the upper 32 bits of an earlier tag.  By epochs themselves those
+// bits stay the same for 256 calls, and one start in 256 then read as a count.
+// kEpochStep is odd (distinct epochs have distinct tags) and near 2^40 over the
+// golden ratio, whose multiples keep apart: by the convergents of kEpochStep /
+// 2^40, those of two epochs less than 1,205,014,437 calls apart differ by 878 at
+// least (modulo 2^40), so their upper 32 bits are not the same.
 constexpr int kEpochShift = 24;
 constexpr uint64_t kCountBits = (uint64_t(1) << kEpochShift) - 1;
 constexpr uint64_t kEpochMask = (uint64_t(1) << (64 - kEpochShift)) - 1;
+constexpr uint64_t kEpochStep = 0x9E3779B97Full;
+static_assert(kEpochStep % 2 == 1 && kEpochStep <= kEpochMask, "epochs and their tags are one to one");
 
 __device__ __forceinline__ uint64_t counter_tag(uint64_t epoch, uint64_t e) {
-    return (epoch ^ ((e + 1) * 0x9E3779B97F4A7C15ull >> 17)) & kEpochMask;
+    return (epoch * kEpochStep ^ ((e + 1) * 0x9E3779B97F4A7C15ull >> 17)) & kEpochMask;
 }
 constexpr uint64_t kFlagsTagIndex = ~uint64_t(0) - 1;
 

@@ -407,3 +407,44 @@ def test_apply_reports_truncation_and_bad_index_together(n, layout):
                 got, _ = run_apply(p_dev, d, mode, x0, ws=ws)
                 assert efs.sparse_status(ws) == efs.SPARSE_TRUNCATED | efs.SPARSE_BAD_INDEX
                 assert_bits_equal(got, want)
+
+
+@pytest.mark.parametrize("between", [(300_007, 3), (200_000, 3)])
+@pytest.mark.parametrize("layout", efs.LAYOUTS)
+def test_counters_half_overwritten_by_another_call(layout, between):
+    # a call of the packed layout writes a 4-byte segment start over the low half
+    # of one of the earlier call's 8-byte counters (both have an odd number of
+    # starts): whatever the epochs are, the next call must not take what is left
+    # for a count.  A tag's low byte lies beside the count, so 256 epochs in a row
+    # hold every one.
+    d, n = (300_007, 3) if layout == "bucketed" else (400_009, 6)
+    d2, n2 = between
+    rng = np.random.default_rng(93)
+
+    def payloads(d, n):
+        ref = []
+        for _ in range(n):
+            i = rng.permutation(d)[: d // 100].astype(np.int32)
+            ref.append((i, rng.standard_normal(i.size).astype(np.float32)))
+        return [(dev(i), dev(v)) for i, v in ref], dev(oracle.accumulate(ref, d))
+    p, want = payloads(d, n)
+    p2, want2 = payloads(d2, n2)
+    ws = efs.new_apply_workspace(p, d, DEV, layout=layout)
+    packed = efs.sparse_apply_workspace_bytes(n2, d2, sum(i.numel() for i, _ in p2))
+    if layout == "packed" and ws.numel() < packed:
+        ws = torch.empty(packed, dtype=torch.uint8, device=DEV)
+    assert ws.numel() >= packed
+    if layout == "packed":
+        assert ws.numel() < efs.sparse_bucket_workspace_bytes(n, d)
+    out, out2 = torch.empty(d, device=DEV), torch.empty(d2, device=DEV)
+    say("half counters", layout, between)
+    wrong = torch.zeros((), dtype=torch.int64, device=DEV)
+    for epoch in range(1 << 16, (1 << 16) + 256):
+        ws.zero_()
+        ws[:8].view(torch.int64).fill_(epoch)   # the next call's
+        for _ in range(2):
+            efs.sparse_accumulate(p, d, out, ws)
+            wrong += (out.view(torch.int32) != want.view(torch.int32)).sum()
+            efs.sparse_accumulate(p2, d2, out2, ws[:packed])
+            wrong += (out2.view(torch.int32) != want2.view(torch.int32)).sum()
+    assert int(wrong) == 0
