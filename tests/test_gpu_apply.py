@@ -416,7 +416,8 @@ def test_counters_half_overwritten_by_another_call(layout, between):
     # of one of the earlier call's 8-byte counters (both have an odd number of
     # starts): whatever the epochs are, the next call must not take what is left
     # for a count.  A tag's low byte lies beside the count, so 256 epochs in a row
-    # hold every one.
+    # hold every one.  Each call has payloads of its own, as what an earlier one left
+    # in the buckets would do for the same pairs.
     d, n = (300_007, 3) if layout == "bucketed" else (400_009, 6)
     d2, n2 = between
     rng = np.random.default_rng(93)
@@ -427,9 +428,9 @@ def test_counters_half_overwritten_by_another_call(layout, between):
             i = rng.permutation(d)[: d // 100].astype(np.int32)
             ref.append((i, rng.standard_normal(i.size).astype(np.float32)))
         return [(dev(i), dev(v)) for i, v in ref], dev(oracle.accumulate(ref, d))
-    p, want = payloads(d, n)
+    first, second = payloads(d, n), payloads(d, n)
     p2, want2 = payloads(d2, n2)
-    ws = efs.new_apply_workspace(p, d, DEV, layout=layout)
+    ws = efs.new_apply_workspace(first[0], d, DEV, layout=layout)
     packed = efs.sparse_apply_workspace_bytes(n2, d2, sum(i.numel() for i, _ in p2))
     if layout == "packed" and ws.numel() < packed:
         ws = torch.empty(packed, dtype=torch.uint8, device=DEV)
@@ -442,7 +443,7 @@ def test_counters_half_overwritten_by_another_call(layout, between):
     for epoch in range(1 << 16, (1 << 16) + 256):
         ws.zero_()
         ws[:8].view(torch.int64).fill_(epoch)   # the next call's
-        for _ in range(2):
+        for p, want in (first, second):
             efs.sparse_accumulate(p, d, out, ws)
             wrong += (out.view(torch.int32) != want.view(torch.int32)).sum()
             efs.sparse_accumulate(p2, d2, out2, ws[:packed])
