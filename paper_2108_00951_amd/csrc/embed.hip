@@ -513,11 +513,15 @@ __global__ __launch_bounds__(kJoinBlock) void embed_join_kernel(const Spread a) 
         const bool there = lane < kHot && place < a.start[a.vocab];
         const int word = there ? a.list[place].word : 0;
         const int n = there ? tokens_of(a, word) : 0;
-        if (lane == 0) s_word[wave] = -1;
-        if (n >= kHot && a.start[word] == place) {   // one lane at most
-            s_word[wave] = word;
-            s_from[wave] = lane;
-            s_length[wave] = n;
+        // one lane at most; lane 0 alone writes what it found (two lanes' stores to one
+        // word are in no order that the compiler has to keep)
+        const uint64_t starts = __ballot(n >= kHot && a.start[word] == place);
+        const int from = starts != 0 ? __ffsll((unsigned long long)starts) - 1 : 0;
+        const int its_word = __builtin_amdgcn_readlane(word, from), length = __builtin_amdgcn_readlane(n, from);
+        if (lane == 0) {
+            s_word[wave] = starts != 0 ? its_word : -1;
+            s_from[wave] = from;
+            s_length[wave] = length;
         }
     }
     __syncthreads();

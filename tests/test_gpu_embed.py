@@ -238,3 +238,20 @@ def test_gradient_against_differences():
         # table +- 1 is rounded: 2^-24 of at most 8, times 2 and the weights' sum
         slack = 2.0 ** -20 * float(weight.abs()[:, c].sum())
         assert abs((loss(up) - loss(down)) / 2.0 - float(grad[v, c])) <= slack
+
+
+@pytest.mark.parametrize("start", range(32))
+def test_split_words_that_start_anywhere_in_a_piece(start):
+    """Words that are summed piece by piece, of which one starts at each place of a
+    piece of 32 sorted tokens; pieces without such a start lie between."""
+    counts = [start, 33, 31, 32 + (32 - start) % 32, 700, 1, 0, 64, 3]
+    counts.append(4300 - sum(counts))
+    ids = np.repeat(np.arange(len(counts)), counts)
+    rng = np.random.default_rng(start)
+    rng.shuffle(ids)
+    dout = torch.from_numpy(rng.integers(-9, 10, (len(ids), 70)).astype(np.float32))
+    want = np.zeros((len(counts), 70))
+    np.add.at(want, ids, dout.numpy())
+    before = torch.ones(len(counts), 70)
+    assert np.array_equal(gradient(dout, ids, len(counts)).cpu().numpy(), want)
+    assert np.array_equal(gradient(dout, ids, len(counts), before=before).cpu().numpy(), want + 1.0)
