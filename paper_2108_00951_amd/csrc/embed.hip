@@ -389,11 +389,15 @@ __global__ __launch_bounds__(kSortBlock) void embed_sort_kernel(const Spread a) 
                 same = own == word ? its : same;
                 left &= ~its;
             }
-            if ((in[k] >> lane) & 1u) {
-                const uint32_t at = mine[own], below = lanes_below(same);
+            // the lanes of a word read its place before one of them moves it on
+            const bool its = (in[k] >> lane) & 1u;
+            const uint32_t at = its ? mine[own] : 0u, below = lanes_below(same);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (its) {
                 a.list[at + below] = Sorted{t + k * kWave + lane, int32_t(first) + own};
                 if (below == 0u) mine[own] = at + uint32_t(__popcll(same));
             }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
 }
