@@ -7,13 +7,14 @@
 //
 // Bytes bound it: x in and y out, x and dy in and dx out.  Measured on one MI355X, 16,384 x
 // 4,096 bf16: forward 51 us (5.3 TB/s), backward 76 us (5.3 TB/s, and 25 MB of partial
-// sums) and 5 for their join; 700 x 650 fp32: 4.9 and 6.9 us; one row of 1,024: 2.6 us,
-// a launch and two sums over a wave.  A row is read once and
-// stays in the registers of one wave, 256 or 1,024 threads, which are left with
+// sums) and 5 for their join; 700 x 650 fp32: forward 5.0 us, backward 4.0 and 4.7 for
+// the columns behind it (each by itself under a profiler; 7.2 together as a graph's
+// nodes); one row of 1,024: 2.6 us, a launch and two sums over a wave.  A row is read
+// once and stays in the registers of one wave, 256 or 1,024 threads, which are left with
 // the same columns row after row, so that the weights are read once too and the
 // sums of dw and db stay in registers until the workgroup ends.  These partial
-// sums go to the workspace and a second launch adds them in order: no atomics,
-// and the same bits each time.
+// sums go to the workspace and a second launch adds them in order, or, of few rows, sums
+// columns of all of them: no atomics, and the same bits each time.
 //
 // The mean is taken first and the squares of x - mean after it: a row whose mean
 // is large against its spread loses nothing by them.  What the rounding of the
@@ -34,8 +35,9 @@ struct Norm {
     float *mean, *rstd;     // forward: may be NULL
     float *partial;         // backward: [groups][2][width], NULL: no partial sums of dw and db
     float *sums;            // backward of long rows: [rows][4]
-    void *dweight, *dbias;  // backward of few rows: written by workgroups of columns
-    int32_t groups;         // backward: workgroups that take rows, before those of columns
+    float *rest;            // backward of few rows: [rows], the mean of x - mean; NULL: not kept
+    void *dweight, *dbias;  // backward of few rows: written by columns
+    int32_t groups;         // backward: workgroups that take rows
     int64_t ld_x, ld_dy, ld_out;
     int32_t rows, width;
     float eps;
@@ -218,46 +220,11 @@ __device__ __forceinline__ Slopes slopes(const float (&s)[3], float rstd, int wi
     return Slopes{rest, rstd * (s[1] / n), rstd * rstd * (along / n)};
 }
 
-// Few rows: dw and db of kColumns columns from all rows, which stay in L2, with the
-// mean as it was stored; beside the workgroups that take rows, and no join.
-constexpr int kColumns = 8;
-
-template <typename T, typename F, int kSize>
-__device__ __forceinline__ void norm_columns(const Norm &a, int64_t first) {
-    __shared__ float s_part[kSize / kWave][2][kColumns];
-    constexpr int kSlots = kSize / kColumns;   // a thread's rows: its slot's, every kSlots
-    const int64_t column = first + threadIdx.x % kColumns;
-    const int slot = threadIdx.x / kColumns;
-    const T *x = static_cast<const T *>(a.x) + column, *dy = static_cast<const T *>(a.dy) + column;
-    float dw = 0.0f, db = 0.0f;
-    if (column < a.width) {
-#pragma unroll 8
-        for (int row = slot; row < a.rows; row += kSlots) {
-            const float v = float(dy[row * a.ld_dy]);
-            dw = fmaf(v, (float(x[row * a.ld_x]) - a.mean[row]) * a.rstd[row], dw);
-            db += v;
-        }
-    }
-#pragma unroll
-    for (int off = kColumns; off < kWave; off <<= 1) dw += __shfl_xor(dw, off), db += __shfl_xor(db, off);
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    if (lane < kColumns) s_part[wave][0][lane] = dw, s_part[wave][1][lane] = db;
-    __syncthreads();
-    if (threadIdx.x >= 2 * kColumns || first + threadIdx.x % kColumns >= a.width) return;
-    const int which = threadIdx.x / kColumns;
-    float sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kSize / kWave; ++w) sum += s_part[w][which][threadIdx.x % kColumns];
-    F *to = static_cast<F *>(which == 0 ? a.dweight : a.dbias);
-    if (to != nullptr) to[column] = F(sum);
-}
-
 template <typename T, typename F, int kThreads, int kPacks, int kSize>
 __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
     constexpr int N = kRowPack<T>, kGroups = kSize / kThreads;
     __shared__ float s_sums[2][kSize / kWave][3];
     __shared__ float s_join[kGroups > 1 ? (kGroups - 1) * kThreads * N : 1];
-    if (int(blockIdx.x) >= a.groups) return norm_columns<T, F, kSize>(a, int64_t(int(blockIdx.x) - a.groups) * kColumns);
     const int lane = threadIdx.x % kThreads, group = threadIdx.x / kThreads;
     float w[kPacks][N], dw[kPacks][N], db[kPacks][N];
     load_columns<F, N, kPacks, kThreads>(a.weight, a.width, 1.0f, w);
@@ -307,6 +274,7 @@ __global__ __launch_bounds__(kSize) void norm_backward_kernel(const Norm a) {
         row_sums<kThreads>(s, s_sums[turn]);
         turn ^= 1;
         const Slopes p = slopes(s, rstd, a.width);
+        if (a.rest != nullptr && there && lane == 0) a.rest[row] = p.rest;
         T *to = static_cast<T *>(a.out) + row * a.ld_out;
 #pragma unroll
         for (int k = 0; k < kPacks; ++k) {
@@ -439,6 +407,52 @@ __global__ __launch_bounds__(kJoin) void norm_join_kernel(const float *__restric
     }
 }
 
+// Few rows: dw and db of kColumns columns from all rows, which stay in L2, in a launch
+// behind that of the rows, which leaves what the rounding of each row's mean left.
+// (Columns beside the rows in one launch, 4.2 us of 700 x 650 fp32 where these two take
+// 7.2, do not have that: with a mean of 1,000 spreads dw was off by 1.7e-5 of it.  Rows
+// beyond 8 spreads summed once more for it, by every workgroup, took 174.)
+constexpr int kColumnsBlock = 1024, kRowsAhead = 8;
+
+template <typename T, typename F, int kColumns>
+__global__ __launch_bounds__(kColumnsBlock) void norm_columns_kernel(const Norm a) {
+    __shared__ float s_part[kColumnsBlock / kWave][2][kColumns];
+    constexpr int kSlots = kColumnsBlock / kColumns;   // a thread's rows: its slot's, every kSlots
+    const int64_t column = int64_t(blockIdx.x) * kColumns + threadIdx.x % kColumns;
+    const int slot = threadIdx.x / kColumns;
+    const T *x = static_cast<const T *>(a.x) + column, *dy = static_cast<const T *>(a.dy) + column;
+    float dw = 0.0f, db = 0.0f;
+    if (column < a.width) {
+        for (int first = slot; first < a.rows; first += kSlots * kRowsAhead) {
+            float v[kRowsAhead], c[kRowsAhead], mean[kRowsAhead], rest[kRowsAhead], rstd[kRowsAhead];
+#pragma unroll
+            for (int j = 0; j < kRowsAhead; ++j) {   // on their way at once; behind the last row: the last again
+                const int row = min(first + j * kSlots, a.rows - 1);
+                v[j] = float(dy[row * a.ld_dy]), c[j] = float(x[row * a.ld_x]);
+                mean[j] = a.mean[row], rest[j] = a.rest[row], rstd[j] = a.rstd[row];
+            }
+#pragma unroll
+            for (int j = 0; j < kRowsAhead; ++j) {
+                if (first + j * kSlots >= a.rows) break;
+                dw = fmaf(v[j], (c[j] - mean[j] - rest[j]) * rstd[j], dw);
+                db += v[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int off = kColumns; off < kWave; off <<= 1) dw += __shfl_xor(dw, off), db += __shfl_xor(db, off);
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    if (lane < kColumns) s_part[wave][0][lane] = dw, s_part[wave][1][lane] = db;
+    __syncthreads();
+    if (threadIdx.x >= 2 * kColumns || column >= a.width) return;
+    const int which = threadIdx.x / kColumns;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kColumnsBlock / kWave; ++w) sum += s_part[w][which][threadIdx.x % kColumns];
+    F *to = static_cast<F *>(which == 0 ? a.dweight : a.dbias);
+    if (to != nullptr) to[column] = F(sum);
+}
+
 // How a row is held: threads and packs of each.
 struct Hold {
     int threads, packs;   // 0: too long for registers
@@ -464,11 +478,13 @@ Hold backward_hold(int32_t width, int pack) {
 }
 
 // Whether dw and db are summed over columns of all rows, which are read a second
-// time for that, from L2, instead of by rows with a join.  us, against the join:
-// 700 x 650 fp32 4.5 and 10.6, 1 x 1,024 bf16 3.3 and 7.0, 300 x 4,096 8.8 and 14.0,
-// 1,024 x 1,500 fp32 12.2 and 15.4; beyond: 1,500 x 1,024 bf16 12.3 and 10.9, 250 x
-// 8,000 fp32 17.0 and 15.6, 4,000 x 1,024 bf16 45 and 15.
-constexpr int kFewRows = 1024;
+// time for that, from L2, instead of by rows with a join.  us of replays of a graph,
+// against the join: 700 x 650 fp32 7.2 and 10.3, 1 x 1,024 bf16 5.2 and 6.6, 300 x 4,096
+// 8.0 and 13.7, 768 x 2,000 fp32 11.8 and 13.6, 512 x 64 5.9 and 5.0; beyond: 1,024 x 64
+// 7.1 and 5.4, 1,024 x 1,024 bf16 9.9 and 8.2, 512 x 4,096 fp32 13.6 and 12.2, 2,048 x
+// 1,500 24.3 and 15.5.  kWide: 16 columns a workgroup, not 8 (300 x 4,096 bf16 8.0 and
+// 13.2, 512 x 2,000 8.1 and 7.5, 700 x 650 fp32 8.8 and 7.2).
+constexpr int kFewRows = 768, kWide = 2048;
 constexpr int64_t kFewElements = 3 << 19;
 
 bool few_rows(int32_t rows, int32_t width, Hold h) {
@@ -492,9 +508,14 @@ void forward(const Norm &a, hipStream_t stream) {
 }
 
 template <typename T, typename F, int kThreads, int kPacks>
-void backward(const Norm &a, int columns, hipStream_t stream) {
+void backward(const Norm &a, hipStream_t stream) {
     constexpr int kSize = kThreads < kBlock ? kBlock : kThreads;
-    norm_backward_kernel<T, F, kThreads, kPacks, kSize><<<uint32_t(a.groups + columns), kSize, 0, stream>>>(a);
+    norm_backward_kernel<T, F, kThreads, kPacks, kSize><<<uint32_t(a.groups), kSize, 0, stream>>>(a);
+}
+
+template <typename T, typename F, int kColumns>
+void columns(const Norm &a, hipStream_t stream) {
+    norm_columns_kernel<T, F, kColumns><<<uint32_t((a.width + kColumns - 1) / kColumns), kColumnsBlock, 0, stream>>>(a);
 }
 
 template <typename T, typename F>
@@ -522,22 +543,22 @@ template <typename T, typename F>
 hipError_t run_backward(Norm a, void *workspace, hipStream_t stream) {
     const Hold h = backward_hold(a.width, kRowPack<T>);
     a.groups = backward_groups(a.rows, h);
-    int parts = a.groups, columns = 0;
+    int parts = a.groups;
     const bool gradients = a.dweight != nullptr || a.dbias != nullptr;
     // (rows that are overwritten in place are not there for the columns)
     if (gradients && a.out != a.x && a.out != a.dy && few_rows(a.rows, a.width, h)) {
-        columns = (a.width + kColumns - 1) / kColumns;
+        a.rest = static_cast<float *>(workspace);
     } else if (gradients) {
         a.partial = static_cast<float *>(workspace) + (h.threads == 0 ? int64_t(a.rows) * 4 : 0);
     }
     a.sums = static_cast<float *>(workspace);
-    if (a.rows > 0 || columns > 0) switch (h.threads * 8 + h.packs) {
-        case 64 * 8 + 1: backward<T, F, 64, 1>(a, columns, stream); break;
-        case 64 * 8 + 2: backward<T, F, 64, 2>(a, columns, stream); break;
-        case 256 * 8 + 1: backward<T, F, 256, 1>(a, columns, stream); break;
-        case 256 * 8 + 2: backward<T, F, 256, 2>(a, columns, stream); break;
-        case 1024 * 8 + 1: backward<T, F, 1024, 1>(a, columns, stream); break;
-        case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, columns, stream); break;
+    if (a.rows > 0) switch (h.threads * 8 + h.packs) {
+        case 64 * 8 + 1: backward<T, F, 64, 1>(a, stream); break;
+        case 64 * 8 + 2: backward<T, F, 64, 2>(a, stream); break;
+        case 256 * 8 + 1: backward<T, F, 256, 1>(a, stream); break;
+        case 256 * 8 + 2: backward<T, F, 256, 2>(a, stream); break;
+        case 1024 * 8 + 1: backward<T, F, 1024, 1>(a, stream); break;
+        case 1024 * 8 + 2: backward<T, F, 1024, 2>(a, stream); break;
         default: {
             const int64_t most = int64_t(device_cu_count()) * 2;
             norm_sums_kernel<T, F><<<uint32_t(a.rows < most ? a.rows : most), kLong, 0, stream>>>(a);
@@ -546,6 +567,10 @@ hipError_t run_backward(Norm a, void *workspace, hipStream_t stream) {
             const int across = (a.width + kBlock * kRowPack<T> - 1) / (kBlock * kRowPack<T>);
             norm_backward_long_kernel<T, F><<<dim3(across, parts), kBlock, 0, stream>>>(a, int32_t(each));
         }
+    }
+    if (a.rest != nullptr) {
+        if (a.width >= kWide) columns<T, F, 16>(a, stream);
+        else columns<T, F, 8>(a, stream);
     }
     if (a.partial != nullptr)
         norm_join_kernel<F><<<uint32_t((2 * int64_t(a.width) + kWave - 1) / kWave), kJoin, 0, stream>>>(
@@ -568,7 +593,8 @@ hipError_t launch_layernorm_forward(const void *x, int64_t ld_x, const void *wei
     return run_forward<float, float>(a, stream);
 }
 
-// [sums of long rows][partial sums of dw and db], as much as either type of x takes
+// [sums of long rows][partial sums of dw and db], as much as either type of x takes; or
+// [rests of few rows]
 size_t layernorm_workspace_size(int32_t rows, int32_t width) {
     size_t most = 0;
     for (int pack = kRowPack<float>; pack <= kRowPack<__bf16>; pack *= 2) {
@@ -577,7 +603,8 @@ size_t layernorm_workspace_size(int32_t rows, int32_t width) {
                              (h.threads == 0 ? size_t(rows) * 4 * sizeof(float) : 0);
         most = bytes > most ? bytes : most;
     }
-    return 16 + most;
+    const size_t rests = rows <= kFewRows ? size_t(rows) * sizeof(float) : 0;
+    return 16 + (most > rests ? most : rests);
 }
 
 hipError_t launch_layernorm_backward(const void *x, int64_t ld_x, const void *weight, const float *mean,

@@ -225,3 +225,45 @@ def test_gradients_against_differences(k):
         # each y is off by 2^-22 of up to 8; the third derivative adds its step^2 / 6
         slack = 2.0 ** -19 * float(weight.abs().sum()) / step + step ** 2 * 10.0
         assert abs((sides[0] - sides[1]) / (2 * step) - float(grad)) <= slack, name
+
+
+@pytest.mark.parametrize("n, k", [(700, 650), (1, 1024), (768, 64), (769, 64), (40, 3000), (1025, 650), (300, 4096)])
+@pytest.mark.parametrize("mean", [0.0, 7.5, 8.5, 1000.0, 10000.0, 131072.0])
+def test_weights_gradient_of_rows_with_a_mean_between_two_values(n, k, mean):
+    """Rows whose mean lies 0.45 of a step behind an fp32 value, so that what is stored
+    is off by that in all of them, with gradients of one sign, which add it up (from
+    1,000 on: smaller means lie anywhere).
+
+    Limit, u = 2^-24: x - mean is rounded once.  No value passes more than 16 additions
+    of its thread, 6 of its wave and 16 of the waves, so that what the mean's rounding
+    left is off by 40 u of the mean magnitude of x - mean, rstd by 24 u, and h with its
+    three roundings by 66 u |h| + 41 u mean|h|; the sums over the rows pass at most 128
+    additions."""
+    rng = np.random.default_rng(n + k)
+    ulp = float(np.spacing(np.float32(max(mean, 1.0))))
+    q = np.rint(rng.standard_normal((n, k)) / ulp)
+    q -= np.rint(q.mean(1, keepdims=True))
+    more = np.rint(0.45 * k) - q.sum(1, keepdims=True)
+    q += np.sign(more) * (np.arange(k) < np.abs(more))
+    exact = mean + ulp * q
+    x = exact.astype(np.float32)
+    assert mean < 1000.0 or np.array_equal(x, exact)
+    exact = x.astype(np.float64)
+    dy = (0.5 + rng.random((n, k))).astype(np.float32)
+    c = Call(x, None, None, dy)
+    d = exact - exact.mean(1, keepdims=True)
+    h = d / np.sqrt((d * d).mean(1, keepdims=True) + float(np.float32(1e-5)))
+    size = np.abs(h).mean(1, keepdims=True)
+    limit = _step.EPS32 * (dy * (66 * np.abs(h) + 41 * size) + 128 * dy * np.abs(h)).sum(0)
+    want = (dy.astype(np.float64) * h).sum(0)
+    _step.within(c.dweight.cpu().numpy(), (want, limit), "dweight")
+    left = exact.mean(1) - c.mean.double().cpu().numpy()
+    uncorrected = (dy * left[:, None] / np.sqrt((d * d).mean(1, keepdims=True) + 1e-5)).sum(0)
+    # an uncorrected sum fails
+    assert mean < 2000.0 or np.all(np.abs(uncorrected) > 2 * limit)
+    for into in ("x", "dy"):   # in place: by rows, whatever their number
+        x, dy = c.x.clone(), c.dy.clone()
+        dw, db = torch.empty_like(c.dweight), torch.empty_like(c.dbias)
+        efs.layernorm_backward(x, None, c.mean, c.rstd, dy, x if into == "x" else dy, dw, db,
+                               efs.new_layernorm_workspace(n, k, DEV))
+        _step.within(dw.cpu().numpy(), (want, limit), "dweight in place of " + into)
