@@ -932,6 +932,16 @@ def _tensor_list(tensors, name, dtypes, sizes, optional=False):
     return arr
 
 
+def _capturing(handle) -> bool:
+    """Whether the stream of this handle records into a graph (the default one cannot)."""
+    if not handle:
+        return False
+    if handle == _stream_handle(None):
+        return _torch.cuda.is_current_stream_capturing()
+    with _torch.cuda.stream(_torch.cuda.ExternalStream(handle)):
+        return _torch.cuda.is_current_stream_capturing()
+
+
 def _size_array(sizes):
     return (ctypes.c_int64 * max(len(sizes), 1))(*sizes)
 
@@ -939,7 +949,8 @@ def _size_array(sizes):
 def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                         weight_decay=0.01, copy=None, factors=None, seed: int = 0, stream=None):
     """adamw_apply with its arguments marshalled once (see prepare_sparse_apply):
-    a callable that takes the step."""
+    a callable that takes the step.  For as long as it lives itself it keeps the lists'
+    tensors, the step tensors of calls that were captured in a graph and the last one."""
     import torch
     lib = load_library()
     g, x, m, v = list(g), list(x), list(m), list(v)
@@ -977,11 +988,14 @@ def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float 
             if step.numel() != 1:
                 raise ValueError("step must have one element")
             _vector(step, "step", torch.int64, _device_of(step, "step"))
-            call.step = step   # alive as long as a graph that this call was captured in
+            call.last = step
+            if _capturing(tail[-1]) and all(t is not step for t in call.steps):
+                call.steps.append(step)   # alive as long as this call, as the graph reads it
             _check(lib, fn(*head, 1, step.data_ptr(), *tail))
         else:
             _check(lib, fn(*head, int(step), None, *tail))
     call.tensors = (tuple(g), tuple(x), tuple(m), tuple(v), copy and tuple(copy), factors)
+    call.steps = []
     return call
 
 

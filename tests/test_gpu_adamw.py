@@ -277,6 +277,47 @@ def test_a_prepared_call_keeps_its_tensors():
     assert all(r() is None for r in alive)
 
 
+@pytest.mark.parametrize("explicit", [False, True])
+def test_a_prepared_call_keeps_the_step_tensors_of_its_graphs(explicit):
+    """Two captures with steps of their own, then eager calls with others, of whose
+    tensors the last is kept; both graphs go on reading theirs."""
+    stream = torch.cuda.Stream()
+    model, plain = Model([300, 5], 32), _step.Adamw(1e-2)
+    g, dg = model.gradients()
+    if not explicit:   # the stream is the one that is current here
+        torch.cuda.set_stream(stream)
+    try:
+        call = efs.prepare_adamw_apply(dg, model.dx, model.dm, model.dv, lr=1e-2, weight_decay=0.0,
+                                       stream=stream if explicit else None)
+    finally:
+        torch.cuda.set_stream(torch.cuda.default_stream())
+    steps = [torch.full((1,), 3 + 4 * i, dtype=torch.int64, device=DEV) for i in range(4)]
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph, step in zip(graphs, steps):
+        with torch.cuda.graph(graph, stream=stream):
+            call(step)
+            call(step)
+    alive = [weakref.ref(t) for t in steps]
+    for step in steps[2:]:
+        call(step)
+    torch.cuda.synchronize()
+    del step
+    steps.clear()
+    gc.collect()
+    assert [r() is not None for r in alive] == [True, True, False, True]
+    other = [torch.full((1,), 10 ** 6, dtype=torch.int64, device=DEV) for _ in range(8)]   # where the others were
+    for graph in (graphs[0], graphs[1], graphs[0]):
+        graph.replay()
+        torch.cuda.synchronize()
+    for t in (11, 15, 3, 3, 7, 7, 3, 3):
+        model.expect(plain, t, g, [0.0, 0.0])
+    model.check("after the replays")
+    del graphs, graph, call, other
+    gc.collect()
+    assert all(r() is None for r in alive)
+
+
 def test_empty_lists_do_nothing():
     efs.adamw_apply([], [], [], [], 1, lr=1e-3)
     none = torch.empty(0, device=DEV)
