@@ -598,7 +598,8 @@ efs_status layernorm_backward(const void *x, int64_t ld_x, const void *weight, c
  * of 4 bits (steps of 2^-10 s), of which no r > 0 becomes 0.  A value between two
  * others is rounded up with the share of its distance from the lower one, by a
  * hash of (seed, the tensor's place in the list, t, element): the same call
- * gives the same bits.  A magnitude that is infinite or NaN is kept as NaN.  x is
+ * gives the same bits.  A magnitude that is infinite or NaN is kept as NaN; one
+ * that is finite stays so (rounded down where the next m or v is 2^128).  x is
  * computed from m and v before they are rounded.  The state of n elements is
  * ceil(n / 256) * 256 bytes (a byte an element, zeros behind the last), then a
  * float s for each 256. */

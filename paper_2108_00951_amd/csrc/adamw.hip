@@ -125,6 +125,7 @@ __device__ __forceinline__ uint32_t mixed(uint32_t z) {
 
 constexpr uint32_t kInfinity = 0x7f800000u, kMagnitude = 0x7fffffffu;
 constexpr uint32_t kNanM = 0x7fu, kNanR = 0xffu;
+constexpr uint32_t kTopM = 0x77u, kTopR = 0xefu;   // the largest below 2^8 of the scale
 
 // The code of a magnitude, of kMantissa bits below the leading one and 4 of
 // exponent, rounded up with the share `dither` / 2^16; e: the block's exponent,
@@ -191,6 +192,14 @@ __device__ __forceinline__ void pack_block(const float (&m)[4], const float (&r)
         for (int i = 0; i < 4; ++i) {
             const uint32_t small = max(encode_small<4>(r[i], random[i] >> 16, two_to(7 - er)), rb[i] != 0u ? 1u : 0u);
             d[i] = rb[i] < least_r ? small : d[i];
+        }
+    }
+    // up to 2^128, which is infinite, no m is rounded, nor r to 2^64, whose square v is
+    if (em == 127 || er == 63) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = em == 127 ? min(c[i], kTopM) : c[i];
+            d[i] = er == 63 ? min(d[i], kTopR) : d[i];
         }
     }
     if (!whole_m || !whole_r) {

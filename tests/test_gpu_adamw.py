@@ -257,6 +257,38 @@ def test_write_and_read_state():
         assert np.all(np.abs(want_r - np.sqrt(v[i])) <= np.maximum(2.0 ** -5 * np.sqrt(v[i]), 2.0 ** -17 * top_r) + 1e-30)
 
 
+def test_states_of_8_bits_stay_finite():
+    """m and v below fp32's largest value whose next one of 8 bits is 2^128: written,
+    and left by steps whose random rounding would take half of them there."""
+    top = np.finfo(np.float32).max
+    values = np.array([top, 0.98 * top, 0.97 * top, 0.96 * top, 0.9 * top, 1.0, 0.0], np.float32)
+    m = np.concatenate([values, -values])
+    v = np.concatenate([values, values])
+    m8, v8 = efs.new_adamw_state([m.size], DEV)
+    efs.adamw_write_state([torch.from_numpy(m).to(DEV)], [torch.from_numpy(v).to(DEV)], m8, v8)
+    gm, gv = (torch.empty(m.size, device=DEV) for _ in range(2))
+    efs.adamw_read_state(m8, v8, [gm], [gv])
+    with np.errstate(over="ignore"):
+        want_m = _step.in_8_bits(np.abs(m), 3, 0, np.float32(0.5))
+        want_r = _step.in_8_bits(np.sqrt(v), 4, 1, np.float32(0.5))
+        want_v = want_r * want_r
+    assert np.isinf(want_m).any() and np.isinf(want_v).any()
+    want_m = np.copysign(np.where(np.isinf(want_m), np.float32(240.0 * 2.0 ** 120), want_m), m)
+    want_v = np.where(np.isinf(want_v), np.float32(248.0 * 2.0 ** 56) ** 2, want_v)
+    np.testing.assert_array_equal(gm.cpu().numpy(), want_m)
+    np.testing.assert_array_equal(gv.cpu().numpy(), want_v)
+    n = 1000
+    x, g = torch.zeros(n, device=DEV), torch.full((n,), float(np.sqrt(0.99 * float(top) / 0.001)), device=DEV)
+    m8, v8 = efs.new_adamw_state([n], DEV)
+    gm, gv = (torch.empty(n, device=DEV) for _ in range(2))
+    for t in (1, 2, 3):   # gradients that leave v where it is
+        efs.adamw_apply([g], [x], m8, v8, t, lr=1e-2, weight_decay=0.0)
+        efs.adamw_read_state(m8, v8, [gm], [gv])
+        assert torch.isfinite(gm).all() and torch.isfinite(gv).all() and torch.isfinite(x).all()
+        assert float(gv.min()) >= 0.8 * float(top)   # 248, 240, 232 of 256, squared
+        g.zero_()
+
+
 def test_a_prepared_call_keeps_its_tensors():
     model = Model([300, 5], 8, copy=True)
     _, g = model.gradients()
