@@ -526,6 +526,14 @@ def _int32(v, name) -> int:
     return v
 
 
+def _int64(v, name) -> int:
+    """As _int32, of 64 bits."""
+    v = int(v)
+    if not -2 ** 63 <= v < 2 ** 63:
+        raise ValueError("%s does not fit 64 bits: %d" % (name, v))
+    return v
+
+
 def _shape_arrays(shapes: Sequence[Tuple[int, int]]):
     n = max(len(shapes), 1)
     rows, cols = (ctypes.c_int32 * n)(), (ctypes.c_int32 * n)()
@@ -662,7 +670,7 @@ def xent_forward(h, w, target, loss, lse, workspace, ignore_index: int = -100, s
     _require(workspace, torch.uint8, "workspace")
     if loss.shape != target.shape or lse.shape != target.shape:
         raise ValueError("loss and lse must be [tokens]")
-    _check(lib, lib.xent_forward(*args, int(ignore_index), _ptr(loss), _ptr(lse), _ptr(workspace),
+    _check(lib, lib.xent_forward(*args, _int64(ignore_index, "ignore_index"), _ptr(loss), _ptr(lse), _ptr(workspace),
                                  workspace.numel(), _stream_handle(stream)))
 
 
@@ -683,7 +691,7 @@ def xent_backward(h, w, target, lse, dloss, dh, dw, workspace, ignore_index: int
         raise TypeError("dh and dw must have the dtype of h and w")
     _require_rows(dh, "dh")
     _require_rows(dw, "dw")
-    _check(lib, lib.xent_backward(*args, int(ignore_index), _ptr(lse), _ptr(dloss), _ptr(dh),
+    _check(lib, lib.xent_backward(*args, _int64(ignore_index, "ignore_index"), _ptr(lse), _ptr(dloss), _ptr(dh),
                                   _row_stride(dh), _ptr(dw), _row_stride(dw), _ptr(workspace),
                                   workspace.numel(), _stream_handle(stream)))
 
@@ -760,7 +768,7 @@ def embed_forward(table, ids, out, scale: float = 1.0, ignore_index: int = -100,
     _check(lib, lib.embed_forward(*_matrix(table, "table", here), table_dtype, _vector(ids, "ids", _torch.int64, here),
                                   *_matrix(out, "out", here), dtype, _int32(ids.shape[0], "tokens"),
                                   _int32(table.shape[0], "vocab"), _int32(table.shape[1], "width"), float(scale),
-                                  int(ignore_index), _status_pointer(status, here), _stream_handle(stream)))
+                                  _int64(ignore_index, "ignore_index"), _status_pointer(status, here), _stream_handle(stream)))
 
 
 def embed_workspace_bytes(tokens: int, vocab: int, width: int) -> int:
@@ -789,7 +797,7 @@ def embed_backward(dout, ids, dtable, workspace, scale: float = 1.0, ignore_inde
     _check(lib, lib.embed_backward(*_matrix(dout, "dout", here), dtype, _vector(ids, "ids", _torch.int64, here),
                                    *_matrix(dtable, "dtable", here), table_dtype, _int32(ids.shape[0], "tokens"),
                                    _int32(dtable.shape[0], "vocab"), _int32(dtable.shape[1], "width"), float(scale),
-                                   int(ignore_index), int(bool(accumulate)), _status_pointer(status, here),
+                                   _int64(ignore_index, "ignore_index"), int(bool(accumulate)), _status_pointer(status, here),
                                    _vector(workspace, "workspace", _torch.uint8, here), workspace.numel(),
                                    _stream_handle(stream)))
 
@@ -879,7 +887,7 @@ STATE_32, STATE_8 = 0, 1
 
 def adamw_state_bytes(size: int) -> int:
     """Bytes of one moment of `size` elements in 8 bits."""
-    return int(load_library().adamw_state_bytes(int(size)))
+    return int(load_library().adamw_state_bytes(_int64(size, "size")))
 
 
 def new_adamw_state(sizes: Sequence[int], device="cuda"):
@@ -993,7 +1001,7 @@ def prepare_adamw_apply(g, x, m, v, lr: float, beta1: float = 0.9, beta2: float 
                 call.steps.append(step)   # alive as long as this call, as the graph reads it
             _check(lib, fn(*head, 1, step.data_ptr(), *tail))
         else:
-            _check(lib, fn(*head, int(step), None, *tail))
+            _check(lib, fn(*head, _int64(step, "step"), None, *tail))
     call.tensors = (tuple(g), tuple(x), tuple(m), tuple(v), copy and tuple(copy), factors)
     call.steps = []
     return call

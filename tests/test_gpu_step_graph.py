@@ -190,3 +190,23 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
                  lambda: efs.layernorm_backward(m.h, w, m.mean, m.rstd, m.dy, m.dh, None, None, m.nws), m.update):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+@pytest.mark.parametrize("wrapped", [2 ** 64, -2 ** 64])
+def test_whole_numbers_past_64_bits_are_refused(wrapped):
+    """An ignored word 2^64 on would be the word itself, and so would a step."""
+    m = Model(50, 32, 20, 32, False)
+    m.batch(0)
+    table = m.views(m.x)[0]
+    before = m.x.clone()
+    loss, lse = torch.empty(20, device=DEV), torch.empty(20, device=DEV)
+    ws = efs.new_xent_workspace(20, 50, 32, torch.float32, DEV)
+    for call in (lambda: efs.embed_forward(table, m.ids, m.h, ignore_index=3 + wrapped),
+                 lambda: efs.embed_backward(m.h, m.ids, table, m.ews, ignore_index=3 + wrapped),
+                 lambda: efs.xent_forward(m.h, table, m.target, loss, lse, ws, ignore_index=3 + wrapped),
+                 lambda: efs.xent_backward(m.h, table, m.target, lse, m.weight, m.dh, torch.empty_like(table), ws,
+                                           ignore_index=3 + wrapped),
+                 lambda: efs.adamw_apply([m.g], [m.x], [torch.zeros_like(m.g)], [torch.zeros_like(m.g)], 3 + wrapped, lr=1.0)):
+        with pytest.raises(ValueError, match="64 bits"):
+            call()
+    assert torch.equal(m.x, before)

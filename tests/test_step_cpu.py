@@ -247,3 +247,11 @@ def test_lists_of_other_tensors_are_refused():
             binding.prepare_adamw_apply(*lists, lr=1e-3)
     with pytest.raises(ValueError, match="as many"):
         binding.adamw_read_state([], [], [f], [f])
+
+
+@pytest.mark.parametrize("size", [2 ** 64 + 5, 2 ** 63, -2 ** 64 + 5])
+def test_sizes_past_64_bits_do_not_wrap(size):
+    with pytest.raises(ValueError, match="64 bits"):
+        binding.adamw_state_bytes(size)
+    with pytest.raises(ValueError, match="64 bits"):
+        binding.new_adamw_state([3, size], "cpu")
