@@ -178,6 +178,38 @@ def test_many_and_long_rows(rows, width):
             assert abs(float(got) - float(terms.sum())) <= 2.0 ** -24 * (rows / 64 + 1000) * float(terms.abs().sum())
 
 
+@pytest.mark.parametrize("rows, width", [((1 << 23) + 3, 2), (100_003, 9), (30_000, 650), (40, 1 << 18), (2, 8193)])
+def test_sums_over_many_rows_miss_none(rows, width):
+    """Gradients that are small whole numbers where x is above its row's mean and 0 where
+    it is not: dbias is exact in any order (below 2^24), and dweight a sum without
+    cancellation, in which one workgroup of 768 is 1.3e-3.
+
+    A value passes the additions of its wave's rows (of 768 workgroups of four at least),
+    the joins of 3 groups, 48 parts and 16 waves: with u = 2^-24 each off by u of the
+    sum; its own roundings, those of the mean and rstd among them, are 66 u, as the
+    rest's is of the row's mean magnitude."""
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    x, w = rand((rows, width), 1), rand((width,), 3)
+    x += 3.0
+    d = x.double()
+    d -= d.mean(1, keepdim=True)
+    dy = torch.randint(1, 4, (rows, width), generator=gen, device=DEV).float() * (d > 0)
+    dx, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    efs.layernorm_forward(x, w, None, dx, mean, rstd)
+    efs.layernorm_backward(x, w, mean, rstd, dy, dx, dw, db, efs.new_layernorm_workspace(rows, width, DEV))
+    assert float(dy.sum(0, dtype=torch.float64).max()) < 2.0 ** 24
+    assert torch.equal(db.double(), dy.sum(0, dtype=torch.float64))
+    rstd64 = 1.0 / torch.sqrt((d * d).mean(1, keepdim=True) + float(np.float32(1e-5)))
+    h = d * rstd64
+    want = (dy * h).sum(0)
+    size = h.abs().mean(1, keepdim=True)
+    limit = 2.0 ** -24 * ((rows / 3072 + 90) * want + 66.0 * want + 66.0 * (dy * size).sum(0))
+    assert torch.all((dw - want).abs() <= limit)
+    # sharp enough to miss one workgroup's rows (of two rows, h may be near 0 in both)
+    assert rows == 2 or torch.all((limit < want / 1000.0) | (want == 0.0))
+
+
 @pytest.mark.parametrize("rows, width", [(530_000, 4099), (33_000, 66_001)])
 def test_norms_past_2_31_elements(rows, width):
     """The last rows give what they give alone."""
