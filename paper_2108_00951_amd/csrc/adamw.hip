@@ -7,8 +7,8 @@
 // each operation rounded to fp32 by itself.  Bytes bound it: 28 of an element
 // with states of 32 bits (g, x, m, v in; x, m, v out), 16 with states of 8.  Measured
 // on one MI355X: 37 M elements of 161 tensors, 32 bits, 198 us (5.3 TB/s, two
-// launches); 134 M, 8 bits, bf16 g and copy (16 bytes an element too) 371 to 431 us
-// (5.8 to 5.0 TB/s), where the vector units are busy throughout: 90 instructions an
+// launches); 134 M, 8 bits, bf16 g and copy (16 bytes an element too) 370 to 440 us
+// (5.8 to 4.9 TB/s), where the vector units are busy throughout: 92 instructions an
 // element, of which the square root, the division and the hash are half; 97 short
 // vectors 5.0 us.
 // A launch takes the tensors of its arguments, kTensors at most, one tile of
@@ -43,7 +43,10 @@ constexpr int kStepTile = kBlock * 4;
 
 constexpr uint32_t kMaxTiles = 1u << 23;   // of one launch, whose threads are counted in 32 bits
 
-// What a step writes is read again a step later, after all else has passed the caches.
+// States are read again a step later, after all else has passed the caches.  x and its
+// copy may be read sooner; through the caches they gain nothing: a step of 10.5 M elements
+// and a pass over the copy behind it 53 us, past the caches 55, of 1 M 9.4 and 9.4, of 42 M
+// 257 and 254.
 constexpr bool kPast = true;
 
 constexpr int32_t kNone = INT32_MIN;   // no tensor of an optional list

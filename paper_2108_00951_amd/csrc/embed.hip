@@ -9,7 +9,7 @@
 //   32,768 rows of 4,096 bf16 looked up              77 us, 4.7 TB/s (5.6 with the rows
 //                                                    that several XCDs fetch)
 //   gradient, 131,072 x 2,048 fp32, 16,384 tokens    167 us, 6.8 TB/s
-//   gradient, 33,278 x 650 fp32, 700 tokens          17 us, 5.2 TB/s
+//   gradient, 33,278 x 650 fp32, 700 tokens          18 us, 4.9 TB/s
 //   gradient, 64 tokens added to 33,278 x 1,024      4.2 us
 //
 // The gradient of few tokens is one launch: a workgroup for each token and 64 packs
@@ -22,7 +22,9 @@
 // workgroup owns some consecutive words and looks through all ids (they stay in L2:
 // 16,384 of them are 128 KiB), so that it knows by itself how many tokens the words
 // before its own have, and which tokens, in their order, each of its own has (13 us
-// for 16,384 tokens, of which the hottest words' workgroup waits longest).  A second
+// for 16,384 tokens, 35 for 65,536, 117 for 262,144, which are 7, 13 and 20 % of the call
+// at 131,072 x 2,048; the workgroup of the hottest words is the last: 57 us for 16,384
+// tokens of which half are its own).  A second
 // launch takes the sorted tokens in pieces of kHot, writes the rows of words with
 // fewer than kHot tokens and sums those of other words piece by piece; a third joins
 // the pieces of a word in order.  So no word is summed by one wave, and nothing depends

@@ -6,10 +6,10 @@
 //   dw = sum over the rows of dy h ;  db = sum over the rows of dy
 //
 // Bytes bound it: x in and y out, x and dy in and dx out.  Measured on one MI355X, 16,384 x
-// 4,096 bf16: forward 51 us (5.3 TB/s), backward 76 us (5.3 TB/s, and 25 MB of partial
-// sums) and 5 for their join; 700 x 650 fp32: forward 5.0 us, backward 4.0 and 4.7 for
-// the columns behind it (each by itself under a profiler; 7.2 together as a graph's
-// nodes); one row of 1,024: 2.6 us, a launch and two sums over a wave.  A row is read
+// 4,096 bf16: forward 54 us (5.0 TB/s), backward 76 us (5.3 TB/s, and 25 MB of partial
+// sums) and 5 for their join; 700 x 650 fp32: forward 4.9 us, backward 4.2 and 5.1 for
+// the columns behind it (each by itself, under a profiler; 7.2 for both as nodes of a
+// graph); one row of 1,024: 2.6 us, a launch and two sums over a wave.  A row is read
 // once and stays in the registers of one wave, 256 or 1,024 threads, which are left with
 // the same columns row after row, so that the weights are read once too and the
 // sums of dw and db stay in registers until the workgroup ends.  These partial
